@@ -28,6 +28,11 @@
  * and ipd_split_loss_grad (the objective's gradient with respect to the
  * student's logits, sparse and dense).
  *
+ * Before the first step, from a prompt to its first proposed token:
+ * ipd_rope_append (rotary positions of new queries and keys, and the write of
+ * their K/V rows into the paged cache, in one launch), with ipd_rope (the
+ * rotation alone, or its gradient) and ipd_rope_table (the angles).
+ *
  * Conventions for every call
  *   - Data pointers are DEVICE pointers owned by the caller; the library never
  *     allocates.  Scratch memory comes from a caller-provided device workspace
@@ -72,6 +77,7 @@ typedef struct CUstream_st *ipd_stream_t; /* same handle as cudaStream_t */
 #define IPD_DEVERR_PLAN 4u       /* work list larger than the workspace     */
 #define IPD_DEVERR_WAIT 5u       /* a bounded pipeline wait ran out         */
 #define IPD_DEVERR_SPAN 6u       /* cu_span / cu_q / cu_new not non-decreasing, or rows past them */
+#define IPD_DEVERR_POSITION 7u   /* a position outside the rotary table */
 
 #define IPD_MAX_BATCHES 8
 #define IPD_MAX_K 32
@@ -463,6 +469,96 @@ int ipd_split_loss_grad(const uint16_t *logits_student, const uint16_t *logits_t
                         int agg_mode, int dir_mode, float grad_scale, int32_t *grad_idx,
                         float *grad_val, void *grad_dense, int dense_dtype, void *workspace,
                         size_t workspace_bytes, ipd_stream_t stream);
+
+/* Rotary positions.  Pair i of a head (of rot_dim / 2 pairs, rot_dim <=
+ * head_dim; the entries from rot_dim on are left as they are) at position p
+ * turns by the angle p f_i:
+ *   y_a = a c - b s,  y_b = b c + a s,  (c, s) = table[p][i]
+ * where (a, b) are the entries (i, i + rot_dim / 2) in the half layout and
+ * (2i, 2i + 1) in the interleaved one.  fp32 arithmetic on the stored inputs,
+ * rounded once (to nearest even) to the output's type. */
+#define IPD_ROPE_HALF 0
+#define IPD_ROPE_INTERLEAVED 1
+
+/* How the frequencies f_i are laid out for contexts longer than the trained
+ * one.  f_i = base^(-2i / rot_dim), then
+ *   LINEAR  f_i / factor (position interpolation)
+ *   NTK     base replaced by base * factor^(rot_dim / (rot_dim - 2))
+ *   YARN    f_i / factor for the frequencies that turn fewer than beta_slow
+ *           times over trained_len positions, f_i for those that turn more
+ *           than beta_fast times, a linear blend over the pair index between
+ *           (Peng et al. 2023); cos and sin carry the factor 0.1 ln(factor) + 1 */
+#define IPD_ROPE_SCALE_NONE 0
+#define IPD_ROPE_SCALE_LINEAR 1
+#define IPD_ROPE_SCALE_NTK 2
+#define IPD_ROPE_SCALE_YARN 3
+typedef struct ipd_rope_scaling {
+  int32_t kind;       /* IPD_ROPE_SCALE_* */
+  double base;        /* > 1 */
+  double factor;      /* >= 1, context extension; unused for NONE */
+  double trained_len; /* YARN: > 0 */
+  double beta_fast;   /* YARN: >= beta_slow (32 in the paper) */
+  double beta_slow;   /* YARN: > 0 (1 in the paper) */
+} ipd_rope_scaling;
+
+/* Fills table [max_pos][rot_dim / 2][2] fp32 (device, 16-byte aligned) with
+ * (cos, sin) of position times frequency, formed in 64 bits and rounded once.
+ * Built once for a model and kept by the caller.  rot_dim is even, 2 .. 256. */
+int ipd_rope_table(float *table, int max_pos, int rot_dim, const ipd_rope_scaling *scaling,
+                   ipd_stream_t stream);
+
+/* Rotates the heads of n_tokens rows.
+ *  x, y      [n_tokens] rows of n_heads x head_dim entries of `dtype`
+ *            (IPD_DTYPE_F32 or IPD_DTYPE_BF16), rows x_stride / y_stride
+ *            entries apart; y may be x (in place), and must not overlap it
+ *            otherwise
+ *  pos       [n_tokens] int32 positions; one outside [0, max_pos) records
+ *            IPD_DEVERR_POSITION and its row is not written
+ *  inverse   0: the rotation; 1: its transpose, which takes the gradient with
+ *            respect to y to the gradient with respect to x
+ * head_dim is at most 256 and rot_dim even.  Rows, strides and head parts of
+ * whole 16-byte pieces take 16-byte loads; any others are taken entry by
+ * entry.  Returns IPD_ERR_INVALID_ARG for a missing or misaligned pointer, a
+ * stride shorter than a row or a bad rot_dim or layout. */
+typedef struct ipd_rope_args {
+  const void *x;
+  void *y;
+  int64_t x_stride, y_stride;
+  const int32_t *pos;
+  const float *table; /* [max_pos][rot_dim / 2][2], 16-byte aligned */
+  int32_t dtype, n_tokens, n_heads, head_dim, max_pos, rot_dim, layout, inverse;
+} ipd_rope_args;
+int ipd_rope(const ipd_rope_args *args, ipd_stream_t stream);
+
+/* Rotary positions of new tokens and the write of their K/V rows into a paged
+ * cache, in one launch: the rotated queries to q_out, the rotated keys and the
+ * values to their page slots, as ipd_kv_append would write them, and the
+ * rotated keys to k_out as well when it is not NULL.
+ *  q, k, v   [total_new] rows of num_q_heads / num_kv_heads / num_kv_heads
+ *            heads of 128 bf16 entries, rows *_stride entries apart (views
+ *            into one projection output, for example).  num_q_heads may be 0
+ *            (q and q_out unused).
+ *  q_out, k_out  rows as q and k; each may be its own input (in place)
+ *  cu_new, seq_len, page_table, max_pages, num_reqs  as for ipd_kv_append.
+ *            A row's position is its place in the sequence, seq_len[r] - n_r + i.
+ * Pointers 16-byte aligned, strides multiples of 8 entries.  A row outside the
+ * request offsets, past the page table or in a page outside the pool is
+ * recorded and skipped as by ipd_kv_append, and so is one whose position is
+ * not in the table (IPD_DEVERR_POSITION): neither its queries nor its keys and
+ * values are written.  IPD_ERR_UNSUPPORTED unless page_size == 16 and
+ * head_dim == 128. */
+typedef struct ipd_rope_append_desc {
+  const uint16_t *q, *k, *v;
+  uint16_t *q_out, *k_out;
+  int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
+  uint16_t *k_pages, *v_pages;
+  int64_t num_pages;
+  const int32_t *cu_new, *seq_len, *page_table;
+  const float *table; /* [max_pos][rot_dim / 2][2], 16-byte aligned */
+  int32_t num_q_heads, num_kv_heads, page_size, head_dim;
+  int32_t max_pages, num_reqs, total_new, max_pos, rot_dim, layout;
+} ipd_rope_append_desc;
+int ipd_rope_append(const ipd_rope_append_desc *desc, ipd_stream_t stream);
 
 /* Measurement aid.  While on, every ipd_verify_attn / ipd_decode_attn call
  * records CUDA events on its stream around its attention kernel alone (not

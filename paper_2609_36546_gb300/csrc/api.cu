@@ -7,17 +7,21 @@ extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_
 extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_score_error();
 extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_loss_error();
 extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_kv_error();
+extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_rope_error();
 
 extern "C" int ipd_get_device_error(uint32_t *code) {
   if (!code) return IPD_ERR_INVALID_ARG;
   if (cudaDeviceSynchronize() != cudaSuccess) return IPD_ERR_CUDA;
-  const unsigned int a = ipd_internal_take_attn_error();
-  const unsigned int b = ipd_internal_take_score_error();
-  const unsigned int c = ipd_internal_take_loss_error();
-  const unsigned int d = ipd_internal_take_kv_error();
-  if (a == 0xffffffffu || b == 0xffffffffu || c == 0xffffffffu || d == 0xffffffffu)
-    return IPD_ERR_CUDA;
-  *code = a ? a : (b ? b : (c ? c : d));
+  // every word is taken (and cleared) before one is returned; the first wins
+  const unsigned int words[] = {ipd_internal_take_attn_error(), ipd_internal_take_score_error(),
+                                ipd_internal_take_loss_error(), ipd_internal_take_kv_error(),
+                                ipd_internal_take_rope_error()};
+  unsigned int first = 0;
+  for (const unsigned int w : words) {
+    if (w == 0xffffffffu) return IPD_ERR_CUDA;
+    if (first == 0) first = w;
+  }
+  *code = first;
   return IPD_OK;
 }
 

@@ -21,7 +21,7 @@ STATUS = {0: "IPD_OK", 1: "IPD_ERR_INVALID_ARG", 2: "IPD_ERR_UNSUPPORTED", 3: "I
           4: "IPD_ERR_CUDA", 5: "IPD_ERR_TIMEOUT", 6: "IPD_ERR_DEVICE", 7: "IPD_ERR_CAPACITY"}
 STATUS_CODES = {v: k for k, v in STATUS.items()}
 DEVERR = {0: "none", 1: "page id", 2: "seq len", 3: "token id", 4: "plan overflow", 5: "wait",
-          6: "span offsets"}
+          6: "span offsets", 7: "rotary position"}
 
 DIR_SPLIT, DIR_REVERSE, DIR_FORWARD, DIR_INVERSE = 0, 1, 2, 3
 AGG_SEQ_MEAN_TOKEN_MEAN, AGG_GLOBAL_TOKEN_MEAN = 0, 1
@@ -34,12 +34,16 @@ EXPORTS = ("ipd_attn_workspace_size", "ipd_verify_attn", "ipd_decode_attn",
            "ipd_score_span_static", "ipd_score_span_ex", "ipd_score_span_needed", "ipd_full_kl",
            "ipd_loss_grad_workspace_size", "ipd_split_loss_grad", "ipd_sample_workspace_size",
            "ipd_sample", "ipd_kv_append", "ipd_kv_append_many", "ipd_set_attn_kernel_timing",
-           "ipd_attn_kernel_time", "ipd_device_readable")
+           "ipd_attn_kernel_time", "ipd_device_readable", "ipd_rope_table", "ipd_rope",
+           "ipd_rope_append")
 # takeover / handback rules (IPD_RULE_*)
 RULE_TOPK, RULE_ENTROPY_S, RULE_ENTROPY_T, RULE_ALWAYS, RULE_NEVER = 0, 1, 2, 3, 4
 # element type of the dense gradient (IPD_DTYPE_*)
 DTYPE_F32, DTYPE_BF16 = 0, 1
 STATIC_MAX_TOKENS = 4096  # IPD_STATIC_MAX_TOKENS
+# rotary layouts and frequency scalings (IPD_ROPE_*, IPD_ROPE_SCALE_*)
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_SCALE = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
 
 class IpdError(RuntimeError):
@@ -90,6 +94,30 @@ class _AttnBatch(ctypes.Structure):
                 ("max_q_len", ctypes.c_int32), ("max_seq_len", ctypes.c_int32), ("out", c_p)]
 
 
+class _RopeScaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("trained_len", ctypes.c_double), ("beta_fast", ctypes.c_double),
+                ("beta_slow", ctypes.c_double)]
+
+
+class _RopeArgs(ctypes.Structure):
+    _fields_ = [("x", c_p), ("y", c_p), ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
+                ("pos", c_p), ("table", c_p)] + \
+        [(n, ctypes.c_int32) for n in ("dtype", "n_tokens", "n_heads", "head_dim", "max_pos",
+                                       "rot_dim", "layout", "inverse")]
+
+
+class _RopeAppendDesc(ctypes.Structure):
+    _fields_ = [(n, c_p) for n in ("q", "k", "v", "q_out", "k_out")] + \
+        [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride",
+                                       "k_out_stride")] + \
+        [("k_pages", c_p), ("v_pages", c_p), ("num_pages", ctypes.c_int64), ("cu_new", c_p),
+         ("seq_len", c_p), ("page_table", c_p), ("table", c_p)] + \
+        [(n, ctypes.c_int32) for n in ("num_q_heads", "num_kv_heads", "page_size", "head_dim",
+                                       "max_pages", "num_reqs", "total_new", "max_pos", "rot_dim",
+                                       "layout")]
+
+
 _lib.ipd_attn_workspace_size.restype = c_sz
 _lib.ipd_attn_workspace_size.argtypes = [ctypes.POINTER(_AttnBatch), c_i,
                                          ctypes.POINTER(_AttnBatch), c_i]
@@ -132,6 +160,12 @@ _lib.ipd_kv_append.argtypes = [c_p, c_p, ctypes.c_int64, c_i, c_i, c_i, c_p, c_p
                                c_i, c_i, c_i, c_p]
 _lib.ipd_kv_append_many.restype = c_i
 _lib.ipd_kv_append_many.argtypes = [ctypes.POINTER(_KvAppendDesc), c_i, c_p]
+_lib.ipd_rope_table.restype = c_i
+_lib.ipd_rope_table.argtypes = [c_p, c_i, c_i, ctypes.POINTER(_RopeScaling), c_p]
+_lib.ipd_rope.restype = c_i
+_lib.ipd_rope.argtypes = [ctypes.POINTER(_RopeArgs), c_p]
+_lib.ipd_rope_append.restype = c_i
+_lib.ipd_rope_append.argtypes = [ctypes.POINTER(_RopeAppendDesc), c_p]
 _lib.ipd_set_attn_kernel_timing.restype = c_i
 _lib.ipd_set_attn_kernel_timing.argtypes = [c_i]
 _lib.ipd_attn_kernel_time.restype = c_i
@@ -402,6 +436,83 @@ def split_loss_grad(logits_student, logits_teacher, topk_s, topk_t, source, cu_s
         _ptr(cu_span), _ptr(n_emit), _ptr(resp_len), _ptr(loss_out8), R, T, V, K, agg_mode,
         dir_mode, grad_scale, _ptr(grad_idx), _ptr(grad_val), _ptr(grad_dense), dtype, None, 0,
         _stream(stream)), "ipd_split_loss_grad")
+
+
+def _refuse(what: str):
+    raise IpdError(STATUS_CODES["IPD_ERR_INVALID_ARG"], what)
+
+
+def _rows(t: torch.Tensor, dtype, what: str) -> int:
+    """Token stride of a [n, heads, head_dim] tensor whose rows are contiguous."""
+    n, h, d = t.shape
+    s0, s1, s2 = t.stride()
+    if t.dtype != dtype or (d > 1 and s2 != 1) or (h > 1 and s1 != d):
+        _refuse(what)
+    return s0 if n > 1 else h * d
+
+
+def _check_table(table: torch.Tensor, what: str):
+    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or \
+            not table.is_contiguous():
+        _refuse(what)
+
+
+def rope_table(table: torch.Tensor, base: float = 1e6, scaling: str = "none", factor: float = 1.0,
+               trained_len: float = 32768.0, beta_fast: float = 32.0, beta_slow: float = 1.0,
+               stream=None):
+    """Fills ``table`` ([max_pos, rot_dim / 2, 2] fp32) with (cos, sin) of
+    position times frequency; ``scaling`` is a key of ROPE_SCALE."""
+    _check_table(table, "ipd_rope_table: table")
+    if scaling not in ROPE_SCALE:
+        _refuse("ipd_rope_table: scaling")
+    c = _RopeScaling(ROPE_SCALE[scaling], base, factor, trained_len, beta_fast, beta_slow)
+    _check(_lib.ipd_rope_table(table.data_ptr(), table.shape[0], 2 * table.shape[1],
+                               ctypes.byref(c), _stream(stream)), "ipd_rope_table")
+
+
+def rope(x: torch.Tensor, out: torch.Tensor, pos: torch.Tensor, table: torch.Tensor,
+         layout: int = ROPE_HALF, inverse: bool = False, stream=None):
+    """Rotates the heads of ``x`` ([n, H, D] bf16 or fp32, rows contiguous) by
+    their positions ``pos`` (int32 [n]) into ``out`` (may be ``x``); ``inverse``
+    applies the transpose, the rotation's gradient."""
+    _check_table(table, "ipd_rope: table")
+    if x.shape != out.shape or pos.dtype != torch.int32 or pos.numel() != x.shape[0] or \
+            not pos.is_contiguous() or x.dtype not in (torch.float32, torch.bfloat16):
+        _refuse("ipd_rope: shapes or types")
+    n, h, d = x.shape
+    a = _RopeArgs(x.data_ptr(), out.data_ptr(), _rows(x, x.dtype, "ipd_rope: x"),
+                  _rows(out, x.dtype, "ipd_rope: out"), pos.data_ptr(), table.data_ptr(),
+                  DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_F32, n, h, d, table.shape[0],
+                  2 * table.shape[1], layout, 1 if inverse else 0)
+    _check(_lib.ipd_rope(ctypes.byref(a), _stream(stream)), "ipd_rope")
+
+
+def rope_append(cache: "KVCache", q: Optional[torch.Tensor], q_out: Optional[torch.Tensor],
+                k_new, v_new, cu_new, seq_len, page_table, table: torch.Tensor,
+                layout: int = ROPE_HALF, k_out: Optional[torch.Tensor] = None, stream=None):
+    """Rotates the new tokens' queries ([n, Hq, 128] bf16, or None) into
+    ``q_out`` and their keys ([n, Hkv, 128]) into the cache's pages (and
+    ``k_out``), and writes their values beside them: kv_append of the rotated
+    rows in one launch.  Each row's position is its place in its sequence."""
+    _check_table(table, "ipd_rope_append: table")
+    bf = torch.bfloat16
+    hkv = cache.num_kv_heads
+    n = k_new.shape[0]
+    if k_new.shape != (n, hkv, 128) or v_new.shape != k_new.shape or \
+            (k_out is not None and k_out.shape != k_new.shape) or (q is None) != (q_out is None) or \
+            (q is not None and (q.shape != q_out.shape or q.shape[0] != n or q.shape[2] != 128)):
+        _refuse("ipd_rope_append: shapes")
+    a = _RopeAppendDesc(
+        _ptr(q), k_new.data_ptr(), v_new.data_ptr(), _ptr(q_out), _ptr(k_out),
+        0 if q is None else _rows(q, bf, "ipd_rope_append: q"),
+        _rows(k_new, bf, "ipd_rope_append: k_new"), _rows(v_new, bf, "ipd_rope_append: v_new"),
+        0 if q is None else _rows(q_out, bf, "ipd_rope_append: q_out"),
+        0 if k_out is None else _rows(k_out, bf, "ipd_rope_append: k_out"),
+        cache.k_pages.data_ptr(), cache.v_pages.data_ptr(), cache.k_pages.shape[0],
+        cu_new.data_ptr(), seq_len.data_ptr(), page_table.data_ptr(), table.data_ptr(),
+        0 if q is None else q.shape[1], hkv, cache.k_pages.shape[2], cache.k_pages.shape[3],
+        page_table.shape[1], cu_new.numel() - 1, n, table.shape[0], 2 * table.shape[1], layout)
+    _check(_lib.ipd_rope_append(ctypes.byref(a), _stream(stream)), "ipd_rope_append")
 
 
 def set_attn_kernel_timing(on: bool):
