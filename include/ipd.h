@@ -31,7 +31,8 @@
  * Before the first step, from a prompt to its first proposed token:
  * ipd_rope_append (rotary positions of new queries and keys, and the write of
  * their K/V rows into the paged cache, in one launch), with ipd_rope (the
- * rotation alone, or its gradient) and ipd_rope_table (the angles).
+ * rotation alone, or its gradient) and ipd_rope_table (the angles), and
+ * ipd_prompt_attn (causal attention of packed whole prompts).
  *
  * Conventions for every call
  *   - Data pointers are DEVICE pointers owned by the caller; the library never
@@ -559,6 +560,41 @@ typedef struct ipd_rope_append_desc {
   int32_t max_pages, num_reqs, total_new, max_pos, rot_dim, layout;
 } ipd_rope_append_desc;
 int ipd_rope_append(const ipd_rope_append_desc *desc, ipd_stream_t stream);
+
+/* Causal attention of whole prompts: num_seqs packed sequences, grouped heads.
+ *  q, out    [total] rows of num_q_heads heads of 128 bf16 entries, rows
+ *            q_stride / out_stride entries apart
+ *  k, v      [total] rows of num_kv_heads heads, rows k_stride / v_stride apart
+ *  cu_seq    [num_seqs + 1] int32 prefix offsets (device): sequence r owns rows
+ *            cu_seq[r] .. cu_seq[r + 1] - 1 of every tensor; it may be empty.
+ *            Rows outside cu_seq[0] .. cu_seq[num_seqs] - 1 are neither read
+ *            for another sequence nor written.
+ *  max_len   host-known upper bound on the sequence lengths
+ *  lse       [num_q_heads][total] fp32 natural log of each row's softmax sum,
+ *            ln sum_j exp(scale q.k_j), or NULL
+ * Query i of a sequence sees keys 0 .. i of it; query head h reads KV head
+ * h / (num_q_heads / num_kv_heads).  out = softmax(scale q K^T) V per query and
+ * head: scores, maxima and sums in fp32, the exponentials rounded to bf16 for
+ * the product with V, the output rounded once more.  Values of keys that a row
+ * does not see never reach it, infinities and NaN included.
+ * Pointers 16-byte aligned, strides multiples of 8 entries.  out must overlap
+ * none of q, k, v.  A sequence whose offsets are out of order or past total
+ * (IPD_DEVERR_SPAN) or that is longer than max_len (IPD_DEVERR_SEQ_LEN) is
+ * recorded and left out.  No workspace.  Returns IPD_ERR_UNSUPPORTED unless
+ * head_dim == 128 and num_q_heads / num_kv_heads <= 128, IPD_ERR_INVALID_ARG
+ * for a missing or misaligned pointer, a stride shorter than a row, heads that
+ * do not divide or a scale that is not positive and finite.
+ * A single query over a cache is ipd_decode_attn; a span, ipd_verify_attn. */
+typedef struct ipd_prompt_args {
+  const uint16_t *q, *k, *v;
+  uint16_t *out;
+  float *lse;
+  const int32_t *cu_seq;
+  int64_t q_stride, k_stride, v_stride, out_stride;
+  int32_t num_q_heads, num_kv_heads, head_dim, num_seqs, total, max_len;
+  float softmax_scale;
+} ipd_prompt_args;
+int ipd_prompt_attn(const ipd_prompt_args *args, ipd_stream_t stream);
 
 /* Measurement aid.  While on, every ipd_verify_attn / ipd_decode_attn call
  * records CUDA events on its stream around its attention kernel alone (not

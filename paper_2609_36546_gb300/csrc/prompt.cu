@@ -1,0 +1,767 @@
+// Causal attention of whole prompts: packed sequences of different lengths,
+// grouped heads, head_dim 128, bf16 in and out.
+//
+//   o_i = sum_{j <= i} p_ij v_j / l_i,  p_ij = exp(scale q_i.k_j - m_i),
+//   l_i = sum_{j <= i} p_ij,            lse_i = m_i + ln l_i
+//
+// one pass over the keys with the running maximum m and sum l in fp32.
+//
+// What bounds it: 4 * 128 flop a head and visible key against 512 bytes of K
+// and V that every query tile shares, so the tensor cores from a few hundred
+// tokens on, and launch and pipeline latency below.
+//
+// Work item: one sequence, one KV head, two tiles of 128 query rows.  A row is
+// (position, query head of the group), so that the group's heads share every
+// K / V tile and a short prompt still fills its rows; a tile is floor(128 / G)
+// positions x G heads, loaded by one TMA box per 64-dim half.  Per 128 keys
+// and tile t:
+//   S_t = Q_t K^T          tcgen05, both operands in shared memory, fp32 in TMEM
+//   P_t = 2^(S_t c - m c)  one thread a row; bf16 back into S_t's TMEM columns
+//   O_t += P_t V           tcgen05, P from TMEM, V from shared memory
+// While one warpgroup exponentiates its tile, the tensor cores work on the
+// other's products.  P is rounded to bf16 (to nearest) for the second product,
+// the operand type of V: a relative error of at most 2^-8 a term, the size of
+// the output's own rounding; sums, maxima and O stay in fp32.  O is rescaled only
+// when a row's maximum has grown by more than 2^8 since the last time (the
+// running maximum only has to keep the exponentials in range).
+//
+// Warps: 0-3 and 4-7 one tile each (softmax, rescale, output), 8 loads, 9
+// issues the products, 10 finds the items, 11 mends V tiles on the diagonal:
+// there P is 0 for keys a row must not see, and 0 x inf or 0 x NaN would leak
+// into rows that come before a broken value or belong to another sequence.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <cudaTypedefs.h>
+#include <stdint.h>
+#include <string.h>
+
+#include "common.cuh"
+
+IPD_DECLARE_ERROR_WORD(g_prompt_err);
+
+namespace {
+
+constexpr int kD = 128;
+constexpr int kRows = 128;                   // rows of a query tile (M)
+constexpr int kKeys = 128;                   // keys of a K / V tile (N)
+constexpr int kTileBytes = kRows * kD * 2;   // 32 KB: a Q, K or V tile
+constexpr int kHalfBytes = kTileBytes / 2;   // its 64-dim halves, 128-byte swizzled rows
+constexpr int kStages = 5;                   // K and V tiles in flight
+constexpr int kSlots = 3;                    // items handed from the item warp to the others
+constexpr int kMendSlots = 4;               // more than the V tiles that can be in flight
+constexpr int kThreads = 384;
+constexpr int kLoadWarp = 8, kMmaWarp = 9, kItemWarp = 10, kMendWarp = 11;
+constexpr uint32_t kTmemCols = 512;          // S_0, S_1, O_0, O_1 of 128 fp32 columns
+__host__ __device__ constexpr uint32_t col_s(int t) { return 128u * (uint32_t)t; }
+__host__ __device__ constexpr uint32_t col_o(int t) { return 256u + 128u * (uint32_t)t; }
+// Registers: launched with 168 a thread; the third warpgroup gives back what
+// the softmax warpgroups need to hold a row's 128 scores.
+constexpr int kRegsLaunch = 168, kRegsAux = 56, kRegsSoftmax = 224;
+static_assert(kMendSlots > (kStages + 1) / 2, "a slot is reused only after its tile was consumed");
+static_assert(256 * kRegsSoftmax + 128 * kRegsAux <= kThreads * kRegsLaunch,
+              "the register split must fit the registers the block was launched with");
+constexpr float kRescaleLog2 = 8.0f;         // growth of the maximum that rescales O
+constexpr int kItemReaders = 8 + 3;          // softmax warps, loader, issuer, mender
+
+struct Item {
+  int start, len;   // the sequence's first token and length
+  int pos;          // first query position
+  int kvh;
+  int nk[2];        // K / V tiles of each query tile (0: the tile has no rows)
+  int first_masked; // first K / V tile in which some row sees only part of the keys
+  int valid;
+  int bad;          // a visible non-finite value was taken out of a diagonal V tile
+};
+
+struct Shared {
+  alignas(1024) uint8_t q[2][kTileBytes];
+  alignas(1024) uint8_t kv[kStages][kTileBytes];
+  uint64_t q_full, q_empty, kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2], o_full[2],
+      o_empty[2], v_landed[kMendSlots], item_full[kSlots], item_empty[kSlots], drain;
+  Item item[kSlots];
+  uint32_t tmem;
+  int abort;
+};
+constexpr int kSharedBytes = (int)sizeof(Shared) + 1024;  // the base is aligned by hand
+static_assert(kSharedBytes <= 232448, "shared memory of one CTA");
+
+struct Params {
+  CUtensorMap q, k, v;
+  const uint16_t *v_ptr;
+  long long v_stride, out_stride;
+  uint16_t *out;
+  float *lse;
+  const int32_t *cu;
+  int num_seqs, total, max_len;
+  int hq, hkv, group;
+  int tile_pos;  // positions of one query tile: floor(128 / group)
+  float scale_log2;
+};
+
+// 3-D tiled TMA load (dims, heads, tokens).
+IPD_DEVINL void tma_load_3d(void *dst, const CUtensorMap *map, int x, int y, int z, uint64_t *bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+      : "memory");
+}
+
+// A wait that gives up after about a second, or as soon as another warp of the
+// CTA has given up.
+IPD_DEVINL bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity)) {
+    if (*abort) return false;
+    if (clock64() - t0 > kWaitLimitCycles) {
+      ipd_set_error(&g_prompt_err, IPD_DEVERR_WAIT);
+      *abort = 1;
+      return false;
+    }
+  }
+  return true;
+}
+IPD_DEVINL bool wait(uint64_t *bar, uint32_t parity, volatile int *abort) {
+  return mbar_try_wait(bar, parity) || wait_slow(bar, parity, abort);
+}
+// the same for a whole warp, with one answer
+IPD_DEVINL bool wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort) {
+  return __all_sync(0xffffffffu, wait(bar, parity, abort)) != 0;
+}
+
+// Phase of the n-th use (0, 1, ...) of a barrier: a consumer waits for it with
+// parity n & 1, a producer for the release of its slot with the other.
+IPD_DEVINL uint32_t full_parity(uint32_t n) { return n & 1u; }
+IPD_DEVINL uint32_t empty_parity(uint32_t n) { return (n & 1u) ^ 1u; }
+
+// --------------------------------------------------------------------------
+// items
+// --------------------------------------------------------------------------
+// Length of sequence r; 0 (recorded once) where the offsets are out of order
+// or past the tensors, or the length is over the caller's bound.
+IPD_DEVINL int seq_len(const Params &P, int r, int *start) {
+  const int a = P.cu[r], b = P.cu[r + 1];
+  *start = a;
+  if (a < 0 || b < a || b > P.total) {
+    ipd_set_error(&g_prompt_err, IPD_DEVERR_SPAN);
+    return 0;
+  }
+  if (b - a > P.max_len) {
+    ipd_set_error(&g_prompt_err, IPD_DEVERR_SEQ_LEN);
+    return 0;
+  }
+  return b - a;
+}
+
+// Items in order of falling cost: level by level from the longest (an item's
+// level is its place along its sequence, which is what it costs), the
+// sequences that reach a level in order, KV heads innermost.  The CTAs take
+// them round by round, every other round backwards, so that the rounds'
+// differences cancel.
+struct ItemFinder {
+  int level;          // items below `before` lie at higher levels
+  long long before;
+  int here;           // (sequence, tile) pairs at `level`
+
+  __device__ void count(const Params &P, int lane, int pt) {
+    int n = 0;
+    for (int r = lane; r < P.num_seqs; r += 32) {
+      int a;
+      n += (seq_len(P, r, &a) + pt - 1) / pt > level ? 1 : 0;
+    }
+    here = __reduce_add_sync(0xffffffffu, n);
+  }
+  __device__ void init(const Params &P, int lane, int pt) {
+    level = (P.max_len + pt - 1) / pt - 1;
+    before = 0;
+    // start at the highest level that has a sequence
+    int top = 0;
+    for (int r = lane; r < P.num_seqs; r += 32) {
+      int a;
+      top = max(top, (seq_len(P, r, &a) + pt - 1) / pt);
+    }
+    level = __reduce_max_sync(0xffffffffu, top) - 1;
+    here = 0;
+    if (level >= 0) count(P, lane, pt);
+  }
+  // the s-th (sequence, tile) pair; pairs are asked for in rising order
+  __device__ bool find(const Params &P, int lane, int pt, long long s, int *seq, int *tile) {
+    while (level >= 0 && s >= before + here) {
+      before += here;
+      --level;
+      if (level >= 0) count(P, lane, pt);
+    }
+    if (level < 0) return false;
+    int rank = (int)(s - before);
+    for (int r0 = 0; r0 < P.num_seqs; r0 += 32) {
+      const int r = r0 + lane;
+      int a, n = 0;
+      if (r < P.num_seqs) n = (seq_len(P, r, &a) + pt - 1) / pt;
+      const uint32_t in = __ballot_sync(0xffffffffu, n > level);
+      const int c = __popc(in);
+      if (rank < c) {
+        *seq = r0 + __fns(in, 0, rank + 1);
+        *tile = level;
+        return true;
+      }
+      rank -= c;
+    }
+    return false;
+  }
+};
+
+__device__ void item_warp(const Params &P, Shared &S, int lane) {
+  const int pt = 2 * P.tile_pos;
+  ItemFinder F;
+  F.init(P, lane, pt);
+  for (uint32_t n = 0;; ++n) {
+    const int slot = n % kSlots;
+    const uint32_t use = n / kSlots;
+    const long long b = (n & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+    const long long idx = (long long)n * gridDim.x + b;
+    int r = 0, tile = 0;
+    const bool ok = F.find(P, lane, pt, idx / P.hkv, &r, &tile);
+    if (!wait_warp(&S.item_empty[slot], empty_parity(use), &S.abort)) return;
+    if (lane == 0) {
+      Item &I = S.item[slot];
+      I.valid = ok;
+      I.bad = 0;
+      if (ok) {
+        I.len = seq_len(P, r, &I.start);
+        I.pos = tile * pt;
+        I.kvh = (int)(idx % P.hkv);
+        for (int t = 0; t < 2; ++t) {
+          const int p0 = I.pos + t * P.tile_pos, p1 = min(I.len, p0 + P.tile_pos);
+          I.nk[t] = p0 < I.len ? (p1 + kKeys - 1) / kKeys : 0;
+        }
+        // tile k is seen whole by every row when its last key is at or before
+        // the item's first position
+        I.first_masked = (I.pos + 1) / kKeys;
+      }
+      mbar_arrive(&S.item_full[slot]);
+    }
+    __syncwarp();
+    if (!ok) return;
+  }
+}
+
+// --------------------------------------------------------------------------
+// loads
+// --------------------------------------------------------------------------
+__device__ void load_warp(const Params &P, Shared &S) {
+  uint32_t ring = 0, n_q = 0, n_mend = 0;
+  const uint32_t q_bytes = (uint32_t)(P.group * P.tile_pos) * kD * 2;
+  for (uint32_t n = 0;; ++n) {
+    const int slot = n % kSlots;
+    if (!wait(&S.item_full[slot], full_parity(n / kSlots), &S.abort)) break;
+    const Item I = S.item[slot];
+    mbar_arrive(&S.item_empty[slot]);
+    if (!I.valid) break;
+    if (!wait(&S.q_empty, empty_parity(n), &S.abort)) break;
+    const int tiles = I.nk[1] > 0 ? 2 : 1;
+    mbar_arrive_expect_tx(&S.q_full, q_bytes * tiles);
+    for (int t = 0; t < tiles; ++t)
+      for (int h = 0; h < 2; ++h)
+        tma_load_3d(S.q[t] + h * kHalfBytes, &P.q, 64 * h, I.kvh * P.group,
+                    I.start + I.pos + t * P.tile_pos, &S.q_full);
+    ++n_q;
+    const int nk = max(I.nk[0], I.nk[1]);
+    bool ok = true;
+    for (int j = 0; j < 2 * nk && ok; ++j, ++ring) {
+      const int st = ring % kStages;
+      ok = wait(&S.kv_empty[st], empty_parity(ring / kStages), &S.abort);
+      if (!ok) break;
+      // a diagonal V tile lands at the mending warp, which then fills the stage
+      uint64_t *landed = &S.kv_full[st];
+      if ((j & 1) && (j >> 1) >= I.first_masked) landed = &S.v_landed[n_mend++ % kMendSlots];
+      mbar_arrive_expect_tx(landed, kTileBytes);
+      for (int h = 0; h < 2; ++h)
+        tma_load_3d(S.kv[st] + h * kHalfBytes, (j & 1) ? &P.v : &P.k, 64 * h, I.kvh,
+                    I.start + (j >> 1) * kKeys, landed);
+    }
+    if (!ok) break;
+  }
+  if (*(volatile int *)&S.abort) {
+    // the CTA gives up: its copies in flight land first (bounded)
+    if (n_q > 0) mbar_wait_bounded(&S.q_full, full_parity(n_q - 1));
+    for (uint32_t s = 0; s < (uint32_t)kStages && s < ring; ++s) {
+      const uint32_t last = ring - 1 - s;
+      mbar_wait_bounded(&S.kv_full[last % kStages], full_parity(last / kStages));
+    }
+    for (uint32_t s = 0; s < (uint32_t)kMendSlots && s < n_mend; ++s) {
+      const uint32_t last = n_mend - 1 - s;
+      mbar_wait_bounded(&S.v_landed[last % kMendSlots], full_parity(last / kMendSlots));
+    }
+  }
+}
+
+// --------------------------------------------------------------------------
+// products
+// --------------------------------------------------------------------------
+__device__ void mma_warp(const Params &P, Shared &S) {
+  constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys, 0);
+  constexpr uint32_t idesc_o = idesc_bf16_f32(kRows, kD, 1);
+  const uint32_t tmem = S.tmem;
+  uint32_t ring = 0, n_p[2] = {0, 0}, n_o[2] = {0, 0};
+  const auto issue_s = [&](int t, int stage) {
+    const uint64_t a0 = sdesc_sw128(smem_u32(S.q[t]), 16, 1024);
+    const uint64_t b0 = sdesc_sw128(smem_u32(S.kv[stage]), 16, 1024);
+#pragma unroll
+    for (int kk = 0; kk < kD / 16; ++kk) {
+      const uint64_t off = (uint64_t)(((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4);
+      tc_mma_bf16(tmem + col_s(t), a0 + off, b0 + off, idesc_s, kk > 0);
+    }
+    tc_commit(&S.s_full[t]);
+  };
+  const auto issue_o = [&](int t, int stage, bool accumulate) {
+    // V is N-major: 64-dim halves kHalfBytes apart, 8-key groups 1024 apart
+    const uint64_t b0 = sdesc_sw128(smem_u32(S.kv[stage]), kHalfBytes, 1024);
+#pragma unroll
+    for (int kk = 0; kk < kKeys / 16; ++kk)
+      tc_mma_bf16_ta(tmem + col_o(t), tmem + col_s(t) + 8 * kk, b0 + (uint64_t)(kk * 2048 >> 4),
+                     idesc_o, accumulate || kk > 0);
+  };
+  bool ok = true;
+  for (uint32_t n = 0; ok; ++n) {
+    const int slot = n % kSlots;
+    if (!(ok = wait(&S.item_full[slot], full_parity(n / kSlots), &S.abort))) break;
+    const Item I = S.item[slot];
+    mbar_arrive(&S.item_empty[slot]);
+    if (!I.valid) break;
+    const int nk = max(I.nk[0], I.nk[1]);
+    if (!(ok = wait(&S.q_full, full_parity(n), &S.abort))) break;
+    int ks = ring % kStages;  // stage of K tile j, then of K tile j + 1
+    if (!(ok = wait(&S.kv_full[ks], full_parity(ring / kStages), &S.abort))) break;
+    tc_fence_after();
+    for (int t = 0; t < 2; ++t)
+      if (I.nk[t] > 0) issue_s(t, ks);
+    tc_commit(&S.kv_empty[ks]);
+    if (nk == 1) tc_commit(&S.q_empty);
+    ++ring;
+    for (int j = 0; j < nk && ok; ++j) {
+      const int vs = ring % kStages;
+      if (!(ok = wait(&S.kv_full[vs], full_parity(ring / kStages), &S.abort))) break;
+      ++ring;
+      const bool more = j + 1 < nk;
+      if (more) {
+        ks = ring % kStages;
+        if (!(ok = wait(&S.kv_full[ks], full_parity(ring / kStages), &S.abort))) break;
+        ++ring;
+      }
+      for (int t = 0; t < 2; ++t) {
+        if (j >= I.nk[t]) continue;
+        if (j == 0) {  // O_t of the item before has been read
+          if (!(ok = wait(&S.o_empty[t], empty_parity(n_o[t]), &S.abort))) break;
+          ++n_o[t];
+        }
+        if (!(ok = wait(&S.p_full[t], full_parity(n_p[t]), &S.abort))) break;
+        ++n_p[t];
+        tc_fence_after();
+        issue_o(t, vs, j > 0);
+        // S_t's columns hold P_t until the product above has read them; the
+        // tensor core takes this thread's instructions in order
+        if (j + 1 < I.nk[t]) issue_s(t, ks);
+        else tc_commit(&S.o_full[t]);
+      }
+      if (!ok) break;
+      tc_commit(&S.kv_empty[vs]);
+      if (more) tc_commit(&S.kv_empty[ks]);
+      if (j + 2 == nk) tc_commit(&S.q_empty);  // the last K tile's products are issued
+    }
+  }
+  if (!ok) {  // the CTA gives up: products in flight end before TMEM is freed
+    tc_commit(&S.drain);
+    mbar_wait_bounded(&S.drain, 0);
+  }
+}
+
+// --------------------------------------------------------------------------
+// V tiles on the diagonal
+// --------------------------------------------------------------------------
+IPD_DEVINL bool bf16_pair_not_finite(uint32_t w) {
+  return (w & 0x7f800000u) == 0x7f800000u || (w & 0x00007f80u) == 0x00007f80u;
+}
+IPD_DEVINL uint32_t drop_not_finite(uint32_t w) {
+  if ((w & 0x7f800000u) == 0x7f800000u) w &= 0x0000ffffu;
+  if ((w & 0x00007f80u) == 0x00007f80u) w &= 0xffff0000u;
+  return w;
+}
+
+// Keys after the item's first position are hidden from some of its rows (or
+// from all: keys past the sequence's end).  Infinities and NaN among them are
+// set to 0 in shared memory; rows that do see one get it back at the end.  The
+// tile's copy completes on a barrier of this warp's own, and its arrival fills
+// the stage for the issuing warp.
+__device__ void mend_warp(const Params &P, Shared &S, int lane) {
+  uint32_t ring = 0, n_mend = 0;
+  for (uint32_t n = 0;; ++n) {
+    const int slot = n % kSlots;
+    if (!wait_warp(&S.item_full[slot], full_parity(n / kSlots), &S.abort)) return;
+    const Item I = S.item[slot];
+    if (!I.valid) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&S.item_empty[slot]);
+      return;
+    }
+    const int nk = max(I.nk[0], I.nk[1]);
+    for (int j = min(I.first_masked, nk); j < nk; ++j) {
+      const int st = (ring + 2 * j + 1) % kStages;  // V tile j's stage
+      if (!wait_warp(&S.v_landed[n_mend % kMendSlots], full_parity(n_mend / kMendSlots), &S.abort))
+        return;
+      ++n_mend;
+      const int row0 = max(0, I.pos + 1 - j * kKeys);
+      bool seen = false;
+      for (int h = 0; h < 2; ++h) {
+        uint4 *v = reinterpret_cast<uint4 *>(S.kv[st] + h * kHalfBytes);
+#pragma unroll 4
+        for (int i = row0 * 8 + lane; i < kKeys * 8; i += 32) {
+          uint4 w = v[i];
+          if (bf16_pair_not_finite(w.x) || bf16_pair_not_finite(w.y) ||
+              bf16_pair_not_finite(w.z) || bf16_pair_not_finite(w.w)) {
+            w.x = drop_not_finite(w.x), w.y = drop_not_finite(w.y);
+            w.z = drop_not_finite(w.z), w.w = drop_not_finite(w.w);
+            v[i] = w;
+            if (j * kKeys + (i >> 3) < I.len) seen = true;
+          }
+        }
+      }
+      fence_proxy_async_smem();
+      const bool bad = __any_sync(0xffffffffu, seen);
+      __syncwarp();
+      if (lane == 0) {
+        if (bad) S.item[slot].bad = 1;
+        mbar_arrive(&S.kv_full[st]);
+      }
+      __syncwarp();
+    }
+    ring += 2 * nk;
+    if (lane == 0) mbar_arrive(&S.item_empty[slot]);
+  }
+}
+
+// --------------------------------------------------------------------------
+// softmax and output of one query tile
+// --------------------------------------------------------------------------
+// O's row in TMEM times f (all warps of the tile, 128 columns).
+IPD_DEVINL void scale_o(uint32_t o, float f) {
+#pragma unroll
+  for (int c = 0; c < kD; c += 32) {
+    uint32_t r[32];
+    tc_ld_32x32b_x32(o + c, r);
+    tc_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
+    tc_st_32x32b_x32(o + c, r);
+  }
+  tc_wait_st();
+}
+
+// The non-finite values of the keys after the item's first position that were
+// taken out of the V tiles, added back to the stored output of a row at `pos`
+// that sees them: any weight of theirs leaves an infinity infinite and a NaN a
+// NaN, so the finite part's rounding does not matter.
+IPD_DEVINL void add_not_finite(const Params &P, const Item &I, int pos, uint16_t *out) {
+#pragma unroll 1
+  for (int d = 0; d < kD; d += 2) {
+    uint32_t *at = reinterpret_cast<uint32_t *>(out + d);
+    float lo = bf16lo(*at), hi = bf16hi(*at);
+#pragma unroll 1
+    for (int key = I.pos + 1; key <= pos; ++key) {
+      const uint32_t w = *reinterpret_cast<const uint32_t *>(
+          P.v_ptr + (long long)(I.start + key) * P.v_stride + (long long)I.kvh * kD + d);
+      if ((w & 0x00007f80u) == 0x00007f80u) lo += bf16lo(w);
+      if ((w & 0x7f800000u) == 0x7f800000u) hi += bf16hi(w);
+    }
+    *at = pack_bf16x2(lo, hi);
+  }
+}
+
+template <bool MASKED>
+IPD_DEVINL float row_max(uint32_t (&s)[kKeys], int lim) {
+  if (MASKED) {
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i)
+      if (i > lim) s[i] = 0xff800000u;
+  }
+  float m[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) m[k] = __uint_as_float(s[k]);
+#pragma unroll
+  for (int i = 4; i < kKeys - 4; i += 8)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      m[k] = fmax3(m[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
+#pragma unroll
+  for (int k = 0; k < 4; ++k) m[k] = fmaxf(m[k], __uint_as_float(s[kKeys - 4 + k]));
+  return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+}
+
+__device__ void softmax_warps(const Params &P, Shared &S, int t, int warp, int lane) {
+  const int row = (warp & 3) * 32 + lane;
+  const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+  const uint32_t s_col = S.tmem + lanes + col_s(t), o_col = S.tmem + lanes + col_o(t);
+  const int row_pos = row / P.group, row_head = row % P.group;
+  const float c = P.scale_log2;
+  const unsigned long long c2 = f2_pack(c, c);
+  uint32_t n_s = 0, n_o = 0;
+  for (uint32_t n = 0;; ++n) {
+    const int slot = n % kSlots;
+    if (!wait_warp(&S.item_full[slot], full_parity(n / kSlots), &S.abort)) return;
+    const Item I = S.item[slot];
+    const int nk = I.valid ? I.nk[t] : 0;
+    if (nk > 0) {
+      const int pos = I.pos + t * P.tile_pos + row_pos;
+      const bool live = row_pos < P.tile_pos && pos < I.len;
+      const int last = min(pos, I.len - 1);  // a row without a query follows the last one
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < nk; ++j) {
+        if (!wait_warp(&S.s_full[t], full_parity(n_s), &S.abort)) return;
+        ++n_s;
+        tc_fence_after();
+        uint32_t s[kKeys];
+#pragma unroll
+        for (int k = 0; k < kKeys; k += 32)
+          tc_ld_32x32b_x32(s_col + k, reinterpret_cast<uint32_t(&)[32]>(s[k]));
+        tc_wait_ld();
+        const float mx = j >= I.first_masked ? row_max<true>(s, last - j * kKeys)
+                                             : row_max<false>(s, 0);
+        if (j == 0) {
+          m = mx;
+        } else {
+          // m is -inf while every visible score has been: the first finite
+          // one then rescales (a sum of zeros)
+          const bool grow = (mx - m) * c > kRescaleLog2;
+          if (__any_sync(0xffffffffu, grow)) {
+            float f = 1.f;
+            if (grow) {
+              f = m == -INFINITY ? 0.f : ex2_approx((m - mx) * c);
+              m = mx;
+            }
+            l *= f;
+            // s_full counted the products before S_t's too: O_t is complete
+            scale_o(o_col, f);
+          }
+        }
+        const float off = m == -INFINITY ? 0.f : -m * c;
+        const unsigned long long off2 = f2_pack(off, off);
+        unsigned long long sum[2] = {0ull, 0ull};
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb) {
+          uint32_t p[32];
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const int e = hb * 64 + 2 * i;
+            float x0, x1;
+            f2_unpack(f2_fma(f2_pack(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, off2),
+                      x0, x1);
+            x0 = ex2_approx(x0);
+            x1 = ex2_approx(x1);
+            sum[i & 1] = f2_add(sum[i & 1], f2_pack(x0, x1));
+            p[i] = pack_bf16x2(x0, x1);
+          }
+          tc_st_32x32b_x32(s_col + 32 * hb, p);
+        }
+        float a, b;
+        f2_unpack(f2_add(sum[0], sum[1]), a, b);
+        l += a + b;
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&S.p_full[t]);
+      }
+      if (!wait_warp(&S.o_full[t], full_parity(n_o), &S.abort)) return;
+      ++n_o;
+      tc_fence_after();
+      const bool bad = *(volatile int *)&S.item[slot].bad != 0;
+      const float inv = 1.f / l;
+      uint16_t *out = P.out + (long long)(I.start + pos) * P.out_stride +
+                      (long long)(I.kvh * P.group + row_head) * kD;
+#pragma unroll
+      for (int k = 0; k < kD; k += 32) {
+        uint32_t o[32];
+        tc_ld_32x32b_x32(o_col + k, o);
+        tc_wait_ld();
+        if (k + 32 == kD) {  // O_t is read: the next item may write it
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&S.o_empty[t]);
+        }
+        if (live) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            w[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<uint4 *>(out + k + 2 * i) =
+                make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+        }
+      }
+      if (bad && live) add_not_finite(P, I, pos, out);
+      if (live && P.lse)
+        P.lse[(long long)(I.kvh * P.group + row_head) * P.total + I.start + pos] =
+            (m == -INFINITY ? -INFINITY : (m * c + log2f(l)) * kLn2);
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&S.item_empty[slot]);
+    if (!I.valid) return;
+  }
+}
+
+__global__ void __launch_bounds__(kThreads, 1) prompt_attn_kernel(const __grid_constant__ Params P) {
+  extern __shared__ uint8_t smem_raw[];
+  Shared &S = *reinterpret_cast<Shared *>(
+      smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(&S.q_full, 1);
+    mbar_init(&S.q_empty, 1);
+    for (int i = 0; i < kStages; ++i) mbar_init(&S.kv_full[i], 1), mbar_init(&S.kv_empty[i], 1);
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&S.s_full[t], 1);
+      mbar_init(&S.p_full[t], 4);
+      mbar_init(&S.o_full[t], 1);
+      mbar_init(&S.o_empty[t], 4);
+    }
+    for (int i = 0; i < kMendSlots; ++i) mbar_init(&S.v_landed[i], 1);
+    mbar_init(&S.drain, 1);
+    for (int i = 0; i < kSlots; ++i)
+      mbar_init(&S.item_full[i], 1), mbar_init(&S.item_empty[i], kItemReaders);
+    S.abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == kMmaWarp) {
+    tc_alloc(&S.tmem, kTmemCols);
+    tc_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRegsAux));
+    if (warp == kItemWarp) {
+      item_warp(P, S, lane);
+    } else if (warp == kMendWarp) {
+      mend_warp(P, S, lane);
+    } else if (lane == 0) {
+      if (warp == kLoadWarp) load_warp(P, S);
+      else mma_warp(P, S);
+    }
+    __syncwarp();
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRegsSoftmax));
+    softmax_warps(P, S, warp >> 2, warp, lane);
+    __syncwarp();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kMmaWarp) tc_dealloc(S.tmem, kTmemCols);
+}
+
+// --------------------------------------------------------------------------
+struct DevInfo {
+  int sms = 0;
+};
+DevInfo g_prompt_dev[64];
+PFN_cuTensorMapEncodeTiled_v12000 g_prompt_encode = nullptr;
+
+int prepare_device(int *sms) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return IPD_ERR_CUDA;
+  if (!g_prompt_encode) {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault,
+                                         &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess || !fn)
+      return IPD_ERR_CUDA;
+    g_prompt_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+  }
+  DevInfo &D = g_prompt_dev[dev];
+  if (D.sms == 0) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        cudaFuncSetAttribute(prompt_attn_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             kSharedBytes) != cudaSuccess)
+      return IPD_ERR_CUDA;
+    D.sms = n;
+  }
+  *sms = D.sms;
+  return IPD_OK;
+}
+
+// [tokens][heads][128] bf16, tokens `stride` entries apart; a box is 64 dims x
+// `heads` heads x `tokens` tokens: rows (token, head) of 128 swizzled bytes.
+int encode(CUtensorMap *m, const void *base, int heads, int tokens, long long stride, int box_heads,
+           int box_tokens) {
+  const cuuint64_t dims[3] = {kD, (cuuint64_t)heads, (cuuint64_t)tokens};
+  const cuuint64_t strides[2] = {kD * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const CUresult r =
+      g_prompt_encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims,
+                      strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? IPD_OK : IPD_ERR_CUDA;
+}
+
+}  // namespace
+
+extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_prompt_error() {
+  unsigned int v = 0, z = 0;
+  if (cudaMemcpyFromSymbol(&v, g_prompt_err, sizeof(v)) != cudaSuccess) return 0xffffffffu;
+  if (cudaMemcpyToSymbol(g_prompt_err, &z, sizeof(z)) != cudaSuccess) return 0xffffffffu;
+  return v;
+}
+
+extern "C" int ipd_prompt_attn(const ipd_prompt_args *args, ipd_stream_t stream) {
+  if (!args) return IPD_ERR_INVALID_ARG;
+  const ipd_prompt_args &a = *args;
+  if (a.num_seqs < 0 || a.total < 0 || a.max_len < 0 || a.num_kv_heads < 1 || a.num_q_heads < 1 ||
+      a.num_q_heads % a.num_kv_heads || !(a.softmax_scale > 0.f) ||
+      !(a.softmax_scale - a.softmax_scale == 0.f))
+    return IPD_ERR_INVALID_ARG;
+  const int group = a.num_q_heads / a.num_kv_heads;
+  if (a.head_dim != kD || group > kRows || a.num_q_heads > 65536) return IPD_ERR_UNSUPPORTED;
+  if (a.total == 0 || a.num_seqs == 0 || a.max_len == 0) return IPD_OK;
+  const long long qrow = (long long)a.num_q_heads * kD, krow = (long long)a.num_kv_heads * kD;
+  if (!a.q || !a.k || !a.v || !a.out || !a.cu_seq) return IPD_ERR_INVALID_ARG;
+  if (a.q_stride < qrow || a.out_stride < qrow || a.k_stride < krow || a.v_stride < krow)
+    return IPD_ERR_INVALID_ARG;
+  const uintptr_t align = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.out |
+                          (uintptr_t)(2 * a.q_stride) | (uintptr_t)(2 * a.k_stride) |
+                          (uintptr_t)(2 * a.v_stride) | (uintptr_t)(2 * a.out_stride);
+  if (align & 15) return IPD_ERR_INVALID_ARG;
+  // the tensor maps hold strides below 2^40 bytes
+  if ((a.q_stride | a.k_stride | a.v_stride) >> 38) return IPD_ERR_UNSUPPORTED;
+  int sms = 0;
+  int st = prepare_device(&sms);
+  if (st != IPD_OK) return st;
+  Params P;
+  memset(&P, 0, sizeof(P));
+  P.tile_pos = kRows / group;
+  if (encode(&P.q, a.q, a.num_q_heads, a.total, a.q_stride, group, P.tile_pos) != IPD_OK ||
+      encode(&P.k, a.k, a.num_kv_heads, a.total, a.k_stride, 1, kKeys) != IPD_OK ||
+      encode(&P.v, a.v, a.num_kv_heads, a.total, a.v_stride, 1, kKeys) != IPD_OK)
+    return IPD_ERR_CUDA;
+  P.v_ptr = a.v;
+  P.v_stride = a.v_stride;
+  P.out = a.out;
+  P.out_stride = a.out_stride;
+  P.lse = a.lse;
+  P.cu = a.cu_seq;
+  P.num_seqs = a.num_seqs;
+  P.total = a.total;
+  P.max_len = a.max_len;
+  P.hq = a.num_q_heads;
+  P.hkv = a.num_kv_heads;
+  P.group = group;
+  P.scale_log2 = a.softmax_scale * kLog2e;
+  // at most one CTA per SM and per item (a sequence's last item may be partial)
+  const long long pt = 2 * P.tile_pos;
+  const long long items = ((long long)a.total / pt + a.num_seqs) * a.num_kv_heads;
+  const int grid = (int)(items < sms ? items : sms);
+  prompt_attn_kernel<<<grid, kThreads, kSharedBytes, reinterpret_cast<cudaStream_t>(stream)>>>(P);
+  return cudaGetLastError() == cudaSuccess ? IPD_OK : IPD_ERR_CUDA;
+}

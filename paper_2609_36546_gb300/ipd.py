@@ -35,7 +35,7 @@ EXPORTS = ("ipd_attn_workspace_size", "ipd_verify_attn", "ipd_decode_attn",
            "ipd_loss_grad_workspace_size", "ipd_split_loss_grad", "ipd_sample_workspace_size",
            "ipd_sample", "ipd_kv_append", "ipd_kv_append_many", "ipd_set_attn_kernel_timing",
            "ipd_attn_kernel_time", "ipd_device_readable", "ipd_rope_table", "ipd_rope",
-           "ipd_rope_append")
+           "ipd_rope_append", "ipd_prompt_attn")
 # takeover / handback rules (IPD_RULE_*)
 RULE_TOPK, RULE_ENTROPY_S, RULE_ENTROPY_T, RULE_ALWAYS, RULE_NEVER = 0, 1, 2, 3, 4
 # element type of the dense gradient (IPD_DTYPE_*)
@@ -118,6 +118,13 @@ class _RopeAppendDesc(ctypes.Structure):
                                        "layout")]
 
 
+class _PromptArgs(ctypes.Structure):
+    _fields_ = [(n, c_p) for n in ("q", "k", "v", "out", "lse", "cu_seq")] + \
+        [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride", "out_stride")] + \
+        [(n, ctypes.c_int32) for n in ("num_q_heads", "num_kv_heads", "head_dim", "num_seqs",
+                                       "total", "max_len")] + [("softmax_scale", ctypes.c_float)]
+
+
 _lib.ipd_attn_workspace_size.restype = c_sz
 _lib.ipd_attn_workspace_size.argtypes = [ctypes.POINTER(_AttnBatch), c_i,
                                          ctypes.POINTER(_AttnBatch), c_i]
@@ -166,6 +173,8 @@ _lib.ipd_rope.restype = c_i
 _lib.ipd_rope.argtypes = [ctypes.POINTER(_RopeArgs), c_p]
 _lib.ipd_rope_append.restype = c_i
 _lib.ipd_rope_append.argtypes = [ctypes.POINTER(_RopeAppendDesc), c_p]
+_lib.ipd_prompt_attn.restype = c_i
+_lib.ipd_prompt_attn.argtypes = [ctypes.POINTER(_PromptArgs), c_p]
 _lib.ipd_set_attn_kernel_timing.restype = c_i
 _lib.ipd_set_attn_kernel_timing.argtypes = [c_i]
 _lib.ipd_attn_kernel_time.restype = c_i
@@ -513,6 +522,27 @@ def rope_append(cache: "KVCache", q: Optional[torch.Tensor], q_out: Optional[tor
         0 if q is None else q.shape[1], hkv, cache.k_pages.shape[2], cache.k_pages.shape[3],
         page_table.shape[1], cu_new.numel() - 1, n, table.shape[0], 2 * table.shape[1], layout)
     _check(_lib.ipd_rope_append(ctypes.byref(a), _stream(stream)), "ipd_rope_append")
+
+
+def prompt_attn(q, k, v, cu_seq, max_len: int, out, softmax_scale: float,
+                lse: Optional[torch.Tensor] = None, stream=None):
+    """Causal attention of packed prompts: q [total, Hq, 128], k and v
+    [total, Hkv, 128], out [total, Hq, 128] bf16 (rows contiguous, any row
+    stride), cu_seq int32 [num_seqs + 1] (device), ``max_len`` a host-known
+    bound on the lengths; lse fp32 [Hq, total] when given."""
+    n, hq, d = q.shape
+    if k.shape != v.shape or k.shape[0] != n or k.shape[2] != d or out.shape != q.shape or \
+            cu_seq.dtype != torch.int32 or not cu_seq.is_contiguous() or \
+            (lse is not None and (lse.shape != (hq, n) or lse.dtype != torch.float32 or
+                                  not lse.is_contiguous())):
+        _refuse("ipd_prompt_attn: shapes or types")
+    bf = torch.bfloat16
+    a = _PromptArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse),
+                    cu_seq.data_ptr(), _rows(q, bf, "ipd_prompt_attn: q"),
+                    _rows(k, bf, "ipd_prompt_attn: k"), _rows(v, bf, "ipd_prompt_attn: v"),
+                    _rows(out, bf, "ipd_prompt_attn: out"), hq, k.shape[1], d,
+                    cu_seq.numel() - 1, n, max_len, softmax_scale)
+    _check(_lib.ipd_prompt_attn(ctypes.byref(a), _stream(stream)), "ipd_prompt_attn")
 
 
 def set_attn_kernel_timing(on: bool):
