@@ -32,7 +32,9 @@
  * ipd_rope_append (rotary positions of new queries and keys, and the write of
  * their K/V rows into the paged cache, in one launch), with ipd_rope (the
  * rotation alone, or its gradient) and ipd_rope_table (the angles), and
- * ipd_prompt_attn (causal attention of packed whole prompts).
+ * ipd_prompt_attn (causal attention of packed whole prompts) and
+ * ipd_sample_trunc (a token per row at a temperature, cut by top-k, min-p and
+ * top-p, from given uniform numbers).
  *
  * Conventions for every call
  *   - Data pointers are DEVICE pointers owned by the caller; the library never
@@ -79,6 +81,7 @@ typedef struct CUstream_st *ipd_stream_t; /* same handle as cudaStream_t */
 #define IPD_DEVERR_WAIT 5u       /* a bounded pipeline wait ran out         */
 #define IPD_DEVERR_SPAN 6u       /* cu_span / cu_q / cu_new not non-decreasing, or rows past them */
 #define IPD_DEVERR_POSITION 7u   /* a position outside the rotary table */
+#define IPD_DEVERR_SETTING 8u    /* a row's sampling settings are not valid */
 
 #define IPD_MAX_BATCHES 8
 #define IPD_MAX_K 32
@@ -595,6 +598,46 @@ typedef struct ipd_prompt_args {
   float softmax_scale;
 } ipd_prompt_args;
 int ipd_prompt_attn(const ipd_prompt_args *args, ipd_stream_t stream);
+
+/* One token per row from softmax(l * inv_temperature), cut by top-k, min-p and
+ * top-p, drawn with the caller's uniform numbers.  (ipd_sample draws from the
+ * whole softmax with its own generator.)  A draw is a fixed function of (row,
+ * settings, u), reproducible on any device: its sums are of whole numbers.
+ * With every fp32 product and sum rounded on its own,
+ *   c   = fl(fp32(log2 e) * inv_temperature)
+ *   x_v = fl(fl(l_v - max l) c), and 0 where l_v is the maximum; NaN counts as -inf
+ *   w_v = floor(2^30 2^x_v + 1/2): x clamped below at -64, i = x rounded to
+ *         nearest even, f = x - i, 2^x = 2^i P(f) truncated to 31 fractional
+ *         bits and halved upwards, P by Horner's rule with the fp32 coefficients
+ *         (bit patterns, lowest degree first) 3F800000 3F317213 3E75FCDB
+ *         3D635D55 3C1E760B 3AAD4281
+ * and the entries in order of falling logit (lower id first among equals):
+ *   1. top-k keeps the first top_k entries (all, if top_k <= 0)
+ *   2. min-p keeps, of those, w_v >= max(1, ceil(min_p 2^30)): entries at least
+ *      min_p times as likely as the likeliest
+ *   3. top-p keeps, of those, the shortest prefix whose mass is at least
+ *      ceil(fp64(top_p) M), M their mass (sum of w); at least the first entry,
+ *      all of them from top_p = 1 on
+ *   4. the token is the entry in which position floor(fp64(u) S) of the running
+ *      sum falls, S the mass of what is kept (clamped to S - 1; 0 for u <= 0 or NaN)
+ *   5. logp is its log-probability among the kept, ln 2 (x - log2(2^-30 S))
+ *  logits    [n_rows] bf16 rows of vocab entries, row_stride entries apart; any
+ *            alignment of whole entries; vocab at most 262,136, odd ones included
+ *  u         [n_rows] fp32 uniform numbers in [0, 1) (device)
+ *  inv_temperature, top_p, min_p  [n_rows] fp32, top_k [n_rows] int32, one
+ *            setting per row (device), each NULL for 1, 1, 0 and no top-k
+ *  tokens    [n_rows] int32; logp [n_rows] fp32 and n_kept [n_rows] int32 (the
+ *            number of entries kept) or NULL
+ * A row without a finite or +inf entry draws -1, with logp -inf and n_kept 0;
+ * so does one whose settings are not valid (log2 e * inv_temperature not positive
+ * and finite, a NaN top_p, a min_p outside [0, 1]), which records
+ * IPD_DEVERR_SETTING.  No workspace.  Returns IPD_ERR_INVALID_ARG for a missing
+ * pointer, a negative size or vocab < 1, IPD_ERR_UNSUPPORTED for a larger vocab. */
+#define IPD_TRUNC_MAX_VOCAB 262136
+int ipd_sample_trunc(const uint16_t *logits, int64_t row_stride, int n_rows, int vocab,
+                     const float *u, const float *inv_temperature, const int32_t *top_k,
+                     const float *top_p, const float *min_p, int32_t *tokens, float *logp,
+                     int32_t *n_kept, ipd_stream_t stream);
 
 /* Measurement aid.  While on, every ipd_verify_attn / ipd_decode_attn call
  * records CUDA events on its stream around its attention kernel alone (not

@@ -21,7 +21,7 @@ STATUS = {0: "IPD_OK", 1: "IPD_ERR_INVALID_ARG", 2: "IPD_ERR_UNSUPPORTED", 3: "I
           4: "IPD_ERR_CUDA", 5: "IPD_ERR_TIMEOUT", 6: "IPD_ERR_DEVICE", 7: "IPD_ERR_CAPACITY"}
 STATUS_CODES = {v: k for k, v in STATUS.items()}
 DEVERR = {0: "none", 1: "page id", 2: "seq len", 3: "token id", 4: "plan overflow", 5: "wait",
-          6: "span offsets", 7: "rotary position"}
+          6: "span offsets", 7: "rotary position", 8: "sampling settings"}
 
 DIR_SPLIT, DIR_REVERSE, DIR_FORWARD, DIR_INVERSE = 0, 1, 2, 3
 AGG_SEQ_MEAN_TOKEN_MEAN, AGG_GLOBAL_TOKEN_MEAN = 0, 1
@@ -35,11 +35,12 @@ EXPORTS = ("ipd_attn_workspace_size", "ipd_verify_attn", "ipd_decode_attn",
            "ipd_loss_grad_workspace_size", "ipd_split_loss_grad", "ipd_sample_workspace_size",
            "ipd_sample", "ipd_kv_append", "ipd_kv_append_many", "ipd_set_attn_kernel_timing",
            "ipd_attn_kernel_time", "ipd_device_readable", "ipd_rope_table", "ipd_rope",
-           "ipd_rope_append", "ipd_prompt_attn")
+           "ipd_rope_append", "ipd_prompt_attn", "ipd_sample_trunc")
 # takeover / handback rules (IPD_RULE_*)
 RULE_TOPK, RULE_ENTROPY_S, RULE_ENTROPY_T, RULE_ALWAYS, RULE_NEVER = 0, 1, 2, 3, 4
 # element type of the dense gradient (IPD_DTYPE_*)
 DTYPE_F32, DTYPE_BF16 = 0, 1
+TRUNC_MAX_VOCAB = 262136  # IPD_TRUNC_MAX_VOCAB
 STATIC_MAX_TOKENS = 4096  # IPD_STATIC_MAX_TOKENS
 # rotary layouts and frequency scalings (IPD_ROPE_*, IPD_ROPE_SCALE_*)
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
@@ -175,6 +176,8 @@ _lib.ipd_rope_append.restype = c_i
 _lib.ipd_rope_append.argtypes = [ctypes.POINTER(_RopeAppendDesc), c_p]
 _lib.ipd_prompt_attn.restype = c_i
 _lib.ipd_prompt_attn.argtypes = [ctypes.POINTER(_PromptArgs), c_p]
+_lib.ipd_sample_trunc.restype = c_i
+_lib.ipd_sample_trunc.argtypes = [c_p, ctypes.c_int64, c_i, c_i] + [c_p] * 9
 _lib.ipd_set_attn_kernel_timing.restype = c_i
 _lib.ipd_set_attn_kernel_timing.argtypes = [c_i]
 _lib.ipd_attn_kernel_time.restype = c_i
@@ -543,6 +546,30 @@ def prompt_attn(q, k, v, cu_seq, max_len: int, out, softmax_scale: float,
                     _rows(out, bf, "ipd_prompt_attn: out"), hq, k.shape[1], d,
                     cu_seq.numel() - 1, n, max_len, softmax_scale)
     _check(_lib.ipd_prompt_attn(ctypes.byref(a), _stream(stream)), "ipd_prompt_attn")
+
+
+def sample_trunc(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor,
+                 inv_temperature: Optional[torch.Tensor] = None,
+                 top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                 min_p: Optional[torch.Tensor] = None, logp: Optional[torch.Tensor] = None,
+                 n_kept: Optional[torch.Tensor] = None, stream=None):
+    """One token per row of ``logits`` ([n, V] bf16, entries contiguous, any row
+    stride) into ``tokens`` (int32 [n]), drawn with the uniform numbers ``u``
+    (fp32 [n]) after the rows' own settings (fp32 [n]; ``top_k`` int32 [n]);
+    ``logp`` (fp32) and ``n_kept`` (int32) take the log-probability of the token
+    among the kept entries and their number."""
+    n, V = logits.shape
+    f, i = torch.float32, torch.int32
+    for t, dt in ((u, f), (tokens, i), (inv_temperature, f), (top_k, i), (top_p, f), (min_p, f),
+                  (logp, f), (n_kept, i)):
+        if t is not None and (t.dtype != dt or t.numel() != n or not t.is_contiguous()):
+            _refuse("ipd_sample_trunc: per-row tensors")
+    if logits.dtype != torch.bfloat16 or (V > 1 and logits.stride(1) != 1):
+        _refuse("ipd_sample_trunc: logits")
+    _check(_lib.ipd_sample_trunc(logits.data_ptr(), logits.stride(0) if n > 1 else V, n, V,
+                                 u.data_ptr(), _ptr(inv_temperature), _ptr(top_k), _ptr(top_p),
+                                 _ptr(min_p), tokens.data_ptr(), _ptr(logp), _ptr(n_kept),
+                                 _stream(stream)), "ipd_sample_trunc")
 
 
 def set_attn_kernel_timing(on: bool):
