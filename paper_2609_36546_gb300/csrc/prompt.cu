@@ -26,9 +26,13 @@
 // running maximum only has to keep the exponentials in range).
 //
 // Warps: 0-3 and 4-7 one tile each (softmax, rescale, output), 8 loads, 9
-// issues the products, 10 finds the items, 11 mends V tiles on the diagonal:
-// there P is 0 for keys a row must not see, and 0 x inf or 0 x NaN would leak
-// into rows that come before a broken value or belong to another sequence.
+// issues the products, 10 finds the items.
+//
+// Keys that some row of an item must not see (the diagonal, the sequence's end)
+// get P = 0, but 0 x inf and 0 x NaN would leak a broken value into rows that
+// come before it or belong to another sequence.  So the softmax warps look
+// through such a V tile before they release P, set what is not finite to 0 in
+// shared memory, and rows that do see it get it back at the end.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cudaTypedefs.h>
@@ -50,7 +54,7 @@ constexpr int kStages = 5;                   // K and V tiles in flight
 constexpr int kSlots = 3;                    // items handed from the item warp to the others
 constexpr int kMendSlots = 4;               // more than the V tiles that can be in flight
 constexpr int kThreads = 384;
-constexpr int kLoadWarp = 8, kMmaWarp = 9, kItemWarp = 10, kMendWarp = 11;
+constexpr int kLoadWarp = 8, kMmaWarp = 9, kItemWarp = 10;  // (warp 11 idles)
 constexpr uint32_t kTmemCols = 512;          // S_0, S_1, O_0, O_1 of 128 fp32 columns
 __host__ __device__ constexpr uint32_t col_s(int t) { return 128u * (uint32_t)t; }
 __host__ __device__ constexpr uint32_t col_o(int t) { return 256u + 128u * (uint32_t)t; }
@@ -61,7 +65,7 @@ static_assert(kMendSlots > (kStages + 1) / 2, "a slot is reused only after its t
 static_assert(256 * kRegsSoftmax + 128 * kRegsAux <= kThreads * kRegsLaunch,
               "the register split must fit the registers the block was launched with");
 constexpr float kRescaleLog2 = 8.0f;         // growth of the maximum that rescales O
-constexpr int kItemReaders = 8 + 3;          // softmax warps, loader, issuer, mender
+constexpr int kItemReaders = 8 + 2;          // softmax warps, loader, issuer
 
 struct Item {
   int start, len;   // the sequence's first token and length
@@ -76,7 +80,7 @@ struct Item {
 struct Shared {
   alignas(1024) uint8_t q[2][kTileBytes];
   alignas(1024) uint8_t kv[kStages][kTileBytes];
-  uint64_t q_full, q_empty, kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2], o_full[2],
+  uint64_t q_full, q_empty, kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2][2], o_full[2],
       o_empty[2], v_landed[kMendSlots], item_full[kSlots], item_empty[kSlots], drain;
   Item item[kSlots];
   uint32_t tmem;
@@ -108,10 +112,15 @@ IPD_DEVINL void tma_load_3d(void *dst, const CUtensorMap *map, int x, int y, int
 }
 
 // A wait that gives up after about a second, or as soon as another warp of the
-// CTA has given up.
+// CTA has given up.  Each try suspends the thread for a while in hardware; the
+// clock and the flag are looked at every few tries only, so that waiting warps
+// leave the issue slots to the others.
 IPD_DEVINL bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort) {
   const long long t0 = clock64();
-  while (!mbar_try_wait(bar, parity)) {
+  while (true) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
     if (*abort) return false;
     if (clock64() - t0 > kWaitLimitCycles) {
       ipd_set_error(&g_prompt_err, IPD_DEVERR_WAIT);
@@ -119,7 +128,6 @@ IPD_DEVINL bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort) {
       return false;
     }
   }
-  return true;
 }
 IPD_DEVINL bool wait(uint64_t *bar, uint32_t parity, volatile int *abort) {
   return mbar_try_wait(bar, parity) || wait_slow(bar, parity, abort);
@@ -162,51 +170,58 @@ struct ItemFinder {
   int level;          // items below `before` lie at higher levels
   long long before;
   int here;           // (sequence, tile) pairs at `level`
+  int start, len;     // sequence `lane`, when there are at most 32 (else read again)
 
+  __device__ int tiles(const Params &P, int r, int lane, int pt) {
+    if (P.num_seqs > 32) {
+      int a;
+      return r < P.num_seqs ? (seq_len(P, r, &a) + pt - 1) / pt : 0;
+    }
+    return (len + pt - 1) / pt;
+  }
   __device__ void count(const Params &P, int lane, int pt) {
     int n = 0;
-    for (int r = lane; r < P.num_seqs; r += 32) {
-      int a;
-      n += (seq_len(P, r, &a) + pt - 1) / pt > level ? 1 : 0;
-    }
+    for (int r = lane; r < P.num_seqs; r += 32) n += tiles(P, r, lane, pt) > level ? 1 : 0;
     here = __reduce_add_sync(0xffffffffu, n);
   }
   __device__ void init(const Params &P, int lane, int pt) {
-    level = (P.max_len + pt - 1) / pt - 1;
+    start = len = 0;
+    if (P.num_seqs <= 32 && lane < P.num_seqs) len = seq_len(P, lane, &start);
     before = 0;
-    // start at the highest level that has a sequence
     int top = 0;
-    for (int r = lane; r < P.num_seqs; r += 32) {
-      int a;
-      top = max(top, (seq_len(P, r, &a) + pt - 1) / pt);
-    }
-    level = __reduce_max_sync(0xffffffffu, top) - 1;
+    for (int r = lane; r < P.num_seqs; r += 32) top = max(top, tiles(P, r, lane, pt));
+    level = __reduce_max_sync(0xffffffffu, top) - 1;  // the highest that has a sequence
     here = 0;
     if (level >= 0) count(P, lane, pt);
   }
-  // the s-th (sequence, tile) pair; pairs are asked for in rising order
-  __device__ bool find(const Params &P, int lane, int pt, long long s, int *seq, int *tile) {
+  // the s-th (sequence, tile) pair: its tile (< 0: there is none), and the
+  // sequence's place; pairs are asked for in rising order
+  __device__ int find(const Params &P, int lane, int pt, long long s, int *at, int *n) {
     while (level >= 0 && s >= before + here) {
       before += here;
       --level;
       if (level >= 0) count(P, lane, pt);
     }
-    if (level < 0) return false;
+    if (level < 0) return -1;
     int rank = (int)(s - before);
     for (int r0 = 0; r0 < P.num_seqs; r0 += 32) {
-      const int r = r0 + lane;
-      int a, n = 0;
-      if (r < P.num_seqs) n = (seq_len(P, r, &a) + pt - 1) / pt;
-      const uint32_t in = __ballot_sync(0xffffffffu, n > level);
+      const uint32_t in = __ballot_sync(0xffffffffu, tiles(P, r0 + lane, lane, pt) > level);
       const int c = __popc(in);
       if (rank < c) {
-        *seq = r0 + __fns(in, 0, rank + 1);
-        *tile = level;
-        return true;
+        const uint32_t hit = __ballot_sync(
+            0xffffffffu, ((in >> lane) & 1u) && __popc(in & ((1u << lane) - 1u)) == rank);
+        const int src = __ffs(hit) - 1;
+        if (P.num_seqs <= 32) {
+          *at = __shfl_sync(0xffffffffu, start, src);
+          *n = __shfl_sync(0xffffffffu, len, src);
+        } else {
+          *n = seq_len(P, r0 + src, at);
+        }
+        return level;
       }
       rank -= c;
     }
-    return false;
+    return -1;
   }
 };
 
@@ -219,15 +234,17 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
     const uint32_t use = n / kSlots;
     const long long b = (n & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
     const long long idx = (long long)n * gridDim.x + b;
-    int r = 0, tile = 0;
-    const bool ok = F.find(P, lane, pt, idx / P.hkv, &r, &tile);
+    int start = 0, len = 0;
+    const int tile = F.find(P, lane, pt, idx / P.hkv, &start, &len);
+    const bool ok = tile >= 0;
     if (!wait_warp(&S.item_empty[slot], empty_parity(use), &S.abort)) return;
     if (lane == 0) {
       Item &I = S.item[slot];
       I.valid = ok;
       I.bad = 0;
       if (ok) {
-        I.len = seq_len(P, r, &I.start);
+        I.start = start;
+        I.len = len;
         I.pos = tile * pt;
         I.kvh = (int)(idx % P.hkv);
         for (int t = 0; t < 2; ++t) {
@@ -271,9 +288,13 @@ __device__ void load_warp(const Params &P, Shared &S) {
       const int st = ring % kStages;
       ok = wait(&S.kv_empty[st], empty_parity(ring / kStages), &S.abort);
       if (!ok) break;
-      // a diagonal V tile lands at the mending warp, which then fills the stage
+      // a V tile with hidden keys lands at the softmax warps, whose release of P
+      // then covers it; its stage counts as filled at once
       uint64_t *landed = &S.kv_full[st];
-      if ((j & 1) && (j >> 1) >= I.first_masked) landed = &S.v_landed[n_mend++ % kMendSlots];
+      if ((j & 1) && (j >> 1) >= I.first_masked) {
+        landed = &S.v_landed[n_mend++ % kMendSlots];
+        mbar_arrive(&S.kv_full[st]);
+      }
       mbar_arrive_expect_tx(landed, kTileBytes);
       for (int h = 0; h < 2; ++h)
         tma_load_3d(S.kv[st] + h * kHalfBytes, (j & 1) ? &P.v : &P.k, 64 * h, I.kvh,
@@ -298,153 +319,156 @@ __device__ void load_warp(const Params &P, Shared &S) {
 // --------------------------------------------------------------------------
 // products
 // --------------------------------------------------------------------------
-__device__ void mma_warp(const Params &P, Shared &S) {
+// The warp's elected lane issues; every other value is the whole warp's, so that
+// the operands stay in uniform registers (issued from a branch of one lane,
+// each product cost its own time again in register moves).
+IPD_DEVINL uint32_t elect_one() {
+  uint32_t e;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(e));
+  return e;
+}
+IPD_DEVINL int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+
+__device__ void mma_warp(const Params &P, Shared &S, int lane) {
   constexpr uint32_t idesc_s = idesc_bf16_f32(kRows, kKeys, 0);
   constexpr uint32_t idesc_o = idesc_bf16_f32(kRows, kD, 1);
-  const uint32_t tmem = S.tmem;
+  constexpr uint64_t kTileStep = kTileBytes >> 4, kHalfStep = kHalfBytes >> 4;
+  const uint32_t tmem = (uint32_t)uniform((int)S.tmem);
+  // descriptors of the first Q tile and stage; V is N-major: 64-dim halves
+  // kHalfBytes apart, 8-key groups 1024 apart
+  const uint64_t q0 = sdesc_sw128((uint32_t)uniform((int)smem_u32(S.q[0])), 16, 1024);
+  const uint64_t k0 = sdesc_sw128((uint32_t)uniform((int)smem_u32(S.kv[0])), 16, 1024);
+  const uint64_t v0 = sdesc_sw128((uint32_t)uniform((int)smem_u32(S.kv[0])), kHalfBytes, 1024);
   uint32_t ring = 0, n_p[2] = {0, 0}, n_o[2] = {0, 0};
   const auto issue_s = [&](int t, int stage) {
-    const uint64_t a0 = sdesc_sw128(smem_u32(S.q[t]), 16, 1024);
-    const uint64_t b0 = sdesc_sw128(smem_u32(S.kv[stage]), 16, 1024);
+    const uint64_t a = q0 + t * kTileStep, b = k0 + stage * kTileStep;
+    if (elect_one()) {
 #pragma unroll
-    for (int kk = 0; kk < kD / 16; ++kk) {
-      const uint64_t off = (uint64_t)(((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4);
-      tc_mma_bf16(tmem + col_s(t), a0 + off, b0 + off, idesc_s, kk > 0);
+      for (int kk = 0; kk < kD / 16; ++kk) {
+        const uint64_t off = (kk >> 2) * kHalfStep + (uint64_t)(32 * (kk & 3) >> 4);
+        tc_mma_bf16(tmem + col_s(t), a + off, b + off, idesc_s, kk > 0);
+      }
+      tc_commit(&S.s_full[t]);
     }
-    tc_commit(&S.s_full[t]);
+    __syncwarp();
   };
-  const auto issue_o = [&](int t, int stage, bool accumulate) {
-    // V is N-major: 64-dim halves kHalfBytes apart, 8-key groups 1024 apart
-    const uint64_t b0 = sdesc_sw128(smem_u32(S.kv[stage]), kHalfBytes, 1024);
+  // keys 64 half .. 64 half + 63
+  const auto issue_o = [&](int t, int stage, int half, bool accumulate) {
+    const uint64_t b = v0 + stage * kTileStep + (uint64_t)(half * 8192 >> 4);
+    const uint32_t a = tmem + col_s(t) + 32 * half;
+    if (elect_one()) {
 #pragma unroll
-    for (int kk = 0; kk < kKeys / 16; ++kk)
-      tc_mma_bf16_ta(tmem + col_o(t), tmem + col_s(t) + 8 * kk, b0 + (uint64_t)(kk * 2048 >> 4),
-                     idesc_o, accumulate || kk > 0);
+      for (int kk = 0; kk < 4; ++kk)
+        tc_mma_bf16_ta(tmem + col_o(t), a + 8 * kk, b + (uint64_t)(2048 * kk >> 4), idesc_o,
+                       accumulate || kk > 0);
+    }
+    __syncwarp();
+  };
+  const auto commit = [&](uint64_t *bar) {
+    if (elect_one()) tc_commit(bar);
+    __syncwarp();
   };
   bool ok = true;
   for (uint32_t n = 0; ok; ++n) {
     const int slot = n % kSlots;
-    if (!(ok = wait(&S.item_full[slot], full_parity(n / kSlots), &S.abort))) break;
-    const Item I = S.item[slot];
-    mbar_arrive(&S.item_empty[slot]);
-    if (!I.valid) break;
-    const int nk = max(I.nk[0], I.nk[1]);
-    if (!(ok = wait(&S.q_full, full_parity(n), &S.abort))) break;
+    if (!(ok = wait_warp(&S.item_full[slot], full_parity(n / kSlots), &S.abort))) break;
+    const int valid = uniform(S.item[slot].valid);
+    const int nk0 = uniform(S.item[slot].nk[0]), nk1 = uniform(S.item[slot].nk[1]);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&S.item_empty[slot]);
+    if (!valid) break;
+    const int nk = max(nk0, nk1);
+    if (!(ok = wait_warp(&S.q_full, full_parity(n), &S.abort))) break;
     int ks = ring % kStages;  // stage of K tile j, then of K tile j + 1
-    if (!(ok = wait(&S.kv_full[ks], full_parity(ring / kStages), &S.abort))) break;
+    if (!(ok = wait_warp(&S.kv_full[ks], full_parity(ring / kStages), &S.abort))) break;
     tc_fence_after();
+#pragma unroll
     for (int t = 0; t < 2; ++t)
-      if (I.nk[t] > 0) issue_s(t, ks);
-    tc_commit(&S.kv_empty[ks]);
-    if (nk == 1) tc_commit(&S.q_empty);
+      if ((t ? nk1 : nk0) > 0) issue_s(t, ks);
+    commit(&S.kv_empty[ks]);
+    if (nk == 1) commit(&S.q_empty);
     ++ring;
+#pragma unroll 1
     for (int j = 0; j < nk && ok; ++j) {
       const int vs = ring % kStages;
-      if (!(ok = wait(&S.kv_full[vs], full_parity(ring / kStages), &S.abort))) break;
+      if (!(ok = wait_warp(&S.kv_full[vs], full_parity(ring / kStages), &S.abort))) break;
       ++ring;
       const bool more = j + 1 < nk;
       if (more) {
         ks = ring % kStages;
-        if (!(ok = wait(&S.kv_full[ks], full_parity(ring / kStages), &S.abort))) break;
+        if (!(ok = wait_warp(&S.kv_full[ks], full_parity(ring / kStages), &S.abort))) break;
         ++ring;
       }
+#pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if (j >= I.nk[t]) continue;
+        const int mine = t ? nk1 : nk0;
+        if (j >= mine) continue;
         if (j == 0) {  // O_t of the item before has been read
-          if (!(ok = wait(&S.o_empty[t], empty_parity(n_o[t]), &S.abort))) break;
+          if (!(ok = wait_warp(&S.o_empty[t], empty_parity(n_o[t]), &S.abort))) break;
           ++n_o[t];
         }
-        if (!(ok = wait(&S.p_full[t], full_parity(n_p[t]), &S.abort))) break;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          ok = wait_warp(&S.p_full[t][half], full_parity(n_p[t]), &S.abort);
+          if (!ok) break;
+          tc_fence_after();
+          issue_o(t, vs, half, j + half > 0);
+        }
+        if (!ok) break;
         ++n_p[t];
-        tc_fence_after();
-        issue_o(t, vs, j > 0);
-        // S_t's columns hold P_t until the product above has read them; the
+        // S_t's columns hold P_t until the products above have read them; the
         // tensor core takes this thread's instructions in order
-        if (j + 1 < I.nk[t]) issue_s(t, ks);
-        else tc_commit(&S.o_full[t]);
+        if (j + 1 < mine) issue_s(t, ks);
+        else commit(&S.o_full[t]);
       }
       if (!ok) break;
-      tc_commit(&S.kv_empty[vs]);
-      if (more) tc_commit(&S.kv_empty[ks]);
-      if (j + 2 == nk) tc_commit(&S.q_empty);  // the last K tile's products are issued
+      commit(&S.kv_empty[vs]);
+      if (more) commit(&S.kv_empty[ks]);
+      if (j + 2 == nk) commit(&S.q_empty);  // the last K tile's products are issued
     }
   }
   if (!ok) {  // the CTA gives up: products in flight end before TMEM is freed
-    tc_commit(&S.drain);
+    commit(&S.drain);
     mbar_wait_bounded(&S.drain, 0);
-  }
-}
-
-// --------------------------------------------------------------------------
-// V tiles on the diagonal
-// --------------------------------------------------------------------------
-IPD_DEVINL bool bf16_pair_not_finite(uint32_t w) {
-  return (w & 0x7f800000u) == 0x7f800000u || (w & 0x00007f80u) == 0x00007f80u;
-}
-IPD_DEVINL uint32_t drop_not_finite(uint32_t w) {
-  if ((w & 0x7f800000u) == 0x7f800000u) w &= 0x0000ffffu;
-  if ((w & 0x00007f80u) == 0x00007f80u) w &= 0xffff0000u;
-  return w;
-}
-
-// Keys after the item's first position are hidden from some of its rows (or
-// from all: keys past the sequence's end).  Infinities and NaN among them are
-// set to 0 in shared memory; rows that do see one get it back at the end.  The
-// tile's copy completes on a barrier of this warp's own, and its arrival fills
-// the stage for the issuing warp.
-__device__ void mend_warp(const Params &P, Shared &S, int lane) {
-  uint32_t ring = 0, n_mend = 0;
-  for (uint32_t n = 0;; ++n) {
-    const int slot = n % kSlots;
-    if (!wait_warp(&S.item_full[slot], full_parity(n / kSlots), &S.abort)) return;
-    const Item I = S.item[slot];
-    if (!I.valid) {
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&S.item_empty[slot]);
-      return;
-    }
-    const int nk = max(I.nk[0], I.nk[1]);
-    for (int j = min(I.first_masked, nk); j < nk; ++j) {
-      const int st = (ring + 2 * j + 1) % kStages;  // V tile j's stage
-      if (!wait_warp(&S.v_landed[n_mend % kMendSlots], full_parity(n_mend / kMendSlots), &S.abort))
-        return;
-      ++n_mend;
-      const int row0 = max(0, I.pos + 1 - j * kKeys);
-      bool seen = false;
-      for (int h = 0; h < 2; ++h) {
-        uint4 *v = reinterpret_cast<uint4 *>(S.kv[st] + h * kHalfBytes);
-#pragma unroll 4
-        for (int i = row0 * 8 + lane; i < kKeys * 8; i += 32) {
-          uint4 w = v[i];
-          if (bf16_pair_not_finite(w.x) || bf16_pair_not_finite(w.y) ||
-              bf16_pair_not_finite(w.z) || bf16_pair_not_finite(w.w)) {
-            w.x = drop_not_finite(w.x), w.y = drop_not_finite(w.y);
-            w.z = drop_not_finite(w.z), w.w = drop_not_finite(w.w);
-            v[i] = w;
-            if (j * kKeys + (i >> 3) < I.len) seen = true;
-          }
-        }
-      }
-      fence_proxy_async_smem();
-      const bool bad = __any_sync(0xffffffffu, seen);
-      __syncwarp();
-      if (lane == 0) {
-        if (bad) S.item[slot].bad = 1;
-        mbar_arrive(&S.kv_full[st]);
-      }
-      __syncwarp();
-    }
-    ring += 2 * nk;
-    if (lane == 0) mbar_arrive(&S.item_empty[slot]);
   }
 }
 
 // --------------------------------------------------------------------------
 // softmax and output of one query tile
 // --------------------------------------------------------------------------
+// Sets the infinities and NaN of a V tile's rows row0 .. 127 to 0 (one
+// warpgroup; thread = 0 .. 127); true if one belonged to a row below row_end.
+IPD_DEVINL uint32_t not_finite2(uint32_t w) {  // bit 15 of each half: its exponent is all ones
+  return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+}
+IPD_DEVINL bool drop_not_finite(uint8_t *tile, int row0, int row_end, int thread) {
+  bool seen = false;
+#pragma unroll 1
+  for (int h = 0; h < 2; ++h) {
+    uint4 *v = reinterpret_cast<uint4 *>(tile + h * kHalfBytes);
+#pragma unroll 4
+    for (int i = thread; i < kKeys * 8; i += 128) {
+      if ((i >> 3) < row0) continue;
+      const uint4 w = v[i];
+      if (not_finite2(w.x) | not_finite2(w.y) | not_finite2(w.z) | not_finite2(w.w)) {
+        const auto clear = [](uint32_t x) {
+          const uint32_t bad = not_finite2(x) >> 15;
+          return x & ~(bad * 0xffffu);
+        };
+        v[i] = make_uint4(clear(w.x), clear(w.y), clear(w.z), clear(w.w));
+        seen = seen || (i >> 3) < row_end;
+      }
+    }
+  }
+  fence_proxy_async_smem();
+  return seen;
+}
+
 // O's row in TMEM times f (all warps of the tile, 128 columns).
 IPD_DEVINL void scale_o(uint32_t o, float f) {
-#pragma unroll
+#pragma unroll 1
   for (int c = 0; c < kD; c += 32) {
     uint32_t r[32];
     tc_ld_32x32b_x32(o + c, r);
@@ -476,24 +500,23 @@ IPD_DEVINL void add_not_finite(const Params &P, const Item &I, int pos, uint16_t
   }
 }
 
+// Largest of 64 scores and m; MASKED: keys past `lim` count as -inf.
 template <bool MASKED>
-IPD_DEVINL float row_max(uint32_t (&s)[kKeys], int lim) {
+IPD_DEVINL float max_of(uint32_t *s, int lim, float m) {
   if (MASKED) {
 #pragma unroll
-    for (int i = 0; i < kKeys; ++i)
+    for (int i = 0; i < 64; ++i)
       if (i > lim) s[i] = 0xff800000u;
   }
-  float m[4];
+  float a[4] = {m, __uint_as_float(s[0]), __uint_as_float(s[1]), __uint_as_float(s[2])};
 #pragma unroll
-  for (int k = 0; k < 4; ++k) m[k] = __uint_as_float(s[k]);
-#pragma unroll
-  for (int i = 4; i < kKeys - 4; i += 8)
+  for (int i = 3; i < 59; i += 8)
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      m[k] = fmax3(m[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
-#pragma unroll
-  for (int k = 0; k < 4; ++k) m[k] = fmaxf(m[k], __uint_as_float(s[kKeys - 4 + k]));
-  return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+      a[k] = fmax3(a[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
+  a[0] = fmax3(a[0], __uint_as_float(s[59]), __uint_as_float(s[60]));
+  a[1] = fmax3(a[1], __uint_as_float(s[61]), __uint_as_float(s[62]));
+  return fmax3(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]), __uint_as_float(s[63]));
 }
 
 __device__ void softmax_warps(const Params &P, Shared &S, int t, int warp, int lane) {
@@ -503,7 +526,7 @@ __device__ void softmax_warps(const Params &P, Shared &S, int t, int warp, int l
   const int row_pos = row / P.group, row_head = row % P.group;
   const float c = P.scale_log2;
   const unsigned long long c2 = f2_pack(c, c);
-  uint32_t n_s = 0, n_o = 0;
+  uint32_t n_s = 0, n_o = 0, ring = 0, n_mend = 0;  // (ring, n_mend: as the loader's, an item at a time)
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
     if (!wait_warp(&S.item_full[slot], full_parity(n / kSlots), &S.abort)) return;
@@ -518,13 +541,26 @@ __device__ void softmax_warps(const Params &P, Shared &S, int t, int warp, int l
         if (!wait_warp(&S.s_full[t], full_parity(n_s), &S.abort)) return;
         ++n_s;
         tc_fence_after();
+        // the second half of the scores is on its way while the first is looked at
         uint32_t s[kKeys];
-#pragma unroll
-        for (int k = 0; k < kKeys; k += 32)
+        const auto load = [&](int k) {
           tc_ld_32x32b_x32(s_col + k, reinterpret_cast<uint32_t(&)[32]>(s[k]));
+        };
+        load(0);
+        load(32);
         tc_wait_ld();
-        const float mx = j >= I.first_masked ? row_max<true>(s, last - j * kKeys)
-                                             : row_max<false>(s, 0);
+        load(64);
+        load(96);
+        float mx;
+        if (j >= I.first_masked) {
+          mx = max_of<true>(s, last - j * kKeys, -INFINITY);
+          tc_wait_ld();
+          mx = max_of<true>(s + 64, last - j * kKeys - 64, mx);
+        } else {
+          mx = max_of<false>(s, 0, -INFINITY);
+          tc_wait_ld();
+          mx = max_of<false>(s + 64, 0, mx);
+        }
         if (j == 0) {
           m = mx;
         } else {
@@ -560,14 +596,22 @@ __device__ void softmax_warps(const Params &P, Shared &S, int t, int warp, int l
             p[i] = pack_bf16x2(x0, x1);
           }
           tc_st_32x32b_x32(s_col + 32 * hb, p);
+          if (hb == 0 && j >= I.first_masked) {
+            const uint32_t c = n_mend + (uint32_t)(j - I.first_masked);
+            if (!wait_warp(&S.v_landed[c % kMendSlots], full_parity(c / kMendSlots), &S.abort))
+              return;
+            if (drop_not_finite(S.kv[(ring + 2 * j + 1) % kStages], max(0, I.pos + 1 - j * kKeys),
+                                I.len - j * kKeys, threadIdx.x & 127))
+              *(volatile int *)&S.item[slot].bad = 1;
+          }
+          tc_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&S.p_full[t][hb]);  // half of the product may start
         }
         float a, b;
         f2_unpack(f2_add(sum[0], sum[1]), a, b);
         l += a + b;
-        tc_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&S.p_full[t]);
       }
       if (!wait_warp(&S.o_full[t], full_parity(n_o), &S.abort)) return;
       ++n_o;
@@ -576,7 +620,7 @@ __device__ void softmax_warps(const Params &P, Shared &S, int t, int warp, int l
       const float inv = 1.f / l;
       uint16_t *out = P.out + (long long)(I.start + pos) * P.out_stride +
                       (long long)(I.kvh * P.group + row_head) * kD;
-#pragma unroll
+#pragma unroll 1
       for (int k = 0; k < kD; k += 32) {
         uint32_t o[32];
         tc_ld_32x32b_x32(o_col + k, o);
@@ -605,6 +649,9 @@ __device__ void softmax_warps(const Params &P, Shared &S, int t, int warp, int l
     __syncwarp();
     if (lane == 0) mbar_arrive(&S.item_empty[slot]);
     if (!I.valid) return;
+    const int tiles = max(I.nk[0], I.nk[1]);
+    ring += 2 * tiles;
+    n_mend += tiles - min(I.first_masked, tiles);
   }
 }
 
@@ -619,7 +666,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attn_kernel(const __grid_c
     for (int i = 0; i < kStages; ++i) mbar_init(&S.kv_full[i], 1), mbar_init(&S.kv_empty[i], 1);
     for (int t = 0; t < 2; ++t) {
       mbar_init(&S.s_full[t], 1);
-      mbar_init(&S.p_full[t], 4);
+      mbar_init(&S.p_full[t][0], 4);
+      mbar_init(&S.p_full[t][1], 4);
       mbar_init(&S.o_full[t], 1);
       mbar_init(&S.o_empty[t], 4);
     }
@@ -639,14 +687,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attn_kernel(const __grid_c
   tc_fence_after();
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRegsAux));
-    if (warp == kItemWarp) {
-      item_warp(P, S, lane);
-    } else if (warp == kMendWarp) {
-      mend_warp(P, S, lane);
-    } else if (lane == 0) {
-      if (warp == kLoadWarp) load_warp(P, S);
-      else mma_warp(P, S);
-    }
+    if (warp == kItemWarp) item_warp(P, S, lane);
+    else if (warp == kMmaWarp) mma_warp(P, S, lane);
+    else if (warp == kLoadWarp && lane == 0) load_warp(P, S);
     __syncwarp();
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRegsSoftmax));
