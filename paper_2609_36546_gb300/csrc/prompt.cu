@@ -26,13 +26,12 @@
 // running maximum only has to keep the exponentials in range).
 //
 // Warps: 0-3 and 4-7 one tile each (softmax, rescale, output), 8 loads, 9
-// issues the products, 10 finds the items.
-//
-// Keys that some row of an item must not see (the diagonal, the sequence's end)
-// get P = 0, but 0 x inf and 0 x NaN would leak a broken value into rows that
-// come before it or belong to another sequence.  So the softmax warps look
-// through such a V tile before they release P, set what is not finite to 0 in
-// shared memory, and rows that do see it get it back at the end.
+// issues the products, 10 finds the items and sends the outputs off, 11 looks
+// through V tiles that hold keys which some row of the item must not see (the
+// diagonal, the sequence's end): their P is 0, but 0 x inf and 0 x NaN would
+// leak a broken value into rows that come before it or belong to another
+// sequence.  What is not finite there is set to 0 in shared memory, and rows
+// that do see it get it back at the end.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cudaTypedefs.h>
@@ -50,11 +49,11 @@ constexpr int kRows = 128;                   // rows of a query tile (M)
 constexpr int kKeys = 128;                   // keys of a K / V tile (N)
 constexpr int kTileBytes = kRows * kD * 2;   // 32 KB: a Q, K or V tile
 constexpr int kHalfBytes = kTileBytes / 2;   // its 64-dim halves, 128-byte swizzled rows
-constexpr int kStages = 5;                   // K and V tiles in flight
+constexpr int kStages = 4;                   // K and V tiles in flight (a fifth gained nothing)
 constexpr int kSlots = 3;                    // items handed from the item warp to the others
 constexpr int kMendSlots = 4;               // more than the V tiles that can be in flight
 constexpr int kThreads = 384;
-constexpr int kLoadWarp = 8, kMmaWarp = 9, kItemWarp = 10;  // (warp 11 idles)
+constexpr int kLoadWarp = 8, kMmaWarp = 9, kItemWarp = 10, kMendWarp = 11;
 constexpr uint32_t kTmemCols = 512;          // S_0, S_1, O_0, O_1 of 128 fp32 columns
 __host__ __device__ constexpr uint32_t col_s(int t) { return 128u * (uint32_t)t; }
 __host__ __device__ constexpr uint32_t col_o(int t) { return 256u + 128u * (uint32_t)t; }
@@ -65,7 +64,7 @@ static_assert(kMendSlots > (kStages + 1) / 2, "a slot is reused only after its t
 static_assert(256 * kRegsSoftmax + 128 * kRegsAux <= kThreads * kRegsLaunch,
               "the register split must fit the registers the block was launched with");
 constexpr float kRescaleLog2 = 8.0f;         // growth of the maximum that rescales O
-constexpr int kItemReaders = 8 + 2;          // softmax warps, loader, issuer
+constexpr int kItemReaders = 8 + 3;          // softmax warps, loader, issuer, mender
 
 struct Item {
   int start, len;   // the sequence's first token and length
@@ -80,8 +79,9 @@ struct Item {
 struct Shared {
   alignas(1024) uint8_t q[2][kTileBytes];
   alignas(1024) uint8_t kv[kStages][kTileBytes];
+  alignas(1024) uint8_t out[2][kHalfBytes];  // a tile's output on its way, as its 64-dim halves
   uint64_t q_full, q_empty, kv_full[kStages], kv_empty[kStages], s_full[2], p_full[2][2], o_full[2],
-      o_empty[2], v_landed[kMendSlots], item_full[kSlots], item_empty[kSlots], drain;
+      o_empty[2], out_full[2], out_free[2], v_landed[kMendSlots], item_full[kSlots], item_empty[kSlots], drain;
   Item item[kSlots];
   uint32_t tmem;
   int abort;
@@ -90,7 +90,7 @@ constexpr int kSharedBytes = (int)sizeof(Shared) + 1024;  // the base is aligned
 static_assert(kSharedBytes <= 232448, "shared memory of one CTA");
 
 struct Params {
-  CUtensorMap q, k, v;
+  CUtensorMap q, k, v, out_map;
   const uint16_t *v_ptr;
   long long v_stride, out_stride;
   uint16_t *out;
@@ -109,6 +109,19 @@ IPD_DEVINL void tma_load_3d(void *dst, const CUtensorMap *map, int x, int y, int
       " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
       "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
       : "memory");
+}
+
+// 3-D tiled TMA store, in a bulk group of the thread.
+IPD_DEVINL void tma_store_3d(const CUtensorMap *map, int x, int y, int z, const void *src) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map),
+      "r"(x), "r"(y), "r"(z), "r"(smem_u32(src))
+      : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// until the thread's bulk stores have read their shared memory
+IPD_DEVINL void tma_store_wait() {
+  asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 
 // A wait that gives up after about a second, or as soon as another warp of the
@@ -225,11 +238,43 @@ struct ItemFinder {
   }
 };
 
+// A tile whose rows all belong to the sequence leaves through shared memory.
+IPD_DEVINL bool leaves(const Params &P, const Item &I, int tile) {
+  return I.pos + (tile + 1) * P.tile_pos <= I.len;
+}
+
+// Sends the output tiles of item n off, tile 0 then tile 1.  The two share one
+// buffer, handed over once an item each way whether or not a tile leaves: every
+// phase of every barrier is then waited for, and none can be mistaken.
+IPD_DEVINL bool send_outputs(const Params &P, Shared &S, uint32_t n, int lane) {
+  const Item &I = S.item[n % kSlots];
+#pragma unroll 1
+  for (int t = 0; t < 2; ++t) {
+    if (!wait_warp(&S.out_full[t], full_parity(n), &S.abort)) return false;
+    if (lane == 0) {
+      if (leaves(P, I, t)) {
+        for (int h = 0; h < 2; ++h)
+          tma_store_3d(&P.out_map, 64 * h, I.kvh * P.group, I.start + I.pos + t * P.tile_pos,
+                       S.out[h]);
+        if (I.bad) {  // rows will be read back: until the stores are complete
+          asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+          __threadfence();
+        }
+        tma_store_wait();
+      }
+      mbar_arrive(&S.out_free[1 - t]);
+    }
+    __syncwarp();
+  }
+  return true;
+}
+
 __device__ void item_warp(const Params &P, Shared &S, int lane) {
   const int pt = 2 * P.tile_pos;
   ItemFinder F;
   F.init(P, lane, pt);
-  for (uint32_t n = 0;; ++n) {
+  uint32_t n = 0;
+  for (;; ++n) {
     const int slot = n % kSlots;
     const uint32_t use = n / kSlots;
     const long long b = (n & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
@@ -237,6 +282,8 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
     int start = 0, len = 0;
     const int tile = F.find(P, lane, pt, idx / P.hkv, &start, &len);
     const bool ok = tile >= 0;
+    // the item that had the slot before
+    if (use > 0 && !send_outputs(P, S, n - kSlots, lane)) return;
     if (!wait_warp(&S.item_empty[slot], empty_parity(use), &S.abort)) return;
     if (lane == 0) {
       Item &I = S.item[slot];
@@ -258,8 +305,11 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
       mbar_arrive(&S.item_full[slot]);
     }
     __syncwarp();
-    if (!ok) return;
+    if (!ok) break;
   }
+  // the items still out: the last kSlots - 1 before the end
+  for (uint32_t m = n > kSlots - 1 ? n - (kSlots - 1) : 0; m < n; ++m)
+    if (!send_outputs(P, S, m, lane)) return;
 }
 
 // --------------------------------------------------------------------------
@@ -288,13 +338,9 @@ __device__ void load_warp(const Params &P, Shared &S) {
       const int st = ring % kStages;
       ok = wait(&S.kv_empty[st], empty_parity(ring / kStages), &S.abort);
       if (!ok) break;
-      // a V tile with hidden keys lands at the softmax warps, whose release of P
-      // then covers it; its stage counts as filled at once
+      // a V tile with hidden keys lands at the mending warp, which then fills the stage
       uint64_t *landed = &S.kv_full[st];
-      if ((j & 1) && (j >> 1) >= I.first_masked) {
-        landed = &S.v_landed[n_mend++ % kMendSlots];
-        mbar_arrive(&S.kv_full[st]);
-      }
+      if ((j & 1) && (j >> 1) >= I.first_masked) landed = &S.v_landed[n_mend++ % kMendSlots];
       mbar_arrive_expect_tx(landed, kTileBytes);
       for (int h = 0; h < 2; ++h)
         tma_load_3d(S.kv[st] + h * kHalfBytes, (j & 1) ? &P.v : &P.k, 64 * h, I.kvh,
@@ -436,36 +482,85 @@ __device__ void mma_warp(const Params &P, Shared &S, int lane) {
 }
 
 // --------------------------------------------------------------------------
-// softmax and output of one query tile
+// V tiles with hidden keys
 // --------------------------------------------------------------------------
-// Sets the infinities and NaN of a V tile's rows row0 .. 127 to 0 (one
-// warpgroup; thread = 0 .. 127); true if one belonged to a row below row_end.
 IPD_DEVINL uint32_t not_finite2(uint32_t w) {  // bit 15 of each half: its exponent is all ones
   return ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
 }
-IPD_DEVINL bool drop_not_finite(uint8_t *tile, int row0, int row_end, int thread) {
-  bool seen = false;
+IPD_DEVINL uint32_t fma0_bf16x2(uint32_t v, uint32_t acc) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(v), "r"(0u), "r"(acc));
+  return d;
+}
+// Whether rows row0 .. 127 of a V tile hold anything that is not finite: 0 x v
+// summed is NaN then, and 0 otherwise.
+IPD_DEVINL bool any_not_finite(const uint8_t *tile, int row0, int lane) {
+  uint32_t a[4] = {0u, 0u, 0u, 0u};
 #pragma unroll 1
   for (int h = 0; h < 2; ++h) {
-    uint4 *v = reinterpret_cast<uint4 *>(tile + h * kHalfBytes);
-#pragma unroll 4
-    for (int i = thread; i < kKeys * 8; i += 128) {
-      if ((i >> 3) < row0) continue;
+    const uint4 *v = reinterpret_cast<const uint4 *>(tile + h * kHalfBytes);
+#pragma unroll 8
+    for (int i = row0 * 8 + lane; i < kKeys * 8; i += 32) {
       const uint4 w = v[i];
-      if (not_finite2(w.x) | not_finite2(w.y) | not_finite2(w.z) | not_finite2(w.w)) {
-        const auto clear = [](uint32_t x) {
-          const uint32_t bad = not_finite2(x) >> 15;
-          return x & ~(bad * 0xffffu);
-        };
-        v[i] = make_uint4(clear(w.x), clear(w.y), clear(w.z), clear(w.w));
-        seen = seen || (i >> 3) < row_end;
-      }
+      a[0] = fma0_bf16x2(w.x, a[0]);
+      a[1] = fma0_bf16x2(w.y, a[1]);
+      a[2] = fma0_bf16x2(w.z, a[2]);
+      a[3] = fma0_bf16x2(w.w, a[3]);
+    }
+  }
+  return __any_sync(0xffffffffu, ((a[0] | a[1] | a[2] | a[3]) & 0x7fff7fffu) != 0u) != 0;
+}
+// Sets them to 0; true if one belonged to a row below row_end.
+IPD_DEVINL bool drop_not_finite(uint8_t *tile, int row0, int row_end, int lane) {
+  bool seen = false;
+#pragma unroll 1
+  for (int i = lane; i < 2 * kKeys * 8; i += 32) {
+    const int r = (i >> 3) & (kKeys - 1);
+    if (r < row0) continue;
+    uint4 *v = reinterpret_cast<uint4 *>(tile) + i;
+    const uint4 w = *v;
+    if (not_finite2(w.x) | not_finite2(w.y) | not_finite2(w.z) | not_finite2(w.w)) {
+      const auto clear = [](uint32_t x) {
+        const uint32_t bad = not_finite2(x) >> 15;
+        return x & ~(bad * 0xffffu);
+      };
+      *v = make_uint4(clear(w.x), clear(w.y), clear(w.z), clear(w.w));
+      seen = seen || r < row_end;
     }
   }
   fence_proxy_async_smem();
-  return seen;
+  return __any_sync(0xffffffffu, seen) != 0;
 }
 
+__device__ void mend_warp(const Params &P, Shared &S, int lane) {
+  uint32_t ring = 0, n_mend = 0;
+  for (uint32_t n = 0;; ++n) {
+    const int slot = n % kSlots;
+    if (!wait_warp(&S.item_full[slot], full_parity(n / kSlots), &S.abort)) return;
+    const Item I = S.item[slot];
+    const int nk = I.valid ? max(I.nk[0], I.nk[1]) : 0;
+    for (int j = I.valid ? min(I.first_masked, nk) : 0; j < nk; ++j, ++n_mend) {
+      if (!wait_warp(&S.v_landed[n_mend % kMendSlots], full_parity(n_mend / kMendSlots), &S.abort))
+        return;
+      const int st = (ring + 2 * j + 1) % kStages;  // V tile j's stage
+      const int row0 = max(0, I.pos + 1 - j * kKeys);
+      if (any_not_finite(S.kv[st], row0, lane)) {
+        const bool seen = drop_not_finite(S.kv[st], row0, I.len - j * kKeys, lane);
+        if (seen && lane == 0) S.item[slot].bad = 1;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&S.kv_full[st]);
+    }
+    ring += 2 * nk;
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&S.item_empty[slot]);
+    if (!I.valid) return;
+  }
+}
+
+// --------------------------------------------------------------------------
+// softmax and output of one query tile
+// --------------------------------------------------------------------------
 // O's row in TMEM times f (all warps of the tile, 128 columns).
 IPD_DEVINL void scale_o(uint32_t o, float f) {
 #pragma unroll 1
@@ -526,11 +621,13 @@ __device__ void softmax_warps(const Params &P, Shared &S, int t, int warp, int l
   const int row_pos = row / P.group, row_head = row % P.group;
   const float c = P.scale_log2;
   const unsigned long long c2 = f2_pack(c, c);
-  uint32_t n_s = 0, n_o = 0, ring = 0, n_mend = 0;  // (ring, n_mend: as the loader's, an item at a time)
+  uint32_t n_s = 0, n_o = 0;
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
     if (!wait_warp(&S.item_full[slot], full_parity(n / kSlots), &S.abort)) return;
-    const Item I = S.item[slot];
+    const Item &I = S.item[slot];  // (there until this warp's release)
+    // tile 0 has the output buffer first, and again when tile 1's has left
+    const uint32_t free_parity = t == 0 ? empty_parity(n) : full_parity(n);
     const int nk = I.valid ? I.nk[t] : 0;
     if (nk > 0) {
       const int pos = I.pos + t * P.tile_pos + row_pos;
@@ -596,14 +693,6 @@ __device__ void softmax_warps(const Params &P, Shared &S, int t, int warp, int l
             p[i] = pack_bf16x2(x0, x1);
           }
           tc_st_32x32b_x32(s_col + 32 * hb, p);
-          if (hb == 0 && j >= I.first_masked) {
-            const uint32_t c = n_mend + (uint32_t)(j - I.first_masked);
-            if (!wait_warp(&S.v_landed[c % kMendSlots], full_parity(c / kMendSlots), &S.abort))
-              return;
-            if (drop_not_finite(S.kv[(ring + 2 * j + 1) % kStages], max(0, I.pos + 1 - j * kKeys),
-                                I.len - j * kKeys, threadIdx.x & 127))
-              *(volatile int *)&S.item[slot].bad = 1;
-          }
           tc_wait_st();
           tc_fence_before();
           __syncwarp();
@@ -620,38 +709,53 @@ __device__ void softmax_warps(const Params &P, Shared &S, int t, int warp, int l
       const float inv = 1.f / l;
       uint16_t *out = P.out + (long long)(I.start + pos) * P.out_stride +
                       (long long)(I.kvh * P.group + row_head) * kD;
-#pragma unroll 1
-      for (int k = 0; k < kD; k += 32) {
-        uint32_t o[32];
-        tc_ld_32x32b_x32(o_col + k, o);
+      uint32_t w[64];
+#pragma unroll
+      for (int k = 0; k < 4; k += 2) {
+        uint32_t o[64];
+        tc_ld_32x32b_x32(o_col + 32 * k, reinterpret_cast<uint32_t(&)[32]>(o[0]));
+        tc_ld_32x32b_x32(o_col + 32 * k + 32, reinterpret_cast<uint32_t(&)[32]>(o[32]));
         tc_wait_ld();
-        if (k + 32 == kD) {  // O_t is read: the next item may write it
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&S.o_empty[t]);
-        }
-        if (live) {
-          uint32_t w[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            w[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+        for (int i = 0; i < 32; ++i)
+          w[16 * k + i] =
+              pack_bf16x2(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&S.o_empty[t]);  // O_t is read: the next item may write it
+      if (leaves(P, I, t)) {
+        // through shared memory and TMA (16-byte stores of 32 rows each would
+        // hold up the SM's other warps)
+        if (!wait_warp(&S.out_free[t], free_parity, &S.abort)) return;
 #pragma unroll
-          for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<uint4 *>(out + k + 2 * i) =
-                make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
-        }
+        for (int i = 0; i < 16; ++i)
+          *reinterpret_cast<uint4 *>(S.out[i >> 3] + row * 128 + (((i & 7) ^ (row & 7)) << 4)) =
+              make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&S.out_full[t]);
+        // (the buffer's next hand-over follows the store)
+        if (bad && !wait_warp(&S.out_free[1 - t], full_parity(n), &S.abort)) return;
+      } else if (live) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          *reinterpret_cast<uint4 *>(out + 8 * i) =
+              make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
       }
       if (bad && live) add_not_finite(P, I, pos, out);
       if (live && P.lse)
         P.lse[(long long)(I.kvh * P.group + row_head) * P.total + I.start + pos] =
             (m == -INFINITY ? -INFINITY : (m * c + log2f(l)) * kLn2);
     }
+    const bool last_item = !I.valid;
+    if (!last_item && !leaves(P, I, t)) {  // the buffer passes by
+      if (!wait_warp(&S.out_free[t], free_parity, &S.abort)) return;
+      if (lane == 0) mbar_arrive(&S.out_full[t]);
+    }
     __syncwarp();
     if (lane == 0) mbar_arrive(&S.item_empty[slot]);
-    if (!I.valid) return;
-    const int tiles = max(I.nk[0], I.nk[1]);
-    ring += 2 * tiles;
-    n_mend += tiles - min(I.first_masked, tiles);
+    if (last_item) return;
   }
 }
 
@@ -660,6 +764,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attn_kernel(const __grid_c
   Shared &S = *reinterpret_cast<Shared *>(
       smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 32 * kLoadWarp) {
+    for (const CUtensorMap *m : {&P.q, &P.k, &P.v, &P.out_map})
+      asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+  }
   if (threadIdx.x == 0) {
     mbar_init(&S.q_full, 1);
     mbar_init(&S.q_empty, 1);
@@ -670,6 +778,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attn_kernel(const __grid_c
       mbar_init(&S.p_full[t][1], 4);
       mbar_init(&S.o_full[t], 1);
       mbar_init(&S.o_empty[t], 4);
+      mbar_init(&S.out_full[t], 4);
+      mbar_init(&S.out_free[t], 1);
     }
     for (int i = 0; i < kMendSlots; ++i) mbar_init(&S.v_landed[i], 1);
     mbar_init(&S.drain, 1);
@@ -689,7 +799,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_attn_kernel(const __grid_c
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRegsAux));
     if (warp == kItemWarp) item_warp(P, S, lane);
     else if (warp == kMmaWarp) mma_warp(P, S, lane);
-    else if (warp == kLoadWarp && lane == 0) load_warp(P, S);
+    else if (warp == kMendWarp) mend_warp(P, S, lane);
+    else if (lane == 0) load_warp(P, S);
     __syncwarp();
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRegsSoftmax));
@@ -777,7 +888,7 @@ extern "C" int ipd_prompt_attn(const ipd_prompt_args *args, ipd_stream_t stream)
                           (uintptr_t)(2 * a.v_stride) | (uintptr_t)(2 * a.out_stride);
   if (align & 15) return IPD_ERR_INVALID_ARG;
   // the tensor maps hold strides below 2^40 bytes
-  if ((a.q_stride | a.k_stride | a.v_stride) >> 38) return IPD_ERR_UNSUPPORTED;
+  if ((a.q_stride | a.k_stride | a.v_stride | a.out_stride) >> 38) return IPD_ERR_UNSUPPORTED;
   int sms = 0;
   int st = prepare_device(&sms);
   if (st != IPD_OK) return st;
@@ -786,7 +897,8 @@ extern "C" int ipd_prompt_attn(const ipd_prompt_args *args, ipd_stream_t stream)
   P.tile_pos = kRows / group;
   if (encode(&P.q, a.q, a.num_q_heads, a.total, a.q_stride, group, P.tile_pos) != IPD_OK ||
       encode(&P.k, a.k, a.num_kv_heads, a.total, a.k_stride, 1, kKeys) != IPD_OK ||
-      encode(&P.v, a.v, a.num_kv_heads, a.total, a.v_stride, 1, kKeys) != IPD_OK)
+      encode(&P.v, a.v, a.num_kv_heads, a.total, a.v_stride, 1, kKeys) != IPD_OK ||
+      encode(&P.out_map, a.out, a.num_q_heads, a.total, a.out_stride, group, P.tile_pos) != IPD_OK)
     return IPD_ERR_CUDA;
   P.v_ptr = a.v;
   P.v_stride = a.v_stride;
