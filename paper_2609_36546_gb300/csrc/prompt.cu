@@ -59,7 +59,7 @@ __host__ __device__ constexpr uint32_t col_s(int t) { return 128u * (uint32_t)t;
 __host__ __device__ constexpr uint32_t col_o(int t) { return 256u + 128u * (uint32_t)t; }
 // Registers: launched with 168 a thread; the third warpgroup gives back what
 // the softmax warpgroups need to hold a row's 128 scores.
-constexpr int kRegsLaunch = 168, kRegsAux = 56, kRegsSoftmax = 224;
+constexpr int kRegsLaunch = 168, kRegsAux = 104, kRegsSoftmax = 200;
 static_assert(kMendSlots > (kStages + 1) / 2, "a slot is reused only after its tile was consumed");
 static_assert(256 * kRegsSoftmax + 128 * kRegsAux <= kThreads * kRegsLaunch,
               "the register split must fit the registers the block was launched with");
@@ -416,64 +416,101 @@ __device__ void mma_warp(const Params &P, Shared &S, int lane) {
     if (elect_one()) tc_commit(bar);
     __syncwarp();
   };
-  bool ok = true;
-  for (uint32_t n = 0; ok; ++n) {
+  // The products run on from item to item: where a tile's last O product is
+  // issued, the first scores of its next item follow.
+  uint32_t n = 0;              // items taken
+  int nk0 = 0, nk1 = 0;        // this item's tiles
+  int next0 = 0, next1 = 0;    // the next one's (none: 0, 0)
+  const auto take = [&]() {
     const int slot = n % kSlots;
-    if (!(ok = wait_warp(&S.item_full[slot], full_parity(n / kSlots), &S.abort))) break;
-    const int valid = uniform(S.item[slot].valid);
-    const int nk0 = uniform(S.item[slot].nk[0]), nk1 = uniform(S.item[slot].nk[1]);
+    if (!wait_warp(&S.item_full[slot], full_parity(n / kSlots), &S.abort)) return false;
+    const Item &I = S.item[slot];
+    const int valid = uniform(I.valid), a = uniform(I.nk[0]), b = uniform(I.nk[1]);
+    next0 = valid ? a : 0;
+    next1 = valid ? b : 0;
     __syncwarp();
     if (lane == 0) mbar_arrive(&S.item_empty[slot]);
-    if (!valid) break;
-    const int nk = max(nk0, nk1);
-    if (!(ok = wait_warp(&S.q_full, full_parity(n), &S.abort))) break;
-    int ks = ring % kStages;  // stage of K tile j, then of K tile j + 1
-    if (!(ok = wait_warp(&S.kv_full[ks], full_parity(ring / kStages), &S.abort))) break;
-    tc_fence_after();
+    ++n;
+    return true;
+  };
+  // O_t += P_t V_j
+  const auto add_o = [&](int t, int stage, int j) {
+    if (j == 0) {  // O_t of the item before has been read
+      if (!wait_warp(&S.o_empty[t], empty_parity(n_o[t]), &S.abort)) return false;
+      ++n_o[t];
+    }
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-      if ((t ? nk1 : nk0) > 0) issue_s(t, ks);
-    commit(&S.kv_empty[ks]);
-    if (nk == 1) commit(&S.q_empty);
-    ++ring;
+    for (int half = 0; half < 2; ++half) {
+      if (!wait_warp(&S.p_full[t][half], full_parity(n_p[t]), &S.abort)) return false;
+      tc_fence_after();
+      issue_o(t, stage, half, j + half > 0);
+    }
+    ++n_p[t];
+    return true;
+  };
+  bool ok = take();
+  int j = -1;
+  while (ok) {
+    // all but the item's last K tile: S_t's columns hold P_t until the products
+    // before have read them; the tensor core takes this thread's instructions
+    // in order
+    const int nk = max(nk0, nk1);
 #pragma unroll 1
-    for (int j = 0; j < nk && ok; ++j) {
-      const int vs = ring % kStages;
+    for (; j >= 0 && j + 1 < nk; ++j) {
+      const int vs = ring % kStages, ks = (ring + 1) % kStages;
       if (!(ok = wait_warp(&S.kv_full[vs], full_parity(ring / kStages), &S.abort))) break;
       ++ring;
-      const bool more = j + 1 < nk;
-      if (more) {
-        ks = ring % kStages;
-        if (!(ok = wait_warp(&S.kv_full[ks], full_parity(ring / kStages), &S.abort))) break;
-        ++ring;
-      }
+      if (!(ok = wait_warp(&S.kv_full[ks], full_parity(ring / kStages), &S.abort))) break;
+      ++ring;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int mine = t ? nk1 : nk0;
         if (j >= mine) continue;
-        if (j == 0) {  // O_t of the item before has been read
-          if (!(ok = wait_warp(&S.o_empty[t], empty_parity(n_o[t]), &S.abort))) break;
-          ++n_o[t];
-        }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          ok = wait_warp(&S.p_full[t][half], full_parity(n_p[t]), &S.abort);
-          if (!ok) break;
-          tc_fence_after();
-          issue_o(t, vs, half, j + half > 0);
-        }
-        if (!ok) break;
-        ++n_p[t];
-        // S_t's columns hold P_t until the products above have read them; the
-        // tensor core takes this thread's instructions in order
+        if (!(ok = add_o(t, vs, j))) break;
         if (j + 1 < mine) issue_s(t, ks);
         else commit(&S.o_full[t]);
       }
       if (!ok) break;
       commit(&S.kv_empty[vs]);
-      if (more) commit(&S.kv_empty[ks]);
-      if (j + 2 == nk) commit(&S.q_empty);  // the last K tile's products are issued
+      commit(&S.kv_empty[ks]);
+      if (j + 2 == nk) commit(&S.q_empty);  // the item's last scores are issued
     }
+    if (!ok) break;
+    // the last one, and the next item's first scores
+    int vs = 0;
+    if (j >= 0) {
+      vs = ring % kStages;
+      if (!(ok = wait_warp(&S.kv_full[vs], full_parity(ring / kStages), &S.abort))) break;
+      ++ring;
+      if (!(ok = take())) break;
+    }
+    const int ks = ring % kStages;
+    bool waited = false;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (j >= 0 && j + 1 == (t ? nk1 : nk0)) {
+        if (!(ok = add_o(t, vs, j))) break;
+        commit(&S.o_full[t]);
+      }
+      if ((t ? next1 : next0) > 0) {
+        if (!waited) {
+          ok = wait_warp(&S.q_full, full_parity(n - 1), &S.abort) &&
+               wait_warp(&S.kv_full[ks], full_parity(ring / kStages), &S.abort);
+          if (!ok) break;
+          tc_fence_after();
+          waited = true;
+        }
+        issue_s(t, ks);
+      }
+    }
+    if (!ok) break;
+    if (j >= 0) commit(&S.kv_empty[vs]);
+    if (next0 == 0) break;  // (a tile 1 without a tile 0 does not occur)
+    commit(&S.kv_empty[ks]);
+    ++ring;
+    nk0 = next0, nk1 = next1;
+    j = 0;
+    if (max(nk0, nk1) == 1) commit(&S.q_empty);
   }
   if (!ok) {  // the CTA gives up: products in flight end before TMEM is freed
     commit(&S.drain);
