@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -126,6 +127,15 @@ class _PromptArgs(ctypes.Structure):
                                        "total", "max_len")] + [("softmax_scale", ctypes.c_float)]
 
 
+# The same three layouts as packed bytes: filling a ctypes structure field by
+# field takes longer than the smallest of these calls runs.
+_PACK_ROPE = struct.Struct("2P2q2P8i")
+_PACK_ROPE_APPEND = struct.Struct("5P5q2Pq4P10i")
+_PACK_PROMPT = struct.Struct("6P4q6if0P")
+for _s, _c in ((_PACK_ROPE, _RopeArgs), (_PACK_ROPE_APPEND, _RopeAppendDesc),
+               (_PACK_PROMPT, _PromptArgs)):
+    assert _s.size == ctypes.sizeof(_c), _c.__name__
+
 _lib.ipd_attn_workspace_size.restype = c_sz
 _lib.ipd_attn_workspace_size.argtypes = [ctypes.POINTER(_AttnBatch), c_i,
                                          ctypes.POINTER(_AttnBatch), c_i]
@@ -171,11 +181,11 @@ _lib.ipd_kv_append_many.argtypes = [ctypes.POINTER(_KvAppendDesc), c_i, c_p]
 _lib.ipd_rope_table.restype = c_i
 _lib.ipd_rope_table.argtypes = [c_p, c_i, c_i, ctypes.POINTER(_RopeScaling), c_p]
 _lib.ipd_rope.restype = c_i
-_lib.ipd_rope.argtypes = [ctypes.POINTER(_RopeArgs), c_p]
+_lib.ipd_rope.argtypes = [c_p, c_p]  # (a packed _RopeArgs, as bytes)
 _lib.ipd_rope_append.restype = c_i
-_lib.ipd_rope_append.argtypes = [ctypes.POINTER(_RopeAppendDesc), c_p]
+_lib.ipd_rope_append.argtypes = [c_p, c_p]  # (a packed _RopeAppendDesc)
 _lib.ipd_prompt_attn.restype = c_i
-_lib.ipd_prompt_attn.argtypes = [ctypes.POINTER(_PromptArgs), c_p]
+_lib.ipd_prompt_attn.argtypes = [c_p, c_p]  # (a packed _PromptArgs)
 _lib.ipd_sample_trunc.restype = c_i
 _lib.ipd_sample_trunc.argtypes = [c_p, ctypes.c_int64, c_i, c_i] + [c_p] * 9
 _lib.ipd_set_attn_kernel_timing.restype = c_i
@@ -199,9 +209,23 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+# the raw handle of the current stream, without the objects around it (a few
+# microseconds a call; the small operators run for as little)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_on_gpu = False  # set once a device has been seen
+
+
 def _stream(stream) -> Optional[int]:
+    global _on_gpu
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
+        if not _on_gpu:
+            if not torch.cuda.is_available():
+                return None
+            torch.cuda.current_stream()  # initialises CUDA in this process
+            _on_gpu = True
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
+        return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -216,8 +240,16 @@ class KVCache:
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor):
         assert k_pages.shape == v_pages.shape and k_pages.dim() == 4
         self.k_pages, self.v_pages = k_pages, v_pages
-        self.c = _KVCache(_ptr(k_pages), _ptr(v_pages), k_pages.shape[0], k_pages.shape[2],
-                          k_pages.shape[1], k_pages.shape[3])
+        self._c = None
+
+    @property
+    def c(self) -> _KVCache:
+        """The C descriptor (made when first asked for)."""
+        if self._c is None:
+            k = self.k_pages
+            self._c = _KVCache(_ptr(k), _ptr(self.v_pages), k.shape[0], k.shape[2], k.shape[1],
+                               k.shape[3])
+        return self._c
 
     @property
     def num_kv_heads(self) -> int:
@@ -454,19 +486,23 @@ def _refuse(what: str):
     raise IpdError(STATUS_CODES["IPD_ERR_INVALID_ARG"], what)
 
 
-def _rows(t: torch.Tensor, dtype, what: str) -> int:
+def _rows(t: torch.Tensor, shape, dtype, what: str) -> int:
     """Token stride of a [n, heads, head_dim] tensor whose rows are contiguous."""
-    n, h, d = t.shape
+    if t.shape != shape or t.dtype is not dtype:
+        _refuse(what)
+    n, h, d = shape
     s0, s1, s2 = t.stride()
-    if t.dtype != dtype or (d > 1 and s2 != 1) or (h > 1 and s1 != d):
+    if (d > 1 and s2 != 1) or (h > 1 and s1 != d):
         _refuse(what)
     return s0 if n > 1 else h * d
 
 
 def _check_table(table: torch.Tensor, what: str):
-    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or \
-            not table.is_contiguous():
+    """(positions, rotated entries) of a rotary table."""
+    s = table.shape
+    if table.dtype is not torch.float32 or len(s) != 3 or s[2] != 2 or not table.is_contiguous():
         _refuse(what)
+    return s[0], 2 * s[1]
 
 
 def rope_table(table: torch.Tensor, base: float = 1e6, scaling: str = "none", factor: float = 1.0,
@@ -487,16 +523,17 @@ def rope(x: torch.Tensor, out: torch.Tensor, pos: torch.Tensor, table: torch.Ten
     """Rotates the heads of ``x`` ([n, H, D] bf16 or fp32, rows contiguous) by
     their positions ``pos`` (int32 [n]) into ``out`` (may be ``x``); ``inverse``
     applies the transpose, the rotation's gradient."""
-    _check_table(table, "ipd_rope: table")
-    if x.shape != out.shape or pos.dtype != torch.int32 or pos.numel() != x.shape[0] or \
-            not pos.is_contiguous() or x.dtype not in (torch.float32, torch.bfloat16):
+    max_pos, rot = _check_table(table, "ipd_rope: table")
+    shape, dt = x.shape, x.dtype
+    if len(shape) != 3 or dt not in (torch.float32, torch.bfloat16) or \
+            pos.dtype is not torch.int32 or pos.shape != shape[:1] or not pos.is_contiguous():
         _refuse("ipd_rope: shapes or types")
-    n, h, d = x.shape
-    a = _RopeArgs(x.data_ptr(), out.data_ptr(), _rows(x, x.dtype, "ipd_rope: x"),
-                  _rows(out, x.dtype, "ipd_rope: out"), pos.data_ptr(), table.data_ptr(),
-                  DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_F32, n, h, d, table.shape[0],
-                  2 * table.shape[1], layout, 1 if inverse else 0)
-    _check(_lib.ipd_rope(ctypes.byref(a), _stream(stream)), "ipd_rope")
+    n, h, d = shape
+    a = _PACK_ROPE.pack(x.data_ptr(), out.data_ptr(), _rows(x, shape, dt, "ipd_rope: x"),
+                        _rows(out, shape, dt, "ipd_rope: out"), pos.data_ptr(), table.data_ptr(),
+                        DTYPE_BF16 if dt is torch.bfloat16 else DTYPE_F32, n, h, d, max_pos, rot,
+                        layout, 1 if inverse else 0)
+    _check(_lib.ipd_rope(a, _stream(stream)), "ipd_rope")
 
 
 def rope_append(cache: "KVCache", q: Optional[torch.Tensor], q_out: Optional[torch.Tensor],
@@ -506,25 +543,30 @@ def rope_append(cache: "KVCache", q: Optional[torch.Tensor], q_out: Optional[tor
     ``q_out`` and their keys ([n, Hkv, 128]) into the cache's pages (and
     ``k_out``), and writes their values beside them: kv_append of the rotated
     rows in one launch.  Each row's position is its place in its sequence."""
-    _check_table(table, "ipd_rope_append: table")
-    bf = torch.bfloat16
-    hkv = cache.num_kv_heads
-    n = k_new.shape[0]
-    if k_new.shape != (n, hkv, 128) or v_new.shape != k_new.shape or \
-            (k_out is not None and k_out.shape != k_new.shape) or (q is None) != (q_out is None) or \
-            (q is not None and (q.shape != q_out.shape or q.shape[0] != n or q.shape[2] != 128)):
+    max_pos, rot = _check_table(table, "ipd_rope_append: table")
+    bf, kp, kshape = torch.bfloat16, cache.k_pages, k_new.shape
+    pages, hkv, ps, hd = kp.shape
+    n, hq = kshape[0], 0
+    q_ptr = qo_ptr = ko_ptr = qs = qos = kos = 0
+    if len(kshape) != 3 or kshape[1] != hkv or kshape[2] != 128 or (q is None) != (q_out is None):
         _refuse("ipd_rope_append: shapes")
-    a = _RopeAppendDesc(
-        _ptr(q), k_new.data_ptr(), v_new.data_ptr(), _ptr(q_out), _ptr(k_out),
-        0 if q is None else _rows(q, bf, "ipd_rope_append: q"),
-        _rows(k_new, bf, "ipd_rope_append: k_new"), _rows(v_new, bf, "ipd_rope_append: v_new"),
-        0 if q is None else _rows(q_out, bf, "ipd_rope_append: q_out"),
-        0 if k_out is None else _rows(k_out, bf, "ipd_rope_append: k_out"),
-        cache.k_pages.data_ptr(), cache.v_pages.data_ptr(), cache.k_pages.shape[0],
-        cu_new.data_ptr(), seq_len.data_ptr(), page_table.data_ptr(), table.data_ptr(),
-        0 if q is None else q.shape[1], hkv, cache.k_pages.shape[2], cache.k_pages.shape[3],
-        page_table.shape[1], cu_new.numel() - 1, n, table.shape[0], 2 * table.shape[1], layout)
-    _check(_lib.ipd_rope_append(ctypes.byref(a), _stream(stream)), "ipd_rope_append")
+    if q is not None:
+        qshape = q.shape
+        if len(qshape) != 3 or qshape[0] != n or qshape[2] != 128:
+            _refuse("ipd_rope_append: q")
+        hq = qshape[1]
+        q_ptr, qs = q.data_ptr(), _rows(q, qshape, bf, "ipd_rope_append: q")
+        qo_ptr, qos = q_out.data_ptr(), _rows(q_out, qshape, bf, "ipd_rope_append: q_out")
+    if k_out is not None:
+        ko_ptr, kos = k_out.data_ptr(), _rows(k_out, kshape, bf, "ipd_rope_append: k_out")
+    a = _PACK_ROPE_APPEND.pack(
+        q_ptr, k_new.data_ptr(), v_new.data_ptr(), qo_ptr, ko_ptr, qs,
+        _rows(k_new, kshape, bf, "ipd_rope_append: k_new"),
+        _rows(v_new, kshape, bf, "ipd_rope_append: v_new"), qos, kos, kp.data_ptr(),
+        cache.v_pages.data_ptr(), pages, cu_new.data_ptr(), seq_len.data_ptr(),
+        page_table.data_ptr(), table.data_ptr(), hq, hkv, ps, hd, page_table.shape[1],
+        cu_new.shape[0] - 1, n, max_pos, rot, layout)
+    _check(_lib.ipd_rope_append(a, _stream(stream)), "ipd_rope_append")
 
 
 def prompt_attn(q, k, v, cu_seq, max_len: int, out, softmax_scale: float,
@@ -533,19 +575,22 @@ def prompt_attn(q, k, v, cu_seq, max_len: int, out, softmax_scale: float,
     [total, Hkv, 128], out [total, Hq, 128] bf16 (rows contiguous, any row
     stride), cu_seq int32 [num_seqs + 1] (device), ``max_len`` a host-known
     bound on the lengths; lse fp32 [Hq, total] when given."""
-    n, hq, d = q.shape
-    if k.shape != v.shape or k.shape[0] != n or k.shape[2] != d or out.shape != q.shape or \
-            cu_seq.dtype != torch.int32 or not cu_seq.is_contiguous() or \
-            (lse is not None and (lse.shape != (hq, n) or lse.dtype != torch.float32 or
-                                  not lse.is_contiguous())):
+    shape, kshape, bf = q.shape, k.shape, torch.bfloat16
+    if len(shape) != 3 or len(kshape) != 3 or kshape[0] != shape[0] or kshape[2] != shape[2] or \
+            cu_seq.dtype is not torch.int32 or not cu_seq.is_contiguous():
         _refuse("ipd_prompt_attn: shapes or types")
-    bf = torch.bfloat16
-    a = _PromptArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _ptr(lse),
-                    cu_seq.data_ptr(), _rows(q, bf, "ipd_prompt_attn: q"),
-                    _rows(k, bf, "ipd_prompt_attn: k"), _rows(v, bf, "ipd_prompt_attn: v"),
-                    _rows(out, bf, "ipd_prompt_attn: out"), hq, k.shape[1], d,
-                    cu_seq.numel() - 1, n, max_len, softmax_scale)
-    _check(_lib.ipd_prompt_attn(ctypes.byref(a), _stream(stream)), "ipd_prompt_attn")
+    n, hq, d = shape
+    if lse is not None and (lse.shape != (hq, n) or lse.dtype is not torch.float32 or
+                            not lse.is_contiguous()):
+        _refuse("ipd_prompt_attn: lse")
+    a = _PACK_PROMPT.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(),
+                          0 if lse is None else lse.data_ptr(), cu_seq.data_ptr(),
+                          _rows(q, shape, bf, "ipd_prompt_attn: q"),
+                          _rows(k, kshape, bf, "ipd_prompt_attn: k"),
+                          _rows(v, kshape, bf, "ipd_prompt_attn: v"),
+                          _rows(out, shape, bf, "ipd_prompt_attn: out"), hq, kshape[1], d,
+                          cu_seq.shape[0] - 1, n, max_len, softmax_scale)
+    _check(_lib.ipd_prompt_attn(a, _stream(stream)), "ipd_prompt_attn")
 
 
 def sample_trunc(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor,
@@ -558,15 +603,17 @@ def sample_trunc(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor,
     (fp32 [n]) after the rows' own settings (fp32 [n]; ``top_k`` int32 [n]);
     ``logp`` (fp32) and ``n_kept`` (int32) take the log-probability of the token
     among the kept entries and their number."""
-    n, V = logits.shape
+    n, V = shape = logits.shape
+    one = shape[:1]
     f, i = torch.float32, torch.int32
     for t, dt in ((u, f), (tokens, i), (inv_temperature, f), (top_k, i), (top_p, f), (min_p, f),
                   (logp, f), (n_kept, i)):
-        if t is not None and (t.dtype != dt or t.numel() != n or not t.is_contiguous()):
+        if t is not None and (t.shape != one or t.dtype is not dt or not t.is_contiguous()):
             _refuse("ipd_sample_trunc: per-row tensors")
-    if logits.dtype != torch.bfloat16 or (V > 1 and logits.stride(1) != 1):
+    row, col = logits.stride()
+    if logits.dtype is not torch.bfloat16 or (V > 1 and col != 1):
         _refuse("ipd_sample_trunc: logits")
-    _check(_lib.ipd_sample_trunc(logits.data_ptr(), logits.stride(0) if n > 1 else V, n, V,
+    _check(_lib.ipd_sample_trunc(logits.data_ptr(), row if n > 1 else V, n, V,
                                  u.data_ptr(), _ptr(inv_temperature), _ptr(top_k), _ptr(top_p),
                                  _ptr(min_p), tokens.data_ptr(), _ptr(logp), _ptr(n_kept),
                                  _stream(stream)), "ipd_sample_trunc")
