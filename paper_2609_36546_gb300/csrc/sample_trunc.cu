@@ -52,8 +52,7 @@ constexpr int kBatch = 4;               // 16-byte vectors in flight a thread
 constexpr uint32_t kLowBits = 0x3800;   // bf16 bits of 2^-15
 constexpr int kSide = 31 * 128;         // bins of a sign; up to the bits of 2^16
 constexpr int kMid = kBins - 2 * kSide;  // bins between the signs
-constexpr int kBlocks = 1024 / kWarps;  // parts of a warp's share in the last look, 32 vectors each
-static_assert((IPD_TRUNC_MAX_VOCAB + 14) / 8 <= kWarps * kBlocks * 32, "a row fits the last look");
+constexpr int kRound = 8;               // see look_up
 constexpr float kMagic = 12582912.f;    // 1.5 * 2^23: x + kMagic rounds x to a whole number
 
 typedef unsigned long long u64;
@@ -91,8 +90,7 @@ struct Shared {
   uint32_t scan_n[kWarps];
   u64 found_before, word;
   uint32_t win_thread, found_key, found_weight, found_n, found_count;
-  uint16_t block[kWarps * kBlocks];  // entries of the drawn value in each block
-  uint32_t block_at, block_rank;
+  uint16_t block[2][kWarps * kRound];  // entries of the drawn value in each block of a round
 };
 
 // ---- cluster ---------------------------------------------------------------
@@ -228,15 +226,17 @@ IPD_DEVINL Scale make_scale(float c, float min_p, uint32_t top_key) {
   C.inf = top_key == kKeyInf;
   C.top = key_value(top_key);
   C.min_w = weight_floor(min_p);
-  // entries below top - 33 / c have x < -32 and so weight 0; as a bf16 value,
-  // rounded down (-inf where no finite one is as low)
-  const float least = C.top - 33.f / C.c;
+  // entries from 33 - log2(min_w) binades of weight below the top on have none (x
+  // < log2(min_w) - 32); as a bf16 value, rounded down (-inf where no finite one
+  // is as low)
+  const float bits = log2f((float)C.min_w);
+  const float least = C.top - (33.f - bits) / C.c;
   const uint32_t b = __float_as_uint(least);
   const uint32_t up = (b >> 31) && (b & 0xffffu) ? 1u : 0u;  // away from 0 is down
   uint32_t h = (b >> 16) + up;
   if ((h & 0x7fffu) >= 0x7f80u) h = 0xff80u;
-  // (top so large that 33 / c is lost in it: its bf16 neighbour is far below)
-  if (exponent(C, bf16f((uint16_t)h)) > -32.f) h += (h & 0x8000u) ? 1u : 0xffffffffu;
+  // (top so large that the distance is lost in it: its bf16 neighbour is far below)
+  if (exponent(C, bf16f((uint16_t)h)) > bits - 32.f) h += (h & 0x8000u) ? 1u : 0xffffffffu;
   C.least2 = h | h << 16;
   C.coarse = !(exponent(C, bf16f((uint16_t)h)) > -100.f);
   return C;
@@ -275,9 +275,10 @@ struct Row {
   const uint16_t *base;
   int shift, end;  // entries shift .. end - 1 of base are the row's
   IPD_DEVINL bool has(int i) const { return i >= shift && i < end; }
+  IPD_DEVINL bool cut(int v) const { return 8 * v < shift || 8 * v + 8 > end; }
   // vector v if it is the row's as a whole and below last, else -inf
   IPD_DEVINL uint4 load(int v, int last) const {
-    if (v < last && 8 * v >= shift && 8 * v + 8 <= end)
+    if (v < last && !cut(v))
       return __ldg(reinterpret_cast<const uint4 *>(base + 8ll * v));
     return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
   }
@@ -287,20 +288,25 @@ struct Row {
   IPD_DEVINL int edge_entry(int i, int first, int last) const {
     const int v = i < 8 ? 0 : end / 8, e = 8 * v + (i & 7);
     if (i >= 16 || v < first || v >= last || !has(e)) return -1;
-    if (8 * v >= shift && 8 * v + 8 <= end) return -1;
+    if (!cut(v)) return -1;
     if (i >= 8 && v == 0) return -1;  // the same vector
     return e;
   }
 };
 
 // ---- bins --------------------------------------------------------------------
+constexpr int kFreeWord = (kLowBits + kSide) & (kBins / 2 - 1);  // of each half, to the next value's
+static_assert(kBins / 2 - kSide == kMid / 2 && (kLowBits & (kBins / 2 - 1)) == kFreeWord + kMid / 2, "");
 // The bins in the order of falling values, p = 0 .. kBins - 1, of a row's one
 // histogram (window < 0) or of a window of keys.
 IPD_DEVINL int word_at(int window, int p) {
   if (window >= 0) return kBins - 1 - p;
-  if (p < kSide) return kSide - 1 - p;
-  if (p >= kSide + kMid) return p - kMid + (kBins / 2 - kSide);
-  return p < kBins / 2 ? p : p + kSide;  // what the signs leave of each half
+  // a value's word: its sign, and the low 12 of its other bits (3,968 values in a
+  // row differ in those); the bins between the signs take the 128 words that
+  // this leaves of each half
+  if (p < kSide) return (int)(kLowBits + kSide - 1 - p) & (kBins / 2 - 1);
+  if (p >= kSide + kMid) return kBins / 2 + ((int)(kLowBits + p - kSide - kMid) & (kBins / 2 - 1));
+  return (kFreeWord + ((p - kSide) & (kMid / 2 - 1))) + (p - kSide < kMid / 2 ? 0 : kBins / 2);
 }
 IPD_DEVINL uint32_t key_at(const Shared &S, int window, int p) {
   if (window >= 0) return (uint32_t)window * kBins + kBins - 1 - p;
@@ -315,18 +321,38 @@ constexpr uint32_t kKeyLow = 0x7fffu - kLowBits - kSide;         // -2^16
 IPD_DEVINL void shared_add(uint32_t addr, uint32_t v) {
   asm volatile("red.shared.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
-// One entry (its bits but the sign, and the sign's half of the bins) into the
-// histogram; true if it is near 0.  (What is below -2^16 is left out; what is
-// from 2^16 up shows in the maximum.)
-IPD_DEVINL bool count_entry(uint32_t hist, uint32_t abs_bits, uint32_t half) {
-  const uint32_t i = abs_bits - kLowBits;
-  if (i < (uint32_t)kSide) shared_add(hist + 4 * (i + half), 1u);
-  return (int)i < 0;
+// the byte offsets of two entries' words
+IPD_DEVINL uint32_t words2(uint32_t w) {
+  return ((w << 2) & 0x3ffc3ffcu) | ((w >> 1) & 0x40004000u);
 }
-// One entry near 0 into the list; 1 for a zero.
-IPD_DEVINL uint32_t count_near(Shared &S, uint32_t b) {
+// 0xffff in each half where the entry is near 0, without a bin of its own
+IPD_DEVINL uint32_t near2(uint32_t w) {
+  const __nv_bfloat162 a = __habs2(*reinterpret_cast<__nv_bfloat162 *>(&w));
+  const uint32_t low = kLowBits * 0x00010001u;
+  return __hlt2_mask(a, *reinterpret_cast<const __nv_bfloat162 *>(&low));
+}
+constexpr uint32_t kLowest2 = (0x8000u | (kLowBits + kSide)) * 0x00010001u;  // -2^16, twice
+constexpr uint32_t kLowestWord = 4 * (kBins / 2 + ((kLowBits + kSide) & (kBins / 2 - 1)));
+// Two entries into the histogram.  What is not above -2^16, and NaN, is left out
+// (a masked row would put all of it on one word, one entry after the other); what
+// is from 2^16 up shows in the maximum; what is near 0 is taken out again
+// (count_near).
+IPD_DEVINL void count2(uint32_t hist, uint32_t w) {
+  const uint32_t z = words2(max2(w, kLowest2)), z0 = z & 0xffffu, z1 = z >> 16;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %1, %3;\n\t"
+      "setp.ne.u32 q, %2, %3;\n\t"
+      "@p red.shared.add.u32 [%4], 1;\n\t"
+      "@q red.shared.add.u32 [%5], 1;\n\t}" ::"r"(0), "r"(z0), "r"(z1), "n"(kLowestWord), "r"(hist + z0), "r"(hist + z1)
+      : "memory");
+}
+// An entry that was counted, if it is near 0, into the list instead; 1 for a zero.
+__device__ __noinline__ uint32_t count_near(Shared &S, uint32_t b) {
   const uint32_t a = b & 0x7fffu;
   if (a >= kLowBits) return 0u;
+  const uint32_t word = words2(b) & 0xffffu;
+  if (word != kLowestWord) shared_add(smem_u32(S.hist) + word, 0xffffffffu);
   if (a == 0u) return 1u;
   const uint32_t n = atomicAdd(&S.near_n, 1u);
   if (n < (uint32_t)kMid) S.near_key[n] = (uint16_t)order_key(b);
@@ -443,85 +469,87 @@ __device__ __noinline__ uint4 edge_vector(const uint16_t *base, int v, int shift
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+IPD_DEVINL uint32_t eq2(uint32_t a, uint32_t b) {  // 0xffff in each half where they are equal
+  return __heq2_mask(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b));
+}
 // The row's id of entry `rank` (in index order, from vector `first` on) of
-// those with this key: counted in blocks of 32 vectors, then looked up in its
-// block, by the thread that finds it.
+// those with this key: in rounds of kRound blocks a warp, 32 vectors a block,
+// counted and then looked up in the block, by the thread that finds it.
 IPD_DEVINL void look_up(Shared &S, const Row &R, int first, int last, uint32_t key, uint32_t rank,
                         int32_t *token) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const uint32_t keep = key == kKeyZero ? 0x7fff7fffu : 0xffffffffu;  // -0 counts as 0
   const uint32_t want = key_bits(key) * 0x00010001u;
-  const auto match = [&](uint32_t w) {  // bits 0 and 1: the word's entries
-    const uint32_t d = (w & keep) ^ want;
-    return (uint32_t)!(d & 0xffffu) | (uint32_t)!(d >> 16) << 1;
+  const auto match = [&](const uint4 &v) {  // a bit for each of the vector's entries (-0 is 0)
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m |= eq2(w[i], want) & (0x00020001u << (2 * i));
+    return (m | m >> 16) & 0xffu;
   };
-  const auto cut = [&](int v) { return v < last && (8 * v < R.shift || 8 * v + 8 > R.end); };
-  const int each = (last - first + 32 * kWarps - 1) / (32 * kWarps);  // blocks of a warp
+  const auto cut = [&](int v) { return v < last && R.cut(v); };
+  constexpr int kMine = kWarps * kRound / 32;  // blocks a lane sums
+  static_assert(kRound % kBatch == 0 && kWarps * kRound % 32 == 0, "rounds of whole batches");
+  int round = 0;
 #pragma unroll 1
-  for (int b0 = 0; b0 < each; b0 += kBatch) {
-    uint4 x[kBatch];
-    const int v0 = first + (warp * each + b0) * 32 + lane;
+  for (int v1 = first; v1 < last; v1 += kWarps * kRound * 32, round ^= 1) {
+#pragma unroll 1
+    for (int b0 = 0; b0 < kRound; b0 += kBatch) {
+      uint4 x[kBatch];
+      const int v0 = v1 + (warp * kRound + b0) * 32 + lane;
 #pragma unroll
-    for (int b = 0; b < kBatch; ++b) x[b] = R.load(b0 + b < each ? v0 + 32 * b : last, last);
+      for (int b = 0; b < kBatch; ++b) x[b] = R.load(v0 + 32 * b, last);
 #pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      if (b0 + b >= each) break;
-      if (cut(v0 + 32 * b)) x[b] = edge_vector(R.base, v0 + 32 * b, R.shift, R.end);
-      uint32_t n = __popc(match(x[b].x)) + __popc(match(x[b].y)) + __popc(match(x[b].z)) +
-                   __popc(match(x[b].w));
-      __syncwarp();
-      n = __reduce_add_sync(0xffffffffu, n);
-      if (lane == 0) S.block[warp * each + b0 + b] = (uint16_t)n;
+      for (int b = 0; b < kBatch; ++b) {
+        if (cut(v0 + 32 * b)) x[b] = edge_vector(R.base, v0 + 32 * b, R.shift, R.end);
+        __syncwarp();
+        const uint32_t n = __reduce_add_sync(0xffffffffu, __popc(match(x[b])));
+        if (lane == 0) S.block[round][warp * kRound + b0 + b] = (uint16_t)n;
+      }
     }
-  }
-  __syncthreads();
-  constexpr int kMine = kWarps * kBlocks / kThreads;
-  uint32_t mine[kMine], n = 0;
+    __syncthreads();
+    // every warp finds the block for itself
+    uint32_t mine[kMine], n = 0;
 #pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    mine[i] = kMine * tid + i < kWarps * each ? S.block[kMine * tid + i] : 0u;
-    n += mine[i];
-  }
-  uint32_t in = n;
+    for (int i = 0; i < kMine; ++i) n += mine[i] = S.block[round][kMine * lane + i];
+    uint32_t in = n;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t y = __shfl_up_sync(0xffffffffu, in, o);
-    if (lane >= o) in += y;
-  }
-  if (lane == 31) S.scan_n[warp] = in;
-  __syncthreads();
-  uint32_t before = in - n;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    const uint32_t y = S.scan_n[w];
-    if (w < warp) before += y;
-  }
-#pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    if (rank >= before && rank - before < mine[i]) {
-      S.block_at = kMine * tid + i;
-      S.block_rank = rank - before;
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, in, o);
+      if (lane >= o) in += y;
     }
-    before += mine[i];
-  }
-  __syncthreads();
-  if (warp != 0) return;  // (of this function)
-  const int v = first + (int)S.block_at * 32 + lane;
-  uint4 x = R.load(v, last);
-  if (cut(v)) x = edge_vector(R.base, v, R.shift, R.end);
-  __syncwarp();
-  uint32_t hits = match(x.x) | match(x.y) << 2 | match(x.z) << 4 | match(x.w) << 6;
-  n = __popc(hits);
-  in = n;
+    const uint32_t all = __shfl_sync(0xffffffffu, in, 31);
+    if (rank >= all) {
+      rank -= all;
+      continue;
+    }
+    if (warp != 0) return;
+    uint32_t before = in - n, at = 0, left = 0;
+    bool here = false;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t y = __shfl_up_sync(0xffffffffu, in, o);
-    if (lane >= o) in += y;
-  }
-  uint32_t left = S.block_rank;
-  if (left >= in - n && left < in) {
-    for (left -= in - n; left; --left) hits &= hits - 1;
-    *token = 8 * v + __ffs(hits) - 1 - R.shift;
+    for (int i = 0; i < kMine; ++i) {
+      if (rank >= before && rank - before < mine[i]) here = true, at = kMine * lane + i, left = rank - before;
+      before += mine[i];
+    }
+    const int from = __ffs(__ballot_sync(0xffffffffu, here)) - 1;
+    at = __shfl_sync(0xffffffffu, at, from);
+    left = __shfl_sync(0xffffffffu, left, from);
+    const int v = v1 + (int)at * 32 + lane;
+    uint4 x = R.load(v, last);
+    if (cut(v)) x = edge_vector(R.base, v, R.shift, R.end);
+    __syncwarp();
+    uint32_t hits = match(x);
+    n = __popc(hits);
+    in = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, in, o);
+      if (lane >= o) in += y;
+    }
+    if (left >= in - n && left < in) {
+      for (left -= in - n; left; --left) hits &= hits - 1;
+      *token = 8 * v + __ffs(hits) - 1 - R.shift;
+    }
+    return;
   }
 }
 
@@ -564,8 +592,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
     if (e >= 0) {
       const uint32_t b = R.base[e];
       largest = max2(largest, b | 0xff800000u);
-      if (count_entry(hist, b & 0x7fffu, (b >> 15) * (kBins / 2))) zeros += count_near(S, b);
+      count2(hist, b | 0xff800000u);
+      zeros += count_near(S, b);
     }
+#pragma unroll 1
     for (int vb = v0 + tid; vb < v1; vb += kBatch * kThreads) {
       uint4 x[kBatch];
 #pragma unroll
@@ -577,15 +607,17 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           largest = max2(largest, w[i]);
-          bool is = count_entry(hist, w[i] & 0x7fffu, (w[i] & 0x8000u) / 0x8000u * (kBins / 2));
-          is |= count_entry(hist, (w[i] >> 16) & 0x7fffu, (w[i] >> 31) * (kBins / 2));
-          if (is) near |= 1u << k;
+          near |= near2(w[i]) & (0x00010001u << k);
+          count2(hist, w[i]);
         }
       }
-      while (near) {
-        const int k = __ffs(near) - 1;
-        near &= near - 1;
-        for (int i = 0; i < 8; ++i) zeros += count_near(S, R.base[8ll * (vb + k * kThreads) + i]);
+      for (near |= near >> 16, near &= 0xffffu; near; near &= near - 1) {
+        const uint4 v = R.load(vb + (__ffs(near) - 1) * kThreads, v1);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (near2(w[i])) zeros += count_near(S, w[i] & 0xffffu) + count_near(S, w[i] >> 16);
+        }
       }
     }
     zeros = __reduce_add_sync(0xffffffffu, zeros);
@@ -736,11 +768,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   // the piece that holds it, if the pieces' histograms tell
   int first = 0, last = n_vec;
   if (csize > 1) {
-    const uint32_t i = (key_bits(key) & 0x7fffu) - kLowBits;
-    if (!windows && i < (uint32_t)kSide) {
+    const uint32_t bits = key_bits(key);
+    if (!windows && (bits & 0x7fffu) - kLowBits < (uint32_t)kSide) {
       uint32_t n = 0;
       if (lane > 0 && lane < (int)csize)
-        n = remote_ld(remote(&S.hist[i + (key & 0x8000u ? 0 : kBins / 2)], lane));
+        n = remote_ld(remote(S.hist, lane) + (words2(bits) & 0xffffu));
       const uint32_t others = __reduce_add_sync(0xffffffffu, n);
       if (lane == 0) n = S.found_count - others;
       uint32_t p = 0;
