@@ -89,7 +89,7 @@ struct Shared {
   u64 scan[kWarps];
   uint32_t scan_n[kWarps];
   u64 found_before, word;
-  uint32_t win_thread, found_key, found_weight, found_n, found_count;
+  uint32_t found_key, found_weight, found_n, found_count;
   uint16_t block[2][kWarps * kRound];  // entries of the drawn value in each block of a round
 };
 
@@ -208,13 +208,12 @@ IPD_DEVINL void weight2(const Scale &S, uint32_t w, uint32_t &w0, uint32_t &w1) 
 IPD_DEVINL float exponent(const Scale &S, float l) {
   return S.inf ? 0.f : __fmul_rn(__fsub_rn(l, S.top), S.c);
 }
-IPD_DEVINL void key_weights(const Scale &S, uint32_t key0, uint32_t key1, uint32_t &w0,
-                            uint32_t &w1) {
+IPD_DEVINL void weights(const Scale &S, uint32_t w, uint32_t &w0, uint32_t &w1) {
   if (S.inf) {
-    w0 = key0 == kKeyInf ? 1u << 30 : 0u;
-    w1 = key1 == kKeyInf ? 1u << 30 : 0u;
+    w0 = (w & 0xffffu) == 0x7f80u ? 1u << 30 : 0u;
+    w1 = w >> 16 == 0x7f80u ? 1u << 30 : 0u;
   } else {
-    weight2(S, key_bits(key0) | key_bits(key1) << 16, w0, w1);
+    weight2(S, w, w0, w1);
   }
 }
 IPD_DEVINL uint32_t weight_floor(float min_p) {
@@ -371,17 +370,26 @@ __device__ __noinline__ void sum_bins(Shared &S) {
     // four bins, in an order that spreads a warp's over the banks
     const int p = kEach * tid + 4 * ((q + lane / (32 / kEach)) & (kEach / 4 - 1));
     const int a = word_at(window, p), b = word_at(window, p + 3);
-    uint4 v = *reinterpret_cast<const uint4 *>(&S.hist[min(a, b)]);
-    if (a > b) v = make_uint4(v.w, v.z, v.y, v.x);
-    if (!(v.x | v.y | v.z | v.w)) continue;
-    const uint32_t c[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int e = 0; e < 4; e += 2) {
-      uint32_t w0, w1;
-      key_weights(C, key_at(S, window, p + e), key_at(S, window, p + e + 1), w0, w1);
-      mass += (u64)w0 * c[e] + (u64)w1 * c[e + 1];
-      n += (w0 ? c[e] : 0u) + (w1 ? c[e + 1] : 0u);
+    const uint4 c = *reinterpret_cast<const uint4 *>(&S.hist[min(a, b)]);
+    if (!(c.x | c.y | c.z | c.w)) continue;
+    // their values: bf16 bits that follow one another, but between the signs
+    const uint32_t bits = key_bits(key_at(S, window, a < b ? p : p + 3));
+    uint32_t v01 = bits * 0x00010001u, v23;
+    if (window < 0 && p >= kSide && p < kSide + kMid) {
+      v01 = bits | key_bits(key_at(S, window, p + 1)) << 16;
+      v23 = key_bits(key_at(S, window, p + 2)) | key_bits(key_at(S, window, p + 3)) << 16;
+    } else if (window >= 0 && (bits & 0x8000u)) {
+      v01 -= 0x00010000u;
+      v23 = v01 - 0x00020002u;
+    } else {
+      v01 += 0x00010000u;
+      v23 = v01 + 0x00020002u;
     }
+    uint32_t w0, w1, w2, w3;
+    weights(C, v01, w0, w1);
+    weights(C, v23, w2, w3);
+    mass += (u64)w0 * c.x + (u64)w1 * c.y + (u64)w2 * c.z + (u64)w3 * c.w;
+    n += (w0 ? c.x : 0u) + (w1 ? c.y : 0u) + (w2 ? c.z : 0u) + (w3 ? c.w : 0u);
   }
   u64 im = mass;
   uint32_t in = n;
@@ -393,14 +401,12 @@ __device__ __noinline__ void sum_bins(Shared &S) {
   }
   if (lane == 31) S.scan[warp] = im, S.scan_n[warp] = in;
   __syncthreads();
-  u64 bm = im - mass;
-  uint32_t bn = in - n;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    const u64 x = S.scan[w];
-    const uint32_t y = S.scan_n[w];
-    if (w < warp) bm += x, bn += y;
-  }
+  // the warps before this one: their sums, below 2^48, in two halves of 24 bits
+  const bool is = lane < warp;
+  const u64 x = is ? S.scan[lane] : 0ull;
+  const u64 bm = im - mass + __reduce_add_sync(0xffffffffu, (uint32_t)x & 0xffffffu) +
+                 ((u64)__reduce_add_sync(0xffffffffu, (uint32_t)(x >> 24)) << 24);
+  const uint32_t bn = in - n + __reduce_add_sync(0xffffffffu, is ? S.scan_n[lane] : 0u);
   S.before[tid] = bm, S.n_before[tid] = bn;
   if (tid == kThreads - 1) S.before[kThreads] = bm + mass, S.n_before[kThreads] = bn + n;
   __syncthreads();
@@ -410,16 +416,15 @@ __device__ __noinline__ void sum_bins(Shared &S) {
 // the entries (`ranks`) or of their masses: into S.found_* its key, its entries
 // and their weight, and the sum and the number of entries above it.
 __device__ __noinline__ void find_bin(Shared &S, bool ranks, u64 t) {
-  const int tid = threadIdx.x, window = S.window;
+  const int tid = threadIdx.x, lane = tid & 31, window = S.window;
   const u64 lo = ranks ? S.n_before[tid] : S.before[tid];
   const u64 hi = ranks ? S.n_before[tid + 1] : S.before[tid + 1];
-  if (t >= lo && t < hi) S.win_thread = tid;
-  __syncthreads();
-  if (tid < 32) {
-    const int win = S.win_thread, p = kEach * win + (tid & (kEach - 1));
+  const uint32_t here = __ballot_sync(0xffffffffu, t >= lo && t < hi);
+  if (here) {  // one warp, for one of its threads
+    const int win = tid - lane + __ffs(here) - 1, p = kEach * win + (lane & (kEach - 1));
     const uint32_t key = key_at(S, window, p), count = S.hist[word_at(window, p)];
     uint32_t w, w1;
-    key_weights(S.scale, key, key, w, w1);
+    weights(S.scale, key_bits(key), w, w1);
     const uint32_t n = w ? count : 0u;
     const u64 mass = (u64)n * w;
     u64 im = mass;
@@ -428,10 +433,10 @@ __device__ __noinline__ void find_bin(Shared &S, bool ranks, u64 t) {
     for (int o = 1; o < kEach; o <<= 1) {
       const u64 x = __shfl_up_sync(0xffffffffu, im, o, kEach);
       const uint32_t y = __shfl_up_sync(0xffffffffu, in, o, kEach);
-      if ((tid & (kEach - 1)) >= o) im += x, in += y;
+      if ((lane & (kEach - 1)) >= o) im += x, in += y;
     }
     const u64 above = S.before[win] + im - mass, first = ranks ? S.n_before[win] + in - n : above;
-    if (tid < kEach && t >= first && t - first < (ranks ? n : mass)) {
+    if (lane < kEach && t >= first && t - first < (ranks ? n : mass)) {
       S.found_key = key;
       S.found_weight = w;
       S.found_before = above;
