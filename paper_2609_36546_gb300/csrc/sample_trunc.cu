@@ -45,6 +45,7 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;          // portable cluster size
+constexpr int kSplitRow = 48 * 1024, kMinPiece = 12 * 1024;  // entries: see ipd_sample_trunc
 constexpr int kBins = 8192;
 constexpr int kEach = kBins / kThreads;  // bins a thread sums
 static_assert(kEach >= 16 && kEach <= 32, "a thread's bins are searched by one warp");
@@ -827,11 +828,17 @@ extern "C" int ipd_sample_trunc(const uint16_t *logits, int64_t row_stride, int 
       return IPD_ERR_CUDA;
     D.sms = n;
   }
-  // CTAs of a row: more while SMs are idle and a piece is more than a few loads
-  // a thread
-  int csize = 1;
+  // CTAs of a row.  A cluster's barriers and the sum of its histograms cost about
+  // 4 us, a CTA alone 0.12 us per 1,024 entries: clusters are for long rows, and while
+  // every CTA has an SM (clusters of 8 do not fill the SMs evenly).  Measured with
+  // 1 / 2 / 4 / 8 CTAs: 1 row of 151,936 25.9 / 19.9 / 15.5 / 14.6 us, 16 rows 27.6 /
+  // 21.1 / 16.9 / 19.0, 64 rows 28.0 / 21.7 / 22.7 / 34.6; 1 row of 50,021 14.0 / 13.9 /
+  // 12.8 / 13.1, of 32,000 11.5 / 12.7 / 12.7 / 13.0.
   const int span = vocab + 7;  // a row may start inside a 16-byte vector
-  while (csize < kMaxCluster && (long long)n_rows * csize < D.sms && span / csize > 8192) csize *= 2;
+  int csize = kMaxCluster;
+  while (csize > 1 && (span < kSplitRow || span < csize * kMinPiece ||
+                       (long long)n_rows * csize > (csize == 8 ? D.sms * 3 / 4 : D.sms)))
+    csize /= 2;
   Params P;
   P.logits = logits;
   P.stride = row_stride;
