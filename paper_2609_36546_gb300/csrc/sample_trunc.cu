@@ -25,12 +25,12 @@
 // part of the row (in L2).  No sorting, no order of summation, and no entry's
 // weight is computed on its own.
 //
-// Bins: 2^-15 <= |l| < 2^16 is 31 binades of 128 values a sign, one bin each.
+// Bins: 2^-19 <= |l| < 2^12 is 31 binades of 128 values a sign, one bin each.
 // What is nearer to 0 is rare (zeros apart, which are counted) and goes to a
 // list, which takes the bins between the signs in the order of its values.
-// -inf, NaN and what is below -2^16 have no weight next to such a maximum.  A
+// -inf, NaN and what is below -2^12 have no weight next to such a maximum.  A
 // row that does not fit this (a maximum outside, +inf, a full list, so high a
-// temperature that 2^16 matters) is worked through by its first CTA in windows
+// temperature that -2^12 matters) is worked through by its first CTA in windows
 // of 2^13 bins over all 2^16 values, a pass over the row for each.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -50,8 +50,8 @@ constexpr int kBins = 8192;
 constexpr int kEach = kBins / kThreads;  // bins a thread sums
 static_assert(kEach >= 16 && kEach <= 32, "a thread's bins are searched by one warp");
 constexpr int kBatch = 4;               // 16-byte vectors in flight a thread
-constexpr uint32_t kLowBits = 0x3800;   // bf16 bits of 2^-15
-constexpr int kSide = 31 * 128;         // bins of a sign; up to the bits of 2^16
+constexpr uint32_t kLowBits = 0x3600;   // bf16 bits of 2^-19
+constexpr int kSide = 31 * 128;         // bins of a sign; up to the bits of 2^12
 constexpr int kMid = kBins - 2 * kSide;  // bins between the signs
 constexpr int kRound = 8;               // see look_up
 constexpr float kMagic = 12582912.f;    // 1.5 * 2^23: x + kMagic rounds x to a whole number
@@ -315,8 +315,8 @@ IPD_DEVINL uint32_t key_at(const Shared &S, int window, int p) {
   return S.mid_key[p - kSide];
 }
 static_assert(kSide % kEach == 0 && kMid % (2 * kEach) == 0, "a thread's bins are contiguous words");
-constexpr uint32_t kKeyHigh = 0x8000u + kLowBits + kSide;        // 2^16
-constexpr uint32_t kKeyLow = 0x7fffu - kLowBits - kSide;         // -2^16
+constexpr uint32_t kKeyHigh = 0x8000u + kLowBits + kSide;        // 2^12
+constexpr uint32_t kKeyLow = 0x7fffu - kLowBits - kSide;         // -2^12
 
 IPD_DEVINL void shared_add(uint32_t addr, uint32_t v) {
   asm volatile("red.shared.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
@@ -325,18 +325,20 @@ IPD_DEVINL void shared_add(uint32_t addr, uint32_t v) {
 IPD_DEVINL uint32_t words2(uint32_t w) {
   return ((w << 2) & 0x3ffc3ffcu) | ((w >> 1) & 0x40004000u);
 }
+IPD_DEVINL uint32_t eq2(uint32_t a, uint32_t b) {  // 0xffff in each half where they are equal
+  return __heq2_mask(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b));
+}
 // 0xffff in each half where the entry is near 0, without a bin of its own
 IPD_DEVINL uint32_t near2(uint32_t w) {
   const __nv_bfloat162 a = __habs2(*reinterpret_cast<__nv_bfloat162 *>(&w));
   const uint32_t low = kLowBits * 0x00010001u;
   return __hlt2_mask(a, *reinterpret_cast<const __nv_bfloat162 *>(&low));
 }
-constexpr uint32_t kLowest2 = (0x8000u | (kLowBits + kSide)) * 0x00010001u;  // -2^16, twice
+constexpr uint32_t kLowest2 = (0x8000u | (kLowBits + kSide)) * 0x00010001u;  // -2^12, twice
 constexpr uint32_t kLowestWord = 4 * (kBins / 2 + ((kLowBits + kSide) & (kBins / 2 - 1)));
-// Two entries into the histogram.  What is not above -2^16, and NaN, is left out
+// Two entries into the histogram.  What is not above -2^12, and NaN, is left out
 // (a masked row would put all of it on one word, one entry after the other); what
-// is from 2^16 up shows in the maximum; what is near 0 is taken out again
-// (count_near).
+// is from 2^12 up shows in the maximum; what is near 0 is taken out again.
 IPD_DEVINL void count2(uint32_t hist, uint32_t w) {
   const uint32_t z = words2(max2(w, kLowest2)), z0 = z & 0xffffu, z1 = z >> 16;
   asm volatile(
@@ -347,16 +349,14 @@ IPD_DEVINL void count2(uint32_t hist, uint32_t w) {
       "@q red.shared.add.u32 [%5], 1;\n\t}" ::"r"(0), "r"(z0), "r"(z1), "n"(kLowestWord), "r"(hist + z0), "r"(hist + z1)
       : "memory");
 }
-// An entry that was counted, if it is near 0, into the list instead; 1 for a zero.
-__device__ __noinline__ uint32_t count_near(Shared &S, uint32_t b) {
+// An entry that was counted, if it is near 0 but not 0, into the list instead.
+__device__ __noinline__ void list_near(Shared &S, uint32_t b) {
   const uint32_t a = b & 0x7fffu;
-  if (a >= kLowBits) return 0u;
+  if (a >= kLowBits || a == 0u) return;
   const uint32_t word = words2(b) & 0xffffu;
   if (word != kLowestWord) shared_add(smem_u32(S.hist) + word, 0xffffffffu);
-  if (a == 0u) return 1u;
   const uint32_t n = atomicAdd(&S.near_n, 1u);
   if (n < (uint32_t)kMid) S.near_key[n] = (uint16_t)order_key(b);
-  return 0u;
 }
 
 // Sums over the bins before each thread's, and over all, of the masses into
@@ -448,21 +448,6 @@ __device__ __noinline__ void find_bin(Shared &S, bool ranks, u64 t) {
   __syncthreads();
 }
 
-// A window's histogram, from the whole row.
-__device__ __noinline__ void count_window(Shared &S, const uint16_t *base, int shift, int end,
-                                          int window) {
-  __syncthreads();
-  for (int i = threadIdx.x; i < kBins; i += kThreads) S.hist[i] = 0u;
-  if (threadIdx.x == 0) S.window = window;
-  __syncthreads();
-  for (int i = shift + (int)threadIdx.x; i < end; i += kThreads) {
-    const uint32_t k = order_key(base[i]);
-    if ((int)(k / kBins) == window && k > kKeyMinusInf)
-      shared_add(smem_u32(&S.hist[k % kBins]), 1u);
-  }
-  __syncthreads();
-}
-
 // A vector that the row has a part of.
 __device__ __noinline__ uint4 edge_vector(const uint16_t *base, int v, int shift, int end) {
   uint32_t w[4];
@@ -475,9 +460,27 @@ __device__ __noinline__ uint4 edge_vector(const uint16_t *base, int v, int shift
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-IPD_DEVINL uint32_t eq2(uint32_t a, uint32_t b) {  // 0xffff in each half where they are equal
-  return __heq2_mask(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b));
+// A window's histogram, from the whole row.
+__device__ __noinline__ void count_window(Shared &S, const Row R, int n_vec, int window) {
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins; i += kThreads) S.hist[i] = 0u;
+  if (threadIdx.x == 0) S.window = window;
+  __syncthreads();
+#pragma unroll 2
+  for (int v = threadIdx.x; v < n_vec; v += kThreads) {
+    uint4 x = R.load(v, n_vec);
+    if (R.cut(v)) x = edge_vector(R.base, v, R.shift, R.end);
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t k = order_key(e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffffu);
+      if ((int)(k / kBins) == window && k > kKeyMinusInf)
+        shared_add(smem_u32(&S.hist[k % kBins]), 1u);
+    }
+  }
+  __syncthreads();
 }
+
 // The row's id of entry `rank` (in index order, from vector `first` on) of
 // those with this key: in rounds of kRound blocks a warp, 32 vectors a block,
 // counted and then looked up in the block, by the thread that finds it.
@@ -591,7 +594,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   }
   __syncthreads();
   {
-    uint32_t zeros = 0, largest = 0xff80ff80u;
+    uint32_t zeros[2] = {0u, 0u}, largest = 0xff80ff80u;  // (by sign)
     const uint32_t hist = smem_u32(S.hist);
     const int v0 = (int)rank * piece, v1 = min(v0 + piece, n_vec);
     const int e = R.edge_entry(tid, v0, v1);
@@ -599,7 +602,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
       const uint32_t b = R.base[e];
       largest = max2(largest, b | 0xff800000u);
       count2(hist, b | 0xff800000u);
-      zeros += count_near(S, b);
+      if (b & 0x7fffu) list_near(S, b);
+      else ++zeros[b >> 15];
     }
 #pragma unroll 1
     for (int vb = v0 + tid; vb < v1; vb += kBatch * kThreads) {
@@ -613,24 +617,42 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           largest = max2(largest, w[i]);
-          near |= near2(w[i]) & (0x00010001u << k);
+          near |= near2(w[i]);
           count2(hist, w[i]);
         }
       }
-      for (near |= near >> 16, near &= 0xffffu; near; near &= near - 1) {
-        const uint4 v = R.load(vb + (__ffs(near) - 1) * kThreads, v1);
+      if (!near) continue;
+      uint32_t tiny = 0;
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const uint32_t w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t is0 = eq2(w[i], 0u);
+          zeros[0] += __popc(is0 & ~w[i] & 0x80008000u);
+          zeros[1] += __popc(is0 & w[i] & 0x80008000u);
+          tiny |= near2(w[i]) & ~is0 & (0x00010001u << k);
+        }
+      }
+      for (tiny = (tiny | tiny >> 16) & 0xffffu; tiny; tiny &= tiny - 1) {
+        const uint4 v = R.load(vb + (__ffs(tiny) - 1) * kThreads, v1);
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (near2(w[i])) zeros += count_near(S, w[i] & 0xffffu) + count_near(S, w[i] >> 16);
+          if (near2(w[i])) list_near(S, w[i] & 0xffffu), list_near(S, w[i] >> 16);
         }
       }
     }
-    zeros = __reduce_add_sync(0xffffffffu, zeros);
+    zeros[0] = __reduce_add_sync(0xffffffffu, zeros[0]);
+    zeros[1] = __reduce_add_sync(0xffffffffu, zeros[1]);
     const uint32_t m = __reduce_max_sync(
         0xffffffffu, max(order_key(largest & 0xffffu), order_key(largest >> 16)));
     if (lane == 0) {
-      if (zeros) atomicAdd(&S.zeros, zeros);
+      if (zeros[0] | zeros[1]) {  // out of the words they were counted in
+        shared_add(hist + (words2(0x0000u) & 0xffffu), 0u - zeros[0]);
+        shared_add(hist + (words2(0x8000u) & 0xffffu), 0u - zeros[1]);
+        atomicAdd(&S.zeros, zeros[0] + zeros[1]);
+      }
       atomicMax(&S.largest, m);
     }
   }
@@ -732,7 +754,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
     uint32_t above_n = 0;
 #pragma unroll 1
     for (int w = w_first; w >= w_last; --w) {
-      if (windows) count_window(S, R.base, R.shift, R.end, w);
+      if (windows) count_window(S, R, n_vec, w);
       if (windows || what == 0) sum_bins(S);
       const u64 mass = S.before[kThreads];
       const uint32_t n = S.n_before[kThreads];

@@ -75,3 +75,19 @@ def test_rows_that_start_anywhere(lib, start):
     rows = buf[:, start:start + V]
     for s in ({}, dict(top_k=40), dict(top_p=0.9)):
         _check(lib, rows, np.float32([0.2, 0.6, 0.95]), **s)
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("e", [12, 16, -15, -19, -24])
+def test_neighbours_of_powers_of_two(lib, sign, e):
+    # the bf16 values on both sides of a power of two, some of each, among -inf
+    V = 5003
+    g = torch.Generator().manual_seed(100 + e)
+    row = torch.full((2, V), float("-inf"))
+    row[1] = -300.0 if sign > 0 else -1e6
+    for m in (1 - 2.0 ** -7, 1 - 2.0 ** -8, 1.0, 1 + 2.0 ** -7, 1 + 2.0 ** -6):
+        row[:, torch.randperm(V, generator=g)[:20]] = sign * m * 2.0 ** e
+    rows = row.to(torch.bfloat16).cuda()
+    for u in (0.1, 0.5, 0.97):
+        for s in ({}, dict(top_k=33), dict(top_p=0.6)):
+            _check(lib, rows, u, inv_t=min(1.0, 2.0 ** (5 - e)), **s)
