@@ -334,27 +334,25 @@ IPD_DEVINL uint32_t near2(uint32_t w) {
   const uint32_t low = kLowBits * 0x00010001u;
   return __hlt2_mask(a, *reinterpret_cast<const __nv_bfloat162 *>(&low));
 }
+IPD_DEVINL uint32_t min_abs2(uint32_t a, uint32_t w) {
+  const __nv_bfloat162 m = __hmin2(*reinterpret_cast<__nv_bfloat162 *>(&a),
+                                   __habs2(*reinterpret_cast<__nv_bfloat162 *>(&w)));
+  return *reinterpret_cast<const uint32_t *>(&m);
+}
 constexpr uint32_t kLowest2 = (0x8000u | (kLowBits + kSide)) * 0x00010001u;  // -2^12, twice
-constexpr uint32_t kLowestWord = 4 * (kBins / 2 + ((kLowBits + kSide) & (kBins / 2 - 1)));
-// Two entries into the histogram.  What is not above -2^12, and NaN, is left out
-// (a masked row would put all of it on one word, one entry after the other); what
-// is from 2^12 up shows in the maximum; what is near 0 is taken out again.
+// Two entries into the histogram.  What is not above -2^12, and NaN, counts as
+// -2^12, whose word is no value's here and is emptied later; what is from 2^12 up
+// shows in the maximum; what is near 0 is taken out again.
 IPD_DEVINL void count2(uint32_t hist, uint32_t w) {
-  const uint32_t z = words2(max2(w, kLowest2)), z0 = z & 0xffffu, z1 = z >> 16;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %1, %3;\n\t"
-      "setp.ne.u32 q, %2, %3;\n\t"
-      "@p red.shared.add.u32 [%4], 1;\n\t"
-      "@q red.shared.add.u32 [%5], 1;\n\t}" ::"r"(0), "r"(z0), "r"(z1), "n"(kLowestWord), "r"(hist + z0), "r"(hist + z1)
-      : "memory");
+  const uint32_t z = words2(max2(w, kLowest2));
+  shared_add(hist + (z & 0xffffu), 1u);
+  shared_add(hist + (z >> 16), 1u);
 }
 // An entry that was counted, if it is near 0 but not 0, into the list instead.
 __device__ __noinline__ void list_near(Shared &S, uint32_t b) {
   const uint32_t a = b & 0x7fffu;
   if (a >= kLowBits || a == 0u) return;
-  const uint32_t word = words2(b) & 0xffffu;
-  if (word != kLowestWord) shared_add(smem_u32(S.hist) + word, 0xffffffffu);
+  shared_add(smem_u32(S.hist) + (words2(b) & 0xffffu), 0xffffffffu);
   const uint32_t n = atomicAdd(&S.near_n, 1u);
   if (n < (uint32_t)kMid) S.near_key[n] = (uint16_t)order_key(b);
 }
@@ -610,18 +608,18 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
       uint4 x[kBatch];
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) x[k] = R.load(vb + k * kThreads, v1);
-      uint32_t near = 0;
+      uint32_t nearest = 0x7f807f80u;  // to 0
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
         const uint32_t w[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           largest = max2(largest, w[i]);
-          near |= near2(w[i]);
+          nearest = min_abs2(nearest, w[i]);
           count2(hist, w[i]);
         }
       }
-      if (!near) continue;
+      if (!near2(nearest)) continue;
       uint32_t tiny = 0;
 #pragma unroll
       for (int k = 0; k < kBatch; ++k) {
@@ -704,7 +702,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
     return;
   }
   const Scale C = make_scale(c, min_p, top_key);
-  if (tid == 0) S.scale = C;
+  if (tid == 0) {
+    S.scale = C;
+    S.hist[kBins / 2 + kFreeWord] = 0;  // what counted as -2^12
+  }
   const uint32_t least_key = C.inf ? kKeyInf : order_key(C.least2 & 0xffffu);
   const uint32_t mid = near + (zeros != 0);
   const bool windows = top_key <= kKeyLow || top_key >= kKeyHigh || mid > (uint32_t)kMid ||
