@@ -42,13 +42,9 @@ IPD_DECLARE_ERROR_WORD(g_trunc_err);
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;          // portable cluster size
 constexpr int kSplitRow = 48 * 1024, kMinPiece = 12 * 1024;  // entries: see ipd_sample_trunc
 constexpr int kBins = 8192;
-constexpr int kEach = kBins / kThreads;  // bins a thread sums
-static_assert(kEach >= 16 && kEach <= 32, "a thread's bins are searched by one warp");
 constexpr int kBatch = 4;               // 16-byte vectors in flight a thread
 constexpr uint32_t kLowBits = 0x3600;   // bf16 bits of 2^-19
 constexpr int kSide = 31 * 128;         // bins of a sign; up to the bits of 2^12
@@ -75,23 +71,6 @@ struct Scale {
   bool coarse;      // the x of least2 is far below -64: bf16 is coarse at l_max
   uint32_t least2;  // a bf16 value (twice) of weight 0 from which on weights are 0
   uint32_t min_w;   // smallest weight that counts (min-p; at least 1)
-};
-
-struct Shared {
-  uint32_t hist[kBins];
-  u64 before[kThreads + 1];       // sums of the bins before a thread's, and of all
-  uint32_t n_before[kThreads + 1];
-  uint16_t near_key[kMid];  // keys of this CTA's entries near 0
-  uint16_t mid_key[kMid];   // first CTA: keys of the bins between the signs
-  uint32_t near_n, zeros, largest;  // entries near 0, zeros, and the piece's largest key
-  uint32_t all_near[kMaxCluster], all_zeros[kMaxCluster], all_largest[kMaxCluster];
-  Scale scale;
-  int window;                     // the bins' keys: see key_at
-  u64 scan[kWarps];
-  uint32_t scan_n[kWarps];
-  u64 found_before, word;
-  uint32_t found_key, found_weight, found_n, found_count;
-  uint16_t block[2][kWarps * kRound];  // entries of the drawn value in each block of a round
 };
 
 // ---- cluster ---------------------------------------------------------------
@@ -259,15 +238,6 @@ IPD_DEVINL uint32_t quotient(u64 a, uint32_t w) {
   else if ((u64)(q + 1) * w <= a) ++q;
   return q;
 }
-// f evaluated by one thread for all (fp64 is slow)
-template <typename F>
-IPD_DEVINL u64 once(Shared &S, F f) {
-  __syncthreads();
-  if (threadIdx.x == 0) S.word = f();
-  __syncthreads();
-  return S.word;
-}
-
 // ---- the row -----------------------------------------------------------------
 // A row may start anywhere: it is read as 16-byte vectors from the boundary
 // before it, entry i of the row at i + shift of those.
@@ -308,48 +278,81 @@ IPD_DEVINL int word_at(int window, int p) {
   if (p >= kSide + kMid) return kBins / 2 + ((int)(kLowBits + p - kSide - kMid) & (kBins / 2 - 1));
   return (kFreeWord + ((p - kSide) & (kMid / 2 - 1))) + (p - kSide < kMid / 2 ? 0 : kBins / 2);
 }
-IPD_DEVINL uint32_t key_at(const Shared &S, int window, int p) {
+// What a row takes by blocks of kThreads.
+template <int kThreads>
+struct Sampler {
+static constexpr int kWarps = kThreads / 32;
+static constexpr int kEach = kBins / kThreads;  // bins a thread sums
+static_assert(kEach >= 16 && kEach <= 32, "a thread's bins are searched by one warp");
+
+struct Shared {
+  uint32_t hist[kBins];
+  u64 before[kThreads + 1];       // sums of the bins before a thread's, and of all
+  uint32_t n_before[kThreads + 1];
+  uint16_t near_key[kMid];  // keys of this CTA's entries near 0
+  uint16_t mid_key[kMid];   // first CTA: keys of the bins between the signs
+  uint32_t near_n, zeros, largest;  // entries near 0, zeros, and the piece's largest key
+  uint32_t all_near[kMaxCluster], all_zeros[kMaxCluster], all_largest[kMaxCluster];
+  Scale scale;
+  int window;                     // the bins' keys: see key_at
+  u64 scan[kWarps];
+  uint32_t scan_n[kWarps];
+  u64 found_before, word;
+  uint32_t found_key, found_weight, found_n, found_count;
+  uint16_t block[2][kWarps * kRound];  // entries of the drawn value in each block of a round
+};
+
+// f evaluated by one thread for all (fp64 is slow)
+template <typename F>
+static IPD_DEVINL u64 once(Shared &S, F f) {
+  __syncthreads();
+  if (threadIdx.x == 0) S.word = f();
+  __syncthreads();
+  return S.word;
+}
+
+static IPD_DEVINL uint32_t key_at(const Shared &S, int window, int p) {
   if (window >= 0) return (uint32_t)window * kBins + kBins - 1 - p;
   if (p < kSide) return 0x8000u + kLowBits + kSide - 1 - p;
   if (p >= kSide + kMid) return 0x7fffu - kLowBits - (p - kSide - kMid);
   return S.mid_key[p - kSide];
 }
 static_assert(kSide % kEach == 0 && kMid % (2 * kEach) == 0, "a thread's bins are contiguous words");
-constexpr uint32_t kKeyHigh = 0x8000u + kLowBits + kSide;        // 2^12
-constexpr uint32_t kKeyLow = 0x7fffu - kLowBits - kSide;         // -2^12
+static constexpr uint32_t kKeyHigh = 0x8000u + kLowBits + kSide;        // 2^12
+static constexpr uint32_t kKeyLow = 0x7fffu - kLowBits - kSide;         // -2^12
 
-IPD_DEVINL void shared_add(uint32_t addr, uint32_t v) {
+static IPD_DEVINL void shared_add(uint32_t addr, uint32_t v) {
   asm volatile("red.shared.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
 // the byte offsets of two entries' words
-IPD_DEVINL uint32_t words2(uint32_t w) {
+static IPD_DEVINL uint32_t words2(uint32_t w) {
   return ((w << 2) & 0x3ffc3ffcu) | ((w >> 1) & 0x40004000u);
 }
-IPD_DEVINL uint32_t eq2(uint32_t a, uint32_t b) {  // 0xffff in each half where they are equal
+static IPD_DEVINL uint32_t eq2(uint32_t a, uint32_t b) {  // 0xffff in each half where they are equal
   return __heq2_mask(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b));
 }
 // 0xffff in each half where the entry is near 0, without a bin of its own
-IPD_DEVINL uint32_t near2(uint32_t w) {
+static IPD_DEVINL uint32_t near2(uint32_t w) {
   const __nv_bfloat162 a = __habs2(*reinterpret_cast<__nv_bfloat162 *>(&w));
   const uint32_t low = kLowBits * 0x00010001u;
   return __hlt2_mask(a, *reinterpret_cast<const __nv_bfloat162 *>(&low));
 }
-IPD_DEVINL uint32_t min_abs2(uint32_t a, uint32_t w) {
+static IPD_DEVINL uint32_t min_abs2(uint32_t a, uint32_t w) {
   const __nv_bfloat162 m = __hmin2(*reinterpret_cast<__nv_bfloat162 *>(&a),
                                    __habs2(*reinterpret_cast<__nv_bfloat162 *>(&w)));
   return *reinterpret_cast<const uint32_t *>(&m);
 }
-constexpr uint32_t kLowest2 = (0x8000u | (kLowBits + kSide)) * 0x00010001u;  // -2^12, twice
+static constexpr uint32_t kLowest2 = (0x8000u | (kLowBits + kSide)) * 0x00010001u;  // -2^12, twice
 // Two entries into the histogram.  What is not above -2^12, and NaN, counts as
 // -2^12, whose word is no value's here and is emptied later; what is from 2^12 up
 // shows in the maximum; what is near 0 is taken out again.
-IPD_DEVINL void count2(uint32_t hist, uint32_t w) {
+static IPD_DEVINL void count2(uint32_t hist, uint32_t w) {
   const uint32_t z = words2(max2(w, kLowest2));
   shared_add(hist + (z & 0xffffu), 1u);
   shared_add(hist + (z >> 16), 1u);
 }
 // An entry that was counted, if it is near 0 but not 0, into the list instead.
-__device__ __noinline__ void list_near(Shared &S, uint32_t b) {
+static __device__ __noinline__ void list_near(Shared &S, uint32_t b) {
   const uint32_t a = b & 0x7fffu;
   if (a >= kLowBits || a == 0u) return;
   shared_add(smem_u32(S.hist) + (words2(b) & 0xffffu), 0xffffffffu);
@@ -359,7 +362,7 @@ __device__ __noinline__ void list_near(Shared &S, uint32_t b) {
 
 // Sums over the bins before each thread's, and over all, of the masses into
 // S.before and of the entries with a weight into S.n_before.
-__device__ __noinline__ void sum_bins(Shared &S) {
+static __device__ __noinline__ void sum_bins(Shared &S) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, window = S.window;
   u64 mass = 0;
   uint32_t n = 0;
@@ -414,7 +417,7 @@ __device__ __noinline__ void sum_bins(Shared &S) {
 // The bin that holds position t, which lies in the sums, of the running sum of
 // the entries (`ranks`) or of their masses: into S.found_* its key, its entries
 // and their weight, and the sum and the number of entries above it.
-__device__ __noinline__ void find_bin(Shared &S, bool ranks, u64 t) {
+static __device__ __noinline__ void find_bin(Shared &S, bool ranks, u64 t) {
   const int tid = threadIdx.x, lane = tid & 31, window = S.window;
   const u64 lo = ranks ? S.n_before[tid] : S.before[tid];
   const u64 hi = ranks ? S.n_before[tid + 1] : S.before[tid + 1];
@@ -447,7 +450,7 @@ __device__ __noinline__ void find_bin(Shared &S, bool ranks, u64 t) {
 }
 
 // A vector that the row has a part of.
-__device__ __noinline__ uint4 edge_vector(const uint16_t *base, int v, int shift, int end) {
+static __device__ __noinline__ uint4 edge_vector(const uint16_t *base, int v, int shift, int end) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -459,7 +462,7 @@ __device__ __noinline__ uint4 edge_vector(const uint16_t *base, int v, int shift
 }
 
 // A window's histogram, from the whole row.
-__device__ __noinline__ void count_window(Shared &S, const Row R, int n_vec, int window) {
+static __device__ __noinline__ void count_window(Shared &S, const Row R, int n_vec, int window) {
   __syncthreads();
   for (int i = threadIdx.x; i < kBins; i += kThreads) S.hist[i] = 0u;
   if (threadIdx.x == 0) S.window = window;
@@ -482,7 +485,7 @@ __device__ __noinline__ void count_window(Shared &S, const Row R, int n_vec, int
 // The row's id of entry `rank` (in index order, from vector `first` on) of
 // those with this key: in rounds of kRound blocks a warp, 32 vectors a block,
 // counted and then looked up in the block, by the thread that finds it.
-IPD_DEVINL void look_up(Shared &S, const Row &R, int first, int last, uint32_t key, uint32_t rank,
+static IPD_DEVINL void look_up(Shared &S, const Row &R, int first, int last, uint32_t key, uint32_t rank,
                         int32_t *token) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t want = key_bits(key) * 0x00010001u;
@@ -560,8 +563,7 @@ IPD_DEVINL void look_up(Shared &S, const Row &R, int first, int last, uint32_t k
   }
 }
 
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads)
-    sample_trunc_kernel(const __grid_constant__ Params P) {
+static IPD_DEVINL void run(const Params &P) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Shared &S = *reinterpret_cast<Shared *>(smem_raw);
   const uint32_t rank = cluster_rank(), csize = cluster_size();
@@ -818,6 +820,13 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads)
   look_up(S, R, first, last, key, j, &P.tokens[row]);
   if (csize > 1) cluster_wait();
 }
+};
+
+template <int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads)
+    sample_trunc_kernel(const __grid_constant__ Params P) {
+  Sampler<kThreads>::run(P);
+}
 
 struct DevInfo {
   int sms = 0;
@@ -875,10 +884,15 @@ extern "C" int ipd_sample_trunc(const uint16_t *logits, int64_t row_stride, int 
   P.logp = logp;
   P.vocab = vocab;
   P.piece = (int)(((span + csize - 1) / csize + 7) / 8 * 8);
+  // Threads of a CTA: 512, two CTAs an SM, or 256 and four once there are rows for
+  // them, whose searches overlap more.  512 / 256 threads: 512 rows of 151,936 74.5 /
+  // 75.0 us, of 50,021 39.4 / 33.9, of 4,096 23.4 / 15.8; 256 rows 41.4 / 48.4, 21.0 /
+  // 21.8, 13.1 / 12.1.
+  const bool narrow = n_rows > 2 * D.sms;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)n_rows * csize);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = sizeof(Shared);
+  cfg.blockDim = dim3(narrow ? 256 : 512);
+  cfg.dynamicSmemBytes = narrow ? sizeof(Sampler<256>::Shared) : sizeof(Sampler<512>::Shared);
   cfg.stream = reinterpret_cast<cudaStream_t>(stream);
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -886,7 +900,8 @@ extern "C" int ipd_sample_trunc(const uint16_t *logits, int64_t row_stride, int 
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, sample_trunc_kernel, P) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&cfg, narrow ? sample_trunc_kernel<256> : sample_trunc_kernel<512>, P) !=
+      cudaSuccess) {
     (void)cudaGetLastError();
     return IPD_ERR_CUDA;
   }

@@ -91,3 +91,18 @@ def test_neighbours_of_powers_of_two(lib, sign, e):
     for u in (0.1, 0.5, 0.97):
         for s in ({}, dict(top_k=33), dict(top_p=0.6)):
             _check(lib, rows, u, inv_t=min(1.0, 2.0 ** (5 - e)), **s)
+
+
+@pytest.mark.parametrize("V", [7, 1003, 50021])
+def test_many_rows(lib, V):
+    # more rows than two for each SM
+    g = torch.Generator().manual_seed(V)
+    n = 331
+    rows = (torch.randn(n, V, generator=g) * 2).to(torch.bfloat16).cuda()
+    rows[17] = float("-inf")
+    rows[29] = 0.0
+    rows[31] *= 1e4
+    rng = np.random.default_rng(V)
+    k = rng.integers(0, 60, n).astype(np.int32)
+    p = rng.choice([1.0, 0.9, 0.4], n).astype(np.float32)
+    _check(lib, rows, rng.random(n, dtype=np.float32), top_k=k, top_p=p)
