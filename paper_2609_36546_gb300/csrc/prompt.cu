@@ -115,6 +115,7 @@ struct Params {
   int num_seqs, total, max_len;
   int hq, hkv, group;
   int tile_pos;  // positions of one query tile: floor(128 / group)
+  uint32_t pos_mul, pos_shift;  // n / (2 tile_pos) = (n * mul >> 32) >> shift, n < 2^31
   float scale_log2;
 };
 
@@ -201,40 +202,44 @@ struct ItemFinder {
   int here;           // (sequence, tile) pairs at `level`
   int start, len;     // sequence `lane`, when there are at most 32 (else read again)
 
-  __device__ int tiles(const Params &P, int r, int lane, int pt) {
-    if (P.num_seqs > 32) {
-      int a;
-      return r < P.num_seqs ? (seq_len(P, r, &a) + pt - 1) / pt : 0;
-    }
-    return (len + pt - 1) / pt;
+  int mine;           // ... and its tiles
+
+  static IPD_DEVINL int tiles_of(const Params &P, int len) {
+    return len > 0 ? (int)(__umulhi((uint32_t)len - 1u, P.pos_mul) >> P.pos_shift) + 1 : 0;
   }
-  __device__ void count(const Params &P, int lane, int pt) {
+  __device__ int tiles(const Params &P, int r) {
+    int a;
+    if (P.num_seqs <= 32) return mine;
+    return r < P.num_seqs ? tiles_of(P, seq_len(P, r, &a)) : 0;
+  }
+  __device__ void count(const Params &P, int lane) {
     int n = 0;
-    for (int r = lane; r < P.num_seqs; r += 32) n += tiles(P, r, lane, pt) > level ? 1 : 0;
+    for (int r = lane; r < P.num_seqs; r += 32) n += tiles(P, r) > level ? 1 : 0;
     here = __reduce_add_sync(0xffffffffu, n);
   }
-  __device__ void init(const Params &P, int lane, int pt) {
+  __device__ void init(const Params &P, int lane) {
     start = len = 0;
     if (P.num_seqs <= 32 && lane < P.num_seqs) len = seq_len(P, lane, &start);
+    mine = tiles_of(P, len);
     before = 0;
     int top = 0;
-    for (int r = lane; r < P.num_seqs; r += 32) top = max(top, tiles(P, r, lane, pt));
+    for (int r = lane; r < P.num_seqs; r += 32) top = max(top, tiles(P, r));
     level = __reduce_max_sync(0xffffffffu, top) - 1;  // the highest that has a sequence
     here = 0;
-    if (level >= 0) count(P, lane, pt);
+    if (level >= 0) count(P, lane);
   }
   // the s-th (sequence, tile) pair: its tile (< 0: there is none), and the
   // sequence's place; pairs are asked for in rising order
-  __device__ int find(const Params &P, int lane, int pt, long long s, int *at, int *n) {
+  __device__ int find(const Params &P, int lane, long long s, int *at, int *n) {
     while (level >= 0 && s >= before + here) {
       before += here;
       --level;
-      if (level >= 0) count(P, lane, pt);
+      if (level >= 0) count(P, lane);
     }
     if (level < 0) return -1;
     int rank = (int)(s - before);
     for (int r0 = 0; r0 < P.num_seqs; r0 += 32) {
-      const uint32_t in = __ballot_sync(0xffffffffu, tiles(P, r0 + lane, lane, pt) > level);
+      const uint32_t in = __ballot_sync(0xffffffffu, tiles(P, r0 + lane) > level);
       const int c = __popc(in);
       if (rank < c) {
         const uint32_t hit = __ballot_sync(
@@ -288,15 +293,24 @@ IPD_DEVINL bool send_outputs(const Params &P, Shared &S, uint32_t n, int lane) {
 __device__ void item_warp(const Params &P, Shared &S, int lane) {
   const int pt = 2 * P.tile_pos;
   ItemFinder F;
-  F.init(P, lane, pt);
+  F.init(P, lane);
+  // this CTA's place in the order, n * gridDim.x + blockIdx.x (or the CTAs from
+  // behind, every other round), as a pair and its KV head; the steps to the
+  // next one of an even and an odd round
+  const uint32_t hkv = P.hkv, step0 = 2 * (gridDim.x - blockIdx.x) - 1, step1 = 2 * blockIdx.x + 1;
+  const uint32_t pairs0 = step0 / hkv, pairs1 = step1 / hkv;
+  long long pair = blockIdx.x / hkv;
+  uint32_t head = blockIdx.x % hkv;
   uint32_t n = 0;
   for (;; ++n) {
     const int slot = n % kSlots;
     const uint32_t use = n / kSlots;
-    const long long b = (n & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
-    const long long idx = (long long)n * gridDim.x + b;
     int start = 0, len = 0;
-    const int tile = F.find(P, lane, pt, idx / P.hkv, &start, &len);
+    const int tile = F.find(P, lane, pair, &start, &len);
+    const uint32_t kvh = head;
+    pair += n & 1 ? pairs1 : pairs0;
+    head += n & 1 ? step1 - pairs1 * hkv : step0 - pairs0 * hkv;
+    if (head >= hkv) head -= hkv, ++pair;
     const bool ok = tile >= 0;
     // the item that had the slot before
     if (use > 0 && !send_outputs(P, S, n - kSlots, lane)) return;
@@ -309,7 +323,7 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
         I.start = start;
         I.len = len;
         I.pos = tile * pt;
-        I.kvh = (int)(idx % P.hkv);
+        I.kvh = (int)kvh;
         for (int t = 0; t < 2; ++t) {
           const int p0 = I.pos + t * P.tile_pos, p1 = min(I.len, p0 + P.tile_pos);
           I.nk[t] = p0 < I.len ? (p1 + kKeys - 1) / kKeys : 0;
@@ -948,6 +962,13 @@ extern "C" int ipd_prompt_attn(const ipd_prompt_args *args, ipd_stream_t stream)
   Params P;
   memset(&P, 0, sizeof(P));
   P.tile_pos = kRows / group;
+  {
+    const uint32_t d = 2u * (uint32_t)P.tile_pos;  // 2 .. 256
+    uint32_t k = 1;
+    while ((1u << k) < d) ++k;
+    P.pos_mul = (uint32_t)((((uint64_t)1 << (31 + k)) + d - 1) / d);
+    P.pos_shift = k - 1;
+  }
   if (encode(&P.q, a.q, a.num_q_heads, a.total, a.q_stride, group, P.tile_pos) != IPD_OK ||
       encode(&P.k, a.k, a.num_kv_heads, a.total, a.k_stride, 1, kKeys) != IPD_OK ||
       encode(&P.v, a.v, a.num_kv_heads, a.total, a.v_stride, 1, kKeys) != IPD_OK ||
