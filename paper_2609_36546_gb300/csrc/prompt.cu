@@ -769,11 +769,15 @@ __device__ void softmax_warps(const Params &P, Shared &S, int t, int warp, int l
         f2_unpack(f2_add(sum[0], sum[1]), a, b);
         l += a + b;
       }
+      // while the last product runs
+      const float inv = 1.f / l;
+      if (live && P.lse)
+        P.lse[(long long)(I.kvh * P.group + row_head) * P.total + I.start + pos] =
+            (m == -INFINITY ? -INFINITY : (m * c + log2f(l)) * kLn2);
       if (!wait_warp(&S.o_full[t], full_parity(n_o), &S.abort)) return;
       ++n_o;
       tc_fence_after();
       const bool bad = *(volatile int *)&S.item[slot].bad != 0;
-      const float inv = 1.f / l;
       uint16_t *out = P.out + (long long)(I.start + pos) * P.out_stride +
                       (long long)(I.kvh * P.group + row_head) * kD;
       uint32_t w[64];
@@ -811,9 +815,6 @@ __device__ void softmax_warps(const Params &P, Shared &S, int t, int warp, int l
               make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
       }
       if (bad && live) add_not_finite(P, I, pos, out);
-      if (live && P.lse)
-        P.lse[(long long)(I.kvh * P.group + row_head) * P.total + I.start + pos] =
-            (m == -INFINITY ? -INFINITY : (m * c + log2f(l)) * kLn2);
     }
     const bool last_item = !I.valid;
     if (!last_item && !leaves(P, I, t)) {  // the buffer passes by
