@@ -42,12 +42,13 @@
 // Items go out by a fixed order, longest first, back and forth over the CTAs;
 // claiming them as CTAs come free gained nothing.
 //
-// Measured (GB300, device time): one sequence of 8,192, 32 / 4 heads, 550 GFLOP: 340
-// us, 1,618 TFLOP/s, 85 % of the measured bf16 GEMM rate; tensor pipe busy 69 % of
+// Measured (GB300, device time): one sequence of 8,192, 32 / 4 heads, 550 GFLOP: 337
+// us, 1,632 TFLOP/s, 85 % of the measured bf16 GEMM rate; tensor pipe busy 69 % of
 // cycles, the rest the hand-over of scores and P.  24 sequences of 0 to 900, 16 /
-// 8 heads, 22.7 GFLOP: 41 us, 550 TFLOP/s; there an item is two or three key tiles,
-// and its start and end (loads, first scores, output) are not all hidden.  One
-// sequence of 29: 8.2 us, launch and one pass through the pipeline.
+// 8 heads, 22.7 GFLOP: 40 us, 561 TFLOP/s; there an item is two or three key tiles,
+// and a tile's end (its last product, the output, the way back to the first scores,
+// about 3,000 cycles with instruction misses) is not all hidden.  One sequence of
+// 29: 7.6 us, launch and one pass through the pipeline.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cudaTypedefs.h>
