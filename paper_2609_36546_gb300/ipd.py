@@ -209,9 +209,11 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+_F32, _BF16, _I32 = torch.float32, torch.bfloat16, torch.int32
 # the raw handle of the current stream, without the objects around it (a few
 # microseconds a call; the small operators run for as little)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _on_gpu = False  # set once a device has been seen
 
 
@@ -224,7 +226,7 @@ def _stream(stream) -> Optional[int]:
             torch.cuda.current_stream()  # initialises CUDA in this process
             _on_gpu = True
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_device())
         return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
@@ -492,7 +494,7 @@ def _rows(t: torch.Tensor, shape, dtype, what: str) -> int:
         _refuse(what)
     n, h, d = shape
     s0, s1, s2 = t.stride()
-    if (d > 1 and s2 != 1) or (h > 1 and s1 != d):
+    if (s2 != 1 or s1 != d) and ((d > 1 and s2 != 1) or (h > 1 and s1 != d)):
         _refuse(what)
     return s0 if n > 1 else h * d
 
@@ -500,7 +502,7 @@ def _rows(t: torch.Tensor, shape, dtype, what: str) -> int:
 def _check_table(table: torch.Tensor, what: str):
     """(positions, rotated entries) of a rotary table."""
     s = table.shape
-    if table.dtype is not torch.float32 or len(s) != 3 or s[2] != 2 or not table.is_contiguous():
+    if len(s) != 3 or s[2] != 2 or table.dtype is not _F32 or not table.is_contiguous():
         _refuse(what)
     return s[0], 2 * s[1]
 
@@ -524,14 +526,14 @@ def rope(x: torch.Tensor, out: torch.Tensor, pos: torch.Tensor, table: torch.Ten
     their positions ``pos`` (int32 [n]) into ``out`` (may be ``x``); ``inverse``
     applies the transpose, the rotation's gradient."""
     max_pos, rot = _check_table(table, "ipd_rope: table")
-    shape, dt = x.shape, x.dtype
-    if len(shape) != 3 or dt not in (torch.float32, torch.bfloat16) or \
-            pos.dtype is not torch.int32 or pos.shape != shape[:1] or not pos.is_contiguous():
+    shape, dt = tuple(x.shape), x.dtype
+    if len(shape) != 3 or (dt is not _BF16 and dt is not _F32) or pos.dtype is not _I32 or \
+            pos.shape != shape[:1] or not pos.is_contiguous():
         _refuse("ipd_rope: shapes or types")
     n, h, d = shape
     a = _PACK_ROPE.pack(x.data_ptr(), out.data_ptr(), _rows(x, shape, dt, "ipd_rope: x"),
                         _rows(out, shape, dt, "ipd_rope: out"), pos.data_ptr(), table.data_ptr(),
-                        DTYPE_BF16 if dt is torch.bfloat16 else DTYPE_F32, n, h, d, max_pos, rot,
+                        DTYPE_BF16 if dt is _BF16 else DTYPE_F32, n, h, d, max_pos, rot,
                         layout, 1 if inverse else 0)
     _check(_lib.ipd_rope(a, _stream(stream)), "ipd_rope")
 
@@ -544,17 +546,17 @@ def rope_append(cache: "KVCache", q: Optional[torch.Tensor], q_out: Optional[tor
     ``k_out``), and writes their values beside them: kv_append of the rotated
     rows in one launch.  Each row's position is its place in its sequence."""
     max_pos, rot = _check_table(table, "ipd_rope_append: table")
-    bf, kp, kshape = torch.bfloat16, cache.k_pages, k_new.shape
+    bf, kp, kshape = _BF16, cache.k_pages, tuple(k_new.shape)
     pages, hkv, ps, hd = kp.shape
     n, hq = kshape[0], 0
     q_ptr = qo_ptr = ko_ptr = qs = qos = kos = 0
-    if len(kshape) != 3 or kshape[1] != hkv or kshape[2] != 128 or (q is None) != (q_out is None):
+    if kshape != (n, hkv, 128) or (q is None) != (q_out is None):
         _refuse("ipd_rope_append: shapes")
     if q is not None:
-        qshape = q.shape
-        if len(qshape) != 3 or qshape[0] != n or qshape[2] != 128:
+        qshape = tuple(q.shape)
+        hq = qshape[1] if len(qshape) == 3 else 0
+        if qshape != (n, hq, 128):
             _refuse("ipd_rope_append: q")
-        hq = qshape[1]
         q_ptr, qs = q.data_ptr(), _rows(q, qshape, bf, "ipd_rope_append: q")
         qo_ptr, qos = q_out.data_ptr(), _rows(q_out, qshape, bf, "ipd_rope_append: q_out")
     if k_out is not None:
@@ -575,9 +577,9 @@ def prompt_attn(q, k, v, cu_seq, max_len: int, out, softmax_scale: float,
     [total, Hkv, 128], out [total, Hq, 128] bf16 (rows contiguous, any row
     stride), cu_seq int32 [num_seqs + 1] (device), ``max_len`` a host-known
     bound on the lengths; lse fp32 [Hq, total] when given."""
-    shape, kshape, bf = q.shape, k.shape, torch.bfloat16
+    shape, kshape, bf = tuple(q.shape), tuple(k.shape), _BF16
     if len(shape) != 3 or len(kshape) != 3 or kshape[0] != shape[0] or kshape[2] != shape[2] or \
-            cu_seq.dtype is not torch.int32 or not cu_seq.is_contiguous():
+            cu_seq.dtype is not _I32 or not cu_seq.is_contiguous():
         _refuse("ipd_prompt_attn: shapes or types")
     n, hq, d = shape
     if lse is not None and (lse.shape != (hq, n) or lse.dtype is not torch.float32 or
@@ -603,9 +605,8 @@ def sample_trunc(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor,
     (fp32 [n]) after the rows' own settings (fp32 [n]; ``top_k`` int32 [n]);
     ``logp`` (fp32) and ``n_kept`` (int32) take the log-probability of the token
     among the kept entries and their number."""
-    n, V = shape = logits.shape
-    one = shape[:1]
-    f, i = torch.float32, torch.int32
+    n, V = logits.shape
+    one, f, i = (n,), _F32, _I32
     for t, dt in ((u, f), (tokens, i), (inv_temperature, f), (top_k, i), (top_p, f), (min_p, f),
                   (logp, f), (n_kept, i)):
         if t is not None and (t.shape != one or t.dtype is not dt or not t.is_contiguous()):
