@@ -97,9 +97,11 @@ IPD_DEVINL uint32_t cluster_size() {
   return r;
 }
 IPD_DEVINL void cluster_arrive() {
+  __syncwarp();  // (both are for whole warps)
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
 IPD_DEVINL void cluster_wait() {
+  __syncwarp();
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 IPD_DEVINL void cluster_sync() {
