@@ -34,14 +34,14 @@
 // of 2^13 bins over all 2^16 values, a pass over the row for each.
 //
 // What bounds it (GB300, device time).  Many rows: the pass over the entries.  512
-// rows of 151,936 take 75 us (2.1 TB/s): the pass alone 50, 29 without its atomics
+// rows of 151,936 take 73 us (2.1 TB/s): the pass alone 50, 29 without its atomics
 // (5.4 TB/s); random words put three to four of a warp's 32 atomics on one bank, and
 // the instructions of the pass (six an entry) and of the searches keep two thirds of
 // the issue slots busy.  Entries near 0 and below the range are kept out of the
 // common path: it has no branch and no predicate.  Few rows: a chain of barriers.  One
-// row of 151,936 takes 13.7 us: reading it 2.2, the cluster's barriers and the sum
-// of its histograms 3, the bins' weights and sums 2.2, the searches 3, the look-up 2;
-// 64 rows take 20.5 us, 33 rows of 50,021 12.4.  A sorted head of the row with the
+// row of 151,936 takes 13.3 us: reading it 2.2, the cluster's barriers and the sum
+// of its histograms 3, the bins' weights and sums 1.8, the searches 3, the look-up 2;
+// 64 rows take 20.3 us, 33 rows of 50,021 12.0.  A sorted head of the row with the
 // searches as the exception took 20.5 us for one row and 174 for 512.  Rows outside
 // the bins' range: 70 to 80 us with a maximum there, 210 with all of it near 0.
 #include <cuda_bf16.h>
@@ -381,25 +381,24 @@ static __device__ __noinline__ void sum_bins(Shared &S) {
   u64 mass = 0;
   uint32_t n = 0;
   const Scale C = S.scale;
+  // the thread's words, from the lowest on, and the bf16 bits of their values, which
+  // follow one another, but between the signs
+  const int p0 = kEach * tid;
+  const bool mids = window < 0 && p0 >= kSide && p0 < kSide + kMid;
+  const int wa = word_at(window, p0), wb = word_at(window, p0 + kEach - 1), word0 = min(wa, wb);
+  const uint32_t bits0 = key_bits(key_at(S, window, wa < wb ? p0 : p0 + kEach - 1));
+  const uint32_t step = window >= 0 && (bits0 & 0x8000u) ? 0xffffffffu : 1u;
 #pragma unroll 1
   for (int q = 0; q < kEach / 4; ++q) {
     // four bins, in an order that spreads a warp's over the banks
-    const int p = kEach * tid + 4 * ((q + lane / (32 / kEach)) & (kEach / 4 - 1));
-    const int a = word_at(window, p), b = word_at(window, p + 3);
-    const uint4 c = *reinterpret_cast<const uint4 *>(&S.hist[min(a, b)]);
+    const int o = 4 * ((q + lane / (32 / kEach)) & (kEach / 4 - 1));
+    const uint4 c = *reinterpret_cast<const uint4 *>(&S.hist[word0 + o]);
     if (!(c.x | c.y | c.z | c.w)) continue;
-    // their values: bf16 bits that follow one another, but between the signs
-    const uint32_t bits = key_bits(key_at(S, window, a < b ? p : p + 3));
-    uint32_t v01 = bits * 0x00010001u, v23;
-    if (window < 0 && p >= kSide && p < kSide + kMid) {
-      v01 = bits | key_bits(key_at(S, window, p + 1)) << 16;
-      v23 = key_bits(key_at(S, window, p + 2)) | key_bits(key_at(S, window, p + 3)) << 16;
-    } else if (window >= 0 && (bits & 0x8000u)) {
-      v01 -= 0x00010000u;
-      v23 = v01 - 0x00020002u;
-    } else {
-      v01 += 0x00010000u;
-      v23 = v01 + 0x00020002u;
+    uint32_t v01 = (bits0 + step * o) * 0x00010001u + (step << 16), v23 = v01 + step * 0x00020002u;
+    if (mids) {
+      const uint16_t *k = &S.mid_key[p0 - kSide + o];
+      v01 = key_bits(k[0]) | key_bits(k[1]) << 16;
+      v23 = key_bits(k[2]) | key_bits(k[3]) << 16;
     }
     uint32_t w0, w1, w2, w3;
     weights(C, v01, w0, w1);
