@@ -34,14 +34,15 @@
 // of 2^13 bins over all 2^16 values, a pass over the row for each.
 //
 // What bounds it (GB300, device time).  Many rows: the pass over the entries.  512
-// rows of 151,936 take 73 us (2.1 TB/s): the pass alone 50, 29 without its atomics
-// (5.4 TB/s); random words put three to four of a warp's 32 atomics on one bank, and
-// the instructions of the pass (six an entry) and of the searches keep two thirds of
-// the issue slots busy.  Entries near 0 and below the range are kept out of the
+// rows of 151,936 take 69 us (2.2 TB/s).  All are in flight at once: the pass takes
+// about 32 us of a row's life (half of that without its atomics: random words put
+// three to four of a warp's 32 on one bank), the searches 8, the look-up up to 20 for
+// an entry far down the row; the last rows' searches and look-ups have nothing left
+// to hide behind.  Entries near 0 and below the range are kept out of the
 // common path: it has no branch and no predicate.  Few rows: a chain of barriers.  One
-// row of 151,936 takes 13.3 us: reading it 2.2, the cluster's barriers and the sum
+// row of 151,936 takes 13.2 us: reading it 2.2, the cluster's barriers and the sum
 // of its histograms 3, the bins' weights and sums 1.8, the searches 3, the look-up 2;
-// 64 rows take 20.3 us, 33 rows of 50,021 12.0.  A sorted head of the row with the
+// 64 rows take 20.1 us, 33 rows of 50,021 12.0.  A sorted head of the row with the
 // searches as the exception took 20.5 us for one row and 174 for 512.  Rows outside
 // the bins' range: 70 to 80 us with a maximum there, 210 with all of it near 0.
 #include <cuda_bf16.h>
@@ -511,23 +512,20 @@ static IPD_DEVINL void look_up(Shared &S, const Row &R, int first, int last, uin
   };
   const auto cut = [&](int v) { return v < last && R.cut(v); };
   constexpr int kMine = kWarps * kRound / 32;  // blocks a lane sums
-  static_assert(kRound % kBatch == 0 && kWarps * kRound % 32 == 0, "rounds of whole batches");
+  static_assert(kWarps * kRound % 32 == 0, "whole lanes of blocks");
   int round = 0;
 #pragma unroll 1
   for (int v1 = first; v1 < last; v1 += kWarps * kRound * 32, round ^= 1) {
-#pragma unroll 1
-    for (int b0 = 0; b0 < kRound; b0 += kBatch) {
-      uint4 x[kBatch];
-      const int v0 = v1 + (warp * kRound + b0) * 32 + lane;
+    uint4 part[kRound];  // all in flight at once
+    const int v0 = v1 + warp * kRound * 32 + lane;
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) x[b] = R.load(v0 + 32 * b, last);
+    for (int b = 0; b < kRound; ++b) part[b] = R.load(v0 + 32 * b, last);
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        if (cut(v0 + 32 * b)) x[b] = edge_vector(R.base, v0 + 32 * b, R.shift, R.end);
-        __syncwarp();
-        const uint32_t n = __reduce_add_sync(0xffffffffu, __popc(match(x[b])));
-        if (lane == 0) S.block[round][warp * kRound + b0 + b] = (uint16_t)n;
-      }
+    for (int b = 0; b < kRound; ++b) {
+      if (cut(v0 + 32 * b)) part[b] = edge_vector(R.base, v0 + 32 * b, R.shift, R.end);
+      __syncwarp();
+      const uint32_t n = __reduce_add_sync(0xffffffffu, __popc(match(part[b])));
+      if (lane == 0) S.block[round][warp * kRound + b] = (uint16_t)n;
     }
     __syncthreads();
     // every warp finds the block for itself
