@@ -544,11 +544,24 @@ def rope_append(cache: "KVCache", q: Optional[torch.Tensor], q_out: Optional[tor
     """Rotates the new tokens' queries ([n, Hq, 128] bf16, or None) into
     ``q_out`` and their keys ([n, Hkv, 128]) into the cache's pages (and
     ``k_out``), and writes their values beside them: kv_append of the rotated
-    rows in one launch.  Each row's position is its place in its sequence."""
+    rows in one launch.  Each row's position is its place in its sequence.
+    ``cu_new`` [R + 1], ``seq_len`` [R] and ``page_table`` [R, max_pages] are
+    contiguous int32 (the last two may hold more rows than R, not fewer)."""
     max_pos, rot = _check_table(table, "ipd_rope_append: table")
-    bf, kp, kshape = _BF16, cache.k_pages, tuple(k_new.shape)
-    pages, hkv, ps, hd = kp.shape
-    n, hq = kshape[0], 0
+    bf, kp, vp, kshape = _BF16, cache.k_pages, cache.v_pages, tuple(k_new.shape)
+    pshape = kp.shape
+    pages, hkv, ps, hd = pshape
+    n, hq, R = kshape[0], 0, cu_new.numel() - 1
+    # what goes on as a bare pointer is read and written as laid out here
+    if kp.dtype is not bf or vp.dtype is not bf or vp.shape != pshape or \
+            not kp.is_contiguous() or not vp.is_contiguous():
+        _refuse("ipd_rope_append: pools")
+    tshape = page_table.shape
+    if cu_new.dtype is not _I32 or seq_len.dtype is not _I32 or page_table.dtype is not _I32 or \
+            cu_new.dim() != 1 or R < 0 or seq_len.numel() < R or len(tshape) != 2 or \
+            tshape[0] < R or not cu_new.is_contiguous() or not seq_len.is_contiguous() or \
+            not page_table.is_contiguous():
+        _refuse("ipd_rope_append: offsets, lengths or page table")
     q_ptr = qo_ptr = ko_ptr = qs = qos = kos = 0
     if kshape != (n, hkv, 128) or (q is None) != (q_out is None):
         _refuse("ipd_rope_append: shapes")
@@ -565,9 +578,9 @@ def rope_append(cache: "KVCache", q: Optional[torch.Tensor], q_out: Optional[tor
         q_ptr, k_new.data_ptr(), v_new.data_ptr(), qo_ptr, ko_ptr, qs,
         _rows(k_new, kshape, bf, "ipd_rope_append: k_new"),
         _rows(v_new, kshape, bf, "ipd_rope_append: v_new"), qos, kos, kp.data_ptr(),
-        cache.v_pages.data_ptr(), pages, cu_new.data_ptr(), seq_len.data_ptr(),
-        page_table.data_ptr(), table.data_ptr(), hq, hkv, ps, hd, page_table.shape[1],
-        cu_new.shape[0] - 1, n, max_pos, rot, layout)
+        vp.data_ptr(), pages, cu_new.data_ptr(), seq_len.data_ptr(),
+        page_table.data_ptr(), table.data_ptr(), hq, hkv, ps, hd, tshape[1],
+        R, n, max_pos, rot, layout)
     _check(_lib.ipd_rope_append(a, _stream(stream)), "ipd_rope_append")
 
 
