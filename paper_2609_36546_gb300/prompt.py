@@ -40,6 +40,8 @@ class PromptPass:
             raise ValueError(f"a prompt of {max(lens)} tokens is longer than the rotary table")
         if page_table.shape[0] != len(lens):
             raise ValueError("one row of the page table a prompt")
+        if lens and max(lens) > 16 * page_table.shape[1]:
+            raise ValueError(f"a prompt of {max(lens)} tokens does not fit the page table's row")
         dev = torch.device(device)
         self.cache, self.table, self.layout, self.scale = cache, table, layout, scale
         self.lens, self.total, self.max_len = lens, sum(lens), max(lens, default=0)
