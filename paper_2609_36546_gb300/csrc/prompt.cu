@@ -55,9 +55,14 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 IPD_DECLARE_ERROR_WORD(g_prompt_err);
+// whether this process has launched (or captured) a kernel that may set the word:
+// a program without these calls does not pay for reading it
+static std::atomic<bool> g_prompt_used{false};
 
 namespace {
 
@@ -932,6 +937,7 @@ int encode(CUtensorMap *m, const void *base, int heads, int tokens, long long st
 }  // namespace
 
 extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_prompt_error() {
+  if (!g_prompt_used.load(std::memory_order_relaxed)) return 0u;
   unsigned int v = 0, z = 0;
   if (cudaMemcpyFromSymbol(&v, g_prompt_err, sizeof(v)) != cudaSuccess) return 0xffffffffu;
   if (cudaMemcpyToSymbol(g_prompt_err, &z, sizeof(z)) != cudaSuccess) return 0xffffffffu;
@@ -993,6 +999,7 @@ extern "C" int ipd_prompt_attn(const ipd_prompt_args *args, ipd_stream_t stream)
   const long long pt = 2 * P.tile_pos;
   const long long items = ((long long)a.total / pt + a.num_seqs) * a.num_kv_heads;
   const int grid = (int)(items < sms ? items : sms);
+  g_prompt_used.store(true, std::memory_order_relaxed);
   prompt_attn_kernel<<<grid, kThreads, kSharedBytes, reinterpret_cast<cudaStream_t>(stream)>>>(P);
   return cudaGetLastError() == cudaSuccess ? IPD_OK : IPD_ERR_CUDA;
 }

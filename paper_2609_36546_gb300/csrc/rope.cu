@@ -27,9 +27,14 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 IPD_DECLARE_ERROR_WORD(g_rope_err);
+// whether this process has launched (or captured) a kernel that may set the word:
+// a program without these calls does not pay for reading it
+static std::atomic<bool> g_rope_used{false};
 
 namespace {
 
@@ -363,6 +368,7 @@ int launch_rope(const ipd_rope_args &a, cudaStream_t st) {
   P.split = head_split(a.n_tokens, a.n_heads, P.hsplit);
   const long long warps = (long long)a.n_tokens * P.split;
   const unsigned grid = (unsigned)((warps + kRopeWarps - 1) / kRopeWarps);
+  g_rope_used.store(true, std::memory_order_relaxed);
   if (vec) rope_kernel<T, true><<<grid, kRopeThreads, 0, st>>>(P);
   else rope_kernel<T, false><<<grid, kRopeThreads, 0, st>>>(P);
   return cudaGetLastError() == cudaSuccess ? IPD_OK : IPD_ERR_CUDA;
@@ -371,6 +377,7 @@ int launch_rope(const ipd_rope_args &a, cudaStream_t st) {
 }  // namespace
 
 extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_rope_error() {
+  if (!g_rope_used.load(std::memory_order_relaxed)) return 0u;
   unsigned int v = 0, z = 0;
   if (cudaMemcpyFromSymbol(&v, g_rope_err, sizeof(v)) != cudaSuccess) return 0xffffffffu;
   if (cudaMemcpyToSymbol(g_rope_err, &z, sizeof(z)) != cudaSuccess) return 0xffffffffu;
@@ -477,6 +484,7 @@ extern "C" int ipd_rope_append(const ipd_rope_append_desc *desc, ipd_stream_t st
   const long long warps = (long long)a.total_new * P.split;
   const unsigned grid = (unsigned)((warps + kRopeWarps - 1) / kRopeWarps);
   const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  g_rope_used.store(true, std::memory_order_relaxed);
   if (vec) rope_append_kernel<true><<<grid, kRopeThreads, 0, s>>>(P);
   else rope_append_kernel<false><<<grid, kRopeThreads, 0, s>>>(P);
   return cudaGetLastError() == cudaSuccess ? IPD_OK : IPD_ERR_CUDA;

@@ -49,9 +49,14 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 IPD_DECLARE_ERROR_WORD(g_trunc_err);
+// whether this process has launched (or captured) a kernel that may set the word:
+// a program without these calls does not pay for reading it
+static std::atomic<bool> g_trunc_used{false};
 
 namespace {
 
@@ -847,6 +852,7 @@ DevInfo g_trunc_dev[64];
 }  // namespace
 
 extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_trunc_error() {
+  if (!g_trunc_used.load(std::memory_order_relaxed)) return 0u;
   unsigned int v = 0, z = 0;
   if (cudaMemcpyFromSymbol(&v, g_trunc_err, sizeof(v)) != cudaSuccess) return 0xffffffffu;
   if (cudaMemcpyToSymbol(g_trunc_err, &z, sizeof(z)) != cudaSuccess) return 0xffffffffu;
@@ -911,6 +917,7 @@ extern "C" int ipd_sample_trunc(const uint16_t *logits, int64_t row_stride, int 
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
+  g_trunc_used.store(true, std::memory_order_relaxed);
   if (cudaLaunchKernelEx(&cfg, narrow ? sample_trunc_kernel<256> : sample_trunc_kernel<512>, P) !=
       cudaSuccess) {
     (void)cudaGetLastError();
