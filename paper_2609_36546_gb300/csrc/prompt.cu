@@ -119,7 +119,7 @@ struct Params {
   float *lse;
   const int32_t *cu;
   int num_seqs, total, max_len;
-  int hq, hkv, group;
+  int hkv, group;
   int tile_pos;  // positions of one query tile: floor(128 / group)
   uint32_t pos_mul, pos_shift;  // n / (2 tile_pos) = (n * mul >> 32) >> shift, n < 2^31
   float scale_log2;
@@ -991,7 +991,6 @@ extern "C" int ipd_prompt_attn(const ipd_prompt_args *args, ipd_stream_t stream)
   P.num_seqs = a.num_seqs;
   P.total = a.total;
   P.max_len = a.max_len;
-  P.hq = a.num_q_heads;
   P.hkv = a.num_kv_heads;
   P.group = group;
   P.scale_log2 = a.softmax_scale * kLog2e;
