@@ -583,7 +583,9 @@ int ipd_rope_append(const ipd_rope_append_desc *desc, ipd_stream_t stream);
  * Pointers 16-byte aligned, strides multiples of 8 entries.  out must overlap
  * none of q, k, v.  A sequence whose offsets are out of order or past total
  * (IPD_DEVERR_SPAN) or that is longer than max_len (IPD_DEVERR_SEQ_LEN) is
- * recorded and left out.  No workspace.  Returns IPD_ERR_UNSUPPORTED unless
+ * recorded and left out.  With max_len, total or num_seqs 0 there is nothing to
+ * do: the offsets are not looked at, nothing is written and nothing recorded.
+ * No workspace.  Returns IPD_ERR_UNSUPPORTED unless
  * head_dim == 128 and num_q_heads / num_kv_heads <= 128, IPD_ERR_INVALID_ARG
  * for a missing or misaligned pointer, a stride shorter than a row, heads that
  * do not divide or a scale that is not positive and finite.

@@ -21,7 +21,8 @@
 // While one warpgroup exponentiates its tile, the tensor cores work on the
 // other's products.  P is rounded to bf16 (to nearest) for the second product,
 // the operand type of V: a relative error of at most 2^-8 a term, the size of
-// the output's own rounding; sums, maxima and O stay in fp32.  O is rescaled only
+// the output's own rounding; sums (of P before that rounding), maxima and O stay
+// in fp32.  O is rescaled only
 // when a row's maximum has grown by more than 2^8 since the last time (the
 // running maximum only has to keep the exponentials in range).
 //
@@ -42,13 +43,16 @@
 // Items go out by a fixed order, longest first, back and forth over the CTAs;
 // claiming them as CTAs come free gained nothing.
 //
-// Measured (GB300, device time): one sequence of 8,192, 32 / 4 heads, 550 GFLOP: 337
-// us, 1,632 TFLOP/s, 85 % of the measured bf16 GEMM rate; tensor pipe busy 69 % of
-// cycles, the rest the hand-over of scores and P.  24 sequences of 0 to 900, 16 /
+// Measured (GB300, device time): one sequence of 8,192, 32 / 4 heads, 550 GFLOP: 337 to
+// 341 us in runs of some 20 to 100 calls (1,632 to 1,612 TFLOP/s, 85 % of the measured
+// bf16 GEMM rate), 361 to 363 in runs of seconds, where the power cap holds the clock
+// at 1,935 MHz (1,515 TFLOP/s, 88 % of the sustained GEMM rate), up to 373 in a run of
+// three calls; tensor pipe busy 69 % of cycles, the rest the hand-over of scores and
+// P.  24 sequences of 0 to 900, 16 /
 // 8 heads, 22.7 GFLOP: 40 us, 561 TFLOP/s; there an item is two or three key tiles,
 // and a tile's end (its last product, the output, the way back to the first scores,
 // about 3,000 cycles with instruction misses) is not all hidden.  One sequence of
-// 29: 7.6 us, launch and one pass through the pipeline.
+// 29: 7.4 to 7.6 us, launch and one pass through the pipeline.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cudaTypedefs.h>
@@ -202,6 +206,12 @@ IPD_DEVINL int seq_len(const Params &P, int r, int *start) {
 // sequences that reach a level in order, KV heads innermost.  The CTAs take
 // them round by round, every other round backwards, so that the rounds'
 // differences cancel.
+//
+// Up to 32 sequences stay in the warp's registers.  With more, each item is
+// looked for from sequence 0 on, two offsets read again for each, so that the
+// search grows with the square of their number and is what bounds a call of
+// hundreds of short ones: 32 / 33 / 333 / 1,024 / 4,000 sequences of 1 to 40, 16 / 8
+// heads, take 12.0 / 12.6 / 76 / 332 / 3,838 us, 512 / 1,024 of 20 to 300 305 / 763.
 struct ItemFinder {
   int level;          // items below `before` lie at higher levels
   long long before;

@@ -42,7 +42,8 @@ constexpr int kRopeThreads = 64;
 constexpr int kRopeWarps = kRopeThreads / 32;
 constexpr int kUnroll = 4;        // heads in flight per lane
 constexpr int kMaxFreqs = 128;    // rot_dim <= 256
-constexpr int kTargetWarps = 152 * 8;  // warps below which a token's heads are split over several
+// warps below which a token's heads are split over several: 8 for each SM of a GB300
+constexpr int kTargetWarps = 152 * 8;
 
 __host__ __device__ constexpr int ceil_div(int a, int b) { return (a + b - 1) / b; }
 

@@ -39,7 +39,8 @@
 // three to four of a warp's 32 on one bank), the searches 8, the look-up up to 20 for
 // an entry far down the row; the last rows' searches and look-ups have nothing left
 // to hide behind.  Entries near 0 and below the range are kept out of the
-// common path: it has no branch and no predicate.  Few rows: a chain of barriers.  One
+// common path: it has no branch for an entry, and one for a thread's batch of 32 (is
+// one of them near 0).  Few rows: a chain of barriers.  One
 // row of 151,936 takes 13.2 us: reading it 2.2, the cluster's barriers and the sum
 // of its histograms 3, the bins' weights and sums 1.8, the searches 3, the look-up 2;
 // 64 rows take 20.1 us, 33 rows of 50,021 12.0.  A sorted head of the row with the
@@ -878,11 +879,13 @@ extern "C" int ipd_sample_trunc(const uint16_t *logits, int64_t row_stride, int 
     D.sms = n;
   }
   // CTAs of a row.  A cluster's barriers and the sum of its histograms cost about
-  // 4 us, a CTA alone 0.12 us per 1,024 entries: clusters are for long rows, and while
-  // every CTA has an SM (clusters of 8 do not fill the SMs evenly).  Measured with
-  // 1 / 2 / 4 / 8 CTAs: 1 row of 151,936 25.9 / 19.9 / 15.5 / 14.6 us, 16 rows 27.6 /
-  // 21.1 / 16.9 / 19.0, 64 rows 28.0 / 21.7 / 22.7 / 34.6; 1 row of 50,021 14.0 / 13.9 /
-  // 12.8 / 13.1, of 32,000 11.5 / 12.7 / 12.7 / 13.0.
+  // 3 us, a CTA alone 0.1 us per 1,024 entries: clusters are for long rows, and while
+  // every CTA has an SM (clusters of 8 do not fill the SMs evenly).  Measured on rows
+  // of mixed settings with 1 / 2 / 4 / 8 CTAs, in us, 151,936 entries: 1 row 23.1 / 18.6
+  // / 14.9 / 14.0, 16 rows 25.0 / 19.9 / 15.6 / 18.1, 48 rows 24.8 / 20.0 / 20.7 / 29.3, 64
+  // rows 25.1 / 20.3 / 21.5 / 33.0, 77 rows 24.9 / 26.0 / 28.8 / 40.3 (two CTAs an SM gain
+  // nothing), 152 rows 28.7 / 29.2 / 46.8 / 72.4; 50,021: 1 row 12.7 / 13.2 / 12.5 / 12.6, 77
+  // rows 14.3 / 17.9 / 23.4 / 35.5; 32,000: 1 row 10.8 / 12.3 / 12.3 / 12.4.
   const int span = vocab + 7;  // a row may start inside a 16-byte vector
   int csize = kMaxCluster;
   while (csize > 1 && (span < kSplitRow || span < csize * kMinPiece ||
@@ -902,9 +905,9 @@ extern "C" int ipd_sample_trunc(const uint16_t *logits, int64_t row_stride, int 
   P.vocab = vocab;
   P.piece = (int)(((span + csize - 1) / csize + 7) / 8 * 8);
   // Threads of a CTA: 512, two CTAs an SM, or 256 and four once there are rows for
-  // them, whose searches overlap more.  512 / 256 threads: 512 rows of 151,936 74.5 /
-  // 75.0 us, of 50,021 39.4 / 33.9, of 4,096 23.4 / 15.8; 256 rows 41.4 / 48.4, 21.0 /
-  // 21.8, 13.1 / 12.1.
+  // them, whose searches overlap more.  512 / 256 threads: 512 rows of 151,936 72.1 /
+  // 69.9 us, of 50,021 38.8 / 32.2, of 4,096 22.7 / 15.3; 400 rows 66.9 / 58.2, 34.4 / 26.6,
+  // 19.4 / 12.8; 304 rows 41.6 / 47.1, 20.7 / 21.1, 12.9 / 11.2.
   const bool narrow = n_rows > 2 * D.sms;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)n_rows * csize);

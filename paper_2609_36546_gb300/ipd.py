@@ -589,7 +589,8 @@ def prompt_attn(q, k, v, cu_seq, max_len: int, out, softmax_scale: float,
     """Causal attention of packed prompts: q [total, Hq, 128], k and v
     [total, Hkv, 128], out [total, Hq, 128] bf16 (rows contiguous, any row
     stride), cu_seq int32 [num_seqs + 1] (device), ``max_len`` a host-known
-    bound on the lengths; lse fp32 [Hq, total] when given."""
+    bound on the lengths (0: every sequence is empty, and nothing is done);
+    lse fp32 [Hq, total] when given."""
     shape, kshape, bf = tuple(q.shape), tuple(k.shape), _BF16
     if len(shape) != 3 or len(kshape) != 3 or kshape[0] != shape[0] or kshape[2] != shape[2] or \
             cu_seq.dtype is not _I32 or not cu_seq.is_contiguous():
