@@ -36,6 +36,13 @@
  * ipd_sample_trunc (a token per row at a temperature, cut by top-k, min-p and
  * top-p, from given uniform numbers).
  *
+ * A verify step over a cache held in 8 bits: ipd_kv8_append (new K/V rows into
+ * pages of e4m3 values with a scale a page, head and tensor), ipd_verify_attn8
+ * (the span-verify and decode attention that reads them), and
+ * ipd_verify_draft (the drafts' verification by rejection: the verdict that
+ * leaves the target's distribution unchanged, where ipd_score_span takes top-K
+ * coverage).
+ *
  * Conventions for every call
  *   - Data pointers are DEVICE pointers owned by the caller; the library never
  *     allocates.  Scratch memory comes from a caller-provided device workspace
@@ -640,6 +647,131 @@ int ipd_sample_trunc(const uint16_t *logits, int64_t row_stride, int n_rows, int
                      const float *u, const float *inv_temperature, const int32_t *top_k,
                      const float *top_p, const float *min_p, int32_t *tokens, float *logp,
                      int32_t *n_kept, ipd_stream_t stream);
+
+/* One paged KV cache held in 8 bits (one attention layer of one model).
+ *  k_pages, v_pages  [num_pages][num_kv_heads][16][128] e4m3 (OCP FP8 E4M3:
+ *            4 exponent bits, 3 mantissa bits, no infinities, NaN 0x7f / 0xff),
+ *            16-byte aligned; pages as in ipd_kv_cache
+ *  k_scale, v_scale  [num_pages][num_kv_heads] one byte b (E8M0): the entries of
+ *            that page and head stand for their value times 2^(b - 127); 255
+ *            makes them NaN
+ * Supported: page_size == 16, head_dim == 128, 1 <= num_kv_heads <= 64. */
+typedef struct ipd_kv8_cache {
+  uint8_t *k_pages, *v_pages;
+  uint8_t *k_scale, *v_scale;
+  int64_t num_pages;
+  int32_t page_size, num_kv_heads, head_dim;
+} ipd_kv8_cache;
+
+/* Appends of new K/V rows (bf16) to 8-bit caches, up to IPD_MAX_BATCHES in one
+ * launch.  Rows, offsets, lengths and page tables as for ipd_kv_append, but for
+ *  k_new, v_new   rows of num_kv_heads x 128 entries, k_stride / v_stride
+ *            entries apart (multiples of 8; views into one projection output)
+ * Per page, head and tensor that gets rows: e is the least whole number with
+ * |x| <= 448 2^e for every finite new entry x, at least -40, and at least the
+ * page's present e when the page holds earlier rows (slots before the first new
+ * one).  b becomes e + 127.  New entries become x 2^-e, rounded to the nearest
+ * e4m3 value (ties to even); infinities and NaN become NaN.  When e grew, the
+ * earlier rows' values are multiplied by 2^(old e - e) and rounded the same way
+ * (exact unless they fall below 2^-6).  Slots after the new rows keep their
+ * bytes.  A scale never falls while its page goes on, a row that starts a page
+ * starts a new scale, and rows overwritten after a rollback count as not held.
+ * A page that gets rows belongs to one request of the call: the scale is the
+ * whole page's.  Errors as for ipd_kv_append (a row at fault is skipped and does
+ * not count for the scale). */
+typedef struct ipd_kv8_append_desc {
+  ipd_kv8_cache cache;
+  const uint16_t *k_new, *v_new;
+  int64_t k_stride, v_stride;
+  const int32_t *cu_new, *seq_len, *page_table;
+  int32_t max_pages, num_reqs, total_new;
+} ipd_kv8_append_desc;
+int ipd_kv8_append(const ipd_kv8_append_desc *appends, int n, ipd_stream_t stream);
+
+/* ipd_attn_batch over an 8-bit cache. */
+typedef struct ipd_attn8_batch {
+  const ipd_kv8_cache *cache;
+  int32_t num_q_heads, num_reqs;
+  const uint16_t *q;
+  const int32_t *cu_q, *seq_len, *page_table;
+  int32_t max_pages, total_q, max_q_len, max_seq_len;
+  uint16_t *out;
+} ipd_attn8_batch;
+
+/* Workspace bytes for one ipd_verify_attn8 call on these batches (host
+ * arithmetic only).  Returns 0 if the batches are invalid. */
+size_t ipd_attn8_workspace_size(const ipd_attn8_batch *verify, int n_verify,
+                                const ipd_attn8_batch *decode, int n_decode);
+
+/* ipd_verify_attn over 8-bit caches: the spans of n_verify batches and the
+ * decode tokens of n_decode batches (the same thing with q_len 1) in one call.
+ * out = softmax(scale q K^T) V per query and head over the values the cache's
+ * entries stand for.  q is carried exactly to 2^-18 of its row's largest entry
+ * into the products; scores, maxima and sums are fp32; the softmax weights enter
+ * the product with V as two e4m3 terms, to 2^-9 of themselves (and 2^-18 of the
+ * row's largest); the output is rounded to bf16 once.  A row's result depends on
+ * no key that it does not see, whatever that key holds, and on no other row.
+ * A page id outside the pool is recorded (IPD_DEVERR_PAGE_ID) and its keys are
+ * left out; a row that is left with none gets 0.  A request whose offsets are out
+ * of order or past total_q (IPD_DEVERR_SPAN), or whose seq_len is below its
+ * q_len, above max_seq_len or with q_len above max_q_len (IPD_DEVERR_SEQ_LEN), is
+ * recorded and its rows are not written.  Returns IPD_ERR_UNSUPPORTED for more
+ * than 128 query heads a KV head or num_pages * num_kv_heads >= 2^27. */
+int ipd_verify_attn8(const ipd_attn8_batch *verify, int n_verify, const ipd_attn8_batch *decode,
+                     int n_decode, float softmax_scale, void *workspace, size_t workspace_bytes,
+                     ipd_stream_t stream);
+
+/* Verification of drafted tokens by rejection, from given uniform numbers, so
+ * that the emitted tokens follow the target's distribution whatever the draft
+ * model's is (Leviathan et al. 2023, Chen et al. 2023): draft t is accepted with
+ * probability min(1, p_t(x_t) / q_t(x_t)); at a request's first rejected draft a
+ * token is drawn from the normalised (p - q)+ of that position, and behind the
+ * drafts, if none was rejected, from the target's next row.  A decision is a
+ * fixed function of (rows, settings, u), reproducible on any device: with the
+ * whole-number weights w_v = floor(2^30 2^x_v + 1/2) of ipd_sample_trunc (x from
+ * the row's own temperature; nothing is cut) for the target's row p and the
+ * draft's q, and Z_p, Z_q their sums,
+ *   accepted  iff fl64(fl64(u w_q(x)) Z_p) < fl64(w_p(x) Z_q)
+ *   residual  r_v = max(0, w_p(v) - floor(w_q(v) m / 2^s)), where Z_p / Z_q, rounded
+ *             to fp64 and cut to its 31 leading bits, is m / 2^s (r = w_p where
+ *             Z_q = 0 or no r_v is positive)
+ *   token     the entry, by token id, in which position floor(fl64(u' S)) of the
+ *             running sum of r falls, S their sum (clamped to S - 1)
+ *  logits_target  [total] bf16 rows of vocab entries, target_stride apart: row t
+ *            is the target's distribution of draft position t
+ *  logits_draft   [total] rows, draft_stride apart: the draft model's
+ *  logits_bonus   [num_reqs] rows, bonus_stride apart: the target's row behind a
+ *            request's drafts, or NULL (a request with all drafts accepted then
+ *            gets next_token -1).  Rows of any alignment of whole entries.
+ *  tokens    [total] int32 drafted tokens; one outside [0, vocab) records
+ *            IPD_DEVERR_TOKEN and is rejected
+ *  cu_draft  [num_reqs + 1] int32 offsets; a request may have no drafts
+ *  u_accept  [total], u_next [num_reqs] fp32 uniform numbers in [0, 1) (a NaN
+ *            u_accept rejects; u_next <= 0 or NaN takes position 0)
+ *  inv_temp_target, inv_temp_draft  [num_reqs] fp32 or NULL for 1 (the target's
+ *            holds for the bonus row too)
+ *  n_accept  [num_reqs] int32: drafts before the first rejected one
+ *  next_token [num_reqs] int32; -1 also where the row it is drawn from has no
+ *            finite or +inf entry
+ *  logp_target, logp_draft  [total] fp32 log-probabilities of the drafted tokens
+ *            at these temperatures (-inf for a row or token without any), or NULL
+ * A request whose temperature is not valid (log2 e * inv_temp not positive and
+ * finite) records IPD_DEVERR_SETTING and gets n_accept 0 and next_token -1, its
+ * logp NaN; one whose offsets are out of order or past total (IPD_DEVERR_SPAN)
+ * the same, with nothing of its drafts written.  Positions that no request's
+ * offsets cover are left as they are.  vocab is at most IPD_TRUNC_MAX_VOCAB. */
+typedef struct ipd_draft_args {
+  const uint16_t *logits_target, *logits_draft, *logits_bonus;
+  int64_t target_stride, draft_stride, bonus_stride;
+  const int32_t *tokens, *cu_draft;
+  const float *u_accept, *u_next, *inv_temp_target, *inv_temp_draft;
+  int32_t *n_accept, *next_token;
+  float *logp_target, *logp_draft;
+  int32_t num_reqs, total, vocab;
+} ipd_draft_args;
+size_t ipd_verify_draft_workspace_size(int num_reqs, int total, int vocab);
+int ipd_verify_draft(const ipd_draft_args *args, void *workspace, size_t workspace_bytes,
+                     ipd_stream_t stream);
 
 /* Measurement aid.  While on, every ipd_verify_attn / ipd_decode_attn call
  * records CUDA events on its stream around its attention kernel alone (not

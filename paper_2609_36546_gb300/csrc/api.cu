@@ -10,6 +10,9 @@ extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_
 extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_rope_error();
 extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_prompt_error();
 extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_trunc_error();
+extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_kv8_error();
+extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_attn8_error();
+extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_draft_error();
 
 extern "C" int ipd_get_device_error(uint32_t *code) {
   if (!code) return IPD_ERR_INVALID_ARG;
@@ -18,7 +21,8 @@ extern "C" int ipd_get_device_error(uint32_t *code) {
   const unsigned int words[] = {ipd_internal_take_attn_error(), ipd_internal_take_score_error(),
                                 ipd_internal_take_loss_error(), ipd_internal_take_kv_error(),
                                 ipd_internal_take_rope_error(), ipd_internal_take_prompt_error(),
-                                ipd_internal_take_trunc_error()};
+                                ipd_internal_take_trunc_error(), ipd_internal_take_kv8_error(),
+                                ipd_internal_take_attn8_error(), ipd_internal_take_draft_error()};
   unsigned int first = 0;
   for (const unsigned int w : words) {
     if (w == 0xffffffffu) return IPD_ERR_CUDA;

@@ -1,0 +1,511 @@
+// Verification of drafted tokens by rejection, from given uniform numbers.
+//
+// With whole-number weights w_v = floor(2^30 2^x_v + 1/2), x_v = fl(fl(l_v - max l) c),
+// c = fl(log2 e / temperature), and their sums Z (below 2^48: exact, in any order):
+//   accepted   u w_q(x) Z_p < w_p(x) Z_q        (fp64, one rounding a product)
+//   residual   r_v = max(0, w_p(v) - (w_q(v) m >> s)),  m 2^-s = Z_p / Z_q in 31 bits
+//   token      the entry in which floor(u' S) falls in the running sum of r, by id
+// so a verdict is a fixed function of (rows, settings, u): no sum depends on an order.
+//
+// Two launches.  Rows: every drafted position's two rows, the maximum in a first
+// look, the weights' sum in a second one (from L2).  Verdicts: a cluster of CTAs a
+// request finds the first rejected draft and goes through that one position's two
+// rows (or the bonus row), each CTA a piece: sums of tiles of 256 entries, then the
+// tile, then the entry that holds the drawn position.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <atomic>
+
+#include "cluster.cuh"
+#include "common.cuh"
+#include "weights.cuh"
+
+IPD_DECLARE_ERROR_WORD(g_draft_err);
+// whether this process has launched (or captured) a kernel that may set the word:
+// a program without these calls does not pay for reading it
+static std::atomic<bool> g_draft_used{false};
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kMaxCluster = 8;
+constexpr int kTile = 256;  // entries a warp sums at once: 8 a lane
+constexpr int kTiles = (IPD_TRUNC_MAX_VOCAB + 8) / kTile + 1;
+
+// What the row pass leaves of a row.
+struct Row {
+  u64 z;         // sum of the weights
+  float top;     // largest logit (-inf: the row has no entry)
+  uint32_t w;    // the drafted token's weight
+};
+
+struct Params {
+  ipd_draft_args a;
+  Row *rows;     // [2 total]: target and draft row of every position
+  int piece;     // 8-entry vectors a CTA takes of a row (verdicts: a multiple of 32)
+};
+
+IPD_DEVINL uint32_t max2(uint32_t a, uint32_t b) {  // of two bf16 each; NaN loses
+  const __nv_bfloat162 m = __hmax2(*reinterpret_cast<__nv_bfloat162 *>(&a),
+                                   *reinterpret_cast<__nv_bfloat162 *>(&b));
+  return *reinterpret_cast<const uint32_t *>(&m);
+}
+
+// A row as whole 16-byte vectors: it may start and end inside one.
+struct RowView {
+  const uint4 *base;
+  int before, entries, n_vec;  // entries of the first vector that are not the row's
+  IPD_DEVINL RowView(const uint16_t *p, int vocab) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    base = reinterpret_cast<const uint4 *>(a & ~(uintptr_t)15);
+    before = (int)(a & 15) / 2;
+    entries = vocab;
+    n_vec = (before + vocab + 7) / 8;
+  }
+  // vector i with -inf in place of what is not the row's
+  IPD_DEVINL uint4 get(int i) const {
+    uint4 v = ldg_stream(base + i);
+    if (i == 0 || i == n_vec - 1) {
+      uint32_t *w = &v.x;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int at = i * 8 + e - before;
+        if (at < 0 || at >= entries) w[e >> 1] = e & 1 ? (w[e >> 1] & 0xffffu) | 0xff800000u : (w[e >> 1] & 0xffff0000u) | 0xff80u;
+      }
+    }
+    return v;
+  }
+};
+
+// Weights of a row's entries.
+struct Weigher {
+  float top, c;
+  bool inf;  // top is +inf: only its equals have a weight
+  IPD_DEVINL Weigher(float t, float cc) : top(t), c(cc), inf(t == INFINITY) {}
+  IPD_DEVINL void two(uint32_t w, uint32_t &w0, uint32_t &w1) const {
+    if (inf) {
+      w0 = (w & 0xffffu) == 0x7f80u ? 1u << 30 : 0u;
+      w1 = w >> 16 == 0x7f80u ? 1u << 30 : 0u;
+      return;
+    }
+    float a, b;
+    f2_unpack(f2_mul(f2_sub(f2_pack(bf16lo(w), bf16hi(w)), f2_pack(top, top)), f2_pack(c, c)), a, b);
+    // (fmaxf drops a NaN: NaN entries, and every entry of a row without any)
+    pow2_weight2(f2_pack(fmaxf(a, -64.f), fmaxf(b, -64.f)), w0, w1);
+  }
+  IPD_DEVINL float x(float l) const { return l == top ? 0.f : __fmul_rn(__fsub_rn(l, top), c); }
+};
+
+IPD_DEVINL float scale_of(const float *inv_temp, int r) {
+  return __fmul_rn(kLog2e, inv_temp ? inv_temp[r] : 1.f);
+}
+IPD_DEVINL bool valid(float c) { return c > 0.f && c < INFINITY; }
+
+IPD_DEVINL u64 warp_sum64(u64 v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+IPD_DEVINL u64 remote_ld64(const void *p, uint32_t rank) {
+  const uint32_t a = remote(p, rank);
+  return (u64)remote_ld(a) | (u64)remote_ld(a + 4) << 32;
+}
+
+// The block's sum / maximum, in every thread (red: kWarps words of its own use).
+IPD_DEVINL u64 block_sum(u64 v, u64 *red) {
+  v = warp_sum64(v);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+  __syncthreads();
+  u64 s = 0;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) s += red[i];
+  return s;
+}
+IPD_DEVINL float block_max(float v, float *red) {
+  v = warp_max(v);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (int i = 1; i < kWarps; ++i) v = fmaxf(v, red[i]);
+  return v;
+}
+
+// Largest entry of vectors [from, to) of a row.
+IPD_DEVINL float piece_max(const RowView &R, int from, int to) {
+  uint32_t m = 0xff80ff80u;
+  for (int i = from + threadIdx.x; i < to; i += kThreads) {
+    const uint4 v = R.get(i);
+    m = max2(m, max2(max2(v.x, v.y), max2(v.z, v.w)));
+  }
+  return fmaxf(bf16lo(m), bf16hi(m));
+}
+
+// The request whose drafts hold position t, or -1.
+IPD_DEVINL int request_of(const ipd_draft_args &a, int t) {
+  if (t < a.cu_draft[0] || t >= a.cu_draft[a.num_reqs]) return -1;
+  int lo = 0, hi = a.num_reqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.cu_draft[mid] <= t) lo = mid;
+    else hi = mid - 1;
+  }
+  auto holds = [&](int r) {
+    const int c0 = a.cu_draft[r], c1 = a.cu_draft[r + 1];
+    return c0 >= 0 && c0 <= t && t < c1 && c1 <= a.total;
+  };
+  if (holds(lo)) return lo;
+  for (int r = 0; r < a.num_reqs; ++r)  // offsets out of order
+    if (holds(r)) return r;
+  return -1;
+}
+
+// ---- rows ------------------------------------------------------------------
+__global__ void __launch_bounds__(kThreads) draft_rows_kernel(const __grid_constant__ Params P) {
+  __shared__ u64 red[kWarps], zs;
+  __shared__ float fred[kWarps], tops;
+  const ipd_draft_args &a = P.a;
+  const uint32_t csize = cluster_size(), rank = cluster_rank();
+  const int row = blockIdx.x / csize, t = row >> 1;
+  const bool draft = row & 1;
+  const int r = request_of(a, t);
+  if (r < 0) return;  // (the whole cluster)
+  const float cp = scale_of(a.inv_temp_target, r), cq = scale_of(a.inv_temp_draft, r);
+  const float c = draft ? cq : cp;
+  const uint16_t *p = draft ? a.logits_draft + (long long)t * a.draft_stride
+                            : a.logits_target + (long long)t * a.target_stride;
+  const RowView R(p, a.vocab);
+  const int from = min((int)rank * P.piece, R.n_vec), to = min(from + P.piece, R.n_vec);
+  float top = block_max(piece_max(R, from, to), fred);
+  if (csize > 1) {
+    if (threadIdx.x == 0) tops = top;
+    cluster_sync();
+    for (uint32_t i = 0; i < csize; ++i) top = fmaxf(top, __uint_as_float(remote_ld(remote(&tops, i))));
+  }
+  const Weigher W(top, c);
+  u64 z = 0;
+  for (int i = from + threadIdx.x; i < to; i += kThreads) {
+    const uint4 v = R.get(i);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t w0, w1;
+      W.two(w[k], w0, w1);
+      z += w0 + w1;
+    }
+  }
+  z = block_sum(z, red);
+  if (csize > 1) {
+    if (threadIdx.x == 0) zs = z;
+    cluster_sync();
+    if (rank == 0) {
+      z = 0;
+      for (uint32_t i = 0; i < csize; ++i) z += remote_ld64(&zs, i);
+    }
+    cluster_sync();  // no CTA leaves while its sums are read
+  }
+  if (rank == 0 && threadIdx.x == 0) {
+    const int tok = a.tokens[t];
+    uint32_t w0 = 0, w1;
+    float logp = __uint_as_float(0x7fc00000u);
+    if (tok < 0 || tok >= a.vocab) {
+      ipd_set_error(&g_draft_err, IPD_DEVERR_TOKEN);
+    } else {
+      const uint16_t l = p[tok];
+      W.two(l | 0xff800000u, w0, w1);
+      const float f = bf16f(l);
+      logp = z == 0 || f != f ? -INFINITY
+                              : (float)(((double)W.x(f) - log2((double)z * 0x1p-30)) * 0.6931471805599453);
+    }
+    if (!valid(cp) || !valid(cq)) logp = __uint_as_float(0x7fc00000u);
+    float *out = draft ? a.logp_draft : a.logp_target;
+    if (out) out[t] = logp;
+    P.rows[row] = Row{z, top, w0};
+  }
+}
+
+// ---- verdicts ----------------------------------------------------------------
+struct Verdict {
+  u64 tile[kTiles];  // sums of the tiles of this CTA's piece
+  u64 red[kWarps];
+  float fred[kWarps];
+  u64 sum;           // ... of the piece
+  float top;
+  int n;             // accepted drafts
+};
+
+IPD_DEVINL bool accepted(const Params &P, int t) {
+  const int tok = P.a.tokens[t];
+  if (tok < 0 || tok >= P.a.vocab) return false;
+  const Row p = P.rows[2 * t], q = P.rows[2 * t + 1];
+  return __dmul_rn(__dmul_rn((double)P.a.u_accept[t], (double)q.w), (double)p.z) <
+         __dmul_rn((double)p.w, (double)q.z);
+}
+
+// What a residual is taken from: the target's row and the draft's, and their ratio.
+struct Residual {
+  RowView p, q;
+  Weigher wp, wq;
+  u64 m;       // 0: nothing is taken off
+  int s, off;  // off: the draft row's entries lie this much further on in its vectors
+
+  // weights of the 8 entries of target vector i
+  IPD_DEVINL void eight(int i, uint32_t (&r)[8]) const {
+    const uint4 v = p.get(i);
+    wp.two(v.x, r[0], r[1]);
+    wp.two(v.y, r[2], r[3]);
+    wp.two(v.z, r[4], r[5]);
+    wp.two(v.w, r[6], r[7]);
+    if (m == 0) return;
+    uint32_t g[8];
+    if (off == 0) {
+      const uint4 o = q.get(i);
+      wq.two(o.x, g[0], g[1]);
+      wq.two(o.y, g[2], g[3]);
+      wq.two(o.z, g[4], g[5]);
+      wq.two(o.w, g[6], g[7]);
+    } else {  // rows of different alignment: entry by entry
+      const uint16_t *l = reinterpret_cast<const uint16_t *>(q.base) + q.before;
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const int at = i * 8 + e - p.before;
+        const uint32_t lo = at >= 0 && at < p.entries ? l[at] : 0xff80u,
+                       hi = at + 1 >= 0 && at + 1 < p.entries ? l[at + 1] : 0xff80u;
+        wq.two(lo | hi << 16, g[e], g[e + 1]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const u64 less = (u64)g[e] * m >> s;
+      r[e] = less >= r[e] ? 0u : r[e] - (uint32_t)less;
+    }
+  }
+};
+
+__global__ void __launch_bounds__(kThreads) draft_verdict_kernel(const __grid_constant__ Params P) {
+  __shared__ Verdict S;
+  const ipd_draft_args &a = P.a;
+  const uint32_t csize = cluster_size(), rank = cluster_rank();
+  const int r = blockIdx.x / csize, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c0 = a.cu_draft[r], c1 = a.cu_draft[r + 1];
+  const float cp = scale_of(a.inv_temp_target, r), cq = scale_of(a.inv_temp_draft, r);
+  const bool spans = c0 >= 0 && c1 >= c0 && c1 <= a.total;
+  if (!spans || !valid(cp) || !valid(cq)) {
+    if (rank == 0 && threadIdx.x == 0) {
+      ipd_set_error(&g_draft_err, spans ? IPD_DEVERR_SETTING : IPD_DEVERR_SPAN);
+      a.n_accept[r] = 0;
+      a.next_token[r] = -1;
+    }
+    return;
+  }
+  if (threadIdx.x == 0) S.n = c1 - c0;
+  __syncthreads();
+  for (int t = c0 + threadIdx.x; t < c1; t += kThreads)
+    if (!accepted(P, t)) {
+      atomicMin(&S.n, t - c0);
+      break;
+    }
+  __syncthreads();
+  const int n = S.n;
+  const bool full = n == c1 - c0;
+  if (rank == 0 && threadIdx.x == 0) a.n_accept[r] = n;
+  const int at = c0 + n;
+  const Row rp = full ? Row{} : P.rows[2 * at], rq = full ? Row{} : P.rows[2 * at + 1];
+  if (full ? !a.logits_bonus : rp.z == 0) {
+    if (rank == 0 && threadIdx.x == 0) a.next_token[r] = -1;
+    return;
+  }
+  const uint16_t *pp = full ? a.logits_bonus + (long long)r * a.bonus_stride
+                            : a.logits_target + (long long)at * a.target_stride;
+  const uint16_t *pq = full ? pp : a.logits_draft + (long long)at * a.draft_stride;
+  const RowView vp(pp, a.vocab), vq(pq, a.vocab);
+  const int from = min((int)rank * P.piece, vp.n_vec), to = min(from + P.piece, vp.n_vec);
+  float top = rp.top;
+  if (full) {
+    top = block_max(piece_max(vp, from, to), S.fred);
+    if (csize > 1) {
+      if (threadIdx.x == 0) S.top = top;
+      cluster_sync();
+      for (uint32_t i = 0; i < csize; ++i) top = fmaxf(top, __uint_as_float(remote_ld(remote(&S.top, i))));
+    }
+  }
+  Residual D{vp, vq, Weigher(top, cp), Weigher(rq.top, cq), 0, 0, vq.before - vp.before};
+  if (!full && rq.z != 0) {
+    int e;
+    const double f = frexp(__ddiv_rn((double)rp.z, (double)rq.z), &e);
+    D.m = (u64)(f * 0x1p31);
+    D.s = 31 - e;  // 13 .. 49
+  }
+  // Sums of the tiles.  A second time with the target's weights alone where
+  // nothing is left of them.
+  const int tiles = (to - from + 31) / 32;
+  u64 total = 0, before = 0;
+  for (int round = 0; round < 2; ++round) {
+    u64 mine = 0;
+    for (int k = warp; k < tiles; k += kWarps) {
+      const int i = from + k * 32 + lane;
+      u64 s = 0;
+      if (i < to) {
+        uint32_t w[8];
+        D.eight(i, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += w[e];
+      }
+      s = warp_sum64(s);
+      if (lane == 0) S.tile[k] = s, mine += s;
+    }
+    __syncthreads();  // (S.red is read by the round before)
+    const u64 sum = block_sum(mine, S.red);
+    total = sum, before = 0;
+    if (csize > 1) {
+      if (threadIdx.x == 0) S.sum = sum;
+      cluster_sync();
+      total = 0;
+      for (uint32_t i = 0; i < csize; ++i) {
+        if (i == rank) before = total;
+        total += remote_ld64(&S.sum, i);
+      }
+      cluster_sync();
+    }
+    if (total != 0 || D.m == 0) break;
+    D.m = 0;
+  }
+  if (total == 0) {  // (a bonus row without an entry)
+    if (rank == 0 && threadIdx.x == 0) a.next_token[r] = -1;
+    return;
+  }
+  const float u = a.u_next[r];
+  const double d = u > 0.f ? floor(__dmul_rn((double)u, (double)total)) : 0.0;
+  const u64 pos = d < (double)total ? (u64)d : total - 1;
+  if (warp != 0 || pos < before) return;
+  u64 left = pos - before;
+  // the tile: 32 at a time
+  int k0 = 0;
+  u64 sum = 0, v = 0;
+  for (;; k0 += 32) {
+    if (k0 >= tiles) return;  // in a later CTA's piece
+    v = k0 + lane < tiles ? S.tile[k0 + lane] : 0;
+    sum = warp_sum64(v);
+    if (left < sum) break;
+    left -= sum;
+  }
+  auto scan = [&](u64 x) {  // inclusive, over the lanes
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    return x;
+  };
+  u64 up = scan(v);
+  int who = __ffs(__ballot_sync(0xffffffffu, left < up)) - 1;
+  left -= __shfl_sync(0xffffffffu, up - v, who);
+  const int i = from + (k0 + who) * 32 + lane;
+  uint32_t w[8] = {};
+  if (i < to) D.eight(i, w);
+  v = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v += w[e];
+  up = scan(v);
+  who = __ffs(__ballot_sync(0xffffffffu, left < up)) - 1;
+  if (lane != who) return;
+  left -= up - v;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (left < w[e]) {
+      a.next_token[r] = i * 8 + e - vp.before;
+      return;
+    }
+    left -= w[e];
+  }
+}
+
+int g_sms[64];
+
+int launch(void (*kernel)(Params), int grid, int csize, const Params &P, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid * csize);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = csize;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, P) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return IPD_ERR_CUDA;
+  }
+  return IPD_OK;
+}
+
+}  // namespace
+
+extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_draft_error() {
+  if (!g_draft_used.load(std::memory_order_relaxed)) return 0u;
+  unsigned int v = 0, z = 0;
+  if (cudaMemcpyFromSymbol(&v, g_draft_err, sizeof(v)) != cudaSuccess) return 0xffffffffu;
+  if (cudaMemcpyToSymbol(g_draft_err, &z, sizeof(z)) != cudaSuccess) return 0xffffffffu;
+  return v;
+}
+
+extern "C" size_t ipd_verify_draft_workspace_size(int num_reqs, int total, int vocab) {
+  if (num_reqs < 0 || total < 0 || vocab < 1) return 0;
+  return (2 * (size_t)total * sizeof(Row) + 255) / 256 * 256;
+}
+
+extern "C" int ipd_verify_draft(const ipd_draft_args *args, void *workspace,
+                                size_t workspace_bytes, ipd_stream_t stream) {
+  if (!args) return IPD_ERR_INVALID_ARG;
+  const ipd_draft_args &a = *args;
+  if (a.num_reqs < 0 || a.total < 0 || a.vocab < 1) return IPD_ERR_INVALID_ARG;
+  if (a.vocab > IPD_TRUNC_MAX_VOCAB || a.total > (1 << 26) || a.num_reqs > (1 << 26))
+    return IPD_ERR_UNSUPPORTED;
+  if (a.num_reqs == 0) return IPD_OK;
+  if (!a.cu_draft || !a.u_next || !a.n_accept || !a.next_token) return IPD_ERR_INVALID_ARG;
+  if (a.total > 0 && (!a.logits_target || !a.logits_draft || !a.tokens || !a.u_accept))
+    return IPD_ERR_INVALID_ARG;
+  if (((uintptr_t)a.logits_target | (uintptr_t)a.logits_draft | (uintptr_t)a.logits_bonus) & 1)
+    return IPD_ERR_INVALID_ARG;
+  if (a.target_stride < 0 || a.draft_stride < 0 || a.bonus_stride < 0) return IPD_ERR_INVALID_ARG;
+  const size_t need = ipd_verify_draft_workspace_size(a.num_reqs, a.total, a.vocab);
+  if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15)))
+    return IPD_ERR_WORKSPACE;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return IPD_ERR_CUDA;
+  if (g_sms[dev] == 0) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+      return IPD_ERR_CUDA;
+    g_sms[dev] = n;
+  }
+  const int sms = g_sms[dev];
+  Params P;
+  memset(&P, 0, sizeof(P));
+  P.a = a;
+  P.rows = static_cast<Row *>(workspace);
+  const int vecs = (a.vocab + 14) / 8;
+  // CTAs of a row: as many (1, 2, 4, 8) as leave every one an SM's quarter
+  auto split = [&](long long rows) {
+    int c = kMaxCluster;
+    while (c > 1 && (rows * c > 4LL * sms || vecs < c * 1024)) c /= 2;
+    return c;
+  };
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  g_draft_used.store(true, std::memory_order_relaxed);
+  if (a.total > 0) {
+    const int c = split(2LL * a.total);
+    P.piece = (vecs + c - 1) / c;
+    if (launch(draft_rows_kernel, 2 * a.total, c, P, st) != IPD_OK) return IPD_ERR_CUDA;
+  }
+  const int c = split(a.num_reqs);
+  P.piece = (vecs + 32 * c - 1) / (32 * c) * 32;
+  return launch(draft_verdict_kernel, a.num_reqs, c, P, st);
+}

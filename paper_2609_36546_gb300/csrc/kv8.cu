@@ -1,0 +1,218 @@
+// Append of new K/V rows into pages of 8-bit values with a power-of-two scale a
+// page, head and tensor.
+//
+//   e    = max(least e with max |x| <= 448 2^e, the page's e if it goes on, -40)
+//   y    = e4m3(x 2^-e)            new rows, to nearest even
+//   held = e4m3(held 2^(e_old-e))  the page's earlier rows, when e grew
+//
+// A power of two keeps the old rows' bits when the scale moves (a product with
+// 2^-k is exact until an entry falls below 2^-6, where it is rounded once), and
+// lets the attention take a scale into an exponent.
+//
+// A run is the new rows of one page: a warp takes a run of one head and tensor,
+// 8 bytes of a row a lane, all of the run's rows (at most 16) in registers, so
+// that the maximum and the rounding read a row once.  A warp looks at a group of
+// consecutive new rows, a lane each, and works through the runs that start there.
+#include <cuda_runtime.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <atomic>
+
+#include "common.cuh"
+#include "e4m3.cuh"
+
+IPD_DECLARE_ERROR_WORD(g_kv8_err);
+// whether this process has launched (or captured) a kernel that may set the word:
+// a program without these calls does not pay for reading it
+static std::atomic<bool> g_kv8_used{false};
+
+namespace {
+
+constexpr int kThreads = 128;
+constexpr int kLeast = 87;  // scale byte of e = -40
+
+struct AppendDev {
+  ipd_kv8_append_desc d;
+  int group;        // new rows a warp looks at: 1 .. 16
+  int groups;       // ... and how many such groups there are
+};
+
+struct AppendParams {
+  AppendDev a[IPD_MAX_BATCHES];
+  long long end[IPD_MAX_BATCHES];  // warps up to and with each append
+  int n;
+};
+
+// The run that starts with new row `tok`: its page (< 0: none starts here, or it
+// is at fault), first slot and number of rows.
+IPD_DEVINL int find_run(const ipd_kv8_append_desc &D, int tok, int *slot, int *rows) {
+  if (tok < D.cu_new[0] || tok >= D.cu_new[D.num_reqs]) {
+    ipd_set_error(&g_kv8_err, IPD_DEVERR_SPAN);
+    return -1;
+  }
+  int lo = 0, hi = D.num_reqs - 1;  // the last request with cu_new[r] <= tok
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (D.cu_new[mid] <= tok) lo = mid;
+    else hi = mid - 1;
+  }
+  const int c0 = D.cu_new[lo], c1 = min(D.cu_new[lo + 1], D.total_new), len = D.seq_len[lo];
+  if (c1 <= tok) {  // offsets out of order
+    ipd_set_error(&g_kv8_err, IPD_DEVERR_SPAN);
+    return -1;
+  }
+  const long long p = (long long)len - (D.cu_new[lo + 1] - c0) + (tok - c0);
+  if (p < 0 || p >= len || (p >> 4) >= D.max_pages) {
+    ipd_set_error(&g_kv8_err, IPD_DEVERR_SEQ_LEN);
+    return -1;
+  }
+  *slot = (int)(p & 15);
+  if (*slot != 0 && tok != c0) return -1;  // its page's run started before it
+  const int page = D.page_table[(size_t)lo * D.max_pages + (size_t)(p >> 4)];
+  if (page < 0 || page >= D.cache.num_pages) {
+    ipd_set_error(&g_kv8_err, IPD_DEVERR_PAGE_ID);
+    return -1;
+  }
+  *rows = min(16 - *slot, c1 - tok);
+  return page;
+}
+
+// largest |entry| among the finite of four bf16, as bits of a non-negative bf16
+IPD_DEVINL uint32_t finite_max(uint2 v) {
+  uint32_t m = 0;
+  const uint32_t w[4] = {v.x & 0x7fffu, v.x >> 16 & 0x7fffu, v.y & 0x7fffu, v.y >> 16 & 0x7fffu};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (w[i] < 0x7f80u) m = max(m, w[i]);
+  return m;
+}
+
+// the least scale byte that brings the bf16 of bits m to 448 or below
+IPD_DEVINL int byte_of(uint32_t m) {
+  if (m == 0) return kLeast;
+  const uint32_t f = __float_as_uint(bf16f((uint16_t)m));
+  if (f < 0x00800000u) return kLeast;  // a subnormal
+  // f = 2^(E - 127) (1 + frac), 448 = 2^8 * 1.75
+  const int E = (int)(f >> 23);
+  return max(kLeast, E - 8 + ((f & 0x7fffffu) > 0x600000u ? 1 : 0));
+}
+
+// four entries times s as e4m3; what is not finite becomes NaN
+IPD_DEVINL uint32_t quantise(uint2 v, float s) {
+  float x[4] = {bf16lo(v.x), bf16hi(v.x), bf16lo(v.y), bf16hi(v.y)};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    x[i] = (__float_as_uint(x[i]) & 0x7f800000u) == 0x7f800000u ? __uint_as_float(0x7fc00000u) : x[i] * s;
+  return e4m3x2(x[0], x[1]) | e4m3x2(x[2], x[3]) << 16;
+}
+
+__global__ void __launch_bounds__(kThreads) kv8_append_kernel(
+    const __grid_constant__ AppendParams P) {
+  const int lane = threadIdx.x & 31;
+  const long long warps = (long long)gridDim.x * (kThreads / 32);
+  for (long long u = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); u < P.end[P.n - 1];
+       u += warps) {
+    int di = 0;
+    while (di + 1 < P.n && u >= P.end[di]) ++di;
+    const AppendDev &A = P.a[di];
+    const ipd_kv8_append_desc &D = A.d;
+    const int hkv = D.cache.num_kv_heads;
+    const long long w = u - (di > 0 ? P.end[di - 1] : 0);
+    const int g = (int)(w / (2 * hkv)), th = (int)(w % (2 * hkv));
+    const bool is_v = th >= hkv;
+    const int h = is_v ? th - hkv : th;
+    const uint16_t *src = is_v ? D.v_new : D.k_new;
+    const long long stride = is_v ? D.v_stride : D.k_stride;
+    uint8_t *pages = is_v ? D.cache.v_pages : D.cache.k_pages;
+    uint8_t *scales = is_v ? D.cache.v_scale : D.cache.k_scale;
+    int page = -1, slot = 0, rows = 0;
+    const int tok = g * A.group + lane;
+    if (lane < A.group && tok < D.total_new) page = find_run(D, tok, &slot, &rows);
+    uint32_t left = __ballot_sync(0xffffffffu, page >= 0);
+    while (left) {
+      const int from = __ffs(left) - 1;
+      left &= left - 1;
+      const int pg = __shfl_sync(0xffffffffu, page, from), s0 = __shfl_sync(0xffffffffu, slot, from),
+                n = __shfl_sync(0xffffffffu, rows, from);
+      const uint16_t *x = src + (long long)(g * A.group + from) * stride + h * 128 + lane * 4;
+      uint8_t *scale = scales + (size_t)pg * hkv + h;
+      uint32_t *dst = reinterpret_cast<uint32_t *>(pages + ((size_t)pg * hkv + h) * 2048) + lane;
+      uint2 v[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        v[i] = i < n ? *reinterpret_cast<const uint2 *>(x + i * stride) : make_uint2(0u, 0u);
+      const int was = s0 > 0 ? *scale : 0;
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) m = max(m, finite_max(v[i]));
+      const int b = max(byte_of(__reduce_max_sync(0xffffffffu, m)), was);
+      if (s0 > 0 && b != was) {
+        const float f = pow2i(was - b);  // b is not 255 where it grew
+#pragma unroll 4
+        for (int i = 0; i < s0; ++i) {
+          float y[4];
+          e4m3x4_to_floats(dst[i * 32], y);
+          dst[i * 32] = e4m3x2(y[0] * f, y[1] * f) | e4m3x2(y[2] * f, y[3] * f) << 16;
+        }
+      }
+      const float f = b == 255 ? __uint_as_float(0x7fc00000u) : pow2i(127 - b);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (i < n) dst[(s0 + i) * 32] = quantise(v[i], f);
+      __syncwarp();  // every lane has read the page's present scale
+      if (lane == 0) *scale = (uint8_t)b;
+    }
+  }
+}
+
+int check(const ipd_kv8_append_desc &a) {
+  const ipd_kv8_cache &c = a.cache;
+  if (a.num_reqs < 0 || a.total_new < 0 || c.num_pages < 0 || c.num_kv_heads < 1 || a.max_pages < 1)
+    return IPD_ERR_INVALID_ARG;
+  if (c.page_size != 16 || c.head_dim != 128 || c.num_kv_heads > 64) return IPD_ERR_UNSUPPORTED;
+  if (a.total_new == 0) return IPD_OK;
+  if (a.num_reqs == 0 || !c.k_pages || !c.v_pages || !c.k_scale || !c.v_scale || !a.k_new ||
+      !a.v_new || !a.cu_new || !a.seq_len || !a.page_table)
+    return IPD_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)c.num_kv_heads * 128;
+  if (a.k_stride < row || a.v_stride < row || (a.k_stride | a.v_stride) & 7) return IPD_ERR_INVALID_ARG;
+  if (((uintptr_t)c.k_pages | (uintptr_t)c.v_pages | (uintptr_t)a.k_new | (uintptr_t)a.v_new) & 15)
+    return IPD_ERR_INVALID_ARG;
+  return IPD_OK;
+}
+
+}  // namespace
+
+extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_kv8_error() {
+  if (!g_kv8_used.load(std::memory_order_relaxed)) return 0u;
+  unsigned int v = 0, z = 0;
+  if (cudaMemcpyFromSymbol(&v, g_kv8_err, sizeof(v)) != cudaSuccess) return 0xffffffffu;
+  if (cudaMemcpyToSymbol(g_kv8_err, &z, sizeof(z)) != cudaSuccess) return 0xffffffffu;
+  return v;
+}
+
+extern "C" int ipd_kv8_append(const ipd_kv8_append_desc *appends, int n, ipd_stream_t stream) {
+  if (n < 0 || n > IPD_MAX_BATCHES || (n > 0 && !appends)) return IPD_ERR_INVALID_ARG;
+  AppendParams P;
+  memset(&P, 0, sizeof(P));
+  long long total = 0;
+  for (int i = 0; i < n; ++i) {
+    const ipd_kv8_append_desc &a = appends[i];
+    const int st = check(a);
+    if (st != IPD_OK) return st;
+    if (a.total_new == 0) continue;  // nothing to write: not part of the launch
+    AppendDev &A = P.a[P.n];
+    A.d = a;
+    A.group = a.total_new >= 4LL * a.num_reqs && a.total_new > 2048 ? 16 : 1;
+    A.groups = (a.total_new + A.group - 1) / A.group;
+    total += (long long)A.groups * 2 * a.cache.num_kv_heads;
+    P.end[P.n++] = total;
+  }
+  if (P.n == 0) return IPD_OK;
+  const long long blocks = (total + kThreads / 32 - 1) / (kThreads / 32);
+  g_kv8_used.store(true, std::memory_order_relaxed);
+  kv8_append_kernel<<<(int)(blocks < 65536 ? blocks : 65536), kThreads, 0,
+                      reinterpret_cast<cudaStream_t>(stream)>>>(P);
+  return cudaGetLastError() == cudaSuccess ? IPD_OK : IPD_ERR_CUDA;
+}

@@ -52,7 +52,9 @@
 
 #include <atomic>
 
+#include "cluster.cuh"
 #include "common.cuh"
+#include "weights.cuh"
 
 IPD_DECLARE_ERROR_WORD(g_trunc_err);
 // whether this process has launched (or captured) a kernel that may set the word:
@@ -69,9 +71,6 @@ constexpr uint32_t kLowBits = 0x3600;   // bf16 bits of 2^-19
 constexpr int kSide = 31 * 128;         // bins of a sign; up to the bits of 2^12
 constexpr int kMid = kBins - 2 * kSide;  // bins between the signs
 constexpr int kRound = 8;               // see look_up
-constexpr float kMagic = 12582912.f;    // 1.5 * 2^23: x + kMagic rounds x to a whole number
-
-typedef unsigned long long u64;
 
 struct Params {
   const uint16_t *logits;
@@ -92,55 +91,6 @@ struct Scale {
   uint32_t min_w;   // smallest weight that counts (min-p; at least 1)
 };
 
-// ---- cluster ---------------------------------------------------------------
-IPD_DEVINL uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-IPD_DEVINL uint32_t cluster_size() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-  return r;
-}
-IPD_DEVINL void cluster_arrive() {
-  __syncwarp();  // (both are for whole warps)
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-}
-IPD_DEVINL void cluster_wait() {
-  __syncwarp();
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-IPD_DEVINL void cluster_sync() {
-  cluster_arrive();
-  cluster_wait();
-}
-IPD_DEVINL uint32_t remote(const void *p, uint32_t rank) {
-  uint32_t r;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
-  return r;
-}
-IPD_DEVINL uint32_t remote_ld(uint32_t addr) {
-  uint32_t v;
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
-  return v;
-}
-IPD_DEVINL void remote_st(uint32_t addr, uint32_t v) {
-  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
-}
-IPD_DEVINL void remote_st4(uint32_t addr, const uint4 &v) {
-  asm volatile("st.shared::cluster.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y),
-               "r"(v.z), "r"(v.w)
-               : "memory");
-}
-IPD_DEVINL uint4 remote_ld4(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "r"(addr)
-               : "memory");
-  return v;
-}
 
 // ---- order keys --------------------------------------------------------------
 // A 16-bit key rises with the bf16 value; NaN counts as -inf, -0 as 0.
@@ -162,16 +112,7 @@ IPD_DEVINL uint32_t max2(uint32_t a, uint32_t b) {
 }
 
 // ---- weights -------------------------------------------------------------------
-IPD_DEVINL u64 f2_mul(u64 a, u64 b) {
-  u64 d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
-// w of two entries: 2^x = 2^i P(f), i = x rounded, f = x - i in [-1/2, 1/2], P
-// by Horner's rule, every product and sum rounded to fp32 on its own; P is a
-// least-squares fit of 2^f on Chebyshev nodes with constant term 1 (relative
-// error below 1.9e-7 with its rounding).
+// w of two entries (pow2_weight2 of their x).
 IPD_DEVINL void weight2(const Scale &S, uint32_t w, uint32_t &w0, uint32_t &w1) {
   w = max2(w, S.least2);
   u64 x = f2_mul(f2_sub(f2_pack(bf16lo(w), bf16hi(w)), f2_pack(S.top, S.top)), f2_pack(S.c, S.c));
@@ -180,28 +121,7 @@ IPD_DEVINL void weight2(const Scale &S, uint32_t w, uint32_t &w0, uint32_t &w1) 
     f2_unpack(x, a, b);
     x = f2_pack(fmaxf(a, -64.f), fmaxf(b, -64.f));
   }
-  const u64 r = f2_add(x, f2_pack(kMagic, kMagic));
-  const u64 f = f2_sub(x, f2_sub(r, f2_pack(kMagic, kMagic)));
-  const float c1 = __uint_as_float(0x3f317213u), c2 = __uint_as_float(0x3e75fcdbu),
-              c3 = __uint_as_float(0x3d635d55u), c4 = __uint_as_float(0x3c1e760bu),
-              c5 = __uint_as_float(0x3aad4281u);
-  u64 p = f2_pack(c5, c5);
-  p = f2_add(f2_mul(p, f), f2_pack(c4, c4));
-  p = f2_add(f2_mul(p, f), f2_pack(c3, c3));
-  p = f2_add(f2_mul(p, f), f2_pack(c2, c2));
-  p = f2_add(f2_mul(p, f), f2_pack(c1, c1));
-  p = f2_add(f2_mul(p, f), f2_pack(1.f, 1.f));
-  float r0, r1, p0, p1;
-  f2_unpack(r, r0, r1);
-  f2_unpack(p, p0, p1);
-  // 2^x: i into the exponent; times 2^31 (exact), truncated, halved upwards
-  const u64 y = f2_mul(f2_pack(__uint_as_float(__float_as_uint(p0) + (__float_as_uint(r0) << 23)),
-                               __uint_as_float(__float_as_uint(p1) + (__float_as_uint(r1) << 23))),
-                       f2_pack(0x1p31f, 0x1p31f));
-  float y0, y1;
-  f2_unpack(y, y0, y1);
-  w0 = (__float2uint_rz(y0) + 1u) >> 1;
-  w1 = (__float2uint_rz(y1) + 1u) >> 1;
+  pow2_weight2(x, w0, w1);
   if (w0 < S.min_w) w0 = 0u;
   if (w1 < S.min_w) w1 = 0u;
 }

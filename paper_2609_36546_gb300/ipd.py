@@ -36,7 +36,9 @@ EXPORTS = ("ipd_attn_workspace_size", "ipd_verify_attn", "ipd_decode_attn",
            "ipd_loss_grad_workspace_size", "ipd_split_loss_grad", "ipd_sample_workspace_size",
            "ipd_sample", "ipd_kv_append", "ipd_kv_append_many", "ipd_set_attn_kernel_timing",
            "ipd_attn_kernel_time", "ipd_device_readable", "ipd_rope_table", "ipd_rope",
-           "ipd_rope_append", "ipd_prompt_attn", "ipd_sample_trunc")
+           "ipd_rope_append", "ipd_prompt_attn", "ipd_sample_trunc", "ipd_kv8_append",
+           "ipd_attn8_workspace_size", "ipd_verify_attn8", "ipd_verify_draft_workspace_size",
+           "ipd_verify_draft")
 # takeover / handback rules (IPD_RULE_*)
 RULE_TOPK, RULE_ENTROPY_S, RULE_ENTROPY_T, RULE_ALWAYS, RULE_NEVER = 0, 1, 2, 3, 4
 # element type of the dense gradient (IPD_DTYPE_*)
@@ -127,13 +129,44 @@ class _PromptArgs(ctypes.Structure):
                                        "total", "max_len")] + [("softmax_scale", ctypes.c_float)]
 
 
-# The same three layouts as packed bytes: filling a ctypes structure field by
+class _KV8Cache(ctypes.Structure):
+    _fields_ = [(n, c_p) for n in ("k_pages", "v_pages", "k_scale", "v_scale")] + \
+        [("num_pages", ctypes.c_int64)] + \
+        [(n, ctypes.c_int32) for n in ("page_size", "num_kv_heads", "head_dim")]
+
+
+class _Kv8AppendDesc(ctypes.Structure):
+    _fields_ = [("cache", _KV8Cache), ("k_new", c_p), ("v_new", c_p), ("k_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64), ("cu_new", c_p), ("seq_len", c_p), ("page_table", c_p)] + \
+        [(n, ctypes.c_int32) for n in ("max_pages", "num_reqs", "total_new")]
+
+
+class _Attn8Batch(ctypes.Structure):
+    _fields_ = [("cache", ctypes.POINTER(_KV8Cache)), ("num_q_heads", ctypes.c_int32),
+                ("num_reqs", ctypes.c_int32), ("q", c_p), ("cu_q", c_p), ("seq_len", c_p),
+                ("page_table", c_p), ("max_pages", ctypes.c_int32), ("total_q", ctypes.c_int32),
+                ("max_q_len", ctypes.c_int32), ("max_seq_len", ctypes.c_int32), ("out", c_p)]
+
+
+class _DraftArgs(ctypes.Structure):
+    _fields_ = [(n, c_p) for n in ("logits_target", "logits_draft", "logits_bonus")] + \
+        [(n, ctypes.c_int64) for n in ("target_stride", "draft_stride", "bonus_stride")] + \
+        [(n, c_p) for n in ("tokens", "cu_draft", "u_accept", "u_next", "inv_temp_target",
+                            "inv_temp_draft", "n_accept", "next_token", "logp_target",
+                            "logp_draft")] + \
+        [(n, ctypes.c_int32) for n in ("num_reqs", "total", "vocab")]
+
+
+# Layouts of the small calls as packed bytes: filling a ctypes structure field by
 # field takes longer than the smallest of these calls runs.
 _PACK_ROPE = struct.Struct("2P2q2P8i")
 _PACK_ROPE_APPEND = struct.Struct("5P5q2Pq4P10i")
 _PACK_PROMPT = struct.Struct("6P4q6if0P")
+_PACK_KV8_APPEND = struct.Struct("4Pq3i4x2P2q3P3i0P")
+_PACK_DRAFT = struct.Struct("3P3q10P3i0P")
 for _s, _c in ((_PACK_ROPE, _RopeArgs), (_PACK_ROPE_APPEND, _RopeAppendDesc),
-               (_PACK_PROMPT, _PromptArgs)):
+               (_PACK_PROMPT, _PromptArgs), (_PACK_KV8_APPEND, _Kv8AppendDesc),
+               (_PACK_DRAFT, _DraftArgs)):
     assert _s.size == ctypes.sizeof(_c), _c.__name__
 
 _lib.ipd_attn_workspace_size.restype = c_sz
@@ -188,6 +221,18 @@ _lib.ipd_prompt_attn.restype = c_i
 _lib.ipd_prompt_attn.argtypes = [c_p, c_p]  # (a packed _PromptArgs)
 _lib.ipd_sample_trunc.restype = c_i
 _lib.ipd_sample_trunc.argtypes = [c_p, ctypes.c_int64, c_i, c_i] + [c_p] * 9
+_lib.ipd_kv8_append.restype = c_i
+_lib.ipd_kv8_append.argtypes = [c_p, c_i, c_p]  # (packed _Kv8AppendDesc, one after the other)
+_lib.ipd_attn8_workspace_size.restype = c_sz
+_lib.ipd_attn8_workspace_size.argtypes = [ctypes.POINTER(_Attn8Batch), c_i,
+                                          ctypes.POINTER(_Attn8Batch), c_i]
+_lib.ipd_verify_attn8.restype = c_i
+_lib.ipd_verify_attn8.argtypes = [ctypes.POINTER(_Attn8Batch), c_i, ctypes.POINTER(_Attn8Batch),
+                                  c_i, ctypes.c_float, c_p, c_sz, c_p]
+_lib.ipd_verify_draft_workspace_size.restype = c_sz
+_lib.ipd_verify_draft_workspace_size.argtypes = [c_i, c_i, c_i]
+_lib.ipd_verify_draft.restype = c_i
+_lib.ipd_verify_draft.argtypes = [c_p, c_p, c_sz, c_p]  # (a packed _DraftArgs)
 _lib.ipd_set_attn_kernel_timing.restype = c_i
 _lib.ipd_set_attn_kernel_timing.argtypes = [c_i]
 _lib.ipd_attn_kernel_time.restype = c_i
@@ -632,6 +677,164 @@ def sample_trunc(logits: torch.Tensor, u: torch.Tensor, tokens: torch.Tensor,
                                  u.data_ptr(), _ptr(inv_temperature), _ptr(top_k), _ptr(top_p),
                                  _ptr(min_p), tokens.data_ptr(), _ptr(logp), _ptr(n_kept),
                                  _stream(stream)), "ipd_sample_trunc")
+
+
+class KVCache8:
+    """A paged KV cache held in 8 bits: k_pages / v_pages [num_pages, Hkv, 16, 128]
+    float8_e4m3fn, k_scale / v_scale [num_pages, Hkv] uint8 or float8_e8m0fnu (an
+    entry stands for its value times 2^(byte - 127)); contiguous.  A new cache
+    needs no particular contents: a page's scale starts with its first row."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: torch.Tensor,
+                 v_scale: torch.Tensor):
+        shape = tuple(k_pages.shape)
+        if len(shape) != 4 or tuple(v_pages.shape) != shape or \
+                k_pages.dtype is not torch.float8_e4m3fn or v_pages.dtype is not k_pages.dtype or \
+                not k_pages.is_contiguous() or not v_pages.is_contiguous():
+            _refuse("KVCache8: pages")
+        for t in (k_scale, v_scale):
+            if tuple(t.shape) != shape[:2] or not t.is_contiguous() or \
+                    t.dtype not in (torch.uint8, torch.float8_e8m0fnu):
+                _refuse("KVCache8: scales")
+        self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
+        self._fields = (k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr(),
+                        v_scale.data_ptr(), shape[0], shape[2], shape[1], shape[3])
+        self.c = _KV8Cache(*self._fields)
+
+    @classmethod
+    def empty(cls, num_pages: int, num_kv_heads: int, device="cuda") -> "KVCache8":
+        page = lambda: torch.zeros(num_pages, num_kv_heads, 16, 128, dtype=torch.uint8,
+                                   device=device).view(torch.float8_e4m3fn)
+        scale = lambda: torch.full((num_pages, num_kv_heads), 127, dtype=torch.uint8, device=device)
+        return cls(page(), page(), scale(), scale())
+
+    @property
+    def num_kv_heads(self) -> int:
+        return self.k_pages.shape[1]
+
+
+def kv8_append_many(appends, stream=None):
+    """Several appends to 8-bit caches in one launch: ``appends`` is a sequence
+    of (cache, k_new, v_new, cu_new, seq_len, page_table) tuples, each as in
+    kv8_append."""
+    packed = b""
+    for cache, k_new, v_new, cu_new, seq_len, page_table in appends:
+        shape, R, tshape = tuple(k_new.shape), cu_new.numel() - 1, page_table.shape
+        f = cache._fields
+        if shape != (shape[0], f[6], f[7]):
+            _refuse("ipd_kv8_append: k_new")
+        if cu_new.dtype is not _I32 or seq_len.dtype is not _I32 or page_table.dtype is not _I32 or \
+                cu_new.dim() != 1 or R < 0 or seq_len.numel() < R or len(tshape) != 2 or \
+                tshape[0] < R or not cu_new.is_contiguous() or not seq_len.is_contiguous() or \
+                not page_table.is_contiguous():
+            _refuse("ipd_kv8_append: offsets, lengths or page table")
+        packed += _PACK_KV8_APPEND.pack(
+            *f, k_new.data_ptr(), v_new.data_ptr(), _rows(k_new, shape, _BF16, "ipd_kv8_append: k_new"),
+            _rows(v_new, shape, _BF16, "ipd_kv8_append: v_new"), cu_new.data_ptr(),
+            seq_len.data_ptr(), page_table.data_ptr(), tshape[1], R, shape[0])
+    _check(_lib.ipd_kv8_append(packed, len(appends), _stream(stream)), "ipd_kv8_append")
+
+
+def kv8_append(cache: KVCache8, k_new, v_new, cu_new, seq_len, page_table, stream=None):
+    """Writes the new tokens' K/V rows ([n, Hkv, 128] bf16, rows contiguous, any
+    row stride) into the 8-bit cache's pages at the last positions of each
+    request's sequence (``seq_len`` is the length after the append), and brings
+    the pages' scales up to date."""
+    kv8_append_many(((cache, k_new, v_new, cu_new, seq_len, page_table),), stream)
+
+
+class AttnBatch8:
+    """One sub-batch of requests attending one 8-bit cache (see ipd_attn8_batch):
+    q [total_q, Hq, 128] bf16, cu_q [R+1], seq_len [R] and page_table
+    [R, max_pages] int32, out like q (all device, contiguous); max_q_len /
+    max_seq_len are host-known bounds."""
+
+    def __init__(self, cache: KVCache8, q, cu_q, seq_len, page_table, out, max_q_len: int,
+                 max_seq_len: int):
+        R = seq_len.numel()
+        if q.dim() != 3 or q.shape[2] != 128 or q.dtype is not _BF16 or out.dtype is not _BF16 or \
+                out.shape != q.shape or not q.is_contiguous() or not out.is_contiguous():
+            _refuse("AttnBatch8: q or out")
+        if any(t.dtype is not _I32 or not t.is_contiguous() for t in (cu_q, seq_len, page_table)) or \
+                cu_q.numel() != R + 1 or page_table.dim() != 2 or page_table.shape[0] < R:
+            _refuse("AttnBatch8: offsets, lengths or page table")
+        self.cache = cache
+        self._keep = (q, cu_q, seq_len, page_table, out)
+        self.c = _Attn8Batch(ctypes.pointer(cache.c), q.shape[1], R, _ptr(q), _ptr(cu_q),
+                             _ptr(seq_len), _ptr(page_table), page_table.shape[1], q.shape[0],
+                             max_q_len, max_seq_len, _ptr(out))
+        self.out = out
+
+
+def _arr8(batches):
+    n = len(batches)
+    if n == 0:
+        return None, 0
+    if n == 1:
+        return ctypes.pointer(batches[0].c), 1
+    return (_Attn8Batch * n)(*[b.c for b in batches]), n
+
+
+def attn8_workspace_size(verify: Sequence[AttnBatch8], decode: Sequence[AttnBatch8] = ()) -> int:
+    va, nv = _arr8(verify)
+    da, nd = _arr8(decode)
+    return int(_lib.ipd_attn8_workspace_size(va, nv, da, nd))
+
+
+def verify_attn8(verify: Sequence[AttnBatch8], decode: Sequence[AttnBatch8], softmax_scale: float,
+                 workspace: torch.Tensor, stream=None):
+    """verify_attn over 8-bit caches (``workspace``: attn8_workspace_size bytes)."""
+    va, nv = _arr8(verify)
+    da, nd = _arr8(decode)
+    _check(_lib.ipd_verify_attn8(va, nv, da, nd, softmax_scale, workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), _stream(stream)),
+           "ipd_verify_attn8")
+
+
+def verify_draft_workspace_size(num_reqs: int, total: int, vocab: int) -> int:
+    return int(_lib.ipd_verify_draft_workspace_size(num_reqs, total, vocab))
+
+
+def _logit_rows(t: torch.Tensor, n: int, V: int) -> int:
+    s = t.shape
+    if len(s) != 2 or s[0] != n or s[1] != V or t.dtype is not _BF16:
+        _refuse("ipd_verify_draft: logits")
+    row, col = t.stride()
+    if V > 1 and col != 1:
+        _refuse("ipd_verify_draft: logits")
+    return row if n > 1 else V
+
+
+def verify_draft(logits_target, logits_draft, tokens, cu_draft, u_accept, u_next, n_accept,
+                 next_token, workspace, logits_bonus: Optional[torch.Tensor] = None,
+                 inv_temp_target: Optional[torch.Tensor] = None,
+                 inv_temp_draft: Optional[torch.Tensor] = None,
+                 logp_target: Optional[torch.Tensor] = None,
+                 logp_draft: Optional[torch.Tensor] = None, stream=None):
+    """Verification of drafted tokens by rejection: ``logits_target`` and
+    ``logits_draft`` [T, V] bf16 (entries contiguous, any row stride), ``tokens``
+    int32 [T], ``cu_draft`` int32 [R + 1], uniform numbers ``u_accept`` fp32 [T] and
+    ``u_next`` fp32 [R]; writes ``n_accept`` and ``next_token`` (int32 [R]) and, where
+    given, the drafted tokens' log-probabilities (fp32 [T]).  ``logits_bonus``
+    [R, V]: the target's rows behind the drafts; the temperatures are fp32 [R]."""
+    T, V = logits_target.shape
+    R = cu_draft.numel() - 1
+    f, i = _F32, _I32
+    for t, n, dt in ((tokens, T, i), (u_accept, T, f), (logp_target, T, f), (logp_draft, T, f),
+                     (cu_draft, R + 1, i), (u_next, R, f), (n_accept, R, i), (next_token, R, i),
+                     (inv_temp_target, R, f), (inv_temp_draft, R, f)):
+        if t is not None and (t.shape != (n,) or t.dtype is not dt or not t.is_contiguous()):
+            _refuse("ipd_verify_draft: per-token or per-request tensors")
+    a = _PACK_DRAFT.pack(
+        logits_target.data_ptr(), logits_draft.data_ptr(), _ptr(logits_bonus) or 0,
+        _logit_rows(logits_target, T, V), _logit_rows(logits_draft, T, V),
+        V if logits_bonus is None else _logit_rows(logits_bonus, R, V), tokens.data_ptr(),
+        cu_draft.data_ptr(), u_accept.data_ptr(), u_next.data_ptr(), _ptr(inv_temp_target) or 0,
+        _ptr(inv_temp_draft) or 0, n_accept.data_ptr(), next_token.data_ptr(),
+        _ptr(logp_target) or 0, _ptr(logp_draft) or 0, R, T, V)
+    _check(_lib.ipd_verify_draft(a, workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), _stream(stream)),
+           "ipd_verify_draft")
 
 
 def set_attn_kernel_timing(on: bool):

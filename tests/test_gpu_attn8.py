@@ -1,0 +1,363 @@
+"""Attention over the 8-bit cache on the GPU against plain attention in 64 bits
+over the values its bytes stand for (needs a GB300).
+
+Tolerance, with a = sum_j w_j |v_j| the weighted mean magnitude of what an output
+averages: the weights enter the product with V as two e4m3 terms, off by at most
+2^-9 of themselves and 2^-18 of the row's largest weight times scale, which over
+all keys is c = 2^-18 max_j (w_j 2^ev_j) sum_j |entry_j|; the output is rounded to
+bf16, 2^-8 (|o| + 2^-9 a).  q is exact to 2^-18 of its row's largest entry: a score
+of 128 terms is off by at most 128 2^-18 |q|max |k|max scale, below 2^-9 at the
+magnitudes here (4, 4 and 1 / 11.3 for most, checked for each case), and so is a
+weight, relative to itself; fp32 scores and sums stay far below.  Together
+2^-8 |o| + (2^-9 + 2^-9 + 2^-10) a + c.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+D = 128
+E4 = torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import __graft_entry__
+    __graft_entry__.build()
+    from paper_2609_36546_gb300 import ipd
+    ipd.device_error()
+    return ipd
+
+
+class Case:
+    def __init__(self, hq, hkv, q_len, length, seed=0, spread=2, spare=4):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        rn = lambda *s: torch.randn(*s, generator=g, device="cuda")
+        ri = lambda lo, hi, *s: torch.randint(lo, hi, s, generator=g, device="cuda")
+        self.hq, self.hkv, self.q_len, self.length = hq, hkv, q_len, length
+        pages = [(x + 15) // 16 for x in length]
+        n = sum(pages) + spare
+        perm, at = torch.randperm(n, generator=g, device="cuda").to(torch.int32), 0
+        self.table = torch.full((len(length), max(1, max(pages))), -1, dtype=torch.int32, device="cuda")
+        for r, x in enumerate(pages):
+            self.table[r, :x] = perm[at:at + x]
+            at += x
+        self.unused = perm[at:].long()
+        self.kp, self.vp = ((rn(n, hkv, 16, D) * 100).clamp(-448, 448).to(E4) for _ in "kv")
+        self.ks, self.vs = ((120 + ri(-spread, spread + 1, n, hkv)).to(torch.uint8) for _ in "kv")
+        self.ks.clamp_(max=120)
+        self.q = rn(sum(q_len), hq, D).to(torch.bfloat16)
+        self.n = n
+
+    def batch(self, lib, out=None):
+        cu = torch.tensor([0] + self.q_len).cumsum(0).to(torch.int32).cuda()
+        self.out = torch.full_like(self.q, 7.0) if out is None else out
+        cache = lib.KVCache8(self.kp, self.vp, self.ks, self.vs)
+        return lib.AttnBatch8(cache, self.q, cu, torch.tensor(self.length, dtype=torch.int32, device="cuda"), self.table,
+                              self.out, max(1, max(self.q_len)), max(1, max(self.length)))
+
+    def wide(self, r, h):
+        page = self.table[r, :(self.length[r] + 15) // 16].long()
+        one = lambda p, s: (p.view(torch.uint8)[page, h].view(E4).double(), torch.exp2(s[page, h].double() - 127)[:, None, None])
+        (k, fk), (v, fv) = one(self.kp, self.ks), one(self.vp, self.vs)
+        n = self.length[r]
+        return (k * fk).view(-1, D)[:n], v.view(-1, D)[:n], fv.expand(-1, 16, 1).reshape(-1)[:n]
+
+    def ref(self, scale):
+        """(output, tolerance) in 64 bits; only visible keys enter a sum."""
+        out = torch.zeros(self.q.shape, dtype=torch.float64, device="cuda")
+        tol, G, row = torch.zeros_like(out), self.hq // self.hkv, 0
+        for r, n in enumerate(self.q_len):
+            for h in range(self.hkv):
+                k, v, fv = self.wide(r, h) if n else (None,) * 3
+                for i in range(n):
+                    m = self.length[r] - n + i + 1
+                    q = self.q[row + i, h * G:(h + 1) * G].double()
+                    w = torch.softmax(q @ k[:m].T * scale, -1) * fv[:m]
+                    x = v[:m]
+                    if torch.isfinite(x).all():
+                        o, a, s = w @ x, w @ x.abs(), x.abs().sum(0)
+                    else:
+                        o = (w[:, :, None] * x).sum(1)
+                        a, s = o.abs().nan_to_num(1.0), torch.ones_like(x[0])
+                    c = 2.0 ** -18 * w.amax(-1, keepdim=True) * s
+                    out[row + i, h * G:(h + 1) * G] = o
+                    tol[row + i, h * G:(h + 1) * G] = 2.0 ** -8 * o.abs() + (2.0 ** -8 + 2.0 ** -10) * a + c
+            row += n
+        return out, tol
+
+
+def _run(lib, *cases, scale=D ** -0.5, decode=0):
+    bs = [c.batch(lib) for c in cases]
+    v, d = bs[:len(bs) - decode], bs[len(bs) - decode:]
+    ws = torch.full((max(256, lib.attn8_workspace_size(v, d)),), 0xff, dtype=torch.uint8, device="cuda")
+    lib.verify_attn8(v, d, scale, ws)
+    return ws
+
+
+def _check(c, scale=D ** -0.5):
+    want, tol = c.ref(scale)
+    fine = torch.isfinite(want)
+    assert torch.equal(fine, torch.isfinite(c.out))
+    err = (c.out.double() - want).abs()
+    assert bool((err <= tol)[fine].all()), float((err / tol)[fine].max())
+    return float((err / tol.clamp_min(1e-30))[fine].max()) if fine.any() else 0.0
+
+
+@pytest.mark.parametrize("hq,hkv,q_len,length", [
+    (16, 8, [1], [1]), (16, 8, [1], [77]), (32, 4, [1], [1000]), (16, 8, [1, 1, 1, 1, 1], [15, 16, 17, 128, 129]),
+    (16, 8, [1, 0, 1], [127, 5, 2049]),
+    (32, 4, [16, 5, 1, 0, 8], [16, 300, 129, 0, 1024]),         # spans up to 128 rows; a whole prompt as a span
+    (32, 4, [8, 9, 2], [500, 501, 640]), (10, 2, [9, 3, 0, 1], [9, 1500, 77, 31]), (7, 1, [3, 1], [200, 7]),
+    (12, 4, [5, 11], [640, 127]), (8, 8, [1, 16], [33, 400]), (128, 1, [1, 2], [300, 130]), (100, 1, [3], [257]),
+    (64, 1, [1, 1], [4000, 20]), (1, 1, [40], [1025]), (64, 64, [2], [90]), (2, 1, [100, 17], [100, 300])])
+def test_attn8(lib, hq, hkv, q_len, length):
+    c = Case(hq, hkv, q_len, length, seed=hq + len(length))
+    _run(lib, c)
+    _check(c)
+    assert lib.device_error() == 0
+
+
+@pytest.mark.parametrize("hq,hkv,q,length", [(32, 4, 1, 30011), (16, 8, 1, 9000), (32, 4, 13, 20000), (4, 2, 3, 70001)])
+def test_long_contexts_are_split(lib, hq, hkv, q, length):
+    c = Case(hq, hkv, [q], [length], seed=q)
+    _run(lib, c)
+    _check(c)
+
+
+def test_many_requests(lib):
+    """More requests than CTAs, lengths 1 to 400, spans 0 to 6."""
+    g = torch.Generator().manual_seed(1)
+    length = torch.randint(1, 401, (400,), generator=g).tolist()
+    q_len = [min(int(x), n) for x, n in zip(torch.randint(0, 7, (400,), generator=g), length)]
+    c = Case(8, 2, q_len, length, seed=2)
+    _run(lib, c)
+    _check(c)
+
+
+def test_several_batches_in_one_call(lib):
+    """Spans over two caches and decode tokens over both, and a batch without
+    queries: the same bytes as one call each."""
+    cs = [Case(32, 4, [8, 3], [300, 4000], seed=1), Case(16, 8, [2, 16], [900, 31], seed=2), Case(4, 4, [0], [20], seed=3),
+          Case(16, 8, [1, 1, 1], [100, 2, 3000], seed=4), Case(32, 4, [1], [777], seed=5)]
+    _run(lib, *cs, decode=2)
+    for c in cs:
+        _check(c)
+
+
+def test_scores_that_grow_and_fall(lib):
+    """Keys that grow along the sequence by powers of two (the running maximum moves
+    far, tile after tile) and that fall; and large queries."""
+    for sign in (1, -1):
+        for q_len, length in (([1, 1], [3000, 513]), ([16, 9], [2000, 700])):
+            c = Case(32, 4, q_len, length, seed=7)
+            for r in range(2):
+                n = (length[r] + 15) // 16
+                step = torch.arange(n, device="cuda") * 6 // n
+                c.ks[c.table[r, :n].long()] = ((118 + sign * step) if sign > 0 else (124 - step)).to(torch.uint8)[:, None]
+            # q is exact to 2^-18: scores of up to 2^7 larger keys need smaller queries
+            c.q.mul_(2.0 ** -4)
+            _run(lib, c)
+            _check(c)
+
+
+def test_values_of_very_different_scale(lib):
+    """Pages whose V scales lie 60 binades apart, dominated by either kind; zero
+    pages with the least scale."""
+    for far in (30, -30):
+        c = Case(16, 8, [1, 4], [900, 2000], seed=3, spread=0)
+        for r in range(2):
+            page = c.table[r, ::3][c.table[r, ::3] >= 0].long()
+            c.vs[page] = torch.tensor(120 + far, dtype=torch.uint8, device="cuda")
+            c.vs[c.table[r, 0].long()] = 60
+            zero = c.table[r, 1].long()
+            c.vs[zero] = 87
+            c.vp.view(torch.uint8)[zero] = 0
+        _run(lib, c)
+        _check(c)
+        # weights that fall steeply: the pages of the larger scale have next to no weight
+        c.ks[c.table[:, ::3][c.table[:, ::3] >= 0].long()] = 90
+        c.q.mul_(4.0)
+        _run(lib, c)
+        _check(c)
+
+
+def test_equal_keys_and_one_row_of_weight(lib):
+    """All keys equal (the output is the mean of V), and one key far above the rest."""
+    c = Case(32, 4, [2], [5000], seed=5)
+    c.kp.view(torch.uint8)[:] = 0x30
+    c.ks.fill_(115)
+    _run(lib, c)
+    _check(c)
+    c.kp.view(torch.uint8)[c.table[0, 3].long(), :, 5] = (torch.sign(c.q[0, ::8].float()) * 100).to(E4).view(torch.uint8)
+    _run(lib, c)
+    _check(c)
+
+
+def test_hidden_bytes_reach_nothing(lib):
+    """NaN in every slot that no row sees: behind a sequence's end, in unused pages,
+    in scales of unused pages; and NaN in a span's own keys reaches the rows that see
+    them, no other."""
+    c = Case(32, 4, [1, 6, 3, 16], [77, 300, 16, 250], seed=6)
+    want, tol = c.ref(D ** -0.5)
+    for r, n in enumerate(c.length):
+        if n % 16:
+            page = c.table[r, n // 16].long()
+            c.kp.view(torch.uint8)[page, :, n % 16:] = 0x7f
+            c.vp.view(torch.uint8)[page, :, n % 16:] = 0xff
+    for p, s in ((c.kp, c.ks), (c.vp, c.vs)):
+        p.view(torch.uint8)[c.unused] = 0x7f
+        s[c.unused] = 255
+    _run(lib, c)
+    assert bool(((c.out.double() - want).abs() <= tol).all())
+    # the span's 4th key of request 1: V in some dims, K of its 5th in one head
+    at = lambda r, pos: (c.table[r, pos // 16].long(), pos % 16)
+    page, slot = at(1, 294 + 3)
+    c.vp.view(torch.uint8)[page, 2, slot, 3:40] = 0x7f
+    page, slot = at(1, 294 + 4)
+    c.kp.view(torch.uint8)[page, 1, slot, 7] = 0xff
+    page, slot = at(3, 234 + 15)
+    c.vp.view(torch.uint8)[page, :, slot, 100] = 0x7f
+    want, tol = c.ref(D ** -0.5)
+    _run(lib, c)
+    nan = torch.isnan(want)
+    assert int(nan.sum()) == 3 * 8 * 37 + 2 * 8 * 128 + 32
+    _check(c)
+
+
+def test_rows_do_not_reach_each_other(lib):
+    """A NaN and an infinite query, and one 2^40 times as large, beside ordinary ones."""
+    c = Case(32, 4, [3, 1], [300, 900], seed=8)
+    want, tol = c.ref(D ** -0.5)
+    c.q[1, 5, 3] = float("nan")
+    c.q[2, 9, 100] = float("inf")
+    c.q[0, 20] *= 2.0 ** 40
+    _run(lib, c)
+    keep = torch.ones(4, 32, dtype=torch.bool, device="cuda")
+    keep[1, 5] = keep[2, 9] = keep[0, 20] = False
+    assert bool(((c.out.double() - want).abs() <= tol)[keep].all())
+    assert bool(torch.isnan(c.out[1, 5]).all())
+    # the large query's weight lies on its best key alone
+    k, v, fv = c.wide(0, 2)
+    m = 300 - 3 + 1
+    best = (c.q[0, 20].double() @ k[:m].T).argmax()
+    assert bool(((c.out[0, 20].double() - v[best] * fv[best]).abs() <= 2.0 ** -7 * v[best].abs() * fv[best] + 1e-9).all())
+
+
+def test_nan_scales_and_zero_queries(lib):
+    c = Case(16, 8, [1, 1, 2], [100, 200, 300], seed=9)
+    c.q[1].zero_()  # equal weights
+    c.ks[c.table[0, 2].long(), 3] = 255
+    c.vs[c.table[2, 1].long(), 6] = 255
+    _run(lib, c)
+    keep = torch.ones(4, 16, dtype=torch.bool, device="cuda")
+    keep[0, 6:8] = keep[2:, 12:14] = False
+    want, tol = c.ref(D ** -0.5)
+    assert bool(((c.out.double() - want).abs() <= tol)[keep].all())
+    assert bool(torch.isnan(c.out[~keep]).all())
+
+
+def test_bad_pages_lengths_and_offsets(lib):
+    """A page outside the pool leaves its keys out (all of them: zeros); a request
+    with a bad length or offsets is not written; the others are as they were."""
+    c = Case(16, 8, [1, 2, 1, 3], [100, 200, 33, 300], seed=10)
+    want, tol = c.ref(D ** -0.5)
+    for what, code in (("page", 1), ("all pages", 1), ("length", 2), ("short", 2), ("offsets", 6)):
+        b = c.batch(lib)
+        q, cu, ln, table, out = b._keep
+        table, other = table.clone(), slice(1, 3)
+        if what == "page":
+            table[1, 3] = c.n + 9
+        elif what == "all pages":
+            table[1] = -1
+        elif what == "length":
+            ln[1] = 301
+        elif what == "short":
+            ln[1] = 1
+        else:
+            cu[2] = 9  # past the tensor for request 1, out of order for request 2
+            other = slice(1, 4)
+        cache = lib.KVCache8(c.kp, c.vp, c.ks, c.vs)
+        b = lib.AttnBatch8(cache, q, cu, ln, table, out, 3, 300)
+        ws = torch.empty(lib.attn8_workspace_size([b]), dtype=torch.uint8, device="cuda")
+        lib.verify_attn8([b], [], D ** -0.5, ws)
+        assert lib.device_error() == code, what
+        rest = torch.ones(7, dtype=torch.bool, device="cuda")
+        rest[other] = False
+        assert bool(((out.double() - want).abs() <= tol)[rest].all()), what
+        if what == "all pages":
+            assert bool((out[1:3] == 0).all())
+        elif what == "page":
+            keys = torch.ones(200, dtype=torch.bool, device="cuda")
+            keys[48:64] = False
+            k, v, fv = c.wide(1, 5)
+            w = torch.softmax(c.q[1, 10].double() @ k[:199][keys[:199]].T * D ** -0.5, -1)
+            o = w @ (v * fv[:, None])[:199][keys[:199]]
+            assert bool(((out[1, 10].double() - o).abs() < 0.02).all())
+        else:
+            assert bool((out[other] == 7.0).all()), what
+
+
+def test_rows_behind_the_last_request_stay(lib):
+    c = Case(16, 8, [1, 2], [50, 60], seed=11)
+    c.q = torch.cat([c.q, c.q])
+    b = c.batch(lib)
+    ws = torch.empty(lib.attn8_workspace_size([b]), dtype=torch.uint8, device="cuda")
+    lib.verify_attn8([b], [], D ** -0.5, ws)
+    assert bool((c.out[3:] == 7.0).all()) and not bool((c.out[:3] == 7.0).all(-1).any())
+
+
+def test_captured_twice_over_one_workspace(lib):
+    """Two captured calls that share a workspace, replayed in turn with new contents,
+    and a call on another stream: bytes as those of a plain call, time after time."""
+    c1, c2 = Case(32, 4, [4, 1], [900, 3000], seed=12), Case(16, 8, [1, 1], [5000, 40], seed=13)
+    b1, b2 = c1.batch(lib), c2.batch(lib)
+    ws = torch.empty(max(lib.attn8_workspace_size([b]) for b in (b1, b2)), dtype=torch.uint8, device="cuda")
+    for b in (b1, b2):
+        lib.verify_attn8([b], [], D ** -0.5, ws)
+    plain = [b.out.clone() for b in (b1, b2)]
+    graphs = []
+    for b in (b1, b2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            lib.verify_attn8([b], [], D ** -0.5, ws)
+        graphs.append(g)
+    for _ in range(3):
+        for b in (b1, b2):
+            b.out.fill_(7.0)
+        ws.fill_(0xff)
+        for g in graphs:
+            g.replay()
+        assert all(torch.equal(b.out, p) for b, p in zip((b1, b2), plain))
+    c1.q.copy_(torch.randn_like(c1.q.float()))
+    graphs[0].replay()
+    _check(c1)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    b2.out.fill_(7.0)
+    torch.cuda.synchronize()
+    lib.verify_attn8([b2], [], D ** -0.5, ws, stream=s)
+    s.synchronize()
+    assert torch.equal(b2.out, plain[1])
+
+
+def test_pools_past_32_bits(lib):
+    """Pages at the end of a pool of more than 2^32 bytes a tensor."""
+    n, hkv = (1 << 18) + 64, 8
+    cache = lib.KVCache8.empty(n, hkv)
+    c = Case(16, 8, [2], [700], seed=14)
+    pages = c.table[0].long()
+    high = torch.arange(n - 60, n - 60 + len(pages), device="cuda")
+    for a, b in ((cache.k_pages, c.kp), (cache.v_pages, c.vp)):
+        a.view(torch.uint8)[high] = b.view(torch.uint8)[pages]
+    cache.k_scale[high], cache.v_scale[high] = c.ks[pages], c.vs[pages]
+    b = c.batch(lib)
+    q, cu, ln, _, out = b._keep
+    b = lib.AttnBatch8(cache, q, cu, ln, high.to(torch.int32)[None].contiguous(), out, 2, 700)
+    ws = torch.empty(lib.attn8_workspace_size([b]), dtype=torch.uint8, device="cuda")
+    lib.verify_attn8([b], [], D ** -0.5, ws)
+    _check(c)

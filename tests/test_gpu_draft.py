@@ -1,0 +1,212 @@
+"""Verification of drafted tokens on the GPU (needs a GB300): verdicts and tokens
+equal to the definition's in whole numbers; log-probabilities to 2^-21 of
+themselves plus 2^-21 (one fp32 rounding, 2^-24 relative; x itself is exact, and
+the weights' sum is off by at most 2^-22 from the softmax's: 1.9e-7 a weight)."""
+import numpy as np
+import pytest
+import torch
+
+from tests import draft_ref as ref
+
+pytestmark = pytest.mark.gpu
+NINF = float("-inf")
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import __graft_entry__
+    __graft_entry__.build()
+    from paper_2609_36546_gb300 import ipd
+    ipd.device_error()
+    return ipd
+
+
+class Case:
+    def __init__(self, k, V, seed=0, noise=0.8, bonus=True, temps=True, sigma=2.0):
+        g = torch.Generator().manual_seed(seed)
+        T, R = sum(k), len(k)
+        self.k, self.V = k, V
+        base = torch.randn(T, V, generator=g) * sigma
+        base.scatter_add_(1, torch.randint(0, V, (T, min(V, 8)), generator=g), torch.full((T, min(V, 8)), 6.0))
+        self.target = base.to(torch.bfloat16)
+        self.draft = (base + noise * torch.randn(T, V, generator=g)).to(torch.bfloat16)
+        self.bonus = (torch.randn(R, V, generator=g) * sigma).to(torch.bfloat16) if bonus else None
+        pick = lambda: torch.tensor([1.0, 1 / 0.7, 1 / 1.3])[torch.randint(0, 3, (R,), generator=g)] if temps else torch.ones(R)
+        self.inv_p, self.inv_q = pick(), pick()
+        per = torch.repeat_interleave(self.inv_q, torch.tensor(k, dtype=torch.int64))[:, None]
+        self.tokens = torch.multinomial(torch.softmax(self.draft.float() * per, -1), 1, generator=g).squeeze(1).int() \
+            if T else torch.zeros(0, dtype=torch.int32)
+        self.u, self.u_next = torch.rand(T, generator=g), torch.rand(R, generator=g)
+        self.temps = temps
+        self.cu = torch.tensor([0] + k).cumsum(0).int()
+
+    def run(self, lib, place=lambda t: t.cuda(), logp=True, stream=None):
+        R, T = len(self.k), sum(self.k)
+        dev = lambda t: None if t is None else t.cuda()
+        self.n, self.nxt = (torch.full((R,), 77, dtype=torch.int32, device="cuda") for _ in "ab")
+        self.lp, self.lq = (torch.full((T,), 77.0, device="cuda") for _ in "ab")
+        ws = torch.full((max(256, lib.verify_draft_workspace_size(R, T, self.V)),), 0xff, dtype=torch.uint8, device="cuda")
+        lib.verify_draft(place(self.target), place(self.draft), dev(self.tokens), dev(self.cu), dev(self.u), dev(self.u_next),
+                         self.n, self.nxt, ws, logits_bonus=None if self.bonus is None else place(self.bonus),
+                         inv_temp_target=dev(self.inv_p) if self.temps else None,
+                         inv_temp_draft=dev(self.inv_q) if self.temps else None,
+                         logp_target=self.lp if logp else None, logp_draft=self.lq if logp else None)
+        return self
+
+    def want(self):
+        f = lambda t: None if t is None else t.float().numpy()
+        return ref.verify(f(self.target), f(self.draft), f(self.bonus), self.tokens.tolist(), self.cu.tolist(),
+                          self.u.tolist(), self.u_next.tolist(), self.inv_p.numpy(), self.inv_q.numpy())
+
+    def check(self):
+        verdict, logp = self.want()
+        assert list(zip(self.n.tolist(), self.nxt.tolist())) == verdict
+        got = torch.stack([self.lp, self.lq], 1).double().cpu().numpy()
+        logp = np.array(logp, dtype=np.float64).reshape(-1, 2)
+        assert np.array_equal(np.isfinite(got), np.isfinite(logp)) and np.array_equal(np.isnan(got), np.isnan(logp))
+        ok = np.isfinite(logp)
+        assert np.all(np.abs(got[ok] - logp[ok]) <= 2.0 ** -21 * np.abs(logp[ok]) + 2.0 ** -21)
+        return verdict
+
+
+@pytest.mark.parametrize("k,V", [([4], 1000), ([1], 8), ([0, 3, 1], 1001), ([2, 5, 0, 7], 4096), ([3], 50021), ([1, 1], 1),
+                                 ([2], 7), ([16, 9], 2049), ([1], 151936), ([2, 2], 151933)])
+@pytest.mark.parametrize("bonus", [True, False])
+def test_verdicts_are_the_definition(lib, k, V, bonus):
+    c = Case(k, V, seed=V + len(k), bonus=bonus).run(lib)
+    c.check()
+    assert lib.device_error() == 0
+
+
+def test_many_requests_of_both_kinds(lib):
+    """600 requests: both outcomes, every split of a row over CTAs."""
+    g = torch.Generator().manual_seed(3)
+    c = Case(torch.randint(0, 5, (600,), generator=g).tolist(), 515, seed=4, noise=1.0).run(lib)
+    verdict = c.check()
+    share = sum(n for n, _ in verdict) / sum(c.k)
+    assert 0.2 < share < 0.95
+
+
+def test_equal_models_accept_everything(lib):
+    c = Case([5, 3], 3001, seed=5, noise=0.0, temps=False)
+    c.u[:] = torch.nextafter(torch.tensor(1.0), torch.tensor(0.0))
+    assert [n for n, _ in c.run(lib).check()] == [5, 3]
+
+
+def test_the_distribution_is_the_target_s(lib):
+    """Small vocabulary, many independent requests of one draft each: the emitted
+    first token (the draft, or the residual's) follows the target's softmax.  Chi
+    square of 40,000 draws over 12 entries: below 40 but for one run in 30,000."""
+    g = torch.Generator().manual_seed(6)
+    R, V = 40000, 12
+    p, q = torch.randn(V, generator=g) * 1.5, torch.randn(V, generator=g) * 1.5
+    c = Case([1] * R, V, seed=7, bonus=False, temps=False)
+    c.target, c.draft = (t.to(torch.bfloat16).expand(R, V).contiguous() for t in (p, q))
+    c.tokens = torch.multinomial(torch.softmax(c.draft[0].float(), -1), R, replacement=True, generator=g).int()
+    c.run(lib)
+    first = torch.where(c.n == 1, c.tokens.cuda(), c.nxt)
+    seen = torch.bincount(first.long(), minlength=V).double().cpu()
+    want = torch.softmax(c.target[0].double(), -1) * R
+    assert float(((seen - want) ** 2 / want).sum()) < 40
+
+
+def test_uniform_numbers_at_the_ends(lib):
+    c = Case([3, 3, 3, 3], 999, seed=8)
+    c.u[:3], c.u[3:6], c.u[6:9] = 0.0, float("nan"), 0.99999994
+    c.u_next[:] = torch.tensor([0.0, 0.99999994, float("nan"), 1.5])
+    c.run(lib).check()
+
+
+def test_unusual_rows(lib):
+    """Rows with nothing left, with NaN, with +inf, masks of the type's lowest value,
+    a draft token the draft model gives nothing, a token the target gives nothing."""
+    c = Case([2, 2, 2, 2, 2, 2, 2, 2], 300, seed=9)
+    low = torch.finfo(torch.bfloat16).min
+    c.target[0] = NINF                                     # the target's row has no entry
+    c.draft[2] = NINF                                      # the draft's row has none
+    c.target[4, ::2], c.draft[4, 1::2] = float("nan"), float("nan")
+    c.target[6, 17] = c.draft[6, 18] = float("inf")
+    c.target[8, 5:], c.draft[8, 7:] = low, low
+    c.draft[10, c.tokens[10]] = NINF
+    c.target[12, c.tokens[12]] = NINF
+    c.target[14:], c.draft[14:] = low, low
+    c.target[13, :], c.draft[13, :] = -0.0, 0.0
+    c.run(lib).check()
+    c.bonus[:] = NINF
+    c.u[:] = 0.0
+    c.run(lib).check()
+
+
+def test_bad_tokens_settings_and_offsets(lib):
+    c = Case([2, 3, 1, 2], 500, seed=10)
+    c.tokens[0], c.tokens[3] = 500, -1
+    c.run(lib).check()
+    assert lib.device_error() == 3
+    c = Case([2, 3, 1, 2], 500, seed=11)
+    want, _ = c.want()
+    for bad in (0.0, -1.0, float("nan"), float("inf"), 3e38):
+        c.inv_q[1] = bad
+        c.run(lib)
+        assert lib.device_error() == 8
+        assert (int(c.n[1]), int(c.nxt[1])) == (0, -1) and bool(torch.isnan(c.lp[2:5]).all())
+        assert [(int(c.n[r]), int(c.nxt[r])) for r in (0, 2, 3)] == [want[r] for r in (0, 2, 3)]
+        assert lib.device_error() == 0
+    c = Case([2, 3, 1, 2], 500, seed=11)
+    for cu in ([0, 2, 5, 6, 9], [0, 2, 5, -1, 8], [-3, 2, 5, 6, 8]):
+        c.cu = torch.tensor(cu).int()
+        c.run(lib)
+        assert lib.device_error() == 6, cu
+        for r in range(4):
+            if not (0 <= cu[r] <= cu[r + 1] <= 8):
+                assert (int(c.n[r]), int(c.nxt[r])) == (0, -1)
+            elif (cu[r], cu[r + 1]) == (int(Case([2, 3, 1, 2], 500, seed=11).cu[r]), int(Case([2, 3, 1, 2], 500, seed=11).cu[r + 1])):
+                assert (int(c.n[r]), int(c.nxt[r])) == want[r], (cu, r)
+    # positions that no offsets cover stay as they are
+    c = Case([2, 3], 100, seed=12)
+    c.cu = torch.tensor([1, 2, 4]).int()
+    c.run(lib)
+    assert float(c.lp[0]) == 77.0 and float(c.lq[4]) == 77.0 and float(c.lp[1]) != 77.0
+
+
+@pytest.mark.parametrize("shift,extra", [(1, 0), (3, 5), (8, 3), (0, 1)])
+def test_rows_of_any_alignment(lib, shift, extra):
+    """Rows that begin inside a 16-byte vector, target and draft differently, beside
+    entries that would change every sum."""
+    c = Case([2, 3], 701, seed=13)
+
+    def place(t):
+        s = shift if t is c.target else 2 * shift + 1 if t is c.draft else 0
+        wide = torch.full((t.shape[0], s + 701 + extra), 99.0, dtype=torch.bfloat16, device="cuda")
+        wide[:, s:s + 701] = t.cuda()
+        return wide[:, s:s + 701]
+
+    c.run(lib, place).check()
+
+
+def test_without_log_probabilities_and_captured(lib):
+    c = Case([2, 4, 0], 2000, seed=14)
+    c.run(lib, logp=False)
+    want, _ = c.want()
+    assert list(zip(c.n.tolist(), c.nxt.tolist())) == want
+    args = [t.cuda() for t in (c.target, c.draft, c.tokens, c.cu, c.u, c.u_next)]
+    n, nxt = (torch.zeros(3, dtype=torch.int32, device="cuda") for _ in "ab")
+    ws = torch.empty(256, dtype=torch.uint8, device="cuda")
+    bonus, ip, iq = c.bonus.cuda(), c.inv_p.cuda(), c.inv_q.cuda()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lib.verify_draft(*args, n, nxt, ws, logits_bonus=bonus, inv_temp_target=ip, inv_temp_draft=iq)
+    for seed in (14, 15, 16):
+        c = Case([2, 4, 0], 2000, seed=seed)
+        for a, b in zip(args + [bonus, ip, iq], (c.target, c.draft, c.tokens, c.cu, c.u, c.u_next, c.bonus, c.inv_p, c.inv_q)):
+            a.copy_(b)
+        ws.fill_(0xff)
+        graph.replay()
+        assert list(zip(n.tolist(), nxt.tolist())) == c.want()[0]
+
+
+def test_no_requests_and_no_drafts(lib):
+    c = Case([0, 0], 123, seed=17).run(lib)
+    c.check()
+    Case([0, 0], 123, seed=18, bonus=False).run(lib).check()
