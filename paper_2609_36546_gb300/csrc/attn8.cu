@@ -5,12 +5,39 @@
 // k_j, v_j e4m3 values, ek, ev the scales of their page and head, key j seen by
 // query i of a span of n where j <= L - n + i.
 //
-// The plainest form: a CTA takes 16 rows (query, head of the group) of one request
-// and KV head over all its keys, 32 at a time, with the running maximum and sum.
+// What bounds it: 256 bytes a key and KV head against 512 flop a row, so HBM; a
+// tile of 128 keys (32 KB) is about 1,400 cycles of an SM's share, which is what
+// everything else has to stay below.  The tensor cores take the cache's bytes as
+// they are (kind::f8f6f4), nothing is unpacked:
+//   S^T = K Q^T   keys are the 128 rows of the product, the rows (query, head of
+//                 the group) its columns; q as two e4m3 terms of its row's scale
+//   O^T = V^T P^T dims are the rows; V and P in the order they lie in, keys last
+// The transposed form makes the cost follow the number of rows (16, 32 or 64
+// columns) and gives every thread one key: a key's scales are two numbers of its
+// thread.  P goes into the second product as two e4m3 terms, the second times 16,
+// side by side as columns; O's two halves are added at the end.
+//
+// Softmax.  p = 2^(s ck ar + dE - ref): ck holds the softmax scale and K's, ar q's
+// row scale, dE V's exponent relative to that of the item's first tile.  ref is the
+// row's largest so far, less 5; it moves (and O and the sums are rescaled) only
+// when a weight would leave 2^8, so most tiles need no maximum across threads.  The
+// reference includes V's scale, since it is the product that has to fit e4m3.
+//
+// Work.  All (request, KV head, block of 128 rows, tile) units in one line, cut into
+// equal parts, a CTA each: nothing is claimed, the cut depends on the lengths alone.
+// A task cut between CTAs leaves normalised partial rows; the CTA that finishes last
+// joins them in order.
+//
+// Warps: 0-3 and 4-7 softmax (tiles in turn; with more than 64 rows 64 rows of every
+// tile each), 8 loads K, 9 loads V, 10 issues the first product, 11 the second, 12
+// finds the items, page ids and scales, 13-15 split the queries.
+#include <cuda.h>
 #include <cuda_runtime.h>
+#include <cudaTypedefs.h>
 #include <stdint.h>
 #include <string.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "common.cuh"
@@ -23,110 +50,1008 @@ static std::atomic<bool> g_attn8_used{false};
 
 namespace {
 
+typedef unsigned long long u64;
+
 constexpr int kD = 128;
 constexpr int kPage = 16;
-constexpr int kRows = 16;
-constexpr int kKeys = 32;
+constexpr int kKeys = 128;                // keys of a tile
+constexpr int kPages = kKeys / kPage;     // its pages
+constexpr int kTileBytes = kKeys * kD;    // 16 KB of K or V
+constexpr int kPageBytes = kPage * kD;
 constexpr int kMaxGroup = 128;
+constexpr int kBlockRows = 128;           // rows of a task
+constexpr int kRows = 64;                 // ... of a softmax warpgroup
+constexpr int kKStages = 3, kVStages = 4;
+constexpr int kMeta = 8;                  // tiles whose page ids and scales are at hand
+constexpr int kBatch = 4;                 // ... fetched at once
+constexpr int kSlots = 3;                 // items handed out
+constexpr int kThreads = 512;
+constexpr int kKWarp = 8, kVWarp = 9, kQkWarp = 10, kPvWarp = 11, kMetaWarp = 12, kQWarps = 3;
+constexpr int kItemReaders = 8 + 4 + kQWarps;
+constexpr int kRegsSoftmax = 200, kRegsAux = 56;
+static_assert(256 * kRegsSoftmax + 256 * kRegsAux <= kThreads * 128,
+              "the register split must fit the registers the block was launched with");
+static_assert(kBatch * kPages == 32, "a lane a page");
+
+constexpr uint32_t kTmemCols = 512;
+__host__ __device__ constexpr uint32_t col_s(int g) { return 64u * (uint32_t)g; }
+__host__ __device__ constexpr uint32_t col_o(int g) { return 128u + 128u * (uint32_t)g; }
+
+constexpr float kBase = 5.f;   // a row's reference is its largest exponent less this
+constexpr float kLimit = 8.f;  // weights stay below 2^8 (e4m3 ends at 448)
+constexpr float kLoScale = 16.f;
+constexpr int kFar = 100;      // V scales further apart than 2^100 count as that far
+constexpr int kNoPage = 1 << 20;  // in place of an exponent: no such page
 
 struct BatchDev {
-  const uint8_t *k, *v, *ks, *vs;
+  const uint8_t *ks, *vs;
   const uint16_t *q;
   uint16_t *out;
   const int *cu_q, *seq_len, *page_table;
-  int num_reqs, hq, hkv, group, max_pages, max_q_len, max_seq_len, total_q, blocks, num_pages;
-};
-struct Params {
-  BatchDev b[IPD_MAX_BATCHES];
-  int end[IPD_MAX_BATCHES];  // CTAs up to and with each batch
-  int n;
-  float scale_log2;
+  int num_reqs, hq, hkv, group, max_pages, max_q_len, max_seq_len, total_q, num_pages;
+  int rows_end;  // a pool row that is not there: loads as zeros
 };
 
-__global__ void __launch_bounds__(128) attn8_kernel(const __grid_constant__ Params P) {
-  __shared__ float q[kRows][kD], k[kKeys][kD + 1], v[kKeys][kD], s[kRows][kKeys], m[kRows], l[kRows],
-      alpha[kRows];
-  int bi = 0;
-  while (bi + 1 < P.n && (int)blockIdx.x >= P.end[bi]) ++bi;
-  const BatchDev &B = P.b[bi];
-  int u = blockIdx.x - (bi ? P.end[bi - 1] : 0);
-  const int rb = u % B.blocks, h = u / B.blocks % B.hkv, r = u / B.blocks / B.hkv;
-  const int c0 = B.cu_q[r], n = B.cu_q[r + 1] - c0, L = B.seq_len[r];
-  const int tid = threadIdx.x;
-  if (n < 0 || c0 < 0 || c0 + n > B.total_q) {
-    if (tid == 0) ipd_set_error(&g_attn8_err, IPD_DEVERR_SPAN);
-    return;
+struct Params {
+  CUtensorMap k[IPD_MAX_BATCHES], v[IPD_MAX_BATCHES];
+  BatchDev b[IPD_MAX_BATCHES];
+  int req_base[IPD_MAX_BATCHES + 1];
+  int n, total_reqs;
+  float scale_log2;
+  long long *prefix;  // [total_reqs + 1] units before each request
+  int4 *info;         // [total_reqs] length, queries, first row, tiles
+  int *done;          // [CTAs] parts of the task that starts in this CTA and goes on
+  float *part;        // [2 CTAs] partial rows: part_rows x 128, then part_rows log-sums
+  int part_rows;
+};
+
+struct Item {
+  int valid, b, c0, n, L, h;
+  int row0, rows;       // first row of the task among the request's, and number
+  int nr, both;         // columns of a warpgroup; whether both take every tile
+  int t0, t1;           // tiles
+  int part, cta0, cta1; // partial slot (-1: whole task) and the CTAs of the task
+};
+
+struct Meta {
+  float ck[kPages];  // K's scale times the softmax scale, in log2
+  int ev[kPages];    // V's exponent (128: NaN), or kNoPage
+  int y[kPages];     // first pool row of the page
+  int gap;           // a page that is not there lies among the keys
+};
+
+struct Shared {
+  alignas(1024) uint8_t k[kKStages][kTileBytes];
+  alignas(1024) uint8_t v[kVStages][kTileBytes];
+  alignas(1024) uint8_t q[2][2][2][kRows * kD];  // buffer, warpgroup, term
+  alignas(1024) uint8_t p[2][kKeys * 2 * kRows]; // a warpgroup's P; at the end, rows on their way
+  alignas(16) float4 state[2][kRows / 2];        // a pair of rows: ar, ar', -ref, -ref'
+  alignas(16) float alpha[2][kRows];
+  alignas(16) float red[2][4][kRows];
+  alignas(16) float qscale[kSlots][2][kRows];
+  float ref[2][kRows], sum[2][kRows];            // what the warpgroups hand each other at an item's end
+  int e0[2];
+  // first key of a span with a NaN in this dim of V, and whether there is one: of an
+  // item of one warpgroup (by warpgroup), and of both
+  int nan_key[3][kD], bad[3];
+  int last, abort;
+  uint32_t tmem;
+  Meta meta[kMeta];
+  Item item[kSlots];
+  uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
+  uint64_t pg_full[kMeta], sc_full[kMeta], meta_empty[kMeta];
+  uint64_t q_full[2], q_empty[2], s_full[2], s_empty[2], p_full[2], pv_done[2];
+  uint64_t item_full[kSlots], item_empty[kSlots], pair, drain[2];
+};
+constexpr int kSharedBytes = (int)sizeof(Shared) + 1024;  // the base is aligned by hand
+static_assert(kSharedBytes <= 232448, "shared memory of one CTA");
+
+// ---- PTX ---------------------------------------------------------------------
+IPD_DEVINL void tma_load_2d(void *dst, const CUtensorMap *map, int x, int y, uint64_t *bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(smem_u32(dst)),
+      "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)), "l"(policy)
+      : "memory");
+}
+// D[tmem] (+)= A[smem] B[smem], e4m3 operands, fp32 accumulation (one thread).
+IPD_DEVINL void tc_mma_f8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Instruction descriptor: e4m3 A and B, fp32 D; transposed operands are MN-major.
+__host__ __device__ constexpr uint32_t idesc_f8(int n, int transposed) {
+  return (1u << 4) | (uint32_t)transposed << 15 | (uint32_t)transposed << 16 | (uint32_t)(n >> 3) << 17 |
+         (128u >> 4) << 24;
+}
+// Shared-memory descriptor with 8-row groups of `row` bytes a row, swizzled over
+// the row (128, 64 or 32 bytes).
+IPD_DEVINL uint64_t sdesc(uint32_t saddr, int row) {
+  const uint64_t layout = row == 128 ? 2 : row == 64 ? 4 : 6;
+  return (uint64_t)((saddr & 0x3ffffu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(8 * row >> 4) << 32 | 1ull << 46 |
+         layout << 61;
+}
+IPD_DEVINL bool bar_or(int id, int threads, bool x) {
+  uint32_t r;
+  __syncwarp();
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 q, %3, 0;\n\t"
+      "barrier.cta.red.or.pred.aligned p, %1, %2, q;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r)
+      : "r"(id), "r"(threads), "r"((uint32_t)x)
+      : "memory");
+  return r != 0;
+}
+IPD_DEVINL void tc_st_32x32b_x16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+IPD_DEVINL void tc_ld_32x32b_x8(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+IPD_DEVINL u64 mul2(u64 a, u64 b) {
+  u64 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+IPD_DEVINL uint32_t half2_of(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+IPD_DEVINL uint32_t half2_sub(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+IPD_DEVINL uint32_t half2_mul(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+IPD_DEVINL void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+IPD_DEVINL void grid_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// ---- waits ---------------------------------------------------------------------
+// A wait that gives up after about a second, or as soon as another warp of the CTA
+// has given up; the clock and the flag are looked at every few tries only.
+IPD_DEVINL bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort) {
+  const long long t0 = clock64();
+  while (true) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+    if (*abort) return false;
+    if (clock64() - t0 > kWaitLimitCycles) {
+      ipd_set_error(&g_attn8_err, IPD_DEVERR_WAIT);
+      *abort = 1;
+      return false;
+    }
   }
-  if (n > B.max_q_len || L < n || L > B.max_seq_len) {
-    if (tid == 0) ipd_set_error(&g_attn8_err, IPD_DEVERR_SEQ_LEN);
-    return;
-  }
-  const int rows = min(kRows, n * B.group - rb * kRows);
-  if (rows <= 0) return;
-  auto at = [&](int i) {  // row i's place in q and out
-    const int row = rb * kRows + i;
-    return ((size_t)(c0 + row / B.group) * B.hq + h * B.group + row % B.group) * kD;
-  };
-  for (int i = 0; i < kRows; ++i) q[i][tid] = i < rows ? bf16f(B.q[at(i) + tid]) * P.scale_log2 : 0.f;
-  if (tid < kRows) m[tid] = -INFINITY, l[tid] = 0.f;
-  float o[kRows] = {};
-  for (int j0 = 0; j0 < L; j0 += kKeys) {
-    __syncthreads();
-    for (int j = 0; j < kKeys; ++j) {
-      const int key = j0 + j;
-      float kk = 0.f, vv = 0.f;
-      if (key < L) {
-        const int page = B.page_table[(size_t)r * B.max_pages + key / kPage];
-        if (page < 0 || page >= B.num_pages) {
-          if (tid == 0) ipd_set_error(&g_attn8_err, IPD_DEVERR_PAGE_ID);
-          kk = __uint_as_float(0xff800000u);  // marks the key
-        } else {
-          const size_t g = (size_t)page * B.hkv + h;
-          float f[4];
-          e4m3x4_to_floats(B.k[(g * kPage + key % kPage) * kD + tid], f);
-          kk = f[0] * e8m0(B.ks[g]);
-          e4m3x4_to_floats(B.v[(g * kPage + key % kPage) * kD + tid], f);
-          vv = f[0] * e8m0(B.vs[g]);
-        }
-      }
-      k[j][tid] = kk;
-      v[j][tid] = vv;
-    }
-    __syncthreads();
-    for (int e = tid; e < kRows * kKeys; e += 128) {
-      const int i = e / kKeys, j = e % kKeys, query = (rb * kRows + i) / B.group;
-      float a = 0.f;
-      for (int d = 0; d < kD; ++d) a = fmaf(q[i][d], k[j][d], a);
-      const bool seen = i < rows && j0 + j <= L - n + query && __float_as_uint(k[j][0]) != 0xff800000u;
-      s[i][j] = seen ? a : -INFINITY;
-    }
-    __syncthreads();
-    if (tid < kRows) {
-      float top = m[tid];
-      for (int j = 0; j < kKeys; ++j) top = fmaxf(top, s[tid][j]);
-      const float ref = top == -INFINITY ? 0.f : top;
-      float sum = 0.f;
-      for (int j = 0; j < kKeys; ++j) sum += exp2f(s[tid][j] - ref);
-      alpha[tid] = exp2f(m[tid] - ref);
-      for (int j = 0; j < kKeys; ++j) s[tid][j] = s[tid][j] == -INFINITY ? -INFINITY : exp2f(s[tid][j] - ref);
-      l[tid] = l[tid] * alpha[tid] + sum;
-      m[tid] = top;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      float a = o[i] * alpha[i];
-      for (int j = 0; j < kKeys; ++j)
-        if (s[i][j] != -INFINITY) a = fmaf(s[i][j], v[j][tid], a);
-      o[i] = a;
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kRows; ++i)
-    if (i < rows) B.out[at(i) + tid] = f2bf16(l[i] == 0.f ? 0.f : o[i] / l[i]);
+}
+// for a whole warp, with one answer
+IPD_DEVINL bool wait(uint64_t *bar, uint32_t parity, volatile int *abort) {
+  return __all_sync(0xffffffffu, mbar_try_wait(bar, parity) || wait_slow(bar, parity, abort)) != 0;
+}
+// The n-th use (0, 1, ...) of a barrier of a ring of `ring`: a consumer waits for it
+// with full(n), a producer for the release of its slot with free(n).
+IPD_DEVINL uint32_t full(uint32_t n, uint32_t ring) { return n / ring & 1u; }
+IPD_DEVINL uint32_t free_(uint32_t n, uint32_t ring) { return (n / ring & 1u) ^ 1u; }
+IPD_DEVINL void arrive_warp(uint64_t *bar, int lane) {
+  __syncwarp();
+  if (lane == 0) mbar_arrive(bar);
 }
 
+// ---- plan ------------------------------------------------------------------------
+IPD_DEVINL int batch_of(const Params &P, int g) {
+  int b = 0;
+  while (b + 1 < P.n && g >= P.req_base[b + 1]) ++b;
+  return b;
+}
+
+// Checks the requests and counts their units; one block.
+__global__ void __launch_bounds__(1024) attn8_plan_kernel(const __grid_constant__ Params P, int ctas) {
+  __shared__ long long warp_units[32];
+  grid_launch();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  for (int i = tid; i < ctas; i += blockDim.x) P.done[i] = 0;
+  long long carry = 0;
+  for (int base = 0; base < P.total_reqs; base += blockDim.x) {
+    const int g = base + tid;
+    long long units = 0;
+    if (g < P.total_reqs) {
+      const int b = batch_of(P, g), r = g - P.req_base[b];
+      const BatchDev &B = P.b[b];
+      const int c0 = B.cu_q[r], c1 = B.cu_q[r + 1], L = B.seq_len[r];
+      const int n = c1 - c0;
+      int tiles = 0;
+      if (c0 < 0 || c1 < c0 || c1 > B.total_q) {
+        ipd_set_error(&g_attn8_err, IPD_DEVERR_SPAN);
+      } else if (n > B.max_q_len || L < n || L > B.max_seq_len) {
+        ipd_set_error(&g_attn8_err, IPD_DEVERR_SEQ_LEN);
+      } else if (n > 0) {
+        tiles = (L + kKeys - 1) / kKeys;
+        units = (long long)tiles * B.hkv * ((n * B.group + kBlockRows - 1) / kBlockRows);
+      }
+      P.info[g] = make_int4(L, n, c0, tiles);
+    }
+    long long up = units;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long x = __shfl_up_sync(0xffffffffu, up, o);
+      if (lane >= o) up += x;
+    }
+    if (lane == 31) warp_units[warp] = up;
+    __syncthreads();
+    long long before = carry, all = 0;
+    for (int w = 0; w < warps; ++w) {
+      if (w < warp) before += warp_units[w];
+      all += warp_units[w];
+    }
+    if (g < P.total_reqs) P.prefix[g] = before + up - units;
+    carry += all;
+    __syncthreads();
+  }
+  if (tid == 0) P.prefix[P.total_reqs] = carry;
+}
+
+// ---- items, page ids and scales (one warp) ----------------------------------------
+__device__ void meta_warp(const Params &P, Shared &S, int lane) {
+  grid_wait();  // what the plan wrote
+  const long long W = P.prefix[P.total_reqs];
+  const long long C = W < (long long)gridDim.x ? W : gridDim.x;
+  uint32_t n = 0, it = 0;
+  long long pos = 0, hi = 0;
+  int g = 0;
+  if (blockIdx.x < C) {
+    pos = blockIdx.x * W / C, hi = (blockIdx.x + 1) * W / C;
+    // the last request with prefix <= pos: 32 probes a round
+    int lo = 0, end = P.total_reqs;  // prefix[lo] <= pos < prefix[end]
+    while (end - lo > 1) {
+      const int step = (end - lo + 31) / 32;
+      const int at = lo + lane * step;
+      const uint32_t in = __ballot_sync(0xffffffffu, at < end && P.prefix[at] <= pos);
+      const int k = 31 - __clz(in);
+      lo += k * step;
+      end = min(end, lo + step);
+    }
+    g = lo;
+  }
+  while (pos < hi) {
+    const int b = batch_of(P, g), r = g - P.req_base[b];
+    const BatchDev &B = P.b[b];
+    const long long first = P.prefix[g], next = P.prefix[g + 1];
+    if (next == first) {  // nothing to do for this request
+      ++g;
+      continue;
+    }
+    const int4 info = P.info[g];
+    const int L = info.x, tiles = info.w, rows_all = info.y * B.group;
+    const int blocks = (rows_all + kBlockRows - 1) / kBlockRows;
+    const long long off = pos - first;
+    const int task = (int)(off / tiles), t0 = (int)(off - (long long)task * tiles);
+    const int t1 = (int)min((long long)tiles, t0 + (hi - pos));
+    const int h = task / blocks, row0 = (task - h * blocks) * kBlockRows;
+    const int slot = n % kSlots;
+    if (!wait(&S.item_empty[slot], free_(n, kSlots), &S.abort)) return;
+    if (lane == 0) {
+      Item &I = S.item[slot];
+      I.valid = 1, I.b = b, I.c0 = info.z, I.n = info.y, I.L = L, I.h = h;
+      I.row0 = row0, I.rows = min(kBlockRows, rows_all - row0);
+      I.both = I.rows > kRows;
+      I.nr = I.rows > 32 ? 64 : I.rows > 16 ? 32 : 16;
+      I.t0 = t0, I.t1 = t1;
+      I.part = t1 - t0 == tiles ? -1 : t0 > 0 ? 2 * (int)blockIdx.x : 2 * (int)blockIdx.x + 1;
+      // CTA i begins at unit floor(i W / C): the last one that begins at p or before
+      const long long p0 = pos - t0, p1 = p0 + tiles - 1;
+      I.cta0 = (int)(((p0 + 1) * C - 1) / W), I.cta1 = (int)(((p1 + 1) * C - 1) / W);
+      mbar_arrive(&S.item_full[slot]);
+    }
+    const int *pages = B.page_table + (size_t)r * B.max_pages;
+    const int n_pages = (L + kPage - 1) / kPage;
+    int id = t0 * kPages + lane < n_pages ? pages[t0 * kPages + lane] : -1;
+    for (int t = t0; t < t1; t += kBatch) {
+      const int page = t * kPages + lane, mine = lane / kPages;
+      const bool inside = page < n_pages && t + mine < t1;
+      const bool ok = inside && id >= 0 && id < B.num_pages;
+      if (inside && !ok) ipd_set_error(&g_attn8_err, IPD_DEVERR_PAGE_ID);
+      const size_t cell = (size_t)(ok ? id : 0) * B.hkv + h;
+      const uint32_t kb = ok ? B.ks[cell] : 127u, vb = ok ? B.vs[cell] : 127u;
+      const int now = min(kBatch, t1 - t);
+      // the slots of the batch: free in order
+      for (int i = 0; i < now; ++i) {
+        const uint32_t m = (it + i) % kMeta;
+        if (!wait(&S.meta_empty[m], free_(it + i, kMeta), &S.abort)) return;
+        const uint32_t gap = __ballot_sync(0xffffffffu, mine == i && inside && !ok);
+        if (mine == i) S.meta[m].y[lane % kPages] = ok ? (int)cell * kPage : B.rows_end;
+        if (lane == 0) S.meta[m].gap = gap != 0;
+        arrive_warp(&S.pg_full[m], lane);
+      }
+      id = page + 32 < n_pages ? pages[page + 32] : -1;  // the next batch's
+      for (int i = 0; i < now; ++i) {
+        const uint32_t m = (it + i) % kMeta;
+        if (mine == i) {
+          S.meta[m].ck[lane % kPages] = e8m0(kb) * P.scale_log2;
+          S.meta[m].ev[lane % kPages] = ok ? (int)vb - 127 : kNoPage;
+        }
+        arrive_warp(&S.sc_full[m], lane);
+      }
+      it += now;
+    }
+    ++n;
+    pos += t1 - t0;
+    if (pos == next) ++g;
+  }
+  const int slot = n % kSlots;
+  if (!wait(&S.item_empty[slot], free_(n, kSlots), &S.abort)) return;
+  if (lane == 0) {
+    S.item[slot].valid = 0;
+    mbar_arrive(&S.item_full[slot]);
+  }
+}
+
+// ---- loads -------------------------------------------------------------------------
+template <bool kIsV>
+__device__ void load_warp(const Params &P, Shared &S, int lane) {
+  constexpr int kRing = kIsV ? kVStages : kKStages;
+  uint64_t *fulls = kIsV ? S.v_full : S.k_full, *empties = kIsV ? S.v_empty : S.k_empty;
+  const uint64_t policy = l2_policy_evict_first();
+  uint32_t it = 0;
+  for (uint32_t n = 0;; ++n) {
+    const int slot = n % kSlots;
+    if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) break;
+    const Item &I = S.item[slot];
+    if (!I.valid) return;
+    const CUtensorMap *map = kIsV ? &P.v[I.b] : &P.k[I.b];
+    const int tiles = I.t1 - I.t0;
+    bool ok = true;
+    for (int t = 0; ok && t < tiles; ++t, ++it) {
+      const uint32_t m = it % kMeta, s = it % kRing;
+      ok = wait(&S.pg_full[m], full(it, kMeta), &S.abort) && wait(&empties[s], free_(it, kRing), &S.abort);
+      if (!ok) break;
+      if (lane == 0) mbar_arrive_expect_tx(&fulls[s], kTileBytes);
+      __syncwarp();
+      if (lane < kPages)
+        tma_load_2d((kIsV ? S.v[s] : S.k[s]) + lane * kPageBytes, map, 0, S.meta[m].y[lane], &fulls[s], policy);
+      __syncwarp();
+    }
+    if (!ok) break;
+    arrive_warp(&S.item_empty[slot], lane);
+  }
+  // given up: the copies in flight land first
+  for (uint32_t k = it > (uint32_t)kRing ? it - kRing : 0; k < it; ++k) {
+    const long long t0 = clock64();
+    while (!mbar_try_wait(&fulls[k % kRing], full(k, kRing)) && clock64() - t0 < kWaitLimitCycles) {
+    }
+  }
+}
+
+// ---- products -----------------------------------------------------------------------
+// until what this thread has issued is complete (bounded): only after giving up
+IPD_DEVINL void drain(uint64_t *bar, int lane) {
+  if (lane == 0) {
+    tc_commit(bar);
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, 0) && clock64() - t0 < kWaitLimitCycles) {
+    }
+  }
+  __syncwarp();
+}
+
+__device__ void qk_warp(Shared &S, int lane) {
+  uint32_t it = 0, used[2] = {0, 0};
+  for (uint32_t n = 0;; ++n) {
+    const int slot = n % kSlots;
+    if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) break;
+    const Item &I = S.item[slot];
+    if (!I.valid) return;
+    const int tiles = I.t1 - I.t0, nr = I.nr;
+    const bool both = I.both;
+    const uint32_t idesc = idesc_f8(nr, 0), buf = n & 1;
+    bool ok = wait(&S.q_full[buf], full(n, 2), &S.abort);
+    for (int t = 0; ok && t < tiles; ++t, ++it) {
+      const uint32_t s = it % kKStages;
+      ok = wait(&S.k_full[s], full(it, kKStages), &S.abort);
+      for (int k = 0; ok && k < (both ? 2 : 1); ++k) {
+        const int g = both ? k : (int)(it & 1);
+        ok = wait(&S.s_empty[g], free_(used[g], 1), &S.abort);
+        if (!ok) break;
+        ++used[g];
+        tc_fence_after();
+        if (lane == 0) {
+          const uint64_t a = sdesc(smem_u32(S.k[s]), 128);
+          const uint64_t hi = sdesc(smem_u32(S.q[buf][both ? k : 0][0]), 128),
+                         lo = sdesc(smem_u32(S.q[buf][both ? k : 0][1]), 128);
+          const uint32_t d = S.tmem + col_s(g);
+#pragma unroll
+          for (int kk = 0; kk < kD / 32; ++kk) {
+            tc_mma_f8(d, a + 2 * kk, hi + 2 * kk, idesc, kk != 0);
+            tc_mma_f8(d, a + 2 * kk, lo + 2 * kk, idesc, 1);
+          }
+          tc_commit(&S.s_full[g]);
+        }
+        __syncwarp();
+      }
+      if (ok && lane == 0) {
+        tc_commit(&S.k_empty[s]);
+        if (t == tiles - 1) tc_commit(&S.q_empty[buf]);
+      }
+      __syncwarp();
+    }
+    if (!ok) break;
+    arrive_warp(&S.item_empty[slot], lane);
+  }
+  drain(&S.drain[0], lane);
+}
+
+__device__ void pv_warp(Shared &S, int lane) {
+  uint32_t it = 0, used[2] = {0, 0};
+  for (uint32_t n = 0;; ++n) {
+    const int slot = n % kSlots;
+    if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) break;
+    const Item &I = S.item[slot];
+    if (!I.valid) return;
+    const int tiles = I.t1 - I.t0, nr = I.nr;
+    const bool both = I.both;
+    const uint32_t idesc = idesc_f8(2 * nr, 1);
+    const uint32_t step = 32 * 2 * nr >> 4;  // 32 keys of P further on
+    bool begun[2] = {false, false}, ok = true;
+    for (int t = 0; ok && t < tiles; ++t, ++it) {
+      const uint32_t s = it % kVStages;
+      ok = wait(&S.v_full[s], full(it, kVStages), &S.abort);
+      for (int k = 0; ok && k < (both ? 2 : 1); ++k) {
+        const int g = both ? k : (int)(it & 1);
+        ok = wait(&S.p_full[g], full(used[g], 1), &S.abort);
+        if (!ok) break;
+        ++used[g];
+        tc_fence_after();
+        if (lane == 0) {
+          const uint64_t a = sdesc(smem_u32(S.v[s]), 128), b = sdesc(smem_u32(S.p[g]), 2 * nr);
+          const uint32_t d = S.tmem + col_o(g);
+#pragma unroll
+          for (int kk = 0; kk < kKeys / 32; ++kk)
+            tc_mma_f8(d, a + (uint64_t)(kk * 32 * kD >> 4), b + (uint64_t)(kk * step), idesc, begun[g] || kk != 0);
+          tc_commit(&S.pv_done[g]);
+        }
+        begun[g] = true;
+        __syncwarp();
+      }
+      if (ok && lane == 0) {
+        tc_commit(&S.v_empty[s]);
+        tc_commit(&S.meta_empty[it % kMeta]);
+      }
+      __syncwarp();
+    }
+    if (!ok) break;
+    arrive_warp(&S.item_empty[slot], lane);
+  }
+  drain(&S.drain[1], lane);
+}
+
+// ---- queries ------------------------------------------------------------------------
+// A row as two e4m3 terms: with 2^e the least power of two that brings its largest
+// entry to 448 or below, hi = e4m3(q 2^-e), lo = e4m3(q 2^-e - hi), which together
+// hold a bf16's eight bits down to 2^-10, 2^-17 of the row's largest entry.
+__device__ void query_warp(const Params &P, Shared &S, int w, int lane) {
+  for (uint32_t n = 0;; ++n) {
+    const int slot = n % kSlots;
+    if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) return;
+    const Item &I = S.item[slot];
+    if (!I.valid) return;
+    const uint32_t buf = n & 1;
+    if (!wait(&S.q_empty[buf], free_(n, 2), &S.abort)) return;
+    const BatchDev &B = P.b[I.b];
+    const int all = I.both ? 2 * kRows : I.nr, group = B.group;
+    constexpr int kAhead = 4;
+    for (int r0 = w; r0 < all; r0 += kAhead * kQWarps) {
+      uint2 x[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int r = r0 + i * kQWarps;
+        x[i] = make_uint2(0u, 0u);
+        if (r < I.rows) {
+          const int row = I.row0 + r, query = row / group;
+          x[i] = *reinterpret_cast<const uint2 *>(
+              B.q + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group + (row - query * group)) * kD + lane * 4);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int r = r0 + i * kQWarps;
+        if (r >= all) break;
+        const uint32_t a = x[i].x & 0x7fff7fffu, c = x[i].y & 0x7fff7fffu;
+        const uint32_t top = __reduce_max_sync(0xffffffffu, max(max(a & 0xffffu, a >> 16), max(c & 0xffffu, c >> 16)));
+        const int E = (int)(top >> 7);
+        // (a largest entry below 2^-100 counts as zero; one that is not finite makes
+        // the row NaN)
+        const int e = E - 127 - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0);
+        const bool none = E < 27 || E == 255;
+        const float f = none ? 0.f : pow2i(-e);
+        float v[4] = {bf16lo(x[i].x) * f, bf16hi(x[i].x) * f, bf16lo(x[i].y) * f, bf16hi(x[i].y) * f};
+        if (none) v[0] = v[1] = v[2] = v[3] = 0.f;
+        const uint32_t hi = e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16;
+        float back[4];
+        e4m3x4_to_floats(hi, back);
+        const uint32_t lo = e4m3x2(v[0] - back[0], v[1] - back[1]) | e4m3x2(v[2] - back[2], v[3] - back[3]) << 16;
+        const int g = r / kRows, rr = r % kRows;
+        const int at = rr * kD + (((lane >> 2) ^ (rr & 7)) << 4) + (lane & 3) * 4;
+        *reinterpret_cast<uint32_t *>(&S.q[buf][g][0][at]) = hi;
+        *reinterpret_cast<uint32_t *>(&S.q[buf][g][1][at]) = lo;
+        if (lane == 0) S.qscale[slot][g][rr] = E == 255 ? __uint_as_float(0x7fc00000u) : none ? 0.f : pow2i(e);
+      }
+    }
+    fence_proxy_async_smem();
+    arrive_warp(&S.q_full[buf], lane);
+    arrive_warp(&S.item_empty[slot], lane);
+  }
+}
+
+// ---- softmax --------------------------------------------------------------------------
+// Reduces 16 values a lane over the lanes, column by column: lane i ends up with
+// column i / 2.
+template <typename Op>
+IPD_DEVINL float column_reduce(float (&a)[16], int lane, Op op) {
+#pragma unroll
+  for (int n = 8, mask = 16; n > 0; n >>= 1, mask >>= 1) {
+    const bool up = lane & mask;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float other = __shfl_xor_sync(0xffffffffu, up ? a[i] : a[i + n], mask);
+      a[i] = op(up ? a[i + n] : a[i], other);
+    }
+  }
+  return op(a[0], __shfl_xor_sync(0xffffffffu, a[0], 1));
+}
+
+struct Softmax {
+  int g, tid, warp, lane;  // warpgroup, and place in it
+  uint32_t tiles, it;      // own tiles so far, tiles of the CTA so far
+  uint32_t pairs;          // barriers with the other warpgroup so far
+  bool ok;                 // no wait of this warp has given up
+};
+
+// The S columns of a tile, one key a thread: issues the loads.
+IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[1][16]) { tc_ld_32x32b_x16(taddr, r[0]); }
+template <int N>
+IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[N][32]) {
+#pragma unroll
+  for (int c = 0; c < N; ++c) tc_ld_32x32b_x32(taddr + 32 * c, r[c]);
+}
+
+// A thread's key of a tile that holds hidden keys: NaN in its V row.  They would reach
+// rows that do not see the key (0 x NaN), so they become 0, and rows that do see
+// it get them back at the end.
+IPD_DEVINL void mend(Shared &S, int set, uint8_t *v, int key_in_tile, int key, int L) {
+  bool wrote = false;
+  for (int i = 0; i < 8; ++i) {
+    const int c = (i + key_in_tile) & 7;
+    uint4 *at = reinterpret_cast<uint4 *>(v + key_in_tile * kD + c * 16);
+    uint4 x = *at;
+    uint32_t *w = &x.x;
+    bool any = false;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) any |= __vcmpeq4(w[k] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
+    if (!any) continue;
+    for (int k = 0; k < 4; ++k)
+      for (int e = 0; e < 4; ++e)
+        if ((w[k] >> 8 * e & 0x7fu) == 0x7fu) {
+          if (key < L) {
+            atomicMin(&S.nan_key[set][((c ^ (key_in_tile & 7)) << 4) + k * 4 + e], key);
+            S.bad[set] = 1;
+          }
+          w[k] &= ~(0xffu << 8 * e);
+        }
+    __threadfence_block();  // noted before it is gone
+    *at = x;
+    wrote = true;
+  }
+  if (wrote) fence_proxy_async_smem();
+}
+
+// Both warpgroups' barrier.  Bounded, as every wait: a warpgroup that has given up
+// does not come.
+IPD_DEVINL void pair_sync(Shared &S, Softmax &X) {
+  arrive_warp(&S.pair, X.lane);
+  X.ok = wait(&S.pair, full(X.pairs, 1), &S.abort) && X.ok;
+  ++X.pairs;
+}
+
+// An item's tiles, and its rows at the end.  A wait that gives up does not leave the
+// way the others go: the warps of a warpgroup meet at barriers.
+template <int NR>
+__device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t item, const Item &I) {
+  const int g = X.g, lane = X.lane, tid = X.tid, slot = item % kSlots;
+  const bool both = I.both;
+  const int n_tiles = I.t1 - I.t0, L = I.L;
+  const uint32_t lanes = (uint32_t)X.warp << 21;  // this warp's 32 TMEM lanes
+  const uint32_t s_addr = S.tmem + lanes + col_s(g), o_addr = S.tmem + lanes + col_o(g);
+  // rows of this warpgroup, and the key from which on some row of the task does not see
+  const int row0 = I.row0 + (both ? g * kRows : 0);
+  const int rows = both ? (g == 0 ? kRows : I.rows - kRows) : I.rows;
+  const int group = P.b[I.b].group;
+  const int sees = L - I.n;  // query i sees keys up to sees + i
+  const int masked = sees + 1 + I.row0 / group;
+  X.ok = wait(&S.q_full[item & 1], full(item, 2), &S.abort) && X.ok;
+  if (tid < NR) {
+    float *st = reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1);
+    st[0] = S.qscale[slot][both ? g : 0][tid];
+    st[2] = 0.f;
+    S.ref[g][tid] = -INFINITY;  // (its largest so far)
+  }
+  named_bar_sync(1 + g, 128);
+  u64 l[NR / 2];
+#pragma unroll
+  for (int i = 0; i < NR / 2; ++i) l[i] = 0;
+  const bool joint = !both && n_tiles > 1;  // both warpgroups have tiles of the same rows
+  const int set = joint || both ? 2 : g;
+  int e0 = 0;
+  bool first = true;
+  for (int t = 0; t < n_tiles; ++t) {
+    const uint32_t it = X.it + t;
+    if (!both && (int)(it & 1) != g) continue;
+    const uint32_t m = it % kMeta;
+    X.ok = wait(&S.sc_full[m], full(it, kMeta), &S.abort) && X.ok;
+    const Meta &M = S.meta[m];
+    const int key0 = (I.t0 + t) * kKeys, key = key0 + tid;
+    const float ck = M.ck[tid / kPage];
+    const int ev = M.ev[tid / kPage];
+    const bool hides = key0 + kKeys > masked || M.gap;
+    if (first) {
+      int top = -kNoPage;
+#pragma unroll
+      for (int i = 0; i < kPages; ++i)
+        if (M.ev[i] != kNoPage && M.ev[i] != 128) top = max(top, M.ev[i]);
+      e0 = top == -kNoPage ? 0 : top;
+    }
+    int de = max(-kFar, min(kFar, ev - e0));
+    int hidden = 0;  // rows before this one do not see the key
+    if (hides) {
+      hidden = ev == kNoPage || key >= L ? NR : (int)max(0LL, min((long long)NR, (long long)(key - sees) * group - row0));
+      if (hidden == NR) de = 0;
+    }
+    const float fk = ev == 128 && hidden < NR ? __uint_as_float(0x7fc00000u) : pow2i(de);
+    X.ok = wait(&S.s_full[g], full(X.tiles, 1), &S.abort) && X.ok;
+    tc_fence_after();
+    float y[NR];
+    {
+      constexpr int N = NR < 32 ? NR : 32;
+      uint32_t raw[NR / N][N];
+      load_scores(s_addr, raw);
+      tc_wait_ld();
+#pragma unroll
+      for (int i = 0; i < NR; ++i) y[i] = __uint_as_float(raw[i / N][i % N]);
+    }
+    tc_fence_before();
+    arrive_warp(&S.s_empty[g], lane);
+    const u64 ck2 = f2_pack(ck, ck);
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < NR; i += 2) {
+      const float4 st = S.state[g][i / 2];
+      f2_unpack(f2_fma(mul2(f2_pack(y[i], y[i + 1]), ck2), f2_pack(st.x, st.y), f2_pack(st.z, st.w)), y[i], y[i + 1]);
+    }
+    if (hides) {
+#pragma unroll
+      for (int i = 0; i < NR; ++i)
+        if (i < hidden) y[i] = -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < NR; i += 2) top = fmax3(top, y[i], y[i + 1]);
+    if (bar_or(1 + g, 128, first || top + (float)de > kLimit)) {
+      // the rows' references move: largest exponent so far, less kBase
+#pragma unroll
+      for (int c = 0; c < NR; c += 16) {
+        float z[16];
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+          const float4 st = S.state[g][(c + i) / 2];
+          z[i] = y[c + i] - st.z + (float)de;
+          z[i + 1] = y[c + i + 1] - st.w + (float)de;
+        }
+        const float x = column_reduce(z, lane, [](float a, float b) { return fmaxf(a, b); });
+        if (!(lane & 1)) S.red[g][X.warp][c + (lane >> 1)] = x;
+      }
+      named_bar_sync(1 + g, 128);
+      if (tid < NR) {
+        const float was = S.ref[g][tid];
+        const float now = fmaxf(fmax3(S.red[g][0][tid], S.red[g][1][tid], S.red[g][2][tid]), fmaxf(S.red[g][3][tid], was));
+        float *st = reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1);
+        // (a row that has seen nothing, or NaN alone, stays at 0)
+        const float old = st[2], ref = now == -INFINITY || now == INFINITY ? -old : now - kBase;
+        S.ref[g][tid] = now;
+        st[2] = -ref;
+        S.alpha[g][tid] = was == -INFINITY ? 0.f : ex2_approx(-old - ref);
+        S.red[g][0][tid] = -old - ref;  // what y moves by
+      }
+      named_bar_sync(1 + g, 128);
+#pragma unroll
+      for (int i = 0; i < NR; ++i) y[i] += S.red[g][0][i];
+      if (!first) {
+#pragma unroll
+        for (int i = 0; i < NR; i += 2) l[i / 2] = mul2(l[i / 2], *reinterpret_cast<const u64 *>(&S.alpha[g][i]));
+        X.ok = wait(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort) && X.ok;
+        tc_fence_after();
+#pragma unroll 1
+        for (int c = 0; c < 2 * NR; c += 16) {
+          uint32_t o[16];
+          tc_ld_32x32b_x16(o_addr + c, o);
+          tc_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * S.alpha[g][(c + i) & (NR - 1)]);
+          tc_st_32x32b_x16(o_addr + c, o);
+        }
+        tc_wait_st();
+        tc_fence_before();
+      }
+      named_bar_sync(1 + g, 128);  // red and alpha are read
+    }
+    // P's buffer is free once this warpgroup's product before is complete
+    if (X.tiles > 0) X.ok = wait(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort) && X.ok;
+    const u64 fk2 = f2_pack(fk, fk);
+    const uint32_t lo16 = half2_of(kLoScale, kLoScale);
+    uint8_t *prow = S.p[g] + tid * 2 * NR;
+    const int turn = NR == 64 ? tid & 7 : NR == 32 ? (tid >> 1) & 3 : (tid >> 2) & 1;
+#pragma unroll
+    for (int c = 0; c < NR; c += 16) {
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t h[2], e[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int i = c + q * 4 + k * 2;
+          const u64 p = f2_pack(ex2_approx(y[i]), ex2_approx(y[i + 1]));
+          l[i / 2] = f2_add(l[i / 2], p);
+          float w0, w1;
+          f2_unpack(mul2(p, fk2), w0, w1);
+          if (hides) {  // (a NaN scale reaches no hidden row)
+            if (i < hidden) w0 = 0.f;
+            if (i + 1 < hidden) w1 = 0.f;
+          }
+          h[k] = half2_of(w0, w1);
+          e[k] = e4m3x2_h2(h[k]);
+        }
+        hi[q] = e[0] | e[1] << 16;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) e[k] = e4m3x2_h2(half2_mul(half2_sub(h[k], h2_from_e4m3x2(e[k])), lo16));
+        lo[q] = e[0] | e[1] << 16;
+      }
+      *reinterpret_cast<uint4 *>(prow + (((c / 16) ^ turn) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4 *>(prow + ((((NR + c) / 16) ^ turn) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+    if (key0 + kKeys > masked) {
+      const uint32_t vs = it % kVStages;
+      X.ok = wait(&S.v_full[vs], full(it, kVStages), &S.abort) && X.ok;
+      if (key >= masked) mend(S, set, S.v[vs], tid, key, L);
+    }
+    fence_proxy_async_smem();
+    arrive_warp(&S.p_full[g], lane);
+    ++X.tiles;
+    first = false;
+  }
+  X.it += n_tiles;
+  // the rows: sums over the threads, the other warpgroup's part, output
+  const bool mine = !first;                         // this warpgroup had a tile
+  if (!mine && !joint && I.part < 0) return;   // (all of the item was the other's)
+  if (mine) {
+#pragma unroll
+    for (int c = 0; c < NR; c += 16) {
+      float z[16];
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) f2_unpack(l[(c + i) / 2], z[i], z[i + 1]);
+      const float x = column_reduce(z, lane, [](float a, float b) { return a + b; });
+      if (!(lane & 1)) S.red[g][X.warp][c + (lane >> 1)] = x;
+    }
+    named_bar_sync(1 + g, 128);
+    if (tid < NR) {
+      S.sum[g][tid] = (S.red[g][0][tid] + S.red[g][1][tid]) + (S.red[g][2][tid] + S.red[g][3][tid]);
+      const float *st = reinterpret_cast<const float *>(&S.state[g][tid >> 1]) + (tid & 1);
+      S.ref[g][tid] = -st[2];
+    }
+    if (tid == 0) S.e0[g] = e0;
+  }
+  if (joint || both) pair_sync(S, X);
+  else named_bar_sync(1 + g, 128);
+  float *part = nullptr;
+  if (I.part >= 0) part = P.part + (size_t)I.part * P.part_rows * (kD + 1);
+  if (mine) {
+    // factor of a row: 2^e0 / its sum, the two parts brought to one reference
+    if (tid < NR) {
+      float ref = S.ref[g][tid], sum = S.sum[g][tid], f = 1.f;
+      if (joint) {
+        const float other = S.ref[1 - g][tid], theirs = S.sum[1 - g][tid];
+        // (a part that has seen nothing has no say in the reference)
+        const float top = sum == 0.f ? other : theirs == 0.f ? ref : fmaxf(ref, other);
+        f = sum == 0.f ? 0.f : ex2_approx(ref - top);
+        sum = sum * f + (theirs == 0.f ? 0.f : theirs * ex2_approx(other - top));
+        ref = top;
+      }
+      // (a score past fp32 leaves no softmax)
+      S.alpha[g][tid] = sum == 0.f ? 0.f : sum == INFINITY ? __uint_as_float(0x7fc00000u) : f / sum * pow2i(e0);
+      if (part && tid < rows && (!joint || g == 0))
+        part[(size_t)P.part_rows * kD + (both ? g * kRows : 0) + tid] = sum == 0.f ? -INFINITY : ref + log2f(sum);
+    }
+    X.ok = wait(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort) && X.ok;
+    tc_fence_after();
+    named_bar_sync(1 + g, 128);
+  }
+  const int d = tid;
+  const bool bad = *(volatile int *)&S.bad[set] != 0;
+  const int nan_key = bad ? S.nan_key[set][d] : 0x7fffffff;
+  const BatchDev &B = P.b[I.b];
+  auto emit = [&](int r, float x) {  // row r of the warpgroup
+    const int row = row0 + r, query = row / group;
+    if (nan_key <= sees + query) x = __uint_as_float(0x7fc00000u);
+    if (part)
+      part[(size_t)((both ? g * kRows : 0) + r) * kD + d] = x;
+    else
+      B.out[((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group + (row - query * group)) * kD + d] = f2bf16(x);
+  };
+  float *give = reinterpret_cast<float *>(S.p[g]);
+  if (mine) {
+    // (with two parts: this warpgroup's half of the rows it will put out stays, the
+    // other half goes through its P buffer)
+    const int half = NR / 2;
+#pragma unroll 1
+    for (int k = 0; k < NR; k += 8) {
+      const bool away = joint && (k < half) == (g == 1);
+      uint32_t a[8], b[8];
+      tc_ld_32x32b_x8(o_addr + k, a);
+      tc_ld_32x32b_x8(o_addr + NR + k, b);
+      tc_wait_ld();
+      if (k >= rows) continue;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = fmaf(__uint_as_float(b[i]), 1.f / kLoScale, __uint_as_float(a[i])) * S.alpha[g][k + i];
+        if (away) give[(k + i - (g == 0 ? half : 0)) * kD + d] = x;
+        else if (!joint) {
+          if (k + i < rows) emit(k + i, x);
+        }
+      }
+    }
+  }
+  if (joint) {
+    pair_sync(S, X);
+    const float *take = reinterpret_cast<const float *>(S.p[1 - g]);
+    const int half = NR / 2, from = g == 0 ? 0 : half;
+#pragma unroll 1
+    for (int k = 0; k < half; k += 8) {
+      uint32_t a[8], b[8];
+      tc_ld_32x32b_x8(o_addr + from + k, a);
+      tc_ld_32x32b_x8(o_addr + NR + from + k, b);
+      tc_wait_ld();
+      if (from + k >= rows) continue;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = from + k + i;
+        const float x = fmaf(__uint_as_float(b[i]), 1.f / kLoScale, __uint_as_float(a[i])) * S.alpha[g][r];
+        if (r < rows) emit(r, x + take[(k + i) * kD + d]);
+      }
+    }
+  }
+  tc_fence_before();
+  if (part) {
+    // the last CTA of the task to get here joins its parts, in order
+    __threadfence();
+    pair_sync(S, X);
+    if (g == 0 && tid == 0) S.last = atomicAdd(&P.done[I.cta0], 1) == I.cta1 - I.cta0;
+    pair_sync(S, X);
+    if (*(volatile int *)&S.last) {
+      __threadfence();
+      const size_t stride = (size_t)P.part_rows * (kD + 1);
+      auto slot_of = [&](int c) { return P.part + (size_t)(c == I.cta0 ? 2 * c + 1 : 2 * c) * stride; };
+      for (int r = g * 4 + X.warp; r < I.rows; r += 8) {
+        float top = -INFINITY;
+        for (int c = I.cta0 + lane; c <= I.cta1; c += 32) top = fmaxf(top, slot_of(c)[(size_t)P.part_rows * kD + r]);
+        top = warp_max(top);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        float sum = 0.f;
+#pragma unroll 4
+        for (int c = I.cta0; c <= I.cta1; ++c) {
+          const float *s = slot_of(c);
+          const float lse = s[(size_t)P.part_rows * kD + r];
+          const float4 x = *reinterpret_cast<const float4 *>(s + (size_t)r * kD + lane * 4);
+          const float w = lse == -INFINITY ? 0.f : ex2_approx(lse - top);
+          sum += w;
+          acc.x += w * x.x, acc.y += w * x.y, acc.z += w * x.z, acc.w += w * x.w;
+        }
+        const float f = sum == 0.f ? 0.f : 1.f / sum;
+        const int row = I.row0 + r, query = row / group;
+        uint2 o = make_uint2((uint32_t)f2bf16(acc.x * f) | (uint32_t)f2bf16(acc.y * f) << 16,
+                             (uint32_t)f2bf16(acc.z * f) | (uint32_t)f2bf16(acc.w * f) << 16);
+        *reinterpret_cast<uint2 *>(B.out + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group +
+                                            (row - query * group)) * kD + lane * 4) = o;
+      }
+    }
+  }
+  // nothing of the item's shared state is read any more
+  if (joint || both || part) pair_sync(S, X);
+  else named_bar_sync(1 + g, 128);
+  if (bad) {
+    if (set == g || g == 0) {
+      S.nan_key[set][tid] = 0x7fffffff;
+      if (tid == 0) S.bad[set] = 0;
+    }
+    if (set == 2) pair_sync(S, X);
+    else named_bar_sync(1 + g, 128);
+  }
+}
+
+__device__ void softmax_warps(const Params &P, Shared &S, int warp, int lane) {
+  Softmax X{warp >> 2, (int)threadIdx.x & 127, warp & 3, lane, 0, 0, 0, true};
+  for (uint32_t n = 0;; ++n) {
+    const int slot = n % kSlots;
+    X.ok = wait(&S.item_full[slot], full(n, kSlots), &S.abort) && X.ok;
+    if (bar_or(1 + X.g, 128, !X.ok)) return;  // the whole warpgroup
+    const Item I = S.item[slot];
+    if (!I.valid) return;
+    if (I.nr == 64) softmax_item<64>(P, S, X, n, I);
+    else if (I.nr == 32) softmax_item<32>(P, S, X, n, I);
+    else softmax_item<16>(P, S, X, n, I);
+    arrive_warp(&S.item_empty[slot], lane);
+  }
+}
+
+__global__ void __launch_bounds__(kThreads, 1) attn8_kernel(const __grid_constant__ Params P) {
+  extern __shared__ uint8_t raw[];
+  Shared &S = *reinterpret_cast<Shared *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x < 3 * kD) S.nan_key[threadIdx.x / kD][threadIdx.x % kD] = 0x7fffffff;
+  if (threadIdx.x == 0) {
+    S.bad[0] = S.bad[1] = S.bad[2] = S.abort = S.last = 0;
+    auto ring = [](uint64_t *b, int n, int count) {
+      for (int i = 0; i < n; ++i) mbar_init(&b[i], count);
+    };
+    ring(S.k_full, kKStages, 1), ring(S.k_empty, kKStages, 1);
+    ring(S.v_full, kVStages, 1), ring(S.v_empty, kVStages, 1);
+    ring(S.pg_full, kMeta, 1), ring(S.sc_full, kMeta, 1), ring(S.meta_empty, kMeta, 1);
+    ring(S.q_full, 2, kQWarps), ring(S.q_empty, 2, 1);
+    ring(S.s_full, 2, 1), ring(S.s_empty, 2, 4);
+    ring(S.p_full, 2, 4), ring(S.pv_done, 2, 1);
+    ring(S.item_full, kSlots, 1), ring(S.item_empty, kSlots, kItemReaders);
+    ring(&S.pair, 1, 8), ring(S.drain, 2, 1);
+    fence_mbar_init();
+  }
+  if (warp == kQkWarp) {
+    tc_alloc(&S.tmem, kTmemCols);
+    tc_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRegsSoftmax));
+    softmax_warps(P, S, warp, lane);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRegsAux));
+    if (warp == kKWarp) load_warp<false>(P, S, lane);
+    else if (warp == kVWarp) load_warp<true>(P, S, lane);
+    else if (warp == kQkWarp) qk_warp(S, lane);
+    else if (warp == kPvWarp) pv_warp(S, lane);
+    else if (warp == kMetaWarp) meta_warp(P, S, lane);
+    else query_warp(P, S, warp - kMetaWarp - 1, lane);
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == kQkWarp) tc_dealloc(S.tmem, kTmemCols);
+}
+
+// ---- host -----------------------------------------------------------------------------
 int validate(const ipd_attn8_batch *b) {
   if (!b || !b->cache) return IPD_ERR_INVALID_ARG;
   const ipd_kv8_cache *c = b->cache;
@@ -164,6 +1089,72 @@ int collect(const ipd_attn8_batch *verify, int nv, const ipd_attn8_batch *decode
   return IPD_OK;
 }
 
+struct DevInfo {
+  int sms = 0;
+};
+DevInfo g_dev[64];
+PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
+
+int prepare_device(int *sms) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return IPD_ERR_CUDA;
+  DevInfo &D = g_dev[dev];
+  if (D.sms == 0) {
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return IPD_ERR_CUDA;
+    if (cudaFuncSetAttribute(attn8_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes) != cudaSuccess)
+      return IPD_ERR_CUDA;
+    D.sms = n;
+  }
+  *sms = D.sms;
+  if (!g_encode) {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess || !fn)
+      return IPD_ERR_CUDA;
+    g_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+  }
+  return IPD_OK;
+}
+
+// A pool as rows of 128 bytes; a box is one page of one head, its rows swizzled.
+int encode_pool(CUtensorMap *m, const void *base, long long rows) {
+  cuuint64_t dims[2] = {(cuuint64_t)kD, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)kD};
+  cuuint32_t box[2] = {(cuuint32_t)kD, (cuuint32_t)kPage}, estr[2] = {1, 1};
+  return g_encode(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? IPD_OK
+             : IPD_ERR_CUDA;
+}
+
+constexpr int kMaxCtas = 256;  // the workspace is laid out for as many
+
+struct Layout {
+  size_t prefix, info, done, part, total;
+  int reqs, part_rows;
+};
+Layout layout(const ipd_attn8_batch *const *bs, int n) {
+  Layout W{};
+  long long rows = 1;
+  for (int i = 0; i < n; ++i) {
+    const ipd_attn8_batch &b = *bs[i];
+    if (b.num_reqs == 0 || b.total_q == 0) continue;
+    W.reqs += b.num_reqs;
+    rows = std::max(rows, (long long)b.max_q_len * (b.num_q_heads / b.cache->num_kv_heads));
+  }
+  W.part_rows = (int)((std::min<long long>(rows, kBlockRows) + 3) / 4 * 4);
+  auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  W.prefix = 0;
+  W.info = up((size_t)(W.reqs + 1) * sizeof(long long));
+  W.done = W.info + up((size_t)W.reqs * sizeof(int4));
+  W.part = W.done + up(kMaxCtas * sizeof(int));
+  W.total = W.part + up((size_t)2 * kMaxCtas * W.part_rows * (kD + 1) * sizeof(float));
+  return W;
+}
+
 }  // namespace
 
 extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_attn8_error() {
@@ -177,36 +1168,74 @@ extern "C" __attribute__((visibility("hidden"))) unsigned int ipd_internal_take_
 extern "C" size_t ipd_attn8_workspace_size(const ipd_attn8_batch *verify, int n_verify,
                                            const ipd_attn8_batch *decode, int n_decode) {
   const ipd_attn8_batch *bs[IPD_MAX_BATCHES];
-  return collect(verify, n_verify, decode, n_decode, bs) == IPD_OK ? 256 : 0;
+  if (collect(verify, n_verify, decode, n_decode, bs) != IPD_OK) return 0;
+  return layout(bs, n_verify + n_decode).total;
 }
 
 extern "C" int ipd_verify_attn8(const ipd_attn8_batch *verify, int n_verify,
                                 const ipd_attn8_batch *decode, int n_decode, float softmax_scale,
                                 void *workspace, size_t workspace_bytes, ipd_stream_t stream) {
   const ipd_attn8_batch *bs[IPD_MAX_BATCHES];
-  const int st = collect(verify, n_verify, decode, n_decode, bs);
+  int st = collect(verify, n_verify, decode, n_decode, bs);
   if (st != IPD_OK) return st;
   if (!(softmax_scale > 0.f) || !(softmax_scale - softmax_scale == 0.f)) return IPD_ERR_INVALID_ARG;
+  const Layout W = layout(bs, n_verify + n_decode);
+  if (W.reqs == 0) return IPD_OK;
+  if (!workspace || workspace_bytes < W.total || ((uintptr_t)workspace & 255)) return IPD_ERR_WORKSPACE;
+  int sms = 0;
+  st = prepare_device(&sms);
+  if (st != IPD_OK) return st;
   Params P;
   memset(&P, 0, sizeof(P));
-  P.scale_log2 = softmax_scale * kLog2e;
-  long long ctas = 0;
+  const ipd_kv8_cache *caches[IPD_MAX_BATCHES];
   for (int i = 0; i < n_verify + n_decode; ++i) {
     const ipd_attn8_batch &b = *bs[i];
     if (b.num_reqs == 0 || b.total_q == 0) continue;
     const ipd_kv8_cache &c = *b.cache;
-    const int group = b.num_q_heads / c.num_kv_heads;
-    const int blocks = (b.max_q_len * group + kRows - 1) / kRows;
-    P.b[P.n] = BatchDev{c.k_pages, c.v_pages, c.k_scale, c.v_scale, b.q, b.out, b.cu_q, b.seq_len,
-                        b.page_table, b.num_reqs, b.num_q_heads, c.num_kv_heads, group, b.max_pages,
-                        b.max_q_len, b.max_seq_len, b.total_q, blocks, (int)c.num_pages};
-    ctas += (long long)b.num_reqs * c.num_kv_heads * blocks;
-    P.end[P.n++] = (int)ctas;
+    int same = 0;
+    while (same < P.n && !(caches[same]->k_pages == c.k_pages && caches[same]->v_pages == c.v_pages &&
+                           caches[same]->num_pages == c.num_pages && caches[same]->num_kv_heads == c.num_kv_heads))
+      ++same;
+    const long long rows = c.num_pages * c.num_kv_heads * kPage;
+    if (same < P.n) {
+      P.k[P.n] = P.k[same], P.v[P.n] = P.v[same];
+    } else if (encode_pool(&P.k[P.n], c.k_pages, rows) != IPD_OK || encode_pool(&P.v[P.n], c.v_pages, rows) != IPD_OK) {
+      return IPD_ERR_CUDA;
+    }
+    caches[P.n] = &c;
+    P.b[P.n] = BatchDev{c.k_scale, c.v_scale, b.q, b.out, b.cu_q, b.seq_len, b.page_table, b.num_reqs, b.num_q_heads,
+                        c.num_kv_heads, b.num_q_heads / c.num_kv_heads, b.max_pages, b.max_q_len, b.max_seq_len,
+                        b.total_q, (int)c.num_pages, (int)rows};
+    P.req_base[P.n + 1] = P.req_base[P.n] + b.num_reqs;
+    ++P.n;
   }
-  if (P.n == 0) return IPD_OK;
-  if (!workspace || workspace_bytes < 256 || ((uintptr_t)workspace & 255)) return IPD_ERR_WORKSPACE;
-  if (ctas > 0x7fffffffLL) return IPD_ERR_UNSUPPORTED;
+  P.total_reqs = W.reqs;
+  P.scale_log2 = softmax_scale * kLog2e;
+  uint8_t *ws = static_cast<uint8_t *>(workspace);
+  P.prefix = reinterpret_cast<long long *>(ws + W.prefix);
+  P.info = reinterpret_cast<int4 *>(ws + W.info);
+  P.done = reinterpret_cast<int *>(ws + W.done);
+  P.part = reinterpret_cast<float *>(ws + W.part);
+  P.part_rows = W.part_rows;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const int ctas = std::min(sms, kMaxCtas);
   g_attn8_used.store(true, std::memory_order_relaxed);
-  attn8_kernel<<<(int)ctas, 128, 0, reinterpret_cast<cudaStream_t>(stream)>>>(P);
-  return cudaGetLastError() == cudaSuccess ? IPD_OK : IPD_ERR_CUDA;
+  attn8_plan_kernel<<<1, W.reqs <= 256 ? 256 : 1024, 0, s>>>(P, ctas);
+  if (cudaGetLastError() != cudaSuccess) return IPD_ERR_CUDA;
+  // begins beside the plan, and waits for it where it reads what the plan wrote
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSharedBytes;
+  cfg.stream = s;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, attn8_kernel, P) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return IPD_ERR_CUDA;
+  }
+  return IPD_OK;
 }

@@ -83,7 +83,7 @@ class Case:
                         o, a, s = w @ x, w @ x.abs(), x.abs().sum(0)
                     else:
                         o = (w[:, :, None] * x).sum(1)
-                        a, s = o.abs().nan_to_num(1.0), torch.ones_like(x[0])
+                        a, s = ((w[:, :, None] * x.abs()).sum(1).nan_to_num(), x.abs().nan_to_num().sum(0))
                     c = 2.0 ** -18 * w.amax(-1, keepdim=True) * s
                     out[row + i, h * G:(h + 1) * G] = o
                     tol[row + i, h * G:(h + 1) * G] = 2.0 ** -8 * o.abs() + (2.0 ** -8 + 2.0 ** -10) * a + c
