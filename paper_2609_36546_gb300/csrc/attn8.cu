@@ -60,22 +60,27 @@ constexpr int kTileBytes = kKeys * kD;    // 16 KB of K or V
 constexpr int kPageBytes = kPage * kD;
 constexpr int kMaxGroup = 128;
 constexpr int kBlockRows = 128;           // rows of a task
-constexpr int kRows = 64;                 // ... of a softmax warpgroup
+constexpr int kGroups = 4;                // softmax warpgroups
+constexpr int kRows = 32;                 // ... and the rows of one
 constexpr int kKStages = 3, kVStages = 4;
 constexpr int kMeta = 8;                  // tiles whose page ids and scales are at hand
 constexpr int kBatch = 4;                 // ... fetched at once
-constexpr int kSlots = 3;                 // items handed out
-constexpr int kThreads = 512;
-constexpr int kKWarp = 8, kVWarp = 9, kQkWarp = 10, kPvWarp = 11, kMetaWarp = 12, kQWarps = 3;
-constexpr int kItemReaders = 8 + 4 + kQWarps;
-constexpr int kRegsSoftmax = 200, kRegsAux = 56;
-static_assert(256 * kRegsSoftmax + 256 * kRegsAux <= kThreads * 128,
+constexpr int kSlots = 5;                 // items handed out
+constexpr int kSoftmaxWarps = 4 * kGroups;
+constexpr int kKWarp = kSoftmaxWarps, kVWarp = kKWarp + 1, kQkWarp = kKWarp + 2, kPvWarp = kKWarp + 3,
+              kMetaWarp = kKWarp + 4, kQWarps = 3;
+constexpr int kThreads = 32 * (kSoftmaxWarps + 5 + kQWarps);
+constexpr int kItemReaders = kSoftmaxWarps + 4 + kQWarps;
+constexpr int kRegsLaunch = 80, kRegsSoftmax = 96, kRegsAux = 48;
+static_assert(32 * kSoftmaxWarps * kRegsSoftmax + 256 * kRegsAux <= kThreads * kRegsLaunch,
               "the register split must fit the registers the block was launched with");
 static_assert(kBatch * kPages == 32, "a lane a page");
 
+// TMEM columns of a warpgroup: scores, O (two terms), and every thread's own sums
 constexpr uint32_t kTmemCols = 512;
-__host__ __device__ constexpr uint32_t col_s(int g) { return 64u * (uint32_t)g; }
-__host__ __device__ constexpr uint32_t col_o(int g) { return 128u + 128u * (uint32_t)g; }
+__host__ __device__ constexpr uint32_t col_s(uint32_t g) { return 32u * g; }
+__host__ __device__ constexpr uint32_t col_o(uint32_t g) { return 128u + 64u * g; }
+__host__ __device__ constexpr uint32_t col_l(uint32_t g) { return 384u + 32u * g; }
 
 constexpr float kBase = 5.f;   // a row's reference is its largest exponent less this
 constexpr float kLimit = 8.f;  // weights stay below 2^8 (e4m3 ends at 448)
@@ -100,7 +105,7 @@ struct Params {
   float scale_log2;
   long long *prefix;  // [total_reqs + 1] units before each request
   int4 *info;         // [total_reqs] length, queries, first row, tiles
-  int *done;          // [CTAs] parts of the task that starts in this CTA and goes on
+  int *done;          // [CTAs][kGroups] parts done of the task that starts in this CTA and goes on, by row group
   float *part;        // [2 CTAs] partial rows: part_rows x 128, then part_rows log-sums
   int part_rows;
 };
@@ -108,7 +113,7 @@ struct Params {
 struct Item {
   int valid, b, c0, n, L, h;
   int row0, rows;       // first row of the task among the request's, and number
-  int nr, both;         // columns of a warpgroup; whether both take every tile
+  int nr, ng, wg;       // rows of a warpgroup (16 or 32); its warpgroups (1, 2 or 4) and their first
   int t0, t1;           // tiles
   int part, cta0, cta1; // partial slot (-1: whole task) and the CTAs of the task
 };
@@ -123,25 +128,24 @@ struct Meta {
 struct Shared {
   alignas(1024) uint8_t k[kKStages][kTileBytes];
   alignas(1024) uint8_t v[kVStages][kTileBytes];
-  alignas(1024) uint8_t q[2][2][2][kRows * kD];  // buffer, warpgroup, term
-  alignas(1024) uint8_t p[2][kKeys * 2 * kRows]; // a warpgroup's P; at the end, rows on their way
-  alignas(16) float4 state[2][kRows / 2];        // a pair of rows: ar, ar', -ref, -ref'
-  alignas(16) float alpha[2][kRows];
-  alignas(16) float red[2][4][kRows];
-  alignas(16) float qscale[kSlots][2][kRows];
-  float ref[2][kRows], sum[2][kRows];            // what the warpgroups hand each other at an item's end
-  int e0[2];
-  // first key of a span with a NaN in this dim of V, and whether there is one: of an
-  // item of one warpgroup (by warpgroup), and of both
-  int nan_key[3][kD], bad[3];
-  int last, abort;
+  alignas(1024) uint8_t q[2][2][kBlockRows * kD];      // buffer, term
+  alignas(1024) uint8_t p[kGroups][kKeys * 2 * kRows]; // a warpgroup's P; at the end, rows on their way
+  alignas(16) float4 state[kGroups][kRows / 2];        // a pair of rows: ar, ar', -ref, -ref'
+  alignas(16) float alpha[kGroups][kRows];
+  alignas(16) float red[kGroups][4][kRows];
+  alignas(16) float qscale[kSlots][kBlockRows];
+  float ref[kGroups][kRows], sum[kGroups][kRows];      // what the warpgroups hand each other at an item's end
+  // first key of a span with a NaN in this dim of V, and whether there is one (by an
+  // item's first warpgroup)
+  int nan_key[kGroups][kD], bad[kGroups];
+  int last[kGroups], abort;
   uint32_t tmem;
   Meta meta[kMeta];
   Item item[kSlots];
   uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
   uint64_t pg_full[kMeta], sc_full[kMeta], meta_empty[kMeta];
-  uint64_t q_full[2], q_empty[2], s_full[2], s_empty[2], p_full[2], pv_done[2];
-  uint64_t item_full[kSlots], item_empty[kSlots], pair, drain[2];
+  uint64_t q_full[kSlots], q_empty[2], s_full[kGroups], s_empty[kGroups], p_full[kGroups], pv_done[kGroups];
+  uint64_t item_full[kSlots], item_empty[kSlots], pair[2], all, drain[2];
 };
 constexpr int kSharedBytes = (int)sizeof(Shared) + 1024;  // the base is aligned by hand
 static_assert(kSharedBytes <= 232448, "shared memory of one CTA");
@@ -226,25 +230,43 @@ IPD_DEVINL void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory");
 IPD_DEVINL void grid_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // ---- waits ---------------------------------------------------------------------
-// A wait that gives up after about a second, or as soon as another warp of the CTA
-// has given up; the clock and the flag are looked at every few tries only.
+// For a whole warp, with one answer.  Gives up after about a second, or as soon as
+// another warp of the CTA has given up.
 IPD_DEVINL bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort) {
   const long long t0 = clock64();
-  while (true) {
+  bool ok;
 #pragma unroll 1
-    for (int i = 0; i < 64; ++i)
-      if (mbar_try_wait(bar, parity)) return true;
-    if (*abort) return false;
+  while (!(ok = mbar_try_wait(bar, parity)) && !*abort)
     if (clock64() - t0 > kWaitLimitCycles) {
       ipd_set_error(&g_attn8_err, IPD_DEVERR_WAIT);
       *abort = 1;
-      return false;
     }
-  }
+  return __all_sync(0xffffffffu, ok) != 0;
 }
-// for a whole warp, with one answer
+__device__ __noinline__ bool wait_slow_call(uint64_t *bar, uint32_t parity, volatile int *abort) {
+  return wait_slow(bar, parity, abort);
+}
 IPD_DEVINL bool wait(uint64_t *bar, uint32_t parity, volatile int *abort) {
-  return __all_sync(0xffffffffu, mbar_try_wait(bar, parity) || wait_slow(bar, parity, abort)) != 0;
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return wait_slow_call(bar, parity, abort);
+}
+// ... without a call, where many registers are live
+IPD_DEVINL bool wait_inline(uint64_t *bar, uint32_t parity, volatile int *abort) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return wait_slow(bar, parity, abort);
+}
+// One lane of a converged warp issues; every other value is the whole warp's, so that
+// operands stay in uniform registers (issued from a branch of one lane, a product
+// or a copy takes hundreds of cycles).
+IPD_DEVINL bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+IPD_DEVINL int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+IPD_DEVINL void commit(uint64_t *bar) {
+  if (elect_one()) tc_commit(bar);
+  __syncwarp();
 }
 // The n-th use (0, 1, ...) of a barrier of a ring of `ring`: a consumer waits for it
 // with full(n), a producer for the release of its slot with free(n).
@@ -267,7 +289,7 @@ __global__ void __launch_bounds__(1024) attn8_plan_kernel(const __grid_constant_
   __shared__ long long warp_units[32];
   grid_launch();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-  for (int i = tid; i < ctas; i += blockDim.x) P.done[i] = 0;
+  for (int i = tid; i < ctas * kGroups; i += blockDim.x) P.done[i] = 0;
   long long carry = 0;
   for (int base = 0; base < P.total_reqs; base += blockDim.x) {
     const int g = base + tid;
@@ -313,7 +335,7 @@ __device__ void meta_warp(const Params &P, Shared &S, int lane) {
   grid_wait();  // what the plan wrote
   const long long W = P.prefix[P.total_reqs];
   const long long C = W < (long long)gridDim.x ? W : gridDim.x;
-  uint32_t n = 0, it = 0;
+  uint32_t n = 0, it = 0, turn = 0;
   long long pos = 0, hi = 0;
   int g = 0;
   if (blockIdx.x < C) {
@@ -351,14 +373,20 @@ __device__ void meta_warp(const Params &P, Shared &S, int lane) {
       Item &I = S.item[slot];
       I.valid = 1, I.b = b, I.c0 = info.z, I.n = info.y, I.L = L, I.h = h;
       I.row0 = row0, I.rows = min(kBlockRows, rows_all - row0);
-      I.both = I.rows > kRows;
-      I.nr = I.rows > 32 ? 64 : I.rows > 16 ? 32 : 16;
+      I.nr = I.rows > 16 ? 32 : 16;
+      I.ng = I.rows > 64 ? 4 : I.rows > 32 ? 2 : 1;
+      // the warpgroups take items in turn, those of two or four together
+      I.wg = (int)((turn + I.ng - 1) & (uint32_t)(kGroups - I.ng));
       I.t0 = t0, I.t1 = t1;
       I.part = t1 - t0 == tiles ? -1 : t0 > 0 ? 2 * (int)blockIdx.x : 2 * (int)blockIdx.x + 1;
       // CTA i begins at unit floor(i W / C): the last one that begins at p or before
       const long long p0 = pos - t0, p1 = p0 + tiles - 1;
       I.cta0 = (int)(((p0 + 1) * C - 1) / W), I.cta1 = (int)(((p1 + 1) * C - 1) / W);
       mbar_arrive(&S.item_full[slot]);
+    }
+    {
+      const int rows = min(kBlockRows, rows_all - row0), ng = rows > 64 ? 4 : rows > 32 ? 2 : 1;
+      turn = ((turn + ng - 1) & (uint32_t)(kGroups - ng)) + ng;
     }
     const int *pages = B.page_table + (size_t)r * B.max_pages;
     const int n_pages = (L + kPage - 1) / kPage;
@@ -408,24 +436,27 @@ template <bool kIsV>
 __device__ void load_warp(const Params &P, Shared &S, int lane) {
   constexpr int kRing = kIsV ? kVStages : kKStages;
   uint64_t *fulls = kIsV ? S.v_full : S.k_full, *empties = kIsV ? S.v_empty : S.k_empty;
+  uint8_t *ring = kIsV ? S.v[0] : S.k[0];
   const uint64_t policy = l2_policy_evict_first();
   uint32_t it = 0;
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
     if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) break;
     const Item &I = S.item[slot];
-    if (!I.valid) return;
-    const CUtensorMap *map = kIsV ? &P.v[I.b] : &P.k[I.b];
-    const int tiles = I.t1 - I.t0;
+    if (!uniform(I.valid)) return;
+    const int b = uniform(I.b), tiles = uniform(I.t1 - I.t0);
+    const CUtensorMap *map = kIsV ? &P.v[b] : &P.k[b];
     bool ok = true;
-    for (int t = 0; ok && t < tiles; ++t, ++it) {
+    for (int t = 0; t < tiles; ++t, ++it) {
       const uint32_t m = it % kMeta, s = it % kRing;
       ok = wait(&S.pg_full[m], full(it, kMeta), &S.abort) && wait(&empties[s], free_(it, kRing), &S.abort);
       if (!ok) break;
-      if (lane == 0) mbar_arrive_expect_tx(&fulls[s], kTileBytes);
-      __syncwarp();
-      if (lane < kPages)
-        tma_load_2d((kIsV ? S.v[s] : S.k[s]) + lane * kPageBytes, map, 0, S.meta[m].y[lane], &fulls[s], policy);
+      if (elect_one()) {
+        mbar_arrive_expect_tx(&fulls[s], kTileBytes);
+#pragma unroll 1
+        for (int i = 0; i < kPages; ++i)
+          tma_load_2d(ring + s * kTileBytes + i * kPageBytes, map, 0, S.meta[m].y[i], &fulls[s], policy);
+      }
       __syncwarp();
     }
     if (!ok) break;
@@ -452,44 +483,41 @@ IPD_DEVINL void drain(uint64_t *bar, int lane) {
 }
 
 __device__ void qk_warp(Shared &S, int lane) {
-  uint32_t it = 0, used[2] = {0, 0};
+  const uint32_t tmem = (uint32_t)uniform((int)S.tmem);
+  const uint64_t k0 = sdesc((uint32_t)uniform((int)smem_u32(S.k[0])), 128),
+                 q0 = sdesc((uint32_t)uniform((int)smem_u32(S.q[0][0])), 128);
+  constexpr uint64_t kTerm = kBlockRows * kD >> 4;  // of descriptors: from a term of q to the next
+  uint32_t it = 0, uses = 0;  // (a bit a warpgroup: parity of its uses)
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
     if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) break;
     const Item &I = S.item[slot];
-    if (!I.valid) return;
-    const int tiles = I.t1 - I.t0, nr = I.nr;
-    const bool both = I.both;
-    const uint32_t idesc = idesc_f8(nr, 0), buf = n & 1;
-    bool ok = wait(&S.q_full[buf], full(n, 2), &S.abort);
+    if (!uniform(I.valid)) return;
+    const int tiles = uniform(I.t1 - I.t0), ng = uniform(I.ng);
+    const uint32_t idesc = idesc_f8(uniform(I.nr) * ng, 0), buf = n & 1;
+    const uint32_t g0 = (uint32_t)uniform(I.wg);
+    bool ok = wait(&S.q_full[slot], full(n, kSlots), &S.abort);
+    const uint64_t q = q0 + (uint64_t)buf * 2 * kTerm;
     for (int t = 0; ok && t < tiles; ++t, ++it) {
       const uint32_t s = it % kKStages;
       ok = wait(&S.k_full[s], full(it, kKStages), &S.abort);
-      for (int k = 0; ok && k < (both ? 2 : 1); ++k) {
-        const int g = both ? k : (int)(it & 1);
-        ok = wait(&S.s_empty[g], free_(used[g], 1), &S.abort);
-        if (!ok) break;
-        ++used[g];
-        tc_fence_after();
-        if (lane == 0) {
-          const uint64_t a = sdesc(smem_u32(S.k[s]), 128);
-          const uint64_t hi = sdesc(smem_u32(S.q[buf][both ? k : 0][0]), 128),
-                         lo = sdesc(smem_u32(S.q[buf][both ? k : 0][1]), 128);
-          const uint32_t d = S.tmem + col_s(g);
-#pragma unroll
-          for (int kk = 0; kk < kD / 32; ++kk) {
-            tc_mma_f8(d, a + 2 * kk, hi + 2 * kk, idesc, kk != 0);
-            tc_mma_f8(d, a + 2 * kk, lo + 2 * kk, idesc, 1);
-          }
-          tc_commit(&S.s_full[g]);
+      for (int i = 0; ok && i < ng; ++i) ok = wait(&S.s_empty[g0 + i], (uses >> (g0 + i) & 1u) ^ 1u, &S.abort);
+      if (!ok) break;
+      uses ^= ((1u << ng) - 1u) << g0;
+      tc_fence_after();
+      const uint64_t k = k0 + (uint64_t)(s * (kTileBytes >> 4));
+      const uint32_t d = tmem + col_s(g0);
+      if (elect_one()) {
+#pragma unroll 1
+        for (int kk = 0; kk < kD / 32; ++kk) {
+          tc_mma_f8(d, k + 2 * kk, q + 2 * kk, idesc, kk != 0);
+          tc_mma_f8(d, k + 2 * kk, q + kTerm + 2 * kk, idesc, 1);
         }
-        __syncwarp();
-      }
-      if (ok && lane == 0) {
-        tc_commit(&S.k_empty[s]);
-        if (t == tiles - 1) tc_commit(&S.q_empty[buf]);
       }
       __syncwarp();
+      for (int i = 0; i < ng; ++i) commit(&S.s_full[g0 + i]);
+      commit(&S.k_empty[s]);
+      if (t == tiles - 1) commit(&S.q_empty[buf]);
     }
     if (!ok) break;
     arrive_warp(&S.item_empty[slot], lane);
@@ -498,42 +526,42 @@ __device__ void qk_warp(Shared &S, int lane) {
 }
 
 __device__ void pv_warp(Shared &S, int lane) {
-  uint32_t it = 0, used[2] = {0, 0};
+  const uint32_t tmem = (uint32_t)uniform((int)S.tmem);
+  const uint64_t v0 = sdesc((uint32_t)uniform((int)smem_u32(S.v[0])), 128);
+  uint32_t it = 0, uses = 0;
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
     if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) break;
     const Item &I = S.item[slot];
-    if (!I.valid) return;
-    const int tiles = I.t1 - I.t0, nr = I.nr;
-    const bool both = I.both;
+    if (!uniform(I.valid)) return;
+    const int tiles = uniform(I.t1 - I.t0), ng = uniform(I.ng), nr = uniform(I.nr);
     const uint32_t idesc = idesc_f8(2 * nr, 1);
-    const uint32_t step = 32 * 2 * nr >> 4;  // 32 keys of P further on
-    bool begun[2] = {false, false}, ok = true;
-    for (int t = 0; ok && t < tiles; ++t, ++it) {
+    const uint64_t p0 = sdesc((uint32_t)uniform((int)smem_u32(S.p[0])), 2 * nr);
+    const uint64_t step = (uint64_t)(32 * 2 * nr >> 4);  // 32 keys of P further on
+    const uint32_t g0 = (uint32_t)uniform(I.wg);
+    bool ok = true;
+    for (int t = 0; t < tiles; ++t, ++it) {
       const uint32_t s = it % kVStages;
       ok = wait(&S.v_full[s], full(it, kVStages), &S.abort);
-      for (int k = 0; ok && k < (both ? 2 : 1); ++k) {
-        const int g = both ? k : (int)(it & 1);
-        ok = wait(&S.p_full[g], full(used[g], 1), &S.abort);
+      const uint64_t v = v0 + (uint64_t)(s * (kTileBytes >> 4));
+      for (int i = 0; ok && i < ng; ++i) {
+        const uint32_t g = g0 + i;
+        ok = wait(&S.p_full[g], uses >> g & 1u, &S.abort);
         if (!ok) break;
-        ++used[g];
         tc_fence_after();
-        if (lane == 0) {
-          const uint64_t a = sdesc(smem_u32(S.v[s]), 128), b = sdesc(smem_u32(S.p[g]), 2 * nr);
-          const uint32_t d = S.tmem + col_o(g);
-#pragma unroll
+        const uint64_t p = p0 + (uint64_t)(g * (uint32_t)(sizeof(S.p[0]) >> 4));
+        if (elect_one()) {
+#pragma unroll 1
           for (int kk = 0; kk < kKeys / 32; ++kk)
-            tc_mma_f8(d, a + (uint64_t)(kk * 32 * kD >> 4), b + (uint64_t)(kk * step), idesc, begun[g] || kk != 0);
+            tc_mma_f8(tmem + col_o(g), v + (uint64_t)(kk * 32 * kD >> 4), p + kk * step, idesc, t != 0 || kk != 0);
           tc_commit(&S.pv_done[g]);
         }
-        begun[g] = true;
         __syncwarp();
       }
-      if (ok && lane == 0) {
-        tc_commit(&S.v_empty[s]);
-        tc_commit(&S.meta_empty[it % kMeta]);
-      }
-      __syncwarp();
+      if (!ok) break;
+      uses ^= ((1u << ng) - 1u) << g0;
+      commit(&S.v_empty[s]);
+      commit(&S.meta_empty[it % kMeta]);
     }
     if (!ok) break;
     arrive_warp(&S.item_empty[slot], lane);
@@ -545,7 +573,10 @@ __device__ void pv_warp(Shared &S, int lane) {
 // A row as two e4m3 terms: with 2^e the least power of two that brings its largest
 // entry to 448 or below, hi = e4m3(q 2^-e), lo = e4m3(q 2^-e - hi), which together
 // hold a bf16's eight bits down to 2^-10, 2^-17 of the row's largest entry.
+// Half a warp a row, eight entries a lane.
 __device__ void query_warp(const Params &P, Shared &S, int w, int lane) {
+  constexpr int kAhead = 4;  // pairs of rows loaded ahead
+  const int half = lane >> 4, part = lane & 15;
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
     if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) return;
@@ -554,47 +585,52 @@ __device__ void query_warp(const Params &P, Shared &S, int w, int lane) {
     const uint32_t buf = n & 1;
     if (!wait(&S.q_empty[buf], free_(n, 2), &S.abort)) return;
     const BatchDev &B = P.b[I.b];
-    const int all = I.both ? 2 * kRows : I.nr, group = B.group;
-    constexpr int kAhead = 4;
-    for (int r0 = w; r0 < all; r0 += kAhead * kQWarps) {
-      uint2 x[kAhead];
+    const int all = I.nr * I.ng, group = B.group;
+    const auto fetch = [&](int r) {
+      if (r >= I.rows) return make_uint4(0u, 0u, 0u, 0u);
+      const int row = I.row0 + r, query = row / group;
+      return *reinterpret_cast<const uint4 *>(
+          B.q + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group + (row - query * group)) * kD + part * 8);
+    };
+    uint4 next[kAhead];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int r = r0 + i * kQWarps;
-        x[i] = make_uint2(0u, 0u);
-        if (r < I.rows) {
-          const int row = I.row0 + r, query = row / group;
-          x[i] = *reinterpret_cast<const uint2 *>(
-              B.q + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group + (row - query * group)) * kD + lane * 4);
-        }
-      }
+    for (int i = 0; i < kAhead; ++i) next[i] = fetch(2 * (w + i * kQWarps) + half);
+#pragma unroll 1
+    for (int r = 2 * w + half; r - half < all; r += 2 * kQWarps) {
+      const uint4 x = next[0];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int r = r0 + i * kQWarps;
-        if (r >= all) break;
-        const uint32_t a = x[i].x & 0x7fff7fffu, c = x[i].y & 0x7fff7fffu;
-        const uint32_t top = __reduce_max_sync(0xffffffffu, max(max(a & 0xffffu, a >> 16), max(c & 0xffffu, c >> 16)));
-        const int E = (int)(top >> 7);
-        // (a largest entry below 2^-100 counts as zero; one that is not finite makes
-        // the row NaN)
-        const int e = E - 127 - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0);
-        const bool none = E < 27 || E == 255;
-        const float f = none ? 0.f : pow2i(-e);
-        float v[4] = {bf16lo(x[i].x) * f, bf16hi(x[i].x) * f, bf16lo(x[i].y) * f, bf16hi(x[i].y) * f};
+      for (int i = 0; i + 1 < kAhead; ++i) next[i] = next[i + 1];
+      next[kAhead - 1] = fetch(r + 2 * kQWarps * kAhead);
+      const uint32_t *xw = &x.x;
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = __vmaxu2(top, xw[i] & 0x7fff7fffu);
+      top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const int E = (int)(top >> 7);
+      // (a largest entry below 2^-100 counts as zero; one that is not finite makes the
+      // row NaN)
+      const int e = E - 127 - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0);
+      const bool none = E < 27 || E == 255;
+      const float f = none ? 0.f : pow2i(-e);
+      uint32_t hi[2], lo[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float v[4] = {bf16lo(xw[2 * k]) * f, bf16hi(xw[2 * k]) * f, bf16lo(xw[2 * k + 1]) * f, bf16hi(xw[2 * k + 1]) * f};
         if (none) v[0] = v[1] = v[2] = v[3] = 0.f;
-        const uint32_t hi = e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16;
+        hi[k] = e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16;
         float back[4];
-        e4m3x4_to_floats(hi, back);
-        const uint32_t lo = e4m3x2(v[0] - back[0], v[1] - back[1]) | e4m3x2(v[2] - back[2], v[3] - back[3]) << 16;
-        const int g = r / kRows, rr = r % kRows;
-        const int at = rr * kD + (((lane >> 2) ^ (rr & 7)) << 4) + (lane & 3) * 4;
-        *reinterpret_cast<uint32_t *>(&S.q[buf][g][0][at]) = hi;
-        *reinterpret_cast<uint32_t *>(&S.q[buf][g][1][at]) = lo;
-        if (lane == 0) S.qscale[slot][g][rr] = E == 255 ? __uint_as_float(0x7fc00000u) : none ? 0.f : pow2i(e);
+        e4m3x4_to_floats(hi[k], back);
+        lo[k] = e4m3x2(v[0] - back[0], v[1] - back[1]) | e4m3x2(v[2] - back[2], v[3] - back[3]) << 16;
       }
+      const int at = r * kD + (((part >> 1) ^ (r & 7)) << 4) + (part & 1) * 8;
+      *reinterpret_cast<uint2 *>(&S.q[buf][0][at]) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint2 *>(&S.q[buf][1][at]) = make_uint2(lo[0], lo[1]);
+      if (part == 0) S.qscale[slot][r] = E == 255 ? __uint_as_float(0x7fc00000u) : none ? 0.f : pow2i(e);
     }
     fence_proxy_async_smem();
-    arrive_warp(&S.q_full[buf], lane);
+    arrive_warp(&S.q_full[slot], lane);
     arrive_warp(&S.item_empty[slot], lane);
   }
 }
@@ -619,91 +655,126 @@ IPD_DEVINL float column_reduce(float (&a)[16], int lane, Op op) {
 struct Softmax {
   int g, tid, warp, lane;  // warpgroup, and place in it
   uint32_t tiles, it;      // own tiles so far, tiles of the CTA so far
-  uint32_t pairs;          // barriers with the other warpgroup so far
+  uint32_t pairs, alls;    // barriers of two and of all warpgroups so far
   bool ok;                 // no wait of this warp has given up
 };
-
-// The S columns of a tile, one key a thread: issues the loads.
-IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[1][16]) { tc_ld_32x32b_x16(taddr, r[0]); }
-template <int N>
-IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[N][32]) {
-#pragma unroll
-  for (int c = 0; c < N; ++c) tc_ld_32x32b_x32(taddr + 32 * c, r[c]);
-}
 
 // A thread's key of a tile that holds hidden keys: NaN in its V row.  They would reach
 // rows that do not see the key (0 x NaN), so they become 0, and rows that do see
 // it get them back at the end.
 IPD_DEVINL void mend(Shared &S, int set, uint8_t *v, int key_in_tile, int key, int L) {
   bool wrote = false;
-  for (int i = 0; i < 8; ++i) {
-    const int c = (i + key_in_tile) & 7;
-    uint4 *at = reinterpret_cast<uint4 *>(v + key_in_tile * kD + c * 16);
-    uint4 x = *at;
-    uint32_t *w = &x.x;
-    bool any = false;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) any |= __vcmpeq4(w[k] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
-    if (!any) continue;
-    for (int k = 0; k < 4; ++k)
-      for (int e = 0; e < 4; ++e)
-        if ((w[k] >> 8 * e & 0x7fu) == 0x7fu) {
-          if (key < L) {
-            atomicMin(&S.nan_key[set][((c ^ (key_in_tile & 7)) << 4) + k * 4 + e], key);
-            S.bad[set] = 1;
-          }
-          w[k] &= ~(0xffu << 8 * e);
+#pragma unroll 1
+  for (int i = 0; i < 32; ++i) {
+    const int c = ((i >> 2) + key_in_tile) & 7, at = c * 16 + (i & 3) * 4;
+    uint32_t *w = reinterpret_cast<uint32_t *>(v + key_in_tile * kD + at);
+    uint32_t x = *w;
+    if (__vcmpeq4(x & 0x7f7f7f7fu, 0x7f7f7f7fu) == 0) continue;
+#pragma unroll 1
+    for (int e = 0; e < 4; ++e)
+      if ((x >> 8 * e & 0x7fu) == 0x7fu) {
+        if (key < L) {
+          atomicMin(&S.nan_key[set][((c ^ (key_in_tile & 7)) << 4) + (i & 3) * 4 + e], key);
+          S.bad[set] = 1;
         }
+        x &= ~(0xffu << 8 * e);
+      }
     __threadfence_block();  // noted before it is gone
-    *at = x;
+    *w = x;
     wrote = true;
   }
   if (wrote) fence_proxy_async_smem();
 }
 
-// Both warpgroups' barrier.  Bounded, as every wait: a warpgroup that has given up
-// does not come.
-IPD_DEVINL void pair_sync(Shared &S, Softmax &X) {
-  arrive_warp(&S.pair, X.lane);
-  X.ok = wait(&S.pair, full(X.pairs, 1), &S.abort) && X.ok;
-  ++X.pairs;
+// Exponents of the rows at a thread's key, against their references.
+template <int NR>
+IPD_DEVINL void exponents(const uint32_t (&s)[NR], const float4 *state, float ck, float (&y)[NR]) {
+  const u64 ck2 = f2_pack(ck, ck);
+#pragma unroll
+  for (int i = 0; i < NR; i += 2) {
+    const float4 st = state[i / 2];
+    f2_unpack(f2_fma(mul2(f2_pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), ck2), f2_pack(st.x, st.y),
+                     f2_pack(st.z, st.w)), y[i], y[i + 1]);
+  }
 }
 
-// An item's tiles, and its rows at the end.  A wait that gives up does not leave the
-// way the others go: the warps of a warpgroup meet at barriers.
+IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[16]) { tc_ld_32x32b_x16(taddr, r); }
+IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[32]) { tc_ld_32x32b_x32(taddr, r); }
+
+// The rows' references move to their largest exponent so far, less kBase; what has
+// been summed moves with them.
 template <int NR>
-__device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t item, const Item &I) {
-  const int g = X.g, lane = X.lane, tid = X.tid, slot = item % kSlots;
-  const bool both = I.both;
-  const int n_tiles = I.t1 - I.t0, L = I.L;
-  const uint32_t lanes = (uint32_t)X.warp << 21;  // this warp's 32 TMEM lanes
-  const uint32_t s_addr = S.tmem + lanes + col_s(g), o_addr = S.tmem + lanes + col_o(g);
-  // rows of this warpgroup, and the key from which on some row of the task does not see
-  const int row0 = I.row0 + (both ? g * kRows : 0);
-  const int rows = both ? (g == 0 ? kRows : I.rows - kRows) : I.rows;
-  const int group = P.b[I.b].group;
-  const int sees = L - I.n;  // query i sees keys up to sees + i
-  const int masked = sees + 1 + I.row0 / group;
-  X.ok = wait(&S.q_full[item & 1], full(item, 2), &S.abort) && X.ok;
-  if (tid < NR) {
-    float *st = reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1);
-    st[0] = S.qscale[slot][both ? g : 0][tid];
-    st[2] = 0.f;
-    S.ref[g][tid] = -INFINITY;  // (its largest so far)
+IPD_DEVINL void move_references(Shared &S, const Softmax &X, float (&y)[NR], float de, bool first, uint32_t o_addr,
+                                uint32_t l_addr) {
+  const int g = X.g, tid = X.tid, lane = X.lane;
+#pragma unroll
+  for (int c = 0; c < NR; c += 16) {
+    float z[16];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float4 st = S.state[g][(c + i) / 2];
+      z[i] = y[c + i] - st.z + de;
+      z[i + 1] = y[c + i + 1] - st.w + de;
+    }
+    const float x = column_reduce(z, lane, [](float a, float b) { return fmaxf(a, b); });
+    if (!(lane & 1)) S.red[g][X.warp][c + (lane >> 1)] = x;
   }
   named_bar_sync(1 + g, 128);
-  u64 l[NR / 2];
+  if (tid < NR) {
+    const float was = S.ref[g][tid];
+    const float now = fmaxf(fmax3(S.red[g][0][tid], S.red[g][1][tid], S.red[g][2][tid]), fmaxf(S.red[g][3][tid], was));
+    float *st = reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1);
+    // (a row that has seen nothing, or NaN alone, stays at 0)
+    const float old = st[2], ref = now == -INFINITY || now == INFINITY ? -old : now - kBase;
+    S.ref[g][tid] = now;
+    st[2] = -ref;
+    S.alpha[g][tid] = was == -INFINITY ? 0.f : ex2_approx(-old - ref);
+    S.red[g][0][tid] = -old - ref;  // what the exponents move by
+  }
+  named_bar_sync(1 + g, 128);
 #pragma unroll
-  for (int i = 0; i < NR / 2; ++i) l[i] = 0;
-  const bool joint = !both && n_tiles > 1;  // both warpgroups have tiles of the same rows
-  const int set = joint || both ? 2 : g;
+  for (int i = 0; i < NR; ++i) y[i] += S.red[g][0][i];
+#pragma unroll 1
+  for (int c = first ? 2 * NR : 0; c < 3 * NR; c += 16) {  // O's halves, and the sums
+    const uint32_t at = c < 2 * NR ? o_addr + c : l_addr + (c - 2 * NR);
+    uint32_t o[16];
+    if (first) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[i] = 0u;
+    } else {
+      tc_ld_32x32b_x16(at, o);
+      tc_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * S.alpha[g][(c + i) & (NR - 1)]);
+    }
+    tc_st_32x32b_x16(at, o);
+  }
+  tc_wait_st();
+  named_bar_sync(1 + g, 128);  // red and alpha are read
+}
+
+// The weights of a warpgroup's rows for its tiles of an item.  A wait that gives up
+// does not leave the way the others go: the warps of a warpgroup meet at barriers.
+// Returns the exponent that V's scales count from.
+template <int NR>
+__device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item &I) {
+  const int g = X.g, lane = X.lane, tid = X.tid;
+  const int n_tiles = I.t1 - I.t0, L = I.L;
+  const uint32_t lanes = (uint32_t)X.warp << 21;  // this warp's 32 TMEM lanes
+  const uint32_t s_addr = S.tmem + lanes + col_s(g), o_addr = S.tmem + lanes + col_o(g), l_addr = S.tmem + lanes + col_l(g);
+  const int row0 = I.row0 + (g - I.wg) * kRows;
+  const int group = P.b[I.b].group;
+  const int sees = L - I.n;                        // query i sees keys up to sees + i
+  const int masked = sees + 1 + I.row0 / group;    // the first key that some row of the task does not see
+  const int turn = NR == 32 ? (tid >> 1) & 3 : (tid >> 2) & 1;  // P's swizzle
+  uint8_t *prow = S.p[g] + tid * 2 * NR;
   int e0 = 0;
   bool first = true;
+#pragma unroll 1
   for (int t = 0; t < n_tiles; ++t) {
     const uint32_t it = X.it + t;
-    if (!both && (int)(it & 1) != g) continue;
     const uint32_t m = it % kMeta;
-    X.ok = wait(&S.sc_full[m], full(it, kMeta), &S.abort) && X.ok;
+    X.ok = wait_inline(&S.sc_full[m], full(it, kMeta), &S.abort) && X.ok;
     const Meta &M = S.meta[m];
     const int key0 = (I.t0 + t) * kKeys, key = key0 + tid;
     const float ck = M.ck[tid / kPage];
@@ -723,103 +794,51 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
       if (hidden == NR) de = 0;
     }
     const float fk = ev == 128 && hidden < NR ? __uint_as_float(0x7fc00000u) : pow2i(de);
-    X.ok = wait(&S.s_full[g], full(X.tiles, 1), &S.abort) && X.ok;
+    X.ok = wait_inline(&S.s_full[g], full(X.tiles, 1), &S.abort) && X.ok;
     tc_fence_after();
     float y[NR];
     {
-      constexpr int N = NR < 32 ? NR : 32;
-      uint32_t raw[NR / N][N];
-      load_scores(s_addr, raw);
+      uint32_t s[NR];
+      load_scores(s_addr, s);
       tc_wait_ld();
-#pragma unroll
-      for (int i = 0; i < NR; ++i) y[i] = __uint_as_float(raw[i / N][i % N]);
+      exponents(s, S.state[g], ck, y);
     }
     tc_fence_before();
     arrive_warp(&S.s_empty[g], lane);
-    const u64 ck2 = f2_pack(ck, ck);
-    float top = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < NR; i += 2) {
-      const float4 st = S.state[g][i / 2];
-      f2_unpack(f2_fma(mul2(f2_pack(y[i], y[i + 1]), ck2), f2_pack(st.x, st.y), f2_pack(st.z, st.w)), y[i], y[i + 1]);
-    }
     if (hides) {
 #pragma unroll
       for (int i = 0; i < NR; ++i)
         if (i < hidden) y[i] = -INFINITY;
     }
+    float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NR; i += 2) top = fmax3(top, y[i], y[i + 1]);
-    if (bar_or(1 + g, 128, first || top + (float)de > kLimit)) {
-      // the rows' references move: largest exponent so far, less kBase
-#pragma unroll
-      for (int c = 0; c < NR; c += 16) {
-        float z[16];
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const float4 st = S.state[g][(c + i) / 2];
-          z[i] = y[c + i] - st.z + (float)de;
-          z[i + 1] = y[c + i + 1] - st.w + (float)de;
-        }
-        const float x = column_reduce(z, lane, [](float a, float b) { return fmaxf(a, b); });
-        if (!(lane & 1)) S.red[g][X.warp][c + (lane >> 1)] = x;
-      }
-      named_bar_sync(1 + g, 128);
-      if (tid < NR) {
-        const float was = S.ref[g][tid];
-        const float now = fmaxf(fmax3(S.red[g][0][tid], S.red[g][1][tid], S.red[g][2][tid]), fmaxf(S.red[g][3][tid], was));
-        float *st = reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1);
-        // (a row that has seen nothing, or NaN alone, stays at 0)
-        const float old = st[2], ref = now == -INFINITY || now == INFINITY ? -old : now - kBase;
-        S.ref[g][tid] = now;
-        st[2] = -ref;
-        S.alpha[g][tid] = was == -INFINITY ? 0.f : ex2_approx(-old - ref);
-        S.red[g][0][tid] = -old - ref;  // what y moves by
-      }
-      named_bar_sync(1 + g, 128);
-#pragma unroll
-      for (int i = 0; i < NR; ++i) y[i] += S.red[g][0][i];
-      if (!first) {
-#pragma unroll
-        for (int i = 0; i < NR; i += 2) l[i / 2] = mul2(l[i / 2], *reinterpret_cast<const u64 *>(&S.alpha[g][i]));
-        X.ok = wait(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort) && X.ok;
-        tc_fence_after();
-#pragma unroll 1
-        for (int c = 0; c < 2 * NR; c += 16) {
-          uint32_t o[16];
-          tc_ld_32x32b_x16(o_addr + c, o);
-          tc_wait_ld();
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * S.alpha[g][(c + i) & (NR - 1)]);
-          tc_st_32x32b_x16(o_addr + c, o);
-        }
-        tc_wait_st();
-        tc_fence_before();
-      }
-      named_bar_sync(1 + g, 128);  // red and alpha are read
-    }
-    // P's buffer is free once this warpgroup's product before is complete
-    if (X.tiles > 0) X.ok = wait(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort) && X.ok;
+    const bool move = bar_or(1 + g, 128, first || top + (float)de > kLimit);
+    // P's buffer is free, and O at rest, once this warpgroup's product before is complete
+    if (X.tiles > 0) X.ok = wait_inline(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort) && X.ok;
+    tc_fence_after();
+    if (move) move_references<NR>(S, X, y, (float)de, first, o_addr, l_addr);
     const u64 fk2 = f2_pack(fk, fk);
     const uint32_t lo16 = half2_of(kLoScale, kLoScale);
-    uint8_t *prow = S.p[g] + tid * 2 * NR;
-    const int turn = NR == 64 ? tid & 7 : NR == 32 ? (tid >> 1) & 3 : (tid >> 2) & 1;
 #pragma unroll
     for (int c = 0; c < NR; c += 16) {
+      uint32_t l[16];
+      tc_ld_32x32b_x16(l_addr + c, l);
       uint32_t hi[4], lo[4];
+      float p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = ex2_approx(y[c + i]);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         uint32_t h[2], e[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const int i = c + q * 4 + k * 2;
-          const u64 p = f2_pack(ex2_approx(y[i]), ex2_approx(y[i + 1]));
-          l[i / 2] = f2_add(l[i / 2], p);
+          const int i = q * 4 + k * 2;
           float w0, w1;
-          f2_unpack(mul2(p, fk2), w0, w1);
+          f2_unpack(mul2(f2_pack(p[i], p[i + 1]), fk2), w0, w1);
           if (hides) {  // (a NaN scale reaches no hidden row)
-            if (i < hidden) w0 = 0.f;
-            if (i + 1 < hidden) w1 = 0.f;
+            if (c + i < hidden) w0 = 0.f;
+            if (c + i + 1 < hidden) w1 = 0.f;
           }
           h[k] = half2_of(w0, w1);
           e[k] = e4m3x2_h2(h[k]);
@@ -831,176 +850,174 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
       }
       *reinterpret_cast<uint4 *>(prow + (((c / 16) ^ turn) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
       *reinterpret_cast<uint4 *>(prow + ((((NR + c) / 16) ^ turn) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      tc_wait_ld();
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        float l0, l1;
+        f2_unpack(f2_add(f2_pack(__uint_as_float(l[i]), __uint_as_float(l[i + 1])), f2_pack(p[i], p[i + 1])), l0, l1);
+        l[i] = __float_as_uint(l0), l[i + 1] = __float_as_uint(l1);
+      }
+      tc_st_32x32b_x16(l_addr + c, l);
     }
-    if (key0 + kKeys > masked) {
+    // (the product takes the first warpgroup's rows before the others')
+    if (key0 + kKeys > masked && g == I.wg) {
       const uint32_t vs = it % kVStages;
-      X.ok = wait(&S.v_full[vs], full(it, kVStages), &S.abort) && X.ok;
-      if (key >= masked) mend(S, set, S.v[vs], tid, key, L);
+      X.ok = wait_inline(&S.v_full[vs], full(it, kVStages), &S.abort) && X.ok;
+      if (key >= masked) mend(S, g, S.v[vs], tid, key, L);
     }
     fence_proxy_async_smem();
+    tc_wait_st();
+    tc_fence_before();
     arrive_warp(&S.p_full[g], lane);
     ++X.tiles;
     first = false;
   }
-  X.it += n_tiles;
-  // the rows: sums over the threads, the other warpgroup's part, output
-  const bool mine = !first;                         // this warpgroup had a tile
-  if (!mine && !joint && I.part < 0) return;   // (all of the item was the other's)
-  if (mine) {
-#pragma unroll
-    for (int c = 0; c < NR; c += 16) {
-      float z[16];
-#pragma unroll
-      for (int i = 0; i < 16; i += 2) f2_unpack(l[(c + i) / 2], z[i], z[i + 1]);
-      const float x = column_reduce(z, lane, [](float a, float b) { return a + b; });
-      if (!(lane & 1)) S.red[g][X.warp][c + (lane >> 1)] = x;
-    }
-    named_bar_sync(1 + g, 128);
-    if (tid < NR) {
-      S.sum[g][tid] = (S.red[g][0][tid] + S.red[g][1][tid]) + (S.red[g][2][tid] + S.red[g][3][tid]);
-      const float *st = reinterpret_cast<const float *>(&S.state[g][tid >> 1]) + (tid & 1);
-      S.ref[g][tid] = -st[2];
-    }
-    if (tid == 0) S.e0[g] = e0;
-  }
-  if (joint || both) pair_sync(S, X);
-  else named_bar_sync(1 + g, 128);
-  float *part = nullptr;
-  if (I.part >= 0) part = P.part + (size_t)I.part * P.part_rows * (kD + 1);
-  if (mine) {
-    // factor of a row: 2^e0 / its sum, the two parts brought to one reference
-    if (tid < NR) {
-      float ref = S.ref[g][tid], sum = S.sum[g][tid], f = 1.f;
-      if (joint) {
-        const float other = S.ref[1 - g][tid], theirs = S.sum[1 - g][tid];
-        // (a part that has seen nothing has no say in the reference)
-        const float top = sum == 0.f ? other : theirs == 0.f ? ref : fmaxf(ref, other);
-        f = sum == 0.f ? 0.f : ex2_approx(ref - top);
-        sum = sum * f + (theirs == 0.f ? 0.f : theirs * ex2_approx(other - top));
-        ref = top;
-      }
-      // (a score past fp32 leaves no softmax)
-      S.alpha[g][tid] = sum == 0.f ? 0.f : sum == INFINITY ? __uint_as_float(0x7fc00000u) : f / sum * pow2i(e0);
-      if (part && tid < rows && (!joint || g == 0))
-        part[(size_t)P.part_rows * kD + (both ? g * kRows : 0) + tid] = sum == 0.f ? -INFINITY : ref + log2f(sum);
-    }
-    X.ok = wait(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort) && X.ok;
-    tc_fence_after();
-    named_bar_sync(1 + g, 128);
-  }
-  const int d = tid;
-  const bool bad = *(volatile int *)&S.bad[set] != 0;
-  const int nan_key = bad ? S.nan_key[set][d] : 0x7fffffff;
+  return e0;
+}
+
+// Joins the parts of a row group of a task that was cut between CTAs, in order.
+IPD_DEVINL void join(const Params &P, const Item &I, int r0, int rows, int warp, int lane) {
   const BatchDev &B = P.b[I.b];
-  auto emit = [&](int r, float x) {  // row r of the warpgroup
-    const int row = row0 + r, query = row / group;
-    if (nan_key <= sees + query) x = __uint_as_float(0x7fc00000u);
-    if (part)
-      part[(size_t)((both ? g * kRows : 0) + r) * kD + d] = x;
-    else
-      B.out[((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group + (row - query * group)) * kD + d] = f2bf16(x);
-  };
-  float *give = reinterpret_cast<float *>(S.p[g]);
-  if (mine) {
-    // (with two parts: this warpgroup's half of the rows it will put out stays, the
-    // other half goes through its P buffer)
-    const int half = NR / 2;
+  const size_t stride = (size_t)P.part_rows * (kD + 1);
+  auto slot_of = [&](int c) { return P.part + (size_t)(c == I.cta0 ? 2 * c + 1 : 2 * c) * stride; };
 #pragma unroll 1
-    for (int k = 0; k < NR; k += 8) {
-      const bool away = joint && (k < half) == (g == 1);
+  for (int r = r0 + warp; r < r0 + rows; r += 4) {
+    float top = -INFINITY;
+#pragma unroll 1
+    for (int c = I.cta0 + lane; c <= I.cta1; c += 32) top = fmaxf(top, slot_of(c)[(size_t)P.part_rows * kD + r]);
+    top = warp_max(top);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll 4
+    for (int c = I.cta0; c <= I.cta1; ++c) {
+      const float *s = slot_of(c);
+      const float lse = s[(size_t)P.part_rows * kD + r];
+      const float4 x = *reinterpret_cast<const float4 *>(s + (size_t)r * kD + lane * 4);
+      const float w = lse == -INFINITY ? 0.f : ex2_approx(lse - top);
+      sum += w;
+      acc.x += w * x.x, acc.y += w * x.y, acc.z += w * x.z, acc.w += w * x.w;
+    }
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    const int row = I.row0 + r, query = row / B.group;
+    *reinterpret_cast<uint2 *>(B.out + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * B.group + (row - query * B.group)) * kD +
+                               lane * 4) =
+        make_uint2((uint32_t)f2bf16(acc.x * f) | (uint32_t)f2bf16(acc.y * f) << 16,
+                   (uint32_t)f2bf16(acc.z * f) | (uint32_t)f2bf16(acc.w * f) << 16);
+  }
+}
+
+// A row group of an item: its tiles, then its rows.
+__device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t item, const Item &I) {
+  const int g = X.g, lane = X.lane, tid = X.tid, slot = item % kSlots;
+  const int nr = I.nr, rg = g - I.wg;
+  X.ok = wait_inline(&S.q_full[slot], full(item, kSlots), &S.abort) && X.ok;
+  if (tid < nr) {
+    float *st = reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1);
+    st[0] = S.qscale[slot][rg * kRows + tid];
+    st[2] = 0.f;
+    S.ref[g][tid] = -INFINITY;  // (its largest so far)
+  }
+  named_bar_sync(1 + g, 128);
+  const int e0 = nr == 32 ? softmax_tiles<32>(P, S, X, I) : softmax_tiles<16>(P, S, X, I);
+  // the sums over the threads
+  const uint32_t lanes = (uint32_t)X.warp << 21, o_addr = S.tmem + lanes + col_o(g), l_addr = S.tmem + lanes + col_l(g);
+#pragma unroll 1
+  for (int c = 0; c < nr; c += 16) {
+    uint32_t l[16];
+    float z[16];
+    tc_ld_32x32b_x16(l_addr + c, l);
+    tc_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = __uint_as_float(l[i]);
+    const float x = column_reduce(z, lane, [](float a, float b) { return a + b; });
+    if (!(lane & 1)) S.red[g][X.warp][c + (lane >> 1)] = x;
+  }
+  named_bar_sync(1 + g, 128);
+  const int rows = min(kRows, I.rows - rg * kRows);  // (none or fewer where the task has no such rows)
+  float *part = I.part >= 0 ? P.part + (size_t)I.part * P.part_rows * (kD + 1) : nullptr;
+  if (tid < nr) {
+    const float sum = (S.red[g][0][tid] + S.red[g][1][tid]) + (S.red[g][2][tid] + S.red[g][3][tid]);
+    // a row's factor: 2^e0 / its sum (a score past fp32 leaves no softmax)
+    S.alpha[g][tid] = sum == 0.f ? 0.f : sum == INFINITY ? __uint_as_float(0x7fc00000u) : pow2i(e0) / sum;
+    if (part && tid < rows) {
+      const float ref = -(reinterpret_cast<const float *>(&S.state[g][tid >> 1]) + (tid & 1))[2];
+      part[(size_t)P.part_rows * kD + rg * kRows + tid] = sum == 0.f ? -INFINITY : ref + log2f(sum);
+    }
+  }
+  X.ok = wait_inline(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort) && X.ok;
+  tc_fence_after();
+  named_bar_sync(1 + g, 128);
+  const bool bad = *(volatile int *)&S.bad[I.wg] != 0;
+  const int d = tid, row0 = I.row0 + rg * kRows, group = P.b[I.b].group;
+  {
+    const BatchDev &B = P.b[I.b];
+    int query = row0 / group, head = row0 - query * group;
+    uint16_t *at = B.out + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group + head) * kD + d;
+    float *to = part + (size_t)(rg * kRows) * kD + d;
+    const size_t turn_over = (size_t)(B.hq - group) * kD;
+    const int nan_key = bad ? S.nan_key[I.wg][d] : 0x7fffffff, sees = I.L - I.n;
+#pragma unroll 1
+    for (int k = 0; k < rows; k += 8) {
       uint32_t a[8], b[8];
       tc_ld_32x32b_x8(o_addr + k, a);
-      tc_ld_32x32b_x8(o_addr + NR + k, b);
+      tc_ld_32x32b_x8(o_addr + nr + k, b);
       tc_wait_ld();
-      if (k >= rows) continue;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float x = fmaf(__uint_as_float(b[i]), 1.f / kLoScale, __uint_as_float(a[i])) * S.alpha[g][k + i];
-        if (away) give[(k + i - (g == 0 ? half : 0)) * kD + d] = x;
-        else if (!joint) {
-          if (k + i < rows) emit(k + i, x);
+        float x = fmaf(__uint_as_float(b[i]), 1.f / kLoScale, __uint_as_float(a[i])) * S.alpha[g][k + i];
+        if (nan_key <= sees + query) x = __uint_as_float(0x7fc00000u);
+        if (k + i < rows) {
+          if (part) *to = x;
+          else *at = f2bf16(x);
         }
-      }
-    }
-  }
-  if (joint) {
-    pair_sync(S, X);
-    const float *take = reinterpret_cast<const float *>(S.p[1 - g]);
-    const int half = NR / 2, from = g == 0 ? 0 : half;
-#pragma unroll 1
-    for (int k = 0; k < half; k += 8) {
-      uint32_t a[8], b[8];
-      tc_ld_32x32b_x8(o_addr + from + k, a);
-      tc_ld_32x32b_x8(o_addr + NR + from + k, b);
-      tc_wait_ld();
-      if (from + k >= rows) continue;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = from + k + i;
-        const float x = fmaf(__uint_as_float(b[i]), 1.f / kLoScale, __uint_as_float(a[i])) * S.alpha[g][r];
-        if (r < rows) emit(r, x + take[(k + i) * kD + d]);
+        to += kD, at += kD;
+        if (++head == group) head = 0, ++query, at += turn_over;
       }
     }
   }
   tc_fence_before();
-  if (part) {
-    // the last CTA of the task to get here joins its parts, in order
+  if (part && rows > 0) {
+    // the last CTA of the task to get here joins its parts
     __threadfence();
-    pair_sync(S, X);
-    if (g == 0 && tid == 0) S.last = atomicAdd(&P.done[I.cta0], 1) == I.cta1 - I.cta0;
-    pair_sync(S, X);
-    if (*(volatile int *)&S.last) {
+    named_bar_sync(1 + g, 128);
+    if (tid == 0) S.last[g] = atomicAdd(&P.done[I.cta0 * kGroups + rg], 1) == I.cta1 - I.cta0;
+    named_bar_sync(1 + g, 128);
+    if (*(volatile int *)&S.last[g]) {
       __threadfence();
-      const size_t stride = (size_t)P.part_rows * (kD + 1);
-      auto slot_of = [&](int c) { return P.part + (size_t)(c == I.cta0 ? 2 * c + 1 : 2 * c) * stride; };
-      for (int r = g * 4 + X.warp; r < I.rows; r += 8) {
-        float top = -INFINITY;
-        for (int c = I.cta0 + lane; c <= I.cta1; c += 32) top = fmaxf(top, slot_of(c)[(size_t)P.part_rows * kD + r]);
-        top = warp_max(top);
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        float sum = 0.f;
-#pragma unroll 4
-        for (int c = I.cta0; c <= I.cta1; ++c) {
-          const float *s = slot_of(c);
-          const float lse = s[(size_t)P.part_rows * kD + r];
-          const float4 x = *reinterpret_cast<const float4 *>(s + (size_t)r * kD + lane * 4);
-          const float w = lse == -INFINITY ? 0.f : ex2_approx(lse - top);
-          sum += w;
-          acc.x += w * x.x, acc.y += w * x.y, acc.z += w * x.z, acc.w += w * x.w;
-        }
-        const float f = sum == 0.f ? 0.f : 1.f / sum;
-        const int row = I.row0 + r, query = row / group;
-        uint2 o = make_uint2((uint32_t)f2bf16(acc.x * f) | (uint32_t)f2bf16(acc.y * f) << 16,
-                             (uint32_t)f2bf16(acc.z * f) | (uint32_t)f2bf16(acc.w * f) << 16);
-        *reinterpret_cast<uint2 *>(B.out + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group +
-                                            (row - query * group)) * kD + lane * 4) = o;
+      join(P, I, rg * kRows, rows, X.warp, lane);
+    }
+  }
+  if (bad) {  // (all warpgroups of the item know the same)
+    uint64_t *bar = I.ng == 4 ? &S.all : &S.pair[I.wg >> 1];
+    for (int i = 0; i < 2; ++i) {
+      if (I.ng == 1) {
+        named_bar_sync(1 + g, 128);
+      } else {
+        uint32_t &uses = I.ng == 4 ? X.alls : X.pairs;
+        arrive_warp(bar, lane);
+        X.ok = wait_inline(bar, uses & 1u, &S.abort) && X.ok;
+        ++uses;
+      }
+      if (i == 0 && rg == 0) {
+        S.nan_key[g][tid] = 0x7fffffff;
+        if (tid == 0) S.bad[g] = 0;
       }
     }
   }
-  // nothing of the item's shared state is read any more
-  if (joint || both || part) pair_sync(S, X);
-  else named_bar_sync(1 + g, 128);
-  if (bad) {
-    if (set == g || g == 0) {
-      S.nan_key[set][tid] = 0x7fffffff;
-      if (tid == 0) S.bad[set] = 0;
-    }
-    if (set == 2) pair_sync(S, X);
-    else named_bar_sync(1 + g, 128);
-  }
+  // state, sums and factors are read, before the next item writes them
+  named_bar_sync(1 + g, 128);
 }
 
 __device__ void softmax_warps(const Params &P, Shared &S, int warp, int lane) {
-  Softmax X{warp >> 2, (int)threadIdx.x & 127, warp & 3, lane, 0, 0, 0, true};
+  Softmax X{warp >> 2, (int)threadIdx.x & 127, warp & 3, lane, 0, 0, 0, 0, true};
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
-    X.ok = wait(&S.item_full[slot], full(n, kSlots), &S.abort) && X.ok;
+    X.ok = wait_inline(&S.item_full[slot], full(n, kSlots), &S.abort) && X.ok;
     if (bar_or(1 + X.g, 128, !X.ok)) return;  // the whole warpgroup
-    const Item I = S.item[slot];
+    const Item &I = S.item[slot];
     if (!I.valid) return;
-    if (I.nr == 64) softmax_item<64>(P, S, X, n, I);
-    else if (I.nr == 32) softmax_item<32>(P, S, X, n, I);
-    else softmax_item<16>(P, S, X, n, I);
+    if (X.g >= I.wg && X.g < I.wg + I.ng) softmax_item(P, S, X, n, I);
+    X.it += I.t1 - I.t0;
     arrive_warp(&S.item_empty[slot], lane);
   }
 }
@@ -1009,20 +1026,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_kernel(const __grid_constan
   extern __shared__ uint8_t raw[];
   Shared &S = *reinterpret_cast<Shared *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (threadIdx.x < 3 * kD) S.nan_key[threadIdx.x / kD][threadIdx.x % kD] = 0x7fffffff;
+  if (threadIdx.x < kGroups * kD) S.nan_key[threadIdx.x / kD][threadIdx.x % kD] = 0x7fffffff;
+  if (threadIdx.x < kGroups) S.bad[threadIdx.x] = 0;
   if (threadIdx.x == 0) {
-    S.bad[0] = S.bad[1] = S.bad[2] = S.abort = S.last = 0;
+    S.abort = 0;
     auto ring = [](uint64_t *b, int n, int count) {
       for (int i = 0; i < n; ++i) mbar_init(&b[i], count);
     };
     ring(S.k_full, kKStages, 1), ring(S.k_empty, kKStages, 1);
     ring(S.v_full, kVStages, 1), ring(S.v_empty, kVStages, 1);
     ring(S.pg_full, kMeta, 1), ring(S.sc_full, kMeta, 1), ring(S.meta_empty, kMeta, 1);
-    ring(S.q_full, 2, kQWarps), ring(S.q_empty, 2, 1);
-    ring(S.s_full, 2, 1), ring(S.s_empty, 2, 4);
-    ring(S.p_full, 2, 4), ring(S.pv_done, 2, 1);
+    ring(S.q_full, kSlots, kQWarps), ring(S.q_empty, 2, 1);
+    ring(S.s_full, kGroups, 1), ring(S.s_empty, kGroups, 4);
+    ring(S.p_full, kGroups, 4), ring(S.pv_done, kGroups, 1);
     ring(S.item_full, kSlots, 1), ring(S.item_empty, kSlots, kItemReaders);
-    ring(&S.pair, 1, 8), ring(S.drain, 2, 1);
+    ring(S.pair, 2, 8), ring(&S.all, 1, kSoftmaxWarps), ring(S.drain, 2, 1);
     fence_mbar_init();
   }
   if (warp == kQkWarp) {
@@ -1032,7 +1050,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_kernel(const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp < 8) {
+  if (warp < kSoftmaxWarps) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRegsSoftmax));
     softmax_warps(P, S, warp, lane);
   } else {
@@ -1150,7 +1168,7 @@ Layout layout(const ipd_attn8_batch *const *bs, int n) {
   W.prefix = 0;
   W.info = up((size_t)(W.reqs + 1) * sizeof(long long));
   W.done = W.info + up((size_t)W.reqs * sizeof(int4));
-  W.part = W.done + up(kMaxCtas * sizeof(int));
+  W.part = W.done + up(kMaxCtas * kGroups * sizeof(int));
   W.total = W.part + up((size_t)2 * kMaxCtas * W.part_rows * (kD + 1) * sizeof(float));
   return W;
 }
