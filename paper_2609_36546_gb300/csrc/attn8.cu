@@ -23,14 +23,15 @@
 // when a weight would leave 2^8, so most tiles need no maximum across threads.  The
 // reference includes V's scale, since it is the product that has to fit e4m3.
 //
-// Work.  All (request, KV head, block of 128 rows, tile) units in one line, cut into
-// equal parts, a CTA each: nothing is claimed, the cut depends on the lengths alone.
+// Work.  All (request, KV head, block of 128 rows, tile) in one line, cut into parts of
+// equal cost, a CTA each: nothing is claimed, the cut depends on the lengths alone.
 // A task cut between CTAs leaves normalised partial rows; the CTA that finishes last
 // joins them in order.
 //
-// Warps: 0-3 and 4-7 softmax (tiles in turn; with more than 64 rows 64 rows of every
-// tile each), 8 loads K, 9 loads V, 10 issues the first product, 11 the second, 12
-// finds the items, page ids and scales, 13-15 split the queries.
+// Warps: 0-15 softmax, four warpgroups that take items in turn (of more than 32 rows
+// two together, of more than 64 four, 32 rows each), 16 loads K, 17 loads V, 18 issues
+// the first product, 19 the second, 20 finds the items, 21 fetches page ids and scales,
+// 22 and 23 split the queries.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cudaTypedefs.h>
@@ -63,14 +64,15 @@ constexpr int kBlockRows = 128;           // rows of a task
 constexpr int kGroups = 4;                // softmax warpgroups
 constexpr int kRows = 32;                 // ... and the rows of one
 constexpr int kKStages = 3, kVStages = 4;
-constexpr int kMeta = 8;                  // tiles whose page ids and scales are at hand
+constexpr int kMeta = 16;                  // tiles whose page ids and scales are at hand
 constexpr int kBatch = 4;                 // ... fetched at once
 constexpr int kSlots = 5;                 // items handed out
 constexpr int kSoftmaxWarps = 4 * kGroups;
 constexpr int kKWarp = kSoftmaxWarps, kVWarp = kKWarp + 1, kQkWarp = kKWarp + 2, kPvWarp = kKWarp + 3,
-              kMetaWarp = kKWarp + 4, kQWarps = 3;
-constexpr int kThreads = 32 * (kSoftmaxWarps + 5 + kQWarps);
-constexpr int kItemReaders = kSoftmaxWarps + 4 + kQWarps;
+              kItemWarp = kKWarp + 4, kPageWarp = kKWarp + 5, kQWarps = 2;
+constexpr int kThreads = 32 * (kSoftmaxWarps + 6 + kQWarps);
+constexpr int kItemReaders = kSoftmaxWarps + 5 + kQWarps;
+constexpr int kQUnits = 8;                // query tiles of 32 rows at hand
 constexpr int kRegsLaunch = 80, kRegsSoftmax = 96, kRegsAux = 48;
 static_assert(32 * kSoftmaxWarps * kRegsSoftmax + 256 * kRegsAux <= kThreads * kRegsLaunch,
               "the register split must fit the registers the block was launched with");
@@ -82,10 +84,13 @@ __host__ __device__ constexpr uint32_t col_s(uint32_t g) { return 32u * g; }
 __host__ __device__ constexpr uint32_t col_o(uint32_t g) { return 128u + 64u * g; }
 __host__ __device__ constexpr uint32_t col_l(uint32_t g) { return 384u + 32u * g; }
 
-constexpr float kBase = 5.f;   // a row's reference is its largest exponent less this
+constexpr float kBase = 4.f;   // a row's reference is its largest exponent less this
 constexpr float kLimit = 8.f;  // weights stay below 2^8 (e4m3 ends at 448)
 constexpr float kLoScale = 16.f;
 constexpr int kFar = 100;      // V scales further apart than 2^100 count as that far
+// What a tile of a task with up to 32, 64 and 128 rows costs, and a task beside its
+// tiles: the line is cut into equal costs.
+constexpr int kCost1 = 4, kCost2 = 5, kCost4 = 9, kItemCost = 6;
 constexpr int kNoPage = 1 << 20;  // in place of an exponent: no such page
 
 struct BatchDev {
@@ -103,7 +108,7 @@ struct Params {
   int req_base[IPD_MAX_BATCHES + 1];
   int n, total_reqs;
   float scale_log2;
-  long long *prefix;  // [total_reqs + 1] units before each request
+  long long *prefix;  // [total_reqs + 1] cost of the requests before each, and the dearest tile's
   int4 *info;         // [total_reqs] length, queries, first row, tiles
   int *done;          // [CTAs][kGroups] parts done of the task that starts in this CTA and goes on, by row group
   float *part;        // [2 CTAs] partial rows: part_rows x 128, then part_rows log-sums
@@ -115,7 +120,10 @@ struct Item {
   int row0, rows;       // first row of the task among the request's, and number
   int nr, ng, wg;       // rows of a warpgroup (16 or 32); its warpgroups (1, 2 or 4) and their first
   int t0, t1;           // tiles
-  int part, cta0, cta1; // partial slot (-1: whole task) and the CTAs of the task
+  int qu;               // first query tile
+  int r, n_pages;       // request of the batch, its pages
+  int part;             // partial slot (-1: the whole task is here)
+  int cta0, ctab, cta1; // the CTAs of the task: cta0, then ctab .. cta1
 };
 
 struct Meta {
@@ -128,13 +136,13 @@ struct Meta {
 struct Shared {
   alignas(1024) uint8_t k[kKStages][kTileBytes];
   alignas(1024) uint8_t v[kVStages][kTileBytes];
-  alignas(1024) uint8_t q[2][2][kBlockRows * kD];      // buffer, term
+  alignas(1024) uint8_t q[2][kQUnits][kRows * kD];     // the two terms of the query tiles
   alignas(1024) uint8_t p[kGroups][kKeys * 2 * kRows]; // a warpgroup's P; at the end, rows on their way
   alignas(16) float4 state[kGroups][kRows / 2];        // a pair of rows: ar, ar', -ref, -ref'
   alignas(16) float alpha[kGroups][kRows];
   alignas(16) float red[kGroups][4][kRows];
   alignas(16) float qscale[kSlots][kBlockRows];
-  float ref[kGroups][kRows], sum[kGroups][kRows];      // what the warpgroups hand each other at an item's end
+  uint32_t over[kGroups][4];                           // rows whose references have to move
   // first key of a span with a NaN in this dim of V, and whether there is one (by an
   // item's first warpgroup)
   int nan_key[kGroups][kD], bad[kGroups];
@@ -144,7 +152,7 @@ struct Shared {
   Item item[kSlots];
   uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
   uint64_t pg_full[kMeta], sc_full[kMeta], meta_empty[kMeta];
-  uint64_t q_full[kSlots], q_empty[2], s_full[kGroups], s_empty[kGroups], p_full[kGroups], pv_done[kGroups];
+  uint64_t q_full[kSlots], q_empty[kQUnits], s_full[kGroups], s_empty[kGroups], p_full[kGroups], pv_done[kGroups];
   uint64_t item_full[kSlots], item_empty[kSlots], pair[2], all, drain[2];
 };
 constexpr int kSharedBytes = (int)sizeof(Shared) + 1024;  // the base is aligned by hand
@@ -206,6 +214,12 @@ IPD_DEVINL void tc_ld_32x32b_x8(uint32_t taddr, uint32_t (&r)[8]) {
                : "r"(taddr)
                : "memory");
 }
+IPD_DEVINL void tc_ld_x1(uint32_t taddr, uint32_t &r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr) : "memory");
+}
+IPD_DEVINL void tc_st_x1(uint32_t taddr, uint32_t r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(r) : "memory");
+}
 IPD_DEVINL u64 mul2(u64 a, u64 b) {
   u64 d;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
@@ -226,34 +240,57 @@ IPD_DEVINL uint32_t half2_mul(uint32_t a, uint32_t b) {
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
+// Four fp16 values as e4m3, and back.
+IPD_DEVINL uint32_t e4m3x4_h(uint32_t h01, uint32_t h23) {
+  uint32_t d;
+  asm("{\n\t.reg .b16 a, b;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 a, %1;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 b, %2;\n\t"
+      "mov.b32 %0, {a, b};\n\t}"
+      : "=r"(d)
+      : "r"(h01), "r"(h23));
+  return d;
+}
+IPD_DEVINL void h_from_e4m3x4(uint32_t v, uint32_t &h01, uint32_t &h23) {
+  asm("{\n\t.reg .b16 a, b;\n\t"
+      "mov.b32 {a, b}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+      : "=r"(h01), "=r"(h23)
+      : "r"(v));
+}
 IPD_DEVINL void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 IPD_DEVINL void grid_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // ---- waits ---------------------------------------------------------------------
 // For a whole warp, with one answer.  Gives up after about a second, or as soon as
-// another warp of the CTA has given up.
-IPD_DEVINL bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort) {
+// another warp of the CTA has given up.  Warps that poll take issue slots from those
+// that work (without a pause they were half of all instructions), so those that run
+// ahead sleep `pause` ns between two looks.
+IPD_DEVINL bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort, uint32_t pause) {
   const long long t0 = clock64();
   bool ok;
 #pragma unroll 1
-  while (!(ok = mbar_try_wait(bar, parity)) && !*abort)
+  while (!(ok = mbar_try_wait(bar, parity)) && !*abort) {
+    if (pause) __nanosleep(pause);
     if (clock64() - t0 > kWaitLimitCycles) {
       ipd_set_error(&g_attn8_err, IPD_DEVERR_WAIT);
       *abort = 1;
     }
+  }
   return __all_sync(0xffffffffu, ok) != 0;
 }
-__device__ __noinline__ bool wait_slow_call(uint64_t *bar, uint32_t parity, volatile int *abort) {
-  return wait_slow(bar, parity, abort);
+__device__ __noinline__ bool wait_slow_call(uint64_t *bar, uint32_t parity, volatile int *abort, uint32_t pause) {
+  return wait_slow(bar, parity, abort, pause);
 }
-IPD_DEVINL bool wait(uint64_t *bar, uint32_t parity, volatile int *abort) {
+IPD_DEVINL bool wait(uint64_t *bar, uint32_t parity, volatile int *abort, uint32_t pause = 200) {
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return wait_slow_call(bar, parity, abort);
+  return wait_slow_call(bar, parity, abort, pause);
 }
 // ... without a call, where many registers are live
 IPD_DEVINL bool wait_inline(uint64_t *bar, uint32_t parity, volatile int *abort) {
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return wait_slow(bar, parity, abort);
+  return wait_slow(bar, parity, abort, 0);
 }
 // One lane of a converged warp issues; every other value is the whole warp's, so that
 // operands stay in uniform registers (issued from a branch of one lane, a product
@@ -284,13 +321,16 @@ IPD_DEVINL int batch_of(const Params &P, int g) {
   return b;
 }
 
-// Checks the requests and counts their units; one block.
+IPD_DEVINL int tile_cost(int rows) { return rows > 64 ? kCost4 : rows > 32 ? kCost2 : kCost1; }
+
+// Checks the requests and adds up their costs; one block.
 __global__ void __launch_bounds__(1024) attn8_plan_kernel(const __grid_constant__ Params P, int ctas) {
   __shared__ long long warp_units[32];
   grid_launch();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   for (int i = tid; i < ctas * kGroups; i += blockDim.x) P.done[i] = 0;
   long long carry = 0;
+  int dearest = 1;
   for (int base = 0; base < P.total_reqs; base += blockDim.x) {
     const int g = base + tid;
     long long units = 0;
@@ -306,7 +346,11 @@ __global__ void __launch_bounds__(1024) attn8_plan_kernel(const __grid_constant_
         ipd_set_error(&g_attn8_err, IPD_DEVERR_SEQ_LEN);
       } else if (n > 0) {
         tiles = (L + kKeys - 1) / kKeys;
-        units = (long long)tiles * B.hkv * ((n * B.group + kBlockRows - 1) / kBlockRows);
+        const int rows = n * B.group, blocks = (rows + kBlockRows - 1) / kBlockRows;
+        dearest = max(dearest, tile_cost(min(rows, kBlockRows)));
+        units = (long long)B.hkv *
+                ((blocks - 1) * (kItemCost + (long long)tiles * tile_cost(min(rows, kBlockRows))) + kItemCost +
+                 (long long)tiles * tile_cost(rows - (blocks - 1) * kBlockRows));
       }
       P.info[g] = make_int4(L, n, c0, tiles);
     }
@@ -327,107 +371,174 @@ __global__ void __launch_bounds__(1024) attn8_plan_kernel(const __grid_constant_
     carry += all;
     __syncthreads();
   }
-  if (tid == 0) P.prefix[P.total_reqs] = carry;
+  dearest = __reduce_max_sync(0xffffffffu, dearest);
+  if (lane == 0) warp_units[warp] = dearest;
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < warps; ++w) warp_units[0] = max(warp_units[0], warp_units[w]);
+    P.prefix[P.total_reqs] = carry, P.prefix[P.total_reqs + 1] = warp_units[0];
+  }
 }
 
-// ---- items, page ids and scales (one warp) ----------------------------------------
-__device__ void meta_warp(const Params &P, Shared &S, int lane) {
+// ---- items (one warp) ----------------------------------------------------------------
+// A task's place in the line: its first tile begins at 0, tile t at kItemCost + t w, and
+// it ends at kItemCost + tiles w, w the cost of one of its tiles.
+// the first tile that begins at `off` or later
+IPD_DEVINL int tile_at(long long off, int w, int tiles) {
+  if (off <= 0) return 0;
+  const long long t = (off - kItemCost + w - 1) / w;
+  return (int)max(1LL, min((long long)tiles, t));
+}
+
+__device__ void item_warp(const Params &P, Shared &S, int lane) {
   grid_wait();  // what the plan wrote
   const long long W = P.prefix[P.total_reqs];
-  const long long C = W < (long long)gridDim.x ? W : gridDim.x;
-  uint32_t n = 0, it = 0, turn = 0;
-  long long pos = 0, hi = 0;
+  // (a part is no shorter than a tile, so that none between a task's ends has no tile)
+  const long long C = max(1LL, min((long long)gridDim.x, W / P.prefix[P.total_reqs + 1]));
+  uint32_t n = 0, turn = 0, unit = 0;
+  const long long lo = blockIdx.x < C ? blockIdx.x * W / C : W, hi = blockIdx.x < C ? (blockIdx.x + 1) * W / C : W;
   int g = 0;
-  if (blockIdx.x < C) {
-    pos = blockIdx.x * W / C, hi = (blockIdx.x + 1) * W / C;
-    // the last request with prefix <= pos: 32 probes a round
-    int lo = 0, end = P.total_reqs;  // prefix[lo] <= pos < prefix[end]
-    while (end - lo > 1) {
-      const int step = (end - lo + 31) / 32;
-      const int at = lo + lane * step;
-      const uint32_t in = __ballot_sync(0xffffffffu, at < end && P.prefix[at] <= pos);
+  if (lo < hi) {
+    // the last request that begins at lo or before: 32 probes a round
+    int from = 0, end = P.total_reqs;  // prefix[from] <= lo < prefix[end]
+    while (end - from > 1) {
+      const int step = (end - from + 31) / 32;
+      const int at = from + lane * step;
+      const uint32_t in = __ballot_sync(0xffffffffu, at < end && P.prefix[at] <= lo);
       const int k = 31 - __clz(in);
-      lo += k * step;
-      end = min(end, lo + step);
+      from += k * step;
+      end = min(end, from + step);
     }
-    g = lo;
+    g = from;
   }
+  long long pos = lo;  // where the next task to look at begins, or this CTA's part
   while (pos < hi) {
-    const int b = batch_of(P, g), r = g - P.req_base[b];
-    const BatchDev &B = P.b[b];
     const long long first = P.prefix[g], next = P.prefix[g + 1];
-    if (next == first) {  // nothing to do for this request
+    if (next <= pos) {  // nothing to do for this request
       ++g;
       continue;
     }
+    const int b = batch_of(P, g);
+    const int group = P.b[b].group;
     const int4 info = P.info[g];
-    const int L = info.x, tiles = info.w, rows_all = info.y * B.group;
-    const int blocks = (rows_all + kBlockRows - 1) / kBlockRows;
-    const long long off = pos - first;
-    const int task = (int)(off / tiles), t0 = (int)(off - (long long)task * tiles);
-    const int t1 = (int)min((long long)tiles, t0 + (hi - pos));
-    const int h = task / blocks, row0 = (task - h * blocks) * kBlockRows;
-    const int slot = n % kSlots;
-    if (!wait(&S.item_empty[slot], free_(n, kSlots), &S.abort)) return;
-    if (lane == 0) {
-      Item &I = S.item[slot];
-      I.valid = 1, I.b = b, I.c0 = info.z, I.n = info.y, I.L = L, I.h = h;
-      I.row0 = row0, I.rows = min(kBlockRows, rows_all - row0);
-      I.nr = I.rows > 16 ? 32 : 16;
-      I.ng = I.rows > 64 ? 4 : I.rows > 32 ? 2 : 1;
-      // the warpgroups take items in turn, those of two or four together
-      I.wg = (int)((turn + I.ng - 1) & (uint32_t)(kGroups - I.ng));
-      I.t0 = t0, I.t1 = t1;
-      I.part = t1 - t0 == tiles ? -1 : t0 > 0 ? 2 * (int)blockIdx.x : 2 * (int)blockIdx.x + 1;
-      // CTA i begins at unit floor(i W / C): the last one that begins at p or before
-      const long long p0 = pos - t0, p1 = p0 + tiles - 1;
-      I.cta0 = (int)(((p0 + 1) * C - 1) / W), I.cta1 = (int)(((p1 + 1) * C - 1) / W);
-      mbar_arrive(&S.item_full[slot]);
-    }
-    {
-      const int rows = min(kBlockRows, rows_all - row0), ng = rows > 64 ? 4 : rows > 32 ? 2 : 1;
-      turn = ((turn + ng - 1) & (uint32_t)(kGroups - ng)) + ng;
-    }
-    const int *pages = B.page_table + (size_t)r * B.max_pages;
-    const int n_pages = (L + kPage - 1) / kPage;
-    int id = t0 * kPages + lane < n_pages ? pages[t0 * kPages + lane] : -1;
-    for (int t = t0; t < t1; t += kBatch) {
-      const int page = t * kPages + lane, mine = lane / kPages;
-      const bool inside = page < n_pages && t + mine < t1;
-      const bool ok = inside && id >= 0 && id < B.num_pages;
-      if (inside && !ok) ipd_set_error(&g_attn8_err, IPD_DEVERR_PAGE_ID);
-      const size_t cell = (size_t)(ok ? id : 0) * B.hkv + h;
-      const uint32_t kb = ok ? B.ks[cell] : 127u, vb = ok ? B.vs[cell] : 127u;
-      const int now = min(kBatch, t1 - t);
-      // the slots of the batch: free in order
-      for (int i = 0; i < now; ++i) {
-        const uint32_t m = (it + i) % kMeta;
-        if (!wait(&S.meta_empty[m], free_(it + i, kMeta), &S.abort)) return;
-        const uint32_t gap = __ballot_sync(0xffffffffu, mine == i && inside && !ok);
-        if (mine == i) S.meta[m].y[lane % kPages] = ok ? (int)cell * kPage : B.rows_end;
-        if (lane == 0) S.meta[m].gap = gap != 0;
-        arrive_warp(&S.pg_full[m], lane);
-      }
-      id = page + 32 < n_pages ? pages[page + 32] : -1;  // the next batch's
-      for (int i = 0; i < now; ++i) {
-        const uint32_t m = (it + i) % kMeta;
-        if (mine == i) {
-          S.meta[m].ck[lane % kPages] = e8m0(kb) * P.scale_log2;
-          S.meta[m].ev[lane % kPages] = ok ? (int)vb - 127 : kNoPage;
+    const int L = info.x, tiles = info.w, rows_all = info.y * group;
+    // (a request's blocks are alike but for the last, which may have fewer rows)
+    const int blocks = (rows_all + kBlockRows - 1) / kBlockRows, last_rows = rows_all - (blocks - 1) * kBlockRows;
+    const int w_full = tile_cost(min(rows_all, kBlockRows)), w_last = tile_cost(last_rows);
+    const long long c_full = kItemCost + (long long)tiles * w_full, c_last = kItemCost + (long long)tiles * w_last;
+    const long long c_head = (blocks - 1) * c_full + c_last;
+    int h = (int)((pos - first) / c_head);
+    long long in_head = pos - first - h * c_head;
+    int block = (int)min((long long)blocks - 1, in_head / c_full);
+    long long at = first + h * c_head + block * c_full;  // the task's beginning
+    while (at < hi && at < next) {
+      const int w = block == blocks - 1 ? w_last : w_full;
+      const long long cost = block == blocks - 1 ? c_last : c_full;
+      const int t0 = tile_at(lo - at, w, tiles), t1 = hi - at >= cost ? tiles : tile_at(hi - at, w, tiles);
+      if (t0 < t1) {
+        const int slot = n % kSlots;
+        if (!wait(&S.item_empty[slot], free_(n, kSlots), &S.abort)) return;
+        const int row0 = block * kBlockRows, rows = min(kBlockRows, rows_all - row0);
+        const int ng = rows > 64 ? 4 : rows > 32 ? 2 : 1;
+        // the warpgroups take items in turn, those of two or four together, and so do
+        // the query tiles
+        const int wg = (int)((turn + ng - 1) & (uint32_t)(kGroups - ng));
+        const int qu = (int)((unit + ng - 1) & (uint32_t)(kQUnits - ng));
+        turn = wg + ng, unit = qu + ng;
+        if (lane == 0) {
+          Item &I = S.item[slot];
+          I.valid = 1, I.b = b, I.c0 = info.z, I.n = info.y, I.L = L, I.h = h;
+          I.row0 = row0, I.rows = rows, I.nr = rows > 16 ? 32 : 16, I.ng = ng, I.wg = wg, I.qu = qu;
+          I.t0 = t0, I.t1 = t1;
+          I.r = g - P.req_base[b], I.n_pages = (L + kPage - 1) / kPage;
+          I.part = t1 - t0 == tiles ? -1 : t0 > 0 ? 2 * (int)blockIdx.x : 2 * (int)blockIdx.x + 1;
+          if (I.part >= 0) {
+            // CTA i begins at floor(i W / C): the last one that begins at p or before
+            const auto cta = [&](int t) {
+              const long long p = at + (t > 0 ? kItemCost + (long long)t * w : 0);
+              return (int)(((p + 1) * C - 1) / W);
+            };
+            I.cta0 = cta(0), I.ctab = max(I.cta0 + 1, cta(1)), I.cta1 = cta(tiles - 1);
+          }
+          mbar_arrive(&S.item_full[slot]);
         }
-        arrive_warp(&S.sc_full[m], lane);
+        __syncwarp();
+        ++n;
       }
-      it += now;
+      at += cost;
+      if (++block == blocks) block = 0, ++h;
     }
-    ++n;
-    pos += t1 - t0;
-    if (pos == next) ++g;
+    pos = min(hi, next);
   }
   const int slot = n % kSlots;
   if (!wait(&S.item_empty[slot], free_(n, kSlots), &S.abort)) return;
   if (lane == 0) {
     S.item[slot].valid = 0;
     mbar_arrive(&S.item_full[slot]);
+  }
+}
+
+// ---- page ids and scales (one warp) ---------------------------------------------------
+// Batches of up to four tiles, a lane a page.  While a batch's scales are under way, so are
+// the next one's page ids, of this item or the next.
+__device__ void page_warp(const Params &P, Shared &S, int lane) {
+  const int mine = lane / kPages;
+  uint32_t n = 0, it = 0;  // items begun; tiles handed out
+  // the batch whose ids are under way, and what is known of it
+  int slot = 0, t = 0, t1 = 0, id = -1, left = 0;
+  const auto fetch = [&]() {  // ids of the next batch; false: there is none
+    if (t >= t1) {
+      slot = n % kSlots;
+      if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) return false;
+      const Item &I = S.item[slot];
+      if (!I.valid) return false;
+      ++n;
+      t = I.t0, t1 = I.t1;
+    }
+    const Item &I = S.item[slot];
+    const int page = t * kPages + lane;
+    left = min(kBatch, t1 - t);
+    id = -1;
+    if (page < I.n_pages && mine < left) {
+      const BatchDev &B = P.b[I.b];
+      id = B.page_table[(size_t)I.r * B.max_pages + page];
+      if (id < 0 || id >= B.num_pages) {
+        ipd_set_error(&g_attn8_err, IPD_DEVERR_PAGE_ID);
+        id = -2;
+      }
+    }
+    return true;
+  };
+  bool more = fetch();
+  while (more) {
+    const Item &I = S.item[slot];
+    const BatchDev &B = P.b[I.b];
+    const int now = left;
+    const bool last = t + now >= t1;
+    const uint32_t used = slot;
+    const bool ok = id >= 0;
+    const size_t cell = (size_t)(ok ? id : 0) * B.hkv + I.h;
+    const uint32_t kb = ok ? B.ks[cell] : 127u, vb = ok ? B.vs[cell] : 127u;
+    for (int i = 0; i < now; ++i) {
+      const uint32_t m = (it + i) % kMeta;
+      if (!wait(&S.meta_empty[m], free_(it + i, kMeta), &S.abort)) return;
+      const uint32_t gap = __ballot_sync(0xffffffffu, mine == i && id == -2);
+      if (mine == i) S.meta[m].y[lane % kPages] = ok ? (int)cell * kPage : B.rows_end;
+      if (lane == 0) S.meta[m].gap = gap != 0;
+      arrive_warp(&S.pg_full[m], lane);
+    }
+    t += now;
+    more = fetch();
+    for (int i = 0; i < now; ++i) {
+      const uint32_t m = (it + i) % kMeta;
+      if (mine == i) {
+        S.meta[m].ck[lane % kPages] = e8m0(kb) * P.scale_log2;
+        S.meta[m].ev[lane % kPages] = ok ? (int)vb - 127 : kNoPage;
+      }
+      arrive_warp(&S.sc_full[m], lane);
+    }
+    it += now;
+    if (last) arrive_warp(&S.item_empty[used], lane);
   }
 }
 
@@ -486,7 +597,7 @@ __device__ void qk_warp(Shared &S, int lane) {
   const uint32_t tmem = (uint32_t)uniform((int)S.tmem);
   const uint64_t k0 = sdesc((uint32_t)uniform((int)smem_u32(S.k[0])), 128),
                  q0 = sdesc((uint32_t)uniform((int)smem_u32(S.q[0][0])), 128);
-  constexpr uint64_t kTerm = kBlockRows * kD >> 4;  // of descriptors: from a term of q to the next
+  constexpr uint64_t kUnit = kRows * kD >> 4, kTerm = kQUnits * kUnit;  // in descriptors
   uint32_t it = 0, uses = 0;  // (a bit a warpgroup: parity of its uses)
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
@@ -494,30 +605,32 @@ __device__ void qk_warp(Shared &S, int lane) {
     const Item &I = S.item[slot];
     if (!uniform(I.valid)) return;
     const int tiles = uniform(I.t1 - I.t0), ng = uniform(I.ng);
-    const uint32_t idesc = idesc_f8(uniform(I.nr) * ng, 0), buf = n & 1;
+    const uint32_t idesc = idesc_f8(uniform(I.nr) * ng, 0), qu = (uint32_t)uniform(I.qu);
     const uint32_t g0 = (uint32_t)uniform(I.wg);
     bool ok = wait(&S.q_full[slot], full(n, kSlots), &S.abort);
-    const uint64_t q = q0 + (uint64_t)buf * 2 * kTerm;
+    const uint64_t q = q0 + qu * kUnit;
     for (int t = 0; ok && t < tiles; ++t, ++it) {
       const uint32_t s = it % kKStages;
-      ok = wait(&S.k_full[s], full(it, kKStages), &S.abort);
-      for (int i = 0; ok && i < ng; ++i) ok = wait(&S.s_empty[g0 + i], (uses >> (g0 + i) & 1u) ^ 1u, &S.abort);
+      ok = wait(&S.k_full[s], full(it, kKStages), &S.abort, 40);
+      for (int i = 0; ok && i < ng; ++i) ok = wait(&S.s_empty[g0 + i], (uses >> (g0 + i) & 1u) ^ 1u, &S.abort, 40);
       if (!ok) break;
       uses ^= ((1u << ng) - 1u) << g0;
       tc_fence_after();
       const uint64_t k = k0 + (uint64_t)(s * (kTileBytes >> 4));
       const uint32_t d = tmem + col_s(g0);
       if (elect_one()) {
-#pragma unroll 1
+#pragma unroll
         for (int kk = 0; kk < kD / 32; ++kk) {
           tc_mma_f8(d, k + 2 * kk, q + 2 * kk, idesc, kk != 0);
           tc_mma_f8(d, k + 2 * kk, q + kTerm + 2 * kk, idesc, 1);
         }
+#pragma unroll 1
+        for (int i = 0; i < ng; ++i) tc_commit(&S.s_full[g0 + i]);
+        tc_commit(&S.k_empty[s]);
       }
       __syncwarp();
-      for (int i = 0; i < ng; ++i) commit(&S.s_full[g0 + i]);
-      commit(&S.k_empty[s]);
-      if (t == tiles - 1) commit(&S.q_empty[buf]);
+      if (t == tiles - 1)
+        for (int i = 0; i < ng; ++i) commit(&S.q_empty[qu + i]);
     }
     if (!ok) break;
     arrive_warp(&S.item_empty[slot], lane);
@@ -542,16 +655,16 @@ __device__ void pv_warp(Shared &S, int lane) {
     bool ok = true;
     for (int t = 0; t < tiles; ++t, ++it) {
       const uint32_t s = it % kVStages;
-      ok = wait(&S.v_full[s], full(it, kVStages), &S.abort);
+      ok = wait(&S.v_full[s], full(it, kVStages), &S.abort, 40);
       const uint64_t v = v0 + (uint64_t)(s * (kTileBytes >> 4));
       for (int i = 0; ok && i < ng; ++i) {
         const uint32_t g = g0 + i;
-        ok = wait(&S.p_full[g], uses >> g & 1u, &S.abort);
+        ok = wait(&S.p_full[g], uses >> g & 1u, &S.abort, 40);
         if (!ok) break;
         tc_fence_after();
         const uint64_t p = p0 + (uint64_t)(g * (uint32_t)(sizeof(S.p[0]) >> 4));
         if (elect_one()) {
-#pragma unroll 1
+#pragma unroll
           for (int kk = 0; kk < kKeys / 32; ++kk)
             tc_mma_f8(tmem + col_o(g), v + (uint64_t)(kk * 32 * kD >> 4), p + kk * step, idesc, t != 0 || kk != 0);
           tc_commit(&S.pv_done[g]);
@@ -577,13 +690,16 @@ __device__ void pv_warp(Shared &S, int lane) {
 __device__ void query_warp(const Params &P, Shared &S, int w, int lane) {
   constexpr int kAhead = 4;  // pairs of rows loaded ahead
   const int half = lane >> 4, part = lane & 15;
+  uint32_t uses = 0;  // (a bit a query tile: parity of its uses)
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
     if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) return;
     const Item &I = S.item[slot];
     if (!I.valid) return;
-    const uint32_t buf = n & 1;
-    if (!wait(&S.q_empty[buf], free_(n, 2), &S.abort)) return;
+    const int qu = I.qu;
+    for (int i = 0; i < I.ng; ++i)
+      if (!wait(&S.q_empty[qu + i], (uses >> (qu + i) & 1u) ^ 1u, &S.abort)) return;
+    uses ^= ((1u << I.ng) - 1u) << qu;
     const BatchDev &B = P.b[I.b];
     const int all = I.nr * I.ng, group = B.group;
     const auto fetch = [&](int r) {
@@ -625,8 +741,8 @@ __device__ void query_warp(const Params &P, Shared &S, int w, int lane) {
         lo[k] = e4m3x2(v[0] - back[0], v[1] - back[1]) | e4m3x2(v[2] - back[2], v[3] - back[3]) << 16;
       }
       const int at = r * kD + (((part >> 1) ^ (r & 7)) << 4) + (part & 1) * 8;
-      *reinterpret_cast<uint2 *>(&S.q[buf][0][at]) = make_uint2(hi[0], hi[1]);
-      *reinterpret_cast<uint2 *>(&S.q[buf][1][at]) = make_uint2(lo[0], lo[1]);
+      *reinterpret_cast<uint2 *>(S.q[0][qu] + at) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint2 *>(S.q[1][qu] + at) = make_uint2(lo[0], lo[1]);
       if (part == 0) S.qscale[slot][r] = E == 255 ? __uint_as_float(0x7fc00000u) : none ? 0.f : pow2i(e);
     }
     fence_proxy_async_smem();
@@ -686,71 +802,105 @@ IPD_DEVINL void mend(Shared &S, int set, uint8_t *v, int key_in_tile, int key, i
   if (wrote) fence_proxy_async_smem();
 }
 
-// Exponents of the rows at a thread's key, against their references.
+// Exponents of the rows (in pairs) at a thread's key, against their references.
 template <int NR>
-IPD_DEVINL void exponents(const uint32_t (&s)[NR], const float4 *state, float ck, float (&y)[NR]) {
+IPD_DEVINL void exponents(const uint32_t (&s)[NR], const float4 *state, float ck, u64 (&y)[NR / 2]) {
   const u64 ck2 = f2_pack(ck, ck);
 #pragma unroll
   for (int i = 0; i < NR; i += 2) {
     const float4 st = state[i / 2];
-    f2_unpack(f2_fma(mul2(f2_pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), ck2), f2_pack(st.x, st.y),
-                     f2_pack(st.z, st.w)), y[i], y[i + 1]);
+    y[i / 2] = f2_fma(mul2(f2_pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), ck2), f2_pack(st.x, st.y),
+                      f2_pack(st.z, st.w));
   }
 }
 
 IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[16]) { tc_ld_32x32b_x16(taddr, r); }
 IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[32]) { tc_ld_32x32b_x32(taddr, r); }
 
-// The rows' references move to their largest exponent so far, less kBase; what has
-// been summed moves with them.
+// An item's first references: the rows' largest exponents in its first tile, less kBase.
 template <int NR>
-IPD_DEVINL void move_references(Shared &S, const Softmax &X, float (&y)[NR], float de, bool first, uint32_t o_addr,
-                                uint32_t l_addr) {
+IPD_DEVINL void first_references(Shared &S, const Softmax &X, u64 (&y)[NR / 2], float de, uint32_t l_addr) {
   const int g = X.g, tid = X.tid, lane = X.lane;
 #pragma unroll
   for (int c = 0; c < NR; c += 16) {
     float z[16];
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      const float4 st = S.state[g][(c + i) / 2];
-      z[i] = y[c + i] - st.z + de;
-      z[i + 1] = y[c + i + 1] - st.w + de;
-    }
+    for (int i = 0; i < 16; i += 2) f2_unpack(f2_add(y[(c + i) / 2], f2_pack(de, de)), z[i], z[i + 1]);
     const float x = column_reduce(z, lane, [](float a, float b) { return fmaxf(a, b); });
     if (!(lane & 1)) S.red[g][X.warp][c + (lane >> 1)] = x;
   }
   named_bar_sync(1 + g, 128);
   if (tid < NR) {
-    const float was = S.ref[g][tid];
-    const float now = fmaxf(fmax3(S.red[g][0][tid], S.red[g][1][tid], S.red[g][2][tid]), fmaxf(S.red[g][3][tid], was));
-    float *st = reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1);
-    // (a row that has seen nothing, or NaN alone, stays at 0)
-    const float old = st[2], ref = now == -INFINITY || now == INFINITY ? -old : now - kBase;
-    S.ref[g][tid] = now;
-    st[2] = -ref;
-    S.alpha[g][tid] = was == -INFINITY ? 0.f : ex2_approx(-old - ref);
-    S.red[g][0][tid] = -old - ref;  // what the exponents move by
+    const float now = fmaxf(fmax3(S.red[g][0][tid], S.red[g][1][tid], S.red[g][2][tid]), S.red[g][3][tid]);
+    // (a row that has seen nothing, NaN alone, or more than fp32 holds stays at 0)
+    const float ref = now == -INFINITY || now == INFINITY ? 0.f : now - kBase;
+    (reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1))[2] = -ref;
+    S.alpha[g][tid] = -ref;
   }
   named_bar_sync(1 + g, 128);
 #pragma unroll
-  for (int i = 0; i < NR; ++i) y[i] += S.red[g][0][i];
+  for (int i = 0; i < NR; i += 2) y[i / 2] = f2_add(y[i / 2], *reinterpret_cast<const u64 *>(&S.alpha[g][i]));
+  uint32_t zero[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) zero[i] = 0u;
 #pragma unroll 1
-  for (int c = first ? 2 * NR : 0; c < 3 * NR; c += 16) {  // O's halves, and the sums
-    const uint32_t at = c < 2 * NR ? o_addr + c : l_addr + (c - 2 * NR);
-    uint32_t o[16];
-    if (first) {
+  for (int c = 0; c < NR; c += 16) tc_st_32x32b_x16(l_addr + c, zero);
+  tc_wait_st();
+}
+
+// Rows whose weights would leave kLimit get new references; O and the sums of just those
+// are rescaled, a TMEM column each.
+template <int NR>
+IPD_DEVINL void move_references(Shared &S, const Softmax &X, u64 (&y)[NR / 2], float de, uint32_t o_addr, uint32_t l_addr) {
+  const int g = X.g, tid = X.tid, lane = X.lane;
+  uint32_t over = 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[i] = 0u;
-    } else {
-      tc_ld_32x32b_x16(at, o);
-      tc_wait_ld();
+  for (int i = 0; i < NR; i += 2) {
+    float y0, y1;
+    f2_unpack(y[i / 2], y0, y1);
+    over |= (y0 + de > kLimit ? 1u << i : 0u) | (y1 + de > kLimit ? 2u << i : 0u);
+  }
+  over = __reduce_or_sync(0xffffffffu, over);
+  if (lane == 0) S.over[g][X.warp] = over;
+  named_bar_sync(1 + g, 128);
+  over = S.over[g][0] | S.over[g][1] | S.over[g][2] | S.over[g][3];
+  // their largest exponents among the tile's keys
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * S.alpha[g][(c + i) & (NR - 1)]);
+  for (int c = 0; c < NR; c += 16) {
+    if ((over >> c & 0xffffu) == 0) continue;
+    float z[16];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) f2_unpack(f2_add(y[(c + i) / 2], f2_pack(de, de)), z[i], z[i + 1]);
+    const float x = column_reduce(z, lane, [](float a, float b) { return fmaxf(a, b); });
+    if (!(lane & 1)) S.red[g][X.warp][c + (lane >> 1)] = x;
+  }
+  named_bar_sync(1 + g, 128);
+  if (tid < NR) {
+    float by = 0.f;  // what the reference rises by
+    if (over >> tid & 1u) {
+      by = fmaxf(fmax3(S.red[g][0][tid], S.red[g][1][tid], S.red[g][2][tid]), S.red[g][3][tid]) - kBase;
+      if (!(by < INFINITY)) by = 0.f;
+      (reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1))[2] -= by;
     }
-    tc_st_32x32b_x16(at, o);
+    S.alpha[g][tid] = -by;
+  }
+  named_bar_sync(1 + g, 128);
+#pragma unroll
+  for (int i = 0; i < NR; i += 2) y[i / 2] = f2_add(y[i / 2], *reinterpret_cast<const u64 *>(&S.alpha[g][i]));
+#pragma unroll 1
+  for (; over; over &= over - 1) {
+    const int r = __ffs(over) - 1;
+    const float f = ex2_approx(S.alpha[g][r]);
+    uint32_t a, b, l;
+    tc_ld_x1(o_addr + r, a);
+    tc_ld_x1(o_addr + NR + r, b);
+    tc_ld_x1(l_addr + r, l);
+    tc_wait_ld();
+    tc_st_x1(o_addr + r, __float_as_uint(__uint_as_float(a) * f));
+    tc_st_x1(o_addr + NR + r, __float_as_uint(__uint_as_float(b) * f));
+    tc_st_x1(l_addr + r, __float_as_uint(__uint_as_float(l) * f));
   }
   tc_wait_st();
-  named_bar_sync(1 + g, 128);  // red and alpha are read
 }
 
 // The weights of a warpgroup's rows for its tiles of an item.  A wait that gives up
@@ -796,7 +946,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
     const float fk = ev == 128 && hidden < NR ? __uint_as_float(0x7fc00000u) : pow2i(de);
     X.ok = wait_inline(&S.s_full[g], full(X.tiles, 1), &S.abort) && X.ok;
     tc_fence_after();
-    float y[NR];
+    u64 y[NR / 2];
     {
       uint32_t s[NR];
       load_scores(s_addr, s);
@@ -806,18 +956,29 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
     tc_fence_before();
     arrive_warp(&S.s_empty[g], lane);
     if (hides) {
+      asm volatile("" ::: "memory");  // (a branch, not 32 predicates)
 #pragma unroll
-      for (int i = 0; i < NR; ++i)
-        if (i < hidden) y[i] = -INFINITY;
+      for (int i = 0; i < NR; i += 2) {
+        float y0, y1;
+        f2_unpack(y[i / 2], y0, y1);
+        y[i / 2] = f2_pack(i < hidden ? -INFINITY : y0, i + 1 < hidden ? -INFINITY : y1);
+      }
     }
     float top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < NR; i += 2) top = fmax3(top, y[i], y[i + 1]);
+    for (int i = 0; i < NR / 2; ++i) {
+      float y0, y1;
+      f2_unpack(y[i], y0, y1);
+      top = fmax3(top, y0, y1);
+    }
     const bool move = bar_or(1 + g, 128, first || top + (float)de > kLimit);
     // P's buffer is free, and O at rest, once this warpgroup's product before is complete
     if (X.tiles > 0) X.ok = wait_inline(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort) && X.ok;
     tc_fence_after();
-    if (move) move_references<NR>(S, X, y, (float)de, first, o_addr, l_addr);
+    if (move) {
+      if (first) first_references<NR>(S, X, y, (float)de, l_addr);
+      else move_references<NR>(S, X, y, (float)de, o_addr, l_addr);
+    }
     const u64 fk2 = f2_pack(fk, fk);
     const uint32_t lo16 = half2_of(kLoScale, kLoScale);
 #pragma unroll
@@ -825,28 +986,21 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
       uint32_t l[16];
       tc_ld_32x32b_x16(l_addr + c, l);
       uint32_t hi[4], lo[4];
-      float p[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) p[i] = ex2_approx(y[c + i]);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        uint32_t h[2], e[2];
+        uint32_t h[2], b[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const int i = q * 4 + k * 2;
-          float w0, w1;
-          f2_unpack(mul2(f2_pack(p[i], p[i + 1]), fk2), w0, w1);
-          if (hides) {  // (a NaN scale reaches no hidden row)
-            if (c + i < hidden) w0 = 0.f;
-            if (c + i + 1 < hidden) w1 = 0.f;
-          }
-          h[k] = half2_of(w0, w1);
-          e[k] = e4m3x2_h2(h[k]);
+          u64 &p = y[c / 2 + q * 2 + k];
+          float p0, p1;
+          f2_unpack(p, p0, p1);
+          p = f2_pack(ex2_approx(p0), ex2_approx(p1));
+          f2_unpack(mul2(p, fk2), p0, p1);
+          h[k] = half2_of(p0, p1);
         }
-        hi[q] = e[0] | e[1] << 16;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) e[k] = e4m3x2_h2(half2_mul(half2_sub(h[k], h2_from_e4m3x2(e[k])), lo16));
-        lo[q] = e[0] | e[1] << 16;
+        hi[q] = e4m3x4_h(h[0], h[1]);
+        h_from_e4m3x4(hi[q], b[0], b[1]);
+        lo[q] = e4m3x4_h(half2_mul(half2_sub(h[0], b[0]), lo16), half2_mul(half2_sub(h[1], b[1]), lo16));
       }
       *reinterpret_cast<uint4 *>(prow + (((c / 16) ^ turn) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
       *reinterpret_cast<uint4 *>(prow + ((((NR + c) / 16) ^ turn) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
@@ -854,10 +1008,17 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
         float l0, l1;
-        f2_unpack(f2_add(f2_pack(__uint_as_float(l[i]), __uint_as_float(l[i + 1])), f2_pack(p[i], p[i + 1])), l0, l1);
+        f2_unpack(f2_add(f2_pack(__uint_as_float(l[i]), __uint_as_float(l[i + 1])), y[(c + i) / 2]), l0, l1);
         l[i] = __float_as_uint(l0), l[i + 1] = __float_as_uint(l1);
       }
       tc_st_32x32b_x16(l_addr + c, l);
+    }
+    if (ev == 128 && hidden > 0 && hidden < NR) {
+      // a NaN scale reaches no row that does not see the key
+#pragma unroll 1
+      for (int i = 0; i < hidden; ++i)
+#pragma unroll 1
+        for (int k = i; k < 2 * NR; k += NR) prow[(((k >> 4) ^ turn) << 4) + (k & 15)] = 0;
     }
     // (the product takes the first warpgroup's rows before the others')
     if (key0 + kKeys > masked && g == I.wg) {
@@ -884,13 +1045,14 @@ IPD_DEVINL void join(const Params &P, const Item &I, int r0, int rows, int warp,
   for (int r = r0 + warp; r < r0 + rows; r += 4) {
     float top = -INFINITY;
 #pragma unroll 1
-    for (int c = I.cta0 + lane; c <= I.cta1; c += 32) top = fmaxf(top, slot_of(c)[(size_t)P.part_rows * kD + r]);
+    for (int c = I.ctab + lane; c <= I.cta1; c += 32) top = fmaxf(top, slot_of(c)[(size_t)P.part_rows * kD + r]);
+    top = fmaxf(top, slot_of(I.cta0)[(size_t)P.part_rows * kD + r]);
     top = warp_max(top);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
 #pragma unroll 4
-    for (int c = I.cta0; c <= I.cta1; ++c) {
-      const float *s = slot_of(c);
+    for (int i = I.ctab - 1; i <= I.cta1; ++i) {
+      const float *s = slot_of(i < I.ctab ? I.cta0 : i);
       const float lse = s[(size_t)P.part_rows * kD + r];
       const float4 x = *reinterpret_cast<const float4 *>(s + (size_t)r * kD + lane * 4);
       const float w = lse == -INFINITY ? 0.f : ex2_approx(lse - top);
@@ -915,7 +1077,6 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
     float *st = reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1);
     st[0] = S.qscale[slot][rg * kRows + tid];
     st[2] = 0.f;
-    S.ref[g][tid] = -INFINITY;  // (its largest so far)
   }
   named_bar_sync(1 + g, 128);
   const int e0 = nr == 32 ? softmax_tiles<32>(P, S, X, I) : softmax_tiles<16>(P, S, X, I);
@@ -980,7 +1141,7 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
     // the last CTA of the task to get here joins its parts
     __threadfence();
     named_bar_sync(1 + g, 128);
-    if (tid == 0) S.last[g] = atomicAdd(&P.done[I.cta0 * kGroups + rg], 1) == I.cta1 - I.cta0;
+    if (tid == 0) S.last[g] = atomicAdd(&P.done[I.cta0 * kGroups + rg], 1) == I.cta1 - I.ctab + 1;
     named_bar_sync(1 + g, 128);
     if (*(volatile int *)&S.last[g]) {
       __threadfence();
@@ -1024,7 +1185,8 @@ __device__ void softmax_warps(const Params &P, Shared &S, int warp, int lane) {
 
 __global__ void __launch_bounds__(kThreads, 1) attn8_kernel(const __grid_constant__ Params P) {
   extern __shared__ uint8_t raw[];
-  Shared &S = *reinterpret_cast<Shared *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  // (an offset from the array, so that accesses stay known as shared memory's)
+  Shared &S = *reinterpret_cast<Shared *>(raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x < kGroups * kD) S.nan_key[threadIdx.x / kD][threadIdx.x % kD] = 0x7fffffff;
   if (threadIdx.x < kGroups) S.bad[threadIdx.x] = 0;
@@ -1036,7 +1198,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_kernel(const __grid_constan
     ring(S.k_full, kKStages, 1), ring(S.k_empty, kKStages, 1);
     ring(S.v_full, kVStages, 1), ring(S.v_empty, kVStages, 1);
     ring(S.pg_full, kMeta, 1), ring(S.sc_full, kMeta, 1), ring(S.meta_empty, kMeta, 1);
-    ring(S.q_full, kSlots, kQWarps), ring(S.q_empty, 2, 1);
+    ring(S.q_full, kSlots, kQWarps), ring(S.q_empty, kQUnits, 1);
     ring(S.s_full, kGroups, 1), ring(S.s_empty, kGroups, 4);
     ring(S.p_full, kGroups, 4), ring(S.pv_done, kGroups, 1);
     ring(S.item_full, kSlots, 1), ring(S.item_empty, kSlots, kItemReaders);
@@ -1059,8 +1221,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_kernel(const __grid_constan
     else if (warp == kVWarp) load_warp<true>(P, S, lane);
     else if (warp == kQkWarp) qk_warp(S, lane);
     else if (warp == kPvWarp) pv_warp(S, lane);
-    else if (warp == kMetaWarp) meta_warp(P, S, lane);
-    else query_warp(P, S, warp - kMetaWarp - 1, lane);
+    else if (warp == kItemWarp) item_warp(P, S, lane);
+    else if (warp == kPageWarp) page_warp(P, S, lane);
+    else query_warp(P, S, warp - kPageWarp - 1, lane);
   }
   __syncwarp();
   tc_fence_before();
@@ -1166,7 +1329,7 @@ Layout layout(const ipd_attn8_batch *const *bs, int n) {
   W.part_rows = (int)((std::min<long long>(rows, kBlockRows) + 3) / 4 * 4);
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   W.prefix = 0;
-  W.info = up((size_t)(W.reqs + 1) * sizeof(long long));
+  W.info = up((size_t)(W.reqs + 2) * sizeof(long long));
   W.done = W.info + up((size_t)W.reqs * sizeof(int4));
   W.part = W.done + up(kMaxCtas * kGroups * sizeof(int));
   W.total = W.part + up((size_t)2 * kMaxCtas * W.part_rows * (kD + 1) * sizeof(float));
