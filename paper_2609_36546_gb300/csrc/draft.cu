@@ -18,6 +18,7 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "cluster.cuh"
@@ -82,21 +83,56 @@ struct RowView {
   }
 };
 
-// Weights of a row's entries.
+// Weights of a row's entries.  How entries far below the top are kept out of the
+// procedure's range: kNear, by a bf16 value of weight 0 that takes the place of all
+// below it (and of NaN); kCoarse, where no bf16 value lies between weight 0 and that
+// range, by a bound on x; kInf, the top is +inf and only its equals have a weight;
+// kNone, the row has no entry.
+enum { kNear, kCoarse, kInf, kNone };
 struct Weigher {
   float top, c;
-  bool inf;  // top is +inf: only its equals have a weight
-  IPD_DEVINL Weigher(float t, float cc) : top(t), c(cc), inf(t == INFINITY) {}
+  uint32_t least2;
+  int mode;
+  IPD_DEVINL Weigher(float t, float cc) : top(t), c(cc), least2(0xff80ff80u), mode(kCoarse) {
+    if (t == INFINITY) mode = kInf;
+    else if (t == -INFINITY) mode = kNone;
+    else {
+      // as a bf16 value, rounded away from the top
+      const float least = t - 34.f / cc;
+      const uint32_t b = __float_as_uint(least);
+      const uint32_t h = (b >> 16) + ((b >> 31) && (b & 0xffffu) ? 1u : 0u);
+      const float at = x(bf16f((uint16_t)h));
+      if (at < -32.f && at > -90.f) least2 = h | h << 16, mode = kNear;
+    }
+  }
+  template <int kMode>
   IPD_DEVINL void two(uint32_t w, uint32_t &w0, uint32_t &w1) const {
-    if (inf) {
-      w0 = (w & 0xffffu) == 0x7f80u ? 1u << 30 : 0u;
-      w1 = w >> 16 == 0x7f80u ? 1u << 30 : 0u;
+    if (kMode == kInf || kMode == kNone) {
+      w0 = kMode == kInf && (w & 0xffffu) == 0x7f80u ? 1u << 30 : 0u;
+      w1 = kMode == kInf && w >> 16 == 0x7f80u ? 1u << 30 : 0u;
       return;
     }
-    float a, b;
-    f2_unpack(f2_mul(f2_sub(f2_pack(bf16lo(w), bf16hi(w)), f2_pack(top, top)), f2_pack(c, c)), a, b);
-    // (fmaxf drops a NaN: NaN entries, and every entry of a row without any)
-    pow2_weight2(f2_pack(fmaxf(a, -64.f), fmaxf(b, -64.f)), w0, w1);
+    if (kMode == kNear) w = max2(w, least2);
+    u64 y = f2_mul(f2_sub(f2_pack(bf16lo(w), bf16hi(w)), f2_pack(top, top)), f2_pack(c, c));
+    if (kMode == kCoarse) {
+      float a, b;
+      f2_unpack(y, a, b);
+      y = f2_pack(fmaxf(a, -64.f), fmaxf(b, -64.f));  // (fmaxf drops a NaN)
+    }
+    pow2_weight2(y, w0, w1);
+  }
+  IPD_DEVINL void any_two(uint32_t w, uint32_t &w0, uint32_t &w1) const {
+    if (mode == kNear) two<kNear>(w, w0, w1);
+    else if (mode == kCoarse) two<kCoarse>(w, w0, w1);
+    else if (mode == kInf) two<kInf>(w, w0, w1);
+    else w0 = w1 = 0;
+  }
+  template <int kMode>
+  IPD_DEVINL void eight(const uint4 &v, uint32_t (&r)[8]) const {
+    two<kMode>(v.x, r[0], r[1]);
+    two<kMode>(v.y, r[2], r[3]);
+    two<kMode>(v.z, r[4], r[5]);
+    two<kMode>(v.w, r[6], r[7]);
   }
   IPD_DEVINL float x(float l) const { return l == top ? 0.f : __fmul_rn(__fsub_rn(l, top), c); }
 };
@@ -167,12 +203,67 @@ IPD_DEVINL int request_of(const ipd_draft_args &a, int t) {
 }
 
 // ---- rows ------------------------------------------------------------------
-__global__ void __launch_bounds__(kThreads) draft_rows_kernel(const __grid_constant__ Params P) {
-  __shared__ u64 red[kWarps], zs;
-  __shared__ float fred[kWarps], tops;
+// A row's maximum and the sum of its weights.  bf16 logits have few values, and entries of
+// one value have one weight: a long piece of a row is read once into a histogram of its
+// values (an integer atomic in shared memory an entry), and the sum is taken from the bins.
+// 2^-19 <= |l| < 2^12 is 31 binades of 128 values a sign, whose low 12 bits and sign are the
+// bin.  What is nearer to 0 goes to a list (zeros are counted); -inf, NaN and what is not
+// above -2^12 have no weight next to such a maximum and go to a bin that no value has.  A
+// row that does not fit this (a maximum outside, a full list, so high a temperature that
+// -2^12 matters) and short pieces are read twice: for the maximum, then, from L2, entry by
+// entry.
+constexpr int kBins = 8192;
+constexpr uint32_t kLowBits = 0x3600;   // bf16 bits of 2^-19
+constexpr uint32_t kHighBits = 0x4580;  // ... of 2^12
+constexpr int kList = 256;
+constexpr int kHistThreads = 256, kPlainThreads = 512;
+constexpr int kHistEntries = 24 * 1024;  // pieces from here on take a histogram: see ipd_verify_draft
+
+// The byte offsets of two entries' bins.
+IPD_DEVINL uint32_t bins2(uint32_t w) { return ((w << 2) & 0x3ffc3ffcu) | ((w >> 1) & 0x40004000u); }
+// The bf16 bits of a bin's value.
+IPD_DEVINL uint32_t bin_bits(uint32_t bin) {
+  const uint32_t low = bin & 0xfffu;
+  return (bin >> 12) << 15 | (low >= (kLowBits & 0xfffu) ? 0x3000u : 0x4000u) | low;
+}
+IPD_DEVINL uint32_t min_abs2(uint32_t a, uint32_t w) {
+  const __nv_bfloat162 m = __hmin2(*reinterpret_cast<__nv_bfloat162 *>(&a), __habs2(*reinterpret_cast<__nv_bfloat162 *>(&w)));
+  return *reinterpret_cast<const uint32_t *>(&m);
+}
+IPD_DEVINL void shared_add(uint32_t addr, uint32_t v) {
+  asm volatile("red.shared.add.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
+template <int kT>
+struct RowShared {
+  u64 red[kT / 32], z;
+  float fred[kT / 32], top;
+  uint32_t zeros, listed;
+  uint16_t list[kList];
+};
+
+// Sum of a thread's weights in a piece, entry by entry.
+template <int kMode, int kT>
+IPD_DEVINL u64 piece_sum(const Weigher &W, const RowView &R, int from, int to) {
+  u64 z = 0;
+  for (int i = from + threadIdx.x; i < to; i += kT) {
+    uint32_t w[8];
+    W.eight<kMode>(R.get(i), w);
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) z += w[k] + w[k + 1];
+  }
+  return z;
+}
+
+template <bool kHist>
+__global__ void __launch_bounds__(kHist ? kHistThreads : kPlainThreads, kHist ? 6 : 3)
+    draft_rows_kernel(const __grid_constant__ Params P) {
+  constexpr int kT = kHist ? kHistThreads : kPlainThreads;
+  extern __shared__ uint4 hist4[];
+  __shared__ RowShared<kT> S;
   const ipd_draft_args &a = P.a;
   const uint32_t csize = cluster_size(), rank = cluster_rank();
-  const int row = blockIdx.x / csize, t = row >> 1;
+  const int row = blockIdx.x / csize, t = row >> 1, tid = threadIdx.x, lane = tid & 31;
   const bool draft = row & 1;
   const int r = request_of(a, t);
   if (r < 0) return;  // (the whole cluster)
@@ -182,35 +273,114 @@ __global__ void __launch_bounds__(kThreads) draft_rows_kernel(const __grid_const
                             : a.logits_target + (long long)t * a.target_stride;
   const RowView R(p, a.vocab);
   const int from = min((int)rank * P.piece, R.n_vec), to = min(from + P.piece, R.n_vec);
-  float top = block_max(piece_max(R, from, to), fred);
+  uint32_t m = 0xff80ff80u;
+  if (kHist) {
+    for (int i = tid; i < kBins / 4; i += kT) hist4[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (tid == 0) S.zeros = S.listed = 0u;
+    __syncthreads();
+    const uint32_t hist = smem_u32(hist4);
+    constexpr uint32_t kLowest2 = (0x8000u | kHighBits) * 0x10001u;
+    constexpr int kAhead = 4;
+    for (int i0 = from + tid; i0 < to; i0 += kAhead * kT) {
+      uint4 v[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        v[k] = i0 + k * kT < to ? R.get(i0 + k * kT) : make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);
+      uint32_t least = 0x7f807f80u;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          m = max2(m, w[e]);
+          least = min_abs2(least, w[e]);
+          const uint32_t b = bins2(max2(w[e], kLowest2));
+          shared_add(hist + (b & 0xffffu), 1u);
+          shared_add(hist + (b >> 16), 1u);
+        }
+      }
+      if (min(least & 0xffffu, least >> 16) < kLowBits) {
+        // entries near 0 were counted in another's bin
+#pragma unroll 1
+        for (int k = 0; k < 8 * kAhead; ++k) {
+          uint32_t w = 0;
+#pragma unroll
+          for (int j = 0; j < kAhead; ++j) {
+            const uint32_t x[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (k >> 1 == 4 * j + e) w = x[e];
+          }
+          w = k & 1 ? w >> 16 : w & 0xffffu;
+          if ((w & 0x7fffu) >= kLowBits) continue;
+          shared_add(hist + (bins2(w) & 0xffffu), 0xffffffffu);
+          if ((w & 0x7fffu) == 0) {
+            atomicAdd(&S.zeros, 1u);
+          } else {
+            const uint32_t n = atomicAdd(&S.listed, 1u);
+            if (n < (uint32_t)kList) S.list[n] = (uint16_t)w;
+          }
+        }
+      }
+    }
+  } else {
+#pragma unroll 4
+    for (int i = from + tid; i < to; i += kT) {
+      const uint4 v = R.get(i);
+      m = max2(m, max2(max2(v.x, v.y), max2(v.z, v.w)));
+    }
+  }
+  float top = warp_max(fmaxf(bf16lo(m), bf16hi(m)));
+  if (lane == 0) S.fred[tid >> 5] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kT / 32; ++i) top = fmaxf(top, S.fred[i]);
   if (csize > 1) {
-    if (threadIdx.x == 0) tops = top;
+    if (tid == 0) S.top = top;
     cluster_sync();
-    for (uint32_t i = 0; i < csize; ++i) top = fmaxf(top, __uint_as_float(remote_ld(remote(&tops, i))));
+    for (uint32_t i = 0; i < csize; ++i) top = fmaxf(top, __uint_as_float(remote_ld(remote(&S.top, i))));
   }
   const Weigher W(top, c);
   u64 z = 0;
-  for (int i = from + threadIdx.x; i < to; i += kThreads) {
-    const uint4 v = R.get(i);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
+  if (kHist && W.mode != kNone && top < 4096.f && W.x(-4096.f) < -32.f && S.listed <= (uint32_t)kList) {
+    const uint32_t *hist = reinterpret_cast<const uint32_t *>(hist4);
+#pragma unroll 2
+    for (int k = 2 * tid; k < kBins; k += 2 * kT) {
+      const uint32_t n0 = hist[k], n1 = hist[k + 1];
+      if ((n0 | n1) == 0u || (k & 0xf80) == (kHighBits & 0xf80)) continue;  // (the bin of no value)
       uint32_t w0, w1;
-      W.two(w[k], w0, w1);
-      z += w0 + w1;
+      W.two<kCoarse>(bin_bits(k) | bin_bits(k + 1) << 16, w0, w1);
+      z += (u64)n0 * w0 + (u64)n1 * w1;
     }
+    for (int k = tid; k <= (int)S.listed; k += kT) {  // the list, and the zeros
+      const bool zero = k == (int)S.listed;
+      uint32_t w0, w1;
+      W.two<kCoarse>((zero ? 0u : S.list[k]) | 0xff800000u, w0, w1);
+      z += (u64)w0 * (zero ? S.zeros : 1u);
+    }
+  } else if (W.mode == kNear) {
+    z = piece_sum<kNear, kT>(W, R, from, to);
+  } else if (W.mode == kCoarse) {
+    z = piece_sum<kCoarse, kT>(W, R, from, to);
+  } else if (W.mode == kInf) {
+    z = piece_sum<kInf, kT>(W, R, from, to);
   }
-  z = block_sum(z, red);
+  z = warp_sum64(z);
+  if (lane == 0) S.red[tid >> 5] = z;
+  __syncthreads();
+  z = 0;
+#pragma unroll
+  for (int i = 0; i < kT / 32; ++i) z += S.red[i];
   if (csize > 1) {
-    if (threadIdx.x == 0) zs = z;
+    if (tid == 0) S.z = z;
     cluster_sync();
     if (rank == 0) {
       z = 0;
-      for (uint32_t i = 0; i < csize; ++i) z += remote_ld64(&zs, i);
+      for (uint32_t i = 0; i < csize; ++i) z += remote_ld64(&S.z, i);
     }
     cluster_sync();  // no CTA leaves while its sums are read
   }
-  if (rank == 0 && threadIdx.x == 0) {
+  if (rank == 0 && tid == 0) {
     const int tok = a.tokens[t];
     uint32_t w0 = 0, w1;
     float logp = __uint_as_float(0x7fc00000u);
@@ -218,7 +388,7 @@ __global__ void __launch_bounds__(kThreads) draft_rows_kernel(const __grid_const
       ipd_set_error(&g_draft_err, IPD_DEVERR_TOKEN);
     } else {
       const uint16_t l = p[tok];
-      W.two(l | 0xff800000u, w0, w1);
+      W.any_two(l | 0xff800000u, w0, w1);
       const float f = bf16f(l);
       logp = z == 0 || f != f ? -INFINITY
                               : (float)(((double)W.x(f) - log2((double)z * 0x1p-30)) * 0.6931471805599453);
@@ -258,28 +428,45 @@ struct Residual {
   // weights of the 8 entries of target vector i
   IPD_DEVINL void eight(int i, uint32_t (&r)[8]) const {
     const uint4 v = p.get(i);
-    wp.two(v.x, r[0], r[1]);
-    wp.two(v.y, r[2], r[3]);
-    wp.two(v.z, r[4], r[5]);
-    wp.two(v.w, r[6], r[7]);
-    if (m == 0) return;
-    uint32_t g[8];
-    if (off == 0) {
-      const uint4 o = q.get(i);
-      wq.two(o.x, g[0], g[1]);
-      wq.two(o.y, g[2], g[3]);
-      wq.two(o.z, g[4], g[5]);
-      wq.two(o.w, g[6], g[7]);
-    } else {  // rows of different alignment: entry by entry
-      const uint16_t *l = reinterpret_cast<const uint16_t *>(q.base) + q.before;
+    uint4 o = v;
+    if (m != 0) {
+      if (off == 0) {
+        o = q.get(i);
+      } else {  // rows of different alignment: entry by entry
+        const uint16_t *l = reinterpret_cast<const uint16_t *>(q.base) + q.before;
+        uint32_t *w = &o.x;
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const int at = i * 8 + e - p.before;
-        const uint32_t lo = at >= 0 && at < p.entries ? l[at] : 0xff80u,
-                       hi = at + 1 >= 0 && at + 1 < p.entries ? l[at + 1] : 0xff80u;
-        wq.two(lo | hi << 16, g[e], g[e + 1]);
+        for (int e = 0; e < 8; e += 2) {
+          const int at = i * 8 + e - p.before;
+          const uint32_t lo = at >= 0 && at < p.entries ? l[at] : 0xff80u,
+                         hi = at + 1 >= 0 && at + 1 < p.entries ? l[at + 1] : 0xff80u;
+          w[e >> 1] = lo | hi << 16;
+        }
       }
     }
+    if (wp.mode == kNear && wq.mode == kNear) {
+      wp.eight<kNear>(v, r);
+      if (m != 0) {
+        uint32_t g[8];
+        wq.eight<kNear>(o, g);
+        take(r, g);
+      }
+    } else {
+      const uint32_t vw[4] = {v.x, v.y, v.z, v.w}, ow[4] = {o.x, o.y, o.z, o.w};
+      uint32_t g[8] = {};
+#pragma unroll 1
+      for (int k = 0; k < 4; ++k) {
+        uint32_t a, b, c, d;
+        wp.any_two(vw[k], a, b);
+        wq.any_two(ow[k], c, d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j == k) r[2 * j] = a, r[2 * j + 1] = b, g[2 * j] = c, g[2 * j + 1] = d;
+      }
+      if (m != 0) take(r, g);
+    }
+  }
+  IPD_DEVINL void take(uint32_t (&r)[8], const uint32_t (&g)[8]) const {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const u64 less = (u64)g[e] * m >> s;
@@ -428,10 +615,11 @@ __global__ void __launch_bounds__(kThreads) draft_verdict_kernel(const __grid_co
 
 int g_sms[64];
 
-int launch(void (*kernel)(Params), int grid, int csize, const Params &P, cudaStream_t stream) {
+int launch(void (*kernel)(Params), int grid, int csize, int threads, int shared, const Params &P, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid * csize);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)shared;
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -492,20 +680,20 @@ extern "C" int ipd_verify_draft(const ipd_draft_args *args, void *workspace,
   P.a = a;
   P.rows = static_cast<Row *>(workspace);
   const int vecs = (a.vocab + 14) / 8;
-  // CTAs of a row: as many (1, 2, 4, 8) as leave every one an SM's quarter
-  auto split = [&](long long rows) {
-    int c = kMaxCluster;
-    while (c > 1 && (rows * c > 4LL * sms || vecs < c * 1024)) c /= 2;
-    return c;
-  };
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   g_draft_used.store(true, std::memory_order_relaxed);
   if (a.total > 0) {
-    const int c = split(2LL * a.total);
+    // CTAs of a row: as many (1, 2, 4, 8) as leave every CTA a quarter of an SM
+    int c = kMaxCluster;
+    while (c > 1 && (2LL * a.total * c > 4LL * sms || vecs < c * 512)) c /= 2;
     P.piece = (vecs + c - 1) / c;
-    if (launch(draft_rows_kernel, 2 * a.total, c, P, st) != IPD_OK) return IPD_ERR_CUDA;
+    const bool hist = P.piece * 8 >= kHistEntries;
+    if (launch(hist ? draft_rows_kernel<true> : draft_rows_kernel<false>, 2 * a.total, c, hist ? kHistThreads : kPlainThreads,
+               hist ? kBins * 4 : 0, P, st) != IPD_OK)
+      return IPD_ERR_CUDA;
   }
-  const int c = split(a.num_reqs);
+  int c = kMaxCluster;
+  while (c > 1 && ((long long)a.num_reqs * c > 4LL * sms || vecs < c * 512)) c /= 2;
   P.piece = (vecs + 32 * c - 1) / (32 * c) * 32;
-  return launch(draft_verdict_kernel, a.num_reqs, c, P, st);
+  return launch(draft_verdict_kernel, a.num_reqs, c, kThreads, 0, P, st);
 }
