@@ -120,6 +120,7 @@ struct Item {
   int row0, rows;       // first row of the task among the request's, and number
   int nr, ng, wg;       // rows of a warpgroup (16 or 32); its warpgroups (1, 2 or 4) and their first
   int t0, t1;           // tiles
+  int masked;           // the first key that some row of the task does not see
   int qu;               // first query tile
   int r, n_pages;       // request of the batch, its pages
   int part;             // partial slot (-1: the whole task is here)
@@ -153,6 +154,7 @@ struct Shared {
   uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
   uint64_t pg_full[kMeta], sc_full[kMeta], meta_empty[kMeta];
   uint64_t q_full[kSlots], q_empty[kQUnits], s_full[kGroups], s_empty[kGroups], p_full[kGroups], pv_done[kGroups];
+  uint64_t v_ready[kGroups], mended[kGroups];  // a tile with hidden keys has landed, and has been looked through
   uint64_t item_full[kSlots], item_empty[kSlots], pair[2], all, drain[2];
 };
 constexpr int kSharedBytes = (int)sizeof(Shared) + 1024;  // the base is aligned by hand
@@ -450,6 +452,7 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
           I.valid = 1, I.b = b, I.c0 = info.z, I.n = info.y, I.L = L, I.h = h;
           I.row0 = row0, I.rows = rows, I.nr = rows > 16 ? 32 : 16, I.ng = ng, I.wg = wg, I.qu = qu;
           I.t0 = t0, I.t1 = t1;
+          I.masked = L - info.y + 1 + row0 / group;
           I.r = g - P.req_base[b], I.n_pages = (L + kPage - 1) / kPage;
           I.part = t1 - t0 == tiles ? -1 : t0 > 0 ? 2 * (int)blockIdx.x : 2 * (int)blockIdx.x + 1;
           if (I.part >= 0) {
@@ -641,13 +644,14 @@ __device__ void qk_warp(Shared &S, int lane) {
 __device__ void pv_warp(Shared &S, int lane) {
   const uint32_t tmem = (uint32_t)uniform((int)S.tmem);
   const uint64_t v0 = sdesc((uint32_t)uniform((int)smem_u32(S.v[0])), 128);
-  uint32_t it = 0, uses = 0;
+  uint32_t it = 0, uses = 0, mends = 0;  // (a bit a warpgroup: parity of its uses)
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
     if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) break;
     const Item &I = S.item[slot];
     if (!uniform(I.valid)) return;
     const int tiles = uniform(I.t1 - I.t0), ng = uniform(I.ng), nr = uniform(I.nr);
+    const int hides = uniform(I.masked / kKeys - I.t0);  // tiles from here on have hidden keys
     const uint32_t idesc = idesc_f8(2 * nr, 1);
     const uint64_t p0 = sdesc((uint32_t)uniform((int)smem_u32(S.p[0])), 2 * nr);
     const uint64_t step = (uint64_t)(32 * 2 * nr >> 4);  // 32 keys of P further on
@@ -660,6 +664,11 @@ __device__ void pv_warp(Shared &S, int lane) {
       for (int i = 0; ok && i < ng; ++i) {
         const uint32_t g = g0 + i;
         ok = wait(&S.p_full[g], uses >> g & 1u, &S.abort, 40);
+        if (ok && i == 0 && t >= hides) {
+          if (lane == 0) mbar_arrive(&S.v_ready[g]);
+          ok = wait(&S.mended[g], mends >> g & 1u, &S.abort, 40);
+          mends ^= 1u << g;
+        }
         if (!ok) break;
         tc_fence_after();
         const uint64_t p = p0 + (uint64_t)(g * (uint32_t)(sizeof(S.p[0]) >> 4));
@@ -771,6 +780,7 @@ IPD_DEVINL float column_reduce(float (&a)[16], int lane, Op op) {
 struct Softmax {
   int g, tid, warp, lane;  // warpgroup, and place in it
   uint32_t tiles, it;      // own tiles so far, tiles of the CTA so far
+  uint32_t mends;          // tiles looked through so far
   uint32_t pairs, alls;    // barriers of two and of all warpgroups so far
   bool ok;                 // no wait of this warp has given up
 };
@@ -915,7 +925,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
   const int row0 = I.row0 + (g - I.wg) * kRows;
   const int group = P.b[I.b].group;
   const int sees = L - I.n;                        // query i sees keys up to sees + i
-  const int masked = sees + 1 + I.row0 / group;    // the first key that some row of the task does not see
+  const int masked = I.masked;
   const int turn = NR == 32 ? (tid >> 1) & 3 : (tid >> 2) & 1;  // P's swizzle
   uint8_t *prow = S.p[g] + tid * 2 * NR;
   int e0 = 0;
@@ -924,6 +934,9 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
   for (int t = 0; t < n_tiles; ++t) {
     const uint32_t it = X.it + t;
     const uint32_t m = it % kMeta;
+    // (first the scores: the tile may be many turns of the ring of scales ahead, which tells
+    // one turn from the next only)
+    X.ok = wait_inline(&S.s_full[g], full(X.tiles, 1), &S.abort) && X.ok;
     X.ok = wait_inline(&S.sc_full[m], full(it, kMeta), &S.abort) && X.ok;
     const Meta &M = S.meta[m];
     const int key0 = (I.t0 + t) * kKeys, key = key0 + tid;
@@ -944,7 +957,6 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
       if (hidden == NR) de = 0;
     }
     const float fk = ev == 128 && hidden < NR ? __uint_as_float(0x7fc00000u) : pow2i(de);
-    X.ok = wait_inline(&S.s_full[g], full(X.tiles, 1), &S.abort) && X.ok;
     tc_fence_after();
     u64 y[NR / 2];
     {
@@ -1020,16 +1032,18 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
 #pragma unroll 1
         for (int k = i; k < 2 * NR; k += NR) prow[(((k >> 4) ^ turn) << 4) + (k & 15)] = 0;
     }
-    // (the product takes the first warpgroup's rows before the others')
-    if (key0 + kKeys > masked && g == I.wg) {
-      const uint32_t vs = it % kVStages;
-      X.ok = wait_inline(&S.v_full[vs], full(it, kVStages), &S.abort) && X.ok;
-      if (key >= masked) mend(S, g, S.v[vs], tid, key, L);
-    }
     fence_proxy_async_smem();
     tc_wait_st();
     tc_fence_before();
     arrive_warp(&S.p_full[g], lane);
+    if (key0 + kKeys > masked && g == I.wg) {
+      // hidden keys: the product waits until the tile has been looked through (it takes
+      // the first warpgroup's rows before the others')
+      X.ok = wait_inline(&S.v_ready[g], full(X.mends, 1), &S.abort) && X.ok;
+      ++X.mends;
+      if (key >= masked) mend(S, g, S.v[it % kVStages], tid, key, L);
+      arrive_warp(&S.mended[g], lane);
+    }
     ++X.tiles;
     first = false;
   }
@@ -1170,7 +1184,7 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
 }
 
 __device__ void softmax_warps(const Params &P, Shared &S, int warp, int lane) {
-  Softmax X{warp >> 2, (int)threadIdx.x & 127, warp & 3, lane, 0, 0, 0, 0, true};
+  Softmax X{warp >> 2, (int)threadIdx.x & 127, warp & 3, lane, 0, 0, 0, 0, 0, true};
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
     X.ok = wait_inline(&S.item_full[slot], full(n, kSlots), &S.abort) && X.ok;
@@ -1201,6 +1215,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_kernel(const __grid_constan
     ring(S.q_full, kSlots, kQWarps), ring(S.q_empty, kQUnits, 1);
     ring(S.s_full, kGroups, 1), ring(S.s_empty, kGroups, 4);
     ring(S.p_full, kGroups, 4), ring(S.pv_done, kGroups, 1);
+    ring(S.v_ready, kGroups, 1), ring(S.mended, kGroups, 4);
     ring(S.item_full, kSlots, 1), ring(S.item_empty, kSlots, kItemReaders);
     ring(S.pair, 2, 8), ring(&S.all, 1, kSoftmaxWarps), ring(S.drain, 2, 1);
     fence_mbar_init();

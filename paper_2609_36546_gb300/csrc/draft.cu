@@ -32,7 +32,7 @@ static std::atomic<bool> g_draft_used{false};
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;  // of a verdict's CTA
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kTile = 256;  // entries a warp sums at once: 8 a lane
@@ -40,15 +40,25 @@ constexpr int kTiles = (IPD_TRUNC_MAX_VOCAB + 8) / kTile + 1;
 
 // What the row pass leaves of a row.
 struct Row {
-  u64 z;         // sum of the weights
-  float top;     // largest logit (-inf: the row has no entry)
-  uint32_t w;    // the drafted token's weight
+  u64 z[kMaxCluster];  // sums of the weights of its pieces
+  float top;           // largest logit (-inf: the row has no entry)
+  uint32_t w;          // the drafted token's weight
+  float x;             // ... and x (-inf: the row's entry there is none)
+  uint32_t pad;
+  IPD_DEVINL u64 sum(int pieces) const {
+    u64 s = 0;
+#pragma unroll
+    for (int i = 0; i < kMaxCluster; ++i)
+      if (i < pieces) s += z[i];
+    return s;
+  }
 };
 
 struct Params {
   ipd_draft_args a;
   Row *rows;     // [2 total]: target and draft row of every position
   int piece;     // 8-entry vectors a CTA takes of a row (verdicts: a multiple of 32)
+  int pieces;    // CTAs of a row in the row pass
 };
 
 IPD_DEVINL uint32_t max2(uint32_t a, uint32_t b) {  // of two bf16 each; NaN loses
@@ -148,6 +158,12 @@ IPD_DEVINL u64 warp_sum64(u64 v) {
   return v;
 }
 
+// ... of values below 2^40: two sums of parts
+IPD_DEVINL u64 warp_sum40(u64 v) {
+  return (u64)__reduce_add_sync(0xffffffffu, (uint32_t)v & 0xffffffu) +
+         ((u64)__reduce_add_sync(0xffffffffu, (uint32_t)(v >> 24)) << 24);
+}
+
 IPD_DEVINL u64 remote_ld64(const void *p, uint32_t rank) {
   const uint32_t a = remote(p, rank);
   return (u64)remote_ld(a) | (u64)remote_ld(a + 4) << 32;
@@ -216,7 +232,7 @@ constexpr int kBins = 8192;
 constexpr uint32_t kLowBits = 0x3600;   // bf16 bits of 2^-19
 constexpr uint32_t kHighBits = 0x4580;  // ... of 2^12
 constexpr int kList = 256;
-constexpr int kHistThreads = 256, kPlainThreads = 512;
+constexpr int kHistThreads = 512, kPlainThreads = 512;
 constexpr int kHistEntries = 24 * 1024;  // pieces from here on take a histogram: see ipd_verify_draft
 
 // The byte offsets of two entries' bins.
@@ -236,8 +252,10 @@ IPD_DEVINL void shared_add(uint32_t addr, uint32_t v) {
 
 template <int kT>
 struct RowShared {
-  u64 red[kT / 32], z;
+  u64 red[kT / 32];
   float fred[kT / 32], top;
+  float cp, cq;           // the request's scales
+  int r;                  // ... and itself (-1: the position is none's)
   uint32_t zeros, listed;
   uint16_t list[kList];
 };
@@ -256,7 +274,7 @@ IPD_DEVINL u64 piece_sum(const Weigher &W, const RowView &R, int from, int to) {
 }
 
 template <bool kHist>
-__global__ void __launch_bounds__(kHist ? kHistThreads : kPlainThreads, kHist ? 6 : 3)
+__global__ void __launch_bounds__(kHist ? kHistThreads : kPlainThreads, kHist ? 4 : 3)
     draft_rows_kernel(const __grid_constant__ Params P) {
   constexpr int kT = kHist ? kHistThreads : kPlainThreads;
   extern __shared__ uint4 hist4[];
@@ -264,13 +282,22 @@ __global__ void __launch_bounds__(kHist ? kHistThreads : kPlainThreads, kHist ? 
   const ipd_draft_args &a = P.a;
   const uint32_t csize = cluster_size(), rank = cluster_rank();
   const int row = blockIdx.x / csize, t = row >> 1, tid = threadIdx.x, lane = tid & 31;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const bool draft = row & 1;
-  const int r = request_of(a, t);
-  if (r < 0) return;  // (the whole cluster)
-  const float cp = scale_of(a.inv_temp_target, r), cq = scale_of(a.inv_temp_draft, r);
-  const float c = draft ? cq : cp;
+  if (tid == kT - 1) {  // beside the first loads
+    const int r = request_of(a, t);
+    S.r = r;
+    S.cp = scale_of(a.inv_temp_target, max(r, 0)), S.cq = scale_of(a.inv_temp_draft, max(r, 0));
+  }
   const uint16_t *p = draft ? a.logits_draft + (long long)t * a.draft_stride
                             : a.logits_target + (long long)t * a.target_stride;
+  // the drafted token's entry
+  int tok = 0;
+  uint16_t entry = 0xff80;
+  if (rank == 0 && tid == 0) {
+    tok = a.tokens[t];
+    if (tok >= 0 && tok < a.vocab) entry = p[tok];
+  }
   const RowView R(p, a.vocab);
   const int from = min((int)rank * P.piece, R.n_vec), to = min(from + P.piece, R.n_vec);
   uint32_t m = 0xff80ff80u;
@@ -280,7 +307,7 @@ __global__ void __launch_bounds__(kHist ? kHistThreads : kPlainThreads, kHist ? 
     __syncthreads();
     const uint32_t hist = smem_u32(hist4);
     constexpr uint32_t kLowest2 = (0x8000u | kHighBits) * 0x10001u;
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 2;
     for (int i0 = from + tid; i0 < to; i0 += kAhead * kT) {
       uint4 v[kAhead];
 #pragma unroll
@@ -338,9 +365,11 @@ __global__ void __launch_bounds__(kHist ? kHistThreads : kPlainThreads, kHist ? 
   if (csize > 1) {
     if (tid == 0) S.top = top;
     cluster_sync();
-    for (uint32_t i = 0; i < csize; ++i) top = fmaxf(top, __uint_as_float(remote_ld(remote(&S.top, i))));
+    if (lane < (int)csize) top = __uint_as_float(remote_ld(remote(&S.top, lane)));
+    top = warp_max(top);
+    cluster_arrive();  // (waited for at the end: no CTA leaves while its maximum is read)
   }
-  const Weigher W(top, c);
+  const Weigher W(top, draft ? S.cq : S.cp);
   u64 z = 0;
   if (kHist && W.mode != kNone && top < 4096.f && W.x(-4096.f) < -32.f && S.listed <= (uint32_t)kList) {
     const uint32_t *hist = reinterpret_cast<const uint32_t *>(hist4);
@@ -368,36 +397,19 @@ __global__ void __launch_bounds__(kHist ? kHistThreads : kPlainThreads, kHist ? 
   z = warp_sum64(z);
   if (lane == 0) S.red[tid >> 5] = z;
   __syncthreads();
-  z = 0;
-#pragma unroll
-  for (int i = 0; i < kT / 32; ++i) z += S.red[i];
-  if (csize > 1) {
-    if (tid == 0) S.z = z;
-    cluster_sync();
+  if (tid == 0 && S.r >= 0) {
+    z = 0;
+    for (int i = 0; i < kT / 32; ++i) z += S.red[i];
+    Row &O = P.rows[row];
+    O.z[rank] = z;
     if (rank == 0) {
-      z = 0;
-      for (uint32_t i = 0; i < csize; ++i) z += remote_ld64(&S.z, i);
+      uint32_t w0, w1;
+      W.any_two(entry | 0xff800000u, w0, w1);
+      const float l = bf16f(entry);
+      O.top = top, O.w = w0, O.x = l != l ? -INFINITY : W.x(l);
     }
-    cluster_sync();  // no CTA leaves while its sums are read
   }
-  if (rank == 0 && tid == 0) {
-    const int tok = a.tokens[t];
-    uint32_t w0 = 0, w1;
-    float logp = __uint_as_float(0x7fc00000u);
-    if (tok < 0 || tok >= a.vocab) {
-      ipd_set_error(&g_draft_err, IPD_DEVERR_TOKEN);
-    } else {
-      const uint16_t l = p[tok];
-      W.any_two(l | 0xff800000u, w0, w1);
-      const float f = bf16f(l);
-      logp = z == 0 || f != f ? -INFINITY
-                              : (float)(((double)W.x(f) - log2((double)z * 0x1p-30)) * 0.6931471805599453);
-    }
-    if (!valid(cp) || !valid(cq)) logp = __uint_as_float(0x7fc00000u);
-    float *out = draft ? a.logp_draft : a.logp_target;
-    if (out) out[t] = logp;
-    P.rows[row] = Row{z, top, w0};
-  }
+  if (csize > 1) cluster_wait();
 }
 
 // ---- verdicts ----------------------------------------------------------------
@@ -406,6 +418,8 @@ struct Verdict {
   u64 red[kWarps];
   float fred[kWarps];
   u64 sum;           // ... of the piece
+  u64 m;             // Residual's
+  int s;
   float top;
   int n;             // accepted drafts
 };
@@ -413,9 +427,22 @@ struct Verdict {
 IPD_DEVINL bool accepted(const Params &P, int t) {
   const int tok = P.a.tokens[t];
   if (tok < 0 || tok >= P.a.vocab) return false;
-  const Row p = P.rows[2 * t], q = P.rows[2 * t + 1];
-  return __dmul_rn(__dmul_rn((double)P.a.u_accept[t], (double)q.w), (double)p.z) <
-         __dmul_rn((double)p.w, (double)q.z);
+  const Row &p = P.rows[2 * t], &q = P.rows[2 * t + 1];
+  return __dmul_rn(__dmul_rn((double)P.a.u_accept[t], (double)q.w), (double)p.sum(P.pieces)) <
+         __dmul_rn((double)p.w, (double)q.sum(P.pieces));
+}
+
+// Log-probability of a drafted token.  (The sum in fp32 is off by 2^-24 of itself, log2f by
+// an ulp of a number no larger than the result.)
+IPD_DEVINL float logp_of(const Params &P, int row) {
+  const int tok = P.a.tokens[row >> 1];
+  if (tok < 0 || tok >= P.a.vocab) {
+    ipd_set_error(&g_draft_err, IPD_DEVERR_TOKEN);
+    return __uint_as_float(0x7fc00000u);
+  }
+  const Row &R = P.rows[row];
+  const u64 z = R.sum(P.pieces);
+  return z == 0 ? -INFINITY : (R.x - log2f((float)z * 0x1p-30f)) * kLn2;
 }
 
 // What a residual is taken from: the target's row and the draft's, and their ratio.
@@ -425,10 +452,10 @@ struct Residual {
   u64 m;       // 0: nothing is taken off
   int s, off;  // off: the draft row's entries lie this much further on in its vectors
 
-  // weights of the 8 entries of target vector i
-  IPD_DEVINL void eight(int i, uint32_t (&r)[8]) const {
-    const uint4 v = p.get(i);
-    uint4 o = v;
+  // target vector i, and the draft row's entries of the same ids
+  IPD_DEVINL void load(int i, uint4 &v, uint4 &o) const {
+    v = p.get(i);
+    o = v;
     if (m != 0) {
       if (off == 0) {
         o = q.get(i);
@@ -444,6 +471,9 @@ struct Residual {
         }
       }
     }
+  }
+  // their weights
+  IPD_DEVINL void eight(const uint4 &v, const uint4 &o, uint32_t (&r)[8]) const {
     if (wp.mode == kNear && wq.mode == kNear) {
       wp.eight<kNear>(v, r);
       if (m != 0) {
@@ -467,16 +497,27 @@ struct Residual {
     }
   }
   IPD_DEVINL void take(uint32_t (&r)[8], const uint32_t (&g)[8]) const {
+    const uint32_t mm = (uint32_t)m;
+    if (s >= 32) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const u64 less = (u64)g[e] * m >> s;
-      r[e] = less >= r[e] ? 0u : r[e] - (uint32_t)less;
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t less = __umulhi(g[e], mm) >> (s - 32);
+        r[e] = max(r[e], less) - less;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const u64 p = (u64)g[e] * mm;
+        const uint32_t hi = (uint32_t)(p >> 32), less = hi >> s ? 0xffffffffu : __funnelshift_r((uint32_t)p, hi, s);
+        r[e] = max(r[e], less) - less;
+      }
     }
   }
 };
 
-__global__ void __launch_bounds__(kThreads) draft_verdict_kernel(const __grid_constant__ Params P) {
+__global__ void __launch_bounds__(kThreads, 2) draft_verdict_kernel(const __grid_constant__ Params P) {
   __shared__ Verdict S;
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // what the row pass wrote
   const ipd_draft_args &a = P.a;
   const uint32_t csize = cluster_size(), rank = cluster_rank();
   const int r = blockIdx.x / csize, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -489,7 +530,19 @@ __global__ void __launch_bounds__(kThreads) draft_verdict_kernel(const __grid_co
       a.n_accept[r] = 0;
       a.next_token[r] = -1;
     }
+    if (spans && rank == 0)
+      for (int t = c0 + threadIdx.x; t < c1; t += kThreads) {
+        if (a.logp_target) a.logp_target[t] = __uint_as_float(0x7fc00000u);
+        if (a.logp_draft) a.logp_draft[t] = __uint_as_float(0x7fc00000u);
+      }
     return;
+  }
+  if (rank == csize - 1) {
+    for (int t = c0 + threadIdx.x; t < c1; t += kThreads) {
+      const float lp = logp_of(P, 2 * t), lq = logp_of(P, 2 * t + 1);
+      if (a.logp_target) a.logp_target[t] = lp;
+      if (a.logp_draft) a.logp_draft[t] = lq;
+    }
   }
   if (threadIdx.x == 0) S.n = c1 - c0;
   __syncthreads();
@@ -503,8 +556,22 @@ __global__ void __launch_bounds__(kThreads) draft_verdict_kernel(const __grid_co
   const bool full = n == c1 - c0;
   if (rank == 0 && threadIdx.x == 0) a.n_accept[r] = n;
   const int at = c0 + n;
-  const Row rp = full ? Row{} : P.rows[2 * at], rq = full ? Row{} : P.rows[2 * at + 1];
-  if (full ? !a.logits_bonus : rp.z == 0) {
+  float top = 0.f, top_q = 0.f;
+  if (!full) {
+    const Row &p = P.rows[2 * at], &q = P.rows[2 * at + 1];
+    top = p.top, top_q = q.top;
+    if (threadIdx.x == 0) {  // (the fp64 unit is narrow: once)
+      const u64 zp = p.sum(P.pieces), zq = q.sum(P.pieces);
+      S.m = 0, S.s = 0;
+      if (zp != 0 && zq != 0) {
+        int e;
+        const double f = frexp(__ddiv_rn((double)zp, (double)zq), &e);
+        S.m = (u64)(f * 0x1p31);
+        S.s = 31 - e;  // 13 .. 49
+      }
+    }
+  }
+  if (full ? !a.logits_bonus : top == -INFINITY) {
     if (rank == 0 && threadIdx.x == 0) a.next_token[r] = -1;
     return;
   }
@@ -513,38 +580,37 @@ __global__ void __launch_bounds__(kThreads) draft_verdict_kernel(const __grid_co
   const uint16_t *pq = full ? pp : a.logits_draft + (long long)at * a.draft_stride;
   const RowView vp(pp, a.vocab), vq(pq, a.vocab);
   const int from = min((int)rank * P.piece, vp.n_vec), to = min(from + P.piece, vp.n_vec);
-  float top = rp.top;
   if (full) {
     top = block_max(piece_max(vp, from, to), S.fred);
     if (csize > 1) {
       if (threadIdx.x == 0) S.top = top;
       cluster_sync();
-      for (uint32_t i = 0; i < csize; ++i) top = fmaxf(top, __uint_as_float(remote_ld(remote(&S.top, i))));
+      if (lane < (int)csize) top = __uint_as_float(remote_ld(remote(&S.top, lane)));
+      top = warp_max(top);
     }
   }
-  Residual D{vp, vq, Weigher(top, cp), Weigher(rq.top, cq), 0, 0, vq.before - vp.before};
-  if (!full && rq.z != 0) {
-    int e;
-    const double f = frexp(__ddiv_rn((double)rp.z, (double)rq.z), &e);
-    D.m = (u64)(f * 0x1p31);
-    D.s = 31 - e;  // 13 .. 49
-  }
+  __syncthreads();
+  Residual D{vp, vq, Weigher(top, cp), Weigher(top_q, cq), full ? 0ull : S.m, full ? 0 : S.s, vq.before - vp.before};
   // Sums of the tiles.  A second time with the target's weights alone where
   // nothing is left of them.
   const int tiles = (to - from + 31) / 32;
   u64 total = 0, before = 0;
   for (int round = 0; round < 2; ++round) {
     u64 mine = 0;
+    uint4 v, o;  // the next tile's, under way
+    if (from + warp * 32 + lane < to) D.load(from + warp * 32 + lane, v, o);
     for (int k = warp; k < tiles; k += kWarps) {
-      const int i = from + k * 32 + lane;
+      const int i = from + k * 32 + lane, ahead = i + kWarps * 32;
+      const uint4 v0 = v, o0 = o;
+      if (ahead < to) D.load(ahead, v, o);
       u64 s = 0;
       if (i < to) {
         uint32_t w[8];
-        D.eight(i, w);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s += w[e];
+        D.eight(v0, o0, w);
+        // (a weight is at most 2^30)
+        s = (u64)(w[0] + w[1] + w[2]) + (u64)(w[3] + w[4] + w[5]) + (u64)(w[6] + w[7]);
       }
-      s = warp_sum64(s);
+      s = warp_sum40(s);
       if (lane == 0) S.tile[k] = s, mine += s;
     }
     __syncthreads();  // (S.red is read by the round before)
@@ -553,11 +619,9 @@ __global__ void __launch_bounds__(kThreads) draft_verdict_kernel(const __grid_co
     if (csize > 1) {
       if (threadIdx.x == 0) S.sum = sum;
       cluster_sync();
-      total = 0;
-      for (uint32_t i = 0; i < csize; ++i) {
-        if (i == rank) before = total;
-        total += remote_ld64(&S.sum, i);
-      }
+      const u64 part = lane < (int)csize ? remote_ld64(&S.sum, lane) : 0ull;
+      total = warp_sum64(part);
+      before = warp_sum64(lane < (int)rank ? part : 0ull);
       cluster_sync();
     }
     if (total != 0 || D.m == 0) break;
@@ -595,7 +659,11 @@ __global__ void __launch_bounds__(kThreads) draft_verdict_kernel(const __grid_co
   left -= __shfl_sync(0xffffffffu, up - v, who);
   const int i = from + (k0 + who) * 32 + lane;
   uint32_t w[8] = {};
-  if (i < to) D.eight(i, w);
+  if (i < to) {
+    uint4 x, y;
+    D.load(i, x, y);
+    D.eight(x, y, w);
+  }
   v = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) v += w[e];
@@ -615,18 +683,21 @@ __global__ void __launch_bounds__(kThreads) draft_verdict_kernel(const __grid_co
 
 int g_sms[64];
 
-int launch(void (*kernel)(Params), int grid, int csize, int threads, int shared, const Params &P, cudaStream_t stream) {
+int launch(void (*kernel)(Params), int grid, int csize, int threads, int shared, bool follows, const Params &P,
+           cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid * csize);
   cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = (size_t)shared;
   cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = csize;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = csize;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = follows ? 2 : 1;  // begins as the kernel before ends, and waits for what that wrote
   if (cudaLaunchKernelEx(&cfg, kernel, P) != cudaSuccess) {
     (void)cudaGetLastError();
     return IPD_ERR_CUDA;
@@ -687,13 +758,14 @@ extern "C" int ipd_verify_draft(const ipd_draft_args *args, void *workspace,
     int c = kMaxCluster;
     while (c > 1 && (2LL * a.total * c > 4LL * sms || vecs < c * 512)) c /= 2;
     P.piece = (vecs + c - 1) / c;
+    P.pieces = c;
     const bool hist = P.piece * 8 >= kHistEntries;
     if (launch(hist ? draft_rows_kernel<true> : draft_rows_kernel<false>, 2 * a.total, c, hist ? kHistThreads : kPlainThreads,
-               hist ? kBins * 4 : 0, P, st) != IPD_OK)
+               hist ? kBins * 4 : 0, false, P, st) != IPD_OK)
       return IPD_ERR_CUDA;
   }
   int c = kMaxCluster;
-  while (c > 1 && ((long long)a.num_reqs * c > 4LL * sms || vecs < c * 512)) c /= 2;
+  while (c > 1 && ((long long)a.num_reqs * c > 2LL * sms || vecs < c * 512)) c /= 2;
   P.piece = (vecs + 32 * c - 1) / (32 * c) * 32;
-  return launch(draft_verdict_kernel, a.num_reqs, c, kThreads, 0, P, st);
+  return launch(draft_verdict_kernel, a.num_reqs, c, kThreads, 0, a.total > 0, P, st);
 }

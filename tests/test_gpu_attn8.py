@@ -139,6 +139,24 @@ def test_many_requests(lib):
     _check(c)
 
 
+@pytest.mark.parametrize("hq,hkv,q_hi,n,lo,hi", [(16, 8, 1, 60, 1500, 5000), (32, 4, 16, 50, 200, 4000), (8, 8, 9, 40, 100, 3000),
+                                                 (12, 2, 14, 90, 1, 2600), (16, 8, 1, 500, 100, 900)])
+def test_many_long_requests(lib, hq, hkv, q_hi, n, lo, hi):
+    """Several tasks a CTA of more tiles than any ring holds, of every number of
+    warpgroups; the same bytes again and again."""
+    g = torch.Generator().manual_seed(hq)
+    length = torch.randint(lo, hi + 1, (n,), generator=g).tolist()
+    q_len = [min(int(x), m) for x, m in zip(torch.randint(0 if q_hi > 1 else 1, q_hi + 1, (n,), generator=g), length)]
+    c = Case(hq, hkv, q_len, length, seed=n)
+    _run(lib, c)
+    _check(c)
+    first = c.out.clone()
+    for _ in range(5):
+        _run(lib, c)
+        assert torch.equal(c.out, first)
+    assert lib.device_error() == 0
+
+
 def test_several_batches_in_one_call(lib):
     """Spans over two caches and decode tokens over both, and a batch without
     queries: the same bytes as one call each."""

@@ -1,7 +1,9 @@
 """Verification of drafted tokens on the GPU (needs a GB300): verdicts and tokens
-equal to the definition's in whole numbers; log-probabilities to 2^-21 of
-themselves plus 2^-21 (one fp32 rounding, 2^-24 relative; x itself is exact, and
-the weights' sum is off by at most 2^-22 from the softmax's: 1.9e-7 a weight)."""
+equal to the definition's in whole numbers; log-probabilities ln 2 (x - log2 Z),
+in fp32, to 2^-21 of themselves plus 2^-21: Z is off by 2^-24 of itself, its log2 by
+2^-23 of a number no larger than the difference (x <= 0), the difference, the factor
+and the product by 2^-24 each, x by one rounding that the definition has too:
+2^-22.4 of the result and 2^-24 in all."""
 import numpy as np
 import pytest
 import torch
@@ -192,7 +194,7 @@ def test_without_log_probabilities_and_captured(lib):
     assert list(zip(c.n.tolist(), c.nxt.tolist())) == want
     args = [t.cuda() for t in (c.target, c.draft, c.tokens, c.cu, c.u, c.u_next)]
     n, nxt = (torch.zeros(3, dtype=torch.int32, device="cuda") for _ in "ab")
-    ws = torch.empty(256, dtype=torch.uint8, device="cuda")
+    ws = torch.empty(lib.verify_draft_workspace_size(3, 6, 2000), dtype=torch.uint8, device="cuda")
     bonus, ip, iq = c.bonus.cuda(), c.inv_p.cuda(), c.inv_q.cuda()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
