@@ -64,14 +64,15 @@ constexpr int kBlockRows = 128;           // rows of a task
 constexpr int kGroups = 4;                // softmax warpgroups
 constexpr int kRows = 32;                 // ... and the rows of one
 constexpr int kKStages = 3, kVStages = 4;
-constexpr int kMeta = 16;                  // tiles whose page ids and scales are at hand
+constexpr int kTiles = 16;                // tiles handed out whose product is not complete
+constexpr int kScales = 16;
 constexpr int kBatch = 4;                 // ... fetched at once
-constexpr int kSlots = 5;                 // items handed out
+constexpr int kSlots = 8;                 // items handed out
 constexpr int kSoftmaxWarps = 4 * kGroups;
 constexpr int kKWarp = kSoftmaxWarps, kVWarp = kKWarp + 1, kQkWarp = kKWarp + 2, kPvWarp = kKWarp + 3,
               kItemWarp = kKWarp + 4, kPageWarp = kKWarp + 5, kQWarps = 2;
 constexpr int kThreads = 32 * (kSoftmaxWarps + 6 + kQWarps);
-constexpr int kItemReaders = kSoftmaxWarps + 5 + kQWarps;
+constexpr int kItemReaders = kSoftmaxWarps + 1 + kQWarps;
 constexpr int kQUnits = 8;                // query tiles of 32 rows at hand
 constexpr int kRegsLaunch = 80, kRegsSoftmax = 96, kRegsAux = 48;
 static_assert(32 * kSoftmaxWarps * kRegsSoftmax + 256 * kRegsAux <= kThreads * kRegsLaunch,
@@ -127,11 +128,31 @@ struct Item {
   int cta0, ctab, cta1; // the CTAs of the task: cta0, then ctab .. cta1
 };
 
-struct Meta {
+// A tile on its way through the loading and issuing warps.
+enum { kFirst = 1, kLast = 2, kHides = 4, kEnd = 8 };
+struct Tile {
+  int y[kPages];  // first pool rows of its pages
+  uint32_t what;  // the rest in one word, which one warp-wide move makes uniform:
+  // its item's first, last; it holds hidden keys; there is none after the one before (4 bits);
+  // warpgroups (3), the first of them (2), 32 rows each or 16 (1), first query tile (3),
+  // the item's place in this CTA's order (4: slot and turn), batch (3)
+};
+static_assert(2 * kSlots == 16 && kQUnits == 8 && kGroups == 4 && IPD_MAX_BATCHES <= 8, "the fields of Tile::what");
+struct What {
+  uint32_t w;
+  IPD_DEVINL bool is(int flag) const { return w & flag; }
+  IPD_DEVINL int ng() const { return w >> 4 & 7u; }
+  IPD_DEVINL int wg() const { return w >> 7 & 3u; }
+  IPD_DEVINL int nr() const { return 16u << (w >> 9 & 1u); }
+  IPD_DEVINL uint32_t qu() const { return w >> 10 & 7u; }
+  IPD_DEVINL uint32_t item() const { return w >> 13 & 15u; }
+  IPD_DEVINL int b() const { return w >> 17 & 7u; }
+};
+// ... and what a warpgroup has to know of it.
+struct Scales {
   float ck[kPages];  // K's scale times the softmax scale, in log2
   int ev[kPages];    // V's exponent (128: NaN), or kNoPage
-  int y[kPages];     // first pool row of the page
-  int gap;           // a page that is not there lies among the keys
+  int gap, v;        // a page that is not there lies among the keys; V's stage
 };
 
 struct Shared {
@@ -149,13 +170,15 @@ struct Shared {
   int nan_key[kGroups][kD], bad[kGroups];
   int last[kGroups], abort;
   uint32_t tmem;
-  Meta meta[kMeta];
+  Tile tile[kTiles];
+  Scales scales[kGroups][kScales];
   Item item[kSlots];
   uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
-  uint64_t pg_full[kMeta], sc_full[kMeta], meta_empty[kMeta];
+  uint64_t tile_full[kTiles], tile_empty[kTiles];
+  uint64_t sc_full[kGroups][kScales], sc_empty[kGroups][kScales];
   uint64_t q_full[kSlots], q_empty[kQUnits], s_full[kGroups], s_empty[kGroups], p_full[kGroups], pv_done[kGroups];
-  uint64_t v_ready[kGroups], mended[kGroups];  // a tile with hidden keys has landed, and has been looked through
-  uint64_t item_full[kSlots], item_empty[kSlots], pair[2], all, drain[2];
+  uint64_t v_ready[kGroups];  // a tile with hidden keys has landed
+  uint64_t item_full[kSlots], item_taken[kSlots], item_empty[kSlots], pair[2], all, drain[2];
 };
 constexpr int kSharedBytes = (int)sizeof(Shared) + 1024;  // the base is aligned by hand
 static_assert(kSharedBytes <= 232448, "shared memory of one CTA");
@@ -397,7 +420,7 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
   const long long W = P.prefix[P.total_reqs];
   // (a part is no shorter than a tile, so that none between a task's ends has no tile)
   const long long C = max(1LL, min((long long)gridDim.x, W / P.prefix[P.total_reqs + 1]));
-  uint32_t n = 0, turn = 0, unit = 0;
+  uint32_t n = 0, unit = 0;
   const long long lo = blockIdx.x < C ? blockIdx.x * W / C : W, hi = blockIdx.x < C ? (blockIdx.x + 1) * W / C : W;
   int g = 0;
   if (lo < hi) {
@@ -442,15 +465,12 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
         if (!wait(&S.item_empty[slot], free_(n, kSlots), &S.abort)) return;
         const int row0 = block * kBlockRows, rows = min(kBlockRows, rows_all - row0);
         const int ng = rows > 64 ? 4 : rows > 32 ? 2 : 1;
-        // the warpgroups take items in turn, those of two or four together, and so do
-        // the query tiles
-        const int wg = (int)((turn + ng - 1) & (uint32_t)(kGroups - ng));
         const int qu = (int)((unit + ng - 1) & (uint32_t)(kQUnits - ng));
-        turn = wg + ng, unit = qu + ng;
+        unit = qu + ng;
         if (lane == 0) {
           Item &I = S.item[slot];
           I.valid = 1, I.b = b, I.c0 = info.z, I.n = info.y, I.L = L, I.h = h;
-          I.row0 = row0, I.rows = rows, I.nr = rows > 16 ? 32 : 16, I.ng = ng, I.wg = wg, I.qu = qu;
+          I.row0 = row0, I.rows = rows, I.nr = rows > 16 ? 32 : 16, I.ng = ng, I.qu = qu;
           I.t0 = t0, I.t1 = t1;
           I.masked = L - info.y + 1 + row0 / group;
           I.r = g - P.req_base[b], I.n_pages = (L + kPage - 1) / kPage;
@@ -481,68 +501,167 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
   }
 }
 
-// ---- page ids and scales (one warp) ---------------------------------------------------
-// Batches of up to four tiles, a lane a page.  While a batch's scales are under way, so are
-// the next one's page ids, of this item or the next.
+// ---- the order of tiles, page ids and scales (one warp) -------------------------------
+// Items are taken in order, each as soon as there is a warpgroup for it (two, four) that has
+// been given all its tiles, and the items under way get a tile each in turn: up to four
+// softmaxes run side by side, and one item's end is hidden behind the others' tiles.
+// Tiles go out four at a time, a lane a page: while a batch's scales are under way, so are
+// the next one's page ids.
+IPD_DEVINL bool mbar_test(uint64_t *bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 __device__ void page_warp(const Params &P, Shared &S, int lane) {
-  const int mine = lane / kPages;
-  uint32_t n = 0, it = 0;  // items begun; tiles handed out
-  // the batch whose ids are under way, and what is known of it
-  int slot = 0, t = 0, t1 = 0, id = -1, left = 0;
-  const auto fetch = [&]() {  // ids of the next batch; false: there is none
-    if (t >= t1) {
-      slot = n % kSlots;
-      if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) return false;
-      const Item &I = S.item[slot];
-      if (!I.valid) return false;
+  const int mine = lane / kPages, place = lane % kPages;  // a lane's tile of a batch, and page
+  uint32_t n = 0, it = 0;    // items taken; tiles handed out
+  int known = 0, units = 0;  // warpgroups that item n wants (0: it has not been looked at), its query tiles
+  bool ended = false, given_up = false;
+  int last_g = kGroups - 1;
+  // lane g < 4: what warpgroup g has been given: the item, its next tile and its end, the
+  // first of its warpgroups, its query tiles; how many tiles the warpgroup has had
+  int w_item = 0, w_t = 0, w_t1 = 0, w_first = 0, w_units = 0;
+  uint32_t w_tiles = 0;
+  // the batch whose ids are under way: a lane's item, tile, first warpgroup, how many tiles
+  // before it are that item's; w_tiles before the batch
+  int e_item = 0, e_t = 0, e_g = 0, e_q = 0, id = -1, left = 0;
+  uint32_t e_tiles = 0;
+
+  // The next batch: left = 0 where there is none, or none yet.  May wait for an item only where
+  // `block`: with tiles in hand that have not gone out, the item could be waiting for theirs to end.
+  const auto fetch = [&](bool block) {
+    left = 0, id = -1;
+    uint32_t act;  // first warpgroups of the items under way
+    while (true) {
+      const bool active = lane < kGroups && w_t < w_t1;
+      const uint32_t busy = __ballot_sync(0xffffffffu, active);
+      act = __ballot_sync(0xffffffffu, active && w_first == lane);
+      if (ended) break;
+      const int slot = n % kSlots;
+      if (known == 0) {
+        // (items under way go on while the next one is not there yet)
+        if (act || !block) {
+          if (!__all_sync(0xffffffffu, mbar_test(&S.item_full[slot], full(n, kSlots)))) break;
+        } else if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort, 20)) {
+          given_up = true;
+          return;
+        }
+        if (!S.item[slot].valid) {
+          ended = true;
+          break;
+        }
+        known = S.item[slot].ng;
+        units = ((1 << known) - 1) << S.item[slot].qu;
+      }
+      // (its query tiles must be those of no item under way: the products, which go by the
+      // order of tiles, would wait for queries that wait for that item's last product)
+      if (__any_sync(0xffffffffu, active && (w_units & units))) break;
+      int g = -1;
+#pragma unroll
+      for (int k = kGroups; k >= 1; --k) {  // the next after the one that had a tile last
+        const int at = (last_g + k) & (kGroups - known);
+        if ((busy >> at & ((1u << known) - 1u)) == 0) g = at;
+      }
+      if (g < 0) break;
+      if (lane == 0) {
+        S.item[slot].wg = g;
+        mbar_arrive(&S.item_taken[slot]);
+      }
+      if (lane >= g && lane < g + known)
+        w_item = (int)n, w_t = S.item[slot].t0, w_t1 = S.item[slot].t1, w_first = g, w_units = units;
       ++n;
-      t = I.t0, t1 = I.t1;
+      known = 0;
     }
-    const Item &I = S.item[slot];
-    const int page = t * kPages + lane;
-    left = min(kBatch, t1 - t);
-    id = -1;
-    if (page < I.n_pages && mine < left) {
-      const BatchDev &B = P.b[I.b];
+    if (act == 0) return;
+    // the items under way in turn, a tile each, and again
+    const int some = __popc(act), turn = mine % some;
+    uint32_t bits = (act | act << kGroups) >> (last_g + 1) & ((1u << kGroups) - 1u);
+    for (int i = 0; i < turn; ++i) bits &= bits - 1;
+    int g = (last_g + __ffs(bits)) & (kGroups - 1), q = mine / some;
+    int t = __shfl_sync(0xffffffffu, w_t, g) + q;
+    const uint32_t past = __ballot_sync(0xffffffffu, t >= __shfl_sync(0xffffffffu, w_t1, g));
+    left = past ? (__ffs(past) - 1) / kPages : kBatch;
+    // (the lanes of tiles past an end do as the last one's do)
+    const int from = min(mine, left - 1) * kPages + place;
+    e_g = __shfl_sync(0xffffffffu, g, from), e_t = __shfl_sync(0xffffffffu, t, from), e_q = __shfl_sync(0xffffffffu, q, from);
+    e_item = __shfl_sync(0xffffffffu, w_item, e_g);
+    e_tiles = w_tiles;
+    last_g = __shfl_sync(0xffffffffu, e_g, 31);
+    int given = 0;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) given += i < left && __shfl_sync(0xffffffffu, e_g, i * kPages) == w_first;
+    if (lane < kGroups && w_t < w_t1) w_t += given, w_tiles += given;
+    const Item &I = S.item[e_item % kSlots];
+    const BatchDev &B = P.b[I.b];
+    const int page = e_t * kPages + place;
+    if (page < I.n_pages) {
       id = B.page_table[(size_t)I.r * B.max_pages + page];
       if (id < 0 || id >= B.num_pages) {
         ipd_set_error(&g_attn8_err, IPD_DEVERR_PAGE_ID);
         id = -2;
       }
     }
-    return true;
   };
-  bool more = fetch();
-  while (more) {
-    const Item &I = S.item[slot];
+  while (true) {
+    if (left == 0) {
+      fetch(true);
+      if (left == 0) break;
+    }
+    const int now = left, item = e_item, t = e_t, g = e_g, q = e_q;
+    const uint32_t tiles = e_tiles, at = it + min(mine, now - 1);
+    const bool leads = mine < now && place == 0;
+    const Item &I = S.item[item % kSlots];
     const BatchDev &B = P.b[I.b];
-    const int now = left;
-    const bool last = t + now >= t1;
-    const uint32_t used = slot;
-    const bool ok = id >= 0;
-    const size_t cell = (size_t)(ok ? id : 0) * B.hkv + I.h;
+    const int ng = I.ng;
+    const bool ok = id >= 0, last = t + 1 == I.t1;
+    const size_t cell = ok ? (size_t)id * B.hkv + I.h : 0;
     const uint32_t kb = ok ? B.ks[cell] : 127u, vb = ok ? B.vs[cell] : 127u;
-    for (int i = 0; i < now; ++i) {
-      const uint32_t m = (it + i) % kMeta;
-      if (!wait(&S.meta_empty[m], free_(it + i, kMeta), &S.abort)) return;
-      const uint32_t gap = __ballot_sync(0xffffffffu, mine == i && id == -2);
-      if (mine == i) S.meta[m].y[lane % kPages] = ok ? (int)cell * kPage : B.rows_end;
-      if (lane == 0) S.meta[m].gap = gap != 0;
-      arrive_warp(&S.pg_full[m], lane);
+    const uint32_t gaps = __ballot_sync(0xffffffffu, id == -2);
+    // (every lane waits for its own tile's barriers)
+    if (!wait(&S.tile_empty[at % kTiles], free_(at, kTiles), &S.abort)) return;
+    Tile &T = S.tile[at % kTiles];
+    if (mine < now) T.y[place] = ok ? (int)cell * kPage : B.rows_end;
+    if (leads) {
+      T.what = (t == I.t0 ? kFirst : 0) | (last ? kLast : 0) | ((t + 1) * kKeys > I.masked ? kHides : 0) | ng << 4 | g << 7 |
+               (I.nr >> 5) << 9 | I.qu << 10 | (item & 15) << 13 | I.b << 17;
     }
-    t += now;
-    more = fetch();
-    for (int i = 0; i < now; ++i) {
-      const uint32_t m = (it + i) % kMeta;
-      if (mine == i) {
-        S.meta[m].ck[lane % kPages] = e8m0(kb) * P.scale_log2;
-        S.meta[m].ev[lane % kPages] = ok ? (int)vb - 127 : kNoPage;
+    __syncwarp();
+    if (leads) mbar_arrive(&S.tile_full[at % kTiles]);
+    __syncwarp();
+    fetch(false);
+    const int most = __reduce_max_sync(0xffffffffu, ng);
+    for (int j = 0; j < most; ++j) {
+      const int to = g + min(j, ng - 1);
+      const uint32_t k = __shfl_sync(0xffffffffu, tiles, to) + q;
+      if (!wait(&S.sc_empty[to][k % kScales], free_(k, kScales), &S.abort, 20)) return;
+      Scales &C = S.scales[to][k % kScales];
+      if (mine < now && j < ng) {
+        C.ck[place] = e8m0(kb) * P.scale_log2;
+        C.ev[place] = ok ? (int)vb - 127 : kNoPage;
+        if (place == 0) C.gap = (gaps >> (mine * kPages) & 0xffu) != 0, C.v = (int)(at % kVStages);
       }
-      arrive_warp(&S.sc_full[m], lane);
+      __syncwarp();
+      if (leads && j < ng) mbar_arrive(&S.sc_full[to][k % kScales]);
     }
+    if (leads && last) mbar_arrive(&S.item_empty[item % kSlots]);
     it += now;
-    if (last) arrive_warp(&S.item_empty[used], lane);
   }
+  if (given_up) return;
+  const uint32_t m = it % kTiles;
+  if (!wait(&S.tile_empty[m], free_(it, kTiles), &S.abort)) return;
+  if (lane == 0) {
+    S.tile[m].what = kEnd;
+    // and the softmax warps hear of the end
+    mbar_arrive(&S.item_taken[n % kSlots]);
+  }
+  arrive_warp(&S.tile_full[m], lane);
 }
 
 // ---- loads -------------------------------------------------------------------------
@@ -553,28 +672,22 @@ __device__ void load_warp(const Params &P, Shared &S, int lane) {
   uint8_t *ring = kIsV ? S.v[0] : S.k[0];
   const uint64_t policy = l2_policy_evict_first();
   uint32_t it = 0;
-  for (uint32_t n = 0;; ++n) {
-    const int slot = n % kSlots;
-    if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) break;
-    const Item &I = S.item[slot];
-    if (!uniform(I.valid)) return;
-    const int b = uniform(I.b), tiles = uniform(I.t1 - I.t0);
+  for (;; ++it) {
+    const uint32_t m = it % kTiles, s = it % kRing;
+    if (!wait(&S.tile_full[m], full(it, kTiles), &S.abort, 40)) break;
+    const Tile &T = S.tile[m];
+    const What what{(uint32_t)uniform((int)T.what)};
+    if (what.is(kEnd)) return;
+    if (!wait(&empties[s], free_(it, kRing), &S.abort, 40)) break;
+    const int b = what.b();
     const CUtensorMap *map = kIsV ? &P.v[b] : &P.k[b];
-    bool ok = true;
-    for (int t = 0; t < tiles; ++t, ++it) {
-      const uint32_t m = it % kMeta, s = it % kRing;
-      ok = wait(&S.pg_full[m], full(it, kMeta), &S.abort) && wait(&empties[s], free_(it, kRing), &S.abort);
-      if (!ok) break;
-      if (elect_one()) {
-        mbar_arrive_expect_tx(&fulls[s], kTileBytes);
+    if (elect_one()) {
+      mbar_arrive_expect_tx(&fulls[s], kTileBytes);
 #pragma unroll 1
-        for (int i = 0; i < kPages; ++i)
-          tma_load_2d(ring + s * kTileBytes + i * kPageBytes, map, 0, S.meta[m].y[i], &fulls[s], policy);
-      }
-      __syncwarp();
+      for (int i = 0; i < kPages; ++i)
+        tma_load_2d(ring + s * kTileBytes + i * kPageBytes, map, 0, T.y[i], &fulls[s], policy);
     }
-    if (!ok) break;
-    arrive_warp(&S.item_empty[slot], lane);
+    __syncwarp();
   }
   // given up: the copies in flight land first
   for (uint32_t k = it > (uint32_t)kRing ? it - kRing : 0; k < it; ++k) {
@@ -601,42 +714,36 @@ __device__ void qk_warp(Shared &S, int lane) {
   const uint64_t k0 = sdesc((uint32_t)uniform((int)smem_u32(S.k[0])), 128),
                  q0 = sdesc((uint32_t)uniform((int)smem_u32(S.q[0][0])), 128);
   constexpr uint64_t kUnit = kRows * kD >> 4, kTerm = kQUnits * kUnit;  // in descriptors
-  uint32_t it = 0, uses = 0;  // (a bit a warpgroup: parity of its uses)
-  for (uint32_t n = 0;; ++n) {
-    const int slot = n % kSlots;
-    if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) break;
-    const Item &I = S.item[slot];
-    if (!uniform(I.valid)) return;
-    const int tiles = uniform(I.t1 - I.t0), ng = uniform(I.ng);
-    const uint32_t idesc = idesc_f8(uniform(I.nr) * ng, 0), qu = (uint32_t)uniform(I.qu);
-    const uint32_t g0 = (uint32_t)uniform(I.wg);
-    bool ok = wait(&S.q_full[slot], full(n, kSlots), &S.abort);
-    const uint64_t q = q0 + qu * kUnit;
-    for (int t = 0; ok && t < tiles; ++t, ++it) {
-      const uint32_t s = it % kKStages;
-      ok = wait(&S.k_full[s], full(it, kKStages), &S.abort, 40);
-      for (int i = 0; ok && i < ng; ++i) ok = wait(&S.s_empty[g0 + i], (uses >> (g0 + i) & 1u) ^ 1u, &S.abort, 40);
-      if (!ok) break;
-      uses ^= ((1u << ng) - 1u) << g0;
-      tc_fence_after();
-      const uint64_t k = k0 + (uint64_t)(s * (kTileBytes >> 4));
-      const uint32_t d = tmem + col_s(g0);
-      if (elect_one()) {
-#pragma unroll
-        for (int kk = 0; kk < kD / 32; ++kk) {
-          tc_mma_f8(d, k + 2 * kk, q + 2 * kk, idesc, kk != 0);
-          tc_mma_f8(d, k + 2 * kk, q + kTerm + 2 * kk, idesc, 1);
-        }
-#pragma unroll 1
-        for (int i = 0; i < ng; ++i) tc_commit(&S.s_full[g0 + i]);
-        tc_commit(&S.k_empty[s]);
-      }
-      __syncwarp();
-      if (t == tiles - 1)
-        for (int i = 0; i < ng; ++i) commit(&S.q_empty[qu + i]);
-    }
+  uint32_t uses = 0;  // (a bit a warpgroup: parity of its uses)
+  for (uint32_t it = 0;; ++it) {
+    const uint32_t m = it % kTiles, s = it % kKStages;
+    if (!wait(&S.tile_full[m], full(it, kTiles), &S.abort, 40)) break;
+    const What what{(uint32_t)uniform((int)S.tile[m].what)};
+    if (what.is(kEnd)) return;
+    const int ng = what.ng(), g0 = what.wg();
+    const uint32_t idesc = idesc_f8(what.nr() * ng, 0), qu = what.qu(), item = what.item();
+    bool ok = true;
+    if (what.is(kFirst)) ok = wait(&S.q_full[item % kSlots], full(item, kSlots), &S.abort, 40);
+    for (int i = 0; ok && i < ng; ++i) ok = wait(&S.s_empty[g0 + i], (uses >> (g0 + i) & 1u) ^ 1u, &S.abort, 40);
+    ok = ok && wait(&S.k_full[s], full(it, kKStages), &S.abort, 40);
     if (!ok) break;
-    arrive_warp(&S.item_empty[slot], lane);
+    uses ^= ((1u << ng) - 1u) << g0;
+    tc_fence_after();
+    const uint64_t k = k0 + (uint64_t)(s * (kTileBytes >> 4)), q = q0 + qu * kUnit;
+    const uint32_t d = tmem + col_s(g0);
+    if (elect_one()) {
+#pragma unroll
+      for (int kk = 0; kk < kD / 32; ++kk) {
+        tc_mma_f8(d, k + 2 * kk, q + 2 * kk, idesc, kk != 0);
+        tc_mma_f8(d, k + 2 * kk, q + kTerm + 2 * kk, idesc, 1);
+      }
+#pragma unroll 1
+      for (int i = 0; i < ng; ++i) tc_commit(&S.s_full[g0 + i]);
+      tc_commit(&S.k_empty[s]);
+    }
+    __syncwarp();
+    if (what.is(kLast))
+      for (int i = 0; i < ng; ++i) commit(&S.q_empty[qu + i]);
   }
   drain(&S.drain[0], lane);
 }
@@ -644,49 +751,41 @@ __device__ void qk_warp(Shared &S, int lane) {
 __device__ void pv_warp(Shared &S, int lane) {
   const uint32_t tmem = (uint32_t)uniform((int)S.tmem);
   const uint64_t v0 = sdesc((uint32_t)uniform((int)smem_u32(S.v[0])), 128);
-  uint32_t it = 0, uses = 0, mends = 0;  // (a bit a warpgroup: parity of its uses)
-  for (uint32_t n = 0;; ++n) {
-    const int slot = n % kSlots;
-    if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) break;
-    const Item &I = S.item[slot];
-    if (!uniform(I.valid)) return;
-    const int tiles = uniform(I.t1 - I.t0), ng = uniform(I.ng), nr = uniform(I.nr);
-    const int hides = uniform(I.masked / kKeys - I.t0);  // tiles from here on have hidden keys
-    const uint32_t idesc = idesc_f8(2 * nr, 1);
-    const uint64_t p0 = sdesc((uint32_t)uniform((int)smem_u32(S.p[0])), 2 * nr);
+  const uint32_t p_addr = (uint32_t)uniform((int)smem_u32(S.p[0]));
+  uint32_t uses = 0;  // (a bit a warpgroup: parity of its uses)
+  for (uint32_t it = 0;; ++it) {
+    const uint32_t m = it % kTiles, s = it % kVStages;
+    if (!wait(&S.tile_full[m], full(it, kTiles), &S.abort, 40)) break;
+    const What what{(uint32_t)uniform((int)S.tile[m].what)};
+    if (what.is(kEnd)) return;
+    const int ng = what.ng(), g0 = what.wg(), nr = what.nr();
+    const uint32_t idesc = idesc_f8(2 * nr, 1), begun = what.is(kFirst) ? 0u : 1u;  // (an item's first tile overwrites O)
+    const uint64_t p0 = sdesc(p_addr, 2 * nr);
     const uint64_t step = (uint64_t)(32 * 2 * nr >> 4);  // 32 keys of P further on
-    const uint32_t g0 = (uint32_t)uniform(I.wg);
-    bool ok = true;
-    for (int t = 0; t < tiles; ++t, ++it) {
-      const uint32_t s = it % kVStages;
-      ok = wait(&S.v_full[s], full(it, kVStages), &S.abort, 40);
-      const uint64_t v = v0 + (uint64_t)(s * (kTileBytes >> 4));
-      for (int i = 0; ok && i < ng; ++i) {
-        const uint32_t g = g0 + i;
-        ok = wait(&S.p_full[g], uses >> g & 1u, &S.abort, 40);
-        if (ok && i == 0 && t >= hides) {
-          if (lane == 0) mbar_arrive(&S.v_ready[g]);
-          ok = wait(&S.mended[g], mends >> g & 1u, &S.abort, 40);
-          mends ^= 1u << g;
-        }
-        if (!ok) break;
-        tc_fence_after();
-        const uint64_t p = p0 + (uint64_t)(g * (uint32_t)(sizeof(S.p[0]) >> 4));
-        if (elect_one()) {
-#pragma unroll
-          for (int kk = 0; kk < kKeys / 32; ++kk)
-            tc_mma_f8(tmem + col_o(g), v + (uint64_t)(kk * 32 * kD >> 4), p + kk * step, idesc, t != 0 || kk != 0);
-          tc_commit(&S.pv_done[g]);
-        }
-        __syncwarp();
-      }
+    bool ok = wait(&S.v_full[s], full(it, kVStages), &S.abort, 40);
+    const uint64_t v = v0 + (uint64_t)(s * (kTileBytes >> 4));
+    for (int i = 0; ok && i < ng; ++i) {
+      const uint32_t g = g0 + i;
+      // (hidden keys: the first warpgroup looks the tile through before its weights count as there)
+      if (i == 0 && what.is(kHides) && lane == 0) mbar_arrive(&S.v_ready[g]);
+      ok = wait(&S.p_full[g], uses >> g & 1u, &S.abort, 40);
       if (!ok) break;
-      uses ^= ((1u << ng) - 1u) << g0;
-      commit(&S.v_empty[s]);
-      commit(&S.meta_empty[it % kMeta]);
+      tc_fence_after();
+      const uint64_t p = p0 + (uint64_t)(g * (uint32_t)(sizeof(S.p[0]) >> 4));
+      if (elect_one()) {
+#pragma unroll
+        for (int kk = 0; kk < kKeys / 32; ++kk)
+          tc_mma_f8(tmem + col_o(g), v + (uint64_t)(kk * 32 * kD >> 4), p + kk * step, idesc, begun | (kk != 0));
+        tc_commit(&S.pv_done[g]);
+        if (i == ng - 1) {
+          tc_commit(&S.v_empty[s]);
+          tc_commit(&S.tile_empty[m]);
+        }
+      }
+      __syncwarp();
     }
     if (!ok) break;
-    arrive_warp(&S.item_empty[slot], lane);
+    uses ^= ((1u << ng) - 1u) << g0;
   }
   drain(&S.drain[1], lane);
 }
@@ -779,7 +878,7 @@ IPD_DEVINL float column_reduce(float (&a)[16], int lane, Op op) {
 
 struct Softmax {
   int g, tid, warp, lane;  // warpgroup, and place in it
-  uint32_t tiles, it;      // own tiles so far, tiles of the CTA so far
+  uint32_t tiles;          // own tiles so far
   uint32_t mends;          // tiles looked through so far
   uint32_t pairs, alls;    // barriers of two and of all warpgroups so far
   bool ok;                 // no wait of this warp has given up
@@ -789,7 +888,15 @@ struct Softmax {
 // rows that do not see the key (0 x NaN), so they become 0, and rows that do see
 // it get them back at the end.
 IPD_DEVINL void mend(Shared &S, int set, uint8_t *v, int key_in_tile, int key, int L) {
-  bool wrote = false;
+  const uint4 *row = reinterpret_cast<const uint4 *>(v + key_in_tile * kD);
+  uint32_t any = 0;  // bit 7 of a byte: one of its like was 0x7f or 0xff
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint4 x = row[(i + key_in_tile) & 7];
+    any |= (x.x & 0x7f7f7f7fu) + 0x01010101u | (x.y & 0x7f7f7f7fu) + 0x01010101u | (x.z & 0x7f7f7f7fu) + 0x01010101u |
+           (x.w & 0x7f7f7f7fu) + 0x01010101u;
+  }
+  if ((any & 0x80808080u) == 0) return;
 #pragma unroll 1
   for (int i = 0; i < 32; ++i) {
     const int c = ((i >> 2) + key_in_tile) & 7, at = c * 16 + (i & 3) * 4;
@@ -807,9 +914,7 @@ IPD_DEVINL void mend(Shared &S, int set, uint8_t *v, int key_in_tile, int key, i
       }
     __threadfence_block();  // noted before it is gone
     *w = x;
-    wrote = true;
   }
-  if (wrote) fence_proxy_async_smem();
 }
 
 // Exponents of the rows (in pairs) at a thread's key, against their references.
@@ -932,13 +1037,10 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
   bool first = true;
 #pragma unroll 1
   for (int t = 0; t < n_tiles; ++t) {
-    const uint32_t it = X.it + t;
-    const uint32_t m = it % kMeta;
-    // (first the scores: the tile may be many turns of the ring of scales ahead, which tells
-    // one turn from the next only)
-    X.ok = wait_inline(&S.s_full[g], full(X.tiles, 1), &S.abort) && X.ok;
-    X.ok = wait_inline(&S.sc_full[m], full(it, kMeta), &S.abort) && X.ok;
-    const Meta &M = S.meta[m];
+    const uint32_t k = X.tiles % kScales;
+    X.ok = wait_inline(&S.sc_full[g][k], full(X.tiles, kScales), &S.abort) && X.ok;
+    const Scales &M = S.scales[g][k];
+    const int v_stage = M.v & (kVStages - 1);  // (in range whatever a warp that gave up has left)
     const int key0 = (I.t0 + t) * kKeys, key = key0 + tid;
     const float ck = M.ck[tid / kPage];
     const int ev = M.ev[tid / kPage];
@@ -957,6 +1059,8 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
       if (hidden == NR) de = 0;
     }
     const float fk = ev == 128 && hidden < NR ? __uint_as_float(0x7fc00000u) : pow2i(de);
+    arrive_warp(&S.sc_empty[g][k], lane);
+    X.ok = wait_inline(&S.s_full[g], full(X.tiles, 1), &S.abort) && X.ok;
     tc_fence_after();
     u64 y[NR / 2];
     {
@@ -1032,18 +1136,17 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
 #pragma unroll 1
         for (int k = i; k < 2 * NR; k += NR) prow[(((k >> 4) ^ turn) << 4) + (k & 15)] = 0;
     }
+    if (key0 + kKeys > masked && g == I.wg) {
+      // hidden keys: the tile is looked through before the product, which takes the first
+      // warpgroup's rows before the others'
+      X.ok = wait_inline(&S.v_ready[g], full(X.mends, 1), &S.abort) && X.ok;
+      ++X.mends;
+      if (key >= masked) mend(S, g, S.v[v_stage], tid, key, L);
+    }
     fence_proxy_async_smem();
     tc_wait_st();
     tc_fence_before();
     arrive_warp(&S.p_full[g], lane);
-    if (key0 + kKeys > masked && g == I.wg) {
-      // hidden keys: the product waits until the tile has been looked through (it takes
-      // the first warpgroup's rows before the others')
-      X.ok = wait_inline(&S.v_ready[g], full(X.mends, 1), &S.abort) && X.ok;
-      ++X.mends;
-      if (key >= masked) mend(S, g, S.v[it % kVStages], tid, key, L);
-      arrive_warp(&S.mended[g], lane);
-    }
     ++X.tiles;
     first = false;
   }
@@ -1184,15 +1287,14 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
 }
 
 __device__ void softmax_warps(const Params &P, Shared &S, int warp, int lane) {
-  Softmax X{warp >> 2, (int)threadIdx.x & 127, warp & 3, lane, 0, 0, 0, 0, 0, true};
+  Softmax X{warp >> 2, (int)threadIdx.x & 127, warp & 3, lane, 0, 0, 0, 0, true};
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
-    X.ok = wait_inline(&S.item_full[slot], full(n, kSlots), &S.abort) && X.ok;
+    X.ok = wait_inline(&S.item_taken[slot], full(n, kSlots), &S.abort) && X.ok;
     if (bar_or(1 + X.g, 128, !X.ok)) return;  // the whole warpgroup
     const Item &I = S.item[slot];
     if (!I.valid) return;
     if (X.g >= I.wg && X.g < I.wg + I.ng) softmax_item(P, S, X, n, I);
-    X.it += I.t1 - I.t0;
     arrive_warp(&S.item_empty[slot], lane);
   }
 }
@@ -1211,12 +1313,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_kernel(const __grid_constan
     };
     ring(S.k_full, kKStages, 1), ring(S.k_empty, kKStages, 1);
     ring(S.v_full, kVStages, 1), ring(S.v_empty, kVStages, 1);
-    ring(S.pg_full, kMeta, 1), ring(S.sc_full, kMeta, 1), ring(S.meta_empty, kMeta, 1);
+    ring(S.tile_full, kTiles, 1), ring(S.tile_empty, kTiles, 1);
+    ring(S.sc_full[0], kGroups * kScales, 1), ring(S.sc_empty[0], kGroups * kScales, 4);
     ring(S.q_full, kSlots, kQWarps), ring(S.q_empty, kQUnits, 1);
     ring(S.s_full, kGroups, 1), ring(S.s_empty, kGroups, 4);
     ring(S.p_full, kGroups, 4), ring(S.pv_done, kGroups, 1);
-    ring(S.v_ready, kGroups, 1), ring(S.mended, kGroups, 4);
-    ring(S.item_full, kSlots, 1), ring(S.item_empty, kSlots, kItemReaders);
+    ring(S.v_ready, kGroups, 1);
+    ring(S.item_full, kSlots, 1), ring(S.item_taken, kSlots, 1), ring(S.item_empty, kSlots, kItemReaders);
     ring(S.pair, 2, 8), ring(&S.all, 1, kSoftmaxWarps), ring(S.drain, 2, 1);
     fence_mbar_init();
   }
