@@ -178,6 +178,7 @@ struct Shared {
   uint64_t sc_full[kGroups][kScales], sc_empty[kGroups][kScales];
   uint64_t q_full[kSlots], q_empty[kQUnits], s_full[kGroups], s_empty[kGroups], p_full[kGroups], pv_done[kGroups];
   uint64_t v_ready[kGroups];  // a tile with hidden keys has landed
+  uint64_t q_open[kSlots];    // the query tiles of an item of several warpgroups are free
   uint64_t item_full[kSlots], item_taken[kSlots], item_empty[kSlots], pair[2], all, drain[2];
 };
 constexpr int kSharedBytes = (int)sizeof(Shared) + 1024;  // the base is aligned by hand
@@ -794,10 +795,65 @@ __device__ void pv_warp(Shared &S, int lane) {
 // A row as two e4m3 terms: with 2^e the least power of two that brings its largest
 // entry to 448 or below, hi = e4m3(q 2^-e), lo = e4m3(q 2^-e - hi), which together
 // hold a bf16's eight bits down to 2^-10, 2^-17 of the row's largest entry.
-// Half a warp a row, eight entries a lane.
+// Half a warp a row, eight entries a lane: this half's rows of an item are r, r + step, ...,
+// `count` of them.
+IPD_DEVINL void convert_queries(const BatchDev &B, const Item &I, Shared &S, int slot, int r, int step, int count, int lane) {
+  constexpr int kAhead = 4;  // rows loaded ahead
+  const int part = lane & 15, group = B.group;
+  const auto fetch = [&](int r) {
+    if (r >= I.rows) return make_uint4(0u, 0u, 0u, 0u);
+    const int row = I.row0 + r, query = row / group;
+    return *reinterpret_cast<const uint4 *>(
+        B.q + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group + (row - query * group)) * kD + part * 8);
+  };
+  uint4 next[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) next[i] = fetch(r + i * step);
+#pragma unroll 1
+  for (; count > 0; --count, r += step) {
+    const uint4 x = next[0];
+#pragma unroll
+    for (int i = 0; i + 1 < kAhead; ++i) next[i] = next[i + 1];
+    next[kAhead - 1] = count > kAhead ? fetch(r + step * kAhead) : x;
+    const uint32_t *xw = &x.x;
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = __vmaxu2(top, xw[i] & 0x7fff7fffu);
+    top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const int E = (int)(top >> 7);
+    // (a largest entry below 2^-100 counts as zero; one that is not finite makes the
+    // row NaN)
+    const int e = E - 127 - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0);
+    const bool none = E < 27 || E == 255;
+    const float f = none ? 0.f : pow2i(-e);
+    uint32_t hi[2], lo[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float v[4] = {bf16lo(xw[2 * k]) * f, bf16hi(xw[2 * k]) * f, bf16lo(xw[2 * k + 1]) * f, bf16hi(xw[2 * k + 1]) * f};
+      if (none) v[0] = v[1] = v[2] = v[3] = 0.f;
+      hi[k] = e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16;
+      float back[4];
+      e4m3x4_to_floats(hi[k], back);
+      lo[k] = e4m3x2(v[0] - back[0], v[1] - back[1]) | e4m3x2(v[2] - back[2], v[3] - back[3]) << 16;
+    }
+    const int at = r * kD + (((part >> 1) ^ (r & 7)) << 4) + (part & 1) * 8;
+    *reinterpret_cast<uint2 *>(S.q[0][I.qu] + at) = make_uint2(hi[0], hi[1]);
+    *reinterpret_cast<uint2 *>(S.q[1][I.qu] + at) = make_uint2(lo[0], lo[1]);
+    if (part == 0) S.qscale[slot][r] = E == 255 ? __uint_as_float(0x7fc00000u) : none ? 0.f : pow2i(e);
+  }
+  fence_proxy_async_smem();
+}
+
+IPD_DEVINL void mbar_arrive_n(uint64_t *bar, int n) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(n) : "memory");
+}
+
+// Two warps convert the queries of tasks of one warpgroup while others are under way.  Those of
+// larger tasks would take them as long as several tiles, with the warpgroups waiting: these
+// do it themselves, once their query tiles are free.
 __device__ void query_warp(const Params &P, Shared &S, int w, int lane) {
-  constexpr int kAhead = 4;  // pairs of rows loaded ahead
-  const int half = lane >> 4, part = lane & 15;
   uint32_t uses = 0;  // (a bit a query tile: parity of its uses)
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
@@ -808,53 +864,13 @@ __device__ void query_warp(const Params &P, Shared &S, int w, int lane) {
     for (int i = 0; i < I.ng; ++i)
       if (!wait(&S.q_empty[qu + i], (uses >> (qu + i) & 1u) ^ 1u, &S.abort)) return;
     uses ^= ((1u << I.ng) - 1u) << qu;
-    const BatchDev &B = P.b[I.b];
-    const int all = I.nr * I.ng, group = B.group;
-    const auto fetch = [&](int r) {
-      if (r >= I.rows) return make_uint4(0u, 0u, 0u, 0u);
-      const int row = I.row0 + r, query = row / group;
-      return *reinterpret_cast<const uint4 *>(
-          B.q + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group + (row - query * group)) * kD + part * 8);
-    };
-    uint4 next[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) next[i] = fetch(2 * (w + i * kQWarps) + half);
-#pragma unroll 1
-    for (int r = 2 * w + half; r - half < all; r += 2 * kQWarps) {
-      const uint4 x = next[0];
-#pragma unroll
-      for (int i = 0; i + 1 < kAhead; ++i) next[i] = next[i + 1];
-      next[kAhead - 1] = fetch(r + 2 * kQWarps * kAhead);
-      const uint32_t *xw = &x.x;
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) top = __vmaxu2(top, xw[i] & 0x7fff7fffu);
-      top = max(top & 0xffffu, top >> 16);
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const int E = (int)(top >> 7);
-      // (a largest entry below 2^-100 counts as zero; one that is not finite makes the
-      // row NaN)
-      const int e = E - 127 - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0);
-      const bool none = E < 27 || E == 255;
-      const float f = none ? 0.f : pow2i(-e);
-      uint32_t hi[2], lo[2];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        float v[4] = {bf16lo(xw[2 * k]) * f, bf16hi(xw[2 * k]) * f, bf16lo(xw[2 * k + 1]) * f, bf16hi(xw[2 * k + 1]) * f};
-        if (none) v[0] = v[1] = v[2] = v[3] = 0.f;
-        hi[k] = e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16;
-        float back[4];
-        e4m3x4_to_floats(hi[k], back);
-        lo[k] = e4m3x2(v[0] - back[0], v[1] - back[1]) | e4m3x2(v[2] - back[2], v[3] - back[3]) << 16;
-      }
-      const int at = r * kD + (((part >> 1) ^ (r & 7)) << 4) + (part & 1) * 8;
-      *reinterpret_cast<uint2 *>(S.q[0][qu] + at) = make_uint2(hi[0], hi[1]);
-      *reinterpret_cast<uint2 *>(S.q[1][qu] + at) = make_uint2(lo[0], lo[1]);
-      if (part == 0) S.qscale[slot][r] = E == 255 ? __uint_as_float(0x7fc00000u) : none ? 0.f : pow2i(e);
+    if (I.ng == 1) {
+      convert_queries(P.b[I.b], I, S, slot, 2 * w + (lane >> 4), 2 * kQWarps, I.nr / (2 * kQWarps), lane);
+      __syncwarp();
+      if (lane == 0) mbar_arrive_n(&S.q_full[slot], kSoftmaxWarps / kQWarps);
+    } else {
+      arrive_warp(&S.q_open[slot], lane);
     }
-    fence_proxy_async_smem();
-    arrive_warp(&S.q_full[slot], lane);
     arrive_warp(&S.item_empty[slot], lane);
   }
 }
@@ -881,6 +897,7 @@ struct Softmax {
   uint32_t tiles;          // own tiles so far
   uint32_t mends;          // tiles looked through so far
   uint32_t pairs, alls;    // barriers of two and of all warpgroups so far
+  uint32_t wide;           // a bit an item's slot: parity of its items of several warpgroups so far
   bool ok;                 // no wait of this warp has given up
 };
 
@@ -1189,6 +1206,13 @@ IPD_DEVINL void join(const Params &P, const Item &I, int r0, int rows, int warp,
 __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t item, const Item &I) {
   const int g = X.g, lane = X.lane, tid = X.tid, slot = item % kSlots;
   const int nr = I.nr, rg = g - I.wg;
+  if (I.ng > 1) {
+    // (the query warps go by every item: this one's turn of the barrier is known by its wide items)
+    X.ok = wait_inline(&S.q_open[slot], X.wide >> slot & 1u, &S.abort) && X.ok;
+    convert_queries(P.b[I.b], I, S, slot, rg * kRows + 2 * X.warp + (lane >> 4), 8, 4, lane);
+    __syncwarp();
+    if (lane == 0) mbar_arrive_n(&S.q_full[slot], kGroups / I.ng);
+  }
   X.ok = wait_inline(&S.q_full[slot], full(item, kSlots), &S.abort) && X.ok;
   if (tid < nr) {
     float *st = reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1);
@@ -1287,7 +1311,7 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
 }
 
 __device__ void softmax_warps(const Params &P, Shared &S, int warp, int lane) {
-  Softmax X{warp >> 2, (int)threadIdx.x & 127, warp & 3, lane, 0, 0, 0, 0, true};
+  Softmax X{warp >> 2, (int)threadIdx.x & 127, warp & 3, lane, 0, 0, 0, 0, 0, true};
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
     X.ok = wait_inline(&S.item_taken[slot], full(n, kSlots), &S.abort) && X.ok;
@@ -1295,6 +1319,7 @@ __device__ void softmax_warps(const Params &P, Shared &S, int warp, int lane) {
     const Item &I = S.item[slot];
     if (!I.valid) return;
     if (X.g >= I.wg && X.g < I.wg + I.ng) softmax_item(P, S, X, n, I);
+    if (I.ng > 1) X.wide ^= 1u << slot;
     arrive_warp(&S.item_empty[slot], lane);
   }
 }
@@ -1315,7 +1340,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_kernel(const __grid_constan
     ring(S.v_full, kVStages, 1), ring(S.v_empty, kVStages, 1);
     ring(S.tile_full, kTiles, 1), ring(S.tile_empty, kTiles, 1);
     ring(S.sc_full[0], kGroups * kScales, 1), ring(S.sc_empty[0], kGroups * kScales, 4);
-    ring(S.q_full, kSlots, kQWarps), ring(S.q_empty, kQUnits, 1);
+    ring(S.q_open, kSlots, kQWarps), ring(S.q_full, kSlots, kSoftmaxWarps), ring(S.q_empty, kQUnits, 1);
     ring(S.s_full, kGroups, 1), ring(S.s_empty, kGroups, 4);
     ring(S.p_full, kGroups, 4), ring(S.pv_done, kGroups, 1);
     ring(S.v_ready, kGroups, 1);
