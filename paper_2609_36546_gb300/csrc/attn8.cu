@@ -91,7 +91,8 @@ constexpr float kLoScale = 16.f;
 constexpr int kFar = 100;      // V scales further apart than 2^100 count as that far
 // What a tile of a task with up to 32, 64 and 128 rows costs, and a task beside its
 // tiles: the line is cut into equal costs.
-constexpr int kCost1 = 4, kCost2 = 5, kCost4 = 9, kItemCost = 6;
+constexpr int kCost1 = 4, kCost2 = 6, kCost4 = 12;
+constexpr int kItem1 = 20, kItem2 = 40, kItem4 = 70;
 constexpr int kNoPage = 1 << 20;  // in place of an exponent: no such page
 
 struct BatchDev {
@@ -348,6 +349,8 @@ IPD_DEVINL int batch_of(const Params &P, int g) {
 }
 
 IPD_DEVINL int tile_cost(int rows) { return rows > 64 ? kCost4 : rows > 32 ? kCost2 : kCost1; }
+IPD_DEVINL int item_cost(int rows) { return rows > 64 ? kItem4 : rows > 32 ? kItem2 : kItem1; }
+IPD_DEVINL long long task_cost(int rows, int tiles) { return item_cost(rows) + (long long)tiles * tile_cost(rows); }
 
 // Checks the requests and adds up their costs; one block.
 __global__ void __launch_bounds__(1024) attn8_plan_kernel(const __grid_constant__ Params P, int ctas) {
@@ -375,8 +378,7 @@ __global__ void __launch_bounds__(1024) attn8_plan_kernel(const __grid_constant_
         const int rows = n * B.group, blocks = (rows + kBlockRows - 1) / kBlockRows;
         dearest = max(dearest, tile_cost(min(rows, kBlockRows)));
         units = (long long)B.hkv *
-                ((blocks - 1) * (kItemCost + (long long)tiles * tile_cost(min(rows, kBlockRows))) + kItemCost +
-                 (long long)tiles * tile_cost(rows - (blocks - 1) * kBlockRows));
+                ((blocks - 1) * task_cost(kBlockRows, tiles) + task_cost(rows - (blocks - 1) * kBlockRows, tiles));
       }
       P.info[g] = make_int4(L, n, c0, tiles);
     }
@@ -407,12 +409,12 @@ __global__ void __launch_bounds__(1024) attn8_plan_kernel(const __grid_constant_
 }
 
 // ---- items (one warp) ----------------------------------------------------------------
-// A task's place in the line: its first tile begins at 0, tile t at kItemCost + t w, and
-// it ends at kItemCost + tiles w, w the cost of one of its tiles.
+// A task's place in the line: its first tile begins at 0, tile t at `item` + t w, and
+// it ends at `item` + tiles w, w the cost of one of its tiles.
 // the first tile that begins at `off` or later
-IPD_DEVINL int tile_at(long long off, int w, int tiles) {
+IPD_DEVINL int tile_at(long long off, int item, int w, int tiles) {
   if (off <= 0) return 0;
-  const long long t = (off - kItemCost + w - 1) / w;
+  const long long t = (off - item + w - 1) / w;
   return (int)max(1LL, min((long long)tiles, t));
 }
 
@@ -450,17 +452,16 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
     const int L = info.x, tiles = info.w, rows_all = info.y * group;
     // (a request's blocks are alike but for the last, which may have fewer rows)
     const int blocks = (rows_all + kBlockRows - 1) / kBlockRows, last_rows = rows_all - (blocks - 1) * kBlockRows;
-    const int w_full = tile_cost(min(rows_all, kBlockRows)), w_last = tile_cost(last_rows);
-    const long long c_full = kItemCost + (long long)tiles * w_full, c_last = kItemCost + (long long)tiles * w_last;
+    const long long c_full = task_cost(kBlockRows, tiles), c_last = task_cost(last_rows, tiles);
     const long long c_head = (blocks - 1) * c_full + c_last;
     int h = (int)((pos - first) / c_head);
     long long in_head = pos - first - h * c_head;
     int block = (int)min((long long)blocks - 1, in_head / c_full);
     long long at = first + h * c_head + block * c_full;  // the task's beginning
     while (at < hi && at < next) {
-      const int w = block == blocks - 1 ? w_last : w_full;
+      const int like = block == blocks - 1 ? last_rows : kBlockRows, w = tile_cost(like), item = item_cost(like);
       const long long cost = block == blocks - 1 ? c_last : c_full;
-      const int t0 = tile_at(lo - at, w, tiles), t1 = hi - at >= cost ? tiles : tile_at(hi - at, w, tiles);
+      const int t0 = tile_at(lo - at, item, w, tiles), t1 = hi - at >= cost ? tiles : tile_at(hi - at, item, w, tiles);
       if (t0 < t1) {
         const int slot = n % kSlots;
         if (!wait(&S.item_empty[slot], free_(n, kSlots), &S.abort)) return;
@@ -479,7 +480,7 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
           if (I.part >= 0) {
             // CTA i begins at floor(i W / C): the last one that begins at p or before
             const auto cta = [&](int t) {
-              const long long p = at + (t > 0 ? kItemCost + (long long)t * w : 0);
+              const long long p = at + (t > 0 ? item + (long long)t * w : 0);
               return (int)(((p + 1) * C - 1) / W);
             };
             I.cta0 = cta(0), I.ctab = max(I.cta0 + 1, cta(1)), I.cta1 = cta(tiles - 1);
@@ -639,8 +640,12 @@ __device__ void page_warp(const Params &P, Shared &S, int lane) {
     fetch(false);
     const int most = __reduce_max_sync(0xffffffffu, ng);
     for (int j = 0; j < most; ++j) {
-      const int to = g + min(j, ng - 1);
-      const uint32_t k = __shfl_sync(0xffffffffu, tiles, to) + q;
+      // (lanes whose tile has fewer wait with another that has not: their own barriers' turn
+      // may be over once they have been arrived at)
+      const uint32_t have = __ballot_sync(0xffffffffu, j < ng);
+      const int as = j < ng ? lane : __ffs(have) - 1;
+      const int to = __shfl_sync(0xffffffffu, g, as) + j;
+      const uint32_t k = __shfl_sync(0xffffffffu, tiles, to) + __shfl_sync(0xffffffffu, q, as);
       if (!wait(&S.sc_empty[to][k % kScales], free_(k, kScales), &S.abort, 20)) return;
       Scales &C = S.scales[to][k % kScales];
       if (mine < now && j < ng) {

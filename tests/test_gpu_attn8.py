@@ -157,6 +157,26 @@ def test_many_long_requests(lib, hq, hkv, q_hi, n, lo, hi):
     assert lib.device_error() == 0
 
 
+@pytest.mark.parametrize("hq,hkv,q_lo,q_hi,n,hi", [(32, 4, 4, 7, 300, 3000), (32, 4, 1, 16, 300, 1500), (32, 4, 3, 12, 200, 150),
+                                                   (64, 8, 1, 5, 100, 700)])
+def test_tasks_of_different_widths_side_by_side(lib, hq, hkv, q_lo, q_hi, n, hi):
+    """Tasks of one, two and four warpgroups in turn in every CTA, warpgroups that wait for
+    their tiles among them."""
+    for seed in range(4):
+        g = torch.Generator().manual_seed(seed)
+        length = torch.randint(q_hi, hi + 1, (n,), generator=g).tolist()
+        q_len = torch.randint(q_lo, q_hi + 1, (n,), generator=g).tolist()
+        c = Case(hq, hkv, q_len, length, seed=seed)
+        _run(lib, c)
+        if seed == 0:
+            _check(c)
+        first = c.out.clone()
+        for _ in range(10):
+            _run(lib, c)
+        assert torch.equal(c.out, first)
+        assert lib.device_error() == 0
+
+
 def test_several_batches_in_one_call(lib):
     """Spans over two caches and decode tokens over both, and a batch without
     queries: the same bytes as one call each."""
