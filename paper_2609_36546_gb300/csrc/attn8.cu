@@ -63,20 +63,17 @@ constexpr int kMaxGroup = 128;
 constexpr int kBlockRows = 128;           // rows of a task
 constexpr int kGroups = 4;                // softmax warpgroups
 constexpr int kRows = 32;                 // ... and the rows of one
-constexpr int kKStages = 3, kVStages = 4;
+constexpr int kKStages = 4, kVStages = 5;
 constexpr int kTiles = 16;                // tiles handed out whose product is not complete
 constexpr int kScales = 16;
 constexpr int kBatch = 4;                 // ... fetched at once
 constexpr int kSlots = 8;                 // items handed out
 constexpr int kSoftmaxWarps = 4 * kGroups;
-constexpr int kKWarp = kSoftmaxWarps, kVWarp = kKWarp + 1, kQkWarp = kKWarp + 2, kPvWarp = kKWarp + 3,
-              kItemWarp = kKWarp + 4, kPageWarp = kKWarp + 5, kQWarps = 2;
-constexpr int kThreads = 32 * (kSoftmaxWarps + 6 + kQWarps);
-constexpr int kItemReaders = kSoftmaxWarps + 1 + kQWarps;
-constexpr int kQUnits = 8;                // query tiles of 32 rows at hand
-constexpr int kRegsLaunch = 80, kRegsSoftmax = 96, kRegsAux = 48;
-static_assert(32 * kSoftmaxWarps * kRegsSoftmax + 256 * kRegsAux <= kThreads * kRegsLaunch,
-              "the register split must fit the registers the block was launched with");
+constexpr int kLoadWarp = kSoftmaxWarps, kQkWarp = kLoadWarp + 1, kPvWarp = kLoadWarp + 2, kItemWarp = kLoadWarp + 3;  // (the fifth: page ids and scales)
+// (no more: the registers are 96 for each thread of 21 warps, 80 for 24; with separate warps for
+// V's loads and for queries ahead of their turn 1,000 requests of 300 keys took 411 us, now 322)
+constexpr int kThreads = 32 * (kSoftmaxWarps + 5);
+constexpr int kItemReaders = kSoftmaxWarps + 1;
 static_assert(kBatch * kPages == 32, "a lane a page");
 
 // TMEM columns of a warpgroup: scores, O (two terms), and every thread's own sums
@@ -123,7 +120,6 @@ struct Item {
   int nr, ng, wg;       // rows of a warpgroup (16 or 32); its warpgroups (1, 2 or 4) and their first
   int t0, t1;           // tiles
   int masked;           // the first key that some row of the task does not see
-  int qu;               // first query tile
   int r, n_pages;       // request of the batch, its pages
   int part;             // partial slot (-1: the whole task is here)
   int cta0, ctab, cta1; // the CTAs of the task: cta0, then ctab .. cta1
@@ -132,22 +128,20 @@ struct Item {
 // A tile on its way through the loading and issuing warps.
 enum { kFirst = 1, kLast = 2, kHides = 4, kEnd = 8 };
 struct Tile {
-  int y[kPages];  // first pool rows of its pages
+  alignas(16) int y[kPages];  // first pool rows of its pages
   uint32_t what;  // the rest in one word, which one warp-wide move makes uniform:
   // its item's first, last; it holds hidden keys; there is none after the one before (4 bits);
-  // warpgroups (3), the first of them (2), 32 rows each or 16 (1), first query tile (3),
-  // the item's place in this CTA's order (4: slot and turn), batch (3)
+  // warpgroups (3), the first of them (2), 32 rows each or 16 (1), the item's place in this CTA's order (4: slot and turn), batch (3)
 };
-static_assert(2 * kSlots == 16 && kQUnits == 8 && kGroups == 4 && IPD_MAX_BATCHES <= 8, "the fields of Tile::what");
+static_assert(2 * kSlots == 16 && kGroups == 4 && IPD_MAX_BATCHES <= 8, "the fields of Tile::what");
 struct What {
   uint32_t w;
   IPD_DEVINL bool is(int flag) const { return w & flag; }
   IPD_DEVINL int ng() const { return w >> 4 & 7u; }
   IPD_DEVINL int wg() const { return w >> 7 & 3u; }
   IPD_DEVINL int nr() const { return 16u << (w >> 9 & 1u); }
-  IPD_DEVINL uint32_t qu() const { return w >> 10 & 7u; }
-  IPD_DEVINL uint32_t item() const { return w >> 13 & 15u; }
-  IPD_DEVINL int b() const { return w >> 17 & 7u; }
+  IPD_DEVINL uint32_t item() const { return w >> 10 & 15u; }
+  IPD_DEVINL int b() const { return w >> 14 & 7u; }
 };
 // ... and what a warpgroup has to know of it.
 struct Scales {
@@ -159,12 +153,11 @@ struct Scales {
 struct Shared {
   alignas(1024) uint8_t k[kKStages][kTileBytes];
   alignas(1024) uint8_t v[kVStages][kTileBytes];
-  alignas(1024) uint8_t q[2][kQUnits][kRows * kD];     // the two terms of the query tiles
+  alignas(1024) uint8_t q[2][kGroups][kRows * kD];     // the two terms of the queries
   alignas(1024) uint8_t p[kGroups][kKeys * 2 * kRows]; // a warpgroup's P; at the end, rows on their way
   alignas(16) float4 state[kGroups][kRows / 2];        // a pair of rows: ar, ar', -ref, -ref'
   alignas(16) float alpha[kGroups][kRows];
   alignas(16) float red[kGroups][4][kRows];
-  alignas(16) float qscale[kSlots][kBlockRows];
   uint32_t over[kGroups][4];                           // rows whose references have to move
   // first key of a span with a NaN in this dim of V, and whether there is one (by an
   // item's first warpgroup)
@@ -177,9 +170,8 @@ struct Shared {
   uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
   uint64_t tile_full[kTiles], tile_empty[kTiles];
   uint64_t sc_full[kGroups][kScales], sc_empty[kGroups][kScales];
-  uint64_t q_full[kSlots], q_empty[kQUnits], s_full[kGroups], s_empty[kGroups], p_full[kGroups], pv_done[kGroups];
+  uint64_t q_full[kSlots], s_full[kGroups], s_empty[kGroups], p_full[kGroups], pv_done[kGroups];
   uint64_t v_ready[kGroups];  // a tile with hidden keys has landed
-  uint64_t q_open[kSlots];    // the query tiles of an item of several warpgroups are free
   uint64_t item_full[kSlots], item_taken[kSlots], item_empty[kSlots], pair[2], all, drain[2];
 };
 constexpr int kSharedBytes = (int)sizeof(Shared) + 1024;  // the base is aligned by hand
@@ -328,10 +320,6 @@ IPD_DEVINL bool elect_one() {
   return r != 0;
 }
 IPD_DEVINL int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
-IPD_DEVINL void commit(uint64_t *bar) {
-  if (elect_one()) tc_commit(bar);
-  __syncwarp();
-}
 // The n-th use (0, 1, ...) of a barrier of a ring of `ring`: a consumer waits for it
 // with full(n), a producer for the release of its slot with free(n).
 IPD_DEVINL uint32_t full(uint32_t n, uint32_t ring) { return n / ring & 1u; }
@@ -423,7 +411,7 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
   const long long W = P.prefix[P.total_reqs];
   // (a part is no shorter than a tile, so that none between a task's ends has no tile)
   const long long C = max(1LL, min((long long)gridDim.x, W / P.prefix[P.total_reqs + 1]));
-  uint32_t n = 0, unit = 0;
+  uint32_t n = 0;
   const long long lo = blockIdx.x < C ? blockIdx.x * W / C : W, hi = blockIdx.x < C ? (blockIdx.x + 1) * W / C : W;
   int g = 0;
   if (lo < hi) {
@@ -467,12 +455,10 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
         if (!wait(&S.item_empty[slot], free_(n, kSlots), &S.abort)) return;
         const int row0 = block * kBlockRows, rows = min(kBlockRows, rows_all - row0);
         const int ng = rows > 64 ? 4 : rows > 32 ? 2 : 1;
-        const int qu = (int)((unit + ng - 1) & (uint32_t)(kQUnits - ng));
-        unit = qu + ng;
         if (lane == 0) {
           Item &I = S.item[slot];
           I.valid = 1, I.b = b, I.c0 = info.z, I.n = info.y, I.L = L, I.h = h;
-          I.row0 = row0, I.rows = rows, I.nr = rows > 16 ? 32 : 16, I.ng = ng, I.qu = qu;
+          I.row0 = row0, I.rows = rows, I.nr = rows > 16 ? 32 : 16, I.ng = ng;
           I.t0 = t0, I.t1 = t1;
           I.masked = L - info.y + 1 + row0 / group;
           I.r = g - P.req_base[b], I.n_pages = (L + kPage - 1) / kPage;
@@ -524,12 +510,12 @@ IPD_DEVINL bool mbar_test(uint64_t *bar, uint32_t parity) {
 __device__ void page_warp(const Params &P, Shared &S, int lane) {
   const int mine = lane / kPages, place = lane % kPages;  // a lane's tile of a batch, and page
   uint32_t n = 0, it = 0;    // items taken; tiles handed out
-  int known = 0, units = 0;  // warpgroups that item n wants (0: it has not been looked at), its query tiles
+  int known = 0;             // warpgroups that item n wants (0: it has not been looked at)
   bool ended = false, given_up = false;
   int last_g = kGroups - 1;
   // lane g < 4: what warpgroup g has been given: the item, its next tile and its end, the
-  // first of its warpgroups, its query tiles; how many tiles the warpgroup has had
-  int w_item = 0, w_t = 0, w_t1 = 0, w_first = 0, w_units = 0;
+  // first of its warpgroups; how many tiles the warpgroup has had
+  int w_item = 0, w_t = 0, w_t1 = 0, w_first = 0;
   uint32_t w_tiles = 0;
   // the batch whose ids are under way: a lane's item, tile, first warpgroup, how many tiles
   // before it are that item's; w_tiles before the batch
@@ -560,11 +546,7 @@ __device__ void page_warp(const Params &P, Shared &S, int lane) {
           break;
         }
         known = S.item[slot].ng;
-        units = ((1 << known) - 1) << S.item[slot].qu;
       }
-      // (its query tiles must be those of no item under way: the products, which go by the
-      // order of tiles, would wait for queries that wait for that item's last product)
-      if (__any_sync(0xffffffffu, active && (w_units & units))) break;
       int g = -1;
 #pragma unroll
       for (int k = kGroups; k >= 1; --k) {  // the next after the one that had a tile last
@@ -577,7 +559,7 @@ __device__ void page_warp(const Params &P, Shared &S, int lane) {
         mbar_arrive(&S.item_taken[slot]);
       }
       if (lane >= g && lane < g + known)
-        w_item = (int)n, w_t = S.item[slot].t0, w_t1 = S.item[slot].t1, w_first = g, w_units = units;
+        w_item = (int)n, w_t = S.item[slot].t0, w_t1 = S.item[slot].t1, w_first = g;
       ++n;
       known = 0;
     }
@@ -632,7 +614,7 @@ __device__ void page_warp(const Params &P, Shared &S, int lane) {
     if (mine < now) T.y[place] = ok ? (int)cell * kPage : B.rows_end;
     if (leads) {
       T.what = (t == I.t0 ? kFirst : 0) | (last ? kLast : 0) | ((t + 1) * kKeys > I.masked ? kHides : 0) | ng << 4 | g << 7 |
-               (I.nr >> 5) << 9 | I.qu << 10 | (item & 15) << 13 | I.b << 17;
+               (I.nr >> 5) << 9 | (item & 15) << 10 | I.b << 14;
     }
     __syncwarp();
     if (leads) mbar_arrive(&S.tile_full[at % kTiles]);
@@ -671,36 +653,44 @@ __device__ void page_warp(const Params &P, Shared &S, int lane) {
 }
 
 // ---- loads -------------------------------------------------------------------------
-template <bool kIsV>
+// A tile's eight pages into a stage.
+IPD_DEVINL void load_tile(const CUtensorMap *map, uint8_t *stage, const Tile &T, uint64_t *bar, uint64_t policy) {
+  const int4 lo = *reinterpret_cast<const int4 *>(T.y), hi = *reinterpret_cast<const int4 *>(T.y + 4);
+  const int y[kPages] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  if (elect_one()) {
+    mbar_arrive_expect_tx(bar, kTileBytes);
+#pragma unroll
+    for (int i = 0; i < kPages; ++i) tma_load_2d(stage + i * kPageBytes, map, 0, y[i], bar, policy);
+  }
+  __syncwarp();
+}
+
 __device__ void load_warp(const Params &P, Shared &S, int lane) {
-  constexpr int kRing = kIsV ? kVStages : kKStages;
-  uint64_t *fulls = kIsV ? S.v_full : S.k_full, *empties = kIsV ? S.v_empty : S.k_empty;
-  uint8_t *ring = kIsV ? S.v[0] : S.k[0];
   const uint64_t policy = l2_policy_evict_first();
-  uint32_t it = 0;
-  for (;; ++it) {
-    const uint32_t m = it % kTiles, s = it % kRing;
+  uint32_t it = 0, vs = 0;  // tiles of K, of V
+  for (;; ++it, ++vs) {
+    const uint32_t m = it % kTiles, k = it % kKStages, v = it % kVStages;
     if (!wait(&S.tile_full[m], full(it, kTiles), &S.abort, 40)) break;
     const Tile &T = S.tile[m];
     const What what{(uint32_t)uniform((int)T.what)};
     if (what.is(kEnd)) return;
-    if (!wait(&empties[s], free_(it, kRing), &S.abort, 40)) break;
     const int b = what.b();
-    const CUtensorMap *map = kIsV ? &P.v[b] : &P.k[b];
-    if (elect_one()) {
-      mbar_arrive_expect_tx(&fulls[s], kTileBytes);
-#pragma unroll 1
-      for (int i = 0; i < kPages; ++i)
-        tma_load_2d(ring + s * kTileBytes + i * kPageBytes, map, 0, T.y[i], &fulls[s], policy);
+    if (!wait(&S.k_empty[k], free_(it, kKStages), &S.abort, 40)) break;
+    load_tile(&P.k[b], S.k[k], T, &S.k_full[k], policy);
+    if (!wait(&S.v_empty[v], free_(it, kVStages), &S.abort, 40)) {
+      ++it;
+      break;
     }
-    __syncwarp();
+    load_tile(&P.v[b], S.v[v], T, &S.v_full[v], policy);
   }
   // given up: the copies in flight land first
-  for (uint32_t k = it > (uint32_t)kRing ? it - kRing : 0; k < it; ++k) {
-    const long long t0 = clock64();
-    while (!mbar_try_wait(&fulls[k % kRing], full(k, kRing)) && clock64() - t0 < kWaitLimitCycles) {
+  const long long t0 = clock64();
+  for (uint32_t i = it > (uint32_t)kKStages ? it - kKStages : 0; i < it; ++i)
+    while (!mbar_try_wait(&S.k_full[i % kKStages], full(i, kKStages)) && clock64() - t0 < kWaitLimitCycles) {
     }
-  }
+  for (uint32_t i = vs > (uint32_t)kVStages ? vs - kVStages : 0; i < vs; ++i)
+    while (!mbar_try_wait(&S.v_full[i % kVStages], full(i, kVStages)) && clock64() - t0 < kWaitLimitCycles) {
+    }
 }
 
 // ---- products -----------------------------------------------------------------------
@@ -719,7 +709,7 @@ __device__ void qk_warp(Shared &S, int lane) {
   const uint32_t tmem = (uint32_t)uniform((int)S.tmem);
   const uint64_t k0 = sdesc((uint32_t)uniform((int)smem_u32(S.k[0])), 128),
                  q0 = sdesc((uint32_t)uniform((int)smem_u32(S.q[0][0])), 128);
-  constexpr uint64_t kUnit = kRows * kD >> 4, kTerm = kQUnits * kUnit;  // in descriptors
+  constexpr uint64_t kUnit = kRows * kD >> 4, kTerm = kGroups * kUnit;  // in descriptors
   uint32_t uses = 0;  // (a bit a warpgroup: parity of its uses)
   for (uint32_t it = 0;; ++it) {
     const uint32_t m = it % kTiles, s = it % kKStages;
@@ -727,7 +717,7 @@ __device__ void qk_warp(Shared &S, int lane) {
     const What what{(uint32_t)uniform((int)S.tile[m].what)};
     if (what.is(kEnd)) return;
     const int ng = what.ng(), g0 = what.wg();
-    const uint32_t idesc = idesc_f8(what.nr() * ng, 0), qu = what.qu(), item = what.item();
+    const uint32_t idesc = idesc_f8(what.nr() * ng, 0), item = what.item();
     bool ok = true;
     if (what.is(kFirst)) ok = wait(&S.q_full[item % kSlots], full(item, kSlots), &S.abort, 40);
     for (int i = 0; ok && i < ng; ++i) ok = wait(&S.s_empty[g0 + i], (uses >> (g0 + i) & 1u) ^ 1u, &S.abort, 40);
@@ -735,7 +725,7 @@ __device__ void qk_warp(Shared &S, int lane) {
     if (!ok) break;
     uses ^= ((1u << ng) - 1u) << g0;
     tc_fence_after();
-    const uint64_t k = k0 + (uint64_t)(s * (kTileBytes >> 4)), q = q0 + qu * kUnit;
+    const uint64_t k = k0 + (uint64_t)(s * (kTileBytes >> 4)), q = q0 + g0 * kUnit;
     const uint32_t d = tmem + col_s(g0);
     if (elect_one()) {
 #pragma unroll
@@ -748,8 +738,6 @@ __device__ void qk_warp(Shared &S, int lane) {
       tc_commit(&S.k_empty[s]);
     }
     __syncwarp();
-    if (what.is(kLast))
-      for (int i = 0; i < ng; ++i) commit(&S.q_empty[qu + i]);
   }
   drain(&S.drain[0], lane);
 }
@@ -800,26 +788,27 @@ __device__ void pv_warp(Shared &S, int lane) {
 // A row as two e4m3 terms: with 2^e the least power of two that brings its largest
 // entry to 448 or below, hi = e4m3(q 2^-e), lo = e4m3(q 2^-e - hi), which together
 // hold a bf16's eight bits down to 2^-10, 2^-17 of the row's largest entry.
-// Half a warp a row, eight entries a lane: this half's rows of an item are r, r + step, ...,
-// `count` of them.
-IPD_DEVINL void convert_queries(const BatchDev &B, const Item &I, Shared &S, int slot, int r, int step, int count, int lane) {
-  constexpr int kAhead = 4;  // rows loaded ahead
-  const int part = lane & 15, group = B.group;
+// Half a warp a row, eight entries a lane; the warpgroup's own rows of the item, whose
+// place is free: the products of the item before are complete.
+IPD_DEVINL void convert_queries(const BatchDev &B, const Item &I, Shared &S, int g, int warp, int lane) {
+  const int first = (g - I.wg) * kRows, group = B.group;  // (rows of the item)
+  constexpr int kAhead = 2;  // rows loaded ahead
+  const int part = lane & 15;
   const auto fetch = [&](int r) {
-    if (r >= I.rows) return make_uint4(0u, 0u, 0u, 0u);
-    const int row = I.row0 + r, query = row / group;
+    if (first + r >= I.rows) return make_uint4(0u, 0u, 0u, 0u);
+    const int row = I.row0 + first + r, query = row / group;
     return *reinterpret_cast<const uint4 *>(
         B.q + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group + (row - query * group)) * kD + part * 8);
   };
   uint4 next[kAhead];
+  int r = 2 * warp + (lane >> 4);
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) next[i] = fetch(r + i * step);
+  for (int i = 0; i < kAhead; ++i) next[i] = fetch(r + i * 8);
 #pragma unroll 1
-  for (; count > 0; --count, r += step) {
+  for (; r < I.nr; r += 8) {
     const uint4 x = next[0];
-#pragma unroll
-    for (int i = 0; i + 1 < kAhead; ++i) next[i] = next[i + 1];
-    next[kAhead - 1] = count > kAhead ? fetch(r + step * kAhead) : x;
+    next[0] = next[1];
+    next[1] = r + 16 < I.nr ? fetch(r + 16) : x;
     const uint32_t *xw = &x.x;
     uint32_t top = 0;
 #pragma unroll
@@ -844,40 +833,19 @@ IPD_DEVINL void convert_queries(const BatchDev &B, const Item &I, Shared &S, int
       lo[k] = e4m3x2(v[0] - back[0], v[1] - back[1]) | e4m3x2(v[2] - back[2], v[3] - back[3]) << 16;
     }
     const int at = r * kD + (((part >> 1) ^ (r & 7)) << 4) + (part & 1) * 8;
-    *reinterpret_cast<uint2 *>(S.q[0][I.qu] + at) = make_uint2(hi[0], hi[1]);
-    *reinterpret_cast<uint2 *>(S.q[1][I.qu] + at) = make_uint2(lo[0], lo[1]);
-    if (part == 0) S.qscale[slot][r] = E == 255 ? __uint_as_float(0x7fc00000u) : none ? 0.f : pow2i(e);
+    *reinterpret_cast<uint2 *>(S.q[0][g] + at) = make_uint2(hi[0], hi[1]);
+    *reinterpret_cast<uint2 *>(S.q[1][g] + at) = make_uint2(lo[0], lo[1]);
+    if (part == 0) {
+      float *st = reinterpret_cast<float *>(&S.state[g][r >> 1]) + (r & 1);
+      st[0] = E == 255 ? __uint_as_float(0x7fc00000u) : none ? 0.f : pow2i(e);
+      st[2] = 0.f;
+    }
   }
   fence_proxy_async_smem();
 }
 
 IPD_DEVINL void mbar_arrive_n(uint64_t *bar, int n) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(n) : "memory");
-}
-
-// Two warps convert the queries of tasks of one warpgroup while others are under way.  Those of
-// larger tasks would take them as long as several tiles, with the warpgroups waiting: these
-// do it themselves, once their query tiles are free.
-__device__ void query_warp(const Params &P, Shared &S, int w, int lane) {
-  uint32_t uses = 0;  // (a bit a query tile: parity of its uses)
-  for (uint32_t n = 0;; ++n) {
-    const int slot = n % kSlots;
-    if (!wait(&S.item_full[slot], full(n, kSlots), &S.abort)) return;
-    const Item &I = S.item[slot];
-    if (!I.valid) return;
-    const int qu = I.qu;
-    for (int i = 0; i < I.ng; ++i)
-      if (!wait(&S.q_empty[qu + i], (uses >> (qu + i) & 1u) ^ 1u, &S.abort)) return;
-    uses ^= ((1u << I.ng) - 1u) << qu;
-    if (I.ng == 1) {
-      convert_queries(P.b[I.b], I, S, slot, 2 * w + (lane >> 4), 2 * kQWarps, I.nr / (2 * kQWarps), lane);
-      __syncwarp();
-      if (lane == 0) mbar_arrive_n(&S.q_full[slot], kSoftmaxWarps / kQWarps);
-    } else {
-      arrive_warp(&S.q_open[slot], lane);
-    }
-    arrive_warp(&S.item_empty[slot], lane);
-  }
 }
 
 // ---- softmax --------------------------------------------------------------------------
@@ -902,7 +870,6 @@ struct Softmax {
   uint32_t tiles;          // own tiles so far
   uint32_t mends;          // tiles looked through so far
   uint32_t pairs, alls;    // barriers of two and of all warpgroups so far
-  uint32_t wide;           // a bit an item's slot: parity of its items of several warpgroups so far
   bool ok;                 // no wait of this warp has given up
 };
 
@@ -1062,7 +1029,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
     const uint32_t k = X.tiles % kScales;
     X.ok = wait_inline(&S.sc_full[g][k], full(X.tiles, kScales), &S.abort) && X.ok;
     const Scales &M = S.scales[g][k];
-    const int v_stage = M.v & (kVStages - 1);  // (in range whatever a warp that gave up has left)
+    const int v_stage = min((uint32_t)M.v, kVStages - 1u);  // (in range whatever a warp that gave up has left)
     const int key0 = (I.t0 + t) * kKeys, key = key0 + tid;
     const float ck = M.ck[tid / kPage];
     const int ev = M.ev[tid / kPage];
@@ -1211,19 +1178,9 @@ IPD_DEVINL void join(const Params &P, const Item &I, int r0, int rows, int warp,
 __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t item, const Item &I) {
   const int g = X.g, lane = X.lane, tid = X.tid, slot = item % kSlots;
   const int nr = I.nr, rg = g - I.wg;
-  if (I.ng > 1) {
-    // (the query warps go by every item: this one's turn of the barrier is known by its wide items)
-    X.ok = wait_inline(&S.q_open[slot], X.wide >> slot & 1u, &S.abort) && X.ok;
-    convert_queries(P.b[I.b], I, S, slot, rg * kRows + 2 * X.warp + (lane >> 4), 8, 4, lane);
-    __syncwarp();
-    if (lane == 0) mbar_arrive_n(&S.q_full[slot], kGroups / I.ng);
-  }
-  X.ok = wait_inline(&S.q_full[slot], full(item, kSlots), &S.abort) && X.ok;
-  if (tid < nr) {
-    float *st = reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1);
-    st[0] = S.qscale[slot][rg * kRows + tid];
-    st[2] = 0.f;
-  }
+  convert_queries(P.b[I.b], I, S, g, X.warp, lane);
+  __syncwarp();
+  if (lane == 0) mbar_arrive_n(&S.q_full[slot], kGroups / I.ng);
   named_bar_sync(1 + g, 128);
   const int e0 = nr == 32 ? softmax_tiles<32>(P, S, X, I) : softmax_tiles<16>(P, S, X, I);
   // the sums over the threads
@@ -1316,7 +1273,7 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
 }
 
 __device__ void softmax_warps(const Params &P, Shared &S, int warp, int lane) {
-  Softmax X{warp >> 2, (int)threadIdx.x & 127, warp & 3, lane, 0, 0, 0, 0, 0, true};
+  Softmax X{warp >> 2, (int)threadIdx.x & 127, warp & 3, lane, 0, 0, 0, 0, true};
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
     X.ok = wait_inline(&S.item_taken[slot], full(n, kSlots), &S.abort) && X.ok;
@@ -1324,7 +1281,6 @@ __device__ void softmax_warps(const Params &P, Shared &S, int warp, int lane) {
     const Item &I = S.item[slot];
     if (!I.valid) return;
     if (X.g >= I.wg && X.g < I.wg + I.ng) softmax_item(P, S, X, n, I);
-    if (I.ng > 1) X.wide ^= 1u << slot;
     arrive_warp(&S.item_empty[slot], lane);
   }
 }
@@ -1345,7 +1301,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_kernel(const __grid_constan
     ring(S.v_full, kVStages, 1), ring(S.v_empty, kVStages, 1);
     ring(S.tile_full, kTiles, 1), ring(S.tile_empty, kTiles, 1);
     ring(S.sc_full[0], kGroups * kScales, 1), ring(S.sc_empty[0], kGroups * kScales, 4);
-    ring(S.q_open, kSlots, kQWarps), ring(S.q_full, kSlots, kSoftmaxWarps), ring(S.q_empty, kQUnits, 1);
+    ring(S.q_full, kSlots, kSoftmaxWarps);
     ring(S.s_full, kGroups, 1), ring(S.s_empty, kGroups, 4);
     ring(S.p_full, kGroups, 4), ring(S.pv_done, kGroups, 1);
     ring(S.v_ready, kGroups, 1);
@@ -1360,19 +1316,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_kernel(const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp < kSoftmaxWarps) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRegsSoftmax));
-    softmax_warps(P, S, warp, lane);
-  } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRegsAux));
-    if (warp == kKWarp) load_warp<false>(P, S, lane);
-    else if (warp == kVWarp) load_warp<true>(P, S, lane);
-    else if (warp == kQkWarp) qk_warp(S, lane);
-    else if (warp == kPvWarp) pv_warp(S, lane);
-    else if (warp == kItemWarp) item_warp(P, S, lane);
-    else if (warp == kPageWarp) page_warp(P, S, lane);
-    else query_warp(P, S, warp - kPageWarp - 1, lane);
-  }
+  if (warp < kSoftmaxWarps) softmax_warps(P, S, warp, lane);
+  else if (warp == kLoadWarp) load_warp(P, S, lane);
+  else if (warp == kQkWarp) qk_warp(S, lane);
+  else if (warp == kPvWarp) pv_warp(S, lane);
+  else if (warp == kItemWarp) item_warp(P, S, lane);
+  else page_warp(P, S, lane);
   __syncwarp();
   tc_fence_before();
   __syncthreads();
