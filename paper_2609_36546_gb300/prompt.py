@@ -7,6 +7,10 @@ a batch of prompts and issues its two calls on one stream:
                    write of their K/V rows into the model's paged cache
   ipd_prompt_attn  causal attention of the packed prompts
 
+Over a cache held in 8 bits the first is three, ipd_rope of the queries and of
+the keys and ipd_kv8_append; the attention reads the prompts' own rows, so its
+output does not depend on the cache's type.
+
 What lies between passes (projections, the LM head) is the caller's; the next
 tokens come from ipd.sample_trunc on the last positions' logits, and from then
 on the model proposes or verifies through VerifyStep over the same cache.
@@ -14,7 +18,7 @@ on the model proposes or verifies through VerifyStep over the same cache.
 from __future__ import annotations
 
 import math
-from typing import Optional, Sequence
+from typing import Optional, Sequence, Union
 
 import torch
 
@@ -24,13 +28,13 @@ from . import ipd
 class PromptPass:
     """Buffers and calls of one model's pass over new prompts.
 
-    cache: the model's ipd.KVCache; table: its rotary table ([max_pos, rot / 2,
+    cache: the model's ipd.KVCache or ipd.KVCache8; table: its rotary table ([max_pos, rot / 2,
     2], see ipd.rope_table); lens: the prompts' lengths (host ints, 0 allowed);
     page_table: [R, max_pages] int32 with the pages of every prompt, as a verify
     step takes it; num_q_heads: query heads.  The prompts start at position 0.
     """
 
-    def __init__(self, cache: ipd.KVCache, table: torch.Tensor, lens: Sequence[int],
+    def __init__(self, cache: Union[ipd.KVCache, ipd.KVCache8], table: torch.Tensor, lens: Sequence[int],
                  page_table: torch.Tensor, num_q_heads: int, layout: int = ipd.ROPE_HALF,
                  scale: float = 1.0 / math.sqrt(128.0), want_lse: bool = False, device="cuda"):
         lens = [int(n) for n in lens]
@@ -53,6 +57,10 @@ class PromptPass:
         # positions of the prompts' last tokens among the packed rows (-1: empty)
         self.last = torch.tensor([int(c) - 1 if n else -1 for c, n in zip(cu[1:], lens)],
                                  dtype=torch.int64)
+        # every row's position in its prompt (the fused append finds them itself)
+        self.pos: Optional[torch.Tensor] = (
+            torch.cat([torch.arange(n, dtype=torch.int32) for n in [0] + lens]).to(dev)
+            if isinstance(cache, ipd.KVCache8) else None)
         bf = dict(dtype=torch.bfloat16, device=dev)
         self.q = torch.empty(self.total, num_q_heads, 128, **bf)
         self.k = torch.empty(self.total, cache.num_kv_heads, 128, **bf)
@@ -61,11 +69,16 @@ class PromptPass:
             torch.empty(num_q_heads, self.total, dtype=torch.float32, device=dev) if want_lse else None)
 
     def run(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, stream=None) -> torch.Tensor:
-        """The two calls on the prompts' projected rows (q [total, Hq, 128], k and
+        """The calls on the prompts' projected rows (q [total, Hq, 128], k and
         v [total, Hkv, 128], before the rotation; views into one projection
         output are fine).  Returns the attention's output ([total, Hq, 128])."""
-        ipd.rope_append(self.cache, q, self.q, k, v, self.cu, self.seq_len, self.page_table,
-                        self.table, layout=self.layout, k_out=self.k, stream=stream)
+        if self.pos is None:
+            ipd.rope_append(self.cache, q, self.q, k, v, self.cu, self.seq_len, self.page_table,
+                            self.table, layout=self.layout, k_out=self.k, stream=stream)
+        else:
+            ipd.rope(q, self.q, self.pos, self.table, layout=self.layout, stream=stream)
+            ipd.rope(k, self.k, self.pos, self.table, layout=self.layout, stream=stream)
+            ipd.kv8_append(self.cache, self.k, v, self.cu, self.seq_len, self.page_table, stream=stream)
         ipd.prompt_attn(self.q, self.k, v, self.cu, self.max_len, self.out, self.scale,
                         lse=self.lse, stream=stream)
         return self.out
