@@ -1142,28 +1142,32 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
   return e0;
 }
 
-// Joins the parts of a row group of a task that was cut between CTAs, in order.
+// Joins the parts of a row group of a task that was cut between CTAs, in order; a warp a row.
 IPD_DEVINL void join(const Params &P, const Item &I, int r0, int rows, int warp, int lane) {
   const BatchDev &B = P.b[I.b];
   const size_t stride = (size_t)P.part_rows * (kD + 1);
-  auto slot_of = [&](int c) { return P.part + (size_t)(c == I.cta0 ? 2 * c + 1 : 2 * c) * stride; };
+  const int more = I.cta1 - I.ctab + 1;  // parts behind the first CTA's
 #pragma unroll 1
   for (int r = r0 + warp; r < r0 + rows; r += 4) {
-    float top = -INFINITY;
+    // (a row's sum and its dims in one place's two parts)
+    const float *lse = P.part + (size_t)P.part_rows * kD + r, *dims = P.part + (size_t)r * kD + lane * 4;
+    const size_t at0 = (2 * (size_t)I.cta0 + 1) * stride;
+    size_t at = 2 * (size_t)I.ctab * stride;
+    const float lse0 = lse[at0];
+    const float4 x0 = *reinterpret_cast<const float4 *>(dims + at0);
+    float top = lse0;
 #pragma unroll 1
-    for (int c = I.ctab + lane; c <= I.cta1; c += 32) top = fmaxf(top, slot_of(c)[(size_t)P.part_rows * kD + r]);
-    top = fmaxf(top, slot_of(I.cta0)[(size_t)P.part_rows * kD + r]);
+    for (int c = lane; c < more; c += 32) top = fmaxf(top, lse[at + c * 2 * stride]);
     top = warp_max(top);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
+    float sum = lse0 == -INFINITY ? 0.f : ex2_approx(lse0 - top);
+    float4 acc = make_float4(sum * x0.x, sum * x0.y, sum * x0.z, sum * x0.w);
 #pragma unroll 4
-    for (int i = I.ctab - 1; i <= I.cta1; ++i) {
-      const float *s = slot_of(i < I.ctab ? I.cta0 : i);
-      const float lse = s[(size_t)P.part_rows * kD + r];
-      const float4 x = *reinterpret_cast<const float4 *>(s + (size_t)r * kD + lane * 4);
-      const float w = lse == -INFINITY ? 0.f : ex2_approx(lse - top);
+    for (int i = 0; i < more; ++i, at += 2 * stride) {
+      const float l = lse[at];
+      const float4 x = *reinterpret_cast<const float4 *>(dims + at);
+      const float w = l == -INFINITY ? 0.f : ex2_approx(l - top);
       sum += w;
-      acc.x += w * x.x, acc.y += w * x.y, acc.z += w * x.z, acc.w += w * x.w;
+      acc.x = fmaf(w, x.x, acc.x), acc.y = fmaf(w, x.y, acc.y), acc.z = fmaf(w, x.z, acc.z), acc.w = fmaf(w, x.w, acc.w);
     }
     const float f = sum == 0.f ? 0.f : 1.f / sum;
     const int row = I.row0 + r, query = row / B.group;
