@@ -34,7 +34,8 @@ namespace {
 
 constexpr int kThreads = 512;  // of a verdict's CTA
 constexpr int kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 8;   // CTAs of a row in the row pass
+constexpr int kMaxVerdict = 16;  // ... of a request's verdict (as many as one may ask for)
 constexpr int kTile = 256;  // entries a warp sums at once: 8 a lane
 constexpr int kTiles = (IPD_TRUNC_MAX_VOCAB + 8) / kTile + 1;
 
@@ -445,6 +446,12 @@ IPD_DEVINL float logp_of(const Params &P, int row) {
   return z == 0 ? -INFINITY : (R.x - log2f((float)z * 0x1p-30f)) * kLn2;
 }
 
+__device__ __noinline__ void logps(const Params &P, int t) {
+  const float lp = logp_of(P, 2 * t), lq = logp_of(P, 2 * t + 1);
+  if (P.a.logp_target) P.a.logp_target[t] = lp;
+  if (P.a.logp_draft) P.a.logp_draft[t] = lq;
+}
+
 // What a residual is taken from: the target's row and the draft's, and their ratio.
 struct Residual {
   RowView p, q;
@@ -537,13 +544,11 @@ __global__ void __launch_bounds__(kThreads, 2) draft_verdict_kernel(const __grid
       }
     return;
   }
-  if (rank == csize - 1) {
-    for (int t = c0 + threadIdx.x; t < c1; t += kThreads) {
-      const float lp = logp_of(P, 2 * t), lq = logp_of(P, 2 * t + 1);
-      if (a.logp_target) a.logp_target[t] = lp;
-      if (a.logp_draft) a.logp_draft[t] = lq;
-    }
-  }
+  // The log-probabilities come last, from warps that the search for the token leaves.
+  const auto report = [&]() {
+    if (rank == csize - 1)
+      for (int t = c0 + threadIdx.x; t < c1; t += kThreads) logps(P, t);
+  };
   if (threadIdx.x == 0) S.n = c1 - c0;
   __syncthreads();
   for (int t = c0 + threadIdx.x; t < c1; t += kThreads)
@@ -563,17 +568,16 @@ __global__ void __launch_bounds__(kThreads, 2) draft_verdict_kernel(const __grid
     if (threadIdx.x == 0) {  // (the fp64 unit is narrow: once)
       const u64 zp = p.sum(P.pieces), zq = q.sum(P.pieces);
       S.m = 0, S.s = 0;
-      if (zp != 0 && zq != 0) {
-        int e;
-        const double f = frexp(__ddiv_rn((double)zp, (double)zq), &e);
-        S.m = (u64)(f * 0x1p31);
-        S.s = 31 - e;  // 13 .. 49
+      if (zp != 0 && zq != 0) {  // (the quotient's leading 31 bits)
+        const u64 f = (u64)__double_as_longlong(__ddiv_rn((double)zp, (double)zq));
+        S.m = (f & 0xfffffffffffffull | 1ull << 52) >> 22;
+        S.s = 31 + 1022 - (int)(f >> 52);  // 13 .. 49
       }
     }
   }
   if (full ? !a.logits_bonus : top == -INFINITY) {
     if (rank == 0 && threadIdx.x == 0) a.next_token[r] = -1;
-    return;
+    return report();
   }
   const uint16_t *pp = full ? a.logits_bonus + (long long)r * a.bonus_stride
                             : a.logits_target + (long long)at * a.target_stride;
@@ -596,6 +600,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_verdict_kernel(const __grid
   const int tiles = (to - from + 31) / 32;
   u64 total = 0, before = 0;
   for (int round = 0; round < 2; ++round) {
+    if (round && csize > 1) cluster_wait();  // (the others have read S.sum)
     u64 mine = 0;
     uint4 v, o;  // the next tile's, under way
     if (from + warp * 32 + lane < to) D.load(from + warp * 32 + lane, v, o);
@@ -622,19 +627,21 @@ __global__ void __launch_bounds__(kThreads, 2) draft_verdict_kernel(const __grid
       const u64 part = lane < (int)csize ? remote_ld64(&S.sum, lane) : 0ull;
       total = warp_sum64(part);
       before = warp_sum64(lane < (int)rank ? part : 0ull);
-      cluster_sync();
+      cluster_arrive();  // (waited for before S.sum changes, and at the end)
     }
     if (total != 0 || D.m == 0) break;
     D.m = 0;
   }
-  if (total == 0) {  // (a bonus row without an entry)
-    if (rank == 0 && threadIdx.x == 0) a.next_token[r] = -1;
-    return;
+  if (csize > 1) cluster_wait();
+  if (total == 0 || warp != 0) {
+    if (total == 0 && rank == 0 && threadIdx.x == 0) a.next_token[r] = -1;  // (a bonus row without an entry)
+    return report();
   }
+  report();
   const float u = a.u_next[r];
   const double d = u > 0.f ? floor(__dmul_rn((double)u, (double)total)) : 0.0;
   const u64 pos = d < (double)total ? (u64)d : total - 1;
-  if (warp != 0 || pos < before) return;
+  if (pos < before) return;
   u64 left = pos - before;
   // the tile: 32 at a time
   int k0 = 0;
@@ -743,6 +750,8 @@ extern "C" int ipd_verify_draft(const ipd_draft_args *args, void *workspace,
     int n = 0;
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
       return IPD_ERR_CUDA;
+    if (cudaFuncSetAttribute(draft_verdict_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+      return IPD_ERR_CUDA;
     g_sms[dev] = n;
   }
   const int sms = g_sms[dev];
@@ -764,7 +773,7 @@ extern "C" int ipd_verify_draft(const ipd_draft_args *args, void *workspace,
                hist ? kBins * 4 : 0, false, P, st) != IPD_OK)
       return IPD_ERR_CUDA;
   }
-  int c = kMaxCluster;
+  int c = kMaxVerdict;
   while (c > 1 && ((long long)a.num_reqs * c > 2LL * sms || vecs < c * 512)) c /= 2;
   P.piece = (vecs + 32 * c - 1) / (32 * c) * 32;
   return launch(draft_verdict_kernel, a.num_reqs, c, kThreads, 0, a.total > 0, P, st);
