@@ -239,11 +239,6 @@ IPD_DEVINL void tc_ld_x1(uint32_t taddr, uint32_t &r) {
 IPD_DEVINL void tc_st_x1(uint32_t taddr, uint32_t r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(r) : "memory");
 }
-IPD_DEVINL u64 mul2(u64 a, u64 b) {
-  u64 d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 IPD_DEVINL uint32_t half2_of(float lo, float hi) {
   uint32_t d;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
@@ -913,7 +908,7 @@ IPD_DEVINL void exponents(const uint32_t (&s)[NR], const float4 *state, float ck
 #pragma unroll
   for (int i = 0; i < NR; i += 2) {
     const float4 st = state[i / 2];
-    y[i / 2] = f2_fma(mul2(f2_pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), ck2), f2_pack(st.x, st.y),
+    y[i / 2] = f2_fma(f2_mul(f2_pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), ck2), f2_pack(st.x, st.y),
                       f2_pack(st.z, st.w));
   }
 }
@@ -1100,7 +1095,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
           float p0, p1;
           f2_unpack(p, p0, p1);
           p = f2_pack(ex2_approx(p0), ex2_approx(p1));
-          f2_unpack(mul2(p, fk2), p0, p1);
+          f2_unpack(f2_mul(p, fk2), p0, p1);
           h[k] = half2_of(p0, p1);
         }
         hi[q] = e4m3x4_h(h[0], h[1]);

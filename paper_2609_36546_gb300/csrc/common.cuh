@@ -300,6 +300,11 @@ IPD_DEVINL unsigned long long f2_add(unsigned long long a, unsigned long long b)
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+IPD_DEVINL unsigned long long f2_mul(unsigned long long a, unsigned long long b) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 IPD_DEVINL unsigned long long f2_sub(unsigned long long a, unsigned long long b) {
   unsigned long long d;
   asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));

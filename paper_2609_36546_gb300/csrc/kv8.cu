@@ -44,14 +44,27 @@ struct AppendParams {
   int n;
 };
 
+// A request with cu_new[r] <= tok, the last one where offsets are in order; 32 probes a
+// round (for a whole warp).
+IPD_DEVINL int request_before(const ipd_kv8_append_desc &D, int tok, int lane) {
+  int from = 0, end = D.num_reqs;
+  while (end - from > 1) {
+    const int step = (end - from + 31) / 32, at = from + lane * step;
+    const uint32_t in = __ballot_sync(0xffffffffu, at < end && D.cu_new[at] <= tok);
+    if (in != 0) from += (31 - __clz(in)) * step;
+    end = min(end, from + step);
+  }
+  return from;
+}
+
 // The run that starts with new row `tok`: its page (< 0: none starts here, or it
-// is at fault), first slot and number of rows.
-IPD_DEVINL int find_run(const ipd_kv8_append_desc &D, int tok, int *slot, int *rows) {
+// is at fault), first slot and number of rows.  Its request is `lo` or a later one.
+IPD_DEVINL int find_run(const ipd_kv8_append_desc &D, int lo, int tok, int *slot, int *rows) {
   if (tok < D.cu_new[0] || tok >= D.cu_new[D.num_reqs]) {
     ipd_set_error(&g_kv8_err, IPD_DEVERR_SPAN);
     return -1;
   }
-  int lo = 0, hi = D.num_reqs - 1;  // the last request with cu_new[r] <= tok
+  int hi = tok < D.cu_new[lo + 1] ? lo : D.num_reqs - 1;  // the last request with cu_new[r] <= tok
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (D.cu_new[mid] <= tok) lo = mid;
@@ -78,13 +91,19 @@ IPD_DEVINL int find_run(const ipd_kv8_append_desc &D, int tok, int *slot, int *r
   return page;
 }
 
-// largest |entry| among the finite of four bf16, as bits of a non-negative bf16
-IPD_DEVINL uint32_t finite_max(uint2 v) {
+IPD_DEVINL uint32_t max_abs2(uint32_t m, const uint4 &v) {
+  return __vmaxu2(__vmaxu2(m, __vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu)),
+                  __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+}
+// largest |entry| among the finite of eight bf16, as bits of a non-negative bf16
+IPD_DEVINL uint32_t finite_max(const uint4 &v) {
   uint32_t m = 0;
-  const uint32_t w[4] = {v.x & 0x7fffu, v.x >> 16 & 0x7fffu, v.y & 0x7fffu, v.y >> 16 & 0x7fffu};
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (w[i] < 0x7f80u) m = max(m, w[i]);
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = w[i] & 0x7fffu, hi = w[i] >> 16 & 0x7fffu;
+    m = max(m, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+  }
   return m;
 }
 
@@ -98,14 +117,21 @@ IPD_DEVINL int byte_of(uint32_t m) {
   return max(kLeast, E - 8 + ((f & 0x7fffffu) > 0x600000u ? 1 : 0));
 }
 
-// four entries times s as e4m3; what is not finite becomes NaN
-IPD_DEVINL uint32_t quantise(uint2 v, float s) {
-  float x[4] = {bf16lo(v.x), bf16hi(v.x), bf16lo(v.y), bf16hi(v.y)};
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    x[i] = (__float_as_uint(x[i]) & 0x7f800000u) == 0x7f800000u ? __uint_as_float(0x7fc00000u) : x[i] * s;
-  return e4m3x2(x[0], x[1]) | e4m3x2(x[2], x[3]) << 16;
+// four values times s as e4m3
+IPD_DEVINL uint32_t four(const float *x, float s) {
+  const unsigned long long ss = f2_pack(s, s);
+  float y[4];
+  f2_unpack(f2_mul(f2_pack(x[0], x[1]), ss), y[0], y[1]);
+  f2_unpack(f2_mul(f2_pack(x[2], x[3]), ss), y[2], y[3]);
+  return e4m3x2(y[0], y[1]) | e4m3x2(y[2], y[3]) << 16;
 }
+// eight entries, none of them an infinity, times s as e4m3
+IPD_DEVINL uint2 quantise(const uint4 &v, float s) {
+  const float x[8] = {bf16lo(v.x), bf16hi(v.x), bf16lo(v.y), bf16hi(v.y), bf16lo(v.z), bf16hi(v.z), bf16lo(v.w), bf16hi(v.w)};
+  return make_uint2(four(x, s), four(x + 4, s));
+}
+
+IPD_DEVINL void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 __global__ void __launch_bounds__(kThreads) kv8_append_kernel(
     const __grid_constant__ AppendParams P) {
@@ -128,38 +154,60 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(
     uint8_t *scales = is_v ? D.cache.v_scale : D.cache.k_scale;
     int page = -1, slot = 0, rows = 0;
     const int tok = g * A.group + lane;
-    if (lane < A.group && tok < D.total_new) page = find_run(D, tok, &slot, &rows);
+    {  // the group's rows on their way to L2, while their places are looked up
+      const int row = g * A.group + (lane >> 1);
+      if (lane < 2 * A.group && row < D.total_new) prefetch_l2(src + row * stride + h * 128 + (lane & 1) * 64);
+    }
+    const int lo = request_before(D, g * A.group, lane);
+    if (lane < A.group && tok < D.total_new) page = find_run(D, lo, tok, &slot, &rows);
     uint32_t left = __ballot_sync(0xffffffffu, page >= 0);
     while (left) {
       const int from = __ffs(left) - 1;
       left &= left - 1;
       const int pg = __shfl_sync(0xffffffffu, page, from), s0 = __shfl_sync(0xffffffffu, slot, from),
                 n = __shfl_sync(0xffffffffu, rows, from);
-      const uint16_t *x = src + (long long)(g * A.group + from) * stride + h * 128 + lane * 4;
+      // half a warp a row, eight entries a lane
+      const int half = lane >> 4, part = lane & 15;
+      const uint16_t *x = src + (long long)(g * A.group + from + half) * stride + h * 128 + part * 8;
       uint8_t *scale = scales + (size_t)pg * hkv + h;
-      uint32_t *dst = reinterpret_cast<uint32_t *>(pages + ((size_t)pg * hkv + h) * 2048) + lane;
-      uint2 v[16];
+      uint2 *dst = reinterpret_cast<uint2 *>(pages + ((size_t)pg * hkv + h) * 2048) + half * 16 + part;
+      uint4 v[8];
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        v[i] = i < n ? *reinterpret_cast<const uint2 *>(x + i * stride) : make_uint2(0u, 0u);
+      for (int i = 0; i < 8; ++i)
+        v[i] = 2 * i + half < n ? *reinterpret_cast<const uint4 *>(x + 2 * i * stride) : make_uint4(0u, 0u, 0u, 0u);
       const int was = s0 > 0 ? *scale : 0;
       uint32_t m = 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) m = max(m, finite_max(v[i]));
-      const int b = max(byte_of(__reduce_max_sync(0xffffffffu, m)), was);
+      for (int i = 0; i < 8; ++i) m = max_abs2(m, v[i]);
+      m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+      if (m >= 0x7f80u) {  // not all of the run's rows are finite
+        m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          uint32_t *w = &v[i].x;
+          m = max(m, finite_max(v[i]));
+          // infinities become NaN (the conversion would take them for 448)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[e] |= __vcmpeq2(w[e] & 0x7fff7fffu, 0x7f807f80u);
+        }
+        m = __reduce_max_sync(0xffffffffu, m);
+      }
+      const int b = max(byte_of(m), was);
       if (s0 > 0 && b != was) {
         const float f = pow2i(was - b);  // b is not 255 where it grew
-#pragma unroll 4
-        for (int i = 0; i < s0; ++i) {
-          float y[4];
-          e4m3x4_to_floats(dst[i * 32], y);
-          dst[i * 32] = e4m3x2(y[0] * f, y[1] * f) | e4m3x2(y[2] * f, y[3] * f) << 16;
+#pragma unroll 2
+        for (int i = half; i < s0; i += 2) {
+          uint2 &w = dst[(i - half) * 16];
+          float y[4], z[4];
+          e4m3x4_to_floats(w.x, y), e4m3x4_to_floats(w.y, z);
+          w = make_uint2(four(y, f), four(z, f));
         }
       }
       const float f = b == 255 ? __uint_as_float(0x7fc00000u) : pow2i(127 - b);
+      dst += s0 * 16;
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i < n) dst[(s0 + i) * 32] = quantise(v[i], f);
+      for (int i = 0; i < 8; ++i)
+        if (2 * i + half < n) dst[i * 32] = quantise(v[i], f);
       __syncwarp();  // every lane has read the page's present scale
       if (lane == 0) *scale = (uint8_t)b;
     }

@@ -4,12 +4,6 @@
 
 typedef unsigned long long u64;
 
-IPD_DEVINL u64 f2_mul(u64 a, u64 b) {
-  u64 d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
 IPD_DEVINL u64 f2_add_rz(u64 a, u64 b) {
   u64 d;
   asm("add.rz.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
