@@ -1137,40 +1137,79 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
   return e0;
 }
 
-// Joins the parts of a row group of a task that was cut between CTAs, in order; a warp a row.
-IPD_DEVINL void join(const Params &P, const Item &I, int r0, int rows, int warp, int lane) {
+// Joins the parts of a row group of a task that was cut between CTAs, in order.  What bounds it is
+// the time until another SM's rows arrive, 1,600 cycles or more at a time: a warp has four parts of
+// two rows under way, or eight of one row where there are no more rows than warps.
+struct Parts {
+  const float *first;  // the first CTA's
+  ptrdiff_t next, step; // from it to the next one's, and on
+  int n;
+};
+template <int kAtOnce, int kParts>
+IPD_DEVINL void join_rows(const Params &P, const Item &I, const Parts &A, int r0, int rows, int warp, int lane) {
   const BatchDev &B = P.b[I.b];
-  const size_t stride = (size_t)P.part_rows * (kD + 1);
-  const int more = I.cta1 - I.ctab + 1;  // parts behind the first CTA's
 #pragma unroll 1
-  for (int r = r0 + warp; r < r0 + rows; r += 4) {
-    // (a row's sum and its dims in one place's two parts)
-    const float *lse = P.part + (size_t)P.part_rows * kD + r, *dims = P.part + (size_t)r * kD + lane * 4;
-    const size_t at0 = (2 * (size_t)I.cta0 + 1) * stride;
-    size_t at = 2 * (size_t)I.ctab * stride;
-    const float lse0 = lse[at0];
-    const float4 x0 = *reinterpret_cast<const float4 *>(dims + at0);
-    float top = lse0;
-#pragma unroll 1
-    for (int c = lane; c < more; c += 32) top = fmaxf(top, lse[at + c * 2 * stride]);
-    top = warp_max(top);
-    float sum = lse0 == -INFINITY ? 0.f : ex2_approx(lse0 - top);
-    float4 acc = make_float4(sum * x0.x, sum * x0.y, sum * x0.z, sum * x0.w);
-#pragma unroll 4
-    for (int i = 0; i < more; ++i, at += 2 * stride) {
-      const float l = lse[at];
-      const float4 x = *reinterpret_cast<const float4 *>(dims + at);
-      const float w = l == -INFINITY ? 0.f : ex2_approx(l - top);
-      sum += w;
-      acc.x = fmaf(w, x.x, acc.x), acc.y = fmaf(w, x.y, acc.y), acc.z = fmaf(w, x.z, acc.z), acc.w = fmaf(w, x.w, acc.w);
+  for (int r = warp; r < rows; r += 4 * kAtOnce) {
+    int at[kAtOnce];
+    float top[kAtOnce], sum[kAtOnce];
+    float4 acc[kAtOnce];
+    const float *sums[kAtOnce], *dims[kAtOnce];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      at[j] = min(r + 4 * j, rows - 1);  // (the last row twice, rather than none)
+      top[j] = -INFINITY, sum[j] = 0.f, acc[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      sums[j] = A.first + (size_t)P.part_rows * kD + r0 + at[j], dims[j] = A.first + (r0 + at[j]) * kD + lane * 4;
     }
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
-    const int row = I.row0 + r, query = row / B.group;
-    *reinterpret_cast<uint2 *>(B.out + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * B.group + (row - query * B.group)) * kD +
-                               lane * 4) =
-        make_uint2((uint32_t)f2bf16(acc.x * f) | (uint32_t)f2bf16(acc.y * f) << 16,
-                   (uint32_t)f2bf16(acc.z * f) | (uint32_t)f2bf16(acc.w * f) << 16);
+#pragma unroll 1
+    for (int i = 0; i < A.n; i += kParts) {
+      float l[kAtOnce][kParts];
+      float4 x[kAtOnce][kParts];
+#pragma unroll
+      for (int k = 0; k < kParts; ++k) {
+        const bool there = i + k < A.n;
+        const ptrdiff_t on = i + k == 0 ? A.next : A.step;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+          l[j][k] = there ? *sums[j] : -INFINITY;
+          x[j][k] = there ? *reinterpret_cast<const float4 *>(dims[j]) : make_float4(0.f, 0.f, 0.f, 0.f);
+          sums[j] += on, dims[j] += on;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        float now = top[j];
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) now = fmaxf(now, l[j][k]);
+        const float base = now == -INFINITY ? 0.f : now, f = ex2_approx(top[j] - base);
+        top[j] = now;
+        sum[j] *= f, acc[j].x *= f, acc[j].y *= f, acc[j].z *= f, acc[j].w *= f;
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) {
+          const float w = ex2_approx(l[j][k] - base);
+          const float4 v = x[j][k];
+          sum[j] += w;
+          acc[j].x = fmaf(w, v.x, acc[j].x), acc[j].y = fmaf(w, v.y, acc[j].y);
+          acc[j].z = fmaf(w, v.z, acc[j].z), acc[j].w = fmaf(w, v.w, acc[j].w);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      const float f = sum[j] == 0.f ? 0.f : 1.f / sum[j];
+      const int row = I.row0 + r0 + at[j], query = row / B.group;
+      *reinterpret_cast<uint2 *>(
+          B.out + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * B.group + (row - query * B.group)) * kD + lane * 4) =
+          make_uint2((uint32_t)f2bf16(acc[j].x * f) | (uint32_t)f2bf16(acc[j].y * f) << 16,
+                     (uint32_t)f2bf16(acc[j].z * f) | (uint32_t)f2bf16(acc[j].w * f) << 16);
+    }
   }
+}
+IPD_DEVINL void join(const Params &P, const Item &I, int r0, int rows, int warp, int lane) {
+  const size_t stride = (size_t)P.part_rows * (kD + 1);
+  const Parts A{P.part + (2 * (size_t)I.cta0 + 1) * stride, (2 * (I.ctab - I.cta0) - 1) * (ptrdiff_t)stride,
+                2 * (ptrdiff_t)stride, I.cta1 - I.ctab + 2};
+  if (rows <= 4) join_rows<1, 8>(P, I, A, r0, rows, warp, lane);
+  else join_rows<2, 4>(P, I, A, r0, rows, warp, lane);
 }
 
 // A row group of an item: its tiles, then its rows.
