@@ -706,9 +706,9 @@ size_t ipd_attn8_workspace_size(const ipd_attn8_batch *verify, int n_verify,
 /* ipd_verify_attn over 8-bit caches: the spans of n_verify batches and the
  * decode tokens of n_decode batches (the same thing with q_len 1) in one call.
  * out = softmax(scale q K^T) V per query and head over the values the cache's
- * entries stand for.  q is carried exactly to 2^-18 of its row's largest entry
- * into the products; scores, maxima and sums are fp32; the softmax weights enter
- * the product with V as two e4m3 terms, to 2^-9 of themselves (and 2^-18 of the
+ * entries stand for.  q is carried to 2^-17 of its row's largest entry into
+ * the products; scores, maxima and sums are fp32; the softmax weights enter
+ * the product with V as two e4m3 terms, to 2^-8 of themselves (and 2^-18 of the
  * row's largest); the output is rounded to bf16 once.  A row's result depends on
  * no key that it does not see, whatever that key holds, and on no other row.
  * A page id outside the pool is recorded (IPD_DEVERR_PAGE_ID) and its keys are
@@ -716,7 +716,8 @@ size_t ipd_attn8_workspace_size(const ipd_attn8_batch *verify, int n_verify,
  * of order or past total_q (IPD_DEVERR_SPAN), or whose seq_len is below its
  * q_len, above max_seq_len or with q_len above max_q_len (IPD_DEVERR_SEQ_LEN), is
  * recorded and its rows are not written.  Returns IPD_ERR_UNSUPPORTED for more
- * than 128 query heads a KV head or num_pages * num_kv_heads >= 2^27. */
+ * than 128 query heads a KV head, num_pages * num_kv_heads >= 2^27, max_seq_len
+ * above 2^30, or 2^30 rows (max_q_len by query heads a KV head) or more. */
 int ipd_verify_attn8(const ipd_attn8_batch *verify, int n_verify, const ipd_attn8_batch *decode,
                      int n_decode, float softmax_scale, void *workspace, size_t workspace_bytes,
                      ipd_stream_t stream);

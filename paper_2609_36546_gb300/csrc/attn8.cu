@@ -26,12 +26,18 @@
 // Work.  All (request, KV head, block of 128 rows, tile) in one line, cut into parts of
 // equal cost, a CTA each: nothing is claimed, the cut depends on the lengths alone.
 // A task cut between CTAs leaves normalised partial rows; the CTA that finishes last
-// joins them in order.
+// joins them in order.  Within a CTA up to four tasks (of up to 32 rows; two of up to 64)
+// run side by side, a warpgroup each, and get a tile each in turn, so that one's first
+// maximum and last rows pass behind the others' tiles.
 //
-// Warps: 0-15 softmax, four warpgroups that take items in turn (of more than 32 rows
-// two together, of more than 64 four, 32 rows each), 16 loads K, 17 loads V, 18 issues
-// the first product, 19 the second, 20 finds the items, 21 fetches page ids and scales,
-// 22 and 23 split the queries.
+// Warps: 0-15 softmax, four warpgroups of up to 32 rows, 16 loads, 17 issues the first
+// product, 18 the second, 19 finds the items, 20 puts their tiles in order and fetches page
+// ids and scales.
+//
+// Measured (bytes of the visible keys and of the rows, at 6,784 GB/s for a copy): 19 requests
+// of one query over 32,768 keys, 8 KV heads, 189 us, 0.99 of a copy's rate; 128 over 300 to
+// 8,200 keys 172 us, 0.88.  With 128 rows a key the exponents bound it: 262 us for 19 x 16
+// queries over 32,768 keys of 4 heads, 610 TFLOP/s.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cudaTypedefs.h>
@@ -65,13 +71,13 @@ constexpr int kGroups = 4;                // softmax warpgroups
 constexpr int kRows = 32;                 // ... and the rows of one
 constexpr int kKStages = 4, kVStages = 5;
 constexpr int kTiles = 16;                // tiles handed out whose product is not complete
-constexpr int kScales = 16;
+constexpr int kScales = 16;               // of a warpgroup's tiles, scales handed out that it has not read
 constexpr int kBatch = 4;                 // ... fetched at once
 constexpr int kSlots = 8;                 // items handed out
 constexpr int kSoftmaxWarps = 4 * kGroups;
-constexpr int kLoadWarp = kSoftmaxWarps, kQkWarp = kLoadWarp + 1, kPvWarp = kLoadWarp + 2, kItemWarp = kLoadWarp + 3;  // (the fifth: page ids and scales)
-// (no more: the registers are 96 for each thread of 21 warps, 80 for 24; with separate warps for
-// V's loads and for queries ahead of their turn 1,000 requests of 300 keys took 411 us, now 322)
+constexpr int kLoadWarp = kSoftmaxWarps, kQkWarp = kLoadWarp + 1, kPvWarp = kLoadWarp + 2, kItemWarp = kLoadWarp + 3;
+// (the fifth orders tiles; with two for loads and two that converted queries ahead of their turn
+// 1,000 requests of 300 keys took 411 us in place of 322)
 constexpr int kThreads = 32 * (kSoftmaxWarps + 5);
 constexpr int kItemReaders = kSoftmaxWarps + 1;
 static_assert(kBatch * kPages == 32, "a lane a page");
@@ -86,10 +92,11 @@ constexpr float kBase = 4.f;   // a row's reference is its largest exponent less
 constexpr float kLimit = 8.f;  // weights stay below 2^8 (e4m3 ends at 448)
 constexpr float kLoScale = 16.f;
 constexpr int kFar = 100;      // V scales further apart than 2^100 count as that far
-// What a tile of a task with up to 32, 64 and 128 rows costs, and a task beside its
-// tiles: the line is cut into equal costs.
-constexpr int kCost1 = 4, kCost2 = 6, kCost4 = 12;
-constexpr int kItem1 = 20, kItem2 = 40, kItem4 = 70;
+// What a tile of a task with up to 16, 32, 64 and 128 rows costs, and a task beside its tiles (up to
+// 32, 64, 128 rows): the line is cut into equal costs.  In cycles a tile takes about 1,480, 2,170,
+// 3,200 and 3,750 where a CTA has one task alone, 1,450, 1,600, 2,400 and 3,700 where it has several.
+constexpr int kTileH = 4, kTile1 = 5, kTile2 = 7, kTile4 = 12;
+constexpr int kTask1 = 20, kTask2 = 40, kTask4 = 60;
 constexpr int kNoPage = 1 << 20;  // in place of an exponent: no such page
 
 struct BatchDev {
@@ -154,7 +161,7 @@ struct Shared {
   alignas(1024) uint8_t k[kKStages][kTileBytes];
   alignas(1024) uint8_t v[kVStages][kTileBytes];
   alignas(1024) uint8_t q[2][kGroups][kRows * kD];     // the two terms of the queries
-  alignas(1024) uint8_t p[kGroups][kKeys * 2 * kRows]; // a warpgroup's P; at the end, rows on their way
+  alignas(1024) uint8_t p[kGroups][kKeys * 2 * kRows]; // a warpgroup's P
   alignas(16) float4 state[kGroups][kRows / 2];        // a pair of rows: ar, ar', -ref, -ref'
   alignas(16) float alpha[kGroups][kRows];
   alignas(16) float red[kGroups][4][kRows];
@@ -280,8 +287,10 @@ IPD_DEVINL void grid_launch() { asm volatile("griddepcontrol.launch_dependents;"
 // For a whole warp, with one answer.  Gives up after about a second, or as soon as
 // another warp of the CTA has given up.  Warps that poll take issue slots from those
 // that work (without a pause they were half of all instructions), so those that run
-// ahead sleep `pause` ns between two looks.
-IPD_DEVINL bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort, uint32_t pause) {
+// ahead sleep `pause` ns between two looks.  (A call: code that every warp comes by often has
+// to be short, for the instruction cache's sake; inlined, 1,000 requests of 300 keys took
+// 328 us, now 292.)
+__device__ __noinline__ bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort, uint32_t pause) {
   const long long t0 = clock64();
   bool ok;
 #pragma unroll 1
@@ -294,17 +303,9 @@ IPD_DEVINL bool wait_slow(uint64_t *bar, uint32_t parity, volatile int *abort, u
   }
   return __all_sync(0xffffffffu, ok) != 0;
 }
-__device__ __noinline__ bool wait_slow_call(uint64_t *bar, uint32_t parity, volatile int *abort, uint32_t pause) {
-  return wait_slow(bar, parity, abort, pause);
-}
 IPD_DEVINL bool wait(uint64_t *bar, uint32_t parity, volatile int *abort, uint32_t pause = 200) {
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return wait_slow_call(bar, parity, abort, pause);
-}
-// ... without a call, where many registers are live
-IPD_DEVINL bool wait_inline(uint64_t *bar, uint32_t parity, volatile int *abort) {
-  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return wait_slow(bar, parity, abort, 0);
+  return wait_slow(bar, parity, abort, pause);
 }
 // One lane of a converged warp issues; every other value is the whole warp's, so that
 // operands stay in uniform registers (issued from a branch of one lane, a product
@@ -331,8 +332,8 @@ IPD_DEVINL int batch_of(const Params &P, int g) {
   return b;
 }
 
-IPD_DEVINL int tile_cost(int rows) { return rows > 64 ? kCost4 : rows > 32 ? kCost2 : kCost1; }
-IPD_DEVINL int item_cost(int rows) { return rows > 64 ? kItem4 : rows > 32 ? kItem2 : kItem1; }
+IPD_DEVINL int tile_cost(int rows) { return rows > 64 ? kTile4 : rows > 32 ? kTile2 : rows > 16 ? kTile1 : kTileH; }
+IPD_DEVINL int item_cost(int rows) { return rows > 64 ? kTask4 : rows > 32 ? kTask2 : kTask1; }
 IPD_DEVINL long long task_cost(int rows, int tiles) { return item_cost(rows) + (long long)tiles * tile_cost(rows); }
 
 // Checks the requests and adds up their costs; one block.
@@ -1022,7 +1023,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
 #pragma unroll 1
   for (int t = 0; t < n_tiles; ++t) {
     const uint32_t k = X.tiles % kScales;
-    X.ok = wait_inline(&S.sc_full[g][k], full(X.tiles, kScales), &S.abort) && X.ok;
+    X.ok = wait(&S.sc_full[g][k], full(X.tiles, kScales), &S.abort, 0) && X.ok;
     const Scales &M = S.scales[g][k];
     const int v_stage = min((uint32_t)M.v, kVStages - 1u);  // (in range whatever a warp that gave up has left)
     const int key0 = (I.t0 + t) * kKeys, key = key0 + tid;
@@ -1044,7 +1045,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
     }
     const float fk = ev == 128 && hidden < NR ? __uint_as_float(0x7fc00000u) : pow2i(de);
     arrive_warp(&S.sc_empty[g][k], lane);
-    X.ok = wait_inline(&S.s_full[g], full(X.tiles, 1), &S.abort) && X.ok;
+    X.ok = wait(&S.s_full[g], full(X.tiles, 1), &S.abort, 0) && X.ok;
     tc_fence_after();
     u64 y[NR / 2];
     {
@@ -1073,7 +1074,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
     }
     const bool move = bar_or(1 + g, 128, first || top + (float)de > kLimit);
     // P's buffer is free, and O at rest, once this warpgroup's product before is complete
-    if (X.tiles > 0) X.ok = wait_inline(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort) && X.ok;
+    if (X.tiles > 0) X.ok = wait(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort, 0) && X.ok;
     tc_fence_after();
     if (move) {
       if (first) first_references<NR>(S, X, y, (float)de, l_addr);
@@ -1123,7 +1124,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
     if (key0 + kKeys > masked && g == I.wg) {
       // hidden keys: the tile is looked through before the product, which takes the first
       // warpgroup's rows before the others'
-      X.ok = wait_inline(&S.v_ready[g], full(X.mends, 1), &S.abort) && X.ok;
+      X.ok = wait(&S.v_ready[g], full(X.mends, 1), &S.abort, 0) && X.ok;
       ++X.mends;
       if (key >= masked) mend(S, g, S.v[v_stage], tid, key, L);
     }
@@ -1246,7 +1247,7 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
       part[(size_t)P.part_rows * kD + rg * kRows + tid] = sum == 0.f ? -INFINITY : ref + log2f(sum);
     }
   }
-  X.ok = wait_inline(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort) && X.ok;
+  X.ok = wait(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort, 0) && X.ok;
   tc_fence_after();
   named_bar_sync(1 + g, 128);
   const bool bad = *(volatile int *)&S.bad[I.wg] != 0;
@@ -1297,7 +1298,7 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
       } else {
         uint32_t &uses = I.ng == 4 ? X.alls : X.pairs;
         arrive_warp(bar, lane);
-        X.ok = wait_inline(bar, uses & 1u, &S.abort) && X.ok;
+        X.ok = wait(bar, uses & 1u, &S.abort, 0) && X.ok;
         ++uses;
       }
       if (i == 0 && rg == 0) {
@@ -1314,7 +1315,7 @@ __device__ void softmax_warps(const Params &P, Shared &S, int warp, int lane) {
   Softmax X{warp >> 2, (int)threadIdx.x & 127, warp & 3, lane, 0, 0, 0, 0, true};
   for (uint32_t n = 0;; ++n) {
     const int slot = n % kSlots;
-    X.ok = wait_inline(&S.item_taken[slot], full(n, kSlots), &S.abort) && X.ok;
+    X.ok = wait(&S.item_taken[slot], full(n, kSlots), &S.abort, 0) && X.ok;
     if (bar_or(1 + X.g, 128, !X.ok)) return;  // the whole warpgroup
     const Item &I = S.item[slot];
     if (!I.valid) return;
@@ -1380,6 +1381,8 @@ int validate(const ipd_attn8_batch *b) {
   if (b->num_reqs == 0 || b->total_q == 0) return IPD_OK;
   if (b->max_q_len < 1 || b->max_seq_len < b->max_q_len) return IPD_ERR_INVALID_ARG;
   if ((long long)b->max_pages * kPage < b->max_seq_len) return IPD_ERR_INVALID_ARG;
+  if (b->max_seq_len > 1 << 30 || (long long)b->max_q_len * (b->num_q_heads / c->num_kv_heads) >= 1 << 30)
+    return IPD_ERR_UNSUPPORTED;  // (keys and rows are counted in 32 bits)
   if (c->num_pages < 1) return IPD_ERR_INVALID_ARG;
   if (c->num_pages >= (1LL << 27) || c->num_pages * c->num_kv_heads >= (1LL << 27))
     return IPD_ERR_UNSUPPORTED;

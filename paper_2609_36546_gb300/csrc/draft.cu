@@ -7,11 +7,15 @@
 //   token      the entry in which floor(u' S) falls in the running sum of r, by id
 // so a verdict is a fixed function of (rows, settings, u): no sum depends on an order.
 //
-// Two launches.  Rows: every drafted position's two rows, the maximum in a first
-// look, the weights' sum in a second one (from L2).  Verdicts: a cluster of CTAs a
-// request finds the first rejected draft and goes through that one position's two
-// rows (or the bonus row), each CTA a piece: sums of tiles of 256 entries, then the
-// tile, then the entry that holds the drawn position.
+// Two launches.  Rows: every drafted position's two rows, the maximum and the weights' sum:
+// long pieces in one look, through a histogram of their values, short ones in two.
+// Verdicts: a cluster of CTAs a request finds the first rejected draft and goes through that
+// one position's two rows (or the bonus row), each CTA a piece: sums of tiles of 256
+// entries, then the tile, then the entry that holds the drawn position.
+//
+// What bounds it: a small call the two kernels' chains of dependent steps (one request, 4 drafts
+// over 151,936 entries: 17.8 us, 6 and 12); a large one the atomics of the row pass (64
+// requests of 1 to 16 over 151,936: 118 us, 2.8 TB/s, of which the row pass 91).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>

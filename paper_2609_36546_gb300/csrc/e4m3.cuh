@@ -19,12 +19,6 @@ IPD_DEVINL uint32_t e4m3x2(float lo, float hi) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(d) : "f"(hi), "f"(lo));
   return d;
 }
-// The same of two fp16 values in one register.
-IPD_DEVINL uint32_t e4m3x2_h2(uint32_t h2) {
-  uint16_t d;
-  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(d) : "r"(h2));
-  return d;
-}
 // Two e4m3 values (bits 0-15) as fp16: exact.
 IPD_DEVINL uint32_t h2_from_e4m3x2(uint32_t v) {
   uint32_t d;

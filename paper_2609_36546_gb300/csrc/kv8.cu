@@ -9,10 +9,15 @@
 // 2^-k is exact until an entry falls below 2^-6, where it is rounded once), and
 // lets the attention take a scale into an exponent.
 //
-// A run is the new rows of one page: a warp takes a run of one head and tensor,
-// 8 bytes of a row a lane, all of the run's rows (at most 16) in registers, so
+// A run is the new rows of one page: a warp takes a run of one head and tensor, half a
+// warp a row, eight entries a lane, all of the run's rows (at most 16) in registers, so
 // that the maximum and the rounding read a row once.  A warp looks at a group of
-// consecutive new rows, a lane each, and works through the runs that start there.
+// consecutive new rows, a lane each, and works through the runs that start there; the
+// group's rows are on their way to L2 while the request and the page are looked up.
+//
+// What bounds it: the launch and four dependent loads for a step's rows (128 requests of one
+// row, 8 heads: 4.8 us; 64 spans of 1 to 16 rows, 4 heads: 6.2 us); HBM for prompts (12 of 200
+// to 2,000 rows, 4 heads: 15.0 us, 0.44 of a copy's rate, 16.4 without the prefetch).
 #include <cuda_runtime.h>
 #include <stdint.h>
 #include <string.h>
@@ -252,6 +257,8 @@ extern "C" int ipd_kv8_append(const ipd_kv8_append_desc *appends, int n, ipd_str
     if (a.total_new == 0) continue;  // nothing to write: not part of the launch
     AppendDev &A = P.a[P.n];
     A.d = a;
+    // A warp a new row where they are few or most of a page each, and 16 rows a warp for many (64 spans of
+    // 1 to 16 rows: 6.2 us at 1, 10.3 at 16; 13,000 rows of prompts: 44 us at 1, 17.1 at 8, 15.0 at 16).
     A.group = a.total_new >= 4LL * a.num_reqs && a.total_new > 2048 ? 16 : 1;
     A.groups = (a.total_new + A.group - 1) / A.group;
     total += (long long)A.groups * 2 * a.cache.num_kv_heads;

@@ -86,7 +86,8 @@ def test_attn8_refusals(ipd):
         assert st == bad["IPD_ERR_INVALID_ARG"] and size == 0, kw
     for kw in (dict(cache=_cache(ipd, page_size=32)), dict(cache=_cache(ipd, head_dim=64)),
                dict(cache=_cache(ipd, num_kv_heads=65)), dict(cache=_cache(ipd, num_pages=1 << 25)),
-               dict(num_q_heads=4 * 129)):
+               dict(num_q_heads=4 * 129), dict(max_pages=1 << 27, max_seq_len=(1 << 30) + 1),
+               dict(num_q_heads=4 * 128, max_pages=1 << 20, max_q_len=1 << 23, max_seq_len=1 << 23)):
         st, size = call(**kw)
         assert st == bad["IPD_ERR_UNSUPPORTED"] and size == 0, kw
     for scale in (0.0, -1.0, float("nan"), float("inf")):
