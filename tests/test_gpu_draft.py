@@ -141,6 +141,44 @@ def test_unusual_rows(lib):
     c.run(lib).check()
 
 
+@pytest.mark.parametrize("R,V", [(90, 9001), (45, 60001), (90, 8193), (160, 8190)])
+def test_long_rows_of_any_values(lib, R, V):
+    """Rows that are read once, by a histogram of their values (whole ones, and pieces of split
+    ones), and those that cannot be: values of both kinds of zero and near it (few, as many as a
+    list holds, more), at both ends of what has a bin, masks, NaN, infinities, a temperature at
+    which nothing is small."""
+    c = Case([2] * R, V, seed=V)
+    t, d = c.target, c.draft
+    low, tiny = torch.finfo(torch.bfloat16).min, torch.finfo(torch.bfloat16).tiny
+    cut = torch.tensor(2.0 ** -19).to(torch.bfloat16)
+    t[0, ::3], t[0, 1::3], d[0, ::2] = 0.0, -0.0, -0.0
+    t[2, :200], d[2, 40:90] = tiny, -tiny
+    t[4, :256], d[4, :256] = cut / 2, -cut / 2            # a full list
+    t[6, :257], d[6, 5000:5257] = cut / 2, cut / 4        # one more
+    t[8, :], d[8, :] = tiny, 0.0
+    t[10, ::5], d[10, 1::5] = cut, -cut                   # the smallest value with a bin
+    t[12, 100], d[12, 101] = 4096.0, 4064.0               # the first without, the last with
+    t[14, 100], d[14, 101] = -4096.0, -4064.0
+    t[16, ::2], d[16, 1::2] = low, NINF
+    t[18, ::2], d[18, ::7] = float("nan"), float("nan")
+    t[20, V - 1] = d[20, 0] = float("inf")
+    t[22, :], d[24, :] = NINF, NINF
+    t[26, 1:], d[26, 1:] = low, low
+    t[28, :], d[28, :] = -3000.0, -5000.0
+    t[30, :], d[30, :] = 5000.0, 3000.0
+    t[32, 3:], d[32, 3:] = NINF, NINF
+    t[34, :], d[34, :] = 1.0, 1.0
+    c.inv_p[18], c.inv_q[18] = 0.004, 0.004               # requests 18 to 20: -4096 has a weight
+    c.inv_p[19], c.inv_q[20] = 0.01, 0.02
+    t[38, ::2], d[40, ::2] = -4090.0, -9000.0
+    c.inv_p[21], c.inv_q[21] = 50.0, 0.7
+    c.run(lib).check()
+    first = c.nxt.clone(), c.n.clone(), c.lp.clone()
+    for x, y in zip(first, (lambda r: (r.nxt, r.n, r.lp))(c.run(lib))):
+        assert torch.equal(x.nan_to_num(), y.nan_to_num())
+    assert lib.device_error() == 0
+
+
 def test_bad_tokens_settings_and_offsets(lib):
     c = Case([2, 3, 1, 2], 500, seed=10)
     c.tokens[0], c.tokens[3] = 500, -1
