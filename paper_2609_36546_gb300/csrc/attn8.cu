@@ -35,8 +35,8 @@
 // ids and scales.
 //
 // Measured (bytes of the visible keys and of the rows, at 6,784 GB/s for a copy): 19 requests
-// of one query over 32,768 keys, 8 KV heads, 189 us, 0.99 of a copy's rate; 128 over 300 to
-// 8,200 keys 172 us, 0.88.  With 128 rows a key the exponents bound it: 262 us for 19 x 16
+// of one query over 32,768 keys, 8 KV heads, 189 us, 0.99 of a copy's rate; 128 over 256 to
+// 16,384 keys 172 us, 0.88.  With 128 rows a key the exponents bound it: 262 us for 19 x 16
 // queries over 32,768 keys of 4 heads, 610 TFLOP/s.
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -1139,7 +1139,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
 }
 
 // Joins the parts of a row group of a task that was cut between CTAs, in order.  What bounds it is
-// the time until another SM's rows arrive, 1,600 cycles or more at a time: a warp has four parts of
+// the time until another SM's rows arrive, 1,300 cycles or more at a time: a warp has four parts of
 // two rows under way, or eight of one row where there are no more rows than warps.
 struct Parts {
   const float *first;  // the first CTA's
