@@ -16,8 +16,9 @@
 // group's rows are on their way to L2 while the request and the page are looked up.
 //
 // What bounds it: the launch and four dependent loads for a step's rows (128 requests of one
-// row, 8 heads: 4.8 us; 64 spans of 1 to 16 rows, 4 heads: 6.2 us); HBM for prompts (12 of 200
-// to 2,000 rows, 4 heads: 15.0 us, 0.44 of a copy's rate, 16.4 without the prefetch).
+// row, 8 heads: 4.8 us; 64 spans of 1 to 16 rows, 4 heads: 5.5 us); for prompts two waves of such
+// chains (12 of 200 to 2,000 rows, 4 heads: 13.1 us, 0.50 of a copy's rate; 24 warps an SM at 80
+// registers, 14.7 us at 111 and 16 warps, 14.3 at 64 with spills).
 #include <cuda_runtime.h>
 #include <stdint.h>
 #include <string.h>
@@ -136,9 +137,16 @@ IPD_DEVINL uint2 quantise(const uint4 &v, float s) {
   return make_uint2(four(x, s), four(x + 4, s));
 }
 
+// ... with NaN for infinities (the conversion would take them for 448)
+IPD_DEVINL uint4 without_infinities(uint4 v) {
+  uint32_t *w = &v.x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] |= __vcmpeq2(w[e], 0x7f807f80u) | __vcmpeq2(w[e], 0xff80ff80u);
+  return v;
+}
 IPD_DEVINL void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
-__global__ void __launch_bounds__(kThreads) kv8_append_kernel(
+__global__ void __launch_bounds__(kThreads, 6) kv8_append_kernel(
     const __grid_constant__ AppendParams P) {
   const int lane = threadIdx.x & 31;
   const long long warps = (long long)gridDim.x * (kThreads / 32);
@@ -185,16 +193,12 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(
 #pragma unroll
       for (int i = 0; i < 8; ++i) m = max_abs2(m, v[i]);
       m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
-      if (m >= 0x7f80u) {  // not all of the run's rows are finite
+      const bool finite = m < 0x7f80u;  // (all of the run's rows)
+      if (!finite) {
         m = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          uint32_t *w = &v[i].x;
-          m = max(m, finite_max(v[i]));
-          // infinities become NaN (the conversion would take them for 448)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] |= __vcmpeq2(w[e] & 0x7fff7fffu, 0x7f807f80u);
-        }
+#pragma unroll 1
+        for (int i = half; i < n; i += 2)  // (read again: what is kept for this are registers of every call's)
+          m = max(m, finite_max(*reinterpret_cast<const uint4 *>(x + (i - half) * stride)));
         m = __reduce_max_sync(0xffffffffu, m);
       }
       const int b = max(byte_of(m), was);
@@ -210,9 +214,15 @@ __global__ void __launch_bounds__(kThreads) kv8_append_kernel(
       }
       const float f = b == 255 ? __uint_as_float(0x7fc00000u) : pow2i(127 - b);
       dst += s0 * 16;
+      if (finite) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (2 * i + half < n) dst[i * 32] = quantise(v[i], f);
+        for (int i = 0; i < 8; ++i)
+          if (2 * i + half < n) dst[i * 32] = quantise(v[i], f);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (2 * i + half < n) dst[i * 32] = quantise(without_infinities(v[i]), f);
+      }
       __syncwarp();  // every lane has read the page's present scale
       if (lane == 0) *scale = (uint8_t)b;
     }
@@ -257,9 +267,10 @@ extern "C" int ipd_kv8_append(const ipd_kv8_append_desc *appends, int n, ipd_str
     if (a.total_new == 0) continue;  // nothing to write: not part of the launch
     AppendDev &A = P.a[P.n];
     A.d = a;
-    // A warp a new row where they are few or most of a page each, and 16 rows a warp for many (64 spans of
-    // 1 to 16 rows: 6.2 us at 1, 10.3 at 16; 13,000 rows of prompts: 44 us at 1, 17.1 at 8, 15.0 at 16).
-    A.group = a.total_new >= 4LL * a.num_reqs && a.total_new > 2048 ? 16 : 1;
+    // Rows a warp looks at: 1 where most start a run, 4 for spans, 16 for many (128 single rows: 4.8 us at 1,
+    // 5.6 at 2; 64 spans of 1 to 16: 6.2 at 1, 5.5 at 2 and 4, 6.2 at 8, 10.3 at 16; 13,000 rows of
+    // prompts: 44 at 1, 17.1 at 8, 13.1 at 16).
+    A.group = a.total_new >= 4LL * a.num_reqs && a.total_new > 2048 ? 16 : a.total_new > 2LL * a.num_reqs ? 4 : 1;
     A.groups = (a.total_new + A.group - 1) / A.group;
     total += (long long)A.groups * 2 * a.cache.num_kv_heads;
     P.end[P.n++] = total;
