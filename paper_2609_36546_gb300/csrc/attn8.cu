@@ -130,6 +130,7 @@ struct Item {
   int r, n_pages;       // request of the batch, its pages
   int part;             // partial slot (-1: the whole task is here)
   int cta0, ctab, cta1; // the CTAs of the task: cta0, then ctab .. cta1
+  int bad;              // a key with NaN in V was hidden from some of its rows (see mend)
 };
 
 // A tile on its way through the loading and issuing warps.
@@ -166,9 +167,8 @@ struct Shared {
   alignas(16) float alpha[kGroups][kRows];
   alignas(16) float red[kGroups][4][kRows];
   uint32_t over[kGroups][4];                           // rows whose references have to move
-  // first key of a span with a NaN in this dim of V, and whether there is one (by an
-  // item's first warpgroup)
-  int nan_key[kGroups][kD], bad[kGroups];
+  // first key of a span with a NaN in this dim of V (by an item's first warpgroup)
+  int nan_key[kGroups][kD];
   int last[kGroups], abort;
   uint32_t tmem;
   Tile tile[kTiles];
@@ -455,7 +455,7 @@ __device__ void item_warp(const Params &P, Shared &S, int lane) {
           Item &I = S.item[slot];
           I.valid = 1, I.b = b, I.c0 = info.z, I.n = info.y, I.L = L, I.h = h;
           I.row0 = row0, I.rows = rows, I.nr = rows > 16 ? 32 : 16, I.ng = ng;
-          I.t0 = t0, I.t1 = t1;
+          I.t0 = t0, I.t1 = t1, I.bad = 0;
           I.masked = L - info.y + 1 + row0 / group;
           I.r = g - P.req_base[b], I.n_pages = (L + kPage - 1) / kPage;
           I.part = t1 - t0 == tiles ? -1 : t0 > 0 ? 2 * (int)blockIdx.x : 2 * (int)blockIdx.x + 1;
@@ -872,7 +872,7 @@ struct Softmax {
 // A thread's key of a tile that holds hidden keys: NaN in its V row.  They would reach
 // rows that do not see the key (0 x NaN), so they become 0, and rows that do see
 // it get them back at the end.
-IPD_DEVINL void mend(Shared &S, int set, uint8_t *v, int key_in_tile, int key, int L) {
+IPD_DEVINL void mend(Shared &S, Item &I, int set, uint8_t *v, int key_in_tile, int key) {
   const uint4 *row = reinterpret_cast<const uint4 *>(v + key_in_tile * kD);
   uint32_t any = 0;  // bit 7 of a byte: one of its like was 0x7f or 0xff
 #pragma unroll
@@ -891,9 +891,9 @@ IPD_DEVINL void mend(Shared &S, int set, uint8_t *v, int key_in_tile, int key, i
 #pragma unroll 1
     for (int e = 0; e < 4; ++e)
       if ((x >> 8 * e & 0x7fu) == 0x7fu) {
-        if (key < L) {
+        if (key < I.L) {
           atomicMin(&S.nan_key[set][((c ^ (key_in_tile & 7)) << 4) + (i & 3) * 4 + e], key);
-          S.bad[set] = 1;
+          I.bad = 1;
         }
         x &= ~(0xffu << 8 * e);
       }
@@ -1007,7 +1007,7 @@ IPD_DEVINL void move_references(Shared &S, const Softmax &X, u64 (&y)[NR / 2], f
 // does not leave the way the others go: the warps of a warpgroup meet at barriers.
 // Returns the exponent that V's scales count from.
 template <int NR>
-__device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item &I) {
+__device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
   const int g = X.g, lane = X.lane, tid = X.tid;
   const int n_tiles = I.t1 - I.t0, L = I.L;
   const uint32_t lanes = (uint32_t)X.warp << 21;  // this warp's 32 TMEM lanes
@@ -1126,7 +1126,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, const Item 
       // warpgroup's rows before the others'
       X.ok = wait(&S.v_ready[g], full(X.mends, 1), &S.abort, 0) && X.ok;
       ++X.mends;
-      if (key >= masked) mend(S, g, S.v[v_stage], tid, key, L);
+      if (key >= masked) mend(S, I, g, S.v[v_stage], tid, key);
     }
     fence_proxy_async_smem();
     tc_wait_st();
@@ -1214,7 +1214,7 @@ IPD_DEVINL void join(const Params &P, const Item &I, int r0, int rows, int warp,
 }
 
 // A row group of an item: its tiles, then its rows.
-__device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t item, const Item &I) {
+__device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t item, Item &I) {
   const int g = X.g, lane = X.lane, tid = X.tid, slot = item % kSlots;
   const int nr = I.nr, rg = g - I.wg;
   convert_queries(P.b[I.b], I, S, g, X.warp, lane);
@@ -1250,7 +1250,7 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
   X.ok = wait(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort, 0) && X.ok;
   tc_fence_after();
   named_bar_sync(1 + g, 128);
-  const bool bad = *(volatile int *)&S.bad[I.wg] != 0;
+  const bool bad = *(volatile int *)&I.bad != 0;
   const int d = tid, row0 = I.row0 + rg * kRows, group = P.b[I.b].group;
   {
     const BatchDev &B = P.b[I.b];
@@ -1301,10 +1301,7 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
         X.ok = wait(bar, uses & 1u, &S.abort, 0) && X.ok;
         ++uses;
       }
-      if (i == 0 && rg == 0) {
-        S.nan_key[g][tid] = 0x7fffffff;
-        if (tid == 0) S.bad[g] = 0;
-      }
+      if (i == 0 && rg == 0) S.nan_key[g][tid] = 0x7fffffff;
     }
   }
   // state, sums and factors are read, before the next item writes them
@@ -1317,7 +1314,7 @@ __device__ void softmax_warps(const Params &P, Shared &S, int warp, int lane) {
     const int slot = n % kSlots;
     X.ok = wait(&S.item_taken[slot], full(n, kSlots), &S.abort, 0) && X.ok;
     if (bar_or(1 + X.g, 128, !X.ok)) return;  // the whole warpgroup
-    const Item &I = S.item[slot];
+    Item &I = S.item[slot];
     if (!I.valid) return;
     if (X.g >= I.wg && X.g < I.wg + I.ng) softmax_item(P, S, X, n, I);
     arrive_warp(&S.item_empty[slot], lane);
@@ -1330,7 +1327,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn8_kernel(const __grid_constan
   Shared &S = *reinterpret_cast<Shared *>(raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x < kGroups * kD) S.nan_key[threadIdx.x / kD][threadIdx.x % kD] = 0x7fffffff;
-  if (threadIdx.x < kGroups) S.bad[threadIdx.x] = 0;
   if (threadIdx.x == 0) {
     S.abort = 0;
     auto ring = [](uint64_t *b, int n, int count) {

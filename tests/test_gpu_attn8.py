@@ -267,6 +267,27 @@ def test_hidden_bytes_reach_nothing(lib):
     _check(c)
 
 
+def test_hidden_nan_in_tasks_side_by_side(lib):
+    """NaN in V of spans' own keys, in some of many short requests of every width: tasks of one, two
+    and four warpgroups note them while others end."""
+    g = torch.Generator().manual_seed(2)
+    n = 150
+    q_len = torch.randint(1, 17, (n,), generator=g).tolist()
+    length = [q + int(x) for q, x in zip(q_len, torch.randint(0, 300, (n,), generator=g))]
+    c = Case(32, 4, q_len, length, seed=12)
+    for r in torch.randperm(n, generator=g)[:90].tolist():
+        pos = length[r] - 1 - int(torch.randint(0, q_len[r], (1,), generator=g))
+        page, head, dim = int(c.table[r, pos // 16]), int(torch.randint(0, 4, (1,), generator=g)), int(torch.randint(0, 128, (1,), generator=g))
+        c.vp.view(torch.uint8)[page, head, pos % 16, dim] = 0x7f
+    _run(lib, c)
+    _check(c)
+    first = c.out.nan_to_num(nan=77.0).clone()
+    for _ in range(20):
+        _run(lib, c)
+        assert torch.equal(c.out.nan_to_num(nan=77.0), first)
+    assert lib.device_error() == 0
+
+
 def test_rows_do_not_reach_each_other(lib):
     """A NaN and an infinite query, and one 2^40 times as large, beside ordinary ones."""
     c = Case(32, 4, [3, 1], [300, 900], seed=8)
