@@ -532,13 +532,13 @@ struct Residual {
 
 __global__ void __launch_bounds__(kThreads, 2) draft_verdict_kernel(const __grid_constant__ Params P) {
   __shared__ Verdict S;
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // what the row pass wrote
   const ipd_draft_args &a = P.a;
   const uint32_t csize = cluster_size(), rank = cluster_rank();
   const int r = blockIdx.x / csize, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c0 = a.cu_draft[r], c1 = a.cu_draft[r + 1];
   const float cp = scale_of(a.inv_temp_target, r), cq = scale_of(a.inv_temp_draft, r);
   const bool spans = c0 >= 0 && c1 >= c0 && c1 <= a.total;
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // what the row pass wrote
   if (!spans || !valid(cp) || !valid(cq)) {
     if (rank == 0 && threadIdx.x == 0) {
       ipd_set_error(&g_draft_err, spans ? IPD_DEVERR_SETTING : IPD_DEVERR_SPAN);
