@@ -70,10 +70,13 @@ constexpr int kBlockRows = 128;           // rows of a task
 constexpr int kGroups = 4;                // softmax warpgroups
 constexpr int kRows = 32;                 // ... and the rows of one
 constexpr int kKStages = 4, kVStages = 5;
-constexpr int kTiles = 16;                // tiles handed out whose product is not complete
+// Tiles handed out whose product is not complete, and items.  (128 requests of 256 to 16,384 keys /
+// 1,000 of 300, us: 195 / 249 with 8 tiles, 172 / 271 with 11, 173 / 294 with 16, 174 / 315 with 32;
+// with 11 and 16 items in place of 8 170 / 255, with 4 175 / 330.)
+constexpr int kTiles = 11;
 constexpr int kScales = 16;               // of a warpgroup's tiles, scales handed out that it has not read
 constexpr int kBatch = 4;                 // ... fetched at once
-constexpr int kSlots = 8;                 // items handed out
+constexpr int kSlots = 16;
 constexpr int kSoftmaxWarps = 4 * kGroups;
 constexpr int kLoadWarp = kSoftmaxWarps, kQkWarp = kLoadWarp + 1, kPvWarp = kLoadWarp + 2, kItemWarp = kLoadWarp + 3;
 // (the fifth orders tiles; with two for loads and two that converted queries ahead of their turn
@@ -139,17 +142,18 @@ struct Tile {
   alignas(16) int y[kPages];  // first pool rows of its pages
   uint32_t what;  // the rest in one word, which one warp-wide move makes uniform:
   // its item's first, last; it holds hidden keys; there is none after the one before (4 bits);
-  // warpgroups (3), the first of them (2), 32 rows each or 16 (1), the item's place in this CTA's order (4: slot and turn), batch (3)
+  // warpgroups (3), the first of them (2), 32 rows each or 16 (1), the item's place
+  // in this CTA's order (5: slot and turn), batch (3)
 };
-static_assert(2 * kSlots == 16 && kGroups == 4 && IPD_MAX_BATCHES <= 8, "the fields of Tile::what");
+static_assert(2 * kSlots == 32 && kGroups == 4 && IPD_MAX_BATCHES <= 8, "the fields of Tile::what");
 struct What {
   uint32_t w;
   IPD_DEVINL bool is(int flag) const { return w & flag; }
   IPD_DEVINL int ng() const { return w >> 4 & 7u; }
   IPD_DEVINL int wg() const { return w >> 7 & 3u; }
   IPD_DEVINL int nr() const { return 16u << (w >> 9 & 1u); }
-  IPD_DEVINL uint32_t item() const { return w >> 10 & 15u; }
-  IPD_DEVINL int b() const { return w >> 14 & 7u; }
+  IPD_DEVINL uint32_t item() const { return w >> 10 & 31u; }
+  IPD_DEVINL int b() const { return w >> 15 & 7u; }
 };
 // ... and what a warpgroup has to know of it.
 struct Scales {
@@ -610,7 +614,7 @@ __device__ void page_warp(const Params &P, Shared &S, int lane) {
     if (mine < now) T.y[place] = ok ? (int)cell * kPage : B.rows_end;
     if (leads) {
       T.what = (t == I.t0 ? kFirst : 0) | (last ? kLast : 0) | ((t + 1) * kKeys > I.masked ? kHides : 0) | ng << 4 | g << 7 |
-               (I.nr >> 5) << 9 | (item & 15) << 10 | I.b << 14;
+               (I.nr >> 5) << 9 | (item & 31) << 10 | I.b << 15;
     }
     __syncwarp();
     if (leads) mbar_arrive(&S.tile_full[at % kTiles]);
