@@ -788,27 +788,42 @@ __device__ void pv_warp(Shared &S, int lane) {
 // A row as two e4m3 terms: with 2^e the least power of two that brings its largest
 // entry to 448 or below, hi = e4m3(q 2^-e), lo = e4m3(q 2^-e - hi), which together
 // hold a bf16's eight bits down to 2^-10, 2^-17 of the row's largest entry.
+// Every eighth row of an item from the r-th on: where it begins in q and out.  (By steps, no
+// division a row: with that, all of a warp's rows under way at once and rows that leave 16 bytes a
+// lane, 300 requests of 4 to 7 queries over 100 to 3,000 keys took 142 us in place of 154, 64 tasks a
+// CTA of 128 rows and four tiles 1,092 in place of 1,243.)
+struct RowWalk {
+  int r, head, group, dh;
+  size_t at, by, over;
+  IPD_DEVINL RowWalk(const BatchDev &B, const Item &I, int first) : r(first), group(B.group) {
+    const int row = I.row0 + first, query = row / group, dq = 8 / group;
+    head = row - query * group, dh = 8 - dq * group;
+    at = ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group + head) * kD;
+    by = ((size_t)dq * B.hq + dh) * kD, over = (size_t)(B.hq - group) * kD;
+  }
+  IPD_DEVINL void step() {
+    r += 8, at += by, head += dh;
+    if (head >= group) head -= group, at += over;
+  }
+};
+
 // Half a warp a row, eight entries a lane; the warpgroup's own rows of the item, whose
 // place is free: the products of the item before are complete.
 IPD_DEVINL void convert_queries(const BatchDev &B, const Item &I, Shared &S, int g, int warp, int lane) {
-  const int first = (g - I.wg) * kRows, group = B.group;  // (rows of the item)
-  constexpr int kAhead = 2;  // rows loaded ahead
+  const int first = (g - I.wg) * kRows;  // (of the item's rows)
   const int part = lane & 15;
-  const auto fetch = [&](int r) {
-    if (first + r >= I.rows) return make_uint4(0u, 0u, 0u, 0u);
-    const int row = I.row0 + first + r, query = row / group;
-    return *reinterpret_cast<const uint4 *>(
-        B.q + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group + (row - query * group)) * kD + part * 8);
-  };
-  uint4 next[kAhead];
-  int r = 2 * warp + (lane >> 4);
+  RowWalk walk(B, I, first + 2 * warp + (lane >> 4));
+  uint4 next[kRows / 8];
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) next[i] = fetch(r + i * 8);
+  for (int i = 0; i < kRows / 8; ++i) {
+    next[i] = walk.r < I.rows ? *reinterpret_cast<const uint4 *>(B.q + walk.at + part * 8) : make_uint4(0u, 0u, 0u, 0u);
+    walk.step();
+  }
 #pragma unroll 1
-  for (; r < I.nr; r += 8) {
+  for (int r = 2 * warp + (lane >> 4); r < I.nr; r += 8) {
     const uint4 x = next[0];
-    next[0] = next[1];
-    next[1] = r + 16 < I.nr ? fetch(r + 16) : x;
+#pragma unroll
+    for (int i = 0; i + 1 < kRows / 8; ++i) next[i] = next[i + 1];
     const uint32_t *xw = &x.x;
     uint32_t top = 0;
 #pragma unroll
@@ -1256,30 +1271,42 @@ __device__ void softmax_item(const Params &P, Shared &S, Softmax &X, uint32_t it
   named_bar_sync(1 + g, 128);
   const bool bad = *(volatile int *)&I.bad != 0;
   const int d = tid, row0 = I.row0 + rg * kRows, group = P.b[I.b].group;
-  {
-    const BatchDev &B = P.b[I.b];
-    int query = row0 / group, head = row0 - query * group;
-    uint16_t *at = B.out + ((size_t)(I.c0 + query) * B.hq + (size_t)I.h * group + head) * kD + d;
-    float *to = part + (size_t)(rg * kRows) * kD + d;
-    const size_t turn_over = (size_t)(B.hq - group) * kD;
-    const int nan_key = bad ? S.nan_key[I.wg][d] : 0x7fffffff, sees = I.L - I.n;
+  const BatchDev &B = P.b[I.b];
+  // a thread a dim: fp32 rows of a part as they are, a task's own by way of P's buffer, in
+  // bf16, so that they leave 16 bytes a lane
+  float *to = part + (size_t)(rg * kRows) * kD + d;
+  uint16_t *stage = reinterpret_cast<uint16_t *>(S.p[g]);
+  static_assert(sizeof(S.p[0]) >= kRows * kD * sizeof(uint16_t), "a warpgroup's rows in P's buffer");
 #pragma unroll 1
-    for (int k = 0; k < rows; k += 8) {
-      uint32_t a[8], b[8];
-      tc_ld_32x32b_x8(o_addr + k, a);
-      tc_ld_32x32b_x8(o_addr + nr + k, b);
-      tc_wait_ld();
+  for (int k = 0; k < rows; k += 8) {
+    uint32_t a[8], b[8];
+    tc_ld_32x32b_x8(o_addr + k, a);
+    tc_ld_32x32b_x8(o_addr + nr + k, b);
+    tc_wait_ld();
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float x = fmaf(__uint_as_float(b[i]), 1.f / kLoScale, __uint_as_float(a[i])) * S.alpha[g][k + i];
-        if (nan_key <= sees + query) x = __uint_as_float(0x7fc00000u);
-        if (k + i < rows) {
-          if (part) *to = x;
-          else *at = f2bf16(x);
-        }
-        to += kD, at += kD;
-        if (++head == group) head = 0, ++query, at += turn_over;
+    for (int i = 0; i < 8; ++i) {
+      const float x = fmaf(__uint_as_float(b[i]), 1.f / kLoScale, __uint_as_float(a[i])) * S.alpha[g][k + i];
+      if (!part) stage[(k + i) * kD + d] = f2bf16(x);
+      else if (k + i < rows) to[(size_t)(k + i) * kD] = x;
+    }
+  }
+  if (bad) {
+    const int nan_key = S.nan_key[I.wg][d], sees = I.L - I.n;
+#pragma unroll 1
+    for (int r = 0; r < rows; ++r)
+      if (nan_key <= sees + (row0 + r) / group) {
+        if (part) to[(size_t)r * kD] = __uint_as_float(0x7fc00000u);
+        else stage[r * kD + d] = 0x7fc0;
       }
+  }
+  if (!part) {
+    named_bar_sync(1 + g, 128);
+    const int r0 = 2 * X.warp + (lane >> 4);
+    const uint16_t *from = stage + r0 * kD + (lane & 15) * 8;
+#pragma unroll 1
+    for (RowWalk walk(B, I, rg * kRows + r0); walk.r < I.rows; walk.step(), from += 8 * kD) {
+      if (walk.r >= (rg + 1) * kRows) break;
+      *reinterpret_cast<uint4 *>(B.out + walk.at + (lane & 15) * 8) = *reinterpret_cast<const uint4 *>(from);
     }
   }
   tc_fence_before();
