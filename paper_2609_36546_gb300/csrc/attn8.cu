@@ -37,7 +37,7 @@
 // Measured (bytes of the visible keys and of the rows, at 6,784 GB/s for a copy): 19 requests
 // of one query over 32,768 keys, 8 KV heads, 189 us, 0.99 of a copy's rate; 128 over 256 to
 // 16,384 keys 172 us, 0.88.  With 128 rows a key the exponents bound it: 262 us for 19 x 16
-// queries over 32,768 keys of 4 heads, 610 TFLOP/s.
+// queries over 32,768 keys of 4 heads, 624 TFLOP/s.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cudaTypedefs.h>
