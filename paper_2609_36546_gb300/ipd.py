@@ -713,25 +713,32 @@ class KVCache8:
         return self.k_pages.shape[1]
 
 
+def _pack_append8(cache: "KVCache8", k_new, v_new, cu_new, seq_len, page_table) -> bytes:
+    f, shape, tshape, R = cache._fields, k_new.shape, page_table.shape, cu_new.shape
+    bf, i32 = _BF16, _I32
+    if len(shape) != 3 or v_new.shape != shape or k_new.dtype is not bf or v_new.dtype is not bf or \
+            shape[1] != f[6] or shape[2] != f[7]:
+        _refuse("ipd_kv8_append: k_new or v_new")
+    if len(R) != 1 or R[0] < 1 or cu_new.dtype is not i32 or seq_len.dtype is not i32 or \
+            page_table.dtype is not i32 or len(tshape) != 2 or seq_len.numel() < R[0] - 1 or \
+            tshape[0] < R[0] - 1 or not cu_new.is_contiguous() or not seq_len.is_contiguous() or \
+            not page_table.is_contiguous():
+        _refuse("ipd_kv8_append: offsets, lengths or page table")
+    n, hkv, _ = shape
+    (ks, kh, kd), (vs, vh, vd) = k_new.stride(), v_new.stride()
+    if kd != 1 or vd != 1 or (hkv > 1 and (kh != 128 or vh != 128)):
+        _refuse("ipd_kv8_append: rows")
+    if n <= 1:
+        ks = vs = hkv * 128
+    return _PACK_KV8_APPEND.pack(*f, k_new.data_ptr(), v_new.data_ptr(), ks, vs, cu_new.data_ptr(),
+                                 seq_len.data_ptr(), page_table.data_ptr(), tshape[1], R[0] - 1, n)
+
+
 def kv8_append_many(appends, stream=None):
     """Several appends to 8-bit caches in one launch: ``appends`` is a sequence
     of (cache, k_new, v_new, cu_new, seq_len, page_table) tuples, each as in
     kv8_append."""
-    packed = b""
-    for cache, k_new, v_new, cu_new, seq_len, page_table in appends:
-        shape, R, tshape = tuple(k_new.shape), cu_new.numel() - 1, page_table.shape
-        f = cache._fields
-        if shape != (shape[0], f[6], f[7]):
-            _refuse("ipd_kv8_append: k_new")
-        if cu_new.dtype is not _I32 or seq_len.dtype is not _I32 or page_table.dtype is not _I32 or \
-                cu_new.dim() != 1 or R < 0 or seq_len.numel() < R or len(tshape) != 2 or \
-                tshape[0] < R or not cu_new.is_contiguous() or not seq_len.is_contiguous() or \
-                not page_table.is_contiguous():
-            _refuse("ipd_kv8_append: offsets, lengths or page table")
-        packed += _PACK_KV8_APPEND.pack(
-            *f, k_new.data_ptr(), v_new.data_ptr(), _rows(k_new, shape, _BF16, "ipd_kv8_append: k_new"),
-            _rows(v_new, shape, _BF16, "ipd_kv8_append: v_new"), cu_new.data_ptr(),
-            seq_len.data_ptr(), page_table.data_ptr(), tshape[1], R, shape[0])
+    packed = b"".join(_pack_append8(*a) for a in appends)
     _check(_lib.ipd_kv8_append(packed, len(appends), _stream(stream)), "ipd_kv8_append")
 
 
@@ -740,7 +747,8 @@ def kv8_append(cache: KVCache8, k_new, v_new, cu_new, seq_len, page_table, strea
     row stride) into the 8-bit cache's pages at the last positions of each
     request's sequence (``seq_len`` is the length after the append), and brings
     the pages' scales up to date."""
-    kv8_append_many(((cache, k_new, v_new, cu_new, seq_len, page_table),), stream)
+    _check(_lib.ipd_kv8_append(_pack_append8(cache, k_new, v_new, cu_new, seq_len, page_table), 1,
+                               _stream(stream)), "ipd_kv8_append")
 
 
 class AttnBatch8:
