@@ -64,6 +64,7 @@ struct Params {
   Row *rows;     // [2 total]: target and draft row of every position
   int piece;     // 8-entry vectors a CTA takes of a row (verdicts: a multiple of 32)
   int pieces;    // CTAs of a row in the row pass
+  float one;     // 1: see pow2_weight2
 };
 
 IPD_DEVINL uint32_t max2(uint32_t a, uint32_t b) {  // of two bf16 each; NaN loses
@@ -105,10 +106,10 @@ struct RowView {
 // kNone, the row has no entry.
 enum { kNear, kCoarse, kInf, kNone };
 struct Weigher {
-  float top, c;
+  float top, c, one;
   uint32_t least2;
   int mode;
-  IPD_DEVINL Weigher(float t, float cc) : top(t), c(cc), least2(0xff80ff80u), mode(kCoarse) {
+  IPD_DEVINL Weigher(float t, float cc, float o) : top(t), c(cc), one(o), least2(0xff80ff80u), mode(kCoarse) {
     if (t == INFINITY) mode = kInf;
     else if (t == -INFINITY) mode = kNone;
     else {
@@ -134,7 +135,7 @@ struct Weigher {
       f2_unpack(y, a, b);
       y = f2_pack(fmaxf(a, -64.f), fmaxf(b, -64.f));  // (fmaxf drops a NaN)
     }
-    pow2_weight2(y, w0, w1);
+    pow2_weight2<true>(y, w0, w1, f2_pack(one, one));
   }
   IPD_DEVINL void any_two(uint32_t w, uint32_t &w0, uint32_t &w1) const {
     if (mode == kNear) two<kNear>(w, w0, w1);
@@ -378,7 +379,7 @@ __global__ void __launch_bounds__(kHist ? kHistThreads : kPlainThreads, kHist ? 
     top = warp_max(top);
     cluster_arrive();  // (waited for at the end: no CTA leaves while its maximum is read)
   }
-  const Weigher W(top, draft ? S.cq : S.cp);
+  const Weigher W(top, draft ? S.cq : S.cp, P.one);
   u64 z = 0;
   if (kHist && W.mode != kNone && top < 4096.f && W.x(-4096.f) < -32.f && S.listed <= (uint32_t)kList) {
     const uint32_t *hist = reinterpret_cast<const uint32_t *>(hist4);
@@ -602,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, 2) draft_verdict_kernel(const __grid
     }
   }
   __syncthreads();
-  Residual D{vp, vq, Weigher(top, cp), Weigher(top_q, cq), full ? 0ull : S.m, full ? 0 : S.s, vq.before - vp.before};
+  Residual D{vp, vq, Weigher(top, cp, P.one), Weigher(top_q, cq, P.one), full ? 0ull : S.m, full ? 0 : S.s, vq.before - vp.before};
   // Sums of the tiles.  A second time with the target's weights alone where
   // nothing is left of them.
   const int tiles = (to - from + 31) / 32;
@@ -767,6 +768,7 @@ extern "C" int ipd_verify_draft(const ipd_draft_args *args, void *workspace,
   memset(&P, 0, sizeof(P));
   P.a = a;
   P.rows = static_cast<Row *>(workspace);
+  P.one = 1.f;
   const int vecs = (a.vocab + 14) / 8;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   g_draft_used.store(true, std::memory_order_relaxed);

@@ -91,6 +91,39 @@ def test_many_requests_of_both_kinds(lib):
     assert 0.2 < share < 0.95
 
 
+@pytest.mark.parametrize("R,V", [(1500, 2), (160, 300), (200, 9001)])
+def test_verdicts_at_their_border(lib, R, V):
+    """For every request the largest uniform number that accepts its draft, and the next one,
+    which rejects it: a weight (below 2^24 for most) that is off by one would move the border."""
+    c = Case([1] * R, V, seed=R, noise=0.6, bonus=False)
+    g = torch.Generator().manual_seed(V)
+    if V == 2:
+        c.target, c.draft = torch.zeros(R, 2, dtype=torch.bfloat16), torch.zeros(R, 2, dtype=torch.bfloat16)
+        c.target[:, 1] = (-3 - 12 * torch.rand(R, generator=g)).to(torch.bfloat16)
+        c.draft[:, 1] = (c.target[:, 1].float() + 0.7 * torch.rand(R, generator=g)).to(torch.bfloat16)
+        c.tokens[:] = 1
+    f = lambda t: t.float().numpy()
+    below, above, used = [], [], []
+    for r in range(R):
+        (_, wp), (_, wq) = ref.weights(f(c.target[r]), c.inv_p[r].numpy()), ref.weights(f(c.draft[r]), c.inv_q[r].numpy())
+        tok, zp, zq = int(c.tokens[r]), int(wp.sum()), int(wq.sum())
+        ok = lambda u: float(u) * float(wq[tok]) * float(zp) < float(wp[tok]) * float(zq)
+        u = np.float32(min(1.0, float(wp[tok]) * zq / max(1.0, float(wq[tok]) * zp)))
+        up, down = np.float32(2), np.float32(0)
+        for _ in range(4):
+            u = np.nextafter(u, up)
+        while u > 0 and not ok(u):
+            u = np.nextafter(u, down)
+        if 0 < u < 1 - 2.0 ** -20:
+            below.append(float(u)), above.append(float(np.nextafter(u, up))), used.append(r)
+    assert len(used) > R // 8
+    for us, want in ((below, 1), (above, 0)):
+        c.u[:] = 0.0
+        c.u[used] = torch.tensor(us)
+        c.run(lib)
+        assert c.n[used].tolist() == [want] * len(used), (want, int((c.n[used] != want).sum()), len(used))
+
+
 def test_equal_models_accept_everything(lib):
     c = Case([5, 3], 3001, seed=5, noise=0.0, temps=False)
     c.u[:] = torch.nextafter(torch.tensor(1.0), torch.tensor(0.0))
