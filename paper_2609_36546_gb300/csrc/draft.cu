@@ -14,8 +14,8 @@
 // entries, then the tile, then the entry that holds the drawn position.
 //
 // What bounds it: a small call the two kernels' chains of dependent steps (one request, 4 drafts
-// over 151,936 entries: 17.7 us, 6 and 12); a large one the atomics of the row pass (64
-// requests of 1 to 16 over 151,936: 118 us, 2.8 TB/s, of which the row pass 91).
+// over 151,936 entries: 18.5 us, 6 and 12); a large one the atomics of the row pass (64
+// requests of 1 to 16 over 151,936: 121 us, 2.7 TB/s, of which the row pass 92).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
