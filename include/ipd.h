@@ -759,8 +759,11 @@ int ipd_verify_attn8(const ipd_attn8_batch *verify, int n_verify, const ipd_attn
  * A request whose temperature is not valid (log2 e * inv_temp not positive and
  * finite) records IPD_DEVERR_SETTING and gets n_accept 0 and next_token -1, its
  * logp NaN; one whose offsets are out of order or past total (IPD_DEVERR_SPAN)
- * the same, with nothing of its drafts written.  Positions that no request's
- * offsets cover are left as they are.  vocab is at most IPD_TRUNC_MAX_VOCAB. */
+ * the same, with nothing of its drafts written, and so does one with a position
+ * that another request's offsets hold too, unless it is the one that the position
+ * counts for (only offsets out of order give a position to two; the other requests
+ * of such a call get their results).  Positions that no request's offsets cover
+ * are left as they are.  vocab is at most IPD_TRUNC_MAX_VOCAB. */
 typedef struct ipd_draft_args {
   const uint16_t *logits_target, *logits_draft, *logits_bonus;
   int64_t target_stride, draft_stride, bonus_stride;

@@ -18,6 +18,7 @@
 // requests of 1 to 16 over 151,936: 121 us, 2.7 TB/s, of which the row pass 92).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <limits.h>
 #include <math.h>
 #include <stdint.h>
 #include <string.h>
@@ -49,7 +50,7 @@ struct Row {
   float top;           // largest logit (-inf: the row has no entry)
   uint32_t w;          // the drafted token's weight
   float x;             // ... and x (-inf: the row's entry there is none)
-  uint32_t pad;
+  int owner;           // the request that it was weighed for
   IPD_DEVINL u64 sum(int pieces) const {
     u64 s = 0;
 #pragma unroll
@@ -205,23 +206,20 @@ IPD_DEVINL float piece_max(const RowView &R, int from, int to) {
   return fmaxf(bf16lo(m), bf16hi(m));
 }
 
-// The request whose drafts hold position t, or -1.
+// Whether request r's drafts hold position t.
+IPD_DEVINL bool holds(const ipd_draft_args &a, int r, int t) {
+  const int c0 = a.cu_draft[r], c1 = a.cu_draft[r + 1];
+  return c0 >= 0 && c0 <= t && t < c1 && c1 <= a.total;
+}
+// The request whose drafts hold position t where the offsets are in order, or -1: none, or they are not.
 IPD_DEVINL int request_of(const ipd_draft_args &a, int t) {
-  if (t < a.cu_draft[0] || t >= a.cu_draft[a.num_reqs]) return -1;
   int lo = 0, hi = a.num_reqs - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (a.cu_draft[mid] <= t) lo = mid;
     else hi = mid - 1;
   }
-  auto holds = [&](int r) {
-    const int c0 = a.cu_draft[r], c1 = a.cu_draft[r + 1];
-    return c0 >= 0 && c0 <= t && t < c1 && c1 <= a.total;
-  };
-  if (holds(lo)) return lo;
-  for (int r = 0; r < a.num_reqs; ++r)  // offsets out of order
-    if (holds(r)) return r;
-  return -1;
+  return holds(a, lo, t) ? lo : -1;
 }
 
 // ---- rows ------------------------------------------------------------------
@@ -265,7 +263,7 @@ struct RowShared {
   u64 red[kT / 32];
   float fred[kT / 32], top;
   float cp, cq;           // the request's scales
-  int r;                  // ... and itself (-1: the position is none's)
+  int r;                  // ... and itself (-1: not found, INT_MAX: the position is none's)
   uint32_t zeros, listed;
   uint16_t list[kList];
 };
@@ -372,6 +370,18 @@ __global__ void __launch_bounds__(kHist ? kHistThreads : kPlainThreads, kHist ? 
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kT / 32; ++i) top = fmaxf(top, S.fred[i]);
+  if (S.r < 0) {
+    // A position behind the last request, or offsets out of order, among which it may be
+    // anyone's: all are looked through, and the first that holds it has it.
+    __syncthreads();
+    if (tid == 0) S.r = INT_MAX;
+    __syncthreads();
+    for (int r = tid; r < a.num_reqs; r += kT)
+      if (holds(a, r, t)) atomicMin(&S.r, r);
+    __syncthreads();
+    if (tid == 0 && S.r != INT_MAX) S.cp = scale_of(a.inv_temp_target, S.r), S.cq = scale_of(a.inv_temp_draft, S.r);
+    __syncthreads();
+  }
   if (csize > 1) {
     if (tid == 0) S.top = top;
     cluster_sync();
@@ -407,7 +417,7 @@ __global__ void __launch_bounds__(kHist ? kHistThreads : kPlainThreads, kHist ? 
   z = warp_sum64(z);
   if (lane == 0) S.red[tid >> 5] = z;
   __syncthreads();
-  if (tid == 0 && S.r >= 0) {
+  if (tid == 0 && S.r != INT_MAX) {
     z = 0;
     for (int i = 0; i < kT / 32; ++i) z += S.red[i];
     Row &O = P.rows[row];
@@ -416,7 +426,7 @@ __global__ void __launch_bounds__(kHist ? kHistThreads : kPlainThreads, kHist ? 
       uint32_t w0, w1;
       W.any_two(entry | 0xff800000u, w0, w1);
       const float l = bf16f(entry);
-      O.top = top, O.w = w0, O.x = l != l ? -INFINITY : W.x(l);
+      O.top = top, O.w = w0, O.x = l != l ? -INFINITY : W.x(l), O.owner = S.r;
     }
   }
   if (csize > 1) cluster_wait();
@@ -540,14 +550,18 @@ __global__ void __launch_bounds__(kThreads, 2) draft_verdict_kernel(const __grid
   const float cp = scale_of(a.inv_temp_target, r), cq = scale_of(a.inv_temp_draft, r);
   const bool spans = c0 >= 0 && c1 >= c0 && c1 <= a.total;
   asm volatile("griddepcontrol.wait;" ::: "memory");  // what the row pass wrote
-  if (!spans || !valid(cp) || !valid(cq)) {
+  const auto refuse = [&](unsigned int code) {
     if (rank == 0 && threadIdx.x == 0) {
-      ipd_set_error(&g_draft_err, spans ? IPD_DEVERR_SETTING : IPD_DEVERR_SPAN);
+      ipd_set_error(&g_draft_err, code);
       a.n_accept[r] = 0;
       a.next_token[r] = -1;
     }
+  };
+  if (!spans || !valid(cp) || !valid(cq)) {
+    refuse(spans ? IPD_DEVERR_SETTING : IPD_DEVERR_SPAN);
     if (spans && rank == 0)
       for (int t = c0 + threadIdx.x; t < c1; t += kThreads) {
+        if (P.rows[2 * t].owner != r) continue;
         if (a.logp_target) a.logp_target[t] = __uint_as_float(0x7fc00000u);
         if (a.logp_draft) a.logp_draft[t] = __uint_as_float(0x7fc00000u);
       }
@@ -560,12 +574,14 @@ __global__ void __launch_bounds__(kThreads, 2) draft_verdict_kernel(const __grid
   };
   if (threadIdx.x == 0) S.n = c1 - c0;
   __syncthreads();
-  for (int t = c0 + threadIdx.x; t < c1; t += kThreads)
-    if (!accepted(P, t)) {
-      atomicMin(&S.n, t - c0);
-      break;
-    }
+  // (offsets out of order can give a position to two requests: its rows are weighed for one)
+  for (int t = c0 + threadIdx.x; t < c1; t += kThreads) {
+    const int owner = P.rows[2 * t].owner;
+    const bool ok = accepted(P, t);
+    if (owner != r || !ok) atomicMin(&S.n, owner != r ? -1 : t - c0);
+  }
   __syncthreads();
+  if (S.n < 0) return refuse(IPD_DEVERR_SPAN);
   const int n = S.n;
   const bool full = n == c1 - c0;
   if (rank == 0 && threadIdx.x == 0) a.n_accept[r] = n;

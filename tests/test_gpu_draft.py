@@ -283,3 +283,57 @@ def test_no_requests_and_no_drafts(lib):
     c = Case([0, 0], 123, seed=17).run(lib)
     c.check()
     Case([0, 0], 123, seed=18, bonus=False).run(lib).check()
+
+
+@pytest.mark.parametrize("V", [700, 30011])
+@pytest.mark.parametrize("cu", [[0, 2, 5, 8, 6], [4, 2, 5], [3, 8, 1, 3, 3], [6, 0, 1, 4, 2, 2], [0, 5, 3], [8, 8, 8, 2, 8]])
+def test_offsets_out_of_order_leave_the_others(lib, V, cu):
+    """Requests whose own offsets are in order get the results that each would get alone,
+    wherever the offsets around them lie; 8 positions, and a workspace of old contents."""
+    R = len(cu) - 1
+    whole = Case([1] * 8, V, seed=19, bonus=False)
+    for seed in range(4):
+        c = Case([0] * R, V, seed=20 + seed)
+        for x in ("target", "draft", "tokens", "u"):
+            setattr(c, x, getattr(whole, x))
+        c.u, c.cu, c.k = torch.rand(8, generator=torch.Generator().manual_seed(seed)), torch.tensor(cu).int(), [0] * (R - 1) + [8]
+        c.run(lib)
+        assert lib.device_error() == 6
+        f = lambda t: t.float().numpy()
+        for r in range(R):
+            a, b = cu[r], cu[r + 1]
+            if a > b:
+                assert (int(c.n[r]), int(c.nxt[r])) == (0, -1)
+                continue
+            verdict, logp = ref.verify(f(c.target[a:b]), f(c.draft[a:b]), f(c.bonus[r:r + 1]), c.tokens[a:b].tolist(), [0, b - a],
+                                       c.u[a:b].tolist(), [float(c.u_next[r])], c.inv_p[r:r + 1].numpy(), c.inv_q[r:r + 1].numpy())
+            assert (int(c.n[r]), int(c.nxt[r])) == verdict[0], (cu, r, seed)
+            got = torch.stack([c.lp, c.lq], 1)[a:b].double().cpu().numpy()
+            logp = np.array(logp, dtype=np.float64).reshape(-1, 2)
+            assert np.all(np.abs(got - logp) <= 2.0 ** -21 * np.abs(logp) + 2.0 ** -21)
+
+
+@pytest.mark.parametrize("cu", [[0, 5, 3, 8], [2, 7, 1, 4, 8], [0, 8, 0, 8], [6, 0, 1, 4, 2, 6]])
+def test_requests_that_share_positions(lib, cu):
+    """Two requests of different temperatures with positions in common: each gets its own
+    result or the one of a request whose offsets are at fault, not a mixture."""
+    R, V, refused = len(cu) - 1, 900, 0
+    for seed in range(12):
+        whole = Case([1] * 8, V, seed=30 + seed, bonus=False, noise=1.5)
+        c = Case([0] * R, V, seed=30 + seed)
+        for x in ("target", "draft", "tokens", "u"):
+            setattr(c, x, getattr(whole, x))
+        c.inv_p, c.inv_q = torch.linspace(0.3, 2.5, R), torch.linspace(2.0, 0.4, R)
+        c.cu, c.k = torch.tensor(cu).int(), [0] * (R - 1) + [8]
+        c.run(lib)
+        assert lib.device_error() == 6
+        f = lambda t: t.float().numpy()
+        for r in range(R):
+            a, b = cu[r], cu[r + 1]
+            got = (int(c.n[r]), int(c.nxt[r]))
+            refused += a <= b and got == (0, -1)
+            if a <= b and got != (0, -1):
+                verdict, _ = ref.verify(f(c.target[a:b]), f(c.draft[a:b]), f(c.bonus[r:r + 1]), c.tokens[a:b].tolist(), [0, b - a],
+                                        c.u[a:b].tolist(), [float(c.u_next[r])], c.inv_p[r:r + 1].numpy(), c.inv_q[r:r + 1].numpy())
+                assert got == verdict[0], (cu, r, seed)
+    assert refused >= 12
