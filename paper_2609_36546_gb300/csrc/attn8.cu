@@ -171,6 +171,7 @@ struct Shared {
   alignas(16) float alpha[kGroups][kRows];
   alignas(16) float red[kGroups][4][kRows];
   uint32_t over[kGroups][4];                           // rows whose references have to move
+  uint32_t unseen[kGroups];                            // rows that have not seen a key of their item
   // first key of a span with a NaN in this dim of V (by an item's first warpgroup)
   int nan_key[kGroups][kD];
   int last[kGroups], abort;
@@ -933,6 +934,25 @@ IPD_DEVINL void exponents(const uint32_t (&s)[NR], const float4 *state, float ck
   }
 }
 
+IPD_DEVINL float redux_max(float x) {
+  float m;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(x));
+  return m;
+}
+// The largest exponents of the rows (V's scale among them) over a warp's keys.
+template <int NR>
+IPD_DEVINL void row_maxima(Shared &S, const Softmax &X, const u64 (&y)[NR / 2], float de) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < NR; i += 2) {
+    float z0, z1;
+    f2_unpack(f2_add(y[i / 2], f2_pack(de, de)), z0, z1);
+    z0 = redux_max(z0), z1 = redux_max(z1);
+    m = X.lane == i ? z0 : X.lane == i + 1 ? z1 : m;
+  }
+  if (X.lane < NR) S.red[X.g][X.warp][X.lane] = m;
+}
+
 IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[16]) { tc_ld_32x32b_x16(taddr, r); }
 IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[32]) { tc_ld_32x32b_x32(taddr, r); }
 
@@ -940,21 +960,19 @@ IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[32]) { tc_ld_32x32b_x3
 template <int NR>
 IPD_DEVINL void first_references(Shared &S, const Softmax &X, u64 (&y)[NR / 2], float de, uint32_t l_addr) {
   const int g = X.g, tid = X.tid, lane = X.lane;
-#pragma unroll
-  for (int c = 0; c < NR; c += 16) {
-    float z[16];
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) f2_unpack(f2_add(y[(c + i) / 2], f2_pack(de, de)), z[i], z[i + 1]);
-    const float x = column_reduce(z, lane, [](float a, float b) { return fmaxf(a, b); });
-    if (!(lane & 1)) S.red[g][X.warp][c + (lane >> 1)] = x;
-  }
+  row_maxima<NR>(S, X, y, de);
   named_bar_sync(1 + g, 128);
-  if (tid < NR) {
-    const float now = fmaxf(fmax3(S.red[g][0][tid], S.red[g][1][tid], S.red[g][2][tid]), S.red[g][3][tid]);
-    // (a row that has seen nothing, NaN alone, or more than fp32 holds stays at 0)
-    const float ref = now == -INFINITY || now == INFINITY ? 0.f : now - kBase;
-    (reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1))[2] = -ref;
-    S.alpha[g][tid] = -ref;
+  if (X.warp == 0) {
+    const int r = lane % NR;
+    const float now = fmaxf(fmax3(S.red[g][0][r], S.red[g][1][r], S.red[g][2][r]), S.red[g][3][r]);
+    // (a row with NaN alone, or more than fp32 holds, stays at 0; so does, for now, one that has seen nothing)
+    const float ref = fabsf(now) < INFINITY ? now - kBase : 0.f;
+    const uint32_t unseen = __ballot_sync(0xffffffffu, now == -INFINITY && lane < NR);
+    if (lane < NR) {
+      (reinterpret_cast<float *>(&S.state[g][r >> 1]) + (r & 1))[2] = -ref;
+      S.alpha[g][r] = -ref;
+    }
+    if (lane == 0) S.unseen[g] = unseen;
   }
   named_bar_sync(1 + g, 128);
 #pragma unroll
@@ -968,7 +986,8 @@ IPD_DEVINL void first_references(Shared &S, const Softmax &X, u64 (&y)[NR / 2], 
 }
 
 // Rows whose weights would leave kLimit get new references; O and the sums of just those
-// are rescaled, a TMEM column each.
+// are rescaled, a TMEM column each.  Rows that see their item's first keys here get their first
+// references (higher or lower: their sums are zeros, and their factor may be past fp32).
 template <int NR>
 IPD_DEVINL void move_references(Shared &S, const Softmax &X, u64 (&y)[NR / 2], float de, uint32_t o_addr, uint32_t l_addr) {
   const int g = X.g, tid = X.tid, lane = X.lane;
@@ -979,33 +998,29 @@ IPD_DEVINL void move_references(Shared &S, const Softmax &X, u64 (&y)[NR / 2], f
     f2_unpack(y[i / 2], y0, y1);
     over |= (y0 + de > kLimit ? 1u << i : 0u) | (y1 + de > kLimit ? 2u << i : 0u);
   }
-  over = __reduce_or_sync(0xffffffffu, over);
+  const uint32_t unseen = S.unseen[g];
+  over = __reduce_or_sync(0xffffffffu, over) | unseen;
   if (lane == 0) S.over[g][X.warp] = over;
   named_bar_sync(1 + g, 128);
   over = S.over[g][0] | S.over[g][1] | S.over[g][2] | S.over[g][3];
-  // their largest exponents among the tile's keys
-#pragma unroll
-  for (int c = 0; c < NR; c += 16) {
-    if ((over >> c & 0xffffu) == 0) continue;
-    float z[16];
-#pragma unroll
-    for (int i = 0; i < 16; i += 2) f2_unpack(f2_add(y[(c + i) / 2], f2_pack(de, de)), z[i], z[i + 1]);
-    const float x = column_reduce(z, lane, [](float a, float b) { return fmaxf(a, b); });
-    if (!(lane & 1)) S.red[g][X.warp][c + (lane >> 1)] = x;
-  }
+  row_maxima<NR>(S, X, y, de);
   named_bar_sync(1 + g, 128);
-  if (tid < NR) {
-    float by = 0.f;  // what the reference rises by
-    if (over >> tid & 1u) {
-      by = fmaxf(fmax3(S.red[g][0][tid], S.red[g][1][tid], S.red[g][2][tid]), S.red[g][3][tid]) - kBase;
-      if (!(by < INFINITY)) by = 0.f;
-      (reinterpret_cast<float *>(&S.state[g][tid >> 1]) + (tid & 1))[2] -= by;
+  if (X.warp == 0) {
+    const int r = lane % NR;
+    float top = 0.f, by = 0.f;  // what the reference rises by
+    if (over >> r & 1u) {
+      top = fmaxf(fmax3(S.red[g][0][r], S.red[g][1][r], S.red[g][2][r]), S.red[g][3][r]);
+      if (fabsf(top) < INFINITY) by = top - kBase;
+      if (lane < NR) (reinterpret_cast<float *>(&S.state[g][r >> 1]) + (r & 1))[2] -= by;
     }
-    S.alpha[g][tid] = -by;
+    if (lane < NR) S.alpha[g][r] = -by;
+    const uint32_t still = __ballot_sync(0xffffffffu, top == -INFINITY) & unseen;
+    if (lane == 0) S.unseen[g] = still;
   }
   named_bar_sync(1 + g, 128);
 #pragma unroll
   for (int i = 0; i < NR; i += 2) y[i / 2] = f2_add(y[i / 2], *reinterpret_cast<const u64 *>(&S.alpha[g][i]));
+  over &= ~unseen;
 #pragma unroll 1
   for (; over; over &= over - 1) {
     const int r = __ffs(over) - 1;
@@ -1091,7 +1106,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
       f2_unpack(y[i], y0, y1);
       top = fmax3(top, y0, y1);
     }
-    const bool move = bar_or(1 + g, 128, first || top + (float)de > kLimit);
+    const bool move = bar_or(1 + g, 128, first || S.unseen[g] || top + (float)de > kLimit);
     // P's buffer is free, and O at rest, once this warpgroup's product before is complete
     if (X.tiles > 0) X.ok = wait(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort, 0) && X.ok;
     tc_fence_after();

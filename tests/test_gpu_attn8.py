@@ -420,3 +420,73 @@ def test_pools_past_32_bits(lib):
     ws = torch.empty(lib.attn8_workspace_size([b]), dtype=torch.uint8, device="cuda")
     lib.verify_attn8([b], [], D ** -0.5, ws)
     _check(c)
+
+
+def _rows_ref(c, r, h, keep=None, scale=D ** -0.5):
+    """(output, tolerance) of request r's rows over KV head h in 64 bits, over the keys in `keep`:
+    the tolerance is the weights' and the output's rounding alone, relative to what an
+    output averages: 2^-8 |o| + (2^-8 + 2^-10) a, a = sum_j w_j |v_j|."""
+    G, n, L = c.hq // c.hkv, c.q_len[r], c.length[r]
+    row, page = sum(c.q_len[:r]), c.table[r, :(L + 15) // 16].long().clamp(0, c.n - 1)
+    one = lambda p, s: (p.view(torch.uint8)[page, h].view(E4).double() *
+                        torch.exp2(s[page, h].double() - 127)[:, None, None]).view(-1, D)[:L]
+    k, v = one(c.kp, c.ks), one(c.vp, c.vs)
+    keep = torch.ones(L, dtype=torch.bool, device="cuda") if keep is None else keep
+    out, tol = [], []
+    for i in range(n):
+        m = keep.clone()
+        m[L - n + i + 1:] = False
+        w = torch.softmax(c.q[row + i, h * G:(h + 1) * G].double() @ k[m].T * scale, -1)
+        o, a = w @ v[m], w @ v[m].abs()
+        out.append(o), tol.append(2.0 ** -8 * o.abs() + (2.0 ** -8 + 2.0 ** -10) * a)
+    return torch.stack(out), torch.stack(tol)
+
+
+def _check_rows(c, r, h, keep=None, scale=D ** -0.5):
+    row, G = sum(c.q_len[:r]), c.hq // c.hkv
+    got = c.out[row:row + c.q_len[r], h * G:(h + 1) * G].double()
+    want, tol = _rows_ref(c, r, h, keep, scale)
+    assert bool(torch.isfinite(got).all())
+    err = (got - want).abs() / tol
+    assert float(err.max()) <= 1, (r, h, float(err.max()))
+
+
+def _along(c, score, noise=0.02):
+    """Keys and queries along one direction: every score is near `score` nats (a number or one
+    a key of request 0 ...)."""
+    g = torch.Generator(device="cuda").manual_seed(99)
+    u = torch.sign(torch.randn(D, generator=g, device="cuda"))
+    c.ks.fill_(120)
+    c.q = (u * 0.75 + noise * torch.randn(c.q.shape, generator=g, device="cuda")).to(torch.bfloat16)
+    unit = 0.75 * D ** 0.5 * 2.0 ** -7  # nats a unit of the entries
+    for r, L in enumerate(c.length):
+        page = c.table[r, :(L + 15) // 16].long()
+        s = score[r] if isinstance(score, (list, tuple)) else torch.full((L,), float(score), device="cuda")
+        s = torch.cat([s, s.new_zeros(16 * len(page) - L)])
+        k = (u * (s / unit)[:, None]).clamp(-448, 448).to(E4).view(torch.uint8).view(len(page), 1, 16, D)
+        c.kp.view(torch.uint8)[page] = k.expand(-1, c.hkv, -1, -1).contiguous()
+
+
+@pytest.mark.parametrize("hq,hkv,q_len,length", [(16, 8, [1, 1], [400, 1000]), (32, 4, [3, 16], [300, 700]), (16, 8, [1], [128 * 300 + 40])])
+@pytest.mark.parametrize("score", [-8, -20, -28])
+def test_a_first_tile_that_is_not_there(lib, hq, hkv, q_len, length, score):
+    """All pages of a part's first tile outside the pool (of every other tile, so that this
+    holds for many parts of a request that is cut): the rest's softmax, however small the scores."""
+    c = Case(hq, hkv, q_len, length, seed=21, spread=0)
+    _along(c, score)
+    b = c.batch(lib)
+    q, cu, ln, table, out = b._keep
+    gone, keep = table.clone(), []
+    for r, L in enumerate(length):
+        m = torch.ones(L, dtype=torch.bool, device="cuda")
+        for t in range(0, (L + 127) // 128, 2):
+            gone[r, 8 * t:8 * t + 8] = c.n + 5
+            m[128 * t:128 * t + 128] = False
+        keep.append(m)
+    b = lib.AttnBatch8(b.cache, q, cu, ln, gone, out, max(q_len), max(length))
+    ws = torch.empty(lib.attn8_workspace_size([b]), dtype=torch.uint8, device="cuda")
+    lib.verify_attn8([b], [], D ** -0.5, ws)
+    assert lib.device_error() == 1
+    for r in range(len(length)):
+        for h in (0, hkv - 1):
+            _check_rows(c, r, h, keep[r])
