@@ -707,9 +707,14 @@ size_t ipd_attn8_workspace_size(const ipd_attn8_batch *verify, int n_verify,
  * decode tokens of n_decode batches (the same thing with q_len 1) in one call.
  * out = softmax(scale q K^T) V per query and head over the values the cache's
  * entries stand for.  q is carried to 2^-17 of its row's largest entry into
- * the products; scores, maxima and sums are fp32; the softmax weights enter
- * the product with V as two e4m3 terms, to 2^-8 of themselves (and 2^-18 of the
- * row's largest); the output is rounded to bf16 once.  A row's result depends on
+ * the products; scores, maxima and sums are fp32; the softmax weights, times V's
+ * scale, enter the product with V as two e4m3 terms, off by at most 2^-9 of
+ * themselves and 2^-19 of the row's largest one: what lies below that beside a
+ * larger one is in the sum of the weights and may be missing in the product.  Over
+ * more than 512 keys the level follows a row down as well, at the next 128 keys (up
+ * to 32 blocks of 128 later where it has risen and fallen often): then the bound is
+ * taken of the largest from there on, so that many small weights behind one large
+ * one count as they are.  The output is rounded to bf16 once.  A row's result depends on
  * no key that it does not see, whatever that key holds, and on no other row.
  * A page id outside the pool is recorded (IPD_DEVERR_PAGE_ID) and its keys are
  * left out; a row that is left with none gets 0.  A request whose offsets are out

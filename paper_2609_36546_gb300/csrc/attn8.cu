@@ -14,14 +14,21 @@
 //   O^T = V^T P^T dims are the rows; V and P in the order they lie in, keys last
 // The transposed form makes the cost follow the number of rows (16, 32 or 64
 // columns) and gives every thread one key: a key's scales are two numbers of its
-// thread.  P goes into the second product as two e4m3 terms, the second times 16,
+// thread.  P goes into the second product as two e4m3 terms, the second times 32,
 // side by side as columns; O's two halves are added at the end.
 //
 // Softmax.  p = 2^(s ck ar + dE - ref): ck holds the softmax scale and K's, ar q's
 // row scale, dE V's exponent relative to that of the item's first tile.  ref is the
-// row's largest so far, less 5; it moves (and O and the sums are rescaled) only
+// row's largest in that tile, less 4; it rises (and O and the sums are rescaled) only
 // when a weight would leave 2^8, so most tiles need no maximum across threads.  The
 // reference includes V's scale, since it is the product that has to fit e4m3.
+// The terms end at 2^-15: 12 to 14 nats below one large weight that V answers with next to
+// nothing, all other keys of a long sequence would be lost.  So references fall too, to a
+// tile's maximum less 4, where all of a row's weights there lie below 2^-7.  This is looked
+// for in a sequence's (part's) second tile, after a rise by more than 2^8, after a fall, and 16
+// tiles after the last move; after far rises the wait doubles, to 32 tiles, so that heads whose
+// tiles differ that much do not swing all the time (64 spans of 1 to 16 over 256 to 16,384 keys,
+// with pages of K scales 1 to 8: 142 us, 209 with a look in every tile, 130 without).
 //
 // Work.  All (request, KV head, block of 128 rows, tile) in one line, cut into parts of
 // equal cost, a CTA each: nothing is claimed, the cut depends on the lengths alone.
@@ -91,9 +98,15 @@ __host__ __device__ constexpr uint32_t col_s(uint32_t g) { return 32u * g; }
 __host__ __device__ constexpr uint32_t col_o(uint32_t g) { return 128u + 64u * g; }
 __host__ __device__ constexpr uint32_t col_l(uint32_t g) { return 384u + 32u * g; }
 
-constexpr float kBase = 4.f;   // a row's reference is its largest exponent less this
-constexpr float kLimit = 8.f;  // weights stay below 2^8 (e4m3 ends at 448)
-constexpr float kLoScale = 16.f;
+constexpr float kBase = 4.f;      // a row's reference is its largest exponent less this
+constexpr float kLimit = 8.f;     // weights stay below 2^8 (e4m3 ends at 448, and their second term too: 8 kLoScale)
+constexpr float kLoScale = 32.f;
+// When references fall: see the head of this file.
+constexpr float kLow = -7.f;      // a tile of lower exponents makes a row's reference fall
+constexpr float kDeep = 64.f;     // ... but no lower than this below its highest: sums and O stay far from fp32's ends
+constexpr float kFarRise = 8.f;   // after a rise by more the next tile is looked through
+constexpr int kIdle = 16, kMostWait = 32;  // tiles between two looks; at most, after far rises
+constexpr int kShort = 4 * kKeys; // sequences up to here: references do not fall
 constexpr int kFar = 100;      // V scales further apart than 2^100 count as that far
 // What a tile of a task with up to 16, 32, 64 and 128 rows costs, and a task beside its tiles (up to
 // 32, 64, 128 rows): the line is cut into equal costs.  In cycles a tile takes about 1,480, 2,170,
@@ -170,8 +183,12 @@ struct Shared {
   alignas(16) float4 state[kGroups][kRows / 2];        // a pair of rows: ar, ar', -ref, -ref'
   alignas(16) float alpha[kGroups][kRows];
   alignas(16) float red[kGroups][4][kRows];
-  uint32_t over[kGroups][4];                           // rows whose references have to move
+  uint32_t over[kGroups][4];                           // rows whose references have to rise
   uint32_t unseen[kGroups];                            // rows that have not seen a key of their item
+  alignas(16) uint32_t below[kGroups][2][4];           // rows that a warp's keys have below kLow (by tiles' parity)
+  uint32_t moved[kGroups], deep[kGroups];              // rows whose sums are rescaled; rows at their floor
+  float floor[kGroups][kRows];                         // how low a row's reference may fall
+  int look[kGroups], gap[kGroups];                     // tiles to the next look for rows that fall; after a far rise
   // first key of a span with a NaN in this dim of V (by an item's first warpgroup)
   int nan_key[kGroups][kD];
   int last[kGroups], abort;
@@ -922,15 +939,16 @@ IPD_DEVINL void mend(Shared &S, Item &I, int set, uint8_t *v, int key_in_tile, i
   }
 }
 
-// Exponents of the rows (in pairs) at a thread's key, against their references.
+// Exponents of the rows' weights (in pairs) at a thread's key, against their references; dz is what
+// V's scale adds.
 template <int NR>
-IPD_DEVINL void exponents(const uint32_t (&s)[NR], const float4 *state, float ck, u64 (&y)[NR / 2]) {
-  const u64 ck2 = f2_pack(ck, ck);
+IPD_DEVINL void exponents(const uint32_t (&s)[NR], const float4 *state, float ck, float dz, u64 (&z)[NR / 2]) {
+  const u64 ck2 = f2_pack(ck, ck), dz2 = f2_pack(dz, dz);
 #pragma unroll
   for (int i = 0; i < NR; i += 2) {
     const float4 st = state[i / 2];
-    y[i / 2] = f2_fma(f2_mul(f2_pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), ck2), f2_pack(st.x, st.y),
-                      f2_pack(st.z, st.w));
+    z[i / 2] = f2_add(f2_fma(f2_mul(f2_pack(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), ck2), f2_pack(st.x, st.y),
+                             f2_pack(st.z, st.w)), dz2);
   }
 }
 
@@ -939,14 +957,14 @@ IPD_DEVINL float redux_max(float x) {
   asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(x));
   return m;
 }
-// The largest exponents of the rows (V's scale among them) over a warp's keys.
+// The largest exponents of the rows over a warp's keys.
 template <int NR>
-IPD_DEVINL void row_maxima(Shared &S, const Softmax &X, const u64 (&y)[NR / 2], float de) {
+IPD_DEVINL void row_maxima(Shared &S, const Softmax &X, const u64 (&z)[NR / 2]) {
   float m = 0.f;
 #pragma unroll
   for (int i = 0; i < NR; i += 2) {
     float z0, z1;
-    f2_unpack(f2_add(y[i / 2], f2_pack(de, de)), z0, z1);
+    f2_unpack(z[i / 2], z0, z1);
     z0 = redux_max(z0), z1 = redux_max(z1);
     m = X.lane == i ? z0 : X.lane == i + 1 ? z1 : m;
   }
@@ -958,9 +976,9 @@ IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[32]) { tc_ld_32x32b_x3
 
 // An item's first references: the rows' largest exponents in its first tile, less kBase.
 template <int NR>
-IPD_DEVINL void first_references(Shared &S, const Softmax &X, u64 (&y)[NR / 2], float de, uint32_t l_addr) {
-  const int g = X.g, tid = X.tid, lane = X.lane;
-  row_maxima<NR>(S, X, y, de);
+IPD_DEVINL void first_references(Shared &S, const Softmax &X, u64 (&z)[NR / 2], uint32_t l_addr) {
+  const int g = X.g, lane = X.lane;
+  row_maxima<NR>(S, X, z);
   named_bar_sync(1 + g, 128);
   if (X.warp == 0) {
     const int r = lane % NR;
@@ -971,12 +989,13 @@ IPD_DEVINL void first_references(Shared &S, const Softmax &X, u64 (&y)[NR / 2], 
     if (lane < NR) {
       (reinterpret_cast<float *>(&S.state[g][r >> 1]) + (r & 1))[2] = -ref;
       S.alpha[g][r] = -ref;
+      S.floor[g][r] = ref - kDeep;
     }
-    if (lane == 0) S.unseen[g] = unseen;
+    if (lane == 0) S.unseen[g] = unseen, S.deep[g] = 0u, S.look[g] = S.gap[g] = 1;
   }
   named_bar_sync(1 + g, 128);
 #pragma unroll
-  for (int i = 0; i < NR; i += 2) y[i / 2] = f2_add(y[i / 2], *reinterpret_cast<const u64 *>(&S.alpha[g][i]));
+  for (int i = 0; i < NR; i += 2) z[i / 2] = f2_add(z[i / 2], *reinterpret_cast<const u64 *>(&S.alpha[g][i]));
   uint32_t zero[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) zero[i] = 0u;
@@ -985,45 +1004,60 @@ IPD_DEVINL void first_references(Shared &S, const Softmax &X, u64 (&y)[NR / 2], 
   tc_wait_st();
 }
 
-// Rows whose weights would leave kLimit get new references; O and the sums of just those
-// are rescaled, a TMEM column each.  Rows that see their item's first keys here get their first
-// references (higher or lower: their sums are zeros, and their factor may be past fp32).
+// Rows whose weights would leave kLimit, rows of `low` and rows that see their item's first keys
+// here get new references: their largest exponents in this tile less kBase.  O and the sums of those
+// that have seen keys are rescaled, a TMEM column each (the others' are zeros, and their factor may
+// be past fp32).
 template <int NR>
-IPD_DEVINL void move_references(Shared &S, const Softmax &X, u64 (&y)[NR / 2], float de, uint32_t o_addr, uint32_t l_addr) {
-  const int g = X.g, tid = X.tid, lane = X.lane;
+IPD_DEVINL void move_references(Shared &S, const Softmax &X, u64 (&z)[NR / 2], uint32_t low, uint32_t o_addr, uint32_t l_addr) {
+  const int g = X.g, lane = X.lane;
   uint32_t over = 0;
 #pragma unroll
   for (int i = 0; i < NR; i += 2) {
-    float y0, y1;
-    f2_unpack(y[i / 2], y0, y1);
-    over |= (y0 + de > kLimit ? 1u << i : 0u) | (y1 + de > kLimit ? 2u << i : 0u);
+    float z0, z1;
+    f2_unpack(z[i / 2], z0, z1);
+    over |= (z0 > kLimit ? 1u << i : 0u) | (z1 > kLimit ? 2u << i : 0u);
   }
-  const uint32_t unseen = S.unseen[g];
-  over = __reduce_or_sync(0xffffffffu, over) | unseen;
+  over = __reduce_or_sync(0xffffffffu, over);
   if (lane == 0) S.over[g][X.warp] = over;
-  named_bar_sync(1 + g, 128);
-  over = S.over[g][0] | S.over[g][1] | S.over[g][2] | S.over[g][3];
-  row_maxima<NR>(S, X, y, de);
+  row_maxima<NR>(S, X, z);
   named_bar_sync(1 + g, 128);
   if (X.warp == 0) {
     const int r = lane % NR;
-    float top = 0.f, by = 0.f;  // what the reference rises by
-    if (over >> r & 1u) {
-      top = fmaxf(fmax3(S.red[g][0][r], S.red[g][1][r], S.red[g][2][r]), S.red[g][3][r]);
-      if (fabsf(top) < INFINITY) by = top - kBase;
-      if (lane < NR) (reinterpret_cast<float *>(&S.state[g][r >> 1]) + (r & 1))[2] -= by;
+    const uint32_t unseen = S.unseen[g], bit = lane < NR ? 1u << r : 0u;
+    over = S.over[g][0] | S.over[g][1] | S.over[g][2] | S.over[g][3];
+    const float top = fmaxf(fmax3(S.red[g][0][r], S.red[g][1][r], S.red[g][2][r]), S.red[g][3][r]);
+    float *state = reinterpret_cast<float *>(&S.state[g][r >> 1]) + (r & 1) + 2;
+    const float ref = -*state, floor = S.floor[g][r];
+    const bool seen = !(unseen >> r & 1u);
+    // (a maximum that is not finite: no key in this tile, NaN alone, or more than fp32 holds)
+    float now = ref;
+    if (((over | low | unseen) >> r & 1u) && fabsf(top) < INFINITY) now = ref + (top - kBase);
+    if (now < ref && seen) now = fminf(ref, fmaxf(now, floor));
+    const float by = now - ref;
+    __syncwarp();
+    if (bit) {
+      *state = -now;
+      S.alpha[g][r] = -by;
+      S.floor[g][r] = seen ? fmaxf(floor, now - kDeep) : now - kDeep;
     }
-    if (lane < NR) S.alpha[g][r] = -by;
     const uint32_t still = __ballot_sync(0xffffffffu, top == -INFINITY) & unseen;
-    if (lane == 0) S.unseen[g] = still;
+    const uint32_t moved = __ballot_sync(0xffffffffu, bit && by != 0.f) & ~unseen;
+    const uint32_t deep = __ballot_sync(0xffffffffu, bit && by < 0.f && now <= floor) & ~unseen;
+    const bool far = __any_sync(0xffffffffu, by > kFarRise && seen);
+    if (lane == 0) {
+      const int gap = S.gap[g];
+      S.unseen[g] = still, S.moved[g] = moved, S.deep[g] = (S.deep[g] & ~moved) | deep;
+      S.look[g] = far ? gap : (moved & low) ? 1 : kIdle;
+      if (far) S.gap[g] = min(2 * gap, kMostWait);
+    }
   }
   named_bar_sync(1 + g, 128);
 #pragma unroll
-  for (int i = 0; i < NR; i += 2) y[i / 2] = f2_add(y[i / 2], *reinterpret_cast<const u64 *>(&S.alpha[g][i]));
-  over &= ~unseen;
+  for (int i = 0; i < NR; i += 2) z[i / 2] = f2_add(z[i / 2], *reinterpret_cast<const u64 *>(&S.alpha[g][i]));
 #pragma unroll 1
-  for (; over; over &= over - 1) {
-    const int r = __ffs(over) - 1;
+  for (uint32_t left = S.moved[g]; left; left &= left - 1) {
+    const int r = __ffs(left) - 1;
     const float f = ex2_approx(S.alpha[g][r]);
     uint32_t a, b, l;
     tc_ld_x1(o_addr + r, a);
@@ -1053,7 +1087,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
   const int turn = NR == 32 ? (tid >> 1) & 3 : (tid >> 2) & 1;  // P's swizzle
   uint8_t *prow = S.p[g] + tid * 2 * NR;
   int e0 = 0;
-  bool first = true;
+  int look = I.L > kShort ? n_tiles : -1;  // the tile that is looked through for rows that fall (-1: none)
 #pragma unroll 1
   for (int t = 0; t < n_tiles; ++t) {
     const uint32_t k = X.tiles % kScales;
@@ -1064,7 +1098,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
     const float ck = M.ck[tid / kPage];
     const int ev = M.ev[tid / kPage];
     const bool hides = key0 + kKeys > masked || M.gap;
-    if (first) {
+    if (t == 0) {
       int top = -kNoPage;
 #pragma unroll
       for (int i = 0; i < kPages; ++i)
@@ -1077,16 +1111,18 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
       hidden = ev == kNoPage || key >= L ? NR : (int)max(0LL, min((long long)NR, (long long)(key - sees) * group - row0));
       if (hidden == NR) de = 0;
     }
-    const float fk = ev == 128 && hidden < NR ? __uint_as_float(0x7fc00000u) : pow2i(de);
+    // what V's scale adds to an exponent (a scale of NaN makes the weights of rows that see the key NaN),
+    // and its inverse, for the sums
+    const float dz = ev == 128 && hidden < NR ? __uint_as_float(0x7fc00000u) : (float)de, inv = pow2i(-de);
     arrive_warp(&S.sc_empty[g][k], lane);
     X.ok = wait(&S.s_full[g], full(X.tiles, 1), &S.abort, 0) && X.ok;
     tc_fence_after();
-    u64 y[NR / 2];
+    u64 z[NR / 2];
     {
       uint32_t s[NR];
       load_scores(s_addr, s);
       tc_wait_ld();
-      exponents(s, S.state[g], ck, y);
+      exponents(s, S.state[g], ck, dz, z);
     }
     tc_fence_before();
     arrive_warp(&S.s_empty[g], lane);
@@ -1094,27 +1130,48 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
       asm volatile("" ::: "memory");  // (a branch, not 32 predicates)
 #pragma unroll
       for (int i = 0; i < NR; i += 2) {
-        float y0, y1;
-        f2_unpack(y[i / 2], y0, y1);
-        y[i / 2] = f2_pack(i < hidden ? -INFINITY : y0, i + 1 < hidden ? -INFINITY : y1);
+        float z0, z1;
+        f2_unpack(z[i / 2], z0, z1);
+        z[i / 2] = f2_pack(i < hidden ? -INFINITY : z0, i + 1 < hidden ? -INFINITY : z1);
       }
     }
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NR / 2; ++i) {
-      float y0, y1;
-      f2_unpack(y[i], y0, y1);
-      top = fmax3(top, y0, y1);
+      float z0, z1;
+      f2_unpack(z[i], z0, z1);
+      top = fmax3(top, z0, z1);
     }
-    const bool move = bar_or(1 + g, 128, first || S.unseen[g] || top + (float)de > kLimit);
+    if (t == look) {
+      uint32_t below = 0;  // a bit a row, the sign of its exponent against kLow
+#pragma unroll
+      for (int i = NR - 2; i >= 0; i -= 2) {
+        float z0, z1;
+        f2_unpack(f2_add(z[i / 2], f2_pack(-kLow, -kLow)), z0, z1);
+        below = __funnelshift_l(__float_as_uint(z1), below, 1);
+        below = __funnelshift_l(__float_as_uint(z0), below, 1);
+      }
+      below = __reduce_and_sync(0xffffffffu, below) & ~S.deep[g];
+      if (lane == 0) S.below[g][t & 1][X.warp] = below;
+    }
+    bool move = bar_or(1 + g, 128, t == 0 || S.unseen[g] || top > kLimit);
+    uint32_t low = 0;  // rows that fall
+    if (t == look) {
+      const uint4 b = *reinterpret_cast<const uint4 *>(S.below[g][t & 1]);
+      low = b.x & b.y & b.z & b.w;
+      move |= low != 0;
+    }
     // P's buffer is free, and O at rest, once this warpgroup's product before is complete
     if (X.tiles > 0) X.ok = wait(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort, 0) && X.ok;
     tc_fence_after();
     if (move) {
-      if (first) first_references<NR>(S, X, y, (float)de, l_addr);
-      else move_references<NR>(S, X, y, (float)de, o_addr, l_addr);
+      if (t == 0) first_references<NR>(S, X, z, l_addr);
+      else move_references<NR>(S, X, z, low, o_addr, l_addr);
+      if (look >= 0) look = t + S.look[g];
+    } else if (t == look) {
+      look = t + kIdle;
     }
-    const u64 fk2 = f2_pack(fk, fk);
+    const u64 inv2 = f2_pack(inv, inv);
     const uint32_t lo16 = half2_of(kLoScale, kLoScale);
 #pragma unroll
     for (int c = 0; c < NR; c += 16) {
@@ -1126,11 +1183,11 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
         uint32_t h[2], b[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          u64 &p = y[c / 2 + q * 2 + k];
+          u64 &p = z[c / 2 + q * 2 + k];
           float p0, p1;
           f2_unpack(p, p0, p1);
-          p = f2_pack(ex2_approx(p0), ex2_approx(p1));
-          f2_unpack(f2_mul(p, fk2), p0, p1);
+          p0 = ex2_approx(p0), p1 = ex2_approx(p1);
+          p = f2_pack(p0, p1);
           h[k] = half2_of(p0, p1);
         }
         hi[q] = e4m3x4_h(h[0], h[1]);
@@ -1143,17 +1200,10 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
         float l0, l1;
-        f2_unpack(f2_add(f2_pack(__uint_as_float(l[i]), __uint_as_float(l[i + 1])), y[(c + i) / 2]), l0, l1);
+        f2_unpack(f2_fma(z[(c + i) / 2], inv2, f2_pack(__uint_as_float(l[i]), __uint_as_float(l[i + 1]))), l0, l1);
         l[i] = __float_as_uint(l0), l[i + 1] = __float_as_uint(l1);
       }
       tc_st_32x32b_x16(l_addr + c, l);
-    }
-    if (ev == 128 && hidden > 0 && hidden < NR) {
-      // a NaN scale reaches no row that does not see the key
-#pragma unroll 1
-      for (int i = 0; i < hidden; ++i)
-#pragma unroll 1
-        for (int k = i; k < 2 * NR; k += NR) prow[(((k >> 4) ^ turn) << 4) + (k & 15)] = 0;
     }
     if (key0 + kKeys > masked && g == I.wg) {
       // hidden keys: the tile is looked through before the product, which takes the first
@@ -1167,7 +1217,6 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
     tc_fence_before();
     arrive_warp(&S.p_full[g], lane);
     ++X.tiles;
-    first = false;
   }
   return e0;
 }

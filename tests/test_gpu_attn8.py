@@ -422,15 +422,18 @@ def test_pools_past_32_bits(lib):
     _check(c)
 
 
-def _rows_ref(c, r, h, keep=None, scale=D ** -0.5):
+def _rows_ref(c, r, h, keep=None, scale=D ** -0.5, ends=False):
     """(output, tolerance) of request r's rows over KV head h in 64 bits, over the keys in `keep`:
     the tolerance is the weights' and the output's rounding alone, relative to what an
-    output averages: 2^-8 |o| + (2^-8 + 2^-10) a, a = sum_j w_j |v_j|."""
+    output averages: 2^-8 |o| + (2^-8 + 2^-10) a, a = sum_j w_j |v_j|.  With `ends` also what the
+    weights' two terms end at: half of e4m3's least value over the second's factor, 2^-10 / 32, beside
+    a largest weight of 2^4 or more: 2^-19 of the row's largest weight times scale, per entry."""
     G, n, L = c.hq // c.hkv, c.q_len[r], c.length[r]
     row, page = sum(c.q_len[:r]), c.table[r, :(L + 15) // 16].long().clamp(0, c.n - 1)
     one = lambda p, s: (p.view(torch.uint8)[page, h].view(E4).double() *
                         torch.exp2(s[page, h].double() - 127)[:, None, None]).view(-1, D)[:L]
     k, v = one(c.kp, c.ks), one(c.vp, c.vs)
+    fv = torch.exp2(c.vs[page, h].double() - 127)[:, None].expand(-1, 16).reshape(-1)[:L]
     keep = torch.ones(L, dtype=torch.bool, device="cuda") if keep is None else keep
     out, tol = [], []
     for i in range(n):
@@ -438,14 +441,15 @@ def _rows_ref(c, r, h, keep=None, scale=D ** -0.5):
         m[L - n + i + 1:] = False
         w = torch.softmax(c.q[row + i, h * G:(h + 1) * G].double() @ k[m].T * scale, -1)
         o, a = w @ v[m], w @ v[m].abs()
-        out.append(o), tol.append(2.0 ** -8 * o.abs() + (2.0 ** -8 + 2.0 ** -10) * a)
+        c0 = 2.0 ** -19 * (w * fv[m]).amax(-1, keepdim=True) * (v[m] / fv[m][:, None]).abs().sum(0) if ends else 0.0
+        out.append(o), tol.append(2.0 ** -8 * o.abs() + (2.0 ** -8 + 2.0 ** -10) * a + c0)
     return torch.stack(out), torch.stack(tol)
 
 
-def _check_rows(c, r, h, keep=None, scale=D ** -0.5):
+def _check_rows(c, r, h, keep=None, scale=D ** -0.5, ends=False):
     row, G = sum(c.q_len[:r]), c.hq // c.hkv
     got = c.out[row:row + c.q_len[r], h * G:(h + 1) * G].double()
-    want, tol = _rows_ref(c, r, h, keep, scale)
+    want, tol = _rows_ref(c, r, h, keep, scale, ends)
     assert bool(torch.isfinite(got).all())
     err = (got - want).abs() / tol
     assert float(err.max()) <= 1, (r, h, float(err.max()))
@@ -490,3 +494,65 @@ def test_a_first_tile_that_is_not_there(lib, hq, hkv, q_len, length, score):
     for r in range(len(length)):
         for h in (0, hkv - 1):
             _check_rows(c, r, h, keep[r])
+
+
+@pytest.mark.parametrize("nats", [6, 10, 12, 13, 14, 20, 25])
+@pytest.mark.parametrize("hq,hkv,q_len,length,at", [(16, 8, [1], [33000], 0), (32, 4, [2], [40000], 0), (32, 4, [16], [35011], 7000),
+                                                    (16, 8, [1, 3], [50000, 40000], 5)])
+def test_one_key_far_above_many(lib, hq, hkv, q_len, length, at, nats):
+    """A key `nats` above all others whose values are zero: the output is the others' mean.  (The 127
+    keys of its own tile, below 2^-8 of all, may be lost beside it.)"""
+    c = Case(hq, hkv, q_len, length, seed=22, spread=0)
+    g = torch.Generator(device="cuda").manual_seed(nats)
+    # (the others between 12 and 13 nats below zero, the one above)
+    low = [-12.5 + torch.rand(L, generator=g, device="cuda") for L in length]
+    for s in low:
+        s[at] = nats - 12.0
+    _along(c, low, noise=0.0)
+    c.vp = c.vp.float().abs().to(E4)
+    for r in range(len(length)):
+        c.vp.view(torch.uint8)[c.table[r, at // 16].long(), :, at % 16] = 0
+    _run(lib, c)
+    for r in range(len(length)):
+        _check_rows(c, r, hkv // 2)
+    assert lib.device_error() == 0
+
+
+@pytest.mark.parametrize("far", [8, 14, 18, 24, 40])
+@pytest.mark.parametrize("hq,hkv,q_len,length,at", [(16, 8, [1], [33000], 0), (32, 4, [4], [40000], 33), (16, 8, [2, 1], [35000, 50000], 60)])
+def test_a_page_of_far_larger_values(lib, hq, hkv, q_len, length, at, far):
+    """A page whose V scale is 2^far larger, zero in most dims: keys of other pages still count there
+    (but for the 112 of its own tile, below 2^-8 of all)."""
+    c = Case(hq, hkv, q_len, length, seed=23, spread=0)
+    c.vp = c.vp.float().abs().to(E4)
+    for r in range(len(length)):
+        page = c.table[r, at].long()
+        c.vs[page] = 120 + far
+        c.vp.view(torch.uint8)[page, :, :, 5:] = 0
+    _run(lib, c)
+    for r in range(len(length)):
+        _check_rows(c, r, 0)
+
+
+@pytest.mark.parametrize("hq,hkv,q_len,length", [(16, 8, [1], [20000]), (32, 4, [16], [9000])])
+def test_scores_that_swing(lib, hq, hkv, q_len, length):
+    """Levels that rise and fall by up to 30 nats from tile to tile, values of the highest ones
+    zero: references move in both directions, and the same bytes come out each time."""
+    c = Case(hq, hkv, q_len, length, seed=24, spread=0)
+    c.vp = c.vp.float().abs().to(E4)
+    L = length[0]
+    tile = torch.arange(L, device="cuda") // 128
+    g = torch.Generator(device="cuda").manual_seed(5)
+    level = torch.tensor([0.0, -25.0, -12.0, -28.0, -5.0, -20.0], device="cuda")[tile % 6]
+    s = level + torch.rand(L, generator=g, device="cuda")
+    _along(c, [s], noise=0.0)
+    flat = c.vp.view(torch.uint8)[c.table[0, :(L + 15) // 16].long()].clone()
+    high = torch.nn.functional.pad(level > -19, (0, flat.shape[0] * 16 - L)).view(-1, 16)
+    flat.permute(0, 2, 1, 3)[high] = 0
+    c.vp.view(torch.uint8)[c.table[0, :(L + 15) // 16].long()] = flat
+    _run(lib, c)
+    for h in (0, hkv - 1):
+        _check_rows(c, 0, h, ends=True)
+    first = c.out.clone()
+    _run(lib, c)
+    assert torch.equal(c.out, first)
