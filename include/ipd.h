@@ -714,8 +714,10 @@ size_t ipd_attn8_workspace_size(const ipd_attn8_batch *verify, int n_verify,
  * more than 512 keys the level follows a row down as well, at the next 128 keys (up
  * to 32 blocks of 128 later where it has risen and fallen often): then the bound is
  * taken of the largest from there on, so that many small weights behind one large
- * one count as they are.  The output is rounded to bf16 once.  A row's result depends on
- * no key that it does not see, whatever that key holds, and on no other row.
+ * one count as they are.  V scales more than 2^80 from the largest of the first
+ * pages that all rows of a block of up to 128 see count as that far.  The output is rounded to
+ * bf16 once.  A row's result depends on no key that it does not see, whatever that
+ * key holds, and on no other row.
  * A page id outside the pool is recorded (IPD_DEVERR_PAGE_ID) and its keys are
  * left out; a row that is left with none gets 0.  A request whose offsets are out
  * of order or past total_q (IPD_DEVERR_SPAN), or whose seq_len is below its

@@ -18,7 +18,7 @@
 // side by side as columns; O's two halves are added at the end.
 //
 // Softmax.  p = 2^(s ck ar + dE - ref): ck holds the softmax scale and K's, ar q's
-// row scale, dE V's exponent relative to that of the item's first tile.  ref is the
+// row scale, dE V's exponent relative to that of the item's first pages.  ref is the
 // row's largest in that tile, less 4; it rises (and O and the sums are rescaled) only
 // when a weight would leave 2^8, so most tiles need no maximum across threads.  The
 // reference includes V's scale, since it is the product that has to fit e4m3.
@@ -107,7 +107,7 @@ constexpr float kDeep = 64.f;     // ... but no lower than this below its highes
 constexpr float kFarRise = 8.f;   // after a rise by more the next tile is looked through
 constexpr int kIdle = 16, kMostWait = 32;  // tiles between two looks; at most, after far rises
 constexpr int kShort = 4 * kKeys; // sequences up to here: references do not fall
-constexpr int kFar = 100;      // V scales further apart than 2^100 count as that far
+constexpr int kFar = 80;       // V scales further than 2^80 from that of the first tile count as that far
 // What a tile of a task with up to 16, 32, 64 and 128 rows costs, and a task beside its tiles (up to
 // 32, 64, 128 rows): the line is cut into equal costs.  In cycles a tile takes about 1,480, 2,170,
 // 3,200 and 3,750 where a CTA has one task alone, 1,450, 1,600, 2,400 and 3,700 where it has several.
@@ -1086,7 +1086,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
   const int masked = I.masked;
   const int turn = NR == 32 ? (tid >> 1) & 3 : (tid >> 2) & 1;  // P's swizzle
   uint8_t *prow = S.p[g] + tid * 2 * NR;
-  int e0 = 0;
+  int e0 = kNoPage;  // (until there is a page)
   int look = I.L > kShort ? n_tiles : -1;  // the tile that is looked through for rows that fall (-1: none)
 #pragma unroll 1
   for (int t = 0; t < n_tiles; ++t) {
@@ -1098,12 +1098,16 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
     const float ck = M.ck[tid / kPage];
     const int ev = M.ev[tid / kPage];
     const bool hides = key0 + kKeys > masked || M.gap;
-    if (t == 0) {
-      int top = -kNoPage;
+    if (e0 == kNoPage) {
+      // the largest of the pages that all rows see, whatever the others hold
+      int top = -kNoPage, there = 0;
 #pragma unroll
-      for (int i = 0; i < kPages; ++i)
-        if (M.ev[i] != kNoPage && M.ev[i] != 128) top = max(top, M.ev[i]);
-      e0 = top == -kNoPage ? 0 : top;
+      for (int i = 0; i < kPages; ++i) {
+        const int e = M.ev[i];
+        there |= e != kNoPage;
+        if (e != kNoPage && e != 128 && key0 + i * kPage < masked) top = max(top, e);
+      }
+      if (there) e0 = top == -kNoPage ? 0 : top;
     }
     int de = max(-kFar, min(kFar, ev - e0));
     int hidden = 0;  // rows before this one do not see the key
@@ -1218,7 +1222,7 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
     arrive_warp(&S.p_full[g], lane);
     ++X.tiles;
   }
-  return e0;
+  return e0 == kNoPage ? 0 : e0;
 }
 
 // Joins the parts of a row group of a task that was cut between CTAs, in order.  What bounds it is

@@ -556,3 +556,49 @@ def test_scores_that_swing(lib, hq, hkv, q_len, length):
     first = c.out.clone()
     _run(lib, c)
     assert torch.equal(c.out, first)
+
+
+@pytest.mark.parametrize("scale", [254, 200, 1])
+@pytest.mark.parametrize("hq,hkv,q_len,length", [(16, 8, [40], [90]), (32, 4, [30], [300]), (4, 4, [100, 20], [260, 40])])
+def test_a_hidden_page_s_scale(lib, hq, hkv, q_len, length, scale):
+    """A page of the span whose V scale lies at an end of the range: rows that do not see it
+    keep their bits, at scales 2^20 apart among the pages that they see."""
+    c = Case(hq, hkv, q_len, length, seed=25, spread=0)
+    for r, L in enumerate(length):
+        c.vs[c.table[r, 1:(L + 15) // 16:3].long()] = 100
+    _run(lib, c)
+    first = c.out.clone()
+    for r in range(len(length)):
+        for h in (0, hkv - 1):
+            _check_rows(c, r, h)
+    row = 0
+    keep = torch.zeros(sum(q_len), dtype=torch.bool, device="cuda")
+    for r, (n, L) in enumerate(zip(q_len, length)):
+        last = (L - 1) // 16 - 1
+        c.vs[c.table[r, last:(L + 15) // 16].long()] = scale
+        see = torch.arange(n, device="cuda") + L - n
+        keep[row:row + n] = see < 16 * last
+        row += n
+    assert 0 < int(keep.sum()) < len(keep)
+    _run(lib, c)
+    assert torch.equal(c.out[keep], first[keep])
+
+
+@pytest.mark.parametrize("byte", [30, 127, 215])
+def test_scales_far_from_one_behind_absent_pages(lib, byte):
+    """V scales 2^97 below and 2^88 above 1, the first tiles' pages outside the pool: exponents count
+    from those of the first pages that there are."""
+    c = Case(16, 8, [1, 2], [300, 1000], seed=26, spread=1)
+    c.vs = (c.vs.int() - 120 + byte).to(torch.uint8)
+    b = c.batch(lib)
+    q, cu, ln, table, out = b._keep
+    gone = table.clone()
+    gone[:, :16] = c.n + 1
+    b = lib.AttnBatch8(b.cache, q, cu, ln, gone, out, 2, 1000)
+    ws = torch.empty(lib.attn8_workspace_size([b]), dtype=torch.uint8, device="cuda")
+    lib.verify_attn8([b], [], D ** -0.5, ws)
+    assert lib.device_error() == 1
+    for r, L in enumerate(c.length):
+        keep = torch.ones(L, dtype=torch.bool, device="cuda")
+        keep[:256] = False
+        _check_rows(c, r, 3, keep)
