@@ -136,7 +136,7 @@ struct Weigher {
       f2_unpack(y, a, b);
       y = f2_pack(fmaxf(a, -64.f), fmaxf(b, -64.f));  // (fmaxf drops a NaN)
     }
-    pow2_weight2<true>(y, w0, w1, f2_pack(one, one));
+    pow2_weight2(y, w0, w1, f2_pack(one, one));
   }
   IPD_DEVINL void any_two(uint32_t w, uint32_t &w0, uint32_t &w1) const {
     if (mode == kNear) two<kNear>(w, w0, w1);

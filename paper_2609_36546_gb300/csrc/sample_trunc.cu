@@ -81,6 +81,7 @@ struct Params {
   int32_t *tokens, *kept;
   float *logp;
   int vocab, piece;  // piece: entries a CTA counts (a multiple of 8)
+  float one;         // 1: see pow2_weight2
 };
 
 struct Scale {
@@ -89,8 +90,8 @@ struct Scale {
   bool coarse;      // the x of least2 is far below -64: bf16 is coarse at l_max
   uint32_t least2;  // a bf16 value (twice) of weight 0 from which on weights are 0
   uint32_t min_w;   // smallest weight that counts (min-p; at least 1)
+  float one;        // 1: see pow2_weight2
 };
-
 
 // ---- order keys --------------------------------------------------------------
 // A 16-bit key rises with the bf16 value; NaN counts as -inf, -0 as 0.
@@ -121,7 +122,7 @@ IPD_DEVINL void weight2(const Scale &S, uint32_t w, uint32_t &w0, uint32_t &w1) 
     f2_unpack(x, a, b);
     x = f2_pack(fmaxf(a, -64.f), fmaxf(b, -64.f));
   }
-  pow2_weight2(x, w0, w1);
+  pow2_weight2(x, w0, w1, f2_pack(S.one, S.one));
   if (w0 < S.min_w) w0 = 0u;
   if (w1 < S.min_w) w1 = 0u;
 }
@@ -140,8 +141,9 @@ IPD_DEVINL void weights(const Scale &S, uint32_t w, uint32_t &w0, uint32_t &w1) 
 IPD_DEVINL uint32_t weight_floor(float min_p) {
   return max(1u, (uint32_t)ceilf(min_p * 0x1p30f));  // exact: a power of two times min_p
 }
-IPD_DEVINL Scale make_scale(float c, float min_p, uint32_t top_key) {
+IPD_DEVINL Scale make_scale(float c, float min_p, uint32_t top_key, float one) {
   Scale C;
+  C.one = one;
   C.c = c;
   C.inf = top_key == kKeyInf;
   C.top = key_value(top_key);
@@ -640,7 +642,7 @@ static IPD_DEVINL void run(const Params &P) {
     if (csize > 1) cluster_sync();
     return;
   }
-  const Scale C = make_scale(c, min_p, top_key);
+  const Scale C = make_scale(c, min_p, top_key, P.one);
   if (tid == 0) {
     S.scale = C;
     S.hist[kBins / 2 + kFreeWord] = 0;  // what counted as -2^12
@@ -823,6 +825,7 @@ extern "C" int ipd_sample_trunc(const uint16_t *logits, int64_t row_stride, int 
   P.kept = n_kept;
   P.logp = logp;
   P.vocab = vocab;
+  P.one = 1.f;
   P.piece = (int)(((span + csize - 1) / csize + 7) / 8 * 8);
   // Threads of a CTA: 512, two CTAs an SM, or 256 and four once there are rows for
   // them, whose searches overlap more.  512 / 256 threads: 512 rows of 151,936 72.1 /

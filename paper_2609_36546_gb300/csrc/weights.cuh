@@ -19,23 +19,21 @@ IPD_DEVINL u64 f2_add_rz(u64 a, u64 b) {
 // values up to 2^24 and all there is above, so that its floor is the exact sum's.
 //
 // The compiler contracts a packed product and sum, explicitly rounded ones too, into one
-// operation.  kApart keeps every product's own rounding: the sum is a product with `one`, a pair
-// of 1 that the compiler does not know, so that there is nothing to contract.
-template <bool kApart = false>
-IPD_DEVINL void pow2_weight2(u64 x, uint32_t &w0, uint32_t &w1, u64 one = 0) {
-  const auto add = [&](u64 product, u64 b) { return kApart ? f2_fma(product, one, b) : f2_add(product, b); };
+// operation.  So that every product keeps its own rounding, the sum is a product with `one`, a pair
+// of 1 that the compiler does not know: there is nothing to contract.
+IPD_DEVINL void pow2_weight2(u64 x, uint32_t &w0, uint32_t &w1, u64 one) {
   const float kMagic = 12582912.f;  // 1.5 * 2^23: x + kMagic rounds x to a whole number
-  const u64 r = add(x, f2_pack(kMagic, kMagic));
-  const u64 f = kApart ? add(x, f2_sub(f2_pack(kMagic, kMagic), r)) : f2_sub(x, f2_sub(r, f2_pack(kMagic, kMagic)));
+  const u64 r = f2_fma(x, one, f2_pack(kMagic, kMagic));
+  const u64 f = f2_fma(x, one, f2_sub(f2_pack(kMagic, kMagic), r));
   const float c1 = __uint_as_float(0x3f317213u) * 0x1p30f, c2 = __uint_as_float(0x3e75fcdbu) * 0x1p30f,
               c3 = __uint_as_float(0x3d635d55u) * 0x1p30f, c4 = __uint_as_float(0x3c1e760bu) * 0x1p30f,
               c5 = __uint_as_float(0x3aad4281u) * 0x1p30f;
   u64 p = f2_pack(c5, c5);
-  p = add(f2_mul(p, f), f2_pack(c4, c4));
-  p = add(f2_mul(p, f), f2_pack(c3, c3));
-  p = add(f2_mul(p, f), f2_pack(c2, c2));
-  p = add(f2_mul(p, f), f2_pack(c1, c1));
-  p = add(f2_mul(p, f), f2_pack(0x1p30f, 0x1p30f));
+  p = f2_fma(f2_mul(p, f), one, f2_pack(c4, c4));
+  p = f2_fma(f2_mul(p, f), one, f2_pack(c3, c3));
+  p = f2_fma(f2_mul(p, f), one, f2_pack(c2, c2));
+  p = f2_fma(f2_mul(p, f), one, f2_pack(c1, c1));
+  p = f2_fma(f2_mul(p, f), one, f2_pack(0x1p30f, 0x1p30f));
   float r0, r1, p0, p1;
   f2_unpack(r, r0, r1);
   f2_unpack(p, p0, p1);

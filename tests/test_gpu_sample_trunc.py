@@ -249,3 +249,26 @@ def test_side_stream_and_repeat(lib):
     lib.sample_trunc(late, u, b, stream=side)
     side.synchronize()
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n,V", [(1500, 2), (300, 700), (60, 60001)])
+def test_weights_at_their_border(lib, n, V):
+    """min_p at an entry's weight keeps it, one unit more drops it: weights below 2^24 are fp32
+    values over 2^30, so one that is off by one would move the border."""
+    g = torch.Generator().manual_seed(n)
+    logits = torch.full((n, V), -float("inf"), dtype=torch.bfloat16)
+    logits[:, 0] = (torch.randn(n, generator=g) * 2).to(torch.bfloat16)
+    at = V - 1 - V // 3
+    logits[:, at] = (logits[:, 0].float() - 4 - 10 * torch.rand(n, generator=g)).to(torch.bfloat16)
+    inv_t = (0.9 + 0.4 * torch.rand(n, generator=g)).numpy()
+    f = logits.float().numpy()
+    w = np.array([_weights(f[r], f[r].max(), inv_t[r])[0][at] for r in range(n)])
+    sharp = (w > 1) & (w < 1 << 24)
+    assert sharp.sum() > n // 2
+    for more, want in ((0, 2), (1, 1)):
+        min_p = ((w + more) * 2.0 ** -30).astype(np.float32)
+        tok, kept = (torch.full((n,), -9, dtype=torch.int32, device="cuda") for _ in "ab")
+        lib.sample_trunc(logits.cuda(), torch.zeros(n, device="cuda"), tok, n_kept=kept,
+                         inv_temperature=torch.from_numpy(inv_t).cuda(), min_p=torch.from_numpy(min_p).cuda())
+        off = kept.cpu().numpy()[sharp] != want
+        assert not off.any(), (want, int(off.sum()), len(off))
