@@ -25,10 +25,11 @@
 // The terms end at 2^-15: 12 to 14 nats below one large weight that V answers with next to
 // nothing, all other keys of a long sequence would be lost.  So references fall too, to a
 // tile's maximum less 4, where all of a row's weights there lie below 2^-7.  This is looked
-// for in a sequence's (part's) second tile, after a rise by more than 2^8, after a fall, and 16
-// tiles after the last move; after far rises the wait doubles, to 32 tiles, so that heads whose
-// tiles differ that much do not swing all the time (64 spans of 1 to 16 over 256 to 16,384 keys,
-// with pages of K scales 1 to 8: 142 us, 209 with a look in every tile, 130 without).
+// for in a part's second tile, in the tile after a fall or a rise by more than 2^8, and 32
+// tiles after the last move; with every far rise the wait behind the next one doubles, to 32
+// tiles, so that heads whose tiles differ that much do not swing all the time (64 spans of 1 to
+// 16 over 256 to 16,384 keys, K scales of pages 2^3 apart: 131 us, 209 with a look in
+// every tile, 130 with none).
 //
 // Work.  All (request, KV head, block of 128 rows, tile) in one line, cut into parts of
 // equal cost, a CTA each: nothing is claimed, the cut depends on the lengths alone.
@@ -105,7 +106,7 @@ constexpr float kLoScale = 32.f;
 constexpr float kLow = -7.f;      // a tile of lower exponents makes a row's reference fall
 constexpr float kDeep = 64.f;     // ... but no lower than this below its highest: sums and O stay far from fp32's ends
 constexpr float kFarRise = 8.f;   // after a rise by more the next tile is looked through
-constexpr int kIdle = 16, kMostWait = 32;  // tiles between two looks; at most, after far rises
+constexpr int kIdle = 32, kMostWait = 32;  // tiles between two looks; at most, after far rises
 constexpr int kShort = 4 * kKeys; // sequences up to here: references do not fall
 constexpr int kFar = 80;       // V scales further than 2^80 from that of the first tile count as that far
 // What a tile of a task with up to 16, 32, 64 and 128 rows costs, and a task beside its tiles (up to
@@ -183,9 +184,8 @@ struct Shared {
   alignas(16) float4 state[kGroups][kRows / 2];        // a pair of rows: ar, ar', -ref, -ref'
   alignas(16) float alpha[kGroups][kRows];
   alignas(16) float red[kGroups][4][kRows];
-  uint32_t over[kGroups][4];                           // rows whose references have to rise
   uint32_t unseen[kGroups];                            // rows that have not seen a key of their item
-  alignas(16) uint32_t below[kGroups][2][4];           // rows that a warp's keys have below kLow (by tiles' parity)
+  uint32_t below[kGroups][4];                          // rows that a warp's keys have below kLow
   uint32_t moved[kGroups], deep[kGroups];              // rows whose sums are rescaled; rows at their floor
   float floor[kGroups][kRows];                         // how low a row's reference may fall
   int look[kGroups], gap[kGroups];                     // tiles to the next look for rows that fall; after a far rise
@@ -974,87 +974,66 @@ IPD_DEVINL void row_maxima(Shared &S, const Softmax &X, const u64 (&z)[NR / 2]) 
 IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[16]) { tc_ld_32x32b_x16(taddr, r); }
 IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[32]) { tc_ld_32x32b_x32(taddr, r); }
 
-// An item's first references: the rows' largest exponents in its first tile, less kBase.
+// New references: of all rows at an item's first tile; afterwards of rows whose weights would leave
+// kLimit, of those that all warps have in `low`, and of rows that see their item's first keys here:
+// the rows' largest exponents in this tile less kBase.  O and the sums of rows that have seen keys are
+// rescaled, a TMEM column each (the others' are zeros, and their factor may be past fp32).
+// (The loop over tiles is short of instruction cache: one piece of code for first and later
+// references took 64 spans from 137 to 131 us.)
 template <int NR>
-IPD_DEVINL void first_references(Shared &S, const Softmax &X, u64 (&z)[NR / 2], uint32_t l_addr) {
+IPD_DEVINL void move_references(Shared &S, const Softmax &X, u64 (&z)[NR / 2], uint32_t low, bool first, uint32_t o_addr, uint32_t l_addr) {
   const int g = X.g, lane = X.lane;
+  if (lane == 0) S.below[g][X.warp] = low;
   row_maxima<NR>(S, X, z);
   named_bar_sync(1 + g, 128);
   if (X.warp == 0) {
     const int r = lane % NR;
-    const float now = fmaxf(fmax3(S.red[g][0][r], S.red[g][1][r], S.red[g][2][r]), S.red[g][3][r]);
-    // (a row with NaN alone, or more than fp32 holds, stays at 0; so does, for now, one that has seen nothing)
-    const float ref = fabsf(now) < INFINITY ? now - kBase : 0.f;
-    const uint32_t unseen = __ballot_sync(0xffffffffu, now == -INFINITY && lane < NR);
-    if (lane < NR) {
-      (reinterpret_cast<float *>(&S.state[g][r >> 1]) + (r & 1))[2] = -ref;
-      S.alpha[g][r] = -ref;
-      S.floor[g][r] = ref - kDeep;
-    }
-    if (lane == 0) S.unseen[g] = unseen, S.deep[g] = 0u, S.look[g] = S.gap[g] = 1;
-  }
-  named_bar_sync(1 + g, 128);
-#pragma unroll
-  for (int i = 0; i < NR; i += 2) z[i / 2] = f2_add(z[i / 2], *reinterpret_cast<const u64 *>(&S.alpha[g][i]));
-  uint32_t zero[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) zero[i] = 0u;
-#pragma unroll 1
-  for (int c = 0; c < NR; c += 16) tc_st_32x32b_x16(l_addr + c, zero);
-  tc_wait_st();
-}
-
-// Rows whose weights would leave kLimit, rows of `low` and rows that see their item's first keys
-// here get new references: their largest exponents in this tile less kBase.  O and the sums of those
-// that have seen keys are rescaled, a TMEM column each (the others' are zeros, and their factor may
-// be past fp32).
-template <int NR>
-IPD_DEVINL void move_references(Shared &S, const Softmax &X, u64 (&z)[NR / 2], uint32_t low, uint32_t o_addr, uint32_t l_addr) {
-  const int g = X.g, lane = X.lane;
-  uint32_t over = 0;
-#pragma unroll
-  for (int i = 0; i < NR; i += 2) {
-    float z0, z1;
-    f2_unpack(z[i / 2], z0, z1);
-    over |= (z0 > kLimit ? 1u << i : 0u) | (z1 > kLimit ? 2u << i : 0u);
-  }
-  over = __reduce_or_sync(0xffffffffu, over);
-  if (lane == 0) S.over[g][X.warp] = over;
-  row_maxima<NR>(S, X, z);
-  named_bar_sync(1 + g, 128);
-  if (X.warp == 0) {
-    const int r = lane % NR;
-    const uint32_t unseen = S.unseen[g], bit = lane < NR ? 1u << r : 0u;
-    over = S.over[g][0] | S.over[g][1] | S.over[g][2] | S.over[g][3];
+    const bool mine = lane < NR;
     const float top = fmaxf(fmax3(S.red[g][0][r], S.red[g][1][r], S.red[g][2][r]), S.red[g][3][r]);
-    float *state = reinterpret_cast<float *>(&S.state[g][r >> 1]) + (r & 1) + 2;
-    const float ref = -*state, floor = S.floor[g][r];
-    const bool seen = !(unseen >> r & 1u);
-    // (a maximum that is not finite: no key in this tile, NaN alone, or more than fp32 holds)
-    float now = ref;
-    if (((over | low | unseen) >> r & 1u) && fabsf(top) < INFINITY) now = ref + (top - kBase);
-    if (now < ref && seen) now = fminf(ref, fmaxf(now, floor));
-    const float by = now - ref;
-    __syncwarp();
-    if (bit) {
-      *state = -now;
-      S.alpha[g][r] = -by;
-      S.floor[g][r] = seen ? fmaxf(floor, now - kDeep) : now - kDeep;
-    }
-    const uint32_t still = __ballot_sync(0xffffffffu, top == -INFINITY) & unseen;
-    const uint32_t moved = __ballot_sync(0xffffffffu, bit && by != 0.f) & ~unseen;
-    const uint32_t deep = __ballot_sync(0xffffffffu, bit && by < 0.f && now <= floor) & ~unseen;
-    const bool far = __any_sync(0xffffffffu, by > kFarRise && seen);
-    if (lane == 0) {
-      const int gap = S.gap[g];
-      S.unseen[g] = still, S.moved[g] = moved, S.deep[g] = (S.deep[g] & ~moved) | deep;
-      S.look[g] = far ? gap : (moved & low) ? 1 : kIdle;
-      if (far) S.gap[g] = min(2 * gap, kMostWait);
+    // (not finite: no key in this tile, NaN alone, or more than fp32 holds)
+    const bool finite = fabsf(top) < INFINITY;
+    const uint32_t none = __ballot_sync(0xffffffffu, mine && top == -INFINITY);
+    float *state = reinterpret_cast<float *>(&S.state[g][r >> 1]) + (r & 1) + 2;  // the reference, negative
+    if (first) {
+      const float ref = finite ? top - kBase : 0.f;
+      if (mine) *state = -ref, S.alpha[g][r] = -ref, S.floor[g][r] = ref - kDeep;
+      if (lane == 0) S.unseen[g] = none, S.moved[g] = 0u, S.deep[g] = 0u, S.look[g] = S.gap[g] = 1;
+    } else {
+      const uint32_t unseen = S.unseen[g];
+      low = S.below[g][0] & S.below[g][1] & S.below[g][2] & S.below[g][3];
+      const float ref = -*state, floor = S.floor[g][r];
+      const bool seen = !(unseen >> r & 1u);
+      float now = ref;
+      if ((top > kLimit || ((low | unseen) >> r & 1u)) && finite) now = ref + (top - kBase);
+      if (now < ref && seen) now = fminf(ref, fmaxf(now, floor));
+      const float by = now - ref;
+      __syncwarp();
+      if (mine) {
+        *state = -now;
+        S.alpha[g][r] = -by;
+        S.floor[g][r] = seen ? fmaxf(floor, now - kDeep) : now - kDeep;
+      }
+      const uint32_t moved = __ballot_sync(0xffffffffu, mine && by != 0.f) & ~unseen;
+      const uint32_t deep = __ballot_sync(0xffffffffu, mine && by < 0.f && now <= floor) & ~unseen;
+      const bool far = __any_sync(0xffffffffu, by > kFarRise && seen);
+      if (lane == 0) {
+        const int gap = S.gap[g];
+        S.unseen[g] = none & unseen, S.moved[g] = moved, S.deep[g] = (S.deep[g] & ~moved) | deep;
+        S.look[g] = far ? gap : (moved & low) ? 1 : kIdle;
+        if (far) S.gap[g] = min(2 * gap, kMostWait);
+      }
     }
   }
   named_bar_sync(1 + g, 128);
 #pragma unroll
   for (int i = 0; i < NR; i += 2) z[i / 2] = f2_add(z[i / 2], *reinterpret_cast<const u64 *>(&S.alpha[g][i]));
+  if (first) {
+    uint32_t zero[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) zero[i] = 0u;
+#pragma unroll 1
+    for (int c = 0; c < NR; c += 16) tc_st_32x32b_x16(l_addr + c, zero);
+  }
 #pragma unroll 1
   for (uint32_t left = S.moved[g]; left; left &= left - 1) {
     const int r = __ffs(left) - 1;
@@ -1146,31 +1125,23 @@ __device__ int softmax_tiles(const Params &P, Shared &S, Softmax &X, Item &I) {
       f2_unpack(z[i], z0, z1);
       top = fmax3(top, z0, z1);
     }
+    uint32_t low = 0;  // a bit a row: its exponents here lie below kLow
     if (t == look) {
-      uint32_t below = 0;  // a bit a row, the sign of its exponent against kLow
 #pragma unroll
       for (int i = NR - 2; i >= 0; i -= 2) {
         float z0, z1;
         f2_unpack(f2_add(z[i / 2], f2_pack(-kLow, -kLow)), z0, z1);
-        below = __funnelshift_l(__float_as_uint(z1), below, 1);
-        below = __funnelshift_l(__float_as_uint(z0), below, 1);
+        low = __funnelshift_l(__float_as_uint(z1), low, 1);
+        low = __funnelshift_l(__float_as_uint(z0), low, 1);
       }
-      below = __reduce_and_sync(0xffffffffu, below) & ~S.deep[g];
-      if (lane == 0) S.below[g][t & 1][X.warp] = below;
+      low = __reduce_and_sync(0xffffffffu, low) & ~S.deep[g];
     }
-    bool move = bar_or(1 + g, 128, t == 0 || S.unseen[g] || top > kLimit);
-    uint32_t low = 0;  // rows that fall
-    if (t == look) {
-      const uint4 b = *reinterpret_cast<const uint4 *>(S.below[g][t & 1]);
-      low = b.x & b.y & b.z & b.w;
-      move |= low != 0;
-    }
+    const bool move = bar_or(1 + g, 128, t == 0 || S.unseen[g] || low || top > kLimit);
     // P's buffer is free, and O at rest, once this warpgroup's product before is complete
     if (X.tiles > 0) X.ok = wait(&S.pv_done[g], full(X.tiles - 1, 1), &S.abort, 0) && X.ok;
     tc_fence_after();
     if (move) {
-      if (t == 0) first_references<NR>(S, X, z, l_addr);
-      else move_references<NR>(S, X, z, low, o_addr, l_addr);
+      move_references<NR>(S, X, z, low, t == 0, o_addr, l_addr);
       if (look >= 0) look = t + S.look[g];
     } else if (t == look) {
       look = t + kIdle;
