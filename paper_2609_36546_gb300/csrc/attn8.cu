@@ -24,7 +24,7 @@
 // reference includes V's scale, since it is the product that has to fit e4m3.
 // The terms end at 2^-15: 12 to 14 nats below one large weight that V answers with next to
 // nothing, all other keys of a long sequence would be lost.  So references fall too, to a
-// tile's maximum less 4, where all of a row's weights there lie below 2^-7.  This is looked
+// tile's maximum less 4, where all of a row's weights there lie below 2^-5.  This is looked
 // for in a part's second tile, in the tile after a fall or a rise by more than 2^8, and 32
 // tiles after the last move; with every far rise the wait behind the next one doubles, to 32
 // tiles, so that heads whose tiles differ that much do not swing all the time (64 spans of 1 to
@@ -103,7 +103,7 @@ constexpr float kBase = 4.f;      // a row's reference is its largest exponent l
 constexpr float kLimit = 8.f;     // weights stay below 2^8 (e4m3 ends at 448, and their second term too: 8 kLoScale)
 constexpr float kLoScale = 32.f;
 // When references fall: see the head of this file.
-constexpr float kLow = -7.f;      // a tile of lower exponents makes a row's reference fall
+constexpr float kLow = -5.f;      // a tile of lower exponents makes a row's reference fall
 constexpr float kDeep = 64.f;     // ... but no lower than this below its highest: sums and O stay far from fp32's ends
 constexpr float kFarRise = 8.f;   // after a rise by more the next tile is looked through
 constexpr int kIdle = 32, kMostWait = 32;  // tiles between two looks; at most, after far rises
