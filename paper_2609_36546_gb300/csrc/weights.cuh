@@ -12,7 +12,7 @@ IPD_DEVINL u64 f2_add_rz(u64 a, u64 b) {
 
 // w = floor(2^30 2^x + 1/2) of two x, -inf excluded (x >= -100 or so): 2^x = 2^i P(f),
 // i = x rounded, f = x - i in [-1/2, 1/2], P by Horner's rule, every product and
-// sum rounded to fp32 on its own; P is a least-squares fit of 2^f on Chebyshev
+// sum rounded to fp32 on its own; P is a least-squares fit of 2^f, relative to it, on Chebyshev
 // nodes with constant term 1 (relative error below 1.9e-7 with its rounding).
 // The factor 2^30 is in the coefficients (a power of two moves through the
 // roundings), and the sum with 1/2 is rounded towards 0: whole numbers are fp32
