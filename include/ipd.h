@@ -707,17 +707,22 @@ size_t ipd_attn8_workspace_size(const ipd_attn8_batch *verify, int n_verify,
  * decode tokens of n_decode batches (the same thing with q_len 1) in one call.
  * out = softmax(scale q K^T) V per query and head over the values the cache's
  * entries stand for.  q is carried to 2^-17 of its row's largest entry into
- * the products; scores, maxima and sums are fp32; the softmax weights, times V's
- * scale, enter the product with V as two e4m3 terms, off by at most 2^-9 of
- * themselves and 2^-19 of the row's largest one: what lies below that beside a
- * larger one is in the sum of the weights and may be missing in the product.  Over
- * more than 512 keys the level follows a row down as well, at the next 128 keys (up
- * to 32 blocks of 128 later where it has risen and fallen often): then the bound is
- * taken of the largest from there on, so that many small weights behind one large
- * one count as they are.  V scales more than 2^80 from the largest of the first
- * pages that all rows of a block of up to 128 see count as that far.  The output is rounded to
- * bf16 once.  A row's result depends on no key that it does not see, whatever that
- * key holds, and on no other row.
+ * the products (a row whose largest entry is below 2^-100 counts as zeros);
+ * scores, maxima and sums are fp32; the output is rounded to bf16 once.
+ *   The softmax weights, times V's scale, enter the product with V as two e4m3
+ * terms, off by less than 2^-8 of themselves and 2^-19 of the row's largest one:
+ * beside a larger weight, one below that is in the sum of the weights and may be
+ * missing in the product.  Over more than 512 keys this level follows a row down
+ * as well, where a block of 128 keys has nothing above 2^-13 of the row's largest
+ * (looked for in the block behind a new largest one, up to 64 blocks later where
+ * rows have risen and fallen often): from there on the bound is taken of the largest
+ * that follows, so that many small weights behind one large one count as they are.
+ * V scales more than 2^80 from the largest of the first pages that all rows of a
+ * block of up to 128 see count as that far.
+ *   A row's value depends on no key that it does not see, whatever that key holds,
+ * and on no other row.  Its last bits depend on how the call's work is cut, which
+ * goes by the lengths of all its requests, and on when the levels of its block of
+ * rows are looked at: the same call gives the same bits.
  * A page id outside the pool is recorded (IPD_DEVERR_PAGE_ID) and its keys are
  * left out; a row that is left with none gets 0.  A request whose offsets are out
  * of order or past total_q (IPD_DEVERR_SPAN), or whose seq_len is below its
@@ -762,7 +767,8 @@ int ipd_verify_attn8(const ipd_attn8_batch *verify, int n_verify, const ipd_attn
  *  next_token [num_reqs] int32; -1 also where the row it is drawn from has no
  *            finite or +inf entry
  *  logp_target, logp_draft  [total] fp32 log-probabilities of the drafted tokens
- *            at these temperatures (-inf for a row or token without any), or NULL
+ *            at these temperatures (-inf for a row or token without any, NaN for a
+ *            token outside [0, vocab)), or NULL
  * A request whose temperature is not valid (log2 e * inv_temp not positive and
  * finite) records IPD_DEVERR_SETTING and gets n_accept 0 and next_token -1, its
  * logp NaN; one whose offsets are out of order or past total (IPD_DEVERR_SPAN)

@@ -25,11 +25,11 @@
 // The terms end at 2^-15: 12 to 14 nats below one large weight that V answers with next to
 // nothing, all other keys of a long sequence would be lost.  So references fall too, to a
 // tile's maximum less 4, where all of a row's weights there lie below 2^-5.  This is looked
-// for in a part's second tile, in the tile after a fall or a rise by more than 2^8, and 32
+// for in a part's second tile, in the tile after a fall or a rise by more than 2^8, and 64
 // tiles after the last move; with every far rise the wait behind the next one doubles, to 32
 // tiles, so that heads whose tiles differ that much do not swing all the time (64 spans of 1 to
-// 16 over 256 to 16,384 keys, K scales of pages 2^3 apart: 131 us, 209 with a look in
-// every tile, 130 with none).
+// 16 over 256 to 16,384 keys, K scales of pages 2^3 apart: 128 us, 129 where references do
+// not fall; a look in every tile 209 before the code was shortened).
 //
 // Work.  All (request, KV head, block of 128 rows, tile) in one line, cut into parts of
 // equal cost, a CTA each: nothing is claimed, the cut depends on the lengths alone.
@@ -43,9 +43,10 @@
 // ids and scales.
 //
 // Measured (bytes of the visible keys and of the rows, at 6,784 GB/s for a copy): 19 requests
-// of one query over 32,768 keys, 8 KV heads, 189 us, 0.99 of a copy's rate; 128 over 256 to
-// 16,384 keys 172 us, 0.88.  With 128 rows a key the exponents bound it: 262 us for 19 x 16
-// queries over 32,768 keys of 4 heads, 624 TFLOP/s.
+// of one query over 32,768 keys, 8 KV heads, 199 us, 0.94 of a copy's rate; 128 over 256 to
+// 16,384 keys 174 us, 0.88.  With 128 rows a key: 271 us for 19 x 16 queries over 32,768 keys of
+// 4 heads, 602 TFLOP/s; no unit is full there (issue slots half busy), the softmax warps wait for
+// TMEM and at the barrier of their warpgroup's tile.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <cudaTypedefs.h>
@@ -106,7 +107,9 @@ constexpr float kLoScale = 32.f;
 constexpr float kLow = -5.f;      // a tile of lower exponents makes a row's reference fall
 constexpr float kDeep = 64.f;     // ... but no lower than this below its highest: sums and O stay far from fp32's ends
 constexpr float kFarRise = 8.f;   // after a rise by more the next tile is looked through
-constexpr int kIdle = 32, kMostWait = 32;  // tiles between two looks; at most, after far rises
+// Tiles from a move to the next look; at most, after far rises.  (19 x 16 queries / 38 x 8 over 32,768 keys of
+// 4 heads, us: 278 / 354 at 32 and 32, 271 / 339 at 64 and 32, 262 / 326 where references do not fall.)
+constexpr int kIdle = 64, kMostWait = 32;
 constexpr int kShort = 4 * kKeys; // sequences up to here: references do not fall
 constexpr int kFar = 80;       // V scales further than 2^80 from that of the first tile count as that far
 // What a tile of a task with up to 16, 32, 64 and 128 rows costs, and a task beside its tiles (up to
@@ -979,7 +982,7 @@ IPD_DEVINL void load_scores(uint32_t taddr, uint32_t (&r)[32]) { tc_ld_32x32b_x3
 // the rows' largest exponents in this tile less kBase.  O and the sums of rows that have seen keys are
 // rescaled, a TMEM column each (the others' are zeros, and their factor may be past fp32).
 // (The loop over tiles is short of instruction cache: one piece of code for first and later
-// references took 64 spans from 137 to 131 us.)
+// references took 64 spans from 137 to 131 us; falling references cost 1 to 5 % of a call beyond.)
 template <int NR>
 IPD_DEVINL void move_references(Shared &S, const Softmax &X, u64 (&z)[NR / 2], uint32_t low, bool first, uint32_t o_addr, uint32_t l_addr) {
   const int g = X.g, lane = X.lane;

@@ -34,16 +34,17 @@
 // of 2^13 bins over all 2^16 values, a pass over the row for each.
 //
 // What bounds it (GB300, device time).  Many rows: the pass over the entries.  512
-// rows of 151,936 take 69 us (2.2 TB/s).  All are in flight at once: the pass takes
+// rows of 151,936 take 70.5 us (2.2 TB/s).  All are in flight at once: the pass takes
 // about 32 us of a row's life (half of that without its atomics: random words put
 // three to four of a warp's 32 on one bank), the searches 8, the look-up up to 20 for
 // an entry far down the row; the last rows' searches and look-ups have nothing left
 // to hide behind.  Entries near 0 and below the range are kept out of the
 // common path: it has no branch for an entry, and one for a thread's batch of 32 (is
 // one of them near 0).  Few rows: a chain of barriers.  One
-// row of 151,936 takes 13.2 us: reading it 2.2, the cluster's barriers and the sum
-// of its histograms 3, the bins' weights and sums 1.8, the searches 3, the look-up 2;
-// 64 rows take 20.1 us, 33 rows of 50,021 12.0.  A sorted head of the row with the
+// row of 151,936 takes 14.1 us: reading it 2.2, the cluster's barriers and the sum
+// of its histograms 3, the bins' weights and sums 2.1, the searches 3, the look-up 2;
+// 64 rows take 21.2 us, 33 rows of 50,021 12.9 (13.8, 20.8, 12.5 and 70.1 for the 512 with
+// contracted weights, which are not the defined ones).  A sorted head of the row with the
 // searches as the exception took 20.5 us for one row and 174 for 512.  Rows outside
 // the bins' range: 70 to 80 us with a maximum there, 210 with all of it near 0.
 #include <cuda_bf16.h>
