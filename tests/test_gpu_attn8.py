@@ -422,12 +422,13 @@ def test_pools_past_32_bits(lib):
     _check(c)
 
 
-def _rows_ref(c, r, h, keep=None, scale=D ** -0.5, ends=False):
+def _rows_ref(c, r, h, keep=None, scale=D ** -0.5, ends=False, block=None):
     """(output, tolerance) of request r's rows over KV head h in 64 bits, over the keys in `keep`:
     the tolerance is the weights' and the output's rounding alone, relative to what an
     output averages: 2^-8 |o| + (2^-8 + 2^-10) a, a = sum_j w_j |v_j|.  With `ends` also what the
     weights' two terms end at: half of e4m3's least value over the second's factor, 2^-10 / 32, beside
-    a largest weight of 2^4 or more: 2^-19 of the row's largest weight times scale, per entry."""
+    a largest weight of 2^4 or more: 2^-19 of the row's largest weight times scale, per entry.  With
+    `block` that of the keys in this block of 128 alone, which may be missing whole: sum w_j |v_j|."""
     G, n, L = c.hq // c.hkv, c.q_len[r], c.length[r]
     row, page = sum(c.q_len[:r]), c.table[r, :(L + 15) // 16].long().clamp(0, c.n - 1)
     one = lambda p, s: (p.view(torch.uint8)[page, h].view(E4).double() *
@@ -442,14 +443,16 @@ def _rows_ref(c, r, h, keep=None, scale=D ** -0.5, ends=False):
         w = torch.softmax(c.q[row + i, h * G:(h + 1) * G].double() @ k[m].T * scale, -1)
         o, a = w @ v[m], w @ v[m].abs()
         c0 = 2.0 ** -19 * (w * fv[m]).amax(-1, keepdim=True) * (v[m] / fv[m][:, None]).abs().sum(0) if ends else 0.0
+        if block is not None:
+            c0 = c0 + w[:, 128 * block:128 * block + 128] @ v[m][128 * block:128 * block + 128].abs()
         out.append(o), tol.append(2.0 ** -8 * o.abs() + (2.0 ** -8 + 2.0 ** -10) * a + c0)
     return torch.stack(out), torch.stack(tol)
 
 
-def _check_rows(c, r, h, keep=None, scale=D ** -0.5, ends=False):
+def _check_rows(c, r, h, keep=None, scale=D ** -0.5, ends=False, block=None):
     row, G = sum(c.q_len[:r]), c.hq // c.hkv
     got = c.out[row:row + c.q_len[r], h * G:(h + 1) * G].double()
-    want, tol = _rows_ref(c, r, h, keep, scale, ends)
+    want, tol = _rows_ref(c, r, h, keep, scale, ends, block)
     assert bool(torch.isfinite(got).all())
     err = (got - want).abs() / tol
     assert float(err.max()) <= 1, (r, h, float(err.max()))
@@ -602,3 +605,27 @@ def test_scales_far_from_one_behind_absent_pages(lib, byte):
         keep = torch.ones(L, dtype=torch.bool, device="cuda")
         keep[:256] = False
         _check_rows(c, r, 3, keep)
+
+
+@pytest.mark.parametrize("hq,hkv,q_len,length", [(16, 8, [1], [33000]), (32, 4, [8, 3], [9000, 2000])])
+@pytest.mark.parametrize("nats", [35, 44, 70, 110])
+def test_one_key_out_of_reach(lib, hq, hkv, q_len, length, nats):
+    """A key so far above the others that references reach their floor, 64 binades below their highest
+    (44 nats), and past it: the others' part is right as far as it counts, and nothing overflows."""
+    c = Case(hq, hkv, q_len, length, seed=27, spread=0)
+    low = [torch.full((L,), -nats / 8 - 0.05, device="cuda") for L in length]
+    for s in low:
+        s[3], s[-200:] = nats / 8, nats / 16
+    _along(c, low, noise=0.0)
+    c.q.mul_(4.0)  # (scores four times as large: `nats` from the lowest to the highest)
+    c.vp = c.vp.float().abs().to(E4)
+    _run(lib, c)
+    for r in range(len(length)):
+        _check_rows(c, r, hkv - 1, ends=True)
+    for r in range(len(length)):  # without the keys between, and the highest one's values
+        c.kp.view(torch.uint8)[c.table[r, (length[r] - 200) // 16 - 1:(length[r] + 15) // 16].long()] = \
+            c.kp.view(torch.uint8)[c.table[r, 5:6].long()]
+        c.vp.view(torch.uint8)[c.table[r, 0].long(), :, 3] = 0
+    _run(lib, c)
+    for r in range(len(length)):
+        _check_rows(c, r, hkv - 1, ends=nats > 44, block=0)
